@@ -332,6 +332,121 @@ kvshot_status kvshot_draft_append_qknorm(const kvshot_attn_desc* desc, const voi
                                          float rope_base, const void* q_norm_w, const void* k_norm_w, float eps,
                                          void* draft_k, void* draft_v, void* q_out, kvshot_stream_t stream);
 
+/*
+ * The 4-bit target cache (not in the paper: a cache-compression variant, a quarter of the bf16 cache's bytes and a bit
+ * more than half of the fp8 one's) and its four entry points: kvshot_cache_extend finds the slots of newly verified
+ * tokens, kvshot_kv4_store quantises their K and V into them, kvshot_draft_attn_kv4 attends to the cache and
+ * kvshot_kv4_load reads values back.
+ *
+ * Values.  A token's K (or V) of one KV head is 8 blocks of 16 consecutive dims.  A block has a scale s, an e4m3 number
+ * (OCP FP8) in [2^-9, 448], and 16 codes, e2m1 numbers (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6 and their negatives); the value of a dim is code * s * 2^k_scale_exp (keys) or 2^v_scale_exp (values).  It has
+ * at most 6 significant bits, so it is exact in bf16, and without the power of two exact in f16.
+ * Quantising a block of x_i, exactly as written (roundings to nearest, ties to the even code):
+ *   y_i = x_i 2^-exp,   s = e4m3(min(max(max_i |y_i| / 6, 2^-9), 448)),   code_i = e2m1(y_i / s), saturating at 6.
+ * An infinity saturates; a NaN makes the block's scale NaN (0x7F), and with it all 16 values.
+ *
+ * Layout.  KVSHOT_KV4_GROUP_TOKENS = 16 consecutive tokens of one KV head are a group of KVSHOT_KV4_GROUP_BYTES = 2304
+ * bytes; a page of page_size tokens (a multiple of 16) holds page_size / 16 groups per KV head:
+ *   cache: [num_pages][hkv][page_size / 16][2304]
+ * Inside a group, with token t in [0, 16):
+ *   byte  c * 256 + t * 16 + i          K codes of dims 32 c + 2 i (low nibble) and 32 c + 2 i + 1, c in [0, 4), i in [0, 16)
+ *   byte  1024 + ...                    V codes, laid out alike
+ *   byte  2048 + t * 8 + b              K scale of block b (dims 16 b .. 16 b + 15)
+ *   byte  2176 + t * 8 + b              V scale of block b
+ * A slot is page * page_size + (place in the page).  A contiguous cache [num_caches][hkv][l_cap / 16][2304] is the same
+ * with one page of l_cap tokens (a multiple of 16) per cache.
+ */
+#define KVSHOT_KV4_GROUP_TOKENS 16
+#define KVSHOT_KV4_GROUP_BYTES 2304
+
+/*
+ * Room for newly verified tokens: block tables and slot maps from lengths, on the device.
+ * Cache c holds seq_lens[c] = L_c tokens in its first ceil(L_c / page_size) pages and gets n_c = new_tokens[c] >= 0
+ * more.  Pages that it lacks come off the end of the list of free pages, in cache order: with need_c new pages for cache
+ * c and base_c = sum over b < c of need_b, its new pages are free_pages[F - 1 - base_c], free_pages[F - 2 - base_c], ...
+ * (F = *free_count), in that order.  Written:
+ *   page_table_out  page_table with the new pages' entries (other entries are copied; in place only new ones are written)
+ *   seq_lens_out    L_c + n_c
+ *   free_count_out  F - sum need_c
+ *   token_start     [C + 1]: cache c's new tokens are token_start[c] .. token_start[c + 1] - 1 of the packed order
+ *   slots, token_cache, positions   [max_tokens]: slot, cache and position L_c + i of each packed token; -1 past the last
+ *                   (a fixed max_tokens keeps the sizes that a captured graph needs).  Any of the three may be NULL.
+ * The slots are those of kvshot_kv4_store, and (page, offset) of any paged cache of this library.
+ * seq_lens_out, page_table_out and free_count_out may be seq_lens, page_table and free_count; nothing else may overlap.
+ * All or nothing: if a length or count is negative or a row, the free list or max_tokens too small, or a free page's id
+ * outside [0, num_pages), KVSHOT_ERR_DEVICE_BOUNDS is recorded and nothing is taken: lengths, table and free list are
+ * copied as they are, token_start is all 0 and the maps all -1.
+ */
+typedef struct kvshot_extend_desc {
+  int32_t num_caches;        /* C in [1, 1024] */
+  int32_t page_size;         /* tokens per page, >= 1 */
+  int32_t max_pages_per_seq; /* row length of page_table */
+  int32_t num_pages;         /* pages in the pool */
+  int32_t num_free;          /* entries of free_pages (an upper bound of *free_count) */
+  int32_t max_tokens;        /* entries of slots, token_cache and positions */
+  int32_t* err_flag;         /* optional device int32, 0 before the call */
+} kvshot_extend_desc;
+
+kvshot_status kvshot_cache_extend(const kvshot_extend_desc* desc, const int32_t* seq_lens, const int32_t* new_tokens,
+                                  const int32_t* page_table, const int32_t* free_pages, const int32_t* free_count,
+                                  int32_t* seq_lens_out, int32_t* page_table_out, int32_t* free_count_out,
+                                  int32_t* token_start, int32_t* slots, int32_t* token_cache, int32_t* positions,
+                                  kvshot_stream_t stream);
+
+/*
+ * kvshot_kv4_store: K and V of num_tokens tokens quantised into the slots slots[t] of the cache.
+ * kvshot_kv4_load:  the values in those slots, as bf16 (exact; beyond bf16's range, infinite).
+ * k, v: [num_tokens][hkv][128] bf16, 16-byte aligned, token t at t * k_stride (v_stride) elements, multiples of 8 and
+ * at least hkv * 128 (0 selects hkv * 128): K and V may be slices of a fused projection's rows.
+ * slots: [num_tokens] int32.  A slot of -1 is passed over (load: zeros); one outside the cache is too, and recorded as
+ * KVSHOT_ERR_DEVICE_BOUNDS.  Slots of one store must differ, or either token may be what the slot then holds.
+ * cache: 16-byte aligned, kvshot_kv4_cache_bytes bytes; other slots keep their values.
+ * num_tokens == 0 is a no-op.
+ */
+typedef struct kvshot_kv4_desc {
+  int32_t num_tokens;  /* T >= 0 */
+  int32_t hkv;         /* KV heads */
+  int32_t head_dim;    /* must be 128 */
+  int32_t page_size;   /* tokens per page, a multiple of 16 (contiguous cache: l_cap) */
+  int32_t num_pages;   /* pages in the cache (contiguous cache: num_caches); num_pages * hkv * page_size < 2^31 */
+  int32_t k_scale_exp; /* |exp| <= 64 */
+  int32_t v_scale_exp;
+  int64_t k_stride;    /* elements between tokens of k, v; 0: hkv * 128 */
+  int64_t v_stride;
+  int32_t* err_flag;   /* optional device int32, 0 before the call */
+} kvshot_kv4_desc;
+
+/* Bytes of a 4-bit cache, 0 if the sizes are invalid. */
+size_t kvshot_kv4_cache_bytes(int32_t num_pages, int32_t hkv, int32_t page_size);
+
+kvshot_status kvshot_kv4_store(const kvshot_kv4_desc* desc, const void* k, const void* v, const int32_t* slots,
+                               void* cache, kvshot_stream_t stream);
+kvshot_status kvshot_kv4_load(const kvshot_kv4_desc* desc, const void* cache, const int32_t* slots, void* k, void* v,
+                              kvshot_stream_t stream);
+
+/*
+ * kvshot_draft_attn over a 4-bit target cache, with an optional sliding window.  Arguments, results and errors as
+ * there, except:
+ *  - cache: the 4-bit cache, paged (page_table != NULL, desc->page_size a multiple of 16) or contiguous (page_table
+ *    NULL, desc->l_cap a multiple of 16), 16-byte aligned; scales 2^desc->k_scale_exp and 2^desc->v_scale_exp.
+ *  - desc->flags: KVSHOT_TREE and KVSHOT_OVERLAP_PREVIOUS (which then covers seq_lens, page_table, cache and
+ *    tree_parent); others return KVSHOT_ERR_UNSUPPORTED.
+ *  - window = W > 0: a node at position p (a node of depth d, 1 for a child of the last verified token, stands at
+ *    L_c + d - 1; the target token j at j) sees a key that it would see otherwise only if the key's position is above
+ *    p - W, or below `sinks`.  A node always sees itself.  window = 0: no window (sinks is not used then).
+ *    Target tokens that no query row sees are not read.
+ *  - q, the softmax weights and the draft K/V are rounded to f16 for the tensor cores (finite magnitudes up to 65504;
+ *    those below 2^-14 lose bits), the cache's values are exact.  The running sums are fp32.
+ *  - A NaN stored in a token or draft slot that some query row sees may reach the other rows of its KV head's group.
+ * The workspace is kvshot_draft_attn_kv4_workspace_size bytes (0 if the descriptor is invalid).
+ */
+size_t kvshot_draft_attn_kv4_workspace_size(const kvshot_attn_desc* desc, int32_t window, int32_t sinks);
+kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* desc, const void* q, const void* cache,
+                                    const int32_t* page_table, const int32_t* seq_lens, const void* draft_k,
+                                    const void* draft_v, const int32_t* tree_parent, int32_t window, int32_t sinks,
+                                    void* out, float* lse, kvshot_stream_t stream);
+
 /* Static description of a status code (never NULL). */
 const char* kvshot_status_string(kvshot_status status);
 

@@ -204,6 +204,8 @@ struct Plan {
   size_t off_lse, off_o, bytes;
 };
 
+}  // namespace
+
 int sm_count() {
   static int cached[64] = {0};
   int dev = 0;
@@ -214,6 +216,8 @@ int sm_count() {
   if (dev >= 0 && dev < 64) cached[dev] = n;
   return n;
 }
+
+namespace {
 
 // CTAs per SM of a plan's kernel: a property of the device, the kernel and its shared memory (so of the number
 // of caches), asked of the runtime once per thread and then kept (one entry: a program's calls mostly agree).
@@ -238,6 +242,8 @@ cudaError_t ctas_per_sm(Kernel kernel, int m_tiles, int rows_per_unit, int C, in
   *per_sm = k.per_sm;
   return cudaSuccess;
 }
+
+}  // namespace
 
 // Checks that do not depend on the cache layout.
 kvshot_status check_common(const kvshot_attn_desc* d) {
@@ -270,6 +276,8 @@ kvshot_status check_common(const kvshot_attn_desc* d) {
   if (static_cast<int64_t>(d->num_caches) * d->hkv * d->n_max >= INT_MAX) return KVSHOT_ERR_UNSUPPORTED;
   return KVSHOT_OK;
 }
+
+namespace {
 
 kvshot_status check_attn_desc(const kvshot_attn_desc* d, bool paged) {
   if (kvshot_status st = check_common(d)) return st;

@@ -124,6 +124,10 @@ void rope_frequencies(float rope_base, double* inv_freq);
 // turns[j] = rope_base^(-2j/128) / 2 pi modulo 1 in units of 2^-64, from the fp64 frequencies (kept like them).
 void rope_turns(float rope_base, uint64_t* turns);
 
+// Descriptor checks that do not depend on the cache layout, and the current device's number of SMs (0: an error).
+kvshot_status check_common(const kvshot_attn_desc* d);
+int sm_count();
+
 // Kernel launchers (one per translation unit).  Return cudaSuccess or the launch error.  `pdl`:
 // launch with programmatic stream serialization (KVSHOT_OVERLAP_PREVIOUS).
 cudaError_t launch_attn_cc(const AttnParams& p, const TensorMaps& maps, bool pdl, cudaStream_t stream);

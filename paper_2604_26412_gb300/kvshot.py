@@ -36,8 +36,12 @@ KVSHOT_TARGET_FP8 = 0x20
 
 EXPORTS = ("kvshot_draft_attn", "kvshot_draft_attn_workspace_size", "kvshot_draft_append", "kvshot_status_string",
            "kvshot_version", "kvshot_draft_attn_static", "kvshot_gated_delta", "kvshot_gated_delta_workspace_size",
-           "kvshot_kv_project", "kvshot_kv_project_workspace_size", "kvshot_draft_append_qknorm")
+           "kvshot_kv_project", "kvshot_kv_project_workspace_size", "kvshot_draft_append_qknorm", "kvshot_cache_extend",
+           "kvshot_kv4_cache_bytes", "kvshot_kv4_store", "kvshot_kv4_load", "kvshot_draft_attn_kv4_workspace_size",
+           "kvshot_draft_attn_kv4")
 KVSHOT_PROJECT_ROPE = 0x1
+KV4_GROUP_TOKENS = 16    # KVSHOT_KV4_GROUP_TOKENS
+KV4_GROUP_BYTES = 2304   # KVSHOT_KV4_GROUP_BYTES
 STATIC_WORKSPACE_BYTES = 64 * 1024 * 1024  # KVSHOT_STATIC_WORKSPACE_BYTES
 
 
@@ -109,6 +113,37 @@ class ProjectDesc(ctypes.Structure):
     ]
 
 
+class ExtendDesc(ctypes.Structure):
+    """Mirror of kvshot_extend_desc."""
+
+    _fields_ = [
+        ("num_caches", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("max_pages_per_seq", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("num_free", ctypes.c_int32),
+        ("max_tokens", ctypes.c_int32),
+        ("err_flag", ctypes.c_void_p),
+    ]
+
+
+class Kv4Desc(ctypes.Structure):
+    """Mirror of kvshot_kv4_desc."""
+
+    _fields_ = [
+        ("num_tokens", ctypes.c_int32),
+        ("hkv", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("k_scale_exp", ctypes.c_int32),
+        ("v_scale_exp", ctypes.c_int32),
+        ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64),
+        ("err_flag", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -148,6 +183,19 @@ def load(build_if_missing: bool = True):
     lib.kvshot_kv_project.restype = ctypes.c_int
     lib.kvshot_kv_project_workspace_size.argtypes = [ctypes.POINTER(ProjectDesc)]
     lib.kvshot_kv_project_workspace_size.restype = ctypes.c_size_t
+    lib.kvshot_cache_extend.argtypes = [ctypes.POINTER(ExtendDesc)] + [P] * 13
+    lib.kvshot_cache_extend.restype = ctypes.c_int
+    lib.kvshot_kv4_cache_bytes.argtypes = [ctypes.c_int32] * 3
+    lib.kvshot_kv4_cache_bytes.restype = ctypes.c_size_t
+    lib.kvshot_kv4_store.argtypes = [ctypes.POINTER(Kv4Desc), P, P, P, P, P]
+    lib.kvshot_kv4_store.restype = ctypes.c_int
+    lib.kvshot_kv4_load.argtypes = [ctypes.POINTER(Kv4Desc), P, P, P, P, P]
+    lib.kvshot_kv4_load.restype = ctypes.c_int
+    lib.kvshot_draft_attn_kv4_workspace_size.argtypes = [ctypes.POINTER(AttnDesc), ctypes.c_int32, ctypes.c_int32]
+    lib.kvshot_draft_attn_kv4_workspace_size.restype = ctypes.c_size_t
+    lib.kvshot_draft_attn_kv4.argtypes = [ctypes.POINTER(AttnDesc), P, P, P, P, P, P, P, ctypes.c_int32, ctypes.c_int32,
+                                          P, P, P]
+    lib.kvshot_draft_attn_kv4.restype = ctypes.c_int
     lib.kvshot_status_string.argtypes = [ctypes.c_int]
     lib.kvshot_status_string.restype = ctypes.c_char_p
     lib.kvshot_version.argtypes = []
@@ -312,3 +360,80 @@ def draft_append_qknorm(desc: AttnDesc, q_in, k_in, v_in, positions, n0: int, n_
                                     draft_k, draft_v, q_out, stream)
     if st != KVSHOT_OK:
         raise KvshotError(st, "kvshot_draft_append_qknorm")
+
+
+def make_extend_desc(*, num_caches, page_size, max_pages_per_seq, num_pages, max_tokens, num_free=None,
+                     err_flag=None) -> ExtendDesc:
+    """num_free: entries of the list of free pages (default: num_pages, the most there can be)."""
+    return ExtendDesc(int(num_caches), int(page_size), int(max_pages_per_seq), int(num_pages),
+                      int(num_pages if num_free is None else num_free), int(max_tokens), _ptr(err_flag))
+
+
+def cache_extend_status(desc: ExtendDesc, seq_lens, new_tokens, page_table, free_pages, free_count, seq_lens_out,
+                        page_table_out, free_count_out, token_start, slots, token_cache, positions, stream=None) -> int:
+    """Call kvshot_cache_extend (pages and slots of newly verified tokens); return its status."""
+    return (_lib or load()).kvshot_cache_extend(_dref(desc), _ptr(seq_lens), _ptr(new_tokens), _ptr(page_table),
+                                          _ptr(free_pages), _ptr(free_count), _ptr(seq_lens_out),
+                                          _ptr(page_table_out), _ptr(free_count_out), _ptr(token_start), _ptr(slots),
+                                          _ptr(token_cache), _ptr(positions), _stream(stream))
+
+
+def cache_extend(desc: ExtendDesc, seq_lens, new_tokens, page_table, free_pages, free_count, seq_lens_out,
+                 page_table_out, free_count_out, token_start, slots, token_cache, positions, stream=None) -> None:
+    st = cache_extend_status(desc, seq_lens, new_tokens, page_table, free_pages, free_count, seq_lens_out,
+                             page_table_out, free_count_out, token_start, slots, token_cache, positions, stream)
+    if st != KVSHOT_OK:
+        raise KvshotError(st, "kvshot_cache_extend")
+
+
+def kv4_cache_bytes(num_pages: int, hkv: int, page_size: int) -> int:
+    """Bytes of a 4-bit cache (0 if the sizes are invalid)."""
+    return int((_lib or load()).kvshot_kv4_cache_bytes(int(num_pages), int(hkv), int(page_size)))
+
+
+def make_kv4_desc(*, num_tokens, hkv, page_size, num_pages, head_dim=128, k_stride=0, v_stride=0, k_scale_exp=0,
+                  v_scale_exp=0, err_flag=None) -> Kv4Desc:
+    return Kv4Desc(int(num_tokens), int(hkv), int(head_dim), int(page_size), int(num_pages), int(k_scale_exp),
+                   int(v_scale_exp), int(k_stride), int(v_stride), _ptr(err_flag))
+
+
+def kv4_store_status(desc: Kv4Desc, k, v, slots, cache, stream=None) -> int:
+    """Call kvshot_kv4_store (K and V quantised into the slots of a 4-bit cache); return its status."""
+    return (_lib or load()).kvshot_kv4_store(_dref(desc), _ptr(k), _ptr(v), _ptr(slots), _ptr(cache), _stream(stream))
+
+
+def kv4_store(desc: Kv4Desc, k, v, slots, cache, stream=None) -> None:
+    st = kv4_store_status(desc, k, v, slots, cache, stream)
+    if st != KVSHOT_OK:
+        raise KvshotError(st, "kvshot_kv4_store")
+
+
+def kv4_load_status(desc: Kv4Desc, cache, slots, k, v, stream=None) -> int:
+    """Call kvshot_kv4_load (the values in the slots of a 4-bit cache, as bf16); return its status."""
+    return (_lib or load()).kvshot_kv4_load(_dref(desc), _ptr(cache), _ptr(slots), _ptr(k), _ptr(v), _stream(stream))
+
+
+def kv4_load(desc: Kv4Desc, cache, slots, k, v, stream=None) -> None:
+    st = kv4_load_status(desc, cache, slots, k, v, stream)
+    if st != KVSHOT_OK:
+        raise KvshotError(st, "kvshot_kv4_load")
+
+
+def draft_attn_kv4_workspace_size(desc: AttnDesc, window: int = 0, sinks: int = 0) -> int:
+    return int((_lib or load()).kvshot_draft_attn_kv4_workspace_size(_dref(desc), int(window), int(sinks)))
+
+
+def draft_attn_kv4_status(desc: AttnDesc, q, cache, page_table, seq_lens, draft_k, draft_v, tree_parent, window: int,
+                          sinks: int, out, lse, stream=None) -> int:
+    """Call kvshot_draft_attn_kv4 (draft attention over a 4-bit target cache) and return its status."""
+    return (_lib or load()).kvshot_draft_attn_kv4(_dref(desc), _ptr(q), _ptr(cache), _ptr(page_table), _ptr(seq_lens),
+                                            _ptr(draft_k), _ptr(draft_v), _ptr(tree_parent), int(window), int(sinks),
+                                            _ptr(out), _ptr(lse), _stream(stream))
+
+
+def draft_attn_kv4(desc: AttnDesc, q, cache, page_table, seq_lens, draft_k, draft_v, tree_parent, window: int,
+                   sinks: int, out, lse, stream=None) -> None:
+    st = draft_attn_kv4_status(desc, q, cache, page_table, seq_lens, draft_k, draft_v, tree_parent, window, sinks, out,
+                               lse, stream)
+    if st != KVSHOT_OK:
+        raise KvshotError(st, "kvshot_draft_attn_kv4")
