@@ -80,8 +80,8 @@ struct Smem {
   uint64_t* mmadone;               // [2]
   uint64_t* anc;                   // [64] each node's ancestors and itself (tree)
   uint64_t* row_anc;               // [64] those of each query row's node
-  float *ref, *alpha, *inv;        // [64] per row
-  int* depth;                      // [64] per row
+  float *ref, *alpha, *inv, *sum;  // [64] per row
+  int *depth, *place;              // [64] per row
   int* wmax;                       // [4][64] per warp and row; sums at a piece's end
   int* par;                        // [64]
   uint32_t* tmem;
@@ -94,7 +94,7 @@ constexpr int kBarriers = 20;  // besides the ring's: 19, and one for the alignm
 template <class CF>
 __host__ __device__ constexpr size_t smem_bytes(int C) {
   return 1024 + 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize +
-         sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + sizeof(uint64_t) * 128 + sizeof(int) * (64 * 9) +
+         sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + sizeof(uint64_t) * 128 + sizeof(int) * (64 * 11) +
          sizeof(int) * (4 + 2 * C + 1);
 }
 
@@ -124,8 +124,10 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.ref = reinterpret_cast<float*>(s.row_anc + 64);
   s.alpha = s.ref + 64;
   s.inv = s.alpha + 64;
-  s.depth = reinterpret_cast<int*>(s.inv + 64);
-  s.wmax = s.depth + 64;
+  s.sum = s.inv + 64;
+  s.depth = reinterpret_cast<int*>(s.sum + 64);
+  s.place = s.depth + 64;
+  s.wmax = s.place + 64;
   s.par = s.wmax + 4 * 64;
   s.tmem = reinterpret_cast<uint32_t*>(s.par + 64);
   s.misc = reinterpret_cast<int*>(s.tmem + 1);
@@ -165,66 +167,74 @@ __device__ __forceinline__ void build_kv4_plan(const AttnParams& p, int* s_len, 
   __syncthreads();
 }
 
-struct Walk {
-  int t, t_begin, t_end;  // tile of this CTA's range
-  int c, hr, lt;          // cache, KV head x row block, tile of the unit
-  int L, ut;              // prefix length, tiles of a unit
+// A run of tiles of one unit that this CTA takes.
+struct Piece {
+  int t, t_end;        // tile of this CTA's range: the piece's first one (its end after next_piece), and the range's end
+  int c, hr;           // cache, KV head x row block
+  int lt0, lt1, ut;    // the piece's tiles of the unit [lt0, lt1), tiles of the unit
+  int h, rb, seq, L;   // KV head, row block, sequence, prefix length
   WindowSpan span;
 
-  __device__ __forceinline__ void load_cache(const AttnParams& p, const int* s_len) {
-    L = s_len[c];
-    span = window_span<kTile>(p, L);
-    ut = span.tiles + p.draft_tiles;
+  // First key of tile lt (token, or draft slot), and its valid keys.
+  __device__ __forceinline__ bool draft(int lt) const { return lt >= span.tiles; }
+  __device__ __forceinline__ int key0(int lt) const {
+    return draft(lt) ? (lt - span.tiles) * kDraftTile : (lt < span.sink_tiles ? lt : lt + span.skip) * kTile;
   }
-  __device__ __forceinline__ void begin(const AttnParams& p, const int* s_len, const int* s_base) {
-    c = hr = lt = 0;
-    t = t_begin = t_end = 0;
-    if (p.unit_ctas > 0) {
-      load_cache(p, s_len);
-      const UnitCut u = unit_cut(p.unit_ctas, ut);
-      hr = blockIdx.x / u.per;
-      lt = (blockIdx.x - hr * u.per) * u.tpc;
-      t_end = hr < p.hkv * p.row_blocks ? min(u.tpc, ut - lt) : 0;
-      return;
-    }
-    const int total = s_base[p.C], tpc = tiles_per_cta(total, p.num_ctas);
-    t = t_begin = min(total, static_cast<int>(blockIdx.x) * tpc);
-    t_end = min(total, t + tpc);
-    if (t >= t_end) return;
-    int lo = 0, hi = p.C - 1;  // last cache whose first tile is <= t
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_base[mid] <= t) lo = mid;
-      else hi = mid - 1;
-    }
-    c = lo;
-    load_cache(p, s_len);
-    const int rem = t - s_base[lo];
-    hr = rem / ut;
-    lt = rem - hr * ut;
+  __device__ __forceinline__ int nkeys(int lt, int n_nodes) const {
+    return draft(lt) ? min(kDraftTile, n_nodes - key0(lt)) : min(kTile, L - key0(lt));
   }
-  __device__ __forceinline__ void next(const AttnParams& p, const int* s_len) {
-    ++t;
-    if (++lt == ut) {
-      lt = 0;
-      if (++hr == p.hkv * p.row_blocks) {
-        hr = 0;
-        ++c;
-        if (t < t_end) load_cache(p, s_len);
-      }
-    }
-  }
-  __device__ __forceinline__ bool draft() const { return lt >= span.tiles; }
-  __device__ __forceinline__ bool first() const { return t == t_begin || lt == 0; }
-  __device__ __forceinline__ bool last() const { return t == t_end - 1 || lt == ut - 1; }
-  // First key of the tile (token, or draft slot), and its valid keys.
-  __device__ __forceinline__ int key0() const {
-    return draft() ? (lt - span.tiles) * kDraftTile : (lt < span.sink_tiles ? lt : lt + span.skip) * kTile;
-  }
-  __device__ __forceinline__ int nkeys(const AttnParams& p) const {
-    return draft() ? min(kDraftTile, p.N - key0()) : min(kTile, L - key0());
-  }
+  __device__ __forceinline__ bool whole() const { return lt0 == 0 && lt1 == ut; }
 };
+
+// The CTA's range; next_piece finds its first piece.
+__device__ __noinline__ void begin_pieces(const AttnParams& p, const int* s_len, const int* s_base, Piece& w) {
+  w.c = w.hr = w.lt1 = w.ut = w.t = w.t_end = 0;
+  if (p.unit_ctas > 0) {
+    w.ut = window_span<kTile>(p, s_len[0]).tiles + p.draft_tiles;
+    const UnitCut u = unit_cut(p.unit_ctas, w.ut);
+    w.hr = blockIdx.x / u.per;
+    w.lt1 = (blockIdx.x - w.hr * u.per) * u.tpc;
+    w.t_end = w.hr < p.hkv * p.row_blocks ? min(u.tpc, w.ut - w.lt1) : 0;
+    return;
+  }
+  const int total = s_base[p.C], tpc = tiles_per_cta(total, p.num_ctas);
+  w.t = min(total, static_cast<int>(blockIdx.x) * tpc);
+  w.t_end = min(total, w.t + tpc);
+  if (w.t >= w.t_end) return;
+  int lo = 0, hi = p.C - 1;  // last cache whose first tile is <= t
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (s_base[mid] <= w.t) lo = mid;
+    else hi = mid - 1;
+  }
+  w.c = lo;
+  w.ut = window_span<kTile>(p, s_len[lo]).tiles + p.draft_tiles;
+  const int rem = w.t - s_base[lo];
+  w.hr = rem / w.ut;
+  w.lt1 = rem - w.hr * w.ut;
+}
+
+// Moves on to the next piece of the range; false at its end.  (Out of line: the roles' loops over the tiles are short.)
+__device__ __noinline__ bool next_piece(const AttnParams& p, const int* s_len, Piece& w) {
+  if (w.t >= w.t_end) return false;
+  if (w.lt1 == w.ut) {
+    w.lt1 = 0;
+    if (++w.hr == p.hkv * p.row_blocks) {
+      w.hr = 0;
+      ++w.c;
+    }
+  }
+  w.L = s_len[w.c];
+  w.span = window_span<kTile>(p, w.L);
+  w.ut = w.span.tiles + p.draft_tiles;
+  w.lt0 = w.lt1;
+  w.lt1 = min(w.ut, w.lt0 + w.t_end - w.t);
+  w.t += w.lt1 - w.lt0;
+  w.h = w.hr / p.row_blocks;
+  w.rb = w.hr - w.h * p.row_blocks;
+  w.seq = w.c / (p.C / p.B);
+  return true;
+}
 
 // ------------------------------------------------------------ loads
 
@@ -235,65 +245,67 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 }
 
 template <class CF>
-__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Smem& sm, Walk w) {
+__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Smem& sm, Piece w) {
   const AttnParams& p = kp.a;
   volatile int* abort = &sm.misc[0];
   const int lane = threadIdx.x & 31;
   int stage = 0, issued = 0;
   uint32_t phase = 0;
-  bool waited = false;
-  const int runs = kTileGroups / kp.run_groups;
-  // Page of this lane's run of groups in the tile at `w` (checked when it is used).
-  auto page_of = [&](const Walk& x) {
-    if (x.t >= x.t_end || x.draft() || lane >= runs) return 0;
-    const int g = x.key0() / kKv4Tokens + lane * kp.run_groups;
-    if (g * kKv4Tokens >= x.L) return 0;
-    return p.paged ? p.page_table[static_cast<size_t>(x.c) * p.max_pages + g / kp.groups_per_page] : x.c;
-  };
-  int next_page = page_of(w);
-  while (w.t < w.t_end) {
-    const bool draft = w.draft();
-    const int h = w.hr / p.row_blocks, key0 = w.key0(), nkeys = w.nkeys(p), c = w.c;
-    int pid = next_page;
-    w.next(p, sm.len);
-    next_page = page_of(w);
-    if (draft && !waited) {  // the draft K/V may come from the preceding kernel
-      wait_for_prerequisite_grid();
-      waited = true;
-    }
-    int ok = 1;
-    if (lane == 0) ok = mbar_wait(smem_addr(&sm.cempty[stage]), phase ^ 1u, p.err, p.wait_ns) && !*abort;
-    ok = __shfl_sync(0xffffffffu, ok, 0);
-    if (!ok) {
-      if (lane == 0) *abort = 1;
-      break;
-    }
-    const uint32_t bar = smem_addr(&sm.cfull[stage]), dst = sm.ring + stage * kStageSize;
-    if (draft) {
-      if (lane == 0) mbar_arrive_expect_tx(bar, static_cast<uint32_t>(nkeys) * 4 * kHeadDim);
-      __syncwarp();
-      if (lane < nkeys) {
-        const size_t row = (static_cast<size_t>(c) * p.hkv + h) * p.n_max + key0 + lane;
-        bulk_load(dst + lane * kDraftRow, kp.draft_k + row * kHeadDim, 2 * kHeadDim, bar);
-        bulk_load(dst + kDraftV + lane * kDraftRow, kp.draft_v + row * kHeadDim, 2 * kHeadDim, bar);
+  bool waited = false, ok = true;
+  // Page ids come 32 to a load, a window of tiles ahead: lane i holds the page of run i % runs of the window's tile
+  // i / runs, and issues that copy.
+  const int runs = kTileGroups / kp.run_groups, ahead = 32 / runs;
+  const int my_tile = lane / runs, my_g0 = (lane % runs) * kp.run_groups;
+  while (ok && next_piece(p, sm.len, w)) {
+    const int32_t* table = p.page_table + (p.paged ? static_cast<size_t>(w.c) * p.max_pages : 0);
+    auto page_of = [&](int lt) {
+      lt += my_tile;
+      if (lt >= w.lt1 || w.draft(lt)) return 0;
+      const int g = w.key0(lt) / kKv4Tokens + my_g0;
+      if (g * kKv4Tokens >= w.L) return 0;
+      return p.paged ? table[g / kp.groups_per_page] : w.c;
+    };
+    int pid = 0, next_pid = page_of(w.lt0), window = w.lt0;
+    for (int lt = w.lt0; lt < w.lt1; ++lt) {
+      if (lt == window) {
+        pid = next_pid;
+        window += ahead;
+        next_pid = page_of(window);
       }
-    } else {
+      const bool draft = w.draft(lt);
+      const int key0 = w.key0(lt), nkeys = w.nkeys(lt, p.N);
+      if (draft && !waited) {  // the draft K/V may come from the preceding kernel
+        wait_for_prerequisite_grid();
+        waited = true;
+      }
+      if (lane == 0) ok = mbar_wait(smem_addr(&sm.cempty[stage]), phase ^ 1u, p.err, p.wait_ns) && !*abort;
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (!ok) {
+        if (lane == 0) *abort = 1;
+        break;
+      }
+      const uint32_t bar = smem_addr(&sm.cfull[stage]), dst = sm.ring + stage * kStageSize;
       const int groups = (nkeys + kKv4Tokens - 1) / kKv4Tokens;
-      if (lane == 0) mbar_arrive_expect_tx(bar, static_cast<uint32_t>(groups) * kKv4Bytes);
+      if (lane == 0) mbar_arrive_expect_tx(bar, draft ? nkeys * 4 * kHeadDim : groups * kKv4Bytes);
       __syncwarp();
-      const int g0 = lane * kp.run_groups, n = min(kp.run_groups, groups - g0);
-      if (lane < runs && n > 0) {
+      if (draft) {
+        if (lane < nkeys) {
+          const size_t row = (static_cast<size_t>(w.c) * p.hkv + w.h) * p.n_max + key0 + lane;
+          bulk_load(dst + lane * kDraftRow, kp.draft_k + row * kHeadDim, 2 * kHeadDim, bar);
+          bulk_load(dst + kDraftV + lane * kDraftRow, kp.draft_v + row * kHeadDim, 2 * kHeadDim, bar);
+        }
+      } else if (my_tile == lt - (window - ahead) && my_g0 < groups) {
         if (p.paged) pid = valid_page_id(p, pid);
-        const int g = key0 / kKv4Tokens + g0, in_page = p.paged ? g % kp.groups_per_page : g;
+        const int g = key0 / kKv4Tokens + my_g0, in_page = p.paged ? g % kp.groups_per_page : g;
         const uint8_t* src =
-            kp.cache + ((static_cast<size_t>(pid) * p.hkv + h) * kp.groups_per_page + in_page) * kKv4Bytes;
-        bulk_load(dst + g0 * kKv4Bytes, src, static_cast<uint32_t>(n) * kKv4Bytes, bar);
+            kp.cache + ((static_cast<size_t>(pid) * p.hkv + w.h) * kp.groups_per_page + in_page) * kKv4Bytes;
+        bulk_load(dst + my_g0 * kKv4Bytes, src, min(kp.run_groups, groups - my_g0) * kKv4Bytes, bar);
       }
-    }
-    ++issued;
-    if (++stage == CF::kStages) {
-      stage = 0;
-      phase ^= 1u;
+      ++issued;
+      if (++stage == CF::kStages) {
+        stage = 0;
+        phase ^= 1u;
+      }
     }
   }
   if (lane == 0) sm.misc[1] = issued;
@@ -319,31 +331,28 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
 
 // q of every piece as f16, rows of 64 dims in two halves (K-major B of QK^T, 128-byte swizzle).
 template <class CF>
-__device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& sm, Walk w) {
+__device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& sm, Piece w) {
   const AttnParams& p = kp.a;
   volatile int* abort = &sm.misc[0];
   const int lane = threadIdx.x & 31;
   wait_for_prerequisite_grid();
-  int piece = 0;
-  for (; w.t < w.t_end; w.next(p, sm.len)) {
-    if (!w.first()) continue;
+  for (int piece = 0; next_piece(p, sm.len, w); ++piece) {
     const int b = piece & 1;
-    const bool ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sm.qempty[b]), ((piece >> 1) & 1) ^ 1u, p.err, p.wait_ns)) &&
-                    !__any_sync(0xffffffffu, *abort);
+    bool ok = !*abort && mbar_wait(smem_addr(&sm.qempty[b]), ((piece >> 1) & 1) ^ 1u, p.err, p.wait_ns);
+    ok = __all_sync(0xffffffffu, ok);
     if (!ok) {
       *abort = 1;
       return;
     }
-    const int h = w.hr / p.row_blocks, rb = w.hr - h * p.row_blocks;
+    const __nv_bfloat16* q = p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim;
+    const int row0 = w.rb * p.rows_per_unit, rows = min(p.rows_per_unit, p.rows_total - row0);
+    const int ch = lane & 15;
 #pragma unroll 4
-    for (int i = lane; i < CF::kNT * 16; i += 32) {
-      const int r = i >> 4, ch = i & 15, rr = rb * p.rows_per_unit + r;
+    for (int r = lane >> 4; r < CF::kNT; r += 2) {
       uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (r < p.rows_per_unit && rr < p.rows_total) {
-        const int nl = rr / p.G, gh = rr - nl * p.G;
-        x = *(reinterpret_cast<const uint4*>(
-                  p.q + ((static_cast<size_t>(w.c) * p.Nq + nl) * p.hq + h * p.G + gh) * kHeadDim) +
-              ch);
+      if (r < rows) {
+        const int nl = (row0 + r) / p.G, gh = row0 + r - nl * p.G;
+        x = reinterpret_cast<const uint4*>(q + (static_cast<size_t>(nl) * p.hq + gh) * kHeadDim)[ch];
       }
       sts128(sm.q + b * CF::kQTile + (ch >> 3) * (CF::kNT * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4),
              make_uint4(bf16x2_to_f16x2(x.x), bf16x2_to_f16x2(x.y), bf16x2_to_f16x2(x.z), bf16x2_to_f16x2(x.w)));
@@ -351,7 +360,6 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& sm, Walk 
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_addr(&sm.qfull[b]));
-    ++piece;
   }
 }
 
@@ -369,135 +377,109 @@ __device__ __forceinline__ void decode16(uint32_t lo, uint32_t hi, uint32_t scal
   }
 }
 
-// The scales of blocks 2 c and 2 c + 1, each in both halves.
-__device__ __forceinline__ uint2 scale_pair(const uint2& sc, int c) {
-  const uint32_t two = e4m3x2_to_f16x2(((c & 2) ? sc.y : sc.x) >> (16 * (c & 1)));
+// Two blocks' scales (the low two bytes), each in both halves.
+__device__ __forceinline__ uint2 scale_pair(uint32_t bytes) {
+  const uint32_t two = e4m3x2_to_f16x2(bytes);
   return make_uint2(__byte_perm(two, two, 0x1010), __byte_perm(two, two, 0x3232));
+}
+
+// 32 dims of one key (16 words) into its row of the V tile: 16-byte chunks 4 c .. 4 c + 3, 128-byte swizzle.
+__device__ __forceinline__ void put_v(uint32_t row, uint32_t sw, int c, const uint32_t* o) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    sts128(row + (c >> 1) * kVHalf + ((((c & 1) * 4 + i) << 4) ^ sw), make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+}
+
+// A draft tile's key (bf16 row at `src`, zeros past the valid keys) into tensor memory (K) or the V tile.
+template <bool kV>
+__device__ __noinline__ void decode_draft(uint32_t src, bool live, uint32_t dst, uint32_t sw) {
+#pragma unroll 1
+  for (int c = 0; c < 4; ++c) {
+    uint32_t o[16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (live) x = lds128(src + (4 * c + i) * 16);
+      o[4 * i] = bf16x2_to_f16x2(x.x);
+      o[4 * i + 1] = bf16x2_to_f16x2(x.y);
+      o[4 * i + 2] = bf16x2_to_f16x2(x.z);
+      o[4 * i + 3] = bf16x2_to_f16x2(x.w);
+    }
+    if constexpr (kV) put_v(dst, sw, c, o);
+    else tmem_st16(dst + 16 * c, o);
+  }
 }
 
 // Warps 4..7 (K, into tensor memory) and 8..11 (V, into shared memory): a thread decodes one key.
 template <class CF, bool kV>
-__device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Walk w) {
+__device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Piece w) {
   const AttnParams& p = kp.a;
   volatile int* abort = &sm.misc[0];
   const int lane = threadIdx.x & 31, key = threadIdx.x & 127;
-  const uint32_t src = sm.ring + (key >> 4) * kKv4Bytes + (key & 15) * kChunkBytes + (kV ? kVCodes : 0);
-  const uint32_t ssrc = sm.ring + (key >> 4) * kKv4Bytes + kScales + (kV ? kScaleBytes : 0) + (key & 15) * 8;
+  const uint32_t group = (key >> 4) * kKv4Bytes;
+  const uint32_t src = sm.ring + group + (key & 15) * kChunkBytes + (kV ? kVCodes : 0);
+  const uint32_t ssrc = sm.ring + group + kScales + (kV ? kScaleBytes : 0) + (key & 15) * 8;
   const uint32_t dsrc = sm.ring + key * kDraftRow + (kV ? kDraftV : 0);
-  const uint32_t trow = tmem + (static_cast<uint32_t>(key & 96) << 16) + CF::kTmemK;
-  int stage = 0;
+  const uint32_t dst = kV ? sm.v + key * 128 : tmem + (static_cast<uint32_t>(key & 96) << 16) + CF::kTmemK;
+  const uint32_t sw = static_cast<uint32_t>(key & 7) << 4;
+  int stage = 0, t = 0;
   uint32_t phase = 0;
-  for (int t = 0; w.t < w.t_end; ++t, w.next(p, sm.len)) {
-    const int nkeys = w.nkeys(p), b = t & 1;
-    const bool draft = w.draft();
+  while (next_piece(p, sm.len, w)) {
     // Keys that no row sees may hold anything; V of them must not be NaN (0 * NaN).
-    bool live = key < nkeys;
-    if (kV && !draft && p.window > 0) {
-      const int k = w.key0() + key;
-      live = live && (k >= w.L + p.min_depth - p.window || k < p.sinks);
-    }
-    bool ok = !*abort && mbar_wait(smem_addr(&sm.cfull[stage]), phase, p.err, p.wait_ns);
-    // The buffer's previous tile has been multiplied.
-    uint64_t* freed = kV ? &sm.pvdone[b] : &sm.kempty[b];
-    auto wait_buffer = [&] {
-      if (ok && t >= 2) ok = mbar_wait(smem_addr(freed), ((t >> 1) & 1) ^ 1u, p.err, p.wait_ns);
-      ok = __all_sync(0xffffffffu, ok);
-      if (kV) return;
-      tc_fence_after();
-    };
-    const uint32_t vdst = sm.v + b * kVTile + key * 128, sw = static_cast<uint32_t>(key & 7) << 4;
-    // 32 dims as 16 words.
-    auto put = [&](int c, const uint32_t* o) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int ch = 4 * c + i;
-        sts128(vdst + (ch >> 3) * kVHalf + ((static_cast<uint32_t>(ch & 7) << 4) ^ sw),
-               make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+    const int lo = kV && p.window > 0 ? w.L + p.min_depth - p.window : 0;
+#pragma unroll 1
+    for (int lt = w.lt0; lt < w.lt1; ++lt, ++t) {
+      const int b = t & 1, key0 = w.key0(lt);
+      const bool draft = w.draft(lt);
+      bool live = key < w.nkeys(lt, p.N);
+      if (kV && !draft) live = live && (key0 + key >= lo || key0 + key < p.sinks);
+      // The tile's bytes, and the buffer: its previous tile has been multiplied.
+      bool ok = !*abort && mbar_wait(smem_addr(&sm.cfull[stage]), phase, p.err, p.wait_ns);
+      if (t >= 2) ok = ok && mbar_wait(smem_addr(kV ? &sm.pvdone[b] : &sm.kempty[b]), ((t >> 1) & 1) ^ 1u, p.err, p.wait_ns);
+      if (!__all_sync(0xffffffffu, ok)) {
+        *abort = 1;
+        return;
       }
-    };
-    if (__all_sync(0xffffffffu, ok)) {
+      if (!kV) tc_fence_after();
+      const uint32_t d = dst + b * (kV ? kVTile : 64), st = stage * kStageSize;
       if (!draft) {
-        uint4 x[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) x[c] = lds128(src + stage * kStageSize + c * kChunkStride);
-        uint2 sc = lds64(ssrc + stage * kStageSize);
-        if (kV && !live) {
-          sc = make_uint2(0u, 0u);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) x[c] = make_uint4(0u, 0u, 0u, 0u);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_addr(&sm.cempty[stage]));
-        wait_buffer();
-        if (ok) {
+        uint2 sc = lds64(ssrc + st);
+        if (kV && !live) sc = make_uint2(0u, 0u);  // (any code times 0 is 0)
+#pragma unroll 1
+        for (int hf = 0; hf < 2; ++hf) {
+          const uint4 x0 = lds128(src + st + hf * 2 * kChunkStride), x1 = lds128(src + st + hf * 2 * kChunkStride + kChunkStride);
+          const uint32_t four = hf ? sc.y : sc.x;
+          uint32_t o[32];
+          const uint2 s0 = scale_pair(four), s1 = scale_pair(four >> 16);
+          decode16(x0.x, x0.y, s0.x, o);
+          decode16(x0.z, x0.w, s0.y, o + 8);
+          decode16(x1.x, x1.y, s1.x, o + 16);
+          decode16(x1.z, x1.w, s1.y, o + 24);
           if constexpr (kV) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              uint32_t o[16];
-              const uint2 s2 = scale_pair(sc, c);
-              decode16(x[c].x, x[c].y, s2.x, o);
-              decode16(x[c].z, x[c].w, s2.y, o + 8);
-              put(c, o);
-            }
+            put_v(d + hf * kVHalf, sw, 0, o);
+            put_v(d + hf * kVHalf, sw, 1, o + 16);
           } else {
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              uint32_t o[32];
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const int c = 2 * hf + i;
-                const uint2 s2 = scale_pair(sc, c);
-                decode16(x[c].x, x[c].y, s2.x, o + 16 * i);
-                decode16(x[c].z, x[c].w, s2.y, o + 16 * i + 8);
-              }
-              tmem_st32(trow + 64 * b + 32 * hf, o);
-            }
+            tmem_st32(d + 32 * hf, o);
           }
         }
       } else {
-        wait_buffer();
-        if (ok) {
-#pragma unroll 1
-          for (int hf = 0; hf < 2; ++hf) {
-            uint32_t o[32];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              uint4 x = make_uint4(0u, 0u, 0u, 0u);
-              if (live) x = lds128(dsrc + stage * kStageSize + (8 * hf + i) * 16);
-              o[4 * i] = bf16x2_to_f16x2(x.x);
-              o[4 * i + 1] = bf16x2_to_f16x2(x.y);
-              o[4 * i + 2] = bf16x2_to_f16x2(x.z);
-              o[4 * i + 3] = bf16x2_to_f16x2(x.w);
-            }
-            if constexpr (kV) {
-              put(2 * hf, o);
-              put(2 * hf + 1, o + 16);
-            } else {
-              tmem_st32(trow + 64 * b + 32 * hf, o);
-            }
-          }
-        }
-        __syncwarp();
-        if (lane == 0 && ok) mbar_arrive(smem_addr(&sm.cempty[stage]));
+        decode_draft<kV>(dsrc + st, live, d, sw);
       }
-    } else {
-      ok = false;
-    }
-    if (!ok) {
-      *abort = 1;
-      return;
-    }
-    if constexpr (kV) {
-      fence_proxy_async_smem();
-    } else {
-      tmem_wait_st();
-      tc_fence_before();
-    }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(smem_addr(kV ? &sm.vfull[b] : &sm.kfull[b]));
-    if (++stage == CF::kStages) {
-      stage = 0;
-      phase ^= 1u;
+      if constexpr (kV) {
+        fence_proxy_async_smem();
+      } else {
+        tmem_wait_st();
+        tc_fence_before();
+      }
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(smem_addr(&sm.cempty[stage]));
+        mbar_arrive(smem_addr(kV ? &sm.vfull[b] : &sm.kfull[b]));
+      }
+      if (++stage == CF::kStages) {
+        stage = 0;
+        phase ^= 1u;
+      }
     }
   }
 }
@@ -505,60 +487,62 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& sm, 
 // ------------------------------------------------------------ MMA issue (one thread each)
 
 template <class CF>
-__device__ __forceinline__ void run_qk(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Walk w) {
+__device__ __forceinline__ void run_qk(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Piece w) {
   const AttnParams& p = kp.a;
   volatile int* abort = &sm.misc[0];
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, false);
-  int piece = -1;
-  for (int t = 0; w.t < w.t_end; ++t, w.next(p, sm.len)) {
-    const int b = t & 1;
-    bool ok = !*abort;
-    if (w.first()) {
-      ++piece;
-      ok = ok && mbar_wait(smem_addr(&sm.qfull[piece & 1]), (piece >> 1) & 1, p.err, p.wait_ns);
-    }
-    if (t >= 2) ok = ok && mbar_wait(smem_addr(&sm.pfull[b]), ((t >> 1) & 1) ^ 1u, p.err, p.wait_ns);  // S has been read
-    ok = ok && mbar_wait(smem_addr(&sm.kfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
-    if (!ok) {
-      *abort = 1;
-      break;
-    }
-    tc_fence_after();
-    const uint32_t q = sm.q + (piece & 1) * CF::kQTile;
+  bool ok = true;
+  for (int piece = 0, t = 0; ok && next_piece(p, sm.len, w); ++piece) {
+    ok = mbar_wait(smem_addr(&sm.qfull[piece & 1]), (piece >> 1) & 1, p.err, p.wait_ns);
+    const uint64_t q = smem_desc_sw128(sm.q + (piece & 1) * CF::kQTile, 16, 1024);
+#pragma unroll 1
+    for (int lt = w.lt0; lt < w.lt1; ++lt, ++t) {
+      const int b = t & 1;
+      ok = ok && !*abort;
+      if (t >= 2) ok = ok && mbar_wait(smem_addr(&sm.pfull[b]), ((t >> 1) & 1) ^ 1u, p.err, p.wait_ns);  // S has been read
+      ok = ok && mbar_wait(smem_addr(&sm.kfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
+      if (!ok) {
+        *abort = 1;
+        break;
+      }
+      tc_fence_after();
 #pragma unroll
-    for (int ks = 0; ks < kHeadDim / 16; ++ks)
-      tc_mma_tmem_a(tmem + CF::kTmemS + b * CF::kNT, tmem + CF::kTmemK + 64 * b + 8 * ks,
-                    smem_desc_sw128(q + (ks >> 2) * (CF::kNT * 128) + (ks & 3) * 32, 16, 1024), idesc, ks > 0);
-    tc_commit(smem_addr(&sm.sfull[b]));
-    tc_commit(smem_addr(&sm.kempty[b]));
-    if (w.last()) tc_commit(smem_addr(&sm.qempty[piece & 1]));
+      for (int ks = 0; ks < kHeadDim / 16; ++ks)
+        tc_mma_tmem_a(tmem + CF::kTmemS + b * CF::kNT, tmem + CF::kTmemK + 64 * b + 8 * ks,
+                      q + (((ks >> 2) * (CF::kNT * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
+      tc_commit(smem_addr(&sm.sfull[b]));
+      tc_commit(smem_addr(&sm.kempty[b]));
+    }
+    if (ok) tc_commit(smem_addr(&sm.qempty[piece & 1]));
   }
   tc_commit(smem_addr(&sm.mmadone[0]));
 }
 
 template <class CF>
-__device__ __forceinline__ void run_pv(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Walk w) {
+__device__ __forceinline__ void run_pv(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Piece w) {
   const AttnParams& p = kp.a;
   volatile int* abort = &sm.misc[0];
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, true, true);
-  int piece = -1;
-  for (int t = 0; w.t < w.t_end; ++t, w.next(p, sm.len)) {
-    const int b = t & 1;
-    bool ok = !*abort;
-    const bool first = w.first();
-    if (first && ++piece > 0) ok = ok && mbar_wait(smem_addr(sm.ofree), (piece - 1) & 1, p.err, p.wait_ns);
-    ok = ok && mbar_wait(smem_addr(&sm.vfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
-    ok = ok && mbar_wait(smem_addr(&sm.pfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
-    if (!ok) {
-      *abort = 1;
-      break;
-    }
-    tc_fence_after();
+  const uint64_t v0 = smem_desc_sw128(sm.v, kVHalf, 1024), p0 = smem_desc_sw128(sm.p, kPTile, 1024);
+  bool ok = true;
+  for (int piece = 0, t = 0; ok && next_piece(p, sm.len, w); ++piece) {
+    if (piece > 0) ok = mbar_wait(smem_addr(sm.ofree), (piece - 1) & 1, p.err, p.wait_ns);
+#pragma unroll 1
+    for (int lt = w.lt0; lt < w.lt1; ++lt, ++t) {
+      const int b = t & 1;
+      ok = ok && !*abort && mbar_wait(smem_addr(&sm.vfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
+      ok = ok && mbar_wait(smem_addr(&sm.pfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
+      if (!ok) {
+        *abort = 1;
+        break;
+      }
+      tc_fence_after();
 #pragma unroll
-    for (int k16 = 0; k16 < kTile / 16; ++k16)  // two 8-key groups of 1 KB each
-      tc_mma(tmem + CF::kTmemO, smem_desc_sw128(sm.v + b * kVTile + k16 * 2048, kVHalf, 1024),
-             smem_desc_sw128(sm.p + b * kPTile + k16 * 2048, kPTile, 1024), idesc, !(first && k16 == 0));
-    tc_commit(smem_addr(&sm.pvdone[b]));
+      for (int k16 = 0; k16 < kTile / 16; ++k16)  // two 8-key groups of 1 KB each
+        tc_mma(tmem + CF::kTmemO, v0 + ((b * kVTile + k16 * 2048) >> 4), p0 + ((b * kPTile + k16 * 2048) >> 4), idesc,
+               lt > w.lt0 || k16 > 0);
+      tc_commit(smem_addr(&sm.pvdone[b]));
+    }
   }
   tc_commit(smem_addr(&sm.mmadone[1]));
 }
@@ -584,226 +568,276 @@ __device__ __forceinline__ int ordered(float f) {
 }
 __device__ __forceinline__ float unordered(int i) { return __int_as_float(i >= 0 ? i : i ^ 0x7fffffff); }
 
+// Sums of the columns over the warp's lanes: N sums to 32 lanes by halving, then plain for what is left.  Lane's v[i],
+// i < the final width, is then the sum of column column0 + i.
+template <int N>
+__device__ __forceinline__ int column_sums(float (&v)[N], int lane, int* column0) {
+  int width = N, col = 0;
+#pragma unroll
+  for (int bit = 16; bit > 0; bit >>= 1) {
+    if (width % 2 == 0) {
+      width /= 2;
+      const bool up = lane & bit;
+      col += up ? width : 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (i < width) {
+          const float send = up ? v[i] : v[i + width], keep = up ? v[i + width] : v[i];
+          v[i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (i < width) v[i] += __shfl_xor_sync(0xffffffffu, v[i], bit);
+    }
+  }
+  *column0 = col;
+  return width;
+}
+
+// The nodes of a unit's rows: depths, ancestors, places in q and out.  All softmax threads.
+__device__ __noinline__ void load_rows(const AttnParams& p, const Smem& sm, int nc, int rb, int seq, bool new_seq) {
+  const int tid = threadIdx.x;
+  named_barrier_sync(kBarSoftmax, kSoftmaxThreads);  // the rows before are no longer read
+  if (new_seq) {
+    for (int i = tid; i < p.N; i += kSoftmaxThreads) {
+      int v = p.tree_parent[static_cast<size_t>(seq) * p.N + i];
+      if (v < -1 || v >= i) {
+        set_error(p.err, KVSHOT_ERR_TREE);
+        v = -1;
+      }
+      sm.par[i] = v;
+    }
+    named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
+    for (int i = tid; i < p.N; i += kSoftmaxThreads) {
+      uint64_t bits = 0;
+      for (int m = i; m >= 0; m = sm.par[m]) bits |= 1ull << m;  // parents strictly decrease
+      sm.anc[i] = bits;
+    }
+    named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
+  }
+  if (tid < nc) {
+    const int rr = rb * p.rows_per_unit + tid;
+    const int nl = min(rr, p.rows_total - 1) / p.G, node = p.N - p.Nq + nl;
+    if (p.tree) sm.row_anc[tid] = sm.anc[node];
+    sm.depth[tid] = p.tree ? __popcll(sm.anc[node]) : node + 1;
+    sm.place[tid] = nl * p.hq + rr - nl * p.G;
+  }
+}
+
+// Bit j: row j sees this thread's key.  `at`: token position or draft slot of the key, which is valid.
+__device__ __noinline__ uint64_t visible_rows(const AttnParams& p, const Smem& sm, int nc, bool draft, int at, int L) {
+  uint64_t bits = 0;
+  const int key_depth = !draft ? 0 : p.tree ? __popcll(sm.anc[at]) : at + 1;
+  const int pos = draft ? L + key_depth - 1 : at;
+  const bool always = p.window == 0 || pos < p.sinks;
+#pragma unroll 1
+  for (int j = 0; j < nc; ++j) {
+    const int d = sm.depth[j];
+    bool v = always || L + d - 1 - pos < p.window;
+    if (draft) v = v && (p.tree ? (sm.row_anc[j] >> at) & 1ull : at < d);
+    bits |= static_cast<uint64_t>(v) << j;
+  }
+  return bits;
+}
+
+// The references of rows whose scores have passed their limit move: sm.ref, and sm.alpha with what O and the sums are
+// to be multiplied by.  All softmax threads.
+__device__ __noinline__ void move_references(const Smem& sm, int nc, uint32_t scores, float qs, uint64_t vis) {
+  const int tid = threadIdx.x, warp = tid >> 5;
+#pragma unroll 1
+  for (int j = 0; j < nc; j += 8) {
+    uint32_t s[8];
+    tmem_ld8(scores + j, s);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = (vis >> (j + i)) & 1ull ? __uint_as_float(s[i]) * qs : -INFINITY;
+      const int m = __reduce_max_sync(0xffffffffu, ordered(x));
+      if ((tid & 31) == 0) sm.wmax[warp * 64 + j + i] = m;
+    }
+  }
+  named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
+  if (tid < nc) {
+    const float m = unordered(max(max(sm.wmax[tid], sm.wmax[64 + tid]), max(sm.wmax[128 + tid], sm.wmax[192 + tid])));
+    const float old = sm.ref[tid], ref = m - old > kRefLimit ? m - kRefBelow : old;
+    sm.ref[tid] = ref;
+    sm.alpha[tid] = ex2(old - ref);
+  }
+  named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
+}
+
+// O of this thread's dim, row by row, times sm.alpha and vs.
+__device__ __noinline__ void rescale_o(const Smem& sm, int nc, uint32_t o_cols, float vs) {
+#pragma unroll 1
+  for (int j = 0; j < nc; j += 8) {
+    uint32_t o[8];
+    tmem_ld8(o_cols + j, o);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * (sm.alpha[j + i] * vs));
+    tmem_st8(o_cols + j, o);
+  }
+  tmem_wait_st();
+}
+
+// A piece's output rows: the final ones, or the piece's part in the workspace.  Thread = dim.
+__device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, const Piece& w, int nc, uint32_t o_cols) {
+  const int tid = threadIdx.x;
+  const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
+  const size_t row0 = static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G;
+  const size_t part = static_cast<size_t>(w.c * p.hkv * p.row_blocks + w.hr + blockIdx.x) * p.rows_per_unit;
+  const bool whole = w.whole();
+  if (tid < rows) {
+    const float sum = sm.sum[tid], lse2 = sum == 0.f ? -INFINITY : sm.ref[tid] + __log2f(sum);
+    if (whole) p.lse[row0 + sm.place[tid]] = lse2 * 0.69314718055994531f;
+    else p.ws_lse[part + tid] = lse2;
+  }
+#pragma unroll 1
+  for (int j = 0; j < nc; j += 8) {
+    uint32_t o[8];
+    tmem_ld8(o_cols + j, o);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (j + i >= rows) break;
+      const float v = __uint_as_float(o[i]) * sm.inv[j + i];
+      if (whole) p.out[(row0 + sm.place[j + i]) * kHeadDim + tid] = __float2bfloat16(v);
+      else p.ws_o[(part + j + i) * kHeadDim + tid] = v;
+    }
+  }
+}
+
 template <class CF>
-__device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Walk w) {
+__device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Piece w) {
   constexpr int NC = CF::kNC;
   const AttnParams& p = kp.a;
   volatile int* abort = &sm.misc[0];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t trow = tmem + (static_cast<uint32_t>(tid & 96) << 16);
-  const int HR = p.hkv * p.row_blocks;
-  float l[NC];         // this thread's keys only
-  int unit_rb = -1, unit_seq = -1, dmax = 0, piece_lt0 = 0, h = 0, rb = 0;
-  bool in_codes = false;  // O is in units of the value codes
+  const uint32_t pdst = sm.p + tid * 128, sw = static_cast<uint32_t>(tid & 7) << 4;
+  int unit_rb = -1, unit_seq = -1, t = 0;
   wait_for_prerequisite_grid();  // outputs and scratch may be the preceding kernel's
-  for (int t = 0; w.t < w.t_end; ++t, w.next(p, sm.len)) {
-    const int b = t & 1, key0 = w.key0(), nkeys = w.nkeys(p);
-    const bool draft = w.draft(), first = w.first();
-    if (first) {
-      h = w.hr / p.row_blocks;
-      rb = w.hr - h * p.row_blocks;
-      piece_lt0 = w.lt;
-      in_codes = !draft;
-      const int seq = w.c / (p.C / p.B);
-      if (rb != unit_rb || (p.tree && seq != unit_seq)) {
-        // The rows' nodes: depths and ancestors.
-        if (p.tree && seq != unit_seq) {
-          named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-          for (int i = tid; i < p.N; i += kSoftmaxThreads) {
-            int v = p.tree_parent[static_cast<size_t>(seq) * p.N + i];
-            if (v < -1 || v >= i) {
-              set_error(p.err, KVSHOT_ERR_TREE);
-              v = -1;
-            }
-            sm.par[i] = v;
+  while (next_piece(p, sm.len, w)) {
+    if (w.rb != unit_rb || (p.tree && w.seq != unit_seq)) {
+      load_rows(p, sm, NC, w.rb, w.seq, p.tree && w.seq != unit_seq);
+      unit_rb = w.rb;
+      unit_seq = w.seq;
+    }
+    if (tid < NC) sm.ref[tid] = kNoRef;
+    named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
+    float l[NC];  // sums over this thread's keys
+#pragma unroll
+    for (int j = 0; j < NC; ++j) l[j] = 0.f;
+    // Tiles from here on (or before the sinks' end) are seen whole by every row.
+    int seen_from = 0;
+    if (p.window > 0) {
+      int dmax = 0;
+#pragma unroll 1
+      for (int j = 0; j < NC; ++j) dmax = max(dmax, sm.depth[j]);
+      seen_from = w.L + dmax - p.window;
+    }
+    bool in_codes = !w.draft(w.lt0);  // O is in units of the value codes
+#pragma unroll 1
+    for (int lt = w.lt0; lt < w.lt1; ++lt, ++t) {
+      const int b = t & 1, key0 = w.key0(lt), nkeys = w.nkeys(lt, p.N);
+      const bool draft = w.draft(lt);
+      const float qs = draft ? p.qscale : p.qscale * p.k_scale;
+      uint64_t vis = ~0ull;
+      if (draft || nkeys < kTile || (key0 < seen_from && key0 + kTile > p.sinks))
+        vis = tid < nkeys ? visible_rows(p, sm, NC, draft, key0 + tid, w.L) : 0ull;
+      bool ok = !*abort && mbar_wait(smem_addr(&sm.sfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      const uint32_t scores = trow + CF::kTmemS + b * CF::kNT;
+      const bool leave_codes = draft && in_codes && p.v_scale != 1.f;
+      if (draft) in_codes = false;
+      float x[NC];
+      for (bool moved = false;; moved = true) {
+        if (ok) {
+          uint32_t s[NC];
+          tmem_ld_cols<NC>(scores, s);
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < NC; j += 4) {
+            const float4 m = *reinterpret_cast<const float4*>(sm.ref + j);
+            x[j] = fmaf(__uint_as_float(s[j]), qs, -m.x);
+            x[j + 1] = fmaf(__uint_as_float(s[j + 1]), qs, -m.y);
+            x[j + 2] = fmaf(__uint_as_float(s[j + 2]), qs, -m.z);
+            x[j + 3] = fmaf(__uint_as_float(s[j + 3]), qs, -m.w);
           }
-          named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-          for (int i = tid; i < p.N; i += kSoftmaxThreads) {
-            uint64_t bits = 0;
-            for (int m = i; m >= 0; m = sm.par[m]) bits |= 1ull << m;  // parents strictly decrease
-            sm.anc[i] = bits;
+          if (vis != ~0ull) {
+#pragma unroll
+            for (int j = 0; j < NC; ++j) x[j] = (vis >> j) & 1ull ? x[j] : -INFINITY;
           }
         }
-        named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-        if (tid < NC) {
-          const int rr = min(rb * p.rows_per_unit + tid, p.rows_total - 1);
-          const int node = p.N - p.Nq + rr / p.G;
-          if (p.tree) sm.row_anc[tid] = sm.anc[node];
-          sm.depth[tid] = p.tree ? __popcll(sm.anc[node]) : node + 1;
-        }
-        unit_rb = rb;
-        unit_seq = seq;
-      }
-      if (tid < NC) sm.ref[tid] = kNoRef;
-      named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-      dmax = 0;
+        if (moved) break;
+        float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        dmax = max(dmax, sm.depth[j]);
-        l[j] = 0.f;
-      }
-    }
-    // Where the tile holds keys that some row does not see.
-    const bool full = !draft && nkeys == kTile &&
-                      (p.window == 0 || key0 >= w.L + dmax - p.window || key0 + kTile <= p.sinks);
-    const float qs = draft ? p.qscale : p.qscale * p.k_scale;
-    const int key = key0 + tid;
-    int key_depth = 0;
-    bool sink = false;
-    if (draft && tid < nkeys) {
-      key_depth = p.tree ? __popcll(sm.anc[key]) : key + 1;
-      sink = w.L + key_depth - 1 < p.sinks;
-    }
-    auto sees = [&](int j) {  // row j sees this thread's key
-      if (tid >= nkeys) return false;
-      const int d = sm.depth[j];
-      if (draft) {
-        const bool line = p.tree ? (sm.row_anc[j] >> key) & 1ull : key < d;
-        return line && (p.window == 0 || d - key_depth < p.window || sink);
-      }
-      return p.window == 0 || key >= w.L + d - p.window || key < p.sinks;
-    };
-    bool ok = !*abort && mbar_wait(smem_addr(&sm.sfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
-    ok = __all_sync(0xffffffffu, ok);
-    tc_fence_after();
-    float x[NC];
-    auto load_scores = [&] {
-      uint32_t s[NC];
-      tmem_ld_cols<NC>(trow + CF::kTmemS + b * CF::kNT, s);
-      tmem_wait_ld();
-#pragma unroll
-      for (int j = 0; j < NC; ++j) x[j] = __uint_as_float(s[j]);
-    };
-    float top = -INFINITY;
-    if (ok) {
-      load_scores();
-#pragma unroll
-      for (int j = 0; j < NC; j += 4) {
-        const float4 m = *reinterpret_cast<const float4*>(sm.ref + j);
-        x[j] = fmaf(x[j], qs, -m.x);
-        x[j + 1] = fmaf(x[j + 1], qs, -m.y);
-        x[j + 2] = fmaf(x[j + 2], qs, -m.z);
-        x[j + 3] = fmaf(x[j + 3], qs, -m.w);
-      }
-      if (!full) {
-#pragma unroll
-        for (int j = 0; j < NC; ++j)
-          if (!sees(j)) x[j] = -INFINITY;
-      }
-#pragma unroll
-      for (int j = 0; j < NC; ++j) top = fmaxf(top, x[j]);
-    }
-    const bool leave_codes = draft && in_codes && p.v_scale != 1.f;
-    if (any_softmax(top > kRefLimit || leave_codes || !ok)) {
-      // A row's reference moves (always with a piece's first keys).
-      if (any_softmax(!ok)) {
-        *abort = 1;
-        return;
-      }
-      load_scores();
-#pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        x[j] = full || sees(j) ? x[j] * qs : -INFINITY;
-        const int m = __reduce_max_sync(0xffffffffu, ordered(x[j]));
-        if (lane == 0) sm.wmax[warp * 64 + j] = m;
-      }
-      named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-      if (tid < NC) {
-        const float m = unordered(max(max(sm.wmax[tid], sm.wmax[64 + tid]), max(sm.wmax[128 + tid], sm.wmax[192 + tid])));
-        const float old = sm.ref[tid], ref = m - old > kRefLimit ? m - kRefBelow : old;
-        sm.ref[tid] = ref;
-        sm.alpha[tid] = ex2(old - ref);
-      }
-      named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-#pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        l[j] *= sm.alpha[j];
-        x[j] -= sm.ref[j];
-      }
-      if (!first) {
-        ok = mbar_wait(smem_addr(&sm.pvdone[b ^ 1]), ((t - 1) >> 1) & 1, p.err, p.wait_ns);
+        for (int j = 0; j < NC; ++j) top = fmaxf(top, x[j]);
+        if (!any_softmax(top > kRefLimit || leave_codes || !ok)) break;
         if (any_softmax(!ok)) {
           *abort = 1;
           return;
         }
-        tc_fence_after();
-        const float vs = leave_codes ? p.v_scale : 1.f;
-        uint32_t o[NC];
-        tmem_ld_cols<NC>(trow + CF::kTmemO, o);
-        tmem_wait_ld();
+        move_references(sm, NC, scores, qs, vis);  // always with a piece's first keys
 #pragma unroll
-        for (int j = 0; j < NC; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * (sm.alpha[j] * vs));
-        tmem_st_cols<NC>(trow + CF::kTmemO, o);
-        tmem_wait_st();
-      }
-    }
-    if (draft) in_codes = false;
-    // P's buffer is free when P.V of the tile before the last is done.
-    ok = t < 2 || mbar_wait(smem_addr(&sm.pvdone[b]), ((t >> 1) & 1) ^ 1u, p.err, p.wait_ns);
-    const uint32_t pdst = sm.p + b * kPTile + tid * 128, sw = static_cast<uint32_t>(tid & 7) << 4;
-#pragma unroll
-    for (int j = 0; j < NC; j += 8) {
-      float e[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        e[i] = ex2(x[j + i]);
-        l[j + i] += e[i];
-      }
-      if (ok)
-        sts128(pdst + ((static_cast<uint32_t>(j) << 1) ^ sw),
-               make_uint4(pack_f16x2(e[0], e[1]), pack_f16x2(e[2], e[3]), pack_f16x2(e[4], e[5]), pack_f16x2(e[6], e[7])));
-    }
-    fence_proxy_async_smem();
-    tc_fence_before();
-    ok = __all_sync(0xffffffffu, ok);
-    if (lane == 0 && ok) mbar_arrive(smem_addr(&sm.pfull[b]));
-    if (!ok) *abort = 1;  // (the next vote takes every softmax thread out)
-    if (w.last()) {
-      // Sums over the keys' threads, then the rows.
-#pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        float v = l[j];
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-        if (lane == 0) sm.wmax[warp * 64 + j] = __float_as_int(v);
-      }
-      ok = ok && mbar_wait(smem_addr(&sm.pvdone[b]), (t >> 1) & 1, p.err, p.wait_ns);
-      if (any_softmax(!ok)) {
-        *abort = 1;
-        return;
-      }
-      tc_fence_after();
-      const bool whole = piece_lt0 == 0 && w.lt == w.ut - 1;
-      const int slot = w.c * HR + w.hr + blockIdx.x;
-      const int rows = min(p.rows_per_unit, p.rows_total - rb * p.rows_per_unit);
-      auto out_row = [&](int j) {
-        const int rr = rb * p.rows_per_unit + j, nl = rr / p.G;
-        return (static_cast<size_t>(w.c) * p.Nq + nl) * p.hq + h * p.G + rr - nl * p.G;
-      };
-      if (tid < NC) {
-        const float sum = (__int_as_float(sm.wmax[tid]) + __int_as_float(sm.wmax[64 + tid])) +
-                          (__int_as_float(sm.wmax[128 + tid]) + __int_as_float(sm.wmax[192 + tid]));
-        sm.inv[tid] = sum > 0.f ? (in_codes ? p.v_scale : 1.f) / sum : sum == 0.f ? 0.f : sum;  // (NaN stays)
-        const float lse2 = sum == 0.f ? -INFINITY : sm.ref[tid] + __log2f(sum);
-        if (tid < rows) {
-          if (whole) p.lse[out_row(tid)] = lse2 * 0.69314718055994531f;
-          else p.ws_lse[static_cast<size_t>(slot) * p.rows_per_unit + tid] = lse2;
+        for (int j = 0; j < NC; ++j) l[j] *= sm.alpha[j];
+        if (lt > w.lt0) {
+          ok = mbar_wait(smem_addr(&sm.pvdone[b ^ 1]), ((t - 1) >> 1) & 1, p.err, p.wait_ns);
+          if (any_softmax(!ok)) {
+            *abort = 1;
+            return;
+          }
+          tc_fence_after();
+          rescale_o(sm, NC, trow + CF::kTmemO, leave_codes ? p.v_scale : 1.f);
         }
       }
-      uint32_t o[NC];
-      tmem_ld_cols<NC>(trow + CF::kTmemO, o);
-      tmem_wait_ld();
-      tc_fence_before();
-      named_barrier_sync(kBarSoftmax, kSoftmaxThreads);  // (and wmax has been read)
-      if (lane == 0) mbar_arrive(smem_addr(sm.ofree));
+      // P's buffer is free when P.V of the tile before the last is done.
+      ok = t < 2 || mbar_wait(smem_addr(&sm.pvdone[b]), ((t >> 1) & 1) ^ 1u, p.err, p.wait_ns);
+      ok = __all_sync(0xffffffffu, ok);
 #pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        if (j >= rows) break;
-        const float v = __uint_as_float(o[j]) * sm.inv[j];
-        if (whole) p.out[out_row(j) * kHeadDim + tid] = __float2bfloat16(v);
-        else p.ws_o[(static_cast<size_t>(slot) * p.rows_per_unit + j) * kHeadDim + tid] = v;
+      for (int j = 0; j < NC; j += 8) {
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          e[i] = ex2(x[j + i]);
+          l[j + i] += e[i];
+        }
+        if (ok)
+          sts128(pdst + b * kPTile + ((static_cast<uint32_t>(j) << 1) ^ sw),
+                 make_uint4(pack_f16x2(e[0], e[1]), pack_f16x2(e[2], e[3]), pack_f16x2(e[4], e[5]), pack_f16x2(e[6], e[7])));
       }
+      fence_proxy_async_smem();
+      tc_fence_before();
+      __syncwarp();
+      if (!ok) *abort = 1;  // (the next vote takes every softmax thread out)
+      else if (lane == 0) mbar_arrive(smem_addr(&sm.pfull[b]));
     }
+    // Sums over the keys' threads, then the rows.
+    int col = 0;
+    const int width = column_sums(l, lane, &col);
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+      if (i < width) sm.wmax[warp * 64 + col + i] = __float_as_int(l[i]);
+    const int tl = t - 1;
+    const bool ok = !*abort && mbar_wait(smem_addr(&sm.pvdone[tl & 1]), (tl >> 1) & 1, p.err, p.wait_ns);
+    if (any_softmax(!ok)) {
+      *abort = 1;
+      return;
+    }
+    if (tid < NC) {
+      const float sum = (__int_as_float(sm.wmax[tid]) + __int_as_float(sm.wmax[64 + tid])) +
+                        (__int_as_float(sm.wmax[128 + tid]) + __int_as_float(sm.wmax[192 + tid]));
+      sm.sum[tid] = sum;
+      sm.inv[tid] = sum == 0.f ? 0.f : (in_codes ? p.v_scale : 1.f) / sum;
+    }
+    named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
+    tc_fence_after();
+    write_rows(p, sm, w, NC, trow + CF::kTmemO);
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_addr(sm.ofree));
   }
 }
 
@@ -842,8 +876,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   build_kv4_plan(p, sm.len, sm.base);  // (barriers inside)
   tc_fence_after();
   const uint32_t tmem = *sm.tmem;
-  Walk w;
-  w.begin(p, sm.len, sm.base);
+  Piece w;
+  begin_pieces(p, sm.len, sm.base, w);
   if (warp < kWarpK) run_softmax<CF>(kp, sm, tmem, w);
   else if (warp < kWarpV) run_decode<CF, false>(kp, sm, tmem, w);
   else if (warp < kWarpLoad) run_decode<CF, true>(kp, sm, tmem, w);
