@@ -9,8 +9,12 @@
 // The cache's bytes stream through a ring of tiles (one bulk copy per run of groups) and are decoded by warps of their
 // own: a thread takes one key's codes, two per conversion (e2m1 -> f16, times the block's scale: both exact), K into
 // tensor memory, V into shared memory.
-// Warp roles: 0..3 softmax and epilogue (thread = key, then dim), 4..7 decode K, 8..11 decode V, 12 loads, 13 issues
-// QK^T and owns tensor memory, 14 issues P.V, 15 stages q (f16).
+// Warp roles: 0..7 two softmax warpgroups (thread = key, then dim), 8..15 two decoding warpgroups (thread = key), 16
+// loads, 17 issues QK^T and owns tensor memory, 18 issues P.V, 19 stages q (f16).  A tile's buffers (K and S in tensor
+// memory, V and P in shared memory) are pair t % 2.  Decoding warpgroup w takes tiles t % 2 == w, K and then V.  Up to
+// 32 rows the softmax warpgroups share the tiles out alike, each with its own references, sums and accumulator O_w,
+// joined by log-sum-exp at a piece's end: a role then has two tiles' time for the latencies of one tile's steps, which
+// bound it.  More rows have the warpgroups take half of the rows each, of every tile.
 // Work plan: the units' tiles laid end to end and cut into equal ranges, one per persistent CTA (kvshot_internal.h);
 // with a window a unit's tiles are those of the sinks and those of the window.
 #include <algorithm>
@@ -41,10 +45,11 @@ static_assert(2 * kDraftV <= kStageSize, "a draft tile fits a stage");
 constexpr int kVHalf = kTile * 128;                // 64 dims of a tile's V: 128 rows of 128 bytes, 128-byte swizzle
 constexpr int kVTile = 2 * kVHalf;
 constexpr int kPTile = kTile * 128;                // P^T: a row of up to 64 query rows per key, 128-byte swizzle
-constexpr int kThreads = 16 * 32;
-constexpr int kSoftmaxThreads = 128;
-constexpr int kWarpK = 4, kWarpV = 8, kWarpLoad = 12, kWarpQk = 13, kWarpPv = 14, kWarpQ = 15;
-constexpr int kBarSoftmax = 1;
+constexpr int kThreads = 20 * 32;
+constexpr int kGroupThreads = 128;                 // a warpgroup
+constexpr int kSoftmaxThreads = 256;
+constexpr int kWarpDecode = 8, kWarpLoad = 16, kWarpQk = 17, kWarpPv = 18, kWarpQ = 19;
+constexpr int kBarGroup = 1, kBarSoftmax = 3;      // named barriers: 1 and 2 of a softmax warpgroup, 3 of both
 // The reference of a row is 2^8 below the maximum it was taken from and moves when a score passes it by 2^15: P stays in
 // f16's normal range for scores down to 2^-22 of the maximum and below its largest number.
 constexpr float kRefBelow = 8.f, kRefLimit = 15.f;
@@ -62,40 +67,43 @@ struct Kv4Params {
 template <int NC>
 struct Cfg {
   static constexpr int kNC = NC;
-  static constexpr int kNT = (NC + 15) / 16 * 16;  // the MMA's N
+  static constexpr int kNT = (NC + 15) / 16 * 16;      // the MMA's N
+  static constexpr bool kByTile = NC <= 32;            // the softmax warpgroups share out the tiles, else the rows
+  static constexpr int kCols = kByTile ? NC : NC / 2;  // rows of a softmax thread
+  static constexpr int kAccs = kByTile ? 2 : 1;        // accumulators
   static constexpr int kStages = NC <= 16 ? 6 : NC <= 32 ? 5 : 4;
   static constexpr int kQTile = kNT * 256;
   static constexpr uint32_t kTmemK = 0, kTmemS = 128, kTmemO = 128 + 2 * kNT;  // columns
-  static constexpr uint32_t kTmemCols = kTmemO + kNT <= 256 ? 256 : 512;
+  static constexpr uint32_t kTmemCols = kTmemO + kAccs * kNT <= 256 ? 256 : 512;
+  static_assert(kTmemO + kAccs * kNT <= 512 && kCols % 8 == 0, "tensor memory");
 };
 
 struct Smem {
-  uint32_t v, p, q, ring;          // shared-memory addresses
-  uint64_t *cfull, *cempty;        // [stages] bytes landed; read by the eight decode warps
-  uint64_t *kfull, *kempty;        // [2] K decoded; QK^T done
-  uint64_t *vfull;                 // [2] V decoded
-  uint64_t *sfull, *pfull, *pvdone;  // [2] QK^T done; P written (and S read); P.V done
-  uint64_t *qfull, *qempty;        // [2] q of a piece staged; its last QK^T done
-  uint64_t* ofree;                 // epilogue has read O
-  uint64_t* mmadone;               // [2]
-  uint64_t* anc;                   // [64] each node's ancestors and itself (tree)
-  uint64_t* row_anc;               // [64] those of each query row's node
-  float *ref, *alpha, *inv, *sum;  // [64] per row
-  int *depth, *place;              // [64] per row
-  int* wmax;                       // [4][64] per warp and row; sums at a piece's end
-  int* par;                        // [64]
+  uint32_t v, p, q, ring;            // shared-memory addresses
+  uint32_t cfull, cempty;            // barriers, by address. [stages] bytes landed; read by their decoding warpgroup
+  uint32_t kfull, vfull;             // [2] K, V decoded
+  uint32_t qkdone, pfull, pvdone;    // [2] QK^T done; P written (and S read); P.V done
+  uint32_t qfull, qempty;            // [2] q of a piece staged; its last QK^T done
+  uint32_t ofree, mmadone;           // epilogue has read O; [2] every MMA issued is done
+  uint64_t *anc, *row_anc;           // [64] each node's ancestors and itself (tree); of each query row's node
+  float *ref, *alpha, *inv;          // [2][64] per warpgroup and row
+  int* wmax;                         // [8][64] per warp and row; sums at a piece's end
+  int *depth, *place;                // [64] per row
+  int* par;                          // [64]
+  int* codes;                        // [2] the warpgroup's accumulator is in units of the value codes
   uint32_t* tmem;
-  int* misc;                       // [0] abort, [1] tiles issued by the loader
+  volatile int* abort;
+  int* issued;                       // tiles issued by the loader
   int *len, *base;
 };
 
-constexpr int kBarriers = 20;  // besides the ring's: 19, and one for the alignment of what follows
+constexpr int kBarriers = 18;  // besides the ring's: 17, and one for the alignment of what follows
 
 template <class CF>
 __host__ __device__ constexpr size_t smem_bytes(int C) {
   return 1024 + 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize +
-         sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + sizeof(uint64_t) * 128 + sizeof(int) * (64 * 11) +
-         sizeof(int) * (4 + 2 * C + 1);
+         sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + sizeof(uint64_t) * 128 +
+         sizeof(int) * (6 * 64 + 8 * 64 + 3 * 64 + 6) + sizeof(int) * (2 * C + 1);
 }
 
 template <class CF>
@@ -106,35 +114,61 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.p = s.v + 2 * kVTile;
   s.q = s.p + 2 * kPTile;
   s.ring = s.q + 2 * CF::kQTile;
-  uint64_t* m = reinterpret_cast<uint64_t*>(b + 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize);
-  s.cfull = m;
-  s.cempty = s.cfull + CF::kStages;
-  s.kfull = s.cempty + CF::kStages;
-  s.kempty = s.kfull + 2;
-  s.vfull = s.kempty + 2;
-  s.sfull = s.vfull + 2;
-  s.pfull = s.sfull + 2;
-  s.pvdone = s.pfull + 2;
-  s.qfull = s.pvdone + 2;
-  s.qempty = s.qfull + 2;
-  s.ofree = s.qempty + 2;
-  s.mmadone = s.ofree + 1;
-  s.anc = m + 2 * CF::kStages + kBarriers;
+  b += 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize;
+  s.cfull = smem_addr(b);
+  s.cempty = s.cfull + 8 * CF::kStages;
+  s.kfull = s.cempty + 8 * CF::kStages;
+  s.vfull = s.kfull + 16;
+  s.qkdone = s.vfull + 16;
+  s.pfull = s.qkdone + 16;
+  s.pvdone = s.pfull + 16;
+  s.qfull = s.pvdone + 16;
+  s.qempty = s.qfull + 16;
+  s.mmadone = s.qempty + 16;
+  s.ofree = s.mmadone + 16;
+  s.anc = reinterpret_cast<uint64_t*>(b) + 2 * CF::kStages + kBarriers;
   s.row_anc = s.anc + 64;
   s.ref = reinterpret_cast<float*>(s.row_anc + 64);
-  s.alpha = s.ref + 64;
-  s.inv = s.alpha + 64;
-  s.sum = s.inv + 64;
-  s.depth = reinterpret_cast<int*>(s.sum + 64);
+  s.alpha = s.ref + 128;
+  s.inv = s.alpha + 128;
+  s.wmax = reinterpret_cast<int*>(s.inv + 128);
+  s.depth = s.wmax + 8 * 64;
   s.place = s.depth + 64;
-  s.wmax = s.place + 64;
-  s.par = s.wmax + 4 * 64;
-  s.tmem = reinterpret_cast<uint32_t*>(s.par + 64);
-  s.misc = reinterpret_cast<int*>(s.tmem + 1);
-  s.len = s.misc + 3;
+  s.par = s.place + 64;
+  s.codes = s.par + 64;
+  s.tmem = reinterpret_cast<uint32_t*>(s.codes + 2);
+  s.abort = reinterpret_cast<volatile int*>(s.tmem + 1);
+  s.issued = s.codes + 4;
+  s.len = s.codes + 6;
   s.base = s.len + C;
   return s;
 }
+
+// Every wait ends: when its phase completes, when another role has given up, or (which gives up) after the call's limit.
+// The inline part is one test.
+__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, int32_t* err, uint64_t limit_ns, volatile int* abort) {
+  const bool poll = limit_ns < kPollBelowNs;  // (a blocking try could sit out a short limit)
+  const uint64_t t0 = global_timer_ns();
+  for (;;) {
+    for (int i = 0; i < (poll ? 1 : 16); ++i)
+      if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
+    if (*abort) return false;
+    if (global_timer_ns() - t0 > limit_ns) break;
+  }
+  set_error(err, KVSHOT_ERR_TIMEOUT);
+  *abort = 1;
+  return false;
+}
+
+struct Waiter {
+  int32_t* err;
+  uint64_t limit;
+  volatile int* abort;
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
+    if (mbar_test_wait(bar, parity)) return true;
+    return wait_slow(bar, parity, err, limit, abort);
+  }
+};
 
 // ------------------------------------------------------------ work plan
 
@@ -245,61 +279,58 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 }
 
 template <class CF>
-__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Smem& sm, Piece w) {
+__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Smem& sm, const Waiter& wait, Piece w) {
   const AttnParams& p = kp.a;
-  volatile int* abort = &sm.misc[0];
   const int lane = threadIdx.x & 31;
   int stage = 0, issued = 0;
   uint32_t phase = 0;
   bool waited = false, ok = true;
-  // Page ids come 32 to a load, a window of tiles ahead: lane i holds the page of run i % runs of the window's tile
+  // Page ids come 32 to a load, a window of tiles ahead: lane i holds the address of run i % runs of the window's tile
   // i / runs, and issues that copy.
   const int runs = kTileGroups / kp.run_groups, ahead = 32 / runs;
   const int my_tile = lane / runs, my_g0 = (lane % runs) * kp.run_groups;
   while (ok && next_piece(p, sm.len, w)) {
     const int32_t* table = p.page_table + (p.paged ? static_cast<size_t>(w.c) * p.max_pages : 0);
-    auto page_of = [&](int lt) {
+    auto group_of = [&](int lt) {  // this lane's first group of the window from tile lt on, or -1
       lt += my_tile;
-      if (lt >= w.lt1 || w.draft(lt)) return 0;
+      if (lt >= w.lt1 || w.draft(lt)) return -1;
       const int g = w.key0(lt) / kKv4Tokens + my_g0;
-      if (g * kKv4Tokens >= w.L) return 0;
-      return p.paged ? table[g / kp.groups_per_page] : w.c;
+      return g * kKv4Tokens < w.L ? g : -1;
     };
-    int pid = 0, next_pid = page_of(w.lt0), window = w.lt0;
+    auto page_of = [&](int g) { return g < 0 ? 0 : p.paged ? table[g / kp.groups_per_page] : w.c; };
+    int window = w.lt0, g = group_of(window), pid = page_of(g);
+    const uint8_t* src = nullptr;
+    uint32_t bytes = 0;
     for (int lt = w.lt0; lt < w.lt1; ++lt) {
       if (lt == window) {
-        pid = next_pid;
+        if (p.paged && g >= 0) pid = valid_page_id(p, pid);
+        src = kp.cache + ((static_cast<size_t>(pid) * p.hkv + w.h) * kp.groups_per_page +
+                          (p.paged ? g % kp.groups_per_page : g)) * kKv4Bytes;
+        bytes = g < 0 ? 0 : min(kp.run_groups, (w.L + kKv4Tokens - 1) / kKv4Tokens - g) * kKv4Bytes;
         window += ahead;
-        next_pid = page_of(window);
+        g = group_of(window);
+        pid = page_of(g);
       }
       const bool draft = w.draft(lt);
-      const int key0 = w.key0(lt), nkeys = w.nkeys(lt, p.N);
+      const int nkeys = w.nkeys(lt, p.N);
       if (draft && !waited) {  // the draft K/V may come from the preceding kernel
         wait_for_prerequisite_grid();
         waited = true;
       }
-      if (lane == 0) ok = mbar_wait(smem_addr(&sm.cempty[stage]), phase ^ 1u, p.err, p.wait_ns) && !*abort;
-      ok = __shfl_sync(0xffffffffu, ok, 0);
-      if (!ok) {
-        if (lane == 0) *abort = 1;
-        break;
-      }
-      const uint32_t bar = smem_addr(&sm.cfull[stage]), dst = sm.ring + stage * kStageSize;
-      const int groups = (nkeys + kKv4Tokens - 1) / kKv4Tokens;
-      if (lane == 0) mbar_arrive_expect_tx(bar, draft ? nkeys * 4 * kHeadDim : groups * kKv4Bytes);
+      ok = __all_sync(0xffffffffu, wait(sm.cempty + 8 * stage, phase ^ 1u));
+      if (!ok) break;
+      const uint32_t bar = sm.cfull + 8 * stage, dst = sm.ring + stage * kStageSize;
+      if (lane == 0)
+        mbar_arrive_expect_tx(bar, draft ? nkeys * 4 * kHeadDim : (nkeys + kKv4Tokens - 1) / kKv4Tokens * kKv4Bytes);
       __syncwarp();
       if (draft) {
         if (lane < nkeys) {
-          const size_t row = (static_cast<size_t>(w.c) * p.hkv + w.h) * p.n_max + key0 + lane;
+          const size_t row = (static_cast<size_t>(w.c) * p.hkv + w.h) * p.n_max + w.key0(lt) + lane;
           bulk_load(dst + lane * kDraftRow, kp.draft_k + row * kHeadDim, 2 * kHeadDim, bar);
           bulk_load(dst + kDraftV + lane * kDraftRow, kp.draft_v + row * kHeadDim, 2 * kHeadDim, bar);
         }
-      } else if (my_tile == lt - (window - ahead) && my_g0 < groups) {
-        if (p.paged) pid = valid_page_id(p, pid);
-        const int g = key0 / kKv4Tokens + my_g0, in_page = p.paged ? g % kp.groups_per_page : g;
-        const uint8_t* src =
-            kp.cache + ((static_cast<size_t>(pid) * p.hkv + w.h) * kp.groups_per_page + in_page) * kKv4Bytes;
-        bulk_load(dst + my_g0 * kKv4Bytes, src, min(kp.run_groups, groups - my_g0) * kKv4Bytes, bar);
+      } else if (my_tile == lt - (window - ahead) && bytes > 0) {
+        bulk_load(dst + my_g0 * kKv4Bytes, src, bytes, bar);
       }
       ++issued;
       if (++stage == CF::kStages) {
@@ -308,7 +339,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Smem& sm, 
       }
     }
   }
-  if (lane == 0) sm.misc[1] = issued;
+  if (lane == 0) *sm.issued = issued;
 }
 
 __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
@@ -331,19 +362,13 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
 
 // q of every piece as f16, rows of 64 dims in two halves (K-major B of QK^T, 128-byte swizzle).
 template <class CF>
-__device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& sm, Piece w) {
+__device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& sm, const Waiter& wait, Piece w) {
   const AttnParams& p = kp.a;
-  volatile int* abort = &sm.misc[0];
   const int lane = threadIdx.x & 31;
   wait_for_prerequisite_grid();
   for (int piece = 0; next_piece(p, sm.len, w); ++piece) {
     const int b = piece & 1;
-    bool ok = !*abort && mbar_wait(smem_addr(&sm.qempty[b]), ((piece >> 1) & 1) ^ 1u, p.err, p.wait_ns);
-    ok = __all_sync(0xffffffffu, ok);
-    if (!ok) {
-      *abort = 1;
-      return;
-    }
+    if (!__all_sync(0xffffffffu, wait(sm.qempty + 8 * b, ((piece >> 1) & 1) ^ 1u))) return;
     const __nv_bfloat16* q = p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim;
     const int row0 = w.rb * p.rows_per_unit, rows = min(p.rows_per_unit, p.rows_total - row0);
     const int ch = lane & 15;
@@ -359,7 +384,7 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& sm, Piece
     }
     fence_proxy_async_smem();
     __syncwarp();
-    if (lane == 0) mbar_arrive(smem_addr(&sm.qfull[b]));
+    if (lane == 0) mbar_arrive(sm.qfull + 8 * b);
   }
 }
 
@@ -410,74 +435,85 @@ __device__ __noinline__ void decode_draft(uint32_t src, bool live, uint32_t dst,
   }
 }
 
-// Warps 4..7 (K, into tensor memory) and 8..11 (V, into shared memory): a thread decodes one key.
-template <class CF, bool kV>
-__device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Piece w) {
+// A decoding warpgroup: the tiles t % 2 == wg, a key to a thread.
+template <class CF>
+__device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& sm, const Waiter& wait, uint32_t tmem, Piece w) {
   const AttnParams& p = kp.a;
-  volatile int* abort = &sm.misc[0];
-  const int lane = threadIdx.x & 31, key = threadIdx.x & 127;
-  const uint32_t group = (key >> 4) * kKv4Bytes;
-  const uint32_t src = sm.ring + group + (key & 15) * kChunkBytes + (kV ? kVCodes : 0);
-  const uint32_t ssrc = sm.ring + group + kScales + (kV ? kScaleBytes : 0) + (key & 15) * 8;
-  const uint32_t dsrc = sm.ring + key * kDraftRow + (kV ? kDraftV : 0);
-  const uint32_t dst = kV ? sm.v + key * 128 : tmem + (static_cast<uint32_t>(key & 96) << 16) + CF::kTmemK;
-  const uint32_t sw = static_cast<uint32_t>(key & 7) << 4;
-  int stage = 0, t = 0;
+  const int lane = threadIdx.x & 31, key = threadIdx.x & 127, wg = (threadIdx.x >> 7) & 1;
+  const uint32_t src0 = sm.ring + (key >> 4) * kKv4Bytes + (key & 15) * kChunkBytes;
+  const uint32_t scale0 = kScales + (key & 15) * 8 - (key & 15) * kChunkBytes;  // from there
+  const uint32_t draft0 = sm.ring + key * kDraftRow;
+  const uint32_t kdst = tmem + (static_cast<uint32_t>(key & 96) << 16) + CF::kTmemK + 64 * wg;
+  const uint32_t vdst = sm.v + wg * kVTile + key * 128, sw = static_cast<uint32_t>(key & 7) << 4;
+  int stage = wg, t = 0, mine = 0;  // the piece's first tile; this warpgroup's tiles so far
   uint32_t phase = 0;
-  while (next_piece(p, sm.len, w)) {
+  for (; next_piece(p, sm.len, w); t += w.lt1 - w.lt0) {
     // Keys that no row sees may hold anything; V of them must not be NaN (0 * NaN).
-    const int lo = kV && p.window > 0 ? w.L + p.min_depth - p.window : 0;
+    const int lo = p.window > 0 ? w.L + p.min_depth - p.window : 0;
 #pragma unroll 1
-    for (int lt = w.lt0; lt < w.lt1; ++lt, ++t) {
-      const int b = t & 1, key0 = w.key0(lt);
+    for (int lt = w.lt0 + ((t ^ wg) & 1); lt < w.lt1; lt += 2, ++mine) {
+      const int key0 = w.key0(lt);
       const bool draft = w.draft(lt);
       bool live = key < w.nkeys(lt, p.N);
-      if (kV && !draft) live = live && (key0 + key >= lo || key0 + key < p.sinks);
-      // The tile's bytes, and the buffer: its previous tile has been multiplied.
-      bool ok = !*abort && mbar_wait(smem_addr(&sm.cfull[stage]), phase, p.err, p.wait_ns);
-      if (t >= 2) ok = ok && mbar_wait(smem_addr(kV ? &sm.pvdone[b] : &sm.kempty[b]), ((t >> 1) & 1) ^ 1u, p.err, p.wait_ns);
-      if (!__all_sync(0xffffffffu, ok)) {
-        *abort = 1;
-        return;
-      }
-      if (!kV) tc_fence_after();
-      const uint32_t d = dst + b * (kV ? kVTile : 64), st = stage * kStageSize;
+      if (!draft) live = live && (key0 + key >= lo || key0 + key < p.sinks);
+      // The tile's bytes; K's buffer: QK^T of its previous tile is done.
+      bool ok = wait(sm.cfull + 8 * stage, phase);
+      ok = ok && wait(sm.qkdone + 8 * wg, (mine & 1) ^ 1u);
+      if (!__all_sync(0xffffffffu, ok)) return;
+      tc_fence_after();
+      const uint32_t src = src0 + stage * kStageSize;
+      uint2 ksc, vsc;
       if (!draft) {
-        uint2 sc = lds64(ssrc + st);
-        if (kV && !live) sc = make_uint2(0u, 0u);  // (any code times 0 is 0)
+        ksc = lds64(src + scale0);
+        vsc = lds64(src + scale0 + kScaleBytes);
+        if (!live) vsc = make_uint2(0u, 0u);  // (any code times 0 is 0)
 #pragma unroll 1
         for (int hf = 0; hf < 2; ++hf) {
-          const uint4 x0 = lds128(src + st + hf * 2 * kChunkStride), x1 = lds128(src + st + hf * 2 * kChunkStride + kChunkStride);
-          const uint32_t four = hf ? sc.y : sc.x;
+          const uint4 x0 = lds128(src + hf * 2 * kChunkStride), x1 = lds128(src + (hf * 2 + 1) * kChunkStride);
+          const uint32_t four = hf ? ksc.y : ksc.x;
           uint32_t o[32];
           const uint2 s0 = scale_pair(four), s1 = scale_pair(four >> 16);
           decode16(x0.x, x0.y, s0.x, o);
           decode16(x0.z, x0.w, s0.y, o + 8);
           decode16(x1.x, x1.y, s1.x, o + 16);
           decode16(x1.z, x1.w, s1.y, o + 24);
-          if constexpr (kV) {
-            put_v(d + hf * kVHalf, sw, 0, o);
-            put_v(d + hf * kVHalf, sw, 1, o + 16);
-          } else {
-            tmem_st32(d + 32 * hf, o);
-          }
+          tmem_st32(kdst + 32 * hf, o);
         }
       } else {
-        decode_draft<kV>(dsrc + st, live, d, sw);
+        decode_draft<false>(draft0 + stage * kStageSize, live, kdst, sw);
       }
-      if constexpr (kV) {
-        fence_proxy_async_smem();
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(sm.kfull + 8 * wg);
+      // V's buffer: P.V of its previous tile is done.
+      if (!__all_sync(0xffffffffu, wait(sm.pvdone + 8 * wg, (mine & 1) ^ 1u))) return;
+      if (!draft) {
+#pragma unroll 1
+        for (int hf = 0; hf < 2; ++hf) {
+          const uint4 x0 = lds128(src + kVCodes + hf * 2 * kChunkStride), x1 = lds128(src + kVCodes + (hf * 2 + 1) * kChunkStride);
+          const uint32_t four = hf ? vsc.y : vsc.x;
+          uint32_t o[32];
+          const uint2 s0 = scale_pair(four), s1 = scale_pair(four >> 16);
+          decode16(x0.x, x0.y, s0.x, o);
+          decode16(x0.z, x0.w, s0.y, o + 8);
+          decode16(x1.x, x1.y, s1.x, o + 16);
+          decode16(x1.z, x1.w, s1.y, o + 24);
+          put_v(vdst + hf * kVHalf, sw, 0, o);
+          put_v(vdst + hf * kVHalf, sw, 1, o + 16);
+        }
       } else {
-        tmem_wait_st();
-        tc_fence_before();
+        decode_draft<true>(draft0 + kDraftV + stage * kStageSize, live, vdst, sw);
       }
+      fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(smem_addr(&sm.cempty[stage]));
-        mbar_arrive(smem_addr(kV ? &sm.vfull[b] : &sm.kfull[b]));
+        mbar_arrive(sm.cempty + 8 * stage);
+        mbar_arrive(sm.vfull + 8 * wg);
       }
-      if (++stage == CF::kStages) {
-        stage = 0;
+      stage += 2;
+      if (stage >= CF::kStages) {
+        stage -= CF::kStages;
         phase ^= 1u;
       }
     }
@@ -487,76 +523,66 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& sm, 
 // ------------------------------------------------------------ MMA issue (one thread each)
 
 template <class CF>
-__device__ __forceinline__ void run_qk(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Piece w) {
+__device__ __forceinline__ void run_qk(const Kv4Params& kp, const Smem& sm, const Waiter& wait, uint32_t tmem, Piece w) {
   const AttnParams& p = kp.a;
-  volatile int* abort = &sm.misc[0];
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, false);
   bool ok = true;
   for (int piece = 0, t = 0; ok && next_piece(p, sm.len, w); ++piece) {
-    ok = mbar_wait(smem_addr(&sm.qfull[piece & 1]), (piece >> 1) & 1, p.err, p.wait_ns);
+    ok = wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1);
     const uint64_t q = smem_desc_sw128(sm.q + (piece & 1) * CF::kQTile, 16, 1024);
 #pragma unroll 1
     for (int lt = w.lt0; lt < w.lt1; ++lt, ++t) {
       const int b = t & 1;
-      ok = ok && !*abort;
-      if (t >= 2) ok = ok && mbar_wait(smem_addr(&sm.pfull[b]), ((t >> 1) & 1) ^ 1u, p.err, p.wait_ns);  // S has been read
-      ok = ok && mbar_wait(smem_addr(&sm.kfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
-      if (!ok) {
-        *abort = 1;
-        break;
-      }
+      ok = ok && wait(sm.pfull + 8 * b, ((t >> 1) & 1) ^ 1u);  // S of the tile before the last has been read
+      ok = ok && wait(sm.kfull + 8 * b, (t >> 1) & 1);
+      if (!ok) break;
       tc_fence_after();
 #pragma unroll
       for (int ks = 0; ks < kHeadDim / 16; ++ks)
         tc_mma_tmem_a(tmem + CF::kTmemS + b * CF::kNT, tmem + CF::kTmemK + 64 * b + 8 * ks,
                       q + (((ks >> 2) * (CF::kNT * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
-      tc_commit(smem_addr(&sm.sfull[b]));
-      tc_commit(smem_addr(&sm.kempty[b]));
+      tc_commit(sm.qkdone + 8 * b);
     }
-    if (ok) tc_commit(smem_addr(&sm.qempty[piece & 1]));
+    if (ok) tc_commit(sm.qempty + 8 * (piece & 1));
   }
-  tc_commit(smem_addr(&sm.mmadone[0]));
+  tc_commit(sm.mmadone);
 }
 
 template <class CF>
-__device__ __forceinline__ void run_pv(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Piece w) {
+__device__ __forceinline__ void run_pv(const Kv4Params& kp, const Smem& sm, const Waiter& wait, uint32_t tmem, Piece w) {
   const AttnParams& p = kp.a;
-  volatile int* abort = &sm.misc[0];
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, true, true);
   const uint64_t v0 = smem_desc_sw128(sm.v, kVHalf, 1024), p0 = smem_desc_sw128(sm.p, kPTile, 1024);
   bool ok = true;
   for (int piece = 0, t = 0; ok && next_piece(p, sm.len, w); ++piece) {
-    if (piece > 0) ok = mbar_wait(smem_addr(sm.ofree), (piece - 1) & 1, p.err, p.wait_ns);
+    if (piece > 0) ok = wait(sm.ofree, (piece - 1) & 1);
 #pragma unroll 1
     for (int lt = w.lt0; lt < w.lt1; ++lt, ++t) {
       const int b = t & 1;
-      ok = ok && !*abort && mbar_wait(smem_addr(&sm.vfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
-      ok = ok && mbar_wait(smem_addr(&sm.pfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
-      if (!ok) {
-        *abort = 1;
-        break;
-      }
+      ok = ok && wait(sm.vfull + 8 * b, (t >> 1) & 1) && wait(sm.pfull + 8 * b, (t >> 1) & 1);
+      if (!ok) break;
       tc_fence_after();
+      const uint32_t o = tmem + CF::kTmemO + (CF::kByTile ? b * CF::kNT : 0);
+      const bool more = lt - w.lt0 >= CF::kAccs;  // the accumulator holds tiles of this piece
 #pragma unroll
       for (int k16 = 0; k16 < kTile / 16; ++k16)  // two 8-key groups of 1 KB each
-        tc_mma(tmem + CF::kTmemO, v0 + ((b * kVTile + k16 * 2048) >> 4), p0 + ((b * kPTile + k16 * 2048) >> 4), idesc,
-               lt > w.lt0 || k16 > 0);
-      tc_commit(smem_addr(&sm.pvdone[b]));
+        tc_mma(o, v0 + ((b * kVTile + k16 * 2048) >> 4), p0 + ((b * kPTile + k16 * 2048) >> 4), idesc, more || k16 > 0);
+      tc_commit(sm.pvdone + 8 * b);
     }
   }
-  tc_commit(smem_addr(&sm.mmadone[1]));
+  tc_commit(sm.mmadone + 8);
 }
 
 // ------------------------------------------------------------ softmax and epilogue
 
-// Whether `x` holds for any of the softmax threads (all of which call it): a barrier with a reduction.
-__device__ __forceinline__ bool any_softmax(bool x) {
+// Whether `x` holds for any of the `threads` threads of a named barrier (all of which call it).
+__device__ __forceinline__ bool any_of(int bar, int threads, bool x) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
       "barrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"(static_cast<uint32_t>(x)), "n"(kBarSoftmax), "n"(kSoftmaxThreads)
+      : "r"(static_cast<uint32_t>(x)), "r"(bar), "r"(threads)
       : "memory");
   return r != 0;
 }
@@ -625,28 +651,29 @@ __device__ __noinline__ void load_rows(const AttnParams& p, const Smem& sm, int 
   }
 }
 
-// Bit j: row j sees this thread's key.  `at`: token position or draft slot of the key, which is valid.
-__device__ __noinline__ uint64_t visible_rows(const AttnParams& p, const Smem& sm, int nc, bool draft, int at, int L) {
+// Bit j: row j0 + j sees this thread's key.  `at`: token position or draft slot of the key, which is valid.
+__device__ __noinline__ uint64_t visible_rows(const AttnParams& p, const Smem& sm, int j0, int n, bool draft, int at, int L) {
   uint64_t bits = 0;
   const int key_depth = !draft ? 0 : p.tree ? __popcll(sm.anc[at]) : at + 1;
   const int pos = draft ? L + key_depth - 1 : at;
   const bool always = p.window == 0 || pos < p.sinks;
 #pragma unroll 1
-  for (int j = 0; j < nc; ++j) {
-    const int d = sm.depth[j];
+  for (int j = 0; j < n; ++j) {
+    const int d = sm.depth[j0 + j];
     bool v = always || L + d - 1 - pos < p.window;
-    if (draft) v = v && (p.tree ? (sm.row_anc[j] >> at) & 1ull : at < d);
+    if (draft) v = v && (p.tree ? (sm.row_anc[j0 + j] >> at) & 1ull : at < d);
     bits |= static_cast<uint64_t>(v) << j;
   }
   return bits;
 }
 
-// The references of rows whose scores have passed their limit move: sm.ref, and sm.alpha with what O and the sums are
-// to be multiplied by.  All softmax threads.
-__device__ __noinline__ void move_references(const Smem& sm, int nc, uint32_t scores, float qs, uint64_t vis) {
-  const int tid = threadIdx.x, warp = tid >> 5;
+// The references of rows whose scores have passed their limit move: ref, and alpha with what O and the sums are to be
+// multiplied by.  The threads of warpgroup wg; n rows from the first of `scores`, `ref` and `alpha` on.
+__device__ __noinline__ void move_references(int* wmax, float* refs, float* alpha, int wg, int n, uint32_t scores, float qs,
+                                             uint64_t vis) {
+  const int tid = threadIdx.x & 127, warp = tid >> 5;
 #pragma unroll 1
-  for (int j = 0; j < nc; j += 8) {
+  for (int j = 0; j < n; j += 8) {
     uint32_t s[8];
     tmem_ld8(scores + j, s);
     tmem_wait_ld();
@@ -654,77 +681,117 @@ __device__ __noinline__ void move_references(const Smem& sm, int nc, uint32_t sc
     for (int i = 0; i < 8; ++i) {
       const float x = (vis >> (j + i)) & 1ull ? __uint_as_float(s[i]) * qs : -INFINITY;
       const int m = __reduce_max_sync(0xffffffffu, ordered(x));
-      if ((tid & 31) == 0) sm.wmax[warp * 64 + j + i] = m;
+      if ((tid & 31) == 0) wmax[warp * 64 + j + i] = m;
     }
   }
-  named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-  if (tid < nc) {
-    const float m = unordered(max(max(sm.wmax[tid], sm.wmax[64 + tid]), max(sm.wmax[128 + tid], sm.wmax[192 + tid])));
-    const float old = sm.ref[tid], ref = m - old > kRefLimit ? m - kRefBelow : old;
-    sm.ref[tid] = ref;
-    sm.alpha[tid] = ex2(old - ref);
+  named_barrier_sync(kBarGroup + wg, kGroupThreads);
+  if (tid < n) {
+    const float m = unordered(max(max(wmax[tid], wmax[64 + tid]), max(wmax[128 + tid], wmax[192 + tid])));
+    const float old = refs[tid], ref = m - old > kRefLimit ? m - kRefBelow : old;
+    refs[tid] = ref;
+    alpha[tid] = ex2(old - ref);
   }
-  named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
+  named_barrier_sync(kBarGroup + wg, kGroupThreads);
 }
 
-// O of this thread's dim, row by row, times sm.alpha and vs.
-__device__ __noinline__ void rescale_o(const Smem& sm, int nc, uint32_t o_cols, float vs) {
+// n rows of O of this thread's dim times alpha and vs.
+__device__ __noinline__ void rescale_o(const float* alpha, int n, uint32_t o_cols, float vs) {
 #pragma unroll 1
-  for (int j = 0; j < nc; j += 8) {
+  for (int j = 0; j < n; j += 8) {
     uint32_t o[8];
     tmem_ld8(o_cols + j, o);
     tmem_wait_ld();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * (sm.alpha[j + i] * vs));
+    for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * (alpha[j + i] * vs));
     tmem_st8(o_cols + j, o);
   }
   tmem_wait_st();
 }
 
-// A piece's output rows: the final ones, or the piece's part in the workspace.  Thread = dim.
-__device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, const Piece& w, int nc, uint32_t o_cols) {
-  const int tid = threadIdx.x;
+// A piece's rows [j0, j1) of this thread's dim: the final ones, or the piece's part in the workspace.  kAccs 2: O and the
+// other accumulator `next` columns on, each with its own weights (0: it holds nothing).
+template <int kAccs>
+__device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, const Piece& w, int j0, int j1, uint32_t o_cols,
+                                        int next) {
+  const int tid = threadIdx.x & 127;
   const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
   const size_t row0 = static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G;
   const size_t part = static_cast<size_t>(w.c * p.hkv * p.row_blocks + w.hr + blockIdx.x) * p.rows_per_unit;
   const bool whole = w.whole();
-  if (tid < rows) {
-    const float sum = sm.sum[tid], lse2 = sum == 0.f ? -INFINITY : sm.ref[tid] + __log2f(sum);
-    if (whole) p.lse[row0 + sm.place[tid]] = lse2 * 0.69314718055994531f;
-    else p.ws_lse[part + tid] = lse2;
-  }
 #pragma unroll 1
-  for (int j = 0; j < nc; j += 8) {
-    uint32_t o[8];
-    tmem_ld8(o_cols + j, o);
+  for (int j = j0; j < j1; j += 4) {
+    uint32_t o[4], o2[4];
+    tmem_ld4(o_cols + j, o);
+    if (kAccs == 2) tmem_ld4(o_cols + next + j, o2);
     tmem_wait_ld();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       if (j + i >= rows) break;
-      const float v = __uint_as_float(o[i]) * sm.inv[j + i];
+      const float a = sm.inv[j + i];
+      float v = a != 0.f ? __uint_as_float(o[i]) * a : 0.f;
+      if (kAccs == 2) {
+        const float a2 = sm.inv[64 + j + i];
+        v += a2 != 0.f ? __uint_as_float(o2[i]) * a2 : 0.f;
+      }
       if (whole) p.out[(row0 + sm.place[j + i]) * kHeadDim + tid] = __float2bfloat16(v);
       else p.ws_o[(part + j + i) * kHeadDim + tid] = v;
     }
   }
 }
 
+// The rows' sums, weights of the accumulators and log-sum-exp.  Thread = row.  had: whether each accumulator holds tiles
+// of this piece.
 template <class CF>
-__device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm, uint32_t tmem, Piece w) {
-  constexpr int NC = CF::kNC;
+__device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, const Piece& w, int j, bool had0, bool had1) {
+  const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
+  auto total = [&](int wg, int col) {
+    const int* x = sm.wmax + wg * 256 + col;
+    return (__int_as_float(x[0]) + __int_as_float(x[64])) + (__int_as_float(x[128]) + __int_as_float(x[192]));
+  };
+  float sum, top;
+  if constexpr (CF::kByTile) {
+    const float r0 = had0 ? sm.ref[j] : kNoRef, r1 = had1 ? sm.ref[64 + j] : kNoRef;
+    top = fmaxf(r0, r1);
+    const float w0 = had0 ? ex2(r0 - top) : 0.f, w1 = had1 ? ex2(r1 - top) : 0.f;
+    sum = (had0 ? w0 * total(0, j) : 0.f) + (had1 ? w1 * total(1, j) : 0.f);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    sm.inv[j] = w0 * inv * (sm.codes[0] ? p.v_scale : 1.f);
+    sm.inv[64 + j] = w1 * inv * (sm.codes[1] ? p.v_scale : 1.f);
+  } else {
+    const int wg = j >= CF::kCols;
+    top = sm.ref[j];
+    sum = total(wg, j - wg * CF::kCols);
+    sm.inv[j] = sum == 0.f ? 0.f : (sm.codes[0] ? p.v_scale : 1.f) / sum;
+  }
+  if (j >= rows) return;
+  const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
+  if (w.whole()) p.lse[static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G + sm.place[j]] = lse2 * 0.69314718055994531f;
+  else p.ws_lse[static_cast<size_t>(w.c * p.hkv * p.row_blocks + w.hr + blockIdx.x) * p.rows_per_unit + j] = lse2;
+}
+
+template <class CF>
+__device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm, const Waiter& wait, uint32_t tmem, Piece w) {
+  constexpr int NC = CF::kCols;
   const AttnParams& p = kp.a;
-  volatile int* abort = &sm.misc[0];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t trow = tmem + (static_cast<uint32_t>(tid & 96) << 16);
-  const uint32_t pdst = sm.p + tid * 128, sw = static_cast<uint32_t>(tid & 7) << 4;
-  int unit_rb = -1, unit_seq = -1, t = 0;
+  const int lane = threadIdx.x & 31, key = threadIdx.x & 127, wg = threadIdx.x >> 7;
+  const int col0 = CF::kByTile ? 0 : wg * NC;  // this thread's first row
+  const uint32_t trow = tmem + (static_cast<uint32_t>(key & 96) << 16);
+  const uint32_t o_cols = trow + CF::kTmemO + (CF::kByTile ? wg * CF::kNT : col0);
+  const uint32_t pdst = sm.p + key * 128, sw = static_cast<uint32_t>(key & 7) << 4;
+  float* ref = sm.ref + (CF::kByTile ? 64 * wg : col0);
+  float* alpha = sm.alpha + (CF::kByTile ? 64 * wg : col0);
+  int* wmax = sm.wmax + 256 * wg;
+  const int bar = kBarGroup + wg;
+  int unit_rb = -1, unit_seq = -1, t0 = 0;
+  bool dead = false;  // this warpgroup has given up: it only keeps up the barriers of both
   wait_for_prerequisite_grid();  // outputs and scratch may be the preceding kernel's
-  while (next_piece(p, sm.len, w)) {
+  for (; next_piece(p, sm.len, w); t0 += w.lt1 - w.lt0) {
     if (w.rb != unit_rb || (p.tree && w.seq != unit_seq)) {
-      load_rows(p, sm, NC, w.rb, w.seq, p.tree && w.seq != unit_seq);
+      load_rows(p, sm, CF::kNC, w.rb, w.seq, p.tree && w.seq != unit_seq);
       unit_rb = w.rb;
       unit_seq = w.seq;
     }
-    if (tid < NC) sm.ref[tid] = kNoRef;
+    if (key < NC) ref[key] = kNoRef;
     named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
     float l[NC];  // sums over this thread's keys
 #pragma unroll
@@ -734,22 +801,25 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm,
     if (p.window > 0) {
       int dmax = 0;
 #pragma unroll 1
-      for (int j = 0; j < NC; ++j) dmax = max(dmax, sm.depth[j]);
+      for (int j = 0; j < CF::kNC; ++j) dmax = max(dmax, sm.depth[j]);
       seen_from = w.L + dmax - p.window;
     }
-    bool in_codes = !w.draft(w.lt0);  // O is in units of the value codes
+    const int lt_first = w.lt0 + (CF::kByTile ? (t0 ^ wg) & 1 : 0);
+    bool in_codes = !w.draft(lt_first);  // O is in units of the value codes
+    int t = t0 + lt_first - w.lt0;
 #pragma unroll 1
-    for (int lt = w.lt0; lt < w.lt1; ++lt, ++t) {
+    for (int lt = lt_first; lt < w.lt1 && !dead; lt += CF::kAccs, t += CF::kAccs) {
       const int b = t & 1, key0 = w.key0(lt), nkeys = w.nkeys(lt, p.N);
       const bool draft = w.draft(lt);
       const float qs = draft ? p.qscale : p.qscale * p.k_scale;
       uint64_t vis = ~0ull;
       if (draft || nkeys < kTile || (key0 < seen_from && key0 + kTile > p.sinks))
-        vis = tid < nkeys ? visible_rows(p, sm, NC, draft, key0 + tid, w.L) : 0ull;
-      bool ok = !*abort && mbar_wait(smem_addr(&sm.sfull[b]), (t >> 1) & 1, p.err, p.wait_ns);
+        vis = key < nkeys ? visible_rows(p, sm, col0, NC, draft, key0 + key, w.L) : 0ull;
+      // S; and the buffer of P, free when P.V of the tile before the last is done (by tile: O is at rest then, too).
+      bool ok = wait(sm.qkdone + 8 * b, (t >> 1) & 1) && wait(sm.pvdone + 8 * b, ((t >> 1) & 1) ^ 1u);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
-      const uint32_t scores = trow + CF::kTmemS + b * CF::kNT;
+      const uint32_t scores = trow + CF::kTmemS + b * CF::kNT + col0;
       const bool leave_codes = draft && in_codes && p.v_scale != 1.f;
       if (draft) in_codes = false;
       float x[NC];
@@ -760,7 +830,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm,
           tmem_wait_ld();
 #pragma unroll
           for (int j = 0; j < NC; j += 4) {
-            const float4 m = *reinterpret_cast<const float4*>(sm.ref + j);
+            const float4 m = *reinterpret_cast<const float4*>(ref + j);
             x[j] = fmaf(__uint_as_float(s[j]), qs, -m.x);
             x[j + 1] = fmaf(__uint_as_float(s[j + 1]), qs, -m.y);
             x[j + 2] = fmaf(__uint_as_float(s[j + 2]), qs, -m.z);
@@ -775,27 +845,22 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm,
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < NC; ++j) top = fmaxf(top, x[j]);
-        if (!any_softmax(top > kRefLimit || leave_codes || !ok)) break;
-        if (any_softmax(!ok)) {
-          *abort = 1;
-          return;
-        }
-        move_references(sm, NC, scores, qs, vis);  // always with a piece's first keys
+        if (!any_of(bar, kGroupThreads, top > kRefLimit || leave_codes || !ok)) break;
+        dead = any_of(bar, kGroupThreads, !ok);
+        if (dead) break;
+        move_references(wmax, ref, alpha, wg, NC, scores, qs, vis);  // always with a warpgroup's first keys of a piece
 #pragma unroll
-        for (int j = 0; j < NC; ++j) l[j] *= sm.alpha[j];
-        if (lt > w.lt0) {
-          ok = mbar_wait(smem_addr(&sm.pvdone[b ^ 1]), ((t - 1) >> 1) & 1, p.err, p.wait_ns);
-          if (any_softmax(!ok)) {
-            *abort = 1;
-            return;
+        for (int j = 0; j < NC; ++j) l[j] *= alpha[j];
+        if (lt > lt_first) {
+          if constexpr (!CF::kByTile) {
+            dead = any_of(bar, kGroupThreads, !wait(sm.pvdone + 8 * (b ^ 1), ((t - 1) >> 1) & 1));
+            if (dead) break;
+            tc_fence_after();
           }
-          tc_fence_after();
-          rescale_o(sm, NC, trow + CF::kTmemO, leave_codes ? p.v_scale : 1.f);
+          rescale_o(alpha, NC, o_cols, leave_codes ? p.v_scale : 1.f);
         }
       }
-      // P's buffer is free when P.V of the tile before the last is done.
-      ok = t < 2 || mbar_wait(smem_addr(&sm.pvdone[b]), ((t >> 1) & 1) ^ 1u, p.err, p.wait_ns);
-      ok = __all_sync(0xffffffffu, ok);
+      if (dead) break;
 #pragma unroll
       for (int j = 0; j < NC; j += 8) {
         float e[8];
@@ -804,40 +869,34 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm,
           e[i] = ex2(x[j + i]);
           l[j + i] += e[i];
         }
-        if (ok)
-          sts128(pdst + b * kPTile + ((static_cast<uint32_t>(j) << 1) ^ sw),
-                 make_uint4(pack_f16x2(e[0], e[1]), pack_f16x2(e[2], e[3]), pack_f16x2(e[4], e[5]), pack_f16x2(e[6], e[7])));
+        sts128(pdst + b * kPTile + ((static_cast<uint32_t>(col0 + j) << 1) ^ sw),
+               make_uint4(pack_f16x2(e[0], e[1]), pack_f16x2(e[2], e[3]), pack_f16x2(e[4], e[5]), pack_f16x2(e[6], e[7])));
       }
       fence_proxy_async_smem();
       tc_fence_before();
       __syncwarp();
-      if (!ok) *abort = 1;  // (the next vote takes every softmax thread out)
-      else if (lane == 0) mbar_arrive(smem_addr(&sm.pfull[b]));
+      if (lane == 0) mbar_arrive(sm.pfull + 8 * b);
     }
     // Sums over the keys' threads, then the rows.
     int col = 0;
     const int width = column_sums(l, lane, &col);
 #pragma unroll
     for (int i = 0; i < NC; ++i)
-      if (i < width) sm.wmax[warp * 64 + col + i] = __float_as_int(l[i]);
-    const int tl = t - 1;
-    const bool ok = !*abort && mbar_wait(smem_addr(&sm.pvdone[tl & 1]), (tl >> 1) & 1, p.err, p.wait_ns);
-    if (any_softmax(!ok)) {
-      *abort = 1;
-      return;
+      if (i < width) wmax[(key >> 5) * 64 + col + i] = __float_as_int(l[i]);
+    if (key == 0) sm.codes[wg] = in_codes;
+    if (!dead && lt_first < w.lt1) {  // O is at rest
+      const int last = t - CF::kAccs;
+      dead = !wait(sm.pvdone + 8 * (last & 1), (last >> 1) & 1);
     }
-    if (tid < NC) {
-      const float sum = (__int_as_float(sm.wmax[tid]) + __int_as_float(sm.wmax[64 + tid])) +
-                        (__int_as_float(sm.wmax[128 + tid]) + __int_as_float(sm.wmax[192 + tid]));
-      sm.sum[tid] = sum;
-      sm.inv[tid] = sum == 0.f ? 0.f : (in_codes ? p.v_scale : 1.f) / sum;
-    }
+    if (any_of(kBarSoftmax, kSoftmaxThreads, dead)) return;
+    const bool two = w.lt1 - w.lt0 > 1;
+    if (threadIdx.x < CF::kNC) join_sums<CF>(p, sm, w, threadIdx.x, two || !(t0 & 1), two || (t0 & 1));
     named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
     tc_fence_after();
-    write_rows(p, sm, w, NC, trow + CF::kTmemO);
+    write_rows<CF::kAccs>(p, sm, w, wg * (CF::kNC / 2), (wg + 1) * (CF::kNC / 2), trow + CF::kTmemO, CF::kNT);
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) mbar_arrive(smem_addr(sm.ofree));
+    if (lane == 0) mbar_arrive(sm.ofree);
   }
 }
 
@@ -850,22 +909,22 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < CF::kStages; ++s) {
-      mbar_init(smem_addr(&sm.cfull[s]), 1);
-      mbar_init(smem_addr(&sm.cempty[s]), 8);
+      mbar_init(sm.cfull + 8 * s, 1);
+      mbar_init(sm.cempty + 8 * s, 4);
     }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(smem_addr(&sm.kfull[b]), 4);
-      mbar_init(smem_addr(&sm.kempty[b]), 1);
-      mbar_init(smem_addr(&sm.vfull[b]), 4);
-      mbar_init(smem_addr(&sm.sfull[b]), 1);
-      mbar_init(smem_addr(&sm.pfull[b]), 4);
-      mbar_init(smem_addr(&sm.pvdone[b]), 1);
-      mbar_init(smem_addr(&sm.qfull[b]), 1);
-      mbar_init(smem_addr(&sm.qempty[b]), 1);
-      mbar_init(smem_addr(&sm.mmadone[b]), 1);
+      mbar_init(sm.kfull + 8 * b, 4);
+      mbar_init(sm.vfull + 8 * b, 4);
+      mbar_init(sm.qkdone + 8 * b, 1);
+      mbar_init(sm.pfull + 8 * b, CF::kByTile ? 4 : 8);
+      mbar_init(sm.pvdone + 8 * b, 1);
+      mbar_init(sm.qfull + 8 * b, 1);
+      mbar_init(sm.qempty + 8 * b, 1);
+      mbar_init(sm.mmadone + 8 * b, 1);
     }
-    mbar_init(smem_addr(sm.ofree), 4);
-    sm.misc[0] = sm.misc[1] = 0;
+    mbar_init(sm.ofree, 8);
+    *sm.abort = 0;
+    *sm.issued = 0;
     fence_mbar_init();
   }
   if (warp == kWarpQk) {
@@ -876,24 +935,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   build_kv4_plan(p, sm.len, sm.base);  // (barriers inside)
   tc_fence_after();
   const uint32_t tmem = *sm.tmem;
+  const Waiter wait{p.err, p.wait_ns, sm.abort};
   Piece w;
   begin_pieces(p, sm.len, sm.base, w);
-  if (warp < kWarpK) run_softmax<CF>(kp, sm, tmem, w);
-  else if (warp < kWarpV) run_decode<CF, false>(kp, sm, tmem, w);
-  else if (warp < kWarpLoad) run_decode<CF, true>(kp, sm, tmem, w);
-  else if (warp == kWarpLoad) run_loader<CF>(kp, sm, w);
-  else if (warp == kWarpQk && lane == 0) run_qk<CF>(kp, sm, tmem, w);
-  else if (warp == kWarpPv && lane == 0) run_pv<CF>(kp, sm, tmem, w);
-  else if (warp == kWarpQ) run_q<CF>(kp, sm, w);
+  if (warp < kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem, w);
+  else if (warp < kWarpLoad) run_decode<CF>(kp, sm, wait, tmem, w);
+  else if (warp == kWarpLoad) run_loader<CF>(kp, sm, wait, w);
+  else if (warp == kWarpQk && lane == 0) run_qk<CF>(kp, sm, wait, tmem, w);
+  else if (warp == kWarpPv && lane == 0) run_pv<CF>(kp, sm, wait, tmem, w);
+  else if (warp == kWarpQ) run_q<CF>(kp, sm, wait, w);
   __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0) {
     // No copy or MMA outlives the CTA, whatever ended it (each wait is bounded).
-    for (int k = max(0, sm.misc[1] - CF::kStages); k < sm.misc[1]; ++k)
-      if (!mbar_wait(smem_addr(&sm.cfull[k % CF::kStages]), (k / CF::kStages) & 1, p.err)) break;
-    mbar_wait(smem_addr(&sm.mmadone[0]), 0, p.err);
-    mbar_wait(smem_addr(&sm.mmadone[1]), 0, p.err);
+    for (int k = max(0, *sm.issued - CF::kStages); k < *sm.issued; ++k)
+      if (!mbar_wait(sm.cfull + 8 * (k % CF::kStages), (k / CF::kStages) & 1, p.err)) break;
+    mbar_wait(sm.mmadone, 0, p.err);
+    mbar_wait(sm.mmadone + 8, 0, p.err);
   }
   __syncthreads();
   tc_fence_after();
