@@ -272,6 +272,9 @@ __device__ __noinline__ bool next_piece(const AttnParams& p, const int* s_len, P
 
 // ------------------------------------------------------------ loads
 
+// The roles keep copies of their own of what they also hand to functions out of line: a variable whose address has been
+// given away is read from local memory again after every barrier and copy.
+
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
@@ -279,8 +282,9 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 }
 
 template <class CF>
-__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Smem& sm, const Waiter& wait, Piece w) {
+__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Smem& smem, const Waiter& wait, Piece next) {
   const AttnParams& p = kp.a;
+  const Smem sm = smem;
   const int lane = threadIdx.x & 31;
   int stage = 0, issued = 0;
   uint32_t phase = 0;
@@ -289,7 +293,8 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Smem& sm, 
   // i / runs, and issues that copy.
   const int runs = kTileGroups / kp.run_groups, ahead = 32 / runs;
   const int my_tile = lane / runs, my_g0 = (lane % runs) * kp.run_groups;
-  while (ok && next_piece(p, sm.len, w)) {
+  while (ok && next_piece(p, sm.len, next)) {
+    const Piece w = next;
     const int32_t* table = p.page_table + (p.paged ? static_cast<size_t>(w.c) * p.max_pages : 0);
     auto group_of = [&](int lt) {  // this lane's first group of the window from tile lt on, or -1
       lt += my_tile;
@@ -362,11 +367,13 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
 
 // q of every piece as f16, rows of 64 dims in two halves (K-major B of QK^T, 128-byte swizzle).
 template <class CF>
-__device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& sm, const Waiter& wait, Piece w) {
+__device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, const Waiter& wait, Piece next) {
   const AttnParams& p = kp.a;
+  const Smem sm = smem;
   const int lane = threadIdx.x & 31;
   wait_for_prerequisite_grid();
-  for (int piece = 0; next_piece(p, sm.len, w); ++piece) {
+  for (int piece = 0; next_piece(p, sm.len, next); ++piece) {
+    const Piece w = next;
     const int b = piece & 1;
     if (!__all_sync(0xffffffffu, wait(sm.qempty + 8 * b, ((piece >> 1) & 1) ^ 1u))) return;
     const __nv_bfloat16* q = p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim;
@@ -437,8 +444,9 @@ __device__ __noinline__ void decode_draft(uint32_t src, bool live, uint32_t dst,
 
 // A decoding warpgroup: the tiles t % 2 == wg, a key to a thread.
 template <class CF>
-__device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& sm, const Waiter& wait, uint32_t tmem, Piece w) {
+__device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem, Piece next) {
   const AttnParams& p = kp.a;
+  const Smem sm = smem;
   const int lane = threadIdx.x & 31, key = threadIdx.x & 127, wg = (threadIdx.x >> 7) & 1;
   const uint32_t src0 = sm.ring + (key >> 4) * kKv4Bytes + (key & 15) * kChunkBytes;
   const uint32_t scale0 = kScales + (key & 15) * 8 - (key & 15) * kChunkBytes;  // from there
@@ -447,7 +455,8 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& sm, 
   const uint32_t vdst = sm.v + wg * kVTile + key * 128, sw = static_cast<uint32_t>(key & 7) << 4;
   int stage = wg, t = 0, mine = 0;  // the piece's first tile; this warpgroup's tiles so far
   uint32_t phase = 0;
-  for (; next_piece(p, sm.len, w); t += w.lt1 - w.lt0) {
+  for (; next_piece(p, sm.len, next); t += next.lt1 - next.lt0) {
+    const Piece w = next;
     // Keys that no row sees may hold anything; V of them must not be NaN (0 * NaN).
     const int lo = p.window > 0 ? w.L + p.min_depth - p.window : 0;
 #pragma unroll 1
@@ -520,57 +529,73 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& sm, 
   }
 }
 
-// ------------------------------------------------------------ MMA issue (one thread each)
+// ------------------------------------------------------------ MMA issue (one warp each)
+
+// A value that is the same in every lane, known to be so.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sync(0xffffffffu, x); }
 
 template <class CF>
-__device__ __forceinline__ void run_qk(const Kv4Params& kp, const Smem& sm, const Waiter& wait, uint32_t tmem, Piece w) {
+__device__ __forceinline__ void run_qk(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem_base, Piece next) {
   const AttnParams& p = kp.a;
+  const Smem sm = smem;
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, false);
+  const uint32_t tmem = uniform(tmem_base);
   bool ok = true;
-  for (int piece = 0, t = 0; ok && next_piece(p, sm.len, w); ++piece) {
-    ok = wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1);
+  int t = 0;
+  for (int piece = 0; __all_sync(0xffffffffu, ok && next_piece(p, sm.len, next)); ++piece) {
+    const int tiles = uniform(next.lt1 - next.lt0);
+    ok = __all_sync(0xffffffffu, wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1));
+    if (!ok) break;
     const uint64_t q = smem_desc_sw128(sm.q + (piece & 1) * CF::kQTile, 16, 1024);
 #pragma unroll 1
-    for (int lt = w.lt0; lt < w.lt1; ++lt, ++t) {
+    for (int i = 0; i < tiles; ++i, ++t) {
       const int b = t & 1;
-      ok = ok && wait(sm.pfull + 8 * b, ((t >> 1) & 1) ^ 1u);  // S of the tile before the last has been read
-      ok = ok && wait(sm.kfull + 8 * b, (t >> 1) & 1);
+      ok = wait(sm.pfull + 8 * b, ((t >> 1) & 1) ^ 1u);  // S of the tile before the last has been read
+      ok = __all_sync(0xffffffffu, ok && wait(sm.kfull + 8 * b, (t >> 1) & 1));
       if (!ok) break;
       tc_fence_after();
 #pragma unroll
       for (int ks = 0; ks < kHeadDim / 16; ++ks)
-        tc_mma_tmem_a(tmem + CF::kTmemS + b * CF::kNT, tmem + CF::kTmemK + 64 * b + 8 * ks,
-                      q + (((ks >> 2) * (CF::kNT * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
-      tc_commit(sm.qkdone + 8 * b);
+        tc_mma_tmem_a_elect(tmem + CF::kTmemS + b * CF::kNT, tmem + CF::kTmemK + 64 * b + 8 * ks,
+                            q + (((ks >> 2) * (CF::kNT * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
+      tc_commit_elect(sm.qkdone + 8 * b);
     }
-    if (ok) tc_commit(sm.qempty + 8 * (piece & 1));
+    if (!ok) break;
+    tc_commit_elect(sm.qempty + 8 * (piece & 1));
   }
-  tc_commit(sm.mmadone);
+  tc_commit_elect(sm.mmadone);
 }
 
 template <class CF>
-__device__ __forceinline__ void run_pv(const Kv4Params& kp, const Smem& sm, const Waiter& wait, uint32_t tmem, Piece w) {
+__device__ __forceinline__ void run_pv(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem_base, Piece next) {
   const AttnParams& p = kp.a;
+  const Smem sm = smem;
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, true, true);
+  const uint32_t tmem = uniform(tmem_base);
   const uint64_t v0 = smem_desc_sw128(sm.v, kVHalf, 1024), p0 = smem_desc_sw128(sm.p, kPTile, 1024);
   bool ok = true;
-  for (int piece = 0, t = 0; ok && next_piece(p, sm.len, w); ++piece) {
-    if (piece > 0) ok = wait(sm.ofree, (piece - 1) & 1);
+  int t = 0;
+  for (int piece = 0; __all_sync(0xffffffffu, ok && next_piece(p, sm.len, next)); ++piece) {
+    const int tiles = uniform(next.lt1 - next.lt0);
+    if (piece > 0) ok = __all_sync(0xffffffffu, wait(sm.ofree, (piece - 1) & 1));
+    if (!ok) break;
 #pragma unroll 1
-    for (int lt = w.lt0; lt < w.lt1; ++lt, ++t) {
+    for (int i = 0; i < tiles; ++i, ++t) {
       const int b = t & 1;
-      ok = ok && wait(sm.vfull + 8 * b, (t >> 1) & 1) && wait(sm.pfull + 8 * b, (t >> 1) & 1);
+      ok = wait(sm.vfull + 8 * b, (t >> 1) & 1);
+      ok = __all_sync(0xffffffffu, ok && wait(sm.pfull + 8 * b, (t >> 1) & 1));
       if (!ok) break;
       tc_fence_after();
       const uint32_t o = tmem + CF::kTmemO + (CF::kByTile ? b * CF::kNT : 0);
-      const bool more = lt - w.lt0 >= CF::kAccs;  // the accumulator holds tiles of this piece
+      const uint32_t more = i >= CF::kAccs;  // the accumulator holds tiles of this piece
 #pragma unroll
       for (int k16 = 0; k16 < kTile / 16; ++k16)  // two 8-key groups of 1 KB each
-        tc_mma(o, v0 + ((b * kVTile + k16 * 2048) >> 4), p0 + ((b * kPTile + k16 * 2048) >> 4), idesc, more || k16 > 0);
-      tc_commit(sm.pvdone + 8 * b);
+        tc_mma_elect(o, v0 + ((b * kVTile + k16 * 2048) >> 4), p0 + ((b * kPTile + k16 * 2048) >> 4), idesc,
+                     k16 > 0 ? 1u : more);
+      tc_commit_elect(sm.pvdone + 8 * b);
     }
   }
-  tc_commit(sm.mmadone + 8);
+  tc_commit_elect(sm.mmadone + 8);
 }
 
 // ------------------------------------------------------------ softmax and epilogue
@@ -770,9 +795,10 @@ __device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, cons
 }
 
 template <class CF>
-__device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm, const Waiter& wait, uint32_t tmem, Piece w) {
+__device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem, Piece next) {
   constexpr int NC = CF::kCols;
   const AttnParams& p = kp.a;
+  const Smem sm = smem;
   const int lane = threadIdx.x & 31, key = threadIdx.x & 127, wg = threadIdx.x >> 7;
   const int col0 = CF::kByTile ? 0 : wg * NC;  // this thread's first row
   const uint32_t trow = tmem + (static_cast<uint32_t>(key & 96) << 16);
@@ -785,9 +811,10 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm,
   int unit_rb = -1, unit_seq = -1, t0 = 0;
   bool dead = false;  // this warpgroup has given up: it only keeps up the barriers of both
   wait_for_prerequisite_grid();  // outputs and scratch may be the preceding kernel's
-  for (; next_piece(p, sm.len, w); t0 += w.lt1 - w.lt0) {
+  for (; next_piece(p, sm.len, next); t0 += next.lt1 - next.lt0) {
+    const Piece w = next;
     if (w.rb != unit_rb || (p.tree && w.seq != unit_seq)) {
-      load_rows(p, sm, CF::kNC, w.rb, w.seq, p.tree && w.seq != unit_seq);
+      load_rows(p, smem, CF::kNC, w.rb, w.seq, p.tree && w.seq != unit_seq);
       unit_rb = w.rb;
       unit_seq = w.seq;
     }
@@ -814,7 +841,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm,
       const float qs = draft ? p.qscale : p.qscale * p.k_scale;
       uint64_t vis = ~0ull;
       if (draft || nkeys < kTile || (key0 < seen_from && key0 + kTile > p.sinks))
-        vis = key < nkeys ? visible_rows(p, sm, col0, NC, draft, key0 + key, w.L) : 0ull;
+        vis = key < nkeys ? visible_rows(p, smem, col0, NC, draft, key0 + key, w.L) : 0ull;
       // S; and the buffer of P, free when P.V of the tile before the last is done (by tile: O is at rest then, too).
       bool ok = wait(sm.qkdone + 8 * b, (t >> 1) & 1) && wait(sm.pvdone + 8 * b, ((t >> 1) & 1) ^ 1u);
       ok = __all_sync(0xffffffffu, ok);
@@ -890,10 +917,10 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sm,
     }
     if (any_of(kBarSoftmax, kSoftmaxThreads, dead)) return;
     const bool two = w.lt1 - w.lt0 > 1;
-    if (threadIdx.x < CF::kNC) join_sums<CF>(p, sm, w, threadIdx.x, two || !(t0 & 1), two || (t0 & 1));
+    if (threadIdx.x < CF::kNC) join_sums<CF>(p, smem, next, threadIdx.x, two || !(t0 & 1), two || (t0 & 1));
     named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
     tc_fence_after();
-    write_rows<CF::kAccs>(p, sm, w, wg * (CF::kNC / 2), (wg + 1) * (CF::kNC / 2), trow + CF::kTmemO, CF::kNT);
+    write_rows<CF::kAccs>(p, smem, next, wg * (CF::kNC / 2), (wg + 1) * (CF::kNC / 2), trow + CF::kTmemO, CF::kNT);
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(sm.ofree);
@@ -941,8 +968,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   if (warp < kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem, w);
   else if (warp < kWarpLoad) run_decode<CF>(kp, sm, wait, tmem, w);
   else if (warp == kWarpLoad) run_loader<CF>(kp, sm, wait, w);
-  else if (warp == kWarpQk && lane == 0) run_qk<CF>(kp, sm, wait, tmem, w);
-  else if (warp == kWarpPv && lane == 0) run_pv<CF>(kp, sm, wait, tmem, w);
+  else if (warp == kWarpQk) run_qk<CF>(kp, sm, wait, tmem, w);
+  else if (warp == kWarpPv) run_pv<CF>(kp, sm, wait, tmem, w);
   else if (warp == kWarpQ) run_q<CF>(kp, sm, wait, w);
   __syncwarp();
   tc_fence_before();

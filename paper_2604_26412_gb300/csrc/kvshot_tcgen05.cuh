@@ -47,6 +47,34 @@ __device__ __forceinline__ void tc_mma_tmem_a(uint32_t d_tmem, uint32_t a_tmem, 
       : "memory");
 }
 
+// The same two and the commit below, called by a whole warp in uniform control flow with operands that are uniform: one
+// elected lane issues.  (The operands go to uniform registers.  Issued from a branch of one lane they are moved there one
+// by one: 45 cycles per MMA against 10 at M = 128, N = 16, K = 16 with A in tensor memory, what the MMA itself takes.)
+__device__ __forceinline__ void tc_mma_elect(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                             uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred one, acc;\n\telect.sync _|one, 0xffffffff;\n\t"
+      "setp.ne.b32 acc, %4, 0;\n\t"
+      "@one tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, acc;\n\t}\n" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tc_mma_tmem_a_elect(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                                    uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred one, acc;\n\telect.sync _|one, 0xffffffff;\n\t"
+      "setp.ne.b32 acc, %4, 0;\n\t"
+      "@one tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, acc;\n\t}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tc_commit_elect(uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred one;\n\telect.sync _|one, 0xffffffff;\n\t"
+      "@one tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(bar)
+      : "memory");
+}
+
 // Arrives (once) on `bar` when every tcgen05 operation this thread issued so far has completed.
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
