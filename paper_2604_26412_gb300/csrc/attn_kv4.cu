@@ -20,6 +20,7 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <type_traits>
 
 #include "kvshot_attn_common.cuh"
 #include "kvshot_kv4.cuh"
@@ -86,7 +87,7 @@ struct Smem {
   uint32_t qfull, qempty;            // [2] q of a piece staged; its last QK^T done
   uint32_t ofree, mmadone;           // epilogue has read O; [2] every MMA issued is done
   uint64_t *anc, *row_anc;           // [64] each node's ancestors and itself (tree); of each query row's node
-  float *ref, *alpha, *inv;          // [2][64] per warpgroup and row
+  float *ref, *alpha, *inv;          // [2][64] per warpgroup and row (ref: negated)
   int* wmax;                         // [8][64] per warp and row; sums at a piece's end
   int *depth, *place;                // [64] per row
   int* par;                          // [64]
@@ -145,7 +146,7 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
 }
 
 // Every wait ends: when its phase completes, when another role has given up, or (which gives up) after the call's limit.
-// The inline part is one test.
+// The inline part is one try, which blocks for a while (a call for each wait took more instructions than it waited for).
 __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, int32_t* err, uint64_t limit_ns, volatile int* abort) {
   const bool poll = limit_ns < kPollBelowNs;  // (a blocking try could sit out a short limit)
   const uint64_t t0 = global_timer_ns();
@@ -164,8 +165,9 @@ struct Waiter {
   int32_t* err;
   uint64_t limit;
   volatile int* abort;
+  bool poll;
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
-    if (mbar_test_wait(bar, parity)) return true;
+    if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
     return wait_slow(bar, parity, err, limit, abort);
   }
 };
@@ -216,6 +218,11 @@ struct Piece {
   }
   __device__ __forceinline__ int nkeys(int lt, int n_nodes) const {
     return draft(lt) ? min(kDraftTile, n_nodes - key0(lt)) : min(kTile, L - key0(lt));
+  }
+  // Whether prefix tile lt holds keys past the last one, or from the sinks' end up to `from`, where a window begins.
+  __device__ __forceinline__ bool masked(int lt, int from, int sinks) const {
+    const int k = key0(lt);
+    return k + kTile > L || (k < from && k + kTile > sinks);
   }
   __device__ __forceinline__ bool whole() const { return lt0 == 0 && lt1 == ut; }
 };
@@ -442,6 +449,14 @@ __device__ __noinline__ void decode_draft(uint32_t src, bool live, uint32_t dst,
   }
 }
 
+// The codes of 32 dims of one key (a chunk) with the two scales in the low bytes of `scales`, as 16 f16x2 words.
+__device__ __forceinline__ void decode32(uint32_t src, uint32_t scales, uint32_t (&o)[16]) {
+  const uint4 x = lds128(src);
+  const uint2 s = scale_pair(scales);
+  decode16(x.x, x.y, s.x, o);
+  decode16(x.z, x.w, s.y, o + 8);
+}
+
 // A decoding warpgroup: the tiles t % 2 == wg, a key to a thread.
 template <class CF>
 __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem, Piece next) {
@@ -453,73 +468,65 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
   const uint32_t draft0 = sm.ring + key * kDraftRow;
   const uint32_t kdst = tmem + (static_cast<uint32_t>(key & 96) << 16) + CF::kTmemK + 64 * wg;
   const uint32_t vdst = sm.v + wg * kVTile + key * 128, sw = static_cast<uint32_t>(key & 7) << 4;
-  int stage = wg, t = 0, mine = 0;  // the piece's first tile; this warpgroup's tiles so far
-  uint32_t phase = 0;
+  const uint32_t qkdone = sm.qkdone + 8 * wg, pvdone = sm.pvdone + 8 * wg, kfull = sm.kfull + 8 * wg, vfull = sm.vfull + 8 * wg;
+  int stage = wg, t = 0;  // t: the piece's first tile
+  uint32_t phase = 0, freed = 1;
   for (; next_piece(p, sm.len, next); t += next.lt1 - next.lt0) {
     const Piece w = next;
     // Keys that no row sees may hold anything; V of them must not be NaN (0 * NaN).
     const int lo = p.window > 0 ? w.L + p.min_depth - p.window : 0;
 #pragma unroll 1
-    for (int lt = w.lt0 + ((t ^ wg) & 1); lt < w.lt1; lt += 2, ++mine) {
-      const int key0 = w.key0(lt);
+    for (int lt = w.lt0 + ((t ^ wg) & 1); lt < w.lt1; lt += 2) {
       const bool draft = w.draft(lt);
-      bool live = key < w.nkeys(lt, p.N);
-      if (!draft) live = live && (key0 + key >= lo || key0 + key < p.sinks);
       // The tile's bytes; K's buffer: QK^T of its previous tile is done.
       bool ok = wait(sm.cfull + 8 * stage, phase);
-      ok = ok && wait(sm.qkdone + 8 * wg, (mine & 1) ^ 1u);
+      ok = ok && wait(qkdone, freed);
       if (!__all_sync(0xffffffffu, ok)) return;
       tc_fence_after();
       const uint32_t src = src0 + stage * kStageSize;
-      uint2 ksc, vsc;
       if (!draft) {
-        ksc = lds64(src + scale0);
-        vsc = lds64(src + scale0 + kScaleBytes);
-        if (!live) vsc = make_uint2(0u, 0u);  // (any code times 0 is 0)
+        uint2 sc = lds64(src + scale0);
 #pragma unroll 1
-        for (int hf = 0; hf < 2; ++hf) {
-          const uint4 x0 = lds128(src + hf * 2 * kChunkStride), x1 = lds128(src + (hf * 2 + 1) * kChunkStride);
-          const uint32_t four = hf ? ksc.y : ksc.x;
-          uint32_t o[32];
-          const uint2 s0 = scale_pair(four), s1 = scale_pair(four >> 16);
-          decode16(x0.x, x0.y, s0.x, o);
-          decode16(x0.z, x0.w, s0.y, o + 8);
-          decode16(x1.x, x1.y, s1.x, o + 16);
-          decode16(x1.z, x1.w, s1.y, o + 24);
-          tmem_st32(kdst + 32 * hf, o);
+        for (int c = 0; c < 4; ++c) {
+          uint32_t o[16];
+          decode32(src + c * kChunkStride, sc.x, o);
+          tmem_st16(kdst + 16 * c, o);
+          sc.x = __funnelshift_r(sc.x, sc.y, 16);
+          sc.y >>= 16;
         }
       } else {
-        decode_draft<false>(draft0 + stage * kStageSize, live, kdst, sw);
+        decode_draft<false>(draft0 + stage * kStageSize, key < w.nkeys(lt, p.N), kdst, sw);
       }
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(sm.kfull + 8 * wg);
+      if (lane == 0) mbar_arrive(kfull);
       // V's buffer: P.V of its previous tile is done.
-      if (!__all_sync(0xffffffffu, wait(sm.pvdone + 8 * wg, (mine & 1) ^ 1u))) return;
+      if (!__all_sync(0xffffffffu, wait(pvdone, freed))) return;
       if (!draft) {
+        uint2 sc = lds64(src + scale0 + kScaleBytes);
+        if (w.masked(lt, lo, p.sinks)) {
+          const int at = w.key0(lt) + key;
+          if (at >= w.L || (at < lo && at >= p.sinks)) sc = make_uint2(0u, 0u);  // (any code times 0 is 0)
+        }
 #pragma unroll 1
-        for (int hf = 0; hf < 2; ++hf) {
-          const uint4 x0 = lds128(src + kVCodes + hf * 2 * kChunkStride), x1 = lds128(src + kVCodes + (hf * 2 + 1) * kChunkStride);
-          const uint32_t four = hf ? vsc.y : vsc.x;
-          uint32_t o[32];
-          const uint2 s0 = scale_pair(four), s1 = scale_pair(four >> 16);
-          decode16(x0.x, x0.y, s0.x, o);
-          decode16(x0.z, x0.w, s0.y, o + 8);
-          decode16(x1.x, x1.y, s1.x, o + 16);
-          decode16(x1.z, x1.w, s1.y, o + 24);
-          put_v(vdst + hf * kVHalf, sw, 0, o);
-          put_v(vdst + hf * kVHalf, sw, 1, o + 16);
+        for (int c = 0; c < 4; ++c) {
+          uint32_t o[16];
+          decode32(src + kVCodes + c * kChunkStride, sc.x, o);
+          put_v(vdst, sw, c, o);
+          sc.x = __funnelshift_r(sc.x, sc.y, 16);
+          sc.y >>= 16;
         }
       } else {
-        decode_draft<true>(draft0 + kDraftV + stage * kStageSize, live, vdst, sw);
+        decode_draft<true>(draft0 + kDraftV + stage * kStageSize, key < w.nkeys(lt, p.N), vdst, sw);
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(sm.cempty + 8 * stage);
-        mbar_arrive(sm.vfull + 8 * wg);
+        mbar_arrive(vfull);
       }
+      freed ^= 1u;
       stage += 2;
       if (stage >= CF::kStages) {
         stage -= CF::kStages;
@@ -540,25 +547,36 @@ __device__ __forceinline__ void run_qk(const Kv4Params& kp, const Smem& smem, co
   const Smem sm = smem;
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, false);
   const uint32_t tmem = uniform(tmem_base);
-  bool ok = true;
+  const uint64_t q0 = smem_desc_sw128(sm.q, 16, 1024);
+  uint32_t phase = 0;  // of the buffers' tiles: flips after the second one
   int t = 0;
-  for (int piece = 0; __all_sync(0xffffffffu, ok && next_piece(p, sm.len, next)); ++piece) {
+  for (int piece = 0; __all_sync(0xffffffffu, next_piece(p, sm.len, next)); ++piece) {
     const int tiles = uniform(next.lt1 - next.lt0);
-    ok = __all_sync(0xffffffffu, wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1));
-    if (!ok) break;
-    const uint64_t q = smem_desc_sw128(sm.q + (piece & 1) * CF::kQTile, 16, 1024);
-#pragma unroll 1
-    for (int i = 0; i < tiles; ++i, ++t) {
-      const int b = t & 1;
-      ok = wait(sm.pfull + 8 * b, ((t >> 1) & 1) ^ 1u);  // S of the tile before the last has been read
-      ok = __all_sync(0xffffffffu, ok && wait(sm.kfull + 8 * b, (t >> 1) & 1));
-      if (!ok) break;
+    if (!__all_sync(0xffffffffu, wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1))) break;
+    const uint64_t q = q0 + (piece & 1) * (CF::kQTile >> 4);
+    // The tile in buffers b.
+    auto step = [&](auto buffer) {
+      constexpr int b = decltype(buffer)::value;
+      bool ok = wait(sm.pfull + 8 * b, phase ^ 1u);  // S of the tile before the last has been read
+      ok = ok && wait(sm.kfull + 8 * b, phase);
+      if (!__all_sync(0xffffffffu, ok)) return false;
       tc_fence_after();
 #pragma unroll
       for (int ks = 0; ks < kHeadDim / 16; ++ks)
         tc_mma_tmem_a_elect(tmem + CF::kTmemS + b * CF::kNT, tmem + CF::kTmemK + 64 * b + 8 * ks,
                             q + (((ks >> 2) * (CF::kNT * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
       tc_commit_elect(sm.qkdone + 8 * b);
+      return true;
+    };
+    bool ok = true;
+#pragma unroll 1
+    for (int i = 0; ok && i < tiles; ++i, ++t) {
+      if ((t & 1) == 0) {
+        ok = step(std::integral_constant<int, 0>{});
+      } else {
+        ok = step(std::integral_constant<int, 1>{});
+        phase ^= 1u;
+      }
     }
     if (!ok) break;
     tc_commit_elect(sm.qempty + 8 * (piece & 1));
@@ -573,27 +591,35 @@ __device__ __forceinline__ void run_pv(const Kv4Params& kp, const Smem& smem, co
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, true, true);
   const uint32_t tmem = uniform(tmem_base);
   const uint64_t v0 = smem_desc_sw128(sm.v, kVHalf, 1024), p0 = smem_desc_sw128(sm.p, kPTile, 1024);
-  bool ok = true;
+  uint32_t phase = 0;
   int t = 0;
-  for (int piece = 0; __all_sync(0xffffffffu, ok && next_piece(p, sm.len, next)); ++piece) {
+  for (int piece = 0; __all_sync(0xffffffffu, next_piece(p, sm.len, next)); ++piece) {
     const int tiles = uniform(next.lt1 - next.lt0);
-    if (piece > 0) ok = __all_sync(0xffffffffu, wait(sm.ofree, (piece - 1) & 1));
-    if (!ok) break;
-#pragma unroll 1
-    for (int i = 0; i < tiles; ++i, ++t) {
-      const int b = t & 1;
-      ok = wait(sm.vfull + 8 * b, (t >> 1) & 1);
-      ok = __all_sync(0xffffffffu, ok && wait(sm.pfull + 8 * b, (t >> 1) & 1));
-      if (!ok) break;
+    if (piece > 0 && !__all_sync(0xffffffffu, wait(sm.ofree, (piece - 1) & 1))) break;
+    auto step = [&](auto buffer, uint32_t more) {  // more: the accumulator holds tiles of this piece
+      constexpr int b = decltype(buffer)::value;
+      bool ok = wait(sm.vfull + 8 * b, phase);
+      ok = ok && wait(sm.pfull + 8 * b, phase);
+      if (!__all_sync(0xffffffffu, ok)) return false;
       tc_fence_after();
-      const uint32_t o = tmem + CF::kTmemO + (CF::kByTile ? b * CF::kNT : 0);
-      const uint32_t more = i >= CF::kAccs;  // the accumulator holds tiles of this piece
 #pragma unroll
       for (int k16 = 0; k16 < kTile / 16; ++k16)  // two 8-key groups of 1 KB each
-        tc_mma_elect(o, v0 + ((b * kVTile + k16 * 2048) >> 4), p0 + ((b * kPTile + k16 * 2048) >> 4), idesc,
-                     k16 > 0 ? 1u : more);
+        tc_mma_elect(tmem + CF::kTmemO + (CF::kByTile ? b * CF::kNT : 0), v0 + ((b * kVTile + k16 * 2048) >> 4),
+                     p0 + ((b * kPTile + k16 * 2048) >> 4), idesc, k16 > 0 ? 1u : more);
       tc_commit_elect(sm.pvdone + 8 * b);
+      return true;
+    };
+    bool ok = true;
+#pragma unroll 1
+    for (int i = 0; ok && i < tiles; ++i, ++t) {
+      if ((t & 1) == 0) {
+        ok = step(std::integral_constant<int, 0>{}, i >= CF::kAccs);
+      } else {
+        ok = step(std::integral_constant<int, 1>{}, i >= CF::kAccs);
+        phase ^= 1u;
+      }
     }
+    if (!ok) break;
   }
   tc_commit_elect(sm.mmadone + 8);
 }
@@ -692,7 +718,7 @@ __device__ __noinline__ uint64_t visible_rows(const AttnParams& p, const Smem& s
   return bits;
 }
 
-// The references of rows whose scores have passed their limit move: ref, and alpha with what O and the sums are to be
+// The references of rows whose scores have passed their limit move: refs (negated), and alpha with what O and the sums are to be
 // multiplied by.  The threads of warpgroup wg; n rows from the first of `scores`, `ref` and `alpha` on.
 __device__ __noinline__ void move_references(int* wmax, float* refs, float* alpha, int wg, int n, uint32_t scores, float qs,
                                              uint64_t vis) {
@@ -712,8 +738,8 @@ __device__ __noinline__ void move_references(int* wmax, float* refs, float* alph
   named_barrier_sync(kBarGroup + wg, kGroupThreads);
   if (tid < n) {
     const float m = unordered(max(max(wmax[tid], wmax[64 + tid]), max(wmax[128 + tid], wmax[192 + tid])));
-    const float old = refs[tid], ref = m - old > kRefLimit ? m - kRefBelow : old;
-    refs[tid] = ref;
+    const float old = -refs[tid], ref = m - old > kRefLimit ? m - kRefBelow : old;
+    refs[tid] = -ref;
     alpha[tid] = ex2(old - ref);
   }
   named_barrier_sync(kBarGroup + wg, kGroupThreads);
@@ -775,7 +801,7 @@ __device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, cons
   };
   float sum, top;
   if constexpr (CF::kByTile) {
-    const float r0 = had0 ? sm.ref[j] : kNoRef, r1 = had1 ? sm.ref[64 + j] : kNoRef;
+    const float r0 = had0 ? -sm.ref[j] : kNoRef, r1 = had1 ? -sm.ref[64 + j] : kNoRef;
     top = fmaxf(r0, r1);
     const float w0 = had0 ? ex2(r0 - top) : 0.f, w1 = had1 ? ex2(r1 - top) : 0.f;
     sum = (had0 ? w0 * total(0, j) : 0.f) + (had1 ? w1 * total(1, j) : 0.f);
@@ -784,7 +810,7 @@ __device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, cons
     sm.inv[64 + j] = w1 * inv * (sm.codes[1] ? p.v_scale : 1.f);
   } else {
     const int wg = j >= CF::kCols;
-    top = sm.ref[j];
+    top = -sm.ref[j];
     sum = total(wg, j - wg * CF::kCols);
     sm.inv[j] = sum == 0.f ? 0.f : (sm.codes[0] ? p.v_scale : 1.f) / sum;
   }
@@ -818,11 +844,11 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
       unit_rb = w.rb;
       unit_seq = w.seq;
     }
-    if (key < NC) ref[key] = kNoRef;
+    if (key < NC) ref[key] = -kNoRef;
     named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-    float l[NC];  // sums over this thread's keys
+    float2 l[NC / 2];  // sums over this thread's keys
 #pragma unroll
-    for (int j = 0; j < NC; ++j) l[j] = 0.f;
+    for (int j = 0; j < NC / 2; ++j) l[j] = make_float2(0.f, 0.f);
     // Tiles from here on (or before the sinks' end) are seen whole by every row.
     int seen_from = 0;
     if (p.window > 0) {
@@ -836,48 +862,54 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     int t = t0 + lt_first - w.lt0;
 #pragma unroll 1
     for (int lt = lt_first; lt < w.lt1 && !dead; lt += CF::kAccs, t += CF::kAccs) {
-      const int b = t & 1, key0 = w.key0(lt), nkeys = w.nkeys(lt, p.N);
+      const int b = CF::kByTile ? wg : t & 1;
+      const uint32_t phase = (t >> 1) & 1;
       const bool draft = w.draft(lt);
       const float qs = draft ? p.qscale : p.qscale * p.k_scale;
       uint64_t vis = ~0ull;
-      if (draft || nkeys < kTile || (key0 < seen_from && key0 + kTile > p.sinks))
-        vis = key < nkeys ? visible_rows(p, smem, col0, NC, draft, key0 + key, w.L) : 0ull;
+      if (draft || w.masked(lt, seen_from, p.sinks)) {
+        const int at = w.key0(lt) + key;
+        vis = key < w.nkeys(lt, p.N) ? visible_rows(p, smem, col0, NC, draft, at, w.L) : 0ull;
+      }
       // S; and the buffer of P, free when P.V of the tile before the last is done (by tile: O is at rest then, too).
-      bool ok = wait(sm.qkdone + 8 * b, (t >> 1) & 1) && wait(sm.pvdone + 8 * b, ((t >> 1) & 1) ^ 1u);
+      bool ok = wait(sm.qkdone + 8 * b, phase);
+      ok = ok && wait(sm.pvdone + 8 * b, phase ^ 1u);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
       const uint32_t scores = trow + CF::kTmemS + b * CF::kNT + col0;
       const bool leave_codes = draft && in_codes && p.v_scale != 1.f;
       if (draft) in_codes = false;
-      float x[NC];
+      float2 x[NC / 2];
       for (bool moved = false;; moved = true) {
-        if (ok) {
-          uint32_t s[NC];
-          tmem_ld_cols<NC>(scores, s);
-          tmem_wait_ld();
+        uint32_t s[NC];
+        tmem_ld_cols<NC>(scores, s);
+        tmem_wait_ld();
 #pragma unroll
-          for (int j = 0; j < NC; j += 4) {
-            const float4 m = *reinterpret_cast<const float4*>(ref + j);
-            x[j] = fmaf(__uint_as_float(s[j]), qs, -m.x);
-            x[j + 1] = fmaf(__uint_as_float(s[j + 1]), qs, -m.y);
-            x[j + 2] = fmaf(__uint_as_float(s[j + 2]), qs, -m.z);
-            x[j + 3] = fmaf(__uint_as_float(s[j + 3]), qs, -m.w);
-          }
-          if (vis != ~0ull) {
+        for (int j = 0; j < NC; j += 4) {
+          const float4 m = *reinterpret_cast<const float4*>(ref + j);  // (negated)
+          x[j / 2] = fma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), make_float2(qs, qs), make_float2(m.x, m.y));
+          x[j / 2 + 1] = fma2(make_float2(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), make_float2(qs, qs), make_float2(m.z, m.w));
+        }
+        if (vis != ~0ull) {
 #pragma unroll
-            for (int j = 0; j < NC; ++j) x[j] = (vis >> j) & 1ull ? x[j] : -INFINITY;
+          for (int j = 0; j < NC; j += 2) {
+            if (!((vis >> j) & 1ull)) x[j / 2].x = -INFINITY;
+            if (!((vis >> j) & 2ull)) x[j / 2].y = -INFINITY;
           }
         }
         if (moved) break;
-        float top = -INFINITY;
+        float top = kRefLimit;
 #pragma unroll
-        for (int j = 0; j < NC; ++j) top = fmaxf(top, x[j]);
+        for (int j = 0; j < NC / 2; ++j) top = max3(top, x[j].x, x[j].y);
         if (!any_of(bar, kGroupThreads, top > kRefLimit || leave_codes || !ok)) break;
         dead = any_of(bar, kGroupThreads, !ok);
         if (dead) break;
         move_references(wmax, ref, alpha, wg, NC, scores, qs, vis);  // always with a warpgroup's first keys of a piece
 #pragma unroll
-        for (int j = 0; j < NC; ++j) l[j] *= alpha[j];
+        for (int j = 0; j < NC / 2; ++j) {
+          l[j].x *= alpha[2 * j];
+          l[j].y *= alpha[2 * j + 1];
+        }
         if (lt > lt_first) {
           if constexpr (!CF::kByTile) {
             dead = any_of(bar, kGroupThreads, !wait(sm.pvdone + 8 * (b ^ 1), ((t - 1) >> 1) & 1));
@@ -890,14 +922,14 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
       if (dead) break;
 #pragma unroll
       for (int j = 0; j < NC; j += 8) {
-        float e[8];
+        uint32_t pk[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          e[i] = ex2(x[j + i]);
-          l[j + i] += e[i];
+        for (int i = 0; i < 4; ++i) {
+          const float2 e = make_float2(ex2(x[j / 2 + i].x), ex2(x[j / 2 + i].y));
+          l[j / 2 + i] = add2(l[j / 2 + i], e);
+          pk[i] = pack_f16x2(e.x, e.y);
         }
-        sts128(pdst + b * kPTile + ((static_cast<uint32_t>(col0 + j) << 1) ^ sw),
-               make_uint4(pack_f16x2(e[0], e[1]), pack_f16x2(e[2], e[3]), pack_f16x2(e[4], e[5]), pack_f16x2(e[6], e[7])));
+        sts128(pdst + b * kPTile + ((static_cast<uint32_t>(col0 + j) << 1) ^ sw), make_uint4(pk[0], pk[1], pk[2], pk[3]));
       }
       fence_proxy_async_smem();
       tc_fence_before();
@@ -906,10 +938,16 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     }
     // Sums over the keys' threads, then the rows.
     int col = 0;
-    const int width = column_sums(l, lane, &col);
+    float sums[NC];
+#pragma unroll
+    for (int j = 0; j < NC / 2; ++j) {
+      sums[2 * j] = l[j].x;
+      sums[2 * j + 1] = l[j].y;
+    }
+    const int width = column_sums(sums, lane, &col);
 #pragma unroll
     for (int i = 0; i < NC; ++i)
-      if (i < width) wmax[(key >> 5) * 64 + col + i] = __float_as_int(l[i]);
+      if (i < width) wmax[(key >> 5) * 64 + col + i] = __float_as_int(sums[i]);
     if (key == 0) sm.codes[wg] = in_codes;
     if (!dead && lt_first < w.lt1) {  // O is at rest
       const int last = t - CF::kAccs;
@@ -962,7 +1000,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   build_kv4_plan(p, sm.len, sm.base);  // (barriers inside)
   tc_fence_after();
   const uint32_t tmem = *sm.tmem;
-  const Waiter wait{p.err, p.wait_ns, sm.abort};
+  const Waiter wait{p.err, p.wait_ns, sm.abort, p.wait_ns < kPollBelowNs};
   Piece w;
   begin_pieces(p, sm.len, sm.base, w);
   if (warp < kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem, w);
