@@ -22,27 +22,17 @@
 #include <cmath>
 #include <type_traits>
 
-#include "kvshot_attn_common.cuh"
-#include "kvshot_kv4.cuh"
+#include "kvshot_kv4_attn.cuh"
 #include "kvshot_tcgen05.cuh"
 
 namespace kvshot {
 namespace {
 
-using namespace dev;
-using namespace kv4;
 using namespace tc;
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-constexpr int kTile = kKv4PrefixTile;              // keys per prefix tile
-constexpr int kTileGroups = kTile / kKv4Tokens;
-constexpr int kStageSize = kTileGroups * kKv4Bytes;
-constexpr int kDraftTile = 32;                     // keys per draft tile: bf16 rows of K and V fill a stage
-constexpr int kDraftRow = 2 * kHeadDim + 16;       // padded: rows 16 bytes apart mod 128, free of bank conflicts
-constexpr int kDraftV = kDraftTile * kDraftRow;
-static_assert(2 * kDraftV <= kStageSize, "a draft tile fits a stage");
 constexpr int kVHalf = kTile * 128;                // 64 dims of a tile's V: 128 rows of 128 bytes, 128-byte swizzle
 constexpr int kVTile = 2 * kVHalf;
 constexpr int kPTile = kTile * 128;                // P^T: a row of up to 64 query rows per key, 128-byte swizzle
@@ -51,19 +41,6 @@ constexpr int kGroupThreads = 128;                 // a warpgroup
 constexpr int kSoftmaxThreads = 256;
 constexpr int kWarpDecode = 8, kWarpLoad = 16, kWarpQk = 17, kWarpPv = 18, kWarpQ = 19;
 constexpr int kBarGroup = 1, kBarSoftmax = 3;      // named barriers: 1 and 2 of a softmax warpgroup, 3 of both
-// The reference of a row is 2^8 below the maximum it was taken from and moves when a score passes it by 2^15: P stays in
-// f16's normal range for scores down to 2^-22 of the maximum and below its largest number.
-constexpr float kRefBelow = 8.f, kRefLimit = 15.f;
-constexpr float kNoRef = -1e30f;                   // no score yet
-
-struct Kv4Params {
-  AttnParams a;
-  const uint8_t* cache;
-  const __nv_bfloat16 *draft_k, *draft_v;
-  int groups_per_page;
-  int run_groups;  // groups of a tile that are always neighbours in memory (a power of two, at most kTileGroups)
-};
-
 // NC: query rows of a unit, a multiple of 8.
 template <int NC>
 struct Cfg {
@@ -79,23 +56,17 @@ struct Cfg {
   static_assert(kTmemO + kAccs * kNT <= 512 && kCols % 8 == 0, "tensor memory");
 };
 
-struct Smem {
-  uint32_t v, p, q, ring;            // shared-memory addresses
-  uint32_t cfull, cempty;            // barriers, by address. [stages] bytes landed; read by their decoding warpgroup
+struct Smem : Ring, Rows {
+  uint32_t v, p, q;                  // shared-memory addresses
   uint32_t kfull, vfull;             // [2] K, V decoded
   uint32_t qkdone, pfull, pvdone;    // [2] QK^T done; P written (and S read); P.V done
   uint32_t qfull, qempty;            // [2] q of a piece staged; its last QK^T done
   uint32_t ofree, mmadone;           // epilogue has read O; [2] every MMA issued is done
-  uint64_t *anc, *row_anc;           // [64] each node's ancestors and itself (tree); of each query row's node
   float *ref, *alpha, *inv;          // [2][64] per warpgroup and row (ref: negated)
   int* wmax;                         // [8][64] per warp and row; sums at a piece's end
-  int *depth, *place;                // [64] per row
-  int* par;                          // [64]
   int* codes;                        // [2] the warpgroup's accumulator is in units of the value codes
   uint32_t* tmem;
   volatile int* abort;
-  int* issued;                       // tiles issued by the loader
-  int *len, *base;
 };
 
 constexpr int kBarriers = 18;  // besides the ring's: 17, and one for the alignment of what follows
@@ -145,233 +116,6 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   return s;
 }
 
-// Every wait ends: when its phase completes, when another role has given up, or (which gives up) after the call's limit.
-// The inline part is one try, which blocks for a while (a call for each wait took more instructions than it waited for).
-__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, int32_t* err, uint64_t limit_ns, volatile int* abort) {
-  const bool poll = limit_ns < kPollBelowNs;  // (a blocking try could sit out a short limit)
-  const uint64_t t0 = global_timer_ns();
-  for (;;) {
-    for (int i = 0; i < (poll ? 1 : 16); ++i)
-      if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
-    if (*abort) return false;
-    if (global_timer_ns() - t0 > limit_ns) break;
-  }
-  set_error(err, KVSHOT_ERR_TIMEOUT);
-  *abort = 1;
-  return false;
-}
-
-struct Waiter {
-  int32_t* err;
-  uint64_t limit;
-  volatile int* abort;
-  bool poll;
-  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
-    if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
-    return wait_slow(bar, parity, err, limit, abort);
-  }
-};
-
-// ------------------------------------------------------------ work plan
-
-__device__ __forceinline__ void build_kv4_plan(const AttnParams& p, int* s_len, int* s_base) {
-  const int HR = p.hkv * p.row_blocks;
-  for (int c = threadIdx.x; c < p.C; c += blockDim.x) {
-    const int L = clamp_len(p, c);
-    s_len[c] = L;
-    s_base[c + 1] = (window_span<kTile>(p, L).tiles + p.draft_tiles) * HR;
-  }
-  __syncthreads();
-  if (p.unit_ctas > 0) return;  // one cache: the cut needs its length alone
-  if (threadIdx.x < 32) {
-    const int lane = threadIdx.x, per = (p.C + 31) / 32, c0 = min(p.C, lane * per), c1 = min(p.C, c0 + per);
-    int v = 0;
-    for (int c = c0; c < c1; ++c) v += s_base[c + 1];
-    int scan = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int t = __shfl_up_sync(0xffffffffu, scan, o);
-      if (lane >= o) scan += t;
-    }
-    int below = scan - v;
-    for (int c = c0; c < c1; ++c) {
-      below += s_base[c + 1];
-      s_base[c + 1] = below;
-    }
-    if (lane == 0) s_base[0] = 0;
-  }
-  __syncthreads();
-}
-
-// A run of tiles of one unit that this CTA takes.
-struct Piece {
-  int t, t_end;        // tile of this CTA's range: the piece's first one (its end after next_piece), and the range's end
-  int c, hr;           // cache, KV head x row block
-  int lt0, lt1, ut;    // the piece's tiles of the unit [lt0, lt1), tiles of the unit
-  int h, rb, seq, L;   // KV head, row block, sequence, prefix length
-  WindowSpan span;
-
-  // First key of tile lt (token, or draft slot), and its valid keys.
-  __device__ __forceinline__ bool draft(int lt) const { return lt >= span.tiles; }
-  __device__ __forceinline__ int key0(int lt) const {
-    return draft(lt) ? (lt - span.tiles) * kDraftTile : (lt < span.sink_tiles ? lt : lt + span.skip) * kTile;
-  }
-  __device__ __forceinline__ int nkeys(int lt, int n_nodes) const {
-    return draft(lt) ? min(kDraftTile, n_nodes - key0(lt)) : min(kTile, L - key0(lt));
-  }
-  // Whether prefix tile lt holds keys past the last one, or from the sinks' end up to `from`, where a window begins.
-  __device__ __forceinline__ bool masked(int lt, int from, int sinks) const {
-    const int k = key0(lt);
-    return k + kTile > L || (k < from && k + kTile > sinks);
-  }
-  __device__ __forceinline__ bool whole() const { return lt0 == 0 && lt1 == ut; }
-};
-
-// The CTA's range; next_piece finds its first piece.
-__device__ __noinline__ void begin_pieces(const AttnParams& p, const int* s_len, const int* s_base, Piece& w) {
-  w.c = w.hr = w.lt1 = w.ut = w.t = w.t_end = 0;
-  if (p.unit_ctas > 0) {
-    w.ut = window_span<kTile>(p, s_len[0]).tiles + p.draft_tiles;
-    const UnitCut u = unit_cut(p.unit_ctas, w.ut);
-    w.hr = blockIdx.x / u.per;
-    w.lt1 = (blockIdx.x - w.hr * u.per) * u.tpc;
-    w.t_end = w.hr < p.hkv * p.row_blocks ? min(u.tpc, w.ut - w.lt1) : 0;
-    return;
-  }
-  const int total = s_base[p.C], tpc = tiles_per_cta(total, p.num_ctas);
-  w.t = min(total, static_cast<int>(blockIdx.x) * tpc);
-  w.t_end = min(total, w.t + tpc);
-  if (w.t >= w.t_end) return;
-  int lo = 0, hi = p.C - 1;  // last cache whose first tile is <= t
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (s_base[mid] <= w.t) lo = mid;
-    else hi = mid - 1;
-  }
-  w.c = lo;
-  w.ut = window_span<kTile>(p, s_len[lo]).tiles + p.draft_tiles;
-  const int rem = w.t - s_base[lo];
-  w.hr = rem / w.ut;
-  w.lt1 = rem - w.hr * w.ut;
-}
-
-// Moves on to the next piece of the range; false at its end.  (Out of line: the roles' loops over the tiles are short.)
-__device__ __noinline__ bool next_piece(const AttnParams& p, const int* s_len, Piece& w) {
-  if (w.t >= w.t_end) return false;
-  if (w.lt1 == w.ut) {
-    w.lt1 = 0;
-    if (++w.hr == p.hkv * p.row_blocks) {
-      w.hr = 0;
-      ++w.c;
-    }
-  }
-  w.L = s_len[w.c];
-  w.span = window_span<kTile>(p, w.L);
-  w.ut = w.span.tiles + p.draft_tiles;
-  w.lt0 = w.lt1;
-  w.lt1 = min(w.ut, w.lt0 + w.t_end - w.t);
-  w.t += w.lt1 - w.lt0;
-  w.h = w.hr / p.row_blocks;
-  w.rb = w.hr - w.h * p.row_blocks;
-  w.seq = w.c / (p.C / p.B);
-  return true;
-}
-
-// ------------------------------------------------------------ loads
-
-// The roles keep copies of their own of what they also hand to functions out of line: a variable whose address has been
-// given away is read from local memory again after every barrier and copy.
-
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
-               : "memory");
-}
-
-template <class CF>
-__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Smem& smem, const Waiter& wait, Piece next) {
-  const AttnParams& p = kp.a;
-  const Smem sm = smem;
-  const int lane = threadIdx.x & 31;
-  int stage = 0, issued = 0;
-  uint32_t phase = 0;
-  bool waited = false, ok = true;
-  // Page ids come 32 to a load, a window of tiles ahead: lane i holds the address of run i % runs of the window's tile
-  // i / runs, and issues that copy.
-  const int runs = kTileGroups / kp.run_groups, ahead = 32 / runs;
-  const int my_tile = lane / runs, my_g0 = (lane % runs) * kp.run_groups;
-  while (ok && next_piece(p, sm.len, next)) {
-    const Piece w = next;
-    const int32_t* table = p.page_table + (p.paged ? static_cast<size_t>(w.c) * p.max_pages : 0);
-    auto group_of = [&](int lt) {  // this lane's first group of the window from tile lt on, or -1
-      lt += my_tile;
-      if (lt >= w.lt1 || w.draft(lt)) return -1;
-      const int g = w.key0(lt) / kKv4Tokens + my_g0;
-      return g * kKv4Tokens < w.L ? g : -1;
-    };
-    auto page_of = [&](int g) { return g < 0 ? 0 : p.paged ? table[g / kp.groups_per_page] : w.c; };
-    int window = w.lt0, g = group_of(window), pid = page_of(g);
-    const uint8_t* src = nullptr;
-    uint32_t bytes = 0;
-    for (int lt = w.lt0; lt < w.lt1; ++lt) {
-      if (lt == window) {
-        if (p.paged && g >= 0) pid = valid_page_id(p, pid);
-        src = kp.cache + ((static_cast<size_t>(pid) * p.hkv + w.h) * kp.groups_per_page +
-                          (p.paged ? g % kp.groups_per_page : g)) * kKv4Bytes;
-        bytes = g < 0 ? 0 : min(kp.run_groups, (w.L + kKv4Tokens - 1) / kKv4Tokens - g) * kKv4Bytes;
-        window += ahead;
-        g = group_of(window);
-        pid = page_of(g);
-      }
-      const bool draft = w.draft(lt);
-      const int nkeys = w.nkeys(lt, p.N);
-      if (draft && !waited) {  // the draft K/V may come from the preceding kernel
-        wait_for_prerequisite_grid();
-        waited = true;
-      }
-      ok = __all_sync(0xffffffffu, wait(sm.cempty + 8 * stage, phase ^ 1u));
-      if (!ok) break;
-      const uint32_t bar = sm.cfull + 8 * stage, dst = sm.ring + stage * kStageSize;
-      if (lane == 0)
-        mbar_arrive_expect_tx(bar, draft ? nkeys * 4 * kHeadDim : (nkeys + kKv4Tokens - 1) / kKv4Tokens * kKv4Bytes);
-      __syncwarp();
-      if (draft) {
-        if (lane < nkeys) {
-          const size_t row = (static_cast<size_t>(w.c) * p.hkv + w.h) * p.n_max + w.key0(lt) + lane;
-          bulk_load(dst + lane * kDraftRow, kp.draft_k + row * kHeadDim, 2 * kHeadDim, bar);
-          bulk_load(dst + kDraftV + lane * kDraftRow, kp.draft_v + row * kHeadDim, 2 * kHeadDim, bar);
-        }
-      } else if (my_tile == lt - (window - ahead) && bytes > 0) {
-        bulk_load(dst + my_g0 * kKv4Bytes, src, bytes, bar);
-      }
-      ++issued;
-      if (++stage == CF::kStages) {
-        stage = 0;
-        phase ^= 1u;
-      }
-    }
-  }
-  if (lane == 0) *sm.issued = issued;
-}
-
-__device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
-  const __half2 v = __floats2half2_rn(bf16_lo(w), bf16_hi(w));
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
-  const __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ void sts128(uint32_t addr, uint4 v) {
-  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
-               : "memory");
-}
-__device__ __forceinline__ uint2 lds64(uint32_t addr) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
-  return v;
-}
-
 // q of every piece as f16, rows of 64 dims in two halves (K-major B of QK^T, 128-byte swizzle).
 template <class CF>
 __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, const Waiter& wait, Piece next) {
@@ -403,24 +147,6 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
 }
 
 // ------------------------------------------------------------ decode
-
-// 16 codes (8 bytes) of one block times its scale, as 8 f16x2 words.
-__device__ __forceinline__ void decode16(uint32_t lo, uint32_t hi, uint32_t scale2, uint32_t* o) {
-  uint32_t a[4], b[4];
-  e2m1x8_to_f16(lo, a);
-  e2m1x8_to_f16(hi, b);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    o[i] = mul_f16x2(a[i], scale2);
-    o[4 + i] = mul_f16x2(b[i], scale2);
-  }
-}
-
-// Two blocks' scales (the low two bytes), each in both halves.
-__device__ __forceinline__ uint2 scale_pair(uint32_t bytes) {
-  const uint32_t two = e4m3x2_to_f16x2(bytes);
-  return make_uint2(__byte_perm(two, two, 0x1010), __byte_perm(two, two, 0x3232));
-}
 
 // 32 dims of one key (16 words) into its row of the V tile: 16-byte chunks 4 c .. 4 c + 3, 128-byte swizzle.
 __device__ __forceinline__ void put_v(uint32_t row, uint32_t sw, int c, const uint32_t* o) {
@@ -638,13 +364,6 @@ __device__ __forceinline__ bool any_of(int bar, int threads, bool x) {
   return r != 0;
 }
 
-// Floats as integers of the same order.
-__device__ __forceinline__ int ordered(float f) {
-  const int i = __float_as_int(f);
-  return i >= 0 ? i : i ^ 0x7fffffff;
-}
-__device__ __forceinline__ float unordered(int i) { return __int_as_float(i >= 0 ? i : i ^ 0x7fffffff); }
-
 // Sums of the columns over the warp's lanes: N sums to 32 lanes by halving, then plain for what is left.  Lane's v[i],
 // i < the final width, is then the sum of column column0 + i.
 template <int N>
@@ -670,52 +389,6 @@ __device__ __forceinline__ int column_sums(float (&v)[N], int lane, int* column0
   }
   *column0 = col;
   return width;
-}
-
-// The nodes of a unit's rows: depths, ancestors, places in q and out.  All softmax threads.
-__device__ __noinline__ void load_rows(const AttnParams& p, const Smem& sm, int nc, int rb, int seq, bool new_seq) {
-  const int tid = threadIdx.x;
-  named_barrier_sync(kBarSoftmax, kSoftmaxThreads);  // the rows before are no longer read
-  if (new_seq) {
-    for (int i = tid; i < p.N; i += kSoftmaxThreads) {
-      int v = p.tree_parent[static_cast<size_t>(seq) * p.N + i];
-      if (v < -1 || v >= i) {
-        set_error(p.err, KVSHOT_ERR_TREE);
-        v = -1;
-      }
-      sm.par[i] = v;
-    }
-    named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-    for (int i = tid; i < p.N; i += kSoftmaxThreads) {
-      uint64_t bits = 0;
-      for (int m = i; m >= 0; m = sm.par[m]) bits |= 1ull << m;  // parents strictly decrease
-      sm.anc[i] = bits;
-    }
-    named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-  }
-  if (tid < nc) {
-    const int rr = rb * p.rows_per_unit + tid;
-    const int nl = min(rr, p.rows_total - 1) / p.G, node = p.N - p.Nq + nl;
-    if (p.tree) sm.row_anc[tid] = sm.anc[node];
-    sm.depth[tid] = p.tree ? __popcll(sm.anc[node]) : node + 1;
-    sm.place[tid] = nl * p.hq + rr - nl * p.G;
-  }
-}
-
-// Bit j: row j0 + j sees this thread's key.  `at`: token position or draft slot of the key, which is valid.
-__device__ __noinline__ uint64_t visible_rows(const AttnParams& p, const Smem& sm, int j0, int n, bool draft, int at, int L) {
-  uint64_t bits = 0;
-  const int key_depth = !draft ? 0 : p.tree ? __popcll(sm.anc[at]) : at + 1;
-  const int pos = draft ? L + key_depth - 1 : at;
-  const bool always = p.window == 0 || pos < p.sinks;
-#pragma unroll 1
-  for (int j = 0; j < n; ++j) {
-    const int d = sm.depth[j0 + j];
-    bool v = always || L + d - 1 - pos < p.window;
-    if (draft) v = v && (p.tree ? (sm.row_anc[j0 + j] >> at) & 1ull : at < d);
-    bits |= static_cast<uint64_t>(v) << j;
-  }
-  return bits;
 }
 
 // The references of rows whose scores have passed their limit move: refs (negated), and alpha with what O and the sums are to be
@@ -840,7 +513,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
   for (; next_piece(p, sm.len, next); t0 += next.lt1 - next.lt0) {
     const Piece w = next;
     if (w.rb != unit_rb || (p.tree && w.seq != unit_seq)) {
-      load_rows(p, smem, CF::kNC, w.rb, w.seq, p.tree && w.seq != unit_seq);
+      load_rows(p, smem, CF::kNC, w.rb, w.seq, p.tree && w.seq != unit_seq, kBarSoftmax, kSoftmaxThreads);
       unit_rb = w.rb;
       unit_seq = w.seq;
     }
@@ -1005,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   begin_pieces(p, sm.len, sm.base, w);
   if (warp < kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem, w);
   else if (warp < kWarpLoad) run_decode<CF>(kp, sm, wait, tmem, w);
-  else if (warp == kWarpLoad) run_loader<CF>(kp, sm, wait, w);
+  else if (warp == kWarpLoad) run_loader<CF::kStages>(kp, sm, wait, w);
   else if (warp == kWarpQk) run_qk<CF>(kp, sm, wait, tmem, w);
   else if (warp == kWarpPv) run_pv<CF>(kp, sm, wait, tmem, w);
   else if (warp == kWarpQ) run_q<CF>(kp, sm, wait, w);
@@ -1043,8 +716,8 @@ cudaError_t launch_cfg(const Kv4Params& kp, bool pdl, cudaStream_t stream) {
 
 cudaError_t launch(const Kv4Params& kp, bool pdl, cudaStream_t stream) {
   switch (kp.a.rows_per_unit) {
-    case 8: return launch_cfg<Cfg<8>>(kp, pdl, stream);
-    case 16: return launch_cfg<Cfg<16>>(kp, pdl, stream);
+    case 8:
+    case 16: return launch_attn_kv4_mma(kp, pdl, stream);
     case 32: return launch_cfg<Cfg<32>>(kp, pdl, stream);
     case 48: return launch_cfg<Cfg<48>>(kp, pdl, stream);
     case 64: return launch_cfg<Cfg<64>>(kp, pdl, stream);
@@ -1087,8 +760,11 @@ kvshot_status make_kv4_plan(const kvshot_attn_desc* d, int32_t window, int32_t s
   int64_t grid = d->num_ctas;
   if (grid == 0) {
     const int sms = sm_count();
-    if (sms < 1) return KVSHOT_ERR_CUDA;
-    grid = std::min<int64_t>(sms, std::max((max_tiles + kMinTiles - 1) / kMinTiles, units));
+    int per_sm = 1;
+    if (pl->rows_per_unit <= 16 && attn_kv4_mma_occupancy(pl->rows_per_unit, d->num_caches, &per_sm) != cudaSuccess)
+      return KVSHOT_ERR_CUDA;
+    if (sms < 1 || per_sm < 1) return KVSHOT_ERR_CUDA;
+    grid = std::min<int64_t>(sms * per_sm, std::max((max_tiles + kMinTiles - 1) / kMinTiles, units));
   }
   pl->num_ctas = static_cast<int>(std::max<int64_t>(1, std::min(grid, max_tiles)));
   const size_t slots = static_cast<size_t>(pl->units) + pl->num_ctas;
