@@ -40,7 +40,7 @@ constexpr int kThreads = 20 * 32;
 constexpr int kGroupThreads = 128;                 // a warpgroup
 constexpr int kSoftmaxThreads = 256;
 constexpr int kWarpDecode = 8, kWarpLoad = 16, kWarpQk = 17, kWarpPv = 18, kWarpQ = 19;
-constexpr int kBarGroup = 1, kBarSoftmax = 3;      // named barriers: 1 and 2 of a softmax warpgroup, 3 of both
+constexpr int kBarGroup = 1;                       // named barriers 1 and 2: the threads of a softmax warpgroup
 // NC: query rows of a unit, a multiple of 8.
 template <int NC>
 struct Cfg {
@@ -62,6 +62,7 @@ struct Smem : Ring, Rows {
   uint32_t qkdone, pfull, pvdone;    // [2] QK^T done; P written (and S read); P.V done
   uint32_t qfull, qempty;            // [2] q of a piece staged; its last QK^T done
   uint32_t ofree, mmadone;           // epilogue has read O; [2] every MMA issued is done
+  uint32_t joined;                   // barrier of the softmax warps
   float *ref, *alpha, *inv;          // [2][64] per warpgroup and row (ref: negated)
   int* wmax;                         // [8][64] per warp and row; sums at a piece's end
   int* codes;                        // [2] the warpgroup's accumulator is in units of the value codes
@@ -69,12 +70,12 @@ struct Smem : Ring, Rows {
   volatile int* abort;
 };
 
-constexpr int kBarriers = 18;  // besides the ring's: 17, and one for the alignment of what follows
+constexpr int kBarriers = 18;  // besides the ring's (an even number: what follows is aligned to 16 bytes)
 
 template <class CF>
 __host__ __device__ constexpr size_t smem_bytes(int C) {
   return 1024 + 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize +
-         sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + sizeof(uint64_t) * 128 +
+         sizeof(TileMeta) * kMetas + sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + sizeof(uint64_t) * 128 +
          sizeof(int) * (6 * 64 + 8 * 64 + 3 * 64 + 6) + sizeof(int) * (2 * C + 1);
 }
 
@@ -87,6 +88,8 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.q = s.p + 2 * kPTile;
   s.ring = s.q + 2 * CF::kQTile;
   b += 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize;
+  s.meta = reinterpret_cast<TileMeta*>(b);
+  b += sizeof(TileMeta) * kMetas;
   s.cfull = smem_addr(b);
   s.cempty = s.cfull + 8 * CF::kStages;
   s.kfull = s.cempty + 8 * CF::kStages;
@@ -98,6 +101,7 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.qempty = s.qfull + 16;
   s.mmadone = s.qempty + 16;
   s.ofree = s.mmadone + 16;
+  s.joined = s.ofree + 8;
   s.anc = reinterpret_cast<uint64_t*>(b) + 2 * CF::kStages + kBarriers;
   s.row_anc = s.anc + 64;
   s.ref = reinterpret_cast<float*>(s.row_anc + 64);
@@ -116,21 +120,34 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   return s;
 }
 
-// q of every piece as f16, rows of 64 dims in two halves (K-major B of QK^T, 128-byte swizzle).
+// q of every piece as f16, rows of 64 dims in two halves (K-major B of QK^T, 128-byte swizzle).  This warp reads every
+// tile's words, and counts among the readers of a stage, so that it cannot fall behind the ring.
 template <class CF>
-__device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, const Waiter& wait, Piece next) {
+__device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, const Waiter& wait) {
   const AttnParams& p = kp.a;
   const Smem sm = smem;
   const int lane = threadIdx.x & 31;
   wait_for_prerequisite_grid();
-  for (int piece = 0; next_piece(p, sm.len, next); ++piece) {
-    const Piece w = next;
+  int stage = 0, piece = 0;
+  uint32_t phase = 0;
+#pragma unroll 1
+  for (int t = 0;; ++t) {
+    if (!__all_sync(0xffffffffu, wait(sm.cfull + 8 * stage, phase))) return;
+    const TileMeta w = sm.meta[t % kMetas];
+    if (lane == 0) mbar_arrive(sm.cempty + 8 * stage);
+    if (++stage == CF::kStages) {
+      stage = 0;
+      phase ^= 1u;
+    }
+    if (w.flags & kStop) return;
+    if (!(w.flags & kFirst)) continue;
     const int b = piece & 1;
     if (!__all_sync(0xffffffffu, wait(sm.qempty + 8 * b, ((piece >> 1) & 1) ^ 1u))) return;
+    ++piece;
     const __nv_bfloat16* q = p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim;
     const int row0 = w.rb * p.rows_per_unit, rows = min(p.rows_per_unit, p.rows_total - row0);
     const int ch = lane & 15;
-#pragma unroll 4
+#pragma unroll 8
     for (int r = lane >> 4; r < CF::kNT; r += 2) {
       uint4 x = make_uint4(0u, 0u, 0u, 0u);
       if (r < rows) {
@@ -185,7 +202,7 @@ __device__ __forceinline__ void decode32(uint32_t src, uint32_t scales, uint32_t
 
 // A decoding warpgroup: the tiles t % 2 == wg, a key to a thread.
 template <class CF>
-__device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem, Piece next) {
+__device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem) {
   const AttnParams& p = kp.a;
   const Smem sm = smem;
   const int lane = threadIdx.x & 31, key = threadIdx.x & 127, wg = (threadIdx.x >> 7) & 1;
@@ -195,69 +212,75 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
   const uint32_t kdst = tmem + (static_cast<uint32_t>(key & 96) << 16) + CF::kTmemK + 64 * wg;
   const uint32_t vdst = sm.v + wg * kVTile + key * 128, sw = static_cast<uint32_t>(key & 7) << 4;
   const uint32_t qkdone = sm.qkdone + 8 * wg, pvdone = sm.pvdone + 8 * wg, kfull = sm.kfull + 8 * wg, vfull = sm.vfull + 8 * wg;
-  int stage = wg, t = 0;  // t: the piece's first tile
+  int stage = wg;
   uint32_t phase = 0, freed = 1;
-  for (; next_piece(p, sm.len, next); t += next.lt1 - next.lt0) {
-    const Piece w = next;
-    // Keys that no row sees may hold anything; V of them must not be NaN (0 * NaN).
-    const int lo = p.window > 0 ? w.L + p.min_depth - p.window : 0;
 #pragma unroll 1
-    for (int lt = w.lt0 + ((t ^ wg) & 1); lt < w.lt1; lt += 2) {
-      const bool draft = w.draft(lt);
-      // The tile's bytes; K's buffer: QK^T of its previous tile is done.
-      bool ok = wait(sm.cfull + 8 * stage, phase);
-      ok = ok && wait(qkdone, freed);
-      if (!__all_sync(0xffffffffu, ok)) return;
-      tc_fence_after();
-      const uint32_t src = src0 + stage * kStageSize;
-      if (!draft) {
-        uint2 sc = lds64(src + scale0);
-#pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          uint32_t o[16];
-          decode32(src + c * kChunkStride, sc.x, o);
-          tmem_st16(kdst + 16 * c, o);
-          sc.x = __funnelshift_r(sc.x, sc.y, 16);
-          sc.y >>= 16;
-        }
-      } else {
-        decode_draft<false>(draft0 + stage * kStageSize, key < w.nkeys(lt, p.N), kdst, sw);
-      }
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(kfull);
-      // V's buffer: P.V of its previous tile is done.
+  for (int t = wg;; t += 2) {
+    // The tile's bytes; K's buffer: QK^T of its previous tile is done.
+    bool ok = wait(sm.cfull + 8 * stage, phase);
+    ok = ok && wait(qkdone, freed);
+    if (!__all_sync(0xffffffffu, ok)) return;
+    tc_fence_after();
+    const int4 meta = *reinterpret_cast<const int4*>(sm.meta + t % kMetas);  // flags, key0, nkeys, L
+    if (meta.x & kStop) {
+      // (P.V of the tile before has to have seen its V, whose phase this one ends.)
       if (!__all_sync(0xffffffffu, wait(pvdone, freed))) return;
-      if (!draft) {
-        uint2 sc = lds64(src + scale0 + kScaleBytes);
-        if (w.masked(lt, lo, p.sinks)) {
-          const int at = w.key0(lt) + key;
-          if (at >= w.L || (at < lo && at >= p.sinks)) sc = make_uint2(0u, 0u);  // (any code times 0 is 0)
-        }
-#pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          uint32_t o[16];
-          decode32(src + kVCodes + c * kChunkStride, sc.x, o);
-          put_v(vdst, sw, c, o);
-          sc.x = __funnelshift_r(sc.x, sc.y, 16);
-          sc.y >>= 16;
-        }
-      } else {
-        decode_draft<true>(draft0 + kDraftV + stage * kStageSize, key < w.nkeys(lt, p.N), vdst, sw);
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
       if (lane == 0) {
-        mbar_arrive(sm.cempty + 8 * stage);
+        mbar_arrive(kfull);
         mbar_arrive(vfull);
       }
-      freed ^= 1u;
-      stage += 2;
-      if (stage >= CF::kStages) {
-        stage -= CF::kStages;
-        phase ^= 1u;
+      return;
+    }
+    const bool draft = meta.x & kDraft;
+    const uint32_t src = src0 + stage * kStageSize;
+    if (!draft) {
+      uint2 sc = lds64(src + scale0);
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        uint32_t o[16];
+        decode32(src + c * kChunkStride, sc.x, o);
+        tmem_st16(kdst + 16 * c, o);
+        sc.x = __funnelshift_r(sc.x, sc.y, 16);
+        sc.y >>= 16;
       }
+    } else {
+      decode_draft<false>(draft0 + stage * kStageSize, key < meta.z, kdst, sw);
+    }
+    tmem_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(kfull);
+    // V's buffer: P.V of its previous tile is done.
+    if (!__all_sync(0xffffffffu, wait(pvdone, freed))) return;
+    if (!draft) {
+      uint2 sc = lds64(src + scale0 + kScaleBytes);
+      if (meta.x & kMasked) {
+        // Keys that no row sees may hold anything; V of them must not be NaN (0 * NaN; any code times 0 is 0).
+        const int at = meta.y + key, lo = p.window > 0 ? meta.w + p.min_depth - p.window : 0;
+        if (key >= meta.z || (at < lo && at >= p.sinks)) sc = make_uint2(0u, 0u);
+      }
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        uint32_t o[16];
+        decode32(src + kVCodes + c * kChunkStride, sc.x, o);
+        put_v(vdst, sw, c, o);
+        sc.x = __funnelshift_r(sc.x, sc.y, 16);
+        sc.y >>= 16;
+      }
+    } else {
+      decode_draft<true>(draft0 + kDraftV + stage * kStageSize, key < meta.z, vdst, sw);
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(sm.cempty + 8 * stage);
+      mbar_arrive(vfull);
+    }
+    freed ^= 1u;
+    stage += 2;
+    if (stage >= CF::kStages) {
+      stage -= CF::kStages;
+      phase ^= 1u;
     }
   }
 }
@@ -268,84 +291,81 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sync(0xffffffffu, x); }
 
 template <class CF>
-__device__ __forceinline__ void run_qk(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem_base, Piece next) {
-  const AttnParams& p = kp.a;
+__device__ __forceinline__ void run_qk(const Smem& smem, const Waiter& wait, uint32_t tmem_base) {
   const Smem sm = smem;
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, false);
   const uint32_t tmem = uniform(tmem_base);
   const uint64_t q0 = smem_desc_sw128(sm.q, 16, 1024);
   uint32_t phase = 0;  // of the buffers' tiles: flips after the second one
-  int t = 0;
-  for (int piece = 0; __all_sync(0xffffffffu, next_piece(p, sm.len, next)); ++piece) {
-    const int tiles = uniform(next.lt1 - next.lt0);
-    if (!__all_sync(0xffffffffu, wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1))) break;
-    const uint64_t q = q0 + (piece & 1) * (CF::kQTile >> 4);
-    // The tile in buffers b.
-    auto step = [&](auto buffer) {
-      constexpr int b = decltype(buffer)::value;
-      bool ok = wait(sm.pfull + 8 * b, phase ^ 1u);  // S of the tile before the last has been read
-      ok = ok && wait(sm.kfull + 8 * b, phase);
-      if (!__all_sync(0xffffffffu, ok)) return false;
+  int t = 0, piece = -1, stops = 0;
+  // The tile in buffers b; false when a wait has given up.
+  auto step = [&](auto buffer) {
+    constexpr int b = decltype(buffer)::value;
+    bool ok = wait(sm.pfull + 8 * b, phase ^ 1u);  // S of the tile before the last has been read
+    ok = ok && wait(sm.kfull + 8 * b, phase);
+    if (!__all_sync(0xffffffffu, ok)) return false;
+    const uint32_t flags = uniform(sm.meta[t % kMetas].flags);
+    if (flags & kStop) {
+      ++stops;  // (its S is nothing, and the softmax sees that)
+    } else {
+      if (flags & kFirst) {
+        ++piece;
+        if (!__all_sync(0xffffffffu, wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1))) return false;
+      }
       tc_fence_after();
+      const uint64_t q = q0 + (piece & 1) * (CF::kQTile >> 4);
 #pragma unroll
       for (int ks = 0; ks < kHeadDim / 16; ++ks)
         tc_mma_tmem_a_elect(tmem + CF::kTmemS + b * CF::kNT, tmem + CF::kTmemK + 64 * b + 8 * ks,
                             q + (((ks >> 2) * (CF::kNT * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
-      tc_commit_elect(sm.qkdone + 8 * b);
-      return true;
-    };
-    bool ok = true;
-#pragma unroll 1
-    for (int i = 0; ok && i < tiles; ++i, ++t) {
-      if ((t & 1) == 0) {
-        ok = step(std::integral_constant<int, 0>{});
-      } else {
-        ok = step(std::integral_constant<int, 1>{});
-        phase ^= 1u;
-      }
+      if (flags & kLast) tc_commit_elect(sm.qempty + 8 * (piece & 1));
     }
-    if (!ok) break;
-    tc_commit_elect(sm.qempty + 8 * (piece & 1));
+    tc_commit_elect(sm.qkdone + 8 * b);
+    ++t;
+    return stops < 2;
+  };
+#pragma unroll 1
+  for (;;) {
+    if (!step(std::integral_constant<int, 0>{}) || !step(std::integral_constant<int, 1>{})) break;
+    phase ^= 1u;
   }
   tc_commit_elect(sm.mmadone);
 }
 
 template <class CF>
-__device__ __forceinline__ void run_pv(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem_base, Piece next) {
-  const AttnParams& p = kp.a;
+__device__ __forceinline__ void run_pv(const Smem& smem, const Waiter& wait, uint32_t tmem_base) {
   const Smem sm = smem;
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, true, true);
   const uint32_t tmem = uniform(tmem_base);
   const uint64_t v0 = smem_desc_sw128(sm.v, kVHalf, 1024), p0 = smem_desc_sw128(sm.p, kPTile, 1024);
   uint32_t phase = 0;
-  int t = 0;
-  for (int piece = 0; __all_sync(0xffffffffu, next_piece(p, sm.len, next)); ++piece) {
-    const int tiles = uniform(next.lt1 - next.lt0);
-    if (piece > 0 && !__all_sync(0xffffffffu, wait(sm.ofree, (piece - 1) & 1))) break;
-    auto step = [&](auto buffer, uint32_t more) {  // more: the accumulator holds tiles of this piece
-      constexpr int b = decltype(buffer)::value;
-      bool ok = wait(sm.vfull + 8 * b, phase);
-      ok = ok && wait(sm.pfull + 8 * b, phase);
-      if (!__all_sync(0xffffffffu, ok)) return false;
-      tc_fence_after();
-#pragma unroll
-      for (int k16 = 0; k16 < kTile / 16; ++k16)  // two 8-key groups of 1 KB each
-        tc_mma_elect(tmem + CF::kTmemO + (CF::kByTile ? b * CF::kNT : 0), v0 + ((b * kVTile + k16 * 2048) >> 4),
-                     p0 + ((b * kPTile + k16 * 2048) >> 4), idesc, k16 > 0 ? 1u : more);
-      tc_commit_elect(sm.pvdone + 8 * b);
-      return true;
-    };
-    bool ok = true;
-#pragma unroll 1
-    for (int i = 0; ok && i < tiles; ++i, ++t) {
-      if ((t & 1) == 0) {
-        ok = step(std::integral_constant<int, 0>{}, i >= CF::kAccs);
-      } else {
-        ok = step(std::integral_constant<int, 1>{}, i >= CF::kAccs);
-        phase ^= 1u;
-      }
+  int t = 0, piece = -1, in_piece = 0;
+  auto step = [&](auto buffer) {
+    constexpr int b = decltype(buffer)::value;
+    if (!__all_sync(0xffffffffu, wait(sm.vfull + 8 * b, phase))) return false;
+    const uint32_t flags = uniform(sm.meta[t % kMetas].flags);
+    if (flags & kStop) return false;
+    bool ok = wait(sm.pfull + 8 * b, phase);
+    if (flags & kFirst) {
+      in_piece = 0;
+      if (++piece > 0) ok = ok && wait(sm.ofree, (piece - 1) & 1);
     }
-    if (!ok) break;
+    if (!__all_sync(0xffffffffu, ok)) return false;
+    tc_fence_after();
+    const uint32_t more = in_piece >= CF::kAccs;  // the accumulator holds tiles of this piece
+#pragma unroll
+    for (int k16 = 0; k16 < kTile / 16; ++k16)  // two 8-key groups of 1 KB each
+      tc_mma_elect(tmem + CF::kTmemO + (CF::kByTile ? b * CF::kNT : 0), v0 + ((b * kVTile + k16 * 2048) >> 4),
+                   p0 + ((b * kPTile + k16 * 2048) >> 4), idesc, k16 > 0 ? 1u : more);
+    tc_commit_elect(sm.pvdone + 8 * b);
+    ++t;
+    ++in_piece;
+    return true;
+  };
+#pragma unroll 1
+  for (;;) {
+    if (!step(std::integral_constant<int, 0>{}) || !step(std::integral_constant<int, 1>{})) break;
+    phase ^= 1u;
   }
   tc_commit_elect(sm.mmadone + 8);
 }
@@ -435,13 +455,13 @@ __device__ __noinline__ void rescale_o(const float* alpha, int n, uint32_t o_col
 // A piece's rows [j0, j1) of this thread's dim: the final ones, or the piece's part in the workspace.  kAccs 2: O and the
 // other accumulator `next` columns on, each with its own weights (0: it holds nothing).
 template <int kAccs>
-__device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, const Piece& w, int j0, int j1, uint32_t o_cols,
+__device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, const TileMeta& w, int j0, int j1, uint32_t o_cols,
                                         int next) {
   const int tid = threadIdx.x & 127;
   const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
   const size_t row0 = static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G;
-  const size_t part = static_cast<size_t>(w.c * p.hkv * p.row_blocks + w.hr + blockIdx.x) * p.rows_per_unit;
-  const bool whole = w.whole();
+  const size_t part = static_cast<size_t>((w.c * p.hkv + w.h) * p.row_blocks + w.rb + blockIdx.x) * p.rows_per_unit;
+  const bool whole = w.flags & kWhole;
 #pragma unroll 1
   for (int j = j0; j < j1; j += 4) {
     uint32_t o[4], o2[4];
@@ -466,7 +486,7 @@ __device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, con
 // The rows' sums, weights of the accumulators and log-sum-exp.  Thread = row.  had: whether each accumulator holds tiles
 // of this piece.
 template <class CF>
-__device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, const Piece& w, int j, bool had0, bool had1) {
+__device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, const TileMeta& w, int j, bool had0, bool had1) {
   const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
   auto total = [&](int wg, int col) {
     const int* x = sm.wmax + wg * 256 + col;
@@ -489,12 +509,12 @@ __device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, cons
   }
   if (j >= rows) return;
   const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
-  if (w.whole()) p.lse[static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G + sm.place[j]] = lse2 * 0.69314718055994531f;
-  else p.ws_lse[static_cast<size_t>(w.c * p.hkv * p.row_blocks + w.hr + blockIdx.x) * p.rows_per_unit + j] = lse2;
+  if (w.flags & kWhole) p.lse[static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G + sm.place[j]] = lse2 * 0.69314718055994531f;
+  else p.ws_lse[static_cast<size_t>((w.c * p.hkv + w.h) * p.row_blocks + w.rb + blockIdx.x) * p.rows_per_unit + j] = lse2;
 }
 
 template <class CF>
-__device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem, Piece next) {
+__device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem) {
   constexpr int NC = CF::kCols;
   const AttnParams& p = kp.a;
   const Smem sm = smem;
@@ -507,109 +527,28 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
   float* alpha = sm.alpha + (CF::kByTile ? 64 * wg : col0);
   int* wmax = sm.wmax + 256 * wg;
   const int bar = kBarGroup + wg;
-  int unit_rb = -1, unit_seq = -1, t0 = 0;
-  bool dead = false;  // this warpgroup has given up: it only keeps up the barriers of both
-  wait_for_prerequisite_grid();  // outputs and scratch may be the preceding kernel's
-  for (; next_piece(p, sm.len, next); t0 += next.lt1 - next.lt0) {
-    const Piece w = next;
-    if (w.rb != unit_rb || (p.tree && w.seq != unit_seq)) {
-      load_rows(p, smem, CF::kNC, w.rb, w.seq, p.tree && w.seq != unit_seq, kBarSoftmax, kSoftmaxThreads);
-      unit_rb = w.rb;
-      unit_seq = w.seq;
-    }
+  WarpSync sync{sm.joined, 0};
+  float2 l[NC / 2];               // sums over this thread's keys
+  bool in_codes = false;          // O is in units of the value codes
+  wait_for_prerequisite_grid();   // outputs and scratch may be the preceding kernel's
+  bool fresh = true;              // this warpgroup has had no tile of the piece
+  int t_first = 0;                // the piece's first tile
+  bool good = true;               // no wait of this warp has given up
+  auto begin = [&](int t) {
+    const TileMeta w = sm.meta[t % kMetas];
+    if (!sync(wait)) return false;  // the piece before has been written out
+    if ((w.flags & kNewRows) &&
+        !load_rows(p, smem, CF::kNC, w.rb, w.seq, w.flags & kNewTree, kSoftmaxThreads, sync, wait))
+      return false;
     if (key < NC) ref[key] = -kNoRef;
-    named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
-    float2 l[NC / 2];  // sums over this thread's keys
 #pragma unroll
     for (int j = 0; j < NC / 2; ++j) l[j] = make_float2(0.f, 0.f);
-    // Tiles from here on (or before the sinks' end) are seen whole by every row.
-    int seen_from = 0;
-    if (p.window > 0) {
-      int dmax = 0;
-#pragma unroll 1
-      for (int j = 0; j < CF::kNC; ++j) dmax = max(dmax, sm.depth[j]);
-      seen_from = w.L + dmax - p.window;
-    }
-    const int lt_first = w.lt0 + (CF::kByTile ? (t0 ^ wg) & 1 : 0);
-    bool in_codes = !w.draft(lt_first);  // O is in units of the value codes
-    int t = t0 + lt_first - w.lt0;
-#pragma unroll 1
-    for (int lt = lt_first; lt < w.lt1 && !dead; lt += CF::kAccs, t += CF::kAccs) {
-      const int b = CF::kByTile ? wg : t & 1;
-      const uint32_t phase = (t >> 1) & 1;
-      const bool draft = w.draft(lt);
-      const float qs = draft ? p.qscale : p.qscale * p.k_scale;
-      uint64_t vis = ~0ull;
-      if (draft || w.masked(lt, seen_from, p.sinks)) {
-        const int at = w.key0(lt) + key;
-        vis = key < w.nkeys(lt, p.N) ? visible_rows(p, smem, col0, NC, draft, at, w.L) : 0ull;
-      }
-      // S; and the buffer of P, free when P.V of the tile before the last is done (by tile: O is at rest then, too).
-      bool ok = wait(sm.qkdone + 8 * b, phase);
-      ok = ok && wait(sm.pvdone + 8 * b, phase ^ 1u);
-      ok = __all_sync(0xffffffffu, ok);
-      tc_fence_after();
-      const uint32_t scores = trow + CF::kTmemS + b * CF::kNT + col0;
-      const bool leave_codes = draft && in_codes && p.v_scale != 1.f;
-      if (draft) in_codes = false;
-      float2 x[NC / 2];
-      for (bool moved = false;; moved = true) {
-        uint32_t s[NC];
-        tmem_ld_cols<NC>(scores, s);
-        tmem_wait_ld();
-#pragma unroll
-        for (int j = 0; j < NC; j += 4) {
-          const float4 m = *reinterpret_cast<const float4*>(ref + j);  // (negated)
-          x[j / 2] = fma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), make_float2(qs, qs), make_float2(m.x, m.y));
-          x[j / 2 + 1] = fma2(make_float2(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), make_float2(qs, qs), make_float2(m.z, m.w));
-        }
-        if (vis != ~0ull) {
-#pragma unroll
-          for (int j = 0; j < NC; j += 2) {
-            if (!((vis >> j) & 1ull)) x[j / 2].x = -INFINITY;
-            if (!((vis >> j) & 2ull)) x[j / 2].y = -INFINITY;
-          }
-        }
-        if (moved) break;
-        float top = kRefLimit;
-#pragma unroll
-        for (int j = 0; j < NC / 2; ++j) top = max3(top, x[j].x, x[j].y);
-        if (!any_of(bar, kGroupThreads, top > kRefLimit || leave_codes || !ok)) break;
-        dead = any_of(bar, kGroupThreads, !ok);
-        if (dead) break;
-        move_references(wmax, ref, alpha, wg, NC, scores, qs, vis);  // always with a warpgroup's first keys of a piece
-#pragma unroll
-        for (int j = 0; j < NC / 2; ++j) {
-          l[j].x *= alpha[2 * j];
-          l[j].y *= alpha[2 * j + 1];
-        }
-        if (lt > lt_first) {
-          if constexpr (!CF::kByTile) {
-            dead = any_of(bar, kGroupThreads, !wait(sm.pvdone + 8 * (b ^ 1), ((t - 1) >> 1) & 1));
-            if (dead) break;
-            tc_fence_after();
-          }
-          rescale_o(alpha, NC, o_cols, leave_codes ? p.v_scale : 1.f);
-        }
-      }
-      if (dead) break;
-#pragma unroll
-      for (int j = 0; j < NC; j += 8) {
-        uint32_t pk[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 e = make_float2(ex2(x[j / 2 + i].x), ex2(x[j / 2 + i].y));
-          l[j / 2 + i] = add2(l[j / 2 + i], e);
-          pk[i] = pack_f16x2(e.x, e.y);
-        }
-        sts128(pdst + b * kPTile + ((static_cast<uint32_t>(col0 + j) << 1) ^ sw), make_uint4(pk[0], pk[1], pk[2], pk[3]));
-      }
-      fence_proxy_async_smem();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(sm.pfull + 8 * b);
-    }
-    // Sums over the keys' threads, then the rows.
+    in_codes = fresh = true;
+    t_first = t;
+    return sync(wait);
+  };
+  // A piece's end, at its last tile t: join the warpgroups and write the rows.
+  auto end = [&](int t) {
     int col = 0;
     float sums[NC];
 #pragma unroll
@@ -622,19 +561,100 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     for (int i = 0; i < NC; ++i)
       if (i < width) wmax[(key >> 5) * 64 + col + i] = __float_as_int(sums[i]);
     if (key == 0) sm.codes[wg] = in_codes;
-    if (!dead && lt_first < w.lt1) {  // O is at rest
-      const int last = t - CF::kAccs;
-      dead = !wait(sm.pvdone + 8 * (last & 1), (last >> 1) & 1);
-    }
-    if (any_of(kBarSoftmax, kSoftmaxThreads, dead)) return;
-    const bool two = w.lt1 - w.lt0 > 1;
-    if (threadIdx.x < CF::kNC) join_sums<CF>(p, smem, next, threadIdx.x, two || !(t0 & 1), two || (t0 & 1));
-    named_barrier_sync(kBarSoftmax, kSoftmaxThreads);
+    // O is at rest: P.V of this warpgroup's last tile of the piece is done.
+    const int mine = CF::kByTile && (t & 1) != wg ? t - 1 : t;
+    const bool ok = fresh || wait(sm.pvdone + 8 * (mine & 1), (mine >> 1) & 1);
+    if (!__all_sync(0xffffffffu, ok) || !sync(wait)) return false;
+    const bool two = t > t_first;
+    if (threadIdx.x < CF::kNC) join_sums<CF>(p, smem, smem.meta[t % kMetas], threadIdx.x, two || !(t & 1), two || (t & 1));
+    if (!sync(wait)) return false;
     tc_fence_after();
-    write_rows<CF::kAccs>(p, smem, next, wg * (CF::kNC / 2), (wg + 1) * (CF::kNC / 2), trow + CF::kTmemO, CF::kNT);
+    write_rows<CF::kAccs>(p, smem, smem.meta[t % kMetas], wg * (CF::kNC / 2), (wg + 1) * (CF::kNC / 2), trow + CF::kTmemO, CF::kNT);
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(sm.ofree);
+    return true;
+  };
+#pragma unroll 1
+  for (int t = CF::kByTile ? wg : 0;; t += CF::kAccs) {
+    const int b = CF::kByTile ? wg : t & 1;
+    const uint32_t phase = (t >> 1) & 1;
+    // S, and with it the words of the tile and of those before it.  (A warp whose wait gives up goes on to the vote: the
+    // warps of a warpgroup leave there, together.)
+    good = good && __all_sync(0xffffffffu, wait(sm.qkdone + 8 * b, phase));
+    if (CF::kByTile && good && t > 0) {  // the tile before is the other warpgroup's
+      const int flags = sm.meta[(t - 1) % kMetas].flags;
+      if (flags & kFirst) good = begin(t - 1);
+      if (good && (flags & kLast)) good = end(t - 1);
+    }
+    const int4 meta = *reinterpret_cast<const int4*>(sm.meta + t % kMetas);  // flags, key0, nkeys, L
+    const bool stop = good && (meta.x & kStop);
+    if (good && (meta.x & kFirst) && !stop) good = begin(t);
+    const bool draft = meta.x & kDraft;
+    const float qs = draft ? p.qscale : p.qscale * p.k_scale;
+    uint64_t vis = ~0ull;
+    if (meta.x & kMasked) vis = rows_seeing(p, smem, meta, meta.w, col0, NC, key);
+    // The buffer of P is free when P.V of the tile before the last is done (by tile: O is at rest then, too).
+    good = good && (stop || __all_sync(0xffffffffu, wait(sm.pvdone + 8 * b, phase ^ 1u)));
+    tc_fence_after();
+    const uint32_t scores = trow + CF::kTmemS + b * CF::kNT + col0;
+    const bool leave_codes = draft && in_codes && !fresh && p.v_scale != 1.f;
+    if (draft) in_codes = false;
+    float2 x[NC / 2];
+    for (bool moved = false;; moved = true) {
+      uint32_t s[NC];
+      tmem_ld_cols<NC>(scores, s);
+      tmem_wait_ld();
+#pragma unroll
+      for (int j = 0; j < NC; j += 4) {
+        const float4 m = *reinterpret_cast<const float4*>(ref + j);  // (negated)
+        x[j / 2] = fma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), make_float2(qs, qs), make_float2(m.x, m.y));
+        x[j / 2 + 1] = fma2(make_float2(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), make_float2(qs, qs), make_float2(m.z, m.w));
+      }
+      if (vis != ~0ull) {
+#pragma unroll
+        for (int j = 0; j < NC; j += 2) {
+          if (!((vis >> j) & 1ull)) x[j / 2].x = -INFINITY;
+          if (!((vis >> j) & 2ull)) x[j / 2].y = -INFINITY;
+        }
+      }
+      if (moved) break;
+      float top = kRefLimit;
+#pragma unroll
+      for (int j = 0; j < NC / 2; ++j) top = max3(top, x[j].x, x[j].y);
+      if (!any_of(bar, kGroupThreads, top > kRefLimit || leave_codes || !good || stop)) break;
+      if (any_of(bar, kGroupThreads, !good) || stop) return;
+      move_references(wmax, ref, alpha, wg, NC, scores, qs, vis);  // always with a warpgroup's first keys of a piece
+#pragma unroll
+      for (int j = 0; j < NC / 2; ++j) {
+        l[j].x *= alpha[2 * j];
+        l[j].y *= alpha[2 * j + 1];
+      }
+      if (!fresh) {
+        if constexpr (!CF::kByTile) {
+          if (any_of(bar, kGroupThreads, !wait(sm.pvdone + 8 * (b ^ 1), ((t - 1) >> 1) & 1))) return;
+          tc_fence_after();
+        }
+        rescale_o(alpha, NC, o_cols, leave_codes ? p.v_scale : 1.f);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NC; j += 8) {
+      uint32_t pk[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 e = make_float2(ex2(x[j / 2 + i].x), ex2(x[j / 2 + i].y));
+        l[j / 2 + i] = add2(l[j / 2 + i], e);
+        pk[i] = pack_f16x2(e.x, e.y);
+      }
+      sts128(pdst + b * kPTile + ((static_cast<uint32_t>(col0 + j) << 1) ^ sw), make_uint4(pk[0], pk[1], pk[2], pk[3]));
+    }
+    fence_proxy_async_smem();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(sm.pfull + 8 * b);
+    fresh = false;
+    if (meta.x & kLast) good = end(t);
   }
 }
 
@@ -644,11 +664,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   const AttnParams& p = kp.a;
   if (threadIdx.x == 0) allow_dependent_launch();  // the merge may be scheduled as CTAs finish
   const Smem sm = carve<CF>(smem_raw, p.C);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
+#pragma unroll 1
     for (int s = 0; s < CF::kStages; ++s) {
       mbar_init(sm.cfull + 8 * s, 1);
-      mbar_init(sm.cempty + 8 * s, 4);
+      mbar_init(sm.cempty + 8 * s, 5);  // a decoding warpgroup's warps, and the one that stages q
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(sm.kfull + 8 * b, 4);
@@ -661,6 +682,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
       mbar_init(sm.mmadone + 8 * b, 1);
     }
     mbar_init(sm.ofree, 8);
+    mbar_init(sm.joined, 8);
     *sm.abort = 0;
     *sm.issued = 0;
     fence_mbar_init();
@@ -670,25 +692,22 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
     tmem_relinquish();
   }
   tc_fence_before();
-  build_kv4_plan(p, sm.len, sm.base);  // (barriers inside)
+  __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *sm.tmem;
   const Waiter wait{p.err, p.wait_ns, sm.abort, p.wait_ns < kPollBelowNs};
-  Piece w;
-  begin_pieces(p, sm.len, sm.base, w);
-  if (warp < kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem, w);
-  else if (warp < kWarpLoad) run_decode<CF>(kp, sm, wait, tmem, w);
-  else if (warp == kWarpLoad) run_loader<CF::kStages>(kp, sm, wait, w);
-  else if (warp == kWarpQk) run_qk<CF>(kp, sm, wait, tmem, w);
-  else if (warp == kWarpPv) run_pv<CF>(kp, sm, wait, tmem, w);
-  else if (warp == kWarpQ) run_q<CF>(kp, sm, wait, w);
+  if (warp < kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem);
+  else if (warp < kWarpLoad) run_decode<CF>(kp, sm, wait, tmem);
+  else if (warp == kWarpLoad) run_loader<CF::kStages, 2>(kp, sm, wait);  // (a last word for each warpgroup)
+  else if (warp == kWarpQk) run_qk<CF>(sm, wait, tmem);
+  else if (warp == kWarpPv) run_pv<CF>(sm, wait, tmem);
+  else run_q<CF>(kp, sm, wait);
   __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0) {
     // No copy or MMA outlives the CTA, whatever ended it (each wait is bounded).
-    for (int k = max(0, *sm.issued - CF::kStages); k < *sm.issued; ++k)
-      if (!mbar_wait(sm.cfull + 8 * (k % CF::kStages), (k / CF::kStages) & 1, p.err)) break;
+    drain<CF::kStages>(p, sm);
     mbar_wait(sm.mmadone, 0, p.err);
     mbar_wait(sm.mmadone + 8, 0, p.err);
   }

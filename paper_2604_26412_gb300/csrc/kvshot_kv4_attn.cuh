@@ -37,12 +37,29 @@ constexpr float kRefBelow = 8.f, kRefLimit = 15.f;
 constexpr float kNoRef = -1e30f;                   // no score yet
 
 
+// What the loading warp says of a tile, beside the tile's bytes.  The other warps follow these words alone: the plan, with
+// its divisions, is code of one warp.  (Code that a CTA runs once costs it ~20 cycles per instruction, most of them spent
+// fetching it: with the plan in every role, finding a piece took each of them 1300 to 3300 cycles.)
+constexpr int kFirst = 1, kLast = 2;   // of the CTA's piece of a unit
+constexpr int kDraft = 4;              // bf16 draft keys, else codes
+constexpr int kMasked = 8;             // holds keys that some query row does not see
+constexpr int kWhole = 16;             // the piece is the whole unit
+constexpr int kNewRows = 32;           // the query rows' nodes differ from the piece's before
+constexpr int kNewTree = 64;           // and so does the draft tree
+constexpr int kStop = 128;             // no tile: the CTA's work is done
+struct TileMeta {
+  int flags, key0, nkeys, L;  // first key (token, or draft slot), valid keys, prefix length
+  int c, h, rb, seq;          // cache, KV head, row block, sequence
+};
+constexpr int kMetas = 16;    // more than the tiles between the loader and the last reader
+
 // Shared-memory parts that both kernels have: the ring of the cache's bytes (addresses of its stages and of its barriers,
-// landed and read), and the query rows' nodes.
+// landed and read) with the tiles' words, and the query rows' nodes.
 struct Ring {
   uint32_t ring, cfull, cempty;
+  TileMeta* meta;   // [kMetas]
   int* issued;      // tiles issued by the loader
-  int *len, *base;  // the plan
+  int *len, *base;  // the loader's plan
 };
 struct Rows {
   uint64_t *anc, *row_anc;  // [64] each node's ancestors and itself (tree); of each query row's node
@@ -77,115 +94,7 @@ struct Waiter {
   }
 };
 
-// ------------------------------------------------------------ work plan
-
-__device__ __forceinline__ void build_kv4_plan(const AttnParams& p, int* s_len, int* s_base) {
-  const int HR = p.hkv * p.row_blocks;
-  for (int c = threadIdx.x; c < p.C; c += blockDim.x) {
-    const int L = clamp_len(p, c);
-    s_len[c] = L;
-    s_base[c + 1] = (window_span<kTile>(p, L).tiles + p.draft_tiles) * HR;
-  }
-  __syncthreads();
-  if (p.unit_ctas > 0) return;  // one cache: the cut needs its length alone
-  if (threadIdx.x < 32) {
-    const int lane = threadIdx.x, per = (p.C + 31) / 32, c0 = min(p.C, lane * per), c1 = min(p.C, c0 + per);
-    int v = 0;
-    for (int c = c0; c < c1; ++c) v += s_base[c + 1];
-    int scan = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int t = __shfl_up_sync(0xffffffffu, scan, o);
-      if (lane >= o) scan += t;
-    }
-    int below = scan - v;
-    for (int c = c0; c < c1; ++c) {
-      below += s_base[c + 1];
-      s_base[c + 1] = below;
-    }
-    if (lane == 0) s_base[0] = 0;
-  }
-  __syncthreads();
-}
-
-// A run of tiles of one unit that this CTA takes.
-struct Piece {
-  int t, t_end;        // tile of this CTA's range: the piece's first one (its end after next_piece), and the range's end
-  int c, hr;           // cache, KV head x row block
-  int lt0, lt1, ut;    // the piece's tiles of the unit [lt0, lt1), tiles of the unit
-  int h, rb, seq, L;   // KV head, row block, sequence, prefix length
-  WindowSpan span;
-
-  // First key of tile lt (token, or draft slot), and its valid keys.
-  __device__ __forceinline__ bool draft(int lt) const { return lt >= span.tiles; }
-  __device__ __forceinline__ int key0(int lt) const {
-    return draft(lt) ? (lt - span.tiles) * kDraftTile : (lt < span.sink_tiles ? lt : lt + span.skip) * kTile;
-  }
-  __device__ __forceinline__ int nkeys(int lt, int n_nodes) const {
-    return draft(lt) ? min(kDraftTile, n_nodes - key0(lt)) : min(kTile, L - key0(lt));
-  }
-  // Whether prefix tile lt holds keys past the last one, or from the sinks' end up to `from`, where a window begins.
-  __device__ __forceinline__ bool masked(int lt, int from, int sinks) const {
-    const int k = key0(lt);
-    return k + kTile > L || (k < from && k + kTile > sinks);
-  }
-  __device__ __forceinline__ bool whole() const { return lt0 == 0 && lt1 == ut; }
-};
-
-// The CTA's range; next_piece finds its first piece.
-__device__ __noinline__ void begin_pieces(const AttnParams& p, const int* s_len, const int* s_base, Piece& w) {
-  w.c = w.hr = w.lt1 = w.ut = w.t = w.t_end = 0;
-  if (p.unit_ctas > 0) {
-    w.ut = window_span<kTile>(p, s_len[0]).tiles + p.draft_tiles;
-    const UnitCut u = unit_cut(p.unit_ctas, w.ut);
-    w.hr = blockIdx.x / u.per;
-    w.lt1 = (blockIdx.x - w.hr * u.per) * u.tpc;
-    w.t_end = w.hr < p.hkv * p.row_blocks ? min(u.tpc, w.ut - w.lt1) : 0;
-    return;
-  }
-  const int total = s_base[p.C], tpc = tiles_per_cta(total, p.num_ctas);
-  w.t = min(total, static_cast<int>(blockIdx.x) * tpc);
-  w.t_end = min(total, w.t + tpc);
-  if (w.t >= w.t_end) return;
-  int lo = 0, hi = p.C - 1;  // last cache whose first tile is <= t
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (s_base[mid] <= w.t) lo = mid;
-    else hi = mid - 1;
-  }
-  w.c = lo;
-  w.ut = window_span<kTile>(p, s_len[lo]).tiles + p.draft_tiles;
-  const int rem = w.t - s_base[lo];
-  w.hr = rem / w.ut;
-  w.lt1 = rem - w.hr * w.ut;
-}
-
-// Moves on to the next piece of the range; false at its end.  (Out of line: the roles' loops over the tiles are short.)
-__device__ __noinline__ bool next_piece(const AttnParams& p, const int* s_len, Piece& w) {
-  if (w.t >= w.t_end) return false;
-  if (w.lt1 == w.ut) {
-    w.lt1 = 0;
-    if (++w.hr == p.hkv * p.row_blocks) {
-      w.hr = 0;
-      ++w.c;
-    }
-  }
-  w.L = s_len[w.c];
-  w.span = window_span<kTile>(p, w.L);
-  w.ut = w.span.tiles + p.draft_tiles;
-  w.lt0 = w.lt1;
-  w.lt1 = min(w.ut, w.lt0 + w.t_end - w.t);
-  w.t += w.lt1 - w.lt0;
-  w.h = w.hr / p.row_blocks;
-  w.rb = w.hr - w.h * p.row_blocks;
-  w.seq = w.c / (p.C / p.B);
-  return true;
-}
-
 // ------------------------------------------------------------ loads
-
-// The roles keep copies of their own of what they also hand to functions out of line: a variable whose address has been
-// given away is read from local memory again after every barrier and copy.
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
@@ -193,44 +102,122 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-// The loading warp: one stage per tile, a copy per run of groups (a draft tile: two per row).
-template <int kStages>
-__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring, const Waiter& wait, Piece next) {
+// Tiles per cache and their sums (sm.len, sm.base), by one warp.
+__device__ __forceinline__ void build_kv4_plan(const AttnParams& p, int HR, int* s_len, int* s_base) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int c = lane; c < p.C; c += 32) {
+    const int L = clamp_len(p, c);
+    s_len[c] = L;
+    s_base[c + 1] = (window_span<kTile>(p, L).tiles + p.draft_tiles) * HR;
+  }
+  __syncwarp();
+  const int per = (p.C + 31) / 32, c0 = min(p.C, lane * per), c1 = min(p.C, c0 + per);
+  int v = 0;
+#pragma unroll 1
+  for (int c = c0; c < c1; ++c) v += s_base[c + 1];
+  int below = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int t = __shfl_up_sync(0xffffffffu, below, o);
+    if (lane >= o) below += t;
+  }
+  below -= v;
+#pragma unroll 1
+  for (int c = c0; c < c1; ++c) {
+    below += s_base[c + 1];
+    s_base[c + 1] = below;
+  }
+  if (lane == 0) s_base[0] = 0;
+  __syncwarp();
+}
+
+// The loading warp: the CTA's tiles, one after another, each a stage of the ring with a copy per run of groups (a draft
+// tile: two per row); at the end `kStops` tiles that say so.
+template <int kStages, int kStops>
+__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring, const Waiter& wait) {
   const AttnParams& p = kp.a;
   const Ring sm = ring;
-  const int lane = threadIdx.x & 31;
-  int stage = 0, issued = 0;
+  const int lane = threadIdx.x & 31, HR = p.hkv * p.row_blocks;
+  // This CTA's range [t, t_end): cache c, KV head x row block hr, tile lt of the unit.
+  int t = 0, t_end, c = 0, hr = 0, lt = 0;
+  if (p.unit_ctas > 0) {
+    if (lane == 0) sm.len[0] = clamp_len(p, 0);
+    __syncwarp();
+    const int ut = window_span<kTile>(p, sm.len[0]).tiles + p.draft_tiles;
+    const UnitCut u = unit_cut(p.unit_ctas, ut);
+    hr = blockIdx.x / u.per;
+    lt = (blockIdx.x - hr * u.per) * u.tpc;
+    t_end = hr < HR ? min(u.tpc, ut - lt) : 0;
+  } else {
+    build_kv4_plan(p, HR, sm.len, sm.base);
+    const int total = sm.base[p.C], tpc = tiles_per_cta(total, p.num_ctas);
+    t = min(total, static_cast<int>(blockIdx.x) * tpc);
+    t_end = min(total, t + tpc);
+    if (t < t_end) {
+      int hi = p.C - 1;  // last cache whose first tile is <= t
+#pragma unroll 1
+      while (c < hi) {
+        const int mid = (c + hi + 1) >> 1;
+        if (sm.base[mid] <= t) c = mid;
+        else hi = mid - 1;
+      }
+      const int rem = t - sm.base[c], ut = window_span<kTile>(p, sm.len[c]).tiles + p.draft_tiles;
+      hr = rem / ut;
+      lt = rem - hr * ut;
+    }
+  }
+  int stage = 0, issued = 0, last_rb = -1, last_seq = -1;
   uint32_t phase = 0;
   bool waited = false, ok = true;
   // Page ids come 32 to a load, a window of tiles ahead: lane i holds the address of run i % runs of the window's tile
   // i / runs, and issues that copy.
   const int runs = kTileGroups / kp.run_groups, ahead = 32 / runs;
   const int my_tile = lane / runs, my_g0 = (lane % runs) * kp.run_groups;
-  while (ok && next_piece(p, sm.len, next)) {
-    const Piece w = next;
-    const int32_t* table = p.page_table + (p.paged ? static_cast<size_t>(w.c) * p.max_pages : 0);
-    auto group_of = [&](int lt) {  // this lane's first group of the window from tile lt on, or -1
-      lt += my_tile;
-      if (lt >= w.lt1 || w.draft(lt)) return -1;
-      const int g = w.key0(lt) / kKv4Tokens + my_g0;
-      return g * kKv4Tokens < w.L ? g : -1;
+#pragma unroll 1
+  for (; ok && t < t_end; lt = 0) {  // a piece
+    const int L = sm.len[c];
+    const WindowSpan span = window_span<kTile>(p, L);
+    const int ut = span.tiles + p.draft_tiles, lt1 = min(ut, lt + t_end - t);
+    const int h = p.row_blocks > 1 ? hr / p.row_blocks : hr, rb = hr - h * p.row_blocks;
+    const int seq = p.C == p.B ? c : c / (p.C / p.B);
+    int flags = kFirst | (lt == 0 && lt1 == ut ? kWhole : 0);
+    if (rb != last_rb) flags |= kNewRows;
+    if (p.tree && seq != last_seq) flags |= kNewRows | kNewTree;
+    last_rb = rb;
+    last_seq = seq;
+    t += lt1 - lt;
+    // A window: rows see keys from L + their depth - window on (and the sinks); a depth is at most N.
+    const int seen_from = p.window > 0 ? L + p.N - p.window : 0;
+    const int32_t* table = p.page_table + (p.paged ? static_cast<size_t>(c) * p.max_pages : 0);
+    auto key_of = [&](int x) { return (x < span.sink_tiles ? x : x + span.skip) * kTile; };  // of a prefix tile
+    auto group_of = [&](int x) {  // this lane's first group of the window from tile x on, or -1
+      x += my_tile;
+      if (x >= lt1 || x >= span.tiles) return -1;
+      const int g = key_of(x) / kKv4Tokens + my_g0;
+      return g * kKv4Tokens < L ? g : -1;
     };
-    auto page_of = [&](int g) { return g < 0 ? 0 : p.paged ? table[g / kp.groups_per_page] : w.c; };
-    int window = w.lt0, g = group_of(window), pid = page_of(g);
+    auto page_of = [&](int g) { return g < 0 ? 0 : p.paged ? table[g / kp.groups_per_page] : c; };
+    int window = lt, g = group_of(window), pid = page_of(g);
     const uint8_t* src = nullptr;
     uint32_t bytes = 0;
-    for (int lt = w.lt0; lt < w.lt1; ++lt) {
+#pragma unroll 1
+    for (; lt < lt1; ++lt) {
       if (lt == window) {
         if (p.paged && g >= 0) pid = valid_page_id(p, pid);
-        src = kp.cache + ((static_cast<size_t>(pid) * p.hkv + w.h) * kp.groups_per_page +
+        src = kp.cache + ((static_cast<size_t>(pid) * p.hkv + h) * kp.groups_per_page +
                           (p.paged ? g % kp.groups_per_page : g)) * kKv4Bytes;
-        bytes = g < 0 ? 0 : min(kp.run_groups, (w.L + kKv4Tokens - 1) / kKv4Tokens - g) * kKv4Bytes;
+        bytes = g < 0 ? 0 : min(kp.run_groups, (L + kKv4Tokens - 1) / kKv4Tokens - g) * kKv4Bytes;
         window += ahead;
         g = group_of(window);
         pid = page_of(g);
       }
-      const bool draft = w.draft(lt);
-      const int nkeys = w.nkeys(lt, p.N);
+      const bool draft = lt >= span.tiles;
+      const int key0 = draft ? (lt - span.tiles) * kDraftTile : key_of(lt);
+      const int nkeys = draft ? min(kDraftTile, p.N - key0) : min(kTile, L - key0);
+      if (draft) flags |= kDraft | kMasked;
+      else if (nkeys < kTile || (key0 < seen_from && key0 + kTile > p.sinks)) flags |= kMasked;
+      if (lt == lt1 - 1) flags |= kLast;
       if (draft && !waited) {  // the draft K/V may come from the preceding kernel
         wait_for_prerequisite_grid();
         waited = true;
@@ -238,27 +225,70 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
       ok = __all_sync(0xffffffffu, wait(sm.cempty + 8 * stage, phase ^ 1u));
       if (!ok) break;
       const uint32_t bar = sm.cfull + 8 * stage, dst = sm.ring + stage * kStageSize;
-      if (lane == 0)
+      if (lane == 0) {
+        int4* m = reinterpret_cast<int4*>(sm.meta + issued % kMetas);
+        m[0] = make_int4(flags, key0, nkeys, L);
+        m[1] = make_int4(c, h, rb, seq);
         mbar_arrive_expect_tx(bar, draft ? nkeys * 4 * kHeadDim : (nkeys + kKv4Tokens - 1) / kKv4Tokens * kKv4Bytes);
+      }
       __syncwarp();
       if (draft) {
         if (lane < nkeys) {
-          const size_t row = (static_cast<size_t>(w.c) * p.hkv + w.h) * p.n_max + w.key0(lt) + lane;
+          const size_t row = (static_cast<size_t>(c) * p.hkv + h) * p.n_max + key0 + lane;
           bulk_load(dst + lane * kDraftRow, kp.draft_k + row * kHeadDim, 2 * kHeadDim, bar);
           bulk_load(dst + kDraftV + lane * kDraftRow, kp.draft_v + row * kHeadDim, 2 * kHeadDim, bar);
         }
       } else if (my_tile == lt - (window - ahead) && bytes > 0) {
         bulk_load(dst + my_g0 * kKv4Bytes, src, bytes, bar);
       }
+      flags &= kWhole;
       ++issued;
       if (++stage == kStages) {
         stage = 0;
         phase ^= 1u;
       }
     }
+    if (++hr == HR) {  // (a piece that ends before its unit is the CTA's last)
+      hr = 0;
+      ++c;
+    }
+  }
+#pragma unroll 1
+  for (int i = 0; ok && i < kStops; ++i) {
+    ok = __all_sync(0xffffffffu, wait(sm.cempty + 8 * stage, phase ^ 1u));
+    if (!ok) break;
+    if (lane == 0) {
+      sm.meta[issued % kMetas].flags = kStop;
+      mbar_arrive(sm.cfull + 8 * stage);
+    }
+    ++issued;
+    if (++stage == kStages) {
+      stage = 0;
+      phase ^= 1u;
+    }
   }
   if (lane == 0) *sm.issued = issued;
 }
+
+// After the roles have ended: no copy outlives the CTA, whatever ended it (each wait is bounded).  One thread.
+template <int kStages>
+__device__ __forceinline__ void drain(const AttnParams& p, const Ring& sm) {
+#pragma unroll 1
+  for (int k = max(0, *sm.issued - kStages); k < *sm.issued; ++k)
+    if (!mbar_wait(sm.cfull + 8 * (k % kStages), (k / kStages) & 1, p.err)) break;
+}
+
+// A barrier among warps that ends like every wait (count: warps; a warp passes it with the phase it has counted).
+struct WarpSync {
+  uint32_t bar, phase;
+  __device__ __forceinline__ bool operator()(const Waiter& wait) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+    const bool ok = __all_sync(0xffffffffu, wait(bar, phase));
+    phase ^= 1u;
+    return ok;
+  }
+};
 
 __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
   const __half2 v = __floats2half2_rn(bf16_lo(w), bf16_hi(w));
@@ -303,12 +333,13 @@ __device__ __forceinline__ int ordered(float f) {
 }
 __device__ __forceinline__ float unordered(int i) { return __int_as_float(i >= 0 ? i : i ^ 0x7fffffff); }
 
-// The nodes of a unit's rows, by the first `threads` threads of the CTA, which all call it (named barrier `bar`).
-__device__ __noinline__ void load_rows(const AttnParams& p, const Rows& sm, int nc, int rb, int seq, bool new_seq, int bar,
-                                       int threads) {
+// The nodes of a unit's rows, by the first `threads` threads of the CTA, which all call it and sync by `sync`.
+__device__ __noinline__ bool load_rows(const AttnParams& p, const Rows& sm, int nc, int rb, int seq, bool new_tree, int threads,
+                                       WarpSync& sync, const Waiter& wait) {
   const int tid = threadIdx.x;
-  named_barrier_sync(bar, threads);  // the rows before are no longer read
-  if (new_seq) {
+  bool ok = true;
+  if (new_tree) {
+#pragma unroll 1
     for (int i = tid; i < p.N; i += threads) {
       int v = p.tree_parent[static_cast<size_t>(seq) * p.N + i];
       if (v < -1 || v >= i) {
@@ -317,13 +348,15 @@ __device__ __noinline__ void load_rows(const AttnParams& p, const Rows& sm, int 
       }
       sm.par[i] = v;
     }
-    named_barrier_sync(bar, threads);
-    for (int i = tid; i < p.N; i += threads) {
+    ok = sync(wait);
+#pragma unroll 1
+    for (int i = tid; ok && i < p.N; i += threads) {
       uint64_t bits = 0;
+#pragma unroll 1
       for (int m = i; m >= 0; m = sm.par[m]) bits |= 1ull << m;  // parents strictly decrease
       sm.anc[i] = bits;
     }
-    named_barrier_sync(bar, threads);
+    ok = ok && sync(wait);
   }
   if (tid < nc) {
     const int rr = rb * p.rows_per_unit + tid;
@@ -332,9 +365,10 @@ __device__ __noinline__ void load_rows(const AttnParams& p, const Rows& sm, int 
     sm.depth[tid] = p.tree ? __popcll(sm.anc[node]) : node + 1;
     sm.place[tid] = nl * p.hq + rr - nl * p.G;
   }
+  return ok && sync(wait);
 }
 
-// Bit j: row j0 + j sees this thread's key.  `at`: token position or draft slot of the key, which is valid.
+// Bit j: row j0 + j sees the key `at` (token position or draft slot) of the tile.
 __device__ __noinline__ uint64_t visible_rows(const AttnParams& p, const Rows& sm, int j0, int n, bool draft, int at, int L) {
   uint64_t bits = 0;
   const int key_depth = !draft ? 0 : p.tree ? __popcll(sm.anc[at]) : at + 1;
@@ -350,6 +384,12 @@ __device__ __noinline__ uint64_t visible_rows(const AttnParams& p, const Rows& s
   return bits;
 }
 
+// The rows from j0 on that see key `key` of a masked tile.
+__device__ __forceinline__ uint64_t rows_seeing(const AttnParams& p, const Rows& sm, const int4& m, int L, int j0, int n, int key) {
+  if (key >= m.z) return 0ull;
+  if (!(m.x & kDraft) && p.window == 0) return ~0ull;
+  return visible_rows(p, sm, j0, n, m.x & kDraft, m.y + key, L);
+}
 
 }  // namespace
 }  // namespace kvshot
