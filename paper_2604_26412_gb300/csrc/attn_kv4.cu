@@ -56,7 +56,10 @@ struct Cfg {
   static_assert(kTmemO + kAccs * kNT <= 512 && kCols % 8 == 0, "tensor memory");
 };
 
-struct Smem : Ring, Rows {
+constexpr int kRowSets = 4;  // more than the pieces between the warp that builds one and its last reader
+
+struct Smem : Ring {
+  Rows* rows;                        // [kRowSets]
   uint32_t v, p, q;                  // shared-memory addresses
   uint32_t kfull, vfull;             // [2] K, V decoded
   uint32_t qkdone, pfull, pvdone;    // [2] QK^T done; P written (and S read); P.V done
@@ -75,8 +78,8 @@ constexpr int kBarriers = 18;  // besides the ring's (an even number: what follo
 template <class CF>
 __host__ __device__ constexpr size_t smem_bytes(int C) {
   return 1024 + 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize +
-         sizeof(TileMeta) * kMetas + sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + sizeof(uint64_t) * 128 +
-         sizeof(int) * (6 * 64 + 8 * 64 + 3 * 64 + 6) + sizeof(int) * (2 * C + 1);
+         sizeof(TileMeta) * kMetas + sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + kRowSets * sizeof(Rows) +
+         sizeof(int) * (6 * 64 + 8 * 64 + 6) + sizeof(int) * (2 * C + 1);
 }
 
 template <class CF>
@@ -102,16 +105,12 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.mmadone = s.qempty + 16;
   s.ofree = s.mmadone + 16;
   s.joined = s.ofree + 8;
-  s.anc = reinterpret_cast<uint64_t*>(b) + 2 * CF::kStages + kBarriers;
-  s.row_anc = s.anc + 64;
-  s.ref = reinterpret_cast<float*>(s.row_anc + 64);
+  s.rows = reinterpret_cast<Rows*>(b + 8 * (2 * CF::kStages + kBarriers));
+  s.ref = reinterpret_cast<float*>(s.rows + kRowSets);
   s.alpha = s.ref + 128;
   s.inv = s.alpha + 128;
   s.wmax = reinterpret_cast<int*>(s.inv + 128);
-  s.depth = s.wmax + 8 * 64;
-  s.place = s.depth + 64;
-  s.par = s.place + 64;
-  s.codes = s.par + 64;
+  s.codes = s.wmax + 8 * 64;
   s.tmem = reinterpret_cast<uint32_t*>(s.codes + 2);
   s.abort = reinterpret_cast<volatile int*>(s.tmem + 1);
   s.issued = s.codes + 4;
@@ -120,15 +119,15 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   return s;
 }
 
-// q of every piece as f16, rows of 64 dims in two halves (K-major B of QK^T, 128-byte swizzle).  This warp reads every
-// tile's words, and counts among the readers of a stage, so that it cannot fall behind the ring.
+// q of every piece as f16, rows of 64 dims in two halves (K-major B of QK^T, 128-byte swizzle), and the rows' nodes.  This
+// warp reads every tile's words, and counts among the readers of a stage, so that it cannot fall behind the ring.
 template <class CF>
 __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, const Waiter& wait) {
   const AttnParams& p = kp.a;
   const Smem sm = smem;
   const int lane = threadIdx.x & 31;
   wait_for_prerequisite_grid();
-  int stage = 0, piece = 0;
+  int stage = 0, piece = 0, set = -1;
   uint32_t phase = 0;
 #pragma unroll 1
   for (int t = 0;; ++t) {
@@ -146,16 +145,36 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
     ++piece;
     const __nv_bfloat16* q = p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim;
     const int row0 = w.rb * p.rows_per_unit, rows = min(p.rows_per_unit, p.rows_total - row0);
+    // 16 bytes of two rows at a time per warp; eight loads of a lane on their way together.
     const int ch = lane & 15;
-#pragma unroll 8
-    for (int r = lane >> 4; r < CF::kNT; r += 2) {
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (r < rows) {
-        const int nl = (row0 + r) / p.G, gh = row0 + r - nl * p.G;
-        x = reinterpret_cast<const uint4*>(q + (static_cast<size_t>(nl) * p.hq + gh) * kHeadDim)[ch];
+    const uint32_t dst = sm.q + b * CF::kQTile + (ch >> 3) * (CF::kNT * 128);
+#pragma unroll 1
+    for (int r0 = lane >> 4; r0 < CF::kNT; r0 += 16) {
+      uint4 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 2 * i, nl = kp.by_group(row0 + r);
+        x[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows)
+          x[i] = reinterpret_cast<const uint4*>(q + (static_cast<size_t>(nl) * p.hq + row0 + r - nl * p.G) * kHeadDim)[ch];
       }
-      sts128(sm.q + b * CF::kQTile + (ch >> 3) * (CF::kNT * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4),
-             make_uint4(bf16x2_to_f16x2(x.x), bf16x2_to_f16x2(x.y), bf16x2_to_f16x2(x.z), bf16x2_to_f16x2(x.w)));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 2 * i;
+        sts128(dst + r * 128 + (((ch & 7) ^ (r & 7)) << 4),
+               make_uint4(bf16x2_to_f16x2(x[i].x), bf16x2_to_f16x2(x[i].y), bf16x2_to_f16x2(x[i].z), bf16x2_to_f16x2(x[i].w)));
+      }
+    }
+    if (w.flags & kNewRows) {
+      // (A set of another row block has the tree of the one before it copied along.)
+      const int before = set & (kRowSets - 1);
+      set = (set + 1) & (kRowSets - 1);
+      if (p.tree && !(w.flags & kNewTree)) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sm.rows[set].anc[lane + 32 * k] = sm.rows[before].anc[lane + 32 * k];
+        __syncwarp();
+      }
+      build_rows(kp, sm.rows[set], CF::kNC, w.rb, w.seq, w.flags & kNewTree);
     }
     fence_proxy_async_smem();
     __syncwarp();
@@ -455,8 +474,8 @@ __device__ __noinline__ void rescale_o(const float* alpha, int n, uint32_t o_col
 // A piece's rows [j0, j1) of this thread's dim: the final ones, or the piece's part in the workspace.  kAccs 2: O and the
 // other accumulator `next` columns on, each with its own weights (0: it holds nothing).
 template <int kAccs>
-__device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, const TileMeta& w, int j0, int j1, uint32_t o_cols,
-                                        int next) {
+__device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, const int* place, const TileMeta& w, int j0, int j1,
+                                        uint32_t o_cols, int next) {
   const int tid = threadIdx.x & 127;
   const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
   const size_t row0 = static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G;
@@ -477,7 +496,7 @@ __device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, con
         const float a2 = sm.inv[64 + j + i];
         v += a2 != 0.f ? __uint_as_float(o2[i]) * a2 : 0.f;
       }
-      if (whole) p.out[(row0 + sm.place[j + i]) * kHeadDim + tid] = __float2bfloat16(v);
+      if (whole) p.out[(row0 + place[j + i]) * kHeadDim + tid] = __float2bfloat16(v);
       else p.ws_o[(part + j + i) * kHeadDim + tid] = v;
     }
   }
@@ -486,7 +505,8 @@ __device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, con
 // The rows' sums, weights of the accumulators and log-sum-exp.  Thread = row.  had: whether each accumulator holds tiles
 // of this piece.
 template <class CF>
-__device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, const TileMeta& w, int j, bool had0, bool had1) {
+__device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, const int* place, const TileMeta& w, int j,
+                                       bool had0, bool had1) {
   const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
   auto total = [&](int wg, int col) {
     const int* x = sm.wmax + wg * 256 + col;
@@ -509,7 +529,7 @@ __device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, cons
   }
   if (j >= rows) return;
   const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
-  if (w.flags & kWhole) p.lse[static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G + sm.place[j]] = lse2 * 0.69314718055994531f;
+  if (w.flags & kWhole) p.lse[static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G + place[j]] = lse2 * 0.69314718055994531f;
   else p.ws_lse[static_cast<size_t>((w.c * p.hkv + w.h) * p.row_blocks + w.rb + blockIdx.x) * p.rows_per_unit + j] = lse2;
 }
 
@@ -534,12 +554,12 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
   bool fresh = true;              // this warpgroup has had no tile of the piece
   int t_first = 0;                // the piece's first tile
   bool good = true;               // no wait of this warp has given up
+  int rb = 0, set = -1;           // the piece's row block, and its set of rows
   auto begin = [&](int t) {
     const TileMeta w = sm.meta[t % kMetas];
     if (!sync(wait)) return false;  // the piece before has been written out
-    if ((w.flags & kNewRows) &&
-        !load_rows(p, smem, CF::kNC, w.rb, w.seq, w.flags & kNewTree, kSoftmaxThreads, sync, wait))
-      return false;
+    rb = w.rb;
+    if (w.flags & kNewRows) set = (set + 1) & (kRowSets - 1);  // (built before q was staged, so before S)
     if (key < NC) ref[key] = -kNoRef;
 #pragma unroll
     for (int j = 0; j < NC / 2; ++j) l[j] = make_float2(0.f, 0.f);
@@ -566,10 +586,10 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     const bool ok = fresh || wait(sm.pvdone + 8 * (mine & 1), (mine >> 1) & 1);
     if (!__all_sync(0xffffffffu, ok) || !sync(wait)) return false;
     const bool two = t > t_first;
-    if (threadIdx.x < CF::kNC) join_sums<CF>(p, smem, smem.meta[t % kMetas], threadIdx.x, two || !(t & 1), two || (t & 1));
+    if (threadIdx.x < CF::kNC) join_sums<CF>(p, smem, sm.rows[set].place, smem.meta[t % kMetas], threadIdx.x, two || !(t & 1), two || (t & 1));
     if (!sync(wait)) return false;
     tc_fence_after();
-    write_rows<CF::kAccs>(p, smem, smem.meta[t % kMetas], wg * (CF::kNC / 2), (wg + 1) * (CF::kNC / 2), trow + CF::kTmemO, CF::kNT);
+    write_rows<CF::kAccs>(p, smem, sm.rows[set].place, smem.meta[t % kMetas], wg * (CF::kNC / 2), (wg + 1) * (CF::kNC / 2), trow + CF::kTmemO, CF::kNT);
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(sm.ofree);
@@ -593,7 +613,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     const bool draft = meta.x & kDraft;
     const float qs = draft ? p.qscale : p.qscale * p.k_scale;
     uint64_t vis = ~0ull;
-    if (meta.x & kMasked) vis = rows_seeing(p, smem, meta, meta.w, col0, NC, key);
+    if (good && !stop && (meta.x & kMasked)) vis = rows_seeing(kp, sm.rows[set], meta, rb, key) >> col0;
     // The buffer of P is free when P.V of the tile before the last is done (by tile: O is at rest then, too).
     good = good && (stop || __all_sync(0xffffffffu, wait(sm.pvdone + 8 * b, phase ^ 1u)));
     tc_fence_after();
@@ -877,6 +897,10 @@ extern "C" kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* d, const 
   kp.draft_v = static_cast<const __nv_bfloat16*>(draft_v);
   kp.groups_per_page = p.page_size / kKv4Tokens;
   kp.run_groups = std::min(kTileGroups, kp.groups_per_page & -kp.groups_per_page);
+  kp.by_page = Div::by(kp.groups_per_page);
+  kp.by_blocks = Div::by(p.row_blocks);
+  kp.by_seq = Div::by(p.C / p.B);
+  kp.by_group = Div::by(p.G);
   if (!paged) kp.run_groups = kTileGroups;  // one page: a tile's groups are neighbours
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (launch(kp, (d->flags & KVSHOT_OVERLAP_PREVIOUS) != 0, s) != cudaSuccess) return KVSHOT_ERR_CUDA;

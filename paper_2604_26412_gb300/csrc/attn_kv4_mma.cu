@@ -34,7 +34,8 @@ struct Cfg {
   static constexpr int kRows = 8 * NR;
 };
 
-struct Smem : Ring, Rows {
+struct Smem : Ring {
+  Rows* rows;
   uint32_t joined;      // barrier of the consumer warps
   float* comb_o;        // [kWarps][rows][kCombStride] a piece's O of each warp
   float *ref, *sum;     // [kWarps][rows] its references and sums; then (ref) its weights
@@ -44,7 +45,7 @@ struct Smem : Ring, Rows {
 template <class CF>
 __host__ __device__ constexpr size_t smem_bytes(int C) {
   return 128 + CF::kStages * kStageSize + sizeof(float) * kWarps * CF::kRows * (kCombStride + 2) +
-         sizeof(TileMeta) * kMetas + sizeof(uint64_t) * (2 * CF::kStages + 1 + 128) + sizeof(int) * (3 * 64 + 4 + 2 * C + 1);
+         sizeof(TileMeta) * kMetas + sizeof(Rows) + sizeof(uint64_t) * (2 * CF::kStages + 2) + sizeof(int) * (4 + 2 * C + 1);
 }
 
 template <class CF>
@@ -60,14 +61,11 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.cfull = smem_addr(m);
   s.cempty = s.cfull + 8 * CF::kStages;
   s.joined = s.cempty + 8 * CF::kStages;
-  s.anc = m + 2 * CF::kStages + 1;
-  s.row_anc = s.anc + 64;
-  s.depth = reinterpret_cast<int*>(s.row_anc + 64);
-  s.place = s.depth + 64;
-  s.par = s.place + 64;
-  s.abort = reinterpret_cast<volatile int*>(s.par + 64);
-  s.issued = s.par + 65;
-  s.len = s.par + 68;
+  s.rows = reinterpret_cast<Rows*>(m + 2 * CF::kStages + 2);
+  int* words = reinterpret_cast<int*>(s.rows + 1);
+  s.abort = reinterpret_cast<volatile int*>(words);
+  s.issued = words + 1;
+  s.len = words + 4;
   s.base = s.len + C;
   return s;
 }
@@ -123,7 +121,7 @@ __device__ __noinline__ bool join_warps(const AttnParams& p, const Smem& sm, con
 #pragma unroll
     for (int k = 0; k < kWarps; ++k) sm.ref[k * n + tid] = ex2(sm.ref[k * n + tid] - top) * inv;
     const float lse2 = total == 0.f ? -INFINITY : top + __log2f(total);
-    if (whole) p.lse[orow0 + sm.place[tid]] = lse2 * 0.69314718055994531f;
+    if (whole) p.lse[orow0 + sm.rows->place[tid]] = lse2 * 0.69314718055994531f;
     else p.ws_lse[part + tid] = lse2;
   }
   if (!sync(wait)) return false;
@@ -132,7 +130,7 @@ __device__ __noinline__ bool join_warps(const AttnParams& p, const Smem& sm, con
     float v = 0.f;
 #pragma unroll
     for (int k = 0; k < kWarps; ++k) v = fmaf(sm.ref[k * n + r], sm.comb_o[(k * n + r) * kCombStride + tid], v);
-    if (whole) p.out[(orow0 + sm.place[r]) * kHeadDim + tid] = __float2bfloat16(v);
+    if (whole) p.out[(orow0 + sm.rows->place[r]) * kHeadDim + tid] = __float2bfloat16(v);
     else p.ws_o[(part + r) * kHeadDim + tid] = v;
   }
   return true;
@@ -156,7 +154,7 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
   float o[8][NR][4], ref[NR][2], l[NR][2];  // rows 8 nr + 2 q4 + e; l: this lane's keys only
   bool in_codes = false;                    // O is in units of the value codes (a warp without draft keys keeps it so)
   wait_for_prerequisite_grid();             // q and the outputs may be the preceding kernel's
-  int stage = 0;
+  int stage = 0, rb = 0;
   uint32_t phase = 0;
 #pragma unroll 1
   for (int t = 0;; ++t) {
@@ -167,14 +165,16 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
     if (meta.x & kFirst) {
       const TileMeta w = sm.meta[t % kMetas];
       if (!sync(wait)) return;  // the piece before has been written out
-      if ((w.flags & kNewRows) &&
-          !load_rows(p, smem, CF::kRows, w.rb, w.seq, w.flags & kNewTree, kWarps * 32, sync, wait))
-        return;
+      rb = w.rb;
+      if (w.flags & kNewRows) {
+        if (warp == 0) build_rows(kp, *sm.rows, CF::kRows, w.rb, w.seq, w.flags & kNewTree);
+        if (!sync(wait)) return;
+      }
       const __nv_bfloat16* qrow = p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim + 8 * q4;
       const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr) {
-        const uint4* src = reinterpret_cast<const uint4*>(qrow + static_cast<size_t>(sm.place[8 * nr + g]) * kHeadDim);
+        const uint4* src = reinterpret_cast<const uint4*>(qrow + static_cast<size_t>(sm.rows->place[8 * nr + g]) * kHeadDim);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           uint4 x = make_uint4(0u, 0u, 0u, 0u);
@@ -242,7 +242,7 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
       if (masked) {
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-          const uint64_t vis = rows_seeing(p, smem, meta, meta.w, 2 * q4, CF::kRows - 2 * q4, kw + 8 * a + g);
+          const uint64_t vis = rows_seeing(kp, *sm.rows, meta, rb, kw + 8 * a + g) >> (2 * q4);
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr)
 #pragma unroll

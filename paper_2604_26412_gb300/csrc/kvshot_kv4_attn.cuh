@@ -7,11 +7,25 @@
 
 namespace kvshot {
 
+// Division by a number that the host knows: n / d for 0 <= n < 2^31.
+struct Div {
+  uint32_t mul, shift, d;
+  static Div by(uint32_t d) {
+    uint32_t l = 0;
+    while ((1ull << l) < d) ++l;
+    return Div{static_cast<uint32_t>(((1ull << 32) * ((1ull << l) - d)) / d + 1), l, d};
+  }
+  __device__ __forceinline__ int operator()(int n) const {
+    return static_cast<int>((__umulhi(static_cast<uint32_t>(n), mul) + static_cast<uint32_t>(n)) >> shift);
+  }
+};
+
 struct Kv4Params {
   AttnParams a;
   const uint8_t* cache;
   const __nv_bfloat16 *draft_k, *draft_v;
   int groups_per_page;
+  Div by_page, by_blocks, by_seq, by_group;  // groups per page, row blocks, caches per sequence, heads per KV head
   int run_groups;  // groups of a tile that are always neighbours in memory (a power of two, at most kTileGroups)
 };
 
@@ -54,17 +68,20 @@ struct TileMeta {
 constexpr int kMetas = 16;    // more than the tiles between the loader and the last reader
 
 // Shared-memory parts that both kernels have: the ring of the cache's bytes (addresses of its stages and of its barriers,
-// landed and read) with the tiles' words, and the query rows' nodes.
+// landed and read) with the tiles' words.
 struct Ring {
   uint32_t ring, cfull, cempty;
   TileMeta* meta;   // [kMetas]
   int* issued;      // tiles issued by the loader
   int *len, *base;  // the loader's plan
 };
+// The query rows of a unit: their places in a cache's q and out, and, of a draft tree, who sees what, as bits of rows.
 struct Rows {
-  uint64_t *anc, *row_anc;  // [64] each node's ancestors and itself (tree); of each query row's node
-  int *depth, *place;       // [64] per row: the node's depth; the row's place in a cache's q and out
-  int* par;                 // [64]
+  uint64_t line[kMaxTreeNodes];       // rows whose node is this one or descends from it
+  uint64_t upto[kMaxTreeNodes + 1];   // rows whose depth is at most x (with a window)
+  uint64_t anc[kMaxTreeNodes];        // nodes: itself and its ancestors
+  int place[64];
+  int parent[kMaxTreeNodes];
 };
 
 // Every wait ends: when its phase completes, when another role has given up, or (which gives up) after the call's limit.
@@ -179,8 +196,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
     const int L = sm.len[c];
     const WindowSpan span = window_span<kTile>(p, L);
     const int ut = span.tiles + p.draft_tiles, lt1 = min(ut, lt + t_end - t);
-    const int h = p.row_blocks > 1 ? hr / p.row_blocks : hr, rb = hr - h * p.row_blocks;
-    const int seq = p.C == p.B ? c : c / (p.C / p.B);
+    const int h = kp.by_blocks(hr), rb = hr - h * p.row_blocks, seq = kp.by_seq(c);
     int flags = kFirst | (lt == 0 && lt1 == ut ? kWhole : 0);
     if (rb != last_rb) flags |= kNewRows;
     if (p.tree && seq != last_seq) flags |= kNewRows | kNewTree;
@@ -197,7 +213,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
       const int g = key_of(x) / kKv4Tokens + my_g0;
       return g * kKv4Tokens < L ? g : -1;
     };
-    auto page_of = [&](int g) { return g < 0 ? 0 : p.paged ? table[g / kp.groups_per_page] : c; };
+    auto page_of = [&](int g) { return g < 0 ? 0 : p.paged ? table[kp.by_page(g)] : c; };
     int window = lt, g = group_of(window), pid = page_of(g);
     const uint8_t* src = nullptr;
     uint32_t bytes = 0;
@@ -206,7 +222,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
       if (lt == window) {
         if (p.paged && g >= 0) pid = valid_page_id(p, pid);
         src = kp.cache + ((static_cast<size_t>(pid) * p.hkv + h) * kp.groups_per_page +
-                          (p.paged ? g % kp.groups_per_page : g)) * kKv4Bytes;
+                          (p.paged ? g - kp.by_page(g) * kp.groups_per_page : g)) * kKv4Bytes;
         bytes = g < 0 ? 0 : min(kp.run_groups, (L + kKv4Tokens - 1) / kKv4Tokens - g) * kKv4Bytes;
         window += ahead;
         g = group_of(window);
@@ -333,62 +349,77 @@ __device__ __forceinline__ int ordered(float f) {
 }
 __device__ __forceinline__ float unordered(int i) { return __int_as_float(i >= 0 ? i : i ^ 0x7fffffff); }
 
-// The nodes of a unit's rows, by the first `threads` threads of the CTA, which all call it and sync by `sync`.
-__device__ __noinline__ bool load_rows(const AttnParams& p, const Rows& sm, int nc, int rb, int seq, bool new_tree, int threads,
-                                       WarpSync& sync, const Waiter& wait) {
-  const int tid = threadIdx.x;
-  bool ok = true;
+// The rows of row block rb, of sequence seq's draft tree, by one warp.
+__device__ __noinline__ void build_rows(const Kv4Params& kp, Rows& r, int nc, int rb, int seq, bool new_tree) {
+  const AttnParams& p = kp.a;
+  const int lane = threadIdx.x & 31;
   if (new_tree) {
-#pragma unroll 1
-    for (int i = tid; i < p.N; i += threads) {
-      int v = p.tree_parent[static_cast<size_t>(seq) * p.N + i];
+    const int* tree = p.tree_parent + static_cast<size_t>(seq) * p.N;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int i = lane + 32 * k;
+      int v = i < p.N ? tree[i] : -1;
       if (v < -1 || v >= i) {
-        set_error(p.err, KVSHOT_ERR_TREE);
+        if (i < p.N) set_error(p.err, KVSHOT_ERR_TREE);
         v = -1;
       }
-      sm.par[i] = v;
+      r.parent[i] = v;
     }
-    ok = sync(wait);
+    __syncwarp();
 #pragma unroll 1
-    for (int i = tid; ok && i < p.N; i += threads) {
+    for (int i = lane; i < p.N; i += 32) {
       uint64_t bits = 0;
 #pragma unroll 1
-      for (int m = i; m >= 0; m = sm.par[m]) bits |= 1ull << m;  // parents strictly decrease
-      sm.anc[i] = bits;
+      for (int m = i; m >= 0; m = r.parent[m]) bits |= 1ull << m;  // parents strictly decrease
+      r.anc[i] = bits;
     }
-    ok = ok && sync(wait);
+    __syncwarp();
   }
-  if (tid < nc) {
-    const int rr = rb * p.rows_per_unit + tid;
-    const int nl = min(rr, p.rows_total - 1) / p.G, node = p.N - p.Nq + nl;
-    if (p.tree) sm.row_anc[tid] = sm.anc[node];
-    sm.depth[tid] = p.tree ? __popcll(sm.anc[node]) : node + 1;
-    sm.place[tid] = nl * p.hq + rr - nl * p.G;
+  uint64_t anc[2];
+  int depth[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int j = lane + 32 * k, rr = rb * p.rows_per_unit + j;
+    const int nl = kp.by_group(min(rr, p.rows_total - 1));
+    if (j < nc) r.place[j] = nl * p.hq + rr - nl * p.G;
+    anc[k] = p.tree ? r.anc[p.N - p.Nq + nl] : 0;
+    depth[k] = __popcll(anc[k]);
   }
-  return ok && sync(wait);
+  if (p.tree) {
+#pragma unroll 4
+    for (int m = 0; m < p.N; ++m) {
+      const uint32_t lo = __ballot_sync(0xffffffffu, (anc[0] >> m) & 1), hi = __ballot_sync(0xffffffffu, (anc[1] >> m) & 1);
+      if (lane == 0) r.line[m] = lo | static_cast<uint64_t>(hi) << 32;
+    }
+#pragma unroll 1
+    for (int x = 0; p.window > 0 && x <= p.N; ++x) {
+      const uint32_t lo = __ballot_sync(0xffffffffu, depth[0] <= x), hi = __ballot_sync(0xffffffffu, depth[1] <= x);
+      if (lane == 0) r.upto[x] = lo | static_cast<uint64_t>(hi) << 32;
+    }
+  }
+  __syncwarp();
 }
 
-// Bit j: row j0 + j sees the key `at` (token position or draft slot) of the tile.
-__device__ __noinline__ uint64_t visible_rows(const AttnParams& p, const Rows& sm, int j0, int n, bool draft, int at, int L) {
-  uint64_t bits = 0;
-  const int key_depth = !draft ? 0 : p.tree ? __popcll(sm.anc[at]) : at + 1;
-  const int pos = draft ? L + key_depth - 1 : at;
-  const bool always = p.window == 0 || pos < p.sinks;
-#pragma unroll 1
-  for (int j = 0; j < n; ++j) {
-    const int d = sm.depth[j0 + j];
-    bool v = always || L + d - 1 - pos < p.window;
-    if (draft) v = v && (p.tree ? (sm.row_anc[j0 + j] >> at) & 1ull : at < d);
-    bits |= static_cast<uint64_t>(v) << j;
+// Bits of the unit's rows that see key `key` of a masked tile (m: its words' flags, key0, nkeys, L).
+__device__ __forceinline__ uint64_t rows_seeing(const Kv4Params& kp, const Rows& r, const int4& m, int rb, int key) {
+  const AttnParams& p = kp.a;
+  if (key >= m.z) return 0ull;
+  const bool draft = m.x & kDraft;
+  if (!draft && p.window == 0) return ~0ull;
+  const int at = m.y + key, L = m.w;
+  // Rows whose node's depth is at most x.  A chain's rows are in the order of depth.
+  auto upto = [&](int x) -> uint64_t {
+    if (p.tree) return x < 0 ? 0ull : r.upto[min(x, p.N)];
+    const int n = min(x - (p.N - p.Nq), p.Nq) * p.G - rb * p.rows_per_unit;
+    return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull;
+  };
+  if (!draft) return at < p.sinks ? ~0ull : upto(at - L + p.window);
+  uint64_t bits = p.tree ? r.line[at] : ~upto(at);
+  if (p.window > 0) {
+    const int depth = p.tree ? __popcll(r.anc[at]) : at + 1;
+    if (L + depth - 1 >= p.sinks) bits &= upto(depth + p.window - 1);
   }
   return bits;
-}
-
-// The rows from j0 on that see key `key` of a masked tile.
-__device__ __forceinline__ uint64_t rows_seeing(const AttnParams& p, const Rows& sm, const int4& m, int L, int j0, int n, int key) {
-  if (key >= m.z) return 0ull;
-  if (!(m.x & kDraft) && p.window == 0) return ~0ull;
-  return visible_rows(p, sm, j0, n, m.x & kDraft, m.y + key, L);
 }
 
 }  // namespace
