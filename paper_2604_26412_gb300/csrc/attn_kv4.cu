@@ -20,7 +20,6 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
-#include <type_traits>
 
 #include "kvshot_kv4_attn.cuh"
 #include "kvshot_tcgen05.cuh"
@@ -38,7 +37,6 @@ constexpr int kVTile = 2 * kVHalf;
 constexpr int kPTile = kTile * 128;                // P^T: a row of up to 64 query rows per key, 128-byte swizzle
 constexpr int kThreads = 20 * 32;
 constexpr int kGroupThreads = 128;                 // a warpgroup
-constexpr int kSoftmaxThreads = 256;
 constexpr int kWarpDecode = 8, kWarpLoad = 16, kWarpQk = 17, kWarpPv = 18, kWarpQ = 19;
 constexpr int kBarGroup = 1;                       // named barriers 1 and 2: the threads of a softmax warpgroup
 // NC: query rows of a unit, a multiple of 8.
@@ -49,7 +47,7 @@ struct Cfg {
   static constexpr bool kByTile = NC <= 32;            // the softmax warpgroups share out the tiles, else the rows
   static constexpr int kCols = kByTile ? NC : NC / 2;  // rows of a softmax thread
   static constexpr int kAccs = kByTile ? 2 : 1;        // accumulators
-  static constexpr int kStages = NC <= 16 ? 6 : NC <= 32 ? 5 : 4;
+  static constexpr int kStages = NC <= 32 ? 5 : 4;
   static constexpr int kQTile = kNT * 256;
   static constexpr uint32_t kTmemK = 0, kTmemS = 128, kTmemO = 128 + 2 * kNT;  // columns
   static constexpr uint32_t kTmemCols = kTmemO + kAccs * kNT <= 256 ? 256 : 512;
@@ -70,7 +68,6 @@ struct Smem : Ring {
   int* wmax;                         // [8][64] per warp and row; sums at a piece's end
   int* codes;                        // [2] the warpgroup's accumulator is in units of the value codes
   uint32_t* tmem;
-  volatile int* abort;
 };
 
 constexpr int kBarriers = 18;  // besides the ring's (an even number: what follows is aligned to 16 bytes)
@@ -91,7 +88,7 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.q = s.p + 2 * kPTile;
   s.ring = s.q + 2 * CF::kQTile;
   b += 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize;
-  s.meta = reinterpret_cast<TileMeta*>(b);
+  s.meta = smem_addr(b);
   b += sizeof(TileMeta) * kMetas;
   s.cfull = smem_addr(b);
   s.cempty = s.cfull + 8 * CF::kStages;
@@ -112,7 +109,6 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.wmax = reinterpret_cast<int*>(s.inv + 128);
   s.codes = s.wmax + 8 * 64;
   s.tmem = reinterpret_cast<uint32_t*>(s.codes + 2);
-  s.abort = reinterpret_cast<volatile int*>(s.tmem + 1);
   s.issued = s.codes + 4;
   s.len = s.codes + 6;
   s.base = s.len + C;
@@ -132,7 +128,7 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
 #pragma unroll 1
   for (int t = 0;; ++t) {
     if (!__all_sync(0xffffffffu, wait(sm.cfull + 8 * stage, phase))) return;
-    const TileMeta w = sm.meta[t % kMetas];
+    const TileMeta w = tile_meta(sm, t);
     if (lane == 0) mbar_arrive(sm.cempty + 8 * stage);
     if (++stage == CF::kStages) {
       stage = 0;
@@ -236,12 +232,13 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
 #pragma unroll 1
   for (int t = wg;; t += 2) {
     // The tile's bytes; K's buffer: QK^T of its previous tile is done.
+    int flags = tile_flags(sm, t);
     bool ok = wait(sm.cfull + 8 * stage, phase);
     ok = ok && wait(qkdone, freed);
     if (!__all_sync(0xffffffffu, ok)) return;
     tc_fence_after();
-    const int4 meta = *reinterpret_cast<const int4*>(sm.meta + t % kMetas);  // flags, key0, nkeys, L
-    if (meta.x & kStop) {
+    if (!is_of(flags, t)) flags = tile_flags(sm, t);
+    if (flags & kStop) {
       // (P.V of the tile before has to have seen its V, whose phase this one ends.)
       if (!__all_sync(0xffffffffu, wait(pvdone, freed))) return;
       if (lane == 0) {
@@ -250,7 +247,7 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
       }
       return;
     }
-    const bool draft = meta.x & kDraft;
+    const bool draft = flags & kDraft;
     const uint32_t src = src0 + stage * kStageSize;
     if (!draft) {
       uint2 sc = lds64(src + scale0);
@@ -263,7 +260,7 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
         sc.y >>= 16;
       }
     } else {
-      decode_draft<false>(draft0 + stage * kStageSize, key < meta.z, kdst, sw);
+      decode_draft<false>(draft0 + stage * kStageSize, key < tile_words(sm, t).z, kdst, sw);
     }
     tmem_wait_st();
     tc_fence_before();
@@ -273,7 +270,8 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
     if (!__all_sync(0xffffffffu, wait(pvdone, freed))) return;
     if (!draft) {
       uint2 sc = lds64(src + scale0 + kScaleBytes);
-      if (meta.x & kMasked) {
+      if (flags & kMasked) {
+        const int4 meta = tile_words(sm, t);  // flags, key0, nkeys, L
         // Keys that no row sees may hold anything; V of them must not be NaN (0 * NaN; any code times 0 is 0).
         const int at = meta.y + key, lo = p.window > 0 ? meta.w + p.min_depth - p.window : 0;
         if (key >= meta.z || (at < lo && at >= p.sinks)) sc = make_uint2(0u, 0u);
@@ -287,7 +285,7 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
         sc.y >>= 16;
       }
     } else {
-      decode_draft<true>(draft0 + kDraftV + stage * kStageSize, key < meta.z, vdst, sw);
+      decode_draft<true>(draft0 + kDraftV + stage * kStageSize, key < tile_words(sm, t).z, vdst, sw);
     }
     fence_proxy_async_smem();
     __syncwarp();
@@ -315,38 +313,36 @@ __device__ __forceinline__ void run_qk(const Smem& smem, const Waiter& wait, uin
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, false);
   const uint32_t tmem = uniform(tmem_base);
   const uint64_t q0 = smem_desc_sw128(sm.q, 16, 1024);
-  uint32_t phase = 0;  // of the buffers' tiles: flips after the second one
-  int t = 0, piece = -1, stops = 0;
-  // The tile in buffers b; false when a wait has given up.
-  auto step = [&](auto buffer) {
-    constexpr int b = decltype(buffer)::value;
+  int piece = -1;
+#pragma unroll 1
+  for (int t = 0, stops = 0; stops < 2; ++t) {
+    const uint32_t b = t & 1, phase = (t >> 1) & 1;
+    uint32_t flags = uniform(tile_flags(sm, t));
     bool ok = wait(sm.pfull + 8 * b, phase ^ 1u);  // S of the tile before the last has been read
     ok = ok && wait(sm.kfull + 8 * b, phase);
-    if (!__all_sync(0xffffffffu, ok)) return false;
-    const uint32_t flags = uniform(sm.meta[t % kMetas].flags);
+    if (!__all_sync(0xffffffffu, ok)) break;
+    if (!is_of(flags, t)) flags = uniform(tile_flags(sm, t));
+    if (flags & kFirst) {
+      ++piece;
+      if (!__all_sync(0xffffffffu, wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1))) break;
+    }
     if (flags & kStop) {
       ++stops;  // (its S is nothing, and the softmax sees that)
     } else {
-      if (flags & kFirst) {
-        ++piece;
-        if (!__all_sync(0xffffffffu, wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1))) return false;
-      }
       tc_fence_after();
-      const uint64_t q = q0 + (piece & 1) * (CF::kQTile >> 4);
+      const uint32_t d = tmem + CF::kTmemS + b * CF::kNT;
+      uint32_t k = tmem + CF::kTmemK + 64 * b;
+      uint64_t q = q0 + (piece & 1) * (CF::kQTile >> 4);
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {  // of the dims
 #pragma unroll
-      for (int ks = 0; ks < kHeadDim / 16; ++ks)
-        tc_mma_tmem_a_elect(tmem + CF::kTmemS + b * CF::kNT, tmem + CF::kTmemK + 64 * b + 8 * ks,
-                            q + (((ks >> 2) * (CF::kNT * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
+        for (int ks = 0; ks < 4; ++ks) tc_mma_tmem_a_elect(d, k + 8 * ks, q + 2 * ks, idesc, half + ks > 0);
+        k += 32;
+        q += CF::kNT * 128 >> 4;
+      }
       if (flags & kLast) tc_commit_elect(sm.qempty + 8 * (piece & 1));
     }
     tc_commit_elect(sm.qkdone + 8 * b);
-    ++t;
-    return stops < 2;
-  };
-#pragma unroll 1
-  for (;;) {
-    if (!step(std::integral_constant<int, 0>{}) || !step(std::integral_constant<int, 1>{})) break;
-    phase ^= 1u;
   }
   tc_commit_elect(sm.mmadone);
 }
@@ -357,34 +353,35 @@ __device__ __forceinline__ void run_pv(const Smem& smem, const Waiter& wait, uin
   constexpr uint32_t idesc = idesc_f16(128, CF::kNT, true, true);
   const uint32_t tmem = uniform(tmem_base);
   const uint64_t v0 = smem_desc_sw128(sm.v, kVHalf, 1024), p0 = smem_desc_sw128(sm.p, kPTile, 1024);
-  uint32_t phase = 0;
-  int t = 0, piece = -1, in_piece = 0;
-  auto step = [&](auto buffer) {
-    constexpr int b = decltype(buffer)::value;
-    if (!__all_sync(0xffffffffu, wait(sm.vfull + 8 * b, phase))) return false;
-    const uint32_t flags = uniform(sm.meta[t % kMetas].flags);
-    if (flags & kStop) return false;
+  int piece = -1, in_piece = 0;
+#pragma unroll 1
+  for (int t = 0;; ++t, ++in_piece) {
+    const uint32_t b = t & 1, phase = (t >> 1) & 1;
+    uint32_t flags = uniform(tile_flags(sm, t));
+    if (!__all_sync(0xffffffffu, wait(sm.vfull + 8 * b, phase))) break;
+    if (!is_of(flags, t)) flags = uniform(tile_flags(sm, t));
+    if (flags & kStop) break;
     bool ok = wait(sm.pfull + 8 * b, phase);
     if (flags & kFirst) {
       in_piece = 0;
       if (++piece > 0) ok = ok && wait(sm.ofree, (piece - 1) & 1);
     }
-    if (!__all_sync(0xffffffffu, ok)) return false;
+    if (!__all_sync(0xffffffffu, ok)) break;
     tc_fence_after();
-    const uint32_t more = in_piece >= CF::kAccs;  // the accumulator holds tiles of this piece
-#pragma unroll
-    for (int k16 = 0; k16 < kTile / 16; ++k16)  // two 8-key groups of 1 KB each
-      tc_mma_elect(tmem + CF::kTmemO + (CF::kByTile ? b * CF::kNT : 0), v0 + ((b * kVTile + k16 * 2048) >> 4),
-                   p0 + ((b * kPTile + k16 * 2048) >> 4), idesc, k16 > 0 ? 1u : more);
-    tc_commit_elect(sm.pvdone + 8 * b);
-    ++t;
-    ++in_piece;
-    return true;
-  };
+    const uint32_t o = tmem + CF::kTmemO + (CF::kByTile ? b * CF::kNT : 0);
+    uint64_t v = v0 + b * (kVTile >> 4), x = p0 + b * (kPTile >> 4);
+    uint32_t more = in_piece >= CF::kAccs;  // the accumulator holds tiles of this piece
 #pragma unroll 1
-  for (;;) {
-    if (!step(std::integral_constant<int, 0>{}) || !step(std::integral_constant<int, 1>{})) break;
-    phase ^= 1u;
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int k16 = 0; k16 < kTile / 32; ++k16) {  // two 8-key groups of 1 KB each
+        tc_mma_elect(o, v + k16 * 128, x + k16 * 128, idesc, more);
+        more = 1;
+      }
+      v += kTile / 32 * 128;
+      x += kTile / 32 * 128;
+    }
+    tc_commit_elect(sm.pvdone + 8 * b);
   }
   tc_commit_elect(sm.mmadone + 8);
 }
@@ -556,7 +553,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
   bool good = true;               // no wait of this warp has given up
   int rb = 0, set = -1;           // the piece's row block, and its set of rows
   auto begin = [&](int t) {
-    const TileMeta w = sm.meta[t % kMetas];
+    const TileMeta w = tile_meta(sm, t);
     if (!sync(wait)) return false;  // the piece before has been written out
     rb = w.rb;
     if (w.flags & kNewRows) set = (set + 1) & (kRowSets - 1);  // (built before q was staged, so before S)
@@ -586,10 +583,10 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     const bool ok = fresh || wait(sm.pvdone + 8 * (mine & 1), (mine >> 1) & 1);
     if (!__all_sync(0xffffffffu, ok) || !sync(wait)) return false;
     const bool two = t > t_first;
-    if (threadIdx.x < CF::kNC) join_sums<CF>(p, smem, sm.rows[set].place, smem.meta[t % kMetas], threadIdx.x, two || !(t & 1), two || (t & 1));
+    if (threadIdx.x < CF::kNC) join_sums<CF>(p, smem, sm.rows[set].place, tile_meta(sm, t), threadIdx.x, two || !(t & 1), two || (t & 1));
     if (!sync(wait)) return false;
     tc_fence_after();
-    write_rows<CF::kAccs>(p, smem, sm.rows[set].place, smem.meta[t % kMetas], wg * (CF::kNC / 2), (wg + 1) * (CF::kNC / 2), trow + CF::kTmemO, CF::kNT);
+    write_rows<CF::kAccs>(p, smem, sm.rows[set].place, tile_meta(sm, t), wg * (CF::kNC / 2), (wg + 1) * (CF::kNC / 2), trow + CF::kTmemO, CF::kNT);
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(sm.ofree);
@@ -601,19 +598,20 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     const uint32_t phase = (t >> 1) & 1;
     // S, and with it the words of the tile and of those before it.  (A warp whose wait gives up goes on to the vote: the
     // warps of a warpgroup leave there, together.)
+    int flags = tile_flags(sm, t), before = CF::kByTile && t > 0 ? tile_flags(sm, t - 1) : 0;
     good = good && __all_sync(0xffffffffu, wait(sm.qkdone + 8 * b, phase));
+    if (!is_of(flags, t)) flags = tile_flags(sm, t);
     if (CF::kByTile && good && t > 0) {  // the tile before is the other warpgroup's
-      const int flags = sm.meta[(t - 1) % kMetas].flags;
-      if (flags & kFirst) good = begin(t - 1);
-      if (good && (flags & kLast)) good = end(t - 1);
+      if (!is_of(before, t - 1)) before = tile_flags(sm, t - 1);
+      if (before & kFirst) good = begin(t - 1);
+      if (good && (before & kLast)) good = end(t - 1);
     }
-    const int4 meta = *reinterpret_cast<const int4*>(sm.meta + t % kMetas);  // flags, key0, nkeys, L
-    const bool stop = good && (meta.x & kStop);
-    if (good && (meta.x & kFirst) && !stop) good = begin(t);
-    const bool draft = meta.x & kDraft;
+    const bool stop = good && (flags & kStop);
+    if (good && (flags & kFirst) && !stop) good = begin(t);
+    const bool draft = flags & kDraft;
     const float qs = draft ? p.qscale : p.qscale * p.k_scale;
     uint64_t vis = ~0ull;
-    if (good && !stop && (meta.x & kMasked)) vis = rows_seeing(kp, sm.rows[set], meta, rb, key) >> col0;
+    if (good && !stop && (flags & kMasked)) vis = rows_seeing(kp, sm.rows[set], tile_words(sm, t), rb, key) >> col0;
     // The buffer of P is free when P.V of the tile before the last is done (by tile: O is at rest then, too).
     good = good && (stop || __all_sync(0xffffffffu, wait(sm.pvdone + 8 * b, phase ^ 1u)));
     tc_fence_after();
@@ -674,7 +672,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     __syncwarp();
     if (lane == 0) mbar_arrive(sm.pfull + 8 * b);
     fresh = false;
-    if (meta.x & kLast) good = end(t);
+    if (flags & kLast) good = end(t);
   }
 }
 
@@ -703,10 +701,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
     }
     mbar_init(sm.ofree, 8);
     mbar_init(sm.joined, 8);
-    *sm.abort = 0;
+    init_waits(p);
     *sm.issued = 0;
     fence_mbar_init();
   }
+  if (warp == kWarpQ && (threadIdx.x & 31) < kMetas)  // (what an earlier CTA left there is of no tile)
+    sts128(sm.meta + (threadIdx.x & 31) * sizeof(TileMeta), make_uint4(~0u, 0u, 0u, 0u));
   if (warp == kWarpQk) {
     tmem_alloc(smem_addr(sm.tmem), CF::kTmemCols);
     tmem_relinquish();
@@ -715,13 +715,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *sm.tmem;
-  const Waiter wait{p.err, p.wait_ns, sm.abort, p.wait_ns < kPollBelowNs};
+  const Waiter wait{p.wait_ns < kPollBelowNs};
   if (warp < kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem);
   else if (warp < kWarpLoad) run_decode<CF>(kp, sm, wait, tmem);
   else if (warp == kWarpLoad) run_loader<CF::kStages, 2>(kp, sm, wait);  // (a last word for each warpgroup)
   else if (warp == kWarpQk) run_qk<CF>(sm, wait, tmem);
   else if (warp == kWarpPv) run_pv<CF>(sm, wait, tmem);
-  else run_q<CF>(kp, sm, wait);
+  else if (warp == kWarpQ) run_q<CF>(kp, sm, wait);
   __syncwarp();
   tc_fence_before();
   __syncthreads();
@@ -736,6 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   if (warp == kWarpQk) tmem_dealloc(tmem, CF::kTmemCols);
 }
 
+constexpr int kMmaRows = 16;
 constexpr int kMaxRows = 64;  // query rows of a unit
 
 int rows_of_unit(int rows) {
@@ -756,7 +757,11 @@ cudaError_t launch_cfg(const Kv4Params& kp, bool pdl, cudaStream_t stream) {
 cudaError_t launch(const Kv4Params& kp, bool pdl, cudaStream_t stream) {
   switch (kp.a.rows_per_unit) {
     case 8:
-    case 16: return launch_attn_kv4_mma(kp, pdl, stream);
+      if (kMmaRows >= 8) return launch_attn_kv4_mma(kp, pdl, stream);
+      return launch_cfg<Cfg<8>>(kp, pdl, stream);
+    case 16:
+      if (kMmaRows >= 16) return launch_attn_kv4_mma(kp, pdl, stream);
+      return launch_cfg<Cfg<16>>(kp, pdl, stream);
     case 32: return launch_cfg<Cfg<32>>(kp, pdl, stream);
     case 48: return launch_cfg<Cfg<48>>(kp, pdl, stream);
     case 64: return launch_cfg<Cfg<64>>(kp, pdl, stream);
@@ -800,7 +805,7 @@ kvshot_status make_kv4_plan(const kvshot_attn_desc* d, int32_t window, int32_t s
   if (grid == 0) {
     const int sms = sm_count();
     int per_sm = 1;
-    if (pl->rows_per_unit <= 16 && attn_kv4_mma_occupancy(pl->rows_per_unit, d->num_caches, &per_sm) != cudaSuccess)
+    if (pl->rows_per_unit <= kMmaRows && attn_kv4_mma_occupancy(pl->rows_per_unit, d->num_caches, &per_sm) != cudaSuccess)
       return KVSHOT_ERR_CUDA;
     if (sms < 1 || per_sm < 1) return KVSHOT_ERR_CUDA;
     grid = std::min<int64_t>(sms * per_sm, std::max((max_tiles + kMinTiles - 1) / kMinTiles, units));

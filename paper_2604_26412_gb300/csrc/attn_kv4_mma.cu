@@ -39,7 +39,6 @@ struct Smem : Ring {
   uint32_t joined;      // barrier of the consumer warps
   float* comb_o;        // [kWarps][rows][kCombStride] a piece's O of each warp
   float *ref, *sum;     // [kWarps][rows] its references and sums; then (ref) its weights
-  volatile int* abort;
 };
 
 template <class CF>
@@ -56,15 +55,15 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.comb_o = reinterpret_cast<float*>(b + CF::kStages * kStageSize);
   s.ref = s.comb_o + kWarps * CF::kRows * kCombStride;
   s.sum = s.ref + kWarps * CF::kRows;
-  s.meta = reinterpret_cast<TileMeta*>(s.sum + kWarps * CF::kRows);
-  uint64_t* m = reinterpret_cast<uint64_t*>(s.meta + kMetas);
+  TileMeta* meta = reinterpret_cast<TileMeta*>(s.sum + kWarps * CF::kRows);
+  s.meta = smem_addr(meta);
+  uint64_t* m = reinterpret_cast<uint64_t*>(meta + kMetas);
   s.cfull = smem_addr(m);
   s.cempty = s.cfull + 8 * CF::kStages;
   s.joined = s.cempty + 8 * CF::kStages;
   s.rows = reinterpret_cast<Rows*>(m + 2 * CF::kStages + 2);
   int* words = reinterpret_cast<int*>(s.rows + 1);
-  s.abort = reinterpret_cast<volatile int*>(words);
-  s.issued = words + 1;
+  s.issued = words;
   s.len = words + 4;
   s.base = s.len + C;
   return s;
@@ -159,11 +158,11 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
 #pragma unroll 1
   for (int t = 0;; ++t) {
     if (!__all_sync(0xffffffffu, wait(sm.cfull + 8 * stage, phase))) return;
-    const int4 meta = *reinterpret_cast<const int4*>(sm.meta + t % kMetas);  // flags, key0, nkeys, L
+    const int4 meta = tile_words(sm, t);  // flags, key0, nkeys, L
     if (meta.x & kStop) return;
     const bool draft = meta.x & kDraft, masked = meta.x & kMasked;
     if (meta.x & kFirst) {
-      const TileMeta w = sm.meta[t % kMetas];
+      const TileMeta w = tile_meta(sm, t);
       if (!sync(wait)) return;  // the piece before has been written out
       rb = w.rb;
       if (w.flags & kNewRows) {
@@ -377,7 +376,7 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
           *reinterpret_cast<float4*>(sm.comb_o + row * kCombStride + 32 * c + 4 * g) =
               make_float4(o[2 * c][nr][e] * vs, o[2 * c + 1][nr][e] * vs, o[2 * c][nr][2 + e] * vs, o[2 * c + 1][nr][2 + e] * vs);
       }
-    if (!join_warps<CF::kRows>(p, smem, sm.meta[t % kMetas], sync, wait)) return;
+    if (!join_warps<CF::kRows>(p, smem, tile_meta(sm, t), sync, wait)) return;
   }
 }
 
@@ -394,12 +393,12 @@ __global__ void __launch_bounds__(kThreads, CF::kMinBlocks) attn_kv4_mma_kernel(
       mbar_init(sm.cempty + 8 * s, kWarps);
     }
     mbar_init(sm.joined, kWarps);
-    *sm.abort = 0;
+    init_waits(p);
     *sm.issued = 0;
     fence_mbar_init();
   }
   __syncthreads();
-  const Waiter wait{p.err, p.wait_ns, sm.abort, p.wait_ns < kPollBelowNs};
+  const Waiter wait{p.wait_ns < kPollBelowNs};
   if (threadIdx.x >= 32 * kWarps) run_loader<CF::kStages, 1>(kp, sm, wait);
   else run_consumer<CF>(kp, sm, wait);
   __syncthreads();

@@ -62,16 +62,17 @@ constexpr int kNewRows = 32;           // the query rows' nodes differ from the 
 constexpr int kNewTree = 64;           // and so does the draft tree
 constexpr int kStop = 128;             // no tile: the CTA's work is done
 struct TileMeta {
-  int flags, key0, nkeys, L;  // first key (token, or draft slot), valid keys, prefix length
+  int flags, key0, nkeys, L;  // (and the tile's number above bit 16); first key (token, or draft slot), valid keys, prefix length
   int c, h, rb, seq;          // cache, KV head, row block, sequence
 };
 constexpr int kMetas = 16;    // more than the tiles between the loader and the last reader
+constexpr int kTagShift = 16;
 
 // Shared-memory parts that both kernels have: the ring of the cache's bytes (addresses of its stages and of its barriers,
 // landed and read) with the tiles' words.
 struct Ring {
   uint32_t ring, cfull, cempty;
-  TileMeta* meta;   // [kMetas]
+  uint32_t meta;    // [kMetas] TileMeta
   int* issued;      // tiles issued by the loader
   int *len, *base;  // the loader's plan
 };
@@ -85,31 +86,71 @@ struct Rows {
 };
 
 // Every wait ends: when its phase completes, when another role has given up, or (which gives up) after the call's limit.
-// The inline part is one try, which blocks for a while (a call for each wait took more instructions than it waited for).
-__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, int32_t* err, uint64_t limit_ns, volatile int* abort) {
-  const bool poll = limit_ns < kPollBelowNs;  // (a blocking try could sit out a short limit)
-  const uint64_t t0 = global_timer_ns();
+// The inline part is one try, which blocks for a while; what the rest needs lies in shared memory, so that the many places
+// that wait are short.
+struct WaitLimits {
+  int32_t* err;
+  uint64_t limit_ns;
+  int abort;  // a wait has given up
+  int poll;   // a limit that a blocking try could sit out
+};
+__device__ __forceinline__ WaitLimits* wait_limits() {
+  __shared__ WaitLimits s_limits;
+  return &s_limits;
+}
+__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity) {
+  volatile WaitLimits* w = wait_limits();
+  const uint64_t t0 = global_timer_ns(), limit = w->limit_ns;
   for (;;) {
-    for (int i = 0; i < (poll ? 1 : 16); ++i)
-      if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
-    if (*abort) return false;
-    if (global_timer_ns() - t0 > limit_ns) break;
+#pragma unroll 1
+    for (int i = 0; i < 16; ++i)
+      if (w->poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
+    if (w->abort) return false;
+    if (global_timer_ns() - t0 > limit) break;
   }
-  set_error(err, KVSHOT_ERR_TIMEOUT);
-  *abort = 1;
+  set_error(w->err, KVSHOT_ERR_TIMEOUT);
+  w->abort = 1;
   return false;
 }
-
+// One thread, before the first wait and a barrier.
+__device__ __forceinline__ void init_waits(const AttnParams& p) {
+  WaitLimits* w = wait_limits();
+  w->err = p.err;
+  w->limit_ns = p.wait_ns;
+  w->abort = 0;
+  w->poll = p.wait_ns < kPollBelowNs;
+}
 struct Waiter {
-  int32_t* err;
-  uint64_t limit;
-  volatile int* abort;
   bool poll;
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
     if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
-    return wait_slow(bar, parity, err, limit, abort);
+    return wait_slow(bar, parity);
   }
 };
+
+__device__ __forceinline__ void sts128(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+               : "memory");
+}
+__device__ __forceinline__ int lds32(uint32_t addr) {
+  int v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// The words of tile t, once something that follows from its landing has been waited for.
+__device__ __forceinline__ int4 tile_words(const Ring& r, int t) {
+  const uint4 v = lds128(r.meta + t % kMetas * sizeof(TileMeta));
+  return make_int4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ TileMeta tile_meta(const Ring& r, int t) {
+  const uint4 v = lds128(r.meta + t % kMetas * sizeof(TileMeta)), w = lds128(r.meta + t % kMetas * sizeof(TileMeta) + 16);
+  return TileMeta{static_cast<int>(v.x), static_cast<int>(v.y), static_cast<int>(v.z), static_cast<int>(v.w),
+                  static_cast<int>(w.x), static_cast<int>(w.y), static_cast<int>(w.z), static_cast<int>(w.w)};
+}
+// Its flags alone, read ahead of the wait; they are the tile's if is_of says so, and else are read again after it.
+__device__ __forceinline__ int tile_flags(const Ring& r, int t) { return lds32(r.meta + t % kMetas * sizeof(TileMeta)); }
+__device__ __forceinline__ bool is_of(int flags, int t) { return ((flags >> kTagShift) & 0xffff) == (t & 0xffff); }
 
 // ------------------------------------------------------------ loads
 
@@ -242,9 +283,9 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
       if (!ok) break;
       const uint32_t bar = sm.cfull + 8 * stage, dst = sm.ring + stage * kStageSize;
       if (lane == 0) {
-        int4* m = reinterpret_cast<int4*>(sm.meta + issued % kMetas);
-        m[0] = make_int4(flags, key0, nkeys, L);
-        m[1] = make_int4(c, h, rb, seq);
+        const uint32_t m = sm.meta + issued % kMetas * sizeof(TileMeta);
+        sts128(m, make_uint4(flags | issued << kTagShift, key0, nkeys, L));
+        sts128(m + 16, make_uint4(c, h, rb, seq));
         mbar_arrive_expect_tx(bar, draft ? nkeys * 4 * kHeadDim : (nkeys + kKv4Tokens - 1) / kKv4Tokens * kKv4Bytes);
       }
       __syncwarp();
@@ -274,7 +315,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
     ok = __all_sync(0xffffffffu, wait(sm.cempty + 8 * stage, phase ^ 1u));
     if (!ok) break;
     if (lane == 0) {
-      sm.meta[issued % kMetas].flags = kStop;
+      sts128(sm.meta + issued % kMetas * sizeof(TileMeta), make_uint4(kStop | issued << kTagShift, 0, 0, 0));
       mbar_arrive(sm.cfull + 8 * stage);
     }
     ++issued;
@@ -313,10 +354,6 @@ __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ void sts128(uint32_t addr, uint4 v) {
-  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
-               : "memory");
 }
 __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   uint2 v;
@@ -401,7 +438,7 @@ __device__ __noinline__ void build_rows(const Kv4Params& kp, Rows& r, int nc, in
 }
 
 // Bits of the unit's rows that see key `key` of a masked tile (m: its words' flags, key0, nkeys, L).
-__device__ __forceinline__ uint64_t rows_seeing(const Kv4Params& kp, const Rows& r, const int4& m, int rb, int key) {
+__device__ __noinline__ uint64_t rows_seeing(const Kv4Params& kp, const Rows& r, const int4& m, int rb, int key) {
   const AttnParams& p = kp.a;
   if (key >= m.z) return 0ull;
   const bool draft = m.x & kDraft;
