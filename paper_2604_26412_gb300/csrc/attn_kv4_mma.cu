@@ -34,16 +34,20 @@ struct Cfg {
   static constexpr int kRows = 8 * NR;
 };
 
+template <int NR>
+constexpr int kQChunk = NR * 32 * 16;  // bytes of a chunk's Q^T fragments
+
 struct Smem : Ring {
   Rows* rows;
   uint32_t joined;      // barrier of the consumer warps
+  uint32_t q;           // [chunk][row step][lane] 16 B: Q^T fragments of the piece's rows
   float* comb_o;        // [kWarps][rows][kCombStride] a piece's O of each warp
   float *ref, *sum;     // [kWarps][rows] its references and sums; then (ref) its weights
 };
 
 template <class CF>
 __host__ __device__ constexpr size_t smem_bytes(int C) {
-  return 128 + CF::kStages * kStageSize + sizeof(float) * kWarps * CF::kRows * (kCombStride + 2) +
+  return 128 + CF::kStages * kStageSize + kQChunk<CF::kNR> * 4 + sizeof(float) * kWarps * CF::kRows * (kCombStride + 2) +
          sizeof(TileMeta) * kMetas + sizeof(Rows) + sizeof(uint64_t) * (2 * CF::kStages + 2) + sizeof(int) * (4 + 2 * C + 1);
 }
 
@@ -52,7 +56,8 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   Smem s;
   uint8_t* b = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~uintptr_t(127));
   s.ring = smem_addr(b);
-  s.comb_o = reinterpret_cast<float*>(b + CF::kStages * kStageSize);
+  s.q = s.ring + CF::kStages * kStageSize;
+  s.comb_o = reinterpret_cast<float*>(b + CF::kStages * kStageSize + 4 * kQChunk<CF::kNR>);
   s.ref = s.comb_o + kWarps * CF::kRows * kCombStride;
   s.sum = s.ref + kWarps * CF::kRows;
   TileMeta* meta = reinterpret_cast<TileMeta*>(s.sum + kWarps * CF::kRows);
@@ -135,6 +140,80 @@ __device__ __noinline__ bool join_warps(const AttnParams& p, const Smem& sm, con
   return true;
 }
 
+// A warp's part of a piece.
+template <int NR>
+struct State {
+  float o[8][NR][4];  // o[2 c + kk][nr][2 a + e]: dim 32 c + 4 g + kk + 2 a of row 8 nr + 2 q4 + e
+  float ref[NR][2], l[NR][2];  // rows 8 nr + 2 q4 + e; l: this lane's keys only
+};
+
+// Scores to P^T fragments: s[i][nr][2 a + e] is key 16 i + 8 a + g, row 8 nr + 2 q4 + e.  `units`: what O is multiplied
+// with when it changes its units (then `change`), which moves the references, too.
+template <int NR, int KG>
+__device__ __forceinline__ void softmax_step(State<NR>& st, const float (&s)[KG][NR][4], float qs, bool change, float units,
+                                             uint32_t (&pb)[KG][NR][2]) {
+  float top[NR][2];
+  bool grow = change;
+#pragma unroll
+  for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float v = fmaxf(s[0][nr][e], s[0][nr][2 + e]);
+#pragma unroll
+      for (int i = 1; i < KG; ++i) v = max3(v, s[i][nr][e], s[i][nr][2 + e]);
+      top[nr][e] = v;
+      grow |= fmaf(v, qs, -st.ref[nr][e]) > kRefLimit;
+    }
+  if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+    for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float v = top[nr][e] * qs;
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+        const float to = v - st.ref[nr][e] > kRefLimit ? v - kRefBelow : st.ref[nr][e];
+        const float alpha = ex2(st.ref[nr][e] - to), o_alpha = alpha * units;
+        st.ref[nr][e] = to;
+        st.l[nr][e] *= alpha;
+#pragma unroll
+        for (int mt = 0; mt < 8; ++mt) {
+          st.o[mt][nr][e] *= o_alpha;
+          st.o[mt][nr][2 + e] *= o_alpha;
+        }
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < KG; ++i)
+#pragma unroll
+    for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        const float e0 = ex2(fmaf(s[i][nr][2 * a], qs, -st.ref[nr][0])), e1 = ex2(fmaf(s[i][nr][2 * a + 1], qs, -st.ref[nr][1]));
+        st.l[nr][0] += e0;
+        st.l[nr][1] += e1;
+        pb[i][nr][a] = movmatrix_trans(pack_f16x2(e0, e1));
+      }
+}
+
+// Keys that the rows' masks hide: scores of key `key` (of the tile) of s[...][nr][2 a + e].
+template <int NR>
+__device__ __forceinline__ void hide(float (&s)[NR][4], const Kv4Params& kp, const Rows& rows, const int4& meta, int rb, int key,
+                                     int q4) {
+#pragma unroll 1
+  for (int a = 0; a < 2; ++a) {
+    const uint64_t vis = rows_seeing(kp, rows, meta, rb, key + 8 * a) >> (2 * q4);
+#pragma unroll
+    for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (!((vis >> (8 * nr + e)) & 1ull)) {
+          if (a == 0) s[nr][e] = -INFINITY;
+          else s[nr][2 + e] = -INFINITY;
+        }
+  }
+}
+
 template <class CF>
 __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& smem, const Waiter& wait) {
   constexpr int NR = CF::kNR;
@@ -145,12 +224,11 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
   // lane % 16), the scales of its keys (K: token g; V: tokens 2 q4, 2 q4 + 1) and which of them it takes.
   const uint32_t kaddr = (lane >> 3) * kChunkStride + (lane & 7) * kChunkBytes;
   const uint32_t vaddr = kVCodes + (lane >> 4) * kChunkStride + (lane & 15) * kChunkBytes;
+  const uint32_t qaddr = sm.q + lane * 16;
   const uint32_t kscale = kScales + g * 8, vscale = kScales + kScaleBytes + q4 * 16;
   const uint32_t ksel = q4 & 2 ? 0x3311u : 0x2200u, vsel = g & 4 ? 0x7351u : 0x6240u;
   WarpSync sync{sm.joined, 0};
-  // Q^T fragments (f16): k-step 2 c + h on dims 32 c + 8 q4 + 4 h + {0, 1}, {2, 3} of row 8 nr + g.
-  uint2 q[8][NR];
-  float o[8][NR][4], ref[NR][2], l[NR][2];  // rows 8 nr + 2 q4 + e; l: this lane's keys only
+  State<NR> st;
   bool in_codes = false;                    // O is in units of the value codes (a warp without draft keys keeps it so)
   wait_for_prerequisite_grid();             // q and the outputs may be the preceding kernel's
   int stage = 0, rb = 0;
@@ -169,62 +247,125 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
         if (warp == 0) build_rows(kp, *sm.rows, CF::kRows, w.rb, w.seq, w.flags & kNewTree);
         if (!sync(wait)) return;
       }
-      const __nv_bfloat16* qrow = p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim + 8 * q4;
+      // Q^T fragments (f16), a chunk by each warp: lane (g, q4) holds dims 32 c + 8 q4 .. + 7 of row 8 nr + g, for the
+      // chunk's two k-steps.
+      const __nv_bfloat16* qrow =
+          p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim + 32 * warp + 8 * q4;
       const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr) {
-        const uint4* src = reinterpret_cast<const uint4*>(qrow + static_cast<size_t>(sm.rows->place[8 * nr + g]) * kHeadDim);
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (8 * nr + g < rows)
+          x = *reinterpret_cast<const uint4*>(qrow + static_cast<size_t>(sm.rows->place[8 * nr + g]) * kHeadDim);
+        sts128(sm.q + warp * kQChunk<NR> + nr * 512 + lane * 16,
+               make_uint4(bf16x2_to_f16x2(x.x), bf16x2_to_f16x2(x.y), bf16x2_to_f16x2(x.z), bf16x2_to_f16x2(x.w)));
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint4 x = make_uint4(0u, 0u, 0u, 0u);
-          if (8 * nr + g < rows) x = src[4 * c];
-          q[2 * c][nr] = make_uint2(bf16x2_to_f16x2(x.x), bf16x2_to_f16x2(x.y));
-          q[2 * c + 1][nr] = make_uint2(bf16x2_to_f16x2(x.z), bf16x2_to_f16x2(x.w));
-        }
-#pragma unroll
-        for (int mt = 0; mt < 8; ++mt) o[mt][nr][0] = o[mt][nr][1] = o[mt][nr][2] = o[mt][nr][3] = 0.f;
-        ref[nr][0] = ref[nr][1] = kNoRef;
-        l[nr][0] = l[nr][1] = 0.f;
+        for (int mt = 0; mt < 8; ++mt) st.o[mt][nr][0] = st.o[mt][nr][1] = st.o[mt][nr][2] = st.o[mt][nr][3] = 0.f;
+        st.ref[nr][0] = st.ref[nr][1] = kNoRef;
+        st.l[nr][0] = st.l[nr][1] = 0.f;
       }
       in_codes = !draft;
+      if (!sync(wait)) return;
     }
-    const float qs = draft ? p.qscale : p.qscale * p.k_scale;
     const uint32_t tile = sm.ring + stage * kStageSize;
-    // 16 keys (a group of the cache) at a time: two groups of a prefix tile to a warp, one of a draft tile.
-    const int last = draft ? warp + 1 : 2 * warp + 2;
-#pragma unroll 1
-    for (int grp = draft ? warp : 2 * warp; grp < last; ++grp) {
-      const int kw = 16 * grp;
-      if (kw >= meta.z) break;
-      const uint32_t at = tile + grp * kKv4Bytes;
-      // S^T: s[nr][2 a + e] is key kw + 8 a + g, row 8 nr + 2 q4 + e.
-      float s[NR][4];
+    if (!draft) {
+      // A warp takes two groups of the cache (32 keys) together.
+      const int kw = 32 * warp;
+      if (kw < meta.z) {
+        const uint32_t at = tile + 2 * warp * kKv4Bytes;
+        float s[2][NR][4];
 #pragma unroll
-      for (int nr = 0; nr < NR; ++nr) s[nr][0] = s[nr][1] = s[nr][2] = s[nr][3] = 0.f;
-      if (!draft) {
-        uint32_t a[4], b[4];  // keys g and g + 8: a word of each chunk
-        ldmatrix_x4(at + kaddr, a[0], a[1], a[2], a[3]);
-        ldmatrix_x4(at + kaddr + 8 * kChunkBytes, b[0], b[1], b[2], b[3]);
-        const uint2 sa = lds64(at + kscale), sb = lds64(at + kscale + 64);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) s[i][nr][0] = s[i][nr][1] = s[i][nr][2] = s[i][nr][3] = 0.f;
+        uint32_t w[2][2][4];  // group, keys g and g + 8: a word of each chunk
+        uint2 sk[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+            ldmatrix_x4(at + i * kKv4Bytes + kaddr + 8 * a * kChunkBytes, w[i][a][0], w[i][a][1], w[i][a][2], w[i][a][3]);
+            sk[i][a] = lds64(at + i * kKv4Bytes + kscale + 64 * a);
+          }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const uint2 sca = scales_of(c < 2 ? sa.x : sa.y, 0, ksel), scb = scales_of(c < 2 ? sb.x : sb.y, 0, ksel);
-          const uint32_t s2a = c & 1 ? sca.y : sca.x, s2b = c & 1 ? scb.y : scb.x;
-          uint32_t fa[4], fb[4];
-          e2m1x8_to_f16(a[c], fa);
-          e2m1x8_to_f16(b[c], fb);
+          uint4 q[NR];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            fa[k] = mul_f16x2(fa[k], s2a);
-            fb[k] = mul_f16x2(fb[k], s2b);
-          }
+          for (int nr = 0; nr < NR; ++nr) q[nr] = lds128(qaddr + c * kQChunk<NR> + nr * 512);
 #pragma unroll
-          for (int nr = 0; nr < NR; ++nr) {
-            mma_f16(s[nr], fa[0], fb[0], fa[1], fb[1], q[2 * c][nr].x, q[2 * c][nr].y);
-            mma_f16(s[nr], fa[2], fb[2], fa[3], fb[3], q[2 * c + 1][nr].x, q[2 * c + 1][nr].y);
+          for (int i = 0; i < 2; ++i) {
+            uint32_t f[2][4];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+              const uint2 pair = scales_of(c < 2 ? sk[i][a].x : sk[i][a].y, 0, ksel);
+              const uint32_t s2 = c & 1 ? pair.y : pair.x;
+              e2m1x8_to_f16(w[i][a][c], f[a]);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) f[a][k] = mul_f16x2(f[a][k], s2);
+            }
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+              mma_f16(s[i][nr], f[0][0], f[1][0], f[0][1], f[1][1], q[nr].x, q[nr].y);
+              mma_f16(s[i][nr], f[0][2], f[1][2], f[0][3], f[1][3], q[nr].z, q[nr].w);
+            }
           }
         }
-      } else {
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) hide<NR>(s[i], kp, *sm.rows, meta, rb, kw + 16 * i + g, q4);
+        }
+        uint32_t pb[2][NR][2];
+        softmax_step<NR, 2>(st, s, p.qscale * p.k_scale, false, 1.f, pb);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t vat = at + i * kKv4Bytes;
+          uint32_t v[4][2];  // chunk; tokens 0..7 and 8..15
+          ldmatrix_x4_trans(vat + vaddr, v[0][0], v[0][1], v[1][0], v[1][1]);
+          ldmatrix_x4_trans(vat + vaddr + 2 * kChunkStride, v[2][0], v[2][1], v[3][0], v[3][1]);
+          uint4 sc[2] = {lds128(vat + vscale), lds128(vat + vscale + 64)};  // tokens 2 q4, 2 q4 + 1 and those + 8
+          if (masked) {
+            // Keys that no row sees may hold anything, NaN scales among it: 0 times them must be 0.
+            const int lo = p.window > 0 ? meta.w + p.min_depth - p.window : 0;
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+              const int key = kw + 16 * i + 8 * a + 2 * q4, pos = meta.y + key;
+              if (key >= meta.z || (pos < lo && pos >= p.sinks)) sc[a].x = sc[a].y = 0u;
+              if (key + 1 >= meta.z || (pos + 1 < lo && pos + 1 >= p.sinks)) sc[a].z = sc[a].w = 0u;
+            }
+          }
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            // Codes of dims 4 g .. 4 g + 3: of keys 2 q4 and 2 q4 + 8, and of the keys after them; then dim by dim the
+            // codes of two neighbouring keys in a byte (dims 0, 2 of the keys and of those + 8; dims 1, 3).
+            const uint32_t x = __byte_perm(v[c][0], v[c][1], 0x5410), y = __byte_perm(v[c][0], v[c][1], 0x7632);
+            uint32_t f[8];
+            e2m1x8_to_f16(select_bits(x, y << 4, 0x0f0f0f0fu), *reinterpret_cast<uint32_t(*)[4]>(&f[0]));
+            e2m1x8_to_f16(select_bits(x >> 4, y, 0x0f0f0f0fu), *reinterpret_cast<uint32_t(*)[4]>(&f[4]));
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+              const uint2 pair = scales_of(c < 2 ? sc[a].x : sc[a].y, c < 2 ? sc[a].z : sc[a].w, vsel);
+              const uint32_t s2 = c & 1 ? pair.y : pair.x;
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                f[2 * a + k] = mul_f16x2(f[2 * a + k], s2);
+                f[4 + 2 * a + k] = mul_f16x2(f[4 + 2 * a + k], s2);
+              }
+            }
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+              mma_f16(st.o[2 * c][nr], f[0], f[1], f[2], f[3], pb[i][nr][0], pb[i][nr][1]);
+              mma_f16(st.o[2 * c + 1][nr], f[4], f[5], f[6], f[7], pb[i][nr][0], pb[i][nr][1]);
+            }
+          }
+        }
+      }
+    } else {
+      // 16 keys to a warp, bf16 (the first two warps).
+      const int kw = 16 * warp;
+      if (kw < meta.z) {
+        float s[1][NR][4];
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) s[0][nr][0] = s[0][nr][1] = s[0][nr][2] = s[0][nr][3] = 0.f;
         const uint32_t krow = tile + (kw + g) * kDraftRow + 16 * q4;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -233,102 +374,15 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
                                  bf16x2_to_f16x2(x.z), bf16x2_to_f16x2(y.z), bf16x2_to_f16x2(x.w), bf16x2_to_f16x2(y.w)};
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr) {
-            mma_f16(s[nr], f[0], f[1], f[2], f[3], q[2 * c][nr].x, q[2 * c][nr].y);
-            mma_f16(s[nr], f[4], f[5], f[6], f[7], q[2 * c + 1][nr].x, q[2 * c + 1][nr].y);
+            const uint4 q = lds128(qaddr + c * kQChunk<NR> + nr * 512);
+            mma_f16(s[0][nr], f[0], f[1], f[2], f[3], q.x, q.y);
+            mma_f16(s[0][nr], f[4], f[5], f[6], f[7], q.z, q.w);
           }
         }
-      }
-      if (masked) {
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          const uint64_t vis = rows_seeing(kp, *sm.rows, meta, rb, kw + 8 * a + g) >> (2 * q4);
-#pragma unroll
-          for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              if (!((vis >> (8 * nr + e)) & 1ull)) s[nr][2 * a + e] = -INFINITY;
-        }
-      }
-      bool grow = draft && in_codes && p.v_scale != 1.f;  // (O leaves the codes)
-      float mx[NR][2];
-#pragma unroll
-      for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          mx[nr][e] = fmaf(fmaxf(s[nr][e], s[nr][2 + e]), qs, -ref[nr][e]);
-          grow |= mx[nr][e] > kRefLimit;
-        }
-      if (__any_sync(0xffffffffu, grow)) {
-        const float vs = draft && in_codes ? p.v_scale : 1.f;
-#pragma unroll
-        for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float v = fmaxf(s[nr][e], s[nr][2 + e]) * qs;
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-            const float to = v - ref[nr][e] > kRefLimit ? v - kRefBelow : ref[nr][e];
-            const float alpha = ex2(ref[nr][e] - to), o_alpha = alpha * vs;
-            ref[nr][e] = to;
-            l[nr][e] *= alpha;
-#pragma unroll
-            for (int mt = 0; mt < 8; ++mt) {
-              o[mt][nr][e] *= o_alpha;
-              o[mt][nr][2 + e] *= o_alpha;
-            }
-          }
-      }
-      if (draft) in_codes = false;
-      uint32_t pb[NR][2];  // P^T fragments
-#pragma unroll
-      for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          const float e0 = ex2(fmaf(s[nr][2 * a], qs, -ref[nr][0])), e1 = ex2(fmaf(s[nr][2 * a + 1], qs, -ref[nr][1]));
-          l[nr][0] += e0;
-          l[nr][1] += e1;
-          pb[nr][a] = movmatrix_trans(pack_f16x2(e0, e1));
-        }
-      if (!draft) {
-        uint32_t v[4][2];  // chunk; tokens 0..7 and 8..15
-        ldmatrix_x4_trans(at + vaddr, v[0][0], v[0][1], v[1][0], v[1][1]);
-        ldmatrix_x4_trans(at + vaddr + 2 * kChunkStride, v[2][0], v[2][1], v[3][0], v[3][1]);
-        uint4 sc[2] = {lds128(at + vscale), lds128(at + vscale + 64)};  // tokens 2 q4, 2 q4 + 1 and those + 8
-        if (masked) {
-          // Keys that no row sees may hold anything, NaN scales among it: 0 times them must be 0.
-          const int lo = p.window > 0 ? meta.w + p.min_depth - p.window : 0;
-#pragma unroll
-          for (int a = 0; a < 2; ++a) {
-            const int key = kw + 8 * a + 2 * q4, pos = meta.y + key;
-            if (key >= meta.z || (pos < lo && pos >= p.sinks)) sc[a].x = sc[a].y = 0u;
-            if (key + 1 >= meta.z || (pos + 1 < lo && pos + 1 >= p.sinks)) sc[a].z = sc[a].w = 0u;
-          }
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          // Codes of dims 4 g .. 4 g + 3: of keys 2 q4 and 2 q4 + 8, and of the keys after them; then dim by dim the
-          // codes of two neighbouring keys in a byte (dims 0, 2 of the keys and of those + 8; dims 1, 3).
-          const uint32_t x = __byte_perm(v[c][0], v[c][1], 0x5410), y = __byte_perm(v[c][0], v[c][1], 0x7632);
-          uint32_t f[8];
-          e2m1x8_to_f16(select_bits(x, y << 4, 0x0f0f0f0fu), *reinterpret_cast<uint32_t(*)[4]>(&f[0]));
-          e2m1x8_to_f16(select_bits(x >> 4, y, 0x0f0f0f0fu), *reinterpret_cast<uint32_t(*)[4]>(&f[4]));
-#pragma unroll
-          for (int a = 0; a < 2; ++a) {
-            const uint2 pair = scales_of(c < 2 ? sc[a].x : sc[a].y, c < 2 ? sc[a].z : sc[a].w, vsel);
-            const uint32_t s2 = c & 1 ? pair.y : pair.x;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              f[2 * a + k] = mul_f16x2(f[2 * a + k], s2);
-              f[4 + 2 * a + k] = mul_f16x2(f[4 + 2 * a + k], s2);
-            }
-          }
-#pragma unroll
-          for (int nr = 0; nr < NR; ++nr) {
-            mma_f16(o[2 * c][nr], f[0], f[1], f[2], f[3], pb[nr][0], pb[nr][1]);
-            mma_f16(o[2 * c + 1][nr], f[4], f[5], f[6], f[7], pb[nr][0], pb[nr][1]);
-          }
-        }
-      } else {
+        hide<NR>(s[0], kp, *sm.rows, meta, rb, kw + g, q4);
+        uint32_t pb[1][NR][2];
+        softmax_step<NR, 1>(st, s, p.qscale, in_codes && p.v_scale != 1.f, in_codes ? p.v_scale : 1.f, pb);
+        in_codes = false;
         const uint32_t vrow = tile + kDraftV + (kw + 2 * q4) * kDraftRow + 8 * g;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -345,8 +399,8 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
           }
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr) {
-            mma_f16(o[2 * c][nr], f[0], f[1], f[2], f[3], pb[nr][0], pb[nr][1]);
-            mma_f16(o[2 * c + 1][nr], f[4], f[5], f[6], f[7], pb[nr][0], pb[nr][1]);
+            mma_f16(st.o[2 * c][nr], f[0], f[1], f[2], f[3], pb[0][nr][0], pb[0][nr][1]);
+            mma_f16(st.o[2 * c + 1][nr], f[4], f[5], f[6], f[7], pb[0][nr][0], pb[0][nr][1]);
           }
         }
       }
@@ -366,15 +420,16 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
       for (int e = 0; e < 2; ++e) {
         const int row = warp * CF::kRows + 8 * nr + 2 * q4 + e;
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) l[nr][e] += __shfl_xor_sync(0xffffffffu, l[nr][e], d);
+        for (int d = 4; d < 32; d <<= 1) st.l[nr][e] += __shfl_xor_sync(0xffffffffu, st.l[nr][e], d);
         if (g == 0) {
-          sm.ref[row] = ref[nr][e];
-          sm.sum[row] = l[nr][e];
+          sm.ref[row] = st.ref[nr][e];
+          sm.sum[row] = st.l[nr][e];
         }
 #pragma unroll
         for (int c = 0; c < 4; ++c)
           *reinterpret_cast<float4*>(sm.comb_o + row * kCombStride + 32 * c + 4 * g) =
-              make_float4(o[2 * c][nr][e] * vs, o[2 * c + 1][nr][e] * vs, o[2 * c][nr][2 + e] * vs, o[2 * c + 1][nr][2 + e] * vs);
+              make_float4(st.o[2 * c][nr][e] * vs, st.o[2 * c + 1][nr][e] * vs, st.o[2 * c][nr][2 + e] * vs,
+                          st.o[2 * c + 1][nr][2 + e] * vs);
       }
     if (!join_warps<CF::kRows>(p, smem, tile_meta(sm, t), sync, wait)) return;
   }
