@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, CF::kMinBlocks) attn_kv4_mma_kernel(
 }
 
 using Cfg8 = Cfg<1, 2, 3>;
-using Cfg16 = Cfg<2, 3, 2>;
+using Cfg16 = Cfg<2, 2, 2>;
 
 // Every plan that kMaxCaches allows fits an SM.
 static_assert(smem_bytes<Cfg8>(kMaxCaches) <= 227 * 1024 && smem_bytes<Cfg16>(kMaxCaches) <= 227 * 1024,

@@ -8,6 +8,20 @@
 #include "kvshot.h"
 
 namespace kvshot {
+
+// Division by a number that the host knows: n / d for 0 <= n < 2^31.
+struct Div {
+  uint32_t mul, shift, d;
+  static Div by(uint32_t d) {
+    uint32_t l = 0;
+    while ((1ull << l) < d) ++l;
+    return Div{static_cast<uint32_t>(((1ull << 32) * ((1ull << l) - d)) / d + 1), l, d};
+  }
+  __device__ __forceinline__ int operator()(int n) const {
+    return static_cast<int>((__umulhi(static_cast<uint32_t>(n), mul) + static_cast<uint32_t>(n)) >> shift);
+  }
+};
+
 namespace kv4 {
 
 constexpr int kKv4Tokens = KVSHOT_KV4_GROUP_TOKENS;
