@@ -29,6 +29,7 @@ struct ExtendParams {
   int32_t *seq_lens_out, *page_table_out, *free_count_out, *token_start, *slots, *token_cache, *positions;
   int32_t* err;
   int C, P, max_pages, num_pages, num_free, max_tokens;
+  int search;             // the largest power of two below C
   Div by_page, by_entry;  // page size, table entries of a cache
 };
 
@@ -78,41 +79,57 @@ __device__ __forceinline__ void block_scan(int64_t& a, int64_t& b, int64_t* warp
   b += warp > 0 ? below_b : 0;
 }
 
-// Whether the call can be met at all (the same answer in all threads), and what this thread's cache gets: tokens before
-// and with its own, length, pages before it.  kPlanThreads threads.
+// Whether the call can be met at all (the same answer in all threads of the cluster), and what this thread's cache gets:
+// tokens before its own, pages before them.  A cluster of kExtendCluster x kPlanThreads threads; every CTA makes the plan
+// for itself, but for the pages that the call takes, which are checked once.  All inputs that an output may be have been
+// read when it returns.
 struct CachePlan {
   int len, count, start, base;
   int free_count, need, total;  // before the call; of all caches
 };
-__device__ __forceinline__ bool extend_plan(const ExtendParams& p, int64_t* scratch, CachePlan* out) {
+struct PlanShared {
+  int64_t sums[64];
+  int ok[kExtendCluster];  // a CTA's answer to the pages it checked
+};
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ bool extend_plan(const ExtendParams& p, PlanShared& s, CachePlan* out) {
+  cluster_arrive();
   const int c = threadIdx.x;
   const int L = c < p.C ? p.seq_lens[c] : 0, n = c < p.C ? p.new_tokens[c] : 0;
   const int F = *p.free_count;
   bool ok = L >= 0 && n >= 0 && F >= 0 && F <= p.num_free;
   const int64_t used = ok ? pages_of(L, p.P) : 0, after = ok ? pages_of(static_cast<int64_t>(L) + n, p.P) : 0;
   ok = ok && after <= p.max_pages;
-  if (ok && c < p.C && n > 0 && L % p.P != 0) {  // the page that the first new token joins
-    const int pid = p.page_table[static_cast<size_t>(c) * p.max_pages + used - 1];
-    ok = pid >= 0 && pid < p.num_pages;
-  }
+  int joined = 0;  // the page that the first new token joins (looked at after the sums, which its load need not hold up)
+  if (ok && c < p.C && n > 0 && L % p.P != 0) joined = p.page_table[static_cast<size_t>(c) * p.max_pages + used - 1];
   int64_t pages = after - used, tokens = n, need, total;
-  block_scan(pages, tokens, scratch, &need, &total);
-  ok = ok && need <= F && total <= p.max_tokens;
+  block_scan(pages, tokens, s.sums, &need, &total);
+  ok = ok && need <= F && total <= p.max_tokens && joined >= 0 && joined < p.num_pages;
   ok = __syncthreads_and(ok);
-  if (ok) {
-    // The pages that the call takes: eight loads in flight to a thread (one at a time took 20 us for 65k pages).
-    int worst = 0;
+  bool good = ok;
+  if (ok) {  // (eight loads of a thread in flight)
+    constexpr int threads = kExtendCluster * kPlanThreads;
 #pragma unroll 1
-    for (int64_t i0 = F - need + threadIdx.x; i0 < F; i0 += 8 * kPlanThreads) {
+    for (int64_t i0 = F - need + blockIdx.x * kPlanThreads + threadIdx.x; i0 < F; i0 += 8 * threads) {
       int pid[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) pid[i] = i0 + i * kPlanThreads < F ? p.free_pages[i0 + i * kPlanThreads] : 0;
+      for (int i = 0; i < 8; ++i) pid[i] = i0 + i * threads < F ? p.free_pages[i0 + i * threads] : 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) worst |= static_cast<unsigned>(pid[i]) >= static_cast<unsigned>(p.num_pages);
+      for (int i = 0; i < 8; ++i) good = good && static_cast<unsigned>(pid[i]) < static_cast<unsigned>(p.num_pages);
     }
-    ok = worst == 0;
   }
-  ok = __syncthreads_and(ok);
+  good = __syncthreads_and(good);
+  cluster_wait();  // (every CTA has started)
+  if (threadIdx.x < kExtendCluster)
+    asm volatile("{\n\t.reg .u32 ra;\n\tmapa.shared::cluster.u32 ra, %0, %1;\n\tst.shared::cluster.s32 [ra], %2;\n\t}" ::"r"(
+                     smem_addr(s.ok + blockIdx.x)),
+                 "r"(threadIdx.x), "r"(static_cast<int>(good))
+                 : "memory");
+  cluster_arrive();
+  cluster_wait();
+#pragma unroll
+  for (int i = 0; i < kExtendCluster; ++i) ok = ok && s.ok[i] != 0;
   *out = CachePlan{L, n, static_cast<int>(tokens) - n, static_cast<int>(pages - (after - used)), F, static_cast<int>(need),
                    static_cast<int>(total)};
   return ok;
@@ -132,48 +149,69 @@ __device__ __forceinline__ void write_plan(const ExtendParams& p, const CachePla
   }
 }
 
-// The table's entries and the packed tokens' maps: this thread's, of `threads`.  free_count: before the call.
+// The table's entries and the packed tokens' maps: this thread's, of `threads`, four at a time.  free_count: before the
+// call.
 __device__ __forceinline__ void extend_fill(const ExtendParams& p, const ExtendPlan& s, int free_count, int thread, int threads) {
   const bool in_place = p.page_table == p.page_table_out;
   const int entries = p.C * p.max_pages;
-#pragma unroll 4
-  for (int i = thread; i < entries; i += threads) {
-    const int c = p.by_entry(i), j = i - c * p.max_pages;
-    const int used = pages_of(p, s.len[c]), after = pages_of(p, s.len[c] + s.start[c + 1] - s.start[c]);
-    if (j >= used && j < after) p.page_table_out[i] = p.free_pages[free_count - 1 - (s.base[c] + j - used)];
-    else if (!in_place) p.page_table_out[i] = p.page_table[i];
+#pragma unroll 1
+  for (int i0 = thread; i0 < entries; i0 += 4 * threads) {
+    const int32_t* from[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + k * threads;
+      from[k] = nullptr;
+      if (i >= entries) continue;
+      const int c = p.by_entry(i), j = i - c * p.max_pages, L = s.len[c];
+      const int used = pages_of(p, L), after = pages_of(p, L + s.start[c + 1] - s.start[c]);
+      if (j >= used && j < after) from[k] = p.free_pages + free_count - 1 - (s.base[c] + j - used);
+      else if (!in_place) from[k] = p.page_table + i;
+    }
+    int pid[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) pid[k] = from[k] ? *from[k] : 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (from[k]) p.page_table_out[i0 + k * threads] = pid[k];
   }
   const int total = s.start[p.C];
-  for (int t = thread; t < p.max_tokens; t += threads) {
-    int slot = -1, cache = -1, pos = -1;
-    if (t < total) {
-      int lo = 0, hi = p.C - 1;  // last cache whose first token is <= t
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (s.start[mid] <= t) lo = mid;
-        else hi = mid - 1;
-      }
-      cache = lo;
-      const int L = s.len[lo];
-      pos = L + t - s.start[lo];
-      const int j = p.by_page(pos), used = pages_of(p, L);
-      const int32_t* entry = j < used ? p.page_table + static_cast<size_t>(lo) * p.max_pages + j
-                                      : p.free_pages + free_count - 1 - (s.base[lo] + j - used);
-      slot = *entry * p.P + (pos - j * p.P);
+#pragma unroll 1
+  for (int t0 = thread; t0 < p.max_tokens; t0 += 4 * threads) {
+    int c[4] = {0, 0, 0, 0};  // last cache whose first token is <= t
+    for (int step = p.search; step > 0; step >>= 1)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c[k] + step < p.C && s.start[c[k] + step] <= t0 + k * threads) c[k] += step;
+    int pos[4], page[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int t = t0 + k * threads, L = s.len[c[k]];
+      pos[k] = L + t - s.start[c[k]];
+      page[k] = 0;
+      if (t >= total) continue;
+      const int j = p.by_page(pos[k]), used = pages_of(p, L);
+      page[k] = j < used ? p.page_table[static_cast<size_t>(c[k]) * p.max_pages + j]
+                         : p.free_pages[free_count - 1 - (s.base[c[k]] + j - used)];
     }
-    if (p.slots) p.slots[t] = slot;
-    if (p.token_cache) p.token_cache[t] = cache;
-    if (p.positions) p.positions[t] = pos;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int t = t0 + k * threads;
+      if (t >= p.max_tokens) break;
+      const bool live = t < total;
+      if (p.slots) p.slots[t] = live ? page[k] * p.P + pos[k] - p.by_page(pos[k]) * p.P : -1;
+      if (p.token_cache) p.token_cache[t] = live ? c[k] : -1;
+      if (p.positions) p.positions[t] = live ? pos[k] : -1;
+    }
   }
 }
 
-// All of a small call in one cluster.  Every CTA makes the plan for itself; the lengths are written once all have read them.
+// All of a small call in one cluster.
 __global__ void __cluster_dims__(kExtendCluster, 1, 1) __launch_bounds__(kPlanThreads)
     extend_cluster_kernel(const __grid_constant__ ExtendParams p) {
-  __shared__ int64_t scratch[64];
+  __shared__ PlanShared shared;
   __shared__ ExtendPlan s;
   CachePlan w;
-  const bool ok = extend_plan(p, scratch, &w);
+  const bool ok = extend_plan(p, shared, &w);
   const int c = threadIdx.x;
   if (c < p.C) {
     s.start[c] = ok ? w.start : 0;
@@ -181,18 +219,19 @@ __global__ void __cluster_dims__(kExtendCluster, 1, 1) __launch_bounds__(kPlanTh
     s.base[c] = w.base;
   }
   if (c == 0) s.start[p.C] = ok ? w.total : 0;
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (blockIdx.x == 0) write_plan(p, w, ok);
+  __syncthreads();
   extend_fill(p, s, w.free_count, blockIdx.x * kPlanThreads + threadIdx.x, kExtendCluster * kPlanThreads);
 }
 
-// A large call: the plan in one CTA, its outputs to the fill kernel's CTAs.
-__global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const __grid_constant__ ExtendParams p) {
-  __shared__ int64_t scratch[64];
+// A large call: the plan in one cluster, its outputs to the fill kernel's CTAs.
+__global__ void __cluster_dims__(kExtendCluster, 1, 1) __launch_bounds__(kPlanThreads)
+    extend_plan_kernel(const __grid_constant__ ExtendParams p) {
+  __shared__ PlanShared shared;
   allow_dependent_launch();
   CachePlan w;
-  const bool ok = extend_plan(p, scratch, &w);
-  write_plan(p, w, ok);
+  const bool ok = extend_plan(p, shared, &w);
+  if (blockIdx.x == 0) write_plan(p, w, ok);
 }
 
 __global__ void __launch_bounds__(kFillThreads) extend_fill_kernel(const __grid_constant__ ExtendParams p) {
@@ -237,112 +276,129 @@ constexpr int kRowThreads = 256;
 constexpr int kRowLanes = kHeadDim / 8;  // threads to a token's K or V of one head: 8 dims each, half a block
 constexpr int kRowTokens = kRowThreads / kRowLanes;
 
-// A thread's place: token t, dims 8 j .. 8 j + 7 of the units [u0, u0 + kUnits) (unit: K or V of a head).
+// A thread's place: token t, dims 8 j .. 8 j + 7 of some heads.
 struct RowPlace {
-  int j, t, u0, slot;
-  uint32_t code;  // byte of its codes in a group's K codes
-  size_t group;   // byte of the slot's group for head 0
-  size_t head;    // from a head's group to the next one's
+  bool live;
+  uint32_t code, scale;  // bytes of its codes and scale in a group (K's)
+  size_t group, head;    // byte of the slot's group for head 0; from a head's group to the next one's
 };
 
-template <int kUnits>
-__device__ __forceinline__ RowPlace row_place(const RowParams& p) {
+__device__ __forceinline__ RowPlace row_place(const RowParams& p, int slot, int j) {
   RowPlace w;
-  w.j = threadIdx.x % kRowLanes;
-  w.t = blockIdx.x * kRowTokens + threadIdx.x / kRowLanes;
-  w.u0 = blockIdx.y * kUnits;
-  w.slot = w.t < p.T ? p.slots[w.t] : -1;
-  if (w.slot < 0 || w.slot >= p.num_slots) {
-    if (w.slot != -1) set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
-    w.slot = -1;
+  w.live = slot >= 0 && slot < p.num_slots;
+  if (!w.live) {
+    if (slot != -1) set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
+    slot = 0;
   }
-  const int page = p.by_page(max(w.slot, 0)), at = max(w.slot, 0) - page * p.P, groups = p.P / kKv4Tokens;
+  const int page = p.by_page(slot), at = slot - page * p.P, groups = p.P / kKv4Tokens, row = at % kKv4Tokens;
   w.head = static_cast<size_t>(groups) * kKv4Bytes;
   w.group = (static_cast<size_t>(page) * p.hkv * groups + at / kKv4Tokens) * kKv4Bytes;
-  w.code = (w.j >> 2) * kChunkStride + at % kKv4Tokens * kChunkBytes + (w.j & 3) * 4;
+  w.code = (j >> 2) * kChunkStride + row * kChunkBytes + (j & 3) * 4;
+  w.scale = kScales + row * (kHeadDim / kBlockDims) + (j >> 1);
   return w;
 }
-__device__ __forceinline__ uint32_t scale_at(const RowParams& p, const RowPlace& w) {
-  return kScales + w.slot % kKv4Tokens * (kHeadDim / kBlockDims) + (w.j >> 1);  // (pages are whole groups)
+
+__device__ __forceinline__ float rcp_approx(float x) {  // to an fp32 step
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
-// Quantises: two threads to a block of 16 dims.  y / s rounds to e2m1, and top / 6 to e4m3, as the exact quotients do:
-// the reciprocal is taken as a number of fp32 below it and the rest, so that the quotient's error is far below the gap
-// between a tie and any other quotient of a bf16 number by an e4m3 one, and a quotient that is a tie comes out as that.
-template <int kUnits>
+// Eight numbers of a block of 16 (the next lane, an odd one, has the others) to codes and the block's scale.
+//
+// y / s rounds to e2m1, and top / 6 to e4m3, as the exact quotients do.  Those are quotients of numbers of at most 8 bits,
+// so any of them is either a tie or at least 2^-9 of itself away from one; and each is computed as y r + y rest with
+// r + rest = 1 / s to some 2^-44, whose fp32 rounding gives a tie exactly.  r lies below 1 / s, so that the rest is above
+// zero: it keeps the sign of a zero, and infinity infinite.
+__device__ __forceinline__ uint32_t quantise(const uint4& x, float unit, uint32_t* scale) {
+  const uint32_t d[4] = {x.x, x.y, x.z, x.w};
+  uint32_t m = 0;  // largest magnitudes, as their bits: a NaN is above infinity
+#pragma unroll
+  for (int k = 0; k < 4; ++k) m = __vmaxu2(m, d[k] & 0x7fff7fffu);
+  m = max(m & 0xffffu, m >> 16);
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  const float top = __uint_as_float(m << 16) * unit;
+  const bool nan = m > 0x7f80u;
+  const uint32_t sc = f32_to_e4m3(fminf(fmaxf(fmaf(top, 0x1.555554p-3f, top * 0x1.555556p-27f), 0x1p-9f), 448.f));
+  const float s = __half2float(__ushort_as_half(static_cast<unsigned short>(e4m3x2_to_f16x2(sc) & 0xffffu)));
+  const float r = rcp_approx(s) * (1.f - 0x1p-22f), rest = fmaf(-r, s, 1.f) * r;
+  const float r1 = r * unit, r0 = rest * unit;
+  uint32_t codes[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float lo = bf16_lo(d[k]), hi = bf16_hi(d[k]);
+    codes[k] = f32x2_to_e2m1(fmaf(lo, r1, lo * r0), fmaf(hi, r1, hi * r0));
+  }
+  *scale = nan ? 0x7fu : sc;
+  return nan ? 0u : __byte_perm(__byte_perm(codes[0], codes[1], 0x0040), __byte_perm(codes[2], codes[3], 0x0040), 0x5410);
+}
+
+template <int kHeads>
 __global__ void __launch_bounds__(kRowThreads) store_kernel(const __grid_constant__ RowParams p) {
-  const int t = blockIdx.x * kRowTokens + threadIdx.x / kRowLanes, u0 = blockIdx.y * kUnits;
-  uint4 x[kUnits];  // (loaded beside the slot, not after it)
+  const int j = threadIdx.x % kRowLanes, t = blockIdx.x * kRowTokens + threadIdx.x / kRowLanes, h0 = blockIdx.y * kHeads;
+  const uint8_t* k = p.k + t * p.k_stride + (h0 * kHeadDim + j * 8) * 2;
+  const uint8_t* v = p.v + t * p.v_stride + (h0 * kHeadDim + j * 8) * 2;
+  uint4 xk[kHeads], xv[kHeads];  // (loaded beside the slot, not after it)
 #pragma unroll
-  for (int i = 0; i < kUnits; ++i) {
-    const int u = u0 + i, h = u >> 1;
-    x[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (t < p.T && u < 2 * p.hkv)
-      x[i] = *reinterpret_cast<const uint4*>(((u & 1) ? p.v + t * p.v_stride : p.k + t * p.k_stride) + (h * kHeadDim + threadIdx.x % kRowLanes * 8) * 2);
-  }
-  const RowPlace w = row_place<kUnits>(p);
-#pragma unroll
-  for (int i = 0; i < kUnits; ++i) {
-    const int u = u0 + i;
-    const uint32_t d[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-    uint32_t m = 0;  // largest magnitudes, as their bits: a NaN is above infinity
-#pragma unroll
-    for (int k = 0; k < 4; ++k) m = __vmaxu2(m, d[k] & 0x7fff7fffu);
-    m = max(m & 0xffffu, m >> 16);
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    const float unit = u & 1 ? p.v_unit : p.k_unit, top = __uint_as_float(m << 16) * unit;
-    const bool nan = m > 0x7f80u;
-    const float sixth = fmaf(top, 0x1.555554p-3f, top * 0x1.555556p-27f);
-    const uint32_t scale = nan ? 0x7fu : f32_to_e4m3(fminf(fmaxf(sixth, 0x1p-9f), 448.f));
-    const float s = __half2float(__ushort_as_half(static_cast<unsigned short>(e4m3x2_to_f16x2(scale) & 0xffffu)));
-    // (The rest is kept above zero: infinity times it has to be infinity, and -0 times it -0.)
-    const float r = __frcp_rd(s), rest = fmaxf(fmaf(-r, s, 1.f) * r, r * 0x1p-60f);
-    const float r1 = r * unit, r0 = rest * unit;
-    uint32_t codes = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float lo = bf16_lo(d[k]), hi = bf16_hi(d[k]);
-      codes |= f32x2_to_e2m1(fmaf(lo, r1, lo * r0), fmaf(hi, r1, hi * r0)) << (8 * k);
+  for (int i = 0; i < kHeads; ++i) {
+    xk[i] = xv[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (t < p.T && h0 + i < p.hkv) {
+      xk[i] = *reinterpret_cast<const uint4*>(k + i * 2 * kHeadDim);
+      xv[i] = *reinterpret_cast<const uint4*>(v + i * 2 * kHeadDim);
     }
-    if (w.slot < 0 || u >= 2 * p.hkv) continue;
-    uint8_t* g = p.cache + w.group + (u >> 1) * w.head;
-    *reinterpret_cast<uint32_t*>(g + (u & 1) * kVCodes + w.code) = nan ? 0u : codes;
-    if (!(w.j & 1)) g[(u & 1) * kScaleBytes + scale_at(p, w)] = static_cast<uint8_t>(scale);
+  }
+  const RowPlace w = row_place(p, t < p.T ? p.slots[t] : -1, j);
+  uint8_t* g = p.cache + w.group + h0 * w.head;
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i, g += w.head) {
+    uint32_t sk, sv;
+    const uint32_t ck = quantise(xk[i], p.k_unit, &sk), cv = quantise(xv[i], p.v_unit, &sv);
+    if (!w.live || h0 + i >= p.hkv) continue;
+    *reinterpret_cast<uint32_t*>(g + w.code) = ck;
+    *reinterpret_cast<uint32_t*>(g + kVCodes + w.code) = cv;
+    if (j & 1) g[kScaleBytes + w.scale] = static_cast<uint8_t>(sv);
+    else g[w.scale] = static_cast<uint8_t>(sk);
   }
 }
 
-// A thread decodes 8 dims of some K and V.
-template <int kUnits>
-__global__ void __launch_bounds__(kRowThreads) load_kernel(const __grid_constant__ RowParams p, uint8_t* k, uint8_t* v) {
-  const RowPlace w = row_place<kUnits>(p);
-  if (w.t >= p.T) return;
-  uint32_t codes[kUnits], s1[kUnits];
+// Eight codes and their scale to bf16 numbers.
+__device__ __forceinline__ uint4 dequantise(uint32_t codes, uint32_t scale, float unit) {
+  const uint32_t s2 = e4m3x2_to_f16x2(scale | (scale << 8));
+  uint32_t f[4], out[4];
+  e2m1x8_to_f16(codes, f);
 #pragma unroll
-  for (int i = 0; i < kUnits; ++i) {
-    const int u = w.u0 + i;
-    codes[i] = s1[i] = 0;
-    if (w.slot >= 0 && u < 2 * p.hkv) {
-      const uint8_t* g = p.cache + w.group + (u >> 1) * w.head;
-      codes[i] = *reinterpret_cast<const uint32_t*>(g + (u & 1) * kVCodes + w.code);
-      s1[i] = g[(u & 1) * kScaleBytes + scale_at(p, w)];
+  for (int n = 0; n < 4; ++n) {
+    const uint32_t x = mul_f16x2(f[n], s2);
+    const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&x));
+    out[n] = pack_bf16x2(y.x * unit, y.y * unit);
+  }
+  return make_uint4(out[0], out[1], out[2], out[3]);
+}
+
+template <int kHeads>
+__global__ void __launch_bounds__(kRowThreads) load_kernel(const __grid_constant__ RowParams p, uint8_t* ko, uint8_t* vo) {
+  const int j = threadIdx.x % kRowLanes, t = blockIdx.x * kRowTokens + threadIdx.x / kRowLanes, h0 = blockIdx.y * kHeads;
+  if (t >= p.T) return;
+  const RowPlace w = row_place(p, p.slots[t], j);
+  const uint8_t* g = p.cache + w.group + h0 * w.head;
+  uint32_t ck[kHeads], cv[kHeads], sk[kHeads], sv[kHeads];
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i, g += w.head) {
+    ck[i] = cv[i] = sk[i] = sv[i] = 0;
+    if (w.live && h0 + i < p.hkv) {
+      ck[i] = *reinterpret_cast<const uint32_t*>(g + w.code);
+      cv[i] = *reinterpret_cast<const uint32_t*>(g + kVCodes + w.code);
+      sk[i] = g[w.scale];
+      sv[i] = g[kScaleBytes + w.scale];
     }
   }
+  uint8_t* k = ko + t * p.k_stride + (h0 * kHeadDim + j * 8) * 2;
+  uint8_t* v = vo + t * p.v_stride + (h0 * kHeadDim + j * 8) * 2;
 #pragma unroll
-  for (int i = 0; i < kUnits; ++i) {
-    const int u = w.u0 + i;
-    if (u >= 2 * p.hkv) break;
-    const uint32_t s2 = e4m3x2_to_f16x2(s1[i] | (s1[i] << 8));
-    const float unit = u & 1 ? p.v_unit : p.k_unit;
-    uint32_t f[4], out[4];
-    e2m1x8_to_f16(codes[i], f);
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const uint32_t x = mul_f16x2(f[n], s2);
-      const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&x));
-      out[n] = pack_bf16x2(y.x * unit, y.y * unit);
-    }
-    uint8_t* dst = ((u & 1) ? v + w.t * p.v_stride : k + w.t * p.k_stride) + ((u >> 1) * kHeadDim + w.j * 8) * 2;
-    *reinterpret_cast<uint4*>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
+  for (int i = 0; i < kHeads; ++i) {
+    if (h0 + i >= p.hkv) break;
+    *reinterpret_cast<uint4*>(k + i * 2 * kHeadDim) = dequantise(ck[i], sk[i], p.k_unit);
+    *reinterpret_cast<uint4*>(v + i * 2 * kHeadDim) = dequantise(cv[i], sv[i], p.v_unit);
   }
 }
 
@@ -375,15 +431,12 @@ kvshot_status check_kv4(const kvshot_kv4_desc* d, bool store, RowParams* p) {
   return KVSHOT_OK;
 }
 
-// Units (K or V of a head) to a thread: several, whose loads are in flight together, once that leaves every SM enough
-// threads.
-constexpr int kManyUnits = 4;
-bool many_units(const RowParams& p, int sms) {
-  return static_cast<int64_t>(p.T) * kRowLanes * 2 * p.hkv / kManyUnits >= static_cast<int64_t>(sms) * 2048;
+// Heads to a thread: four, whose loads are in flight together, once that leaves every SM enough threads.
+constexpr int kManyHeads = 4;
+bool many_heads(const RowParams& p, int sms) {
+  return static_cast<int64_t>(p.T) * kRowLanes * p.hkv / kManyHeads >= static_cast<int64_t>(sms) * 2048;
 }
-dim3 row_grid(const RowParams& p, int units) {
-  return dim3((p.T + kRowTokens - 1) / kRowTokens, (2 * p.hkv + units - 1) / units);
-}
+dim3 row_grid(const RowParams& p, int heads) { return dim3((p.T + kRowTokens - 1) / kRowTokens, (p.hkv + heads - 1) / heads); }
 
 }  // namespace
 }  // namespace kvshot
@@ -415,18 +468,20 @@ extern "C" kvshot_status kvshot_cache_extend(const kvshot_extend_desc* d, const 
                         static_cast<const void*>(token_start), static_cast<const void*>(slots),
                         static_cast<const void*>(token_cache), static_cast<const void*>(positions)})
     if (!aligned(p, 4)) return KVSHOT_ERR_ALIGN;
+  int search = 0;
+  for (int s = 1; s < d->num_caches; s *= 2) search = s;
   ExtendParams p{seq_lens,       new_tokens,     page_table,    free_pages,  free_count,
                  seq_lens_out,   page_table_out, free_count_out, token_start, slots,
                  token_cache,    positions,      d->err_flag,   d->num_caches, d->page_size,
                  d->max_pages_per_seq, d->num_pages, d->num_free, d->max_tokens,
-                 Div::by(d->page_size), Div::by(d->max_pages_per_seq)};
+                 search, Div::by(d->page_size), Div::by(d->max_pages_per_seq)};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const int most = std::max(d->max_tokens, d->num_caches * d->max_pages_per_seq);
   if (most <= kClusterItems) {
     const cudaError_t e = launch_maybe_pdl(extend_cluster_kernel, dim3(kExtendCluster), dim3(kPlanThreads), 0, false, s, p);
     return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
   }
-  if (launch_maybe_pdl(extend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, false, s, p) != cudaSuccess)
+  if (launch_maybe_pdl(extend_plan_kernel, dim3(kExtendCluster), dim3(kPlanThreads), 0, false, s, p) != cudaSuccess)
     return KVSHOT_ERR_CUDA;
   const int grid = std::min((most + kFillThreads - 1) / kFillThreads, 1024);
   const cudaError_t e = launch_maybe_pdl(extend_fill_kernel, dim3(grid), dim3(kFillThreads), 0, true, s, p);
@@ -452,8 +507,8 @@ extern "C" kvshot_status kvshot_kv4_store(const kvshot_kv4_desc* d, const void* 
   p.cache = static_cast<uint8_t*>(cache);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e =
-      many_units(p, sm_count())
-          ? launch_maybe_pdl(store_kernel<kManyUnits>, row_grid(p, kManyUnits), dim3(kRowThreads), 0, false, s, p)
+      many_heads(p, sm_count())
+          ? launch_maybe_pdl(store_kernel<kManyHeads>, row_grid(p, kManyHeads), dim3(kRowThreads), 0, false, s, p)
           : launch_maybe_pdl(store_kernel<1>, row_grid(p, 1), dim3(kRowThreads), 0, false, s, p);
   return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
 }
@@ -471,8 +526,8 @@ extern "C" kvshot_status kvshot_kv4_load(const kvshot_kv4_desc* d, const void* c
   uint8_t *kb = static_cast<uint8_t*>(k), *vb = static_cast<uint8_t*>(v);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e =
-      many_units(p, sm_count())
-          ? launch_maybe_pdl(load_kernel<kManyUnits>, row_grid(p, kManyUnits), dim3(kRowThreads), 0, false, s, p, kb, vb)
+      many_heads(p, sm_count())
+          ? launch_maybe_pdl(load_kernel<kManyHeads>, row_grid(p, kManyHeads), dim3(kRowThreads), 0, false, s, p, kb, vb)
           : launch_maybe_pdl(load_kernel<1>, row_grid(p, 1), dim3(kRowThreads), 0, false, s, p, kb, vb);
   return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
 }
