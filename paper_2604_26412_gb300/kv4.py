@@ -1,0 +1,110 @@
+"""A 4-bit target cache with its page tables: the state that a drafting server keeps between verification steps.
+
+Between two drafting steps the target has verified some tokens of each sequence.  grow() finds room for them
+(kvshot_cache_extend) and quantises their K and V into it (kvshot_kv4_store); DraftStep(target_kv4=...) then drafts over
+the cache (kvshot_draft_attn_kv4), and values() reads tokens back (kvshot_kv4_load).  Lengths, tables and the list of
+free pages live on the device and are changed there in stream order: a step needs no word from the host, and grow() can
+be captured in a graph together with the step (its sizes are those of the buffers it is given).
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from . import kvshot
+
+
+class Kv4Cache:
+    def __init__(self, num_caches: int, hkv: int, num_pages: int, max_pages_per_seq: int, *, page_size: int = 16,
+                 max_tokens: int, k_scale_exp: int = 0, v_scale_exp: int = 0, device="cuda"):
+        """max_tokens: the most tokens that one grow() adds, over all caches."""
+        size = kvshot.kv4_cache_bytes(num_pages, hkv, page_size)
+        if size == 0:
+            raise kvshot.KvshotError(kvshot.KVSHOT_ERR_SHAPE, "kvshot_kv4_cache_bytes")
+        self.num_caches, self.hkv, self.page_size, self.num_pages = num_caches, hkv, page_size, num_pages
+        self.k_scale_exp, self.v_scale_exp, self.max_tokens = k_scale_exp, v_scale_exp, max_tokens
+
+        def i32(*shape):
+            return torch.zeros(shape, dtype=torch.int32, device=device)
+
+        self.data = torch.empty(size, dtype=torch.uint8, device=device)
+        self.seq_lens, self.page_table = i32(num_caches), i32(num_caches, max_pages_per_seq)
+        self.free_pages = torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device)  # taken from its end
+        self.free_count = torch.full((1,), num_pages, dtype=torch.int32, device=device)
+        self.err = i32(1)
+        # Of the last grow(): first packed token of each cache; slot, cache and position of each packed token (or -1).
+        self.token_start = i32(num_caches + 1)
+        self.slots, self.token_cache, self.positions = i32(max_tokens), i32(max_tokens), i32(max_tokens)
+        self._extend = kvshot.make_extend_desc(num_caches=num_caches, page_size=page_size,
+                                               max_pages_per_seq=max_pages_per_seq, num_pages=num_pages,
+                                               max_tokens=max_tokens, err_flag=self.err)
+
+    @property
+    def max_seq_len(self) -> int:
+        return self.page_table.shape[1] * self.page_size
+
+    def _rows(self, num_tokens: int, k_stride: int = 0, v_stride: int = 0) -> kvshot.Kv4Desc:
+        return kvshot.make_kv4_desc(num_tokens=num_tokens, hkv=self.hkv, page_size=self.page_size,
+                                    num_pages=self.num_pages, k_scale_exp=self.k_scale_exp,
+                                    v_scale_exp=self.v_scale_exp, k_stride=k_stride, v_stride=v_stride,
+                                    err_flag=self.err)
+
+    def extend(self, new_tokens: torch.Tensor, stream=None) -> None:
+        """Pages and slots for new_tokens[c] (int32 [num_caches]) more tokens of each cache; self.slots are theirs."""
+        kvshot.cache_extend(self._extend, self.seq_lens, new_tokens, self.page_table, self.free_pages, self.free_count,
+                            self.seq_lens, self.page_table, self.free_count, self.token_start, self.slots,
+                            self.token_cache, self.positions, stream)
+
+    def store(self, k: torch.Tensor, v: torch.Tensor, slots: Optional[torch.Tensor] = None, stream=None) -> None:
+        """K and V [T, hkv, 128] (bf16; rows may be slices of wider ones) into slots [T] (default: the first T of
+        self.slots)."""
+        t = k.shape[0]
+        slots = self.slots if slots is None else slots
+        if k.shape != v.shape or k.shape[1:] != (self.hkv, 128) or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
+            raise ValueError(f"k and v must be bf16 [T, {self.hkv}, 128]")
+        if t > slots.shape[0]:
+            raise ValueError(f"{t} tokens for {slots.shape[0]} slots")
+        if t == 0:
+            return
+        for x in (k, v):
+            if x.stride()[1:] != (128, 1):
+                raise ValueError("a token's heads must be contiguous")
+        stride = (k.stride(0), v.stride(0)) if t > 1 else (0, 0)
+        kvshot.kv4_store(self._rows(t, *stride), k, v, slots, self.data, stream)
+
+    def grow(self, new_tokens: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+        """extend(), then store(): K and V packed cache after cache.  Rows past the new tokens are not stored."""
+        stream = kvshot._stream(stream)
+        self.extend(new_tokens, stream)
+        self.store(k, v, stream=stream)
+
+    def values(self, slots: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """K and V [T, hkv, 128] (bf16) of slots [T]; -1 gives zeros."""
+        shape = (slots.shape[0], self.hkv, 128)
+        k, v = (torch.empty(shape, dtype=torch.bfloat16, device=self.data.device) for _ in range(2))
+        if slots.shape[0]:
+            kvshot.kv4_load(self._rows(slots.shape[0]), self.data, slots, k, v, stream)
+        return k, v
+
+    def error_code(self) -> int:
+        return int(self.err.item())
+
+
+def of_inputs(inp, page_size: int = 16, spare_pages: int = 0, spare_tokens: int = 0, k_exp: int = 0,
+              v_exp: int = 0) -> Kv4Cache:
+    """A 4-bit cache that holds the target prefixes of inp (workloads.Inputs), stored through the library, with spare_pages
+    more pages in the pool and room for spare_tokens more tokens of each cache."""
+    s, lens = inp.spec, inp.seq_lens
+    pages = [-(-n // page_size) for n in s.seq_lens]
+    row = max(1, -(-(s.max_seq_len + spare_tokens) // page_size))
+    cache = Kv4Cache(s.num_caches, s.hkv, max(1, sum(pages) + spare_pages), row, page_size=page_size,
+                     max_tokens=max(1, sum(s.seq_lens), spare_tokens * s.num_caches), k_scale_exp=k_exp,
+                     v_scale_exp=v_exp, device=inp.target_k.device)
+    cache.extend(lens)
+    n = sum(s.seq_lens)
+    c, pos = cache.token_cache[:n].long(), cache.positions[:n].long()
+    size = s.page_size if inp.page_table is not None else inp.l_cap
+    page = inp.page_table[c, pos // size].long() if inp.page_table is not None else c
+    cache.store(inp.target_k[page, :, pos % size], inp.target_v[page, :, pos % size])
+    return cache

@@ -4,7 +4,8 @@ A step drafts every level of the draft chain/tree once: for each drafting
 step d (Nq_d new nodes), the new nodes' q/k/v are RoPE'd and appended
 (kvshot_draft_append), then the new nodes attend over [target prefix | draft
 KV so far] (kvshot_draft_attn).  In "whole" mode all N nodes are appended
-once and attend together (whole-tree verification shape).
+once and attend together (whole-tree verification shape).  The target prefix is
+bf16, fp8 or 4 bits; the 4-bit cache grows between steps (kv4.Kv4Cache).
 
 Only device memory is handled here (torch allocations); all arithmetic runs
 in libkvshot's kernels.
@@ -17,19 +18,28 @@ import torch
 
 from . import kvshot
 from . import workloads as wl
+from .kv4 import Kv4Cache
 
 
 class DraftStep:
     def __init__(self, inp: wl.Inputs, mode: str = "per_depth", flags: int = 0, num_ctas: int = 0,
-                 scale: float = 0.0, err_flag: bool = True, target_fp8=None, qk_norm=None):
+                 scale: float = 0.0, err_flag: bool = True, target_fp8=None, qk_norm=None,
+                 target_kv4: Optional[Kv4Cache] = None, window: int = 0, sinks: int = 0):
         """target_fp8: optional (codes_k, codes_v, k_scale_exp, v_scale_exp), an e4m3 copy of the target
         cache (workloads.fp8_target) to attend instead of inp.target_k / inp.target_v.
         qk_norm: optional (q_norm_w, k_norm_w, eps): the append normalises q and k per head first
-        (kvshot_draft_append_qknorm)."""
+        (kvshot_draft_append_qknorm).
+        target_kv4: optional 4-bit cache to attend, with its own lengths and tables, instead of inp's target cache;
+        then also window and sinks (kvshot_draft_attn_kv4)."""
         if mode not in ("per_depth", "whole"):
             raise ValueError(mode)
+        if target_kv4 is None and (window or sinks):
+            raise ValueError("a window needs the 4-bit target cache")
+        if target_kv4 is not None and target_fp8 is not None:
+            raise ValueError("one target cache")
         self.inp, self.mode = inp, mode
         self.qk_norm = qk_norm
+        self.kv4, self.window, self.sinks = target_kv4, window, sinks
         s = inp.spec
         k_exp = v_exp = 0
         if target_fp8 is not None:
@@ -37,6 +47,10 @@ class DraftStep:
             flags |= kvshot.KVSHOT_TARGET_FP8
         else:
             self.target_k, self.target_v = inp.target_k, inp.target_v
+        if target_kv4 is not None:
+            if (target_kv4.num_caches, target_kv4.hkv) != (s.num_caches, s.hkv):
+                raise ValueError("the 4-bit cache is of other caches or heads")
+            k_exp, v_exp = target_kv4.k_scale_exp, target_kv4.v_scale_exp
         dev = inp.target_k.device
         self.device = dev
         C, N = s.num_caches, s.n_nodes
@@ -56,6 +70,12 @@ class DraftStep:
         self.out: List[torch.Tensor] = [torch.empty_like(q) for q in self.q_in]
         self.lse: List[torch.Tensor] = [torch.empty(q.shape[:3], dtype=torch.float32, device=dev) for q in self.q_in]
         paged = inp.page_table is not None
+        cache = dict(max_seq_len=s.max_seq_len, page_size=s.page_size if paged else 0,
+                     max_pages_per_seq=inp.page_table.shape[1] if paged else 0,
+                     num_pages=inp.num_pages if paged else 0, l_cap=inp.l_cap)
+        if target_kv4 is not None:
+            cache = dict(max_seq_len=target_kv4.max_seq_len, page_size=target_kv4.page_size,
+                         max_pages_per_seq=target_kv4.page_table.shape[1], num_pages=target_kv4.num_pages)
         self.descs = []
         self.parents: List[torch.Tensor] = []  # [B, n_nodes] of each call (tree_parent's row stride is n_nodes)
         n0 = 0
@@ -64,14 +84,15 @@ class DraftStep:
             self.parents.append(inp.tree_parent[:, :n0].contiguous())
             self.descs.append(kvshot.make_desc(
                 num_caches=C, num_seqs=s.num_seqs, hq=s.hq, hkv=s.hkv, n_nodes=n0, n_query=n_step,
-                n_max=inp.n_max, max_seq_len=s.max_seq_len, head_dim=s.head_dim,
-                page_size=s.page_size if paged else 0,
-                max_pages_per_seq=inp.page_table.shape[1] if paged else 0,
-                num_pages=inp.num_pages if paged else 0, l_cap=inp.l_cap, scale=scale, tree=s.tree,
+                n_max=inp.n_max, head_dim=s.head_dim, scale=scale, tree=s.tree, **cache,
                 # the attention call follows this step's own append kernel, which writes only q and the draft K/V
                 flags=flags | kvshot.KVSHOT_OVERLAP_PREVIOUS, num_ctas=num_ctas, err_flag=self.err,
                 k_scale_exp=k_exp, v_scale_exp=v_exp))
-        ws = max(kvshot.workspace_size(d) for d in self.descs)
+        if target_kv4 is not None:
+            ws = [kvshot.draft_attn_kv4_workspace_size(d, window, sinks) for d in self.descs]
+        else:
+            ws = [kvshot.workspace_size(d) for d in self.descs]
+        ws = max(ws) if min(ws) > 0 else 0
         if ws == 0:
             raise kvshot.KvshotError(kvshot.KVSHOT_ERR_SHAPE, "kvshot_draft_attn_workspace_size")
         self.workspace = torch.empty(ws, dtype=torch.uint8, device=dev)
@@ -98,8 +119,13 @@ class DraftStep:
             else:
                 kvshot.draft_append(d, self.q_in[i], self.k_in[i], self.v_in[i], self.pos[i], n0, n_step,
                                     inp.spec.rope_base, self.draft_k, self.draft_v, self.q_rot[i], stream)
-            kvshot.draft_attn(d, self.q_rot[i], self.target_k, self.target_v, inp.page_table, inp.seq_lens,
-                              self.draft_k, self.draft_v, self.parents[i], self.out[i], self.lse[i], stream)
+            if self.kv4 is not None:
+                kvshot.draft_attn_kv4(d, self.q_rot[i], self.kv4.data, self.kv4.page_table, self.kv4.seq_lens,
+                                      self.draft_k, self.draft_v, self.parents[i], self.window, self.sinks,
+                                      self.out[i], self.lse[i], stream)
+            else:
+                kvshot.draft_attn(d, self.q_rot[i], self.target_k, self.target_v, inp.page_table, inp.seq_lens,
+                                  self.draft_k, self.draft_v, self.parents[i], self.out[i], self.lse[i], stream)
             n0 += n_step
 
     def error_code(self) -> int:
