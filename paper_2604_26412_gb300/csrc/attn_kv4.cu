@@ -63,6 +63,7 @@ struct Smem : Ring {
   uint32_t qkdone, pfull, pvdone;    // [2] QK^T done; P written (and S read); P.V done
   uint32_t qfull, qempty;            // [2] q of a piece staged; its last QK^T done
   uint32_t ofree, mmadone;           // epilogue has read O; [2] every MMA issued is done
+  uint32_t rfull;                    // [kRowSets] a piece's rows built
   uint32_t joined;                   // barrier of the softmax warps
   float *ref, *alpha, *inv;          // [2][64] per warpgroup and row (ref: negated)
   int* wmax;                         // [8][64] per warp and row; sums at a piece's end
@@ -70,7 +71,7 @@ struct Smem : Ring {
   uint32_t* tmem;
 };
 
-constexpr int kBarriers = 18;  // besides the ring's (an even number: what follows is aligned to 16 bytes)
+constexpr int kBarriers = 18 + kRowSets;  // besides the ring's (an even number: what follows is aligned to 16 bytes)
 
 template <class CF>
 __host__ __device__ constexpr size_t smem_bytes(int C) {
@@ -102,6 +103,7 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.mmadone = s.qempty + 16;
   s.ofree = s.mmadone + 16;
   s.joined = s.ofree + 8;
+  s.rfull = s.joined + 8;
   s.rows = reinterpret_cast<Rows*>(b + 8 * (2 * CF::kStages + kBarriers));
   s.ref = reinterpret_cast<float*>(s.rows + kRowSets);
   s.alpha = s.ref + 128;
@@ -138,7 +140,6 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
     if (!(w.flags & kFirst)) continue;
     const int b = piece & 1;
     if (!__all_sync(0xffffffffu, wait(sm.qempty + 8 * b, ((piece >> 1) & 1) ^ 1u))) return;
-    ++piece;
     const __nv_bfloat16* q = p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim;
     const int row0 = w.rb * p.rows_per_unit, rows = min(p.rows_per_unit, p.rows_total - row0);
     // 16 bytes of two rows at a time per warp; eight loads of a lane on their way together.
@@ -161,6 +162,9 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
                make_uint4(bf16x2_to_f16x2(x[i].x), bf16x2_to_f16x2(x[i].y), bf16x2_to_f16x2(x[i].z), bf16x2_to_f16x2(x[i].w)));
       }
     }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(sm.qfull + 8 * b);
     if (w.flags & kNewRows) {
       // (A set of another row block has the tree of the one before it copied along.)
       const int before = set & (kRowSets - 1);
@@ -172,9 +176,9 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
       }
       build_rows(kp, sm.rows[set], CF::kNC, w.rb, w.seq, w.flags & kNewTree);
     }
-    fence_proxy_async_smem();
     __syncwarp();
-    if (lane == 0) mbar_arrive(sm.qfull + 8 * b);
+    if (lane == 0) mbar_arrive(sm.rfull + 8 * (piece & (kRowSets - 1)));
+    ++piece;
   }
 }
 
@@ -430,7 +434,7 @@ __device__ __forceinline__ int column_sums(float (&v)[N], int lane, int* column0
 // The references of rows whose scores have passed their limit move: refs (negated), and alpha with what O and the sums are to be
 // multiplied by.  The threads of warpgroup wg; n rows from the first of `scores`, `ref` and `alpha` on.
 __device__ __noinline__ void move_references(int* wmax, float* refs, float* alpha, int wg, int n, uint32_t scores, float qs,
-                                             uint64_t vis) {
+                                             uint64_t vis, bool fresh) {
   const int tid = threadIdx.x & 127, warp = tid >> 5;
 #pragma unroll 1
   for (int j = 0; j < n; j += 8) {
@@ -447,7 +451,7 @@ __device__ __noinline__ void move_references(int* wmax, float* refs, float* alph
   named_barrier_sync(kBarGroup + wg, kGroupThreads);
   if (tid < n) {
     const float m = unordered(max(max(wmax[tid], wmax[64 + tid]), max(wmax[128 + tid], wmax[192 + tid])));
-    const float old = -refs[tid], ref = m - old > kRefLimit ? m - kRefBelow : old;
+    const float old = fresh ? kNoRef : -refs[tid], ref = m - old > kRefLimit ? m - kRefBelow : old;
     refs[tid] = -ref;
     alpha[tid] = ex2(old - ref);
   }
@@ -474,28 +478,30 @@ template <int kAccs>
 __device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, const int* place, const TileMeta& w, int j0, int j1,
                                         uint32_t o_cols, int next) {
   const int tid = threadIdx.x & 127;
-  const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
   const size_t row0 = static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G;
   const size_t part = static_cast<size_t>((w.c * p.hkv + w.h) * p.row_blocks + w.rb + blockIdx.x) * p.rows_per_unit;
   const bool whole = w.flags & kWhole;
+  const int end = whole ? min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit) : j1;  // (a part has room for all rows)
+  __nv_bfloat16* out = p.out + row0 * kHeadDim + tid;
+  float* ws = p.ws_o + (part + j0) * kHeadDim + tid;
+  const uint32_t inv = smem_addr(sm.inv), places = smem_addr(place);
 #pragma unroll 1
   for (int j = j0; j < j1; j += 4) {
     uint32_t o[4], o2[4];
     tmem_ld4(o_cols + j, o);
     if (kAccs == 2) tmem_ld4(o_cols + next + j, o2);
+    const uint4 a = lds128(inv + 4 * j), at = lds128(places + 4 * j);
+    const uint4 a2 = kAccs == 2 ? lds128(inv + 4 * (64 + j)) : a;
+    const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {a2.x, a2.y, a2.z, a2.w}, to[4] = {at.x, at.y, at.z, at.w};
     tmem_wait_ld();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (j + i >= rows) break;
-      const float a = sm.inv[j + i];
-      float v = a != 0.f ? __uint_as_float(o[i]) * a : 0.f;
-      if (kAccs == 2) {
-        const float a2 = sm.inv[64 + j + i];
-        v += a2 != 0.f ? __uint_as_float(o2[i]) * a2 : 0.f;
-      }
-      if (whole) p.out[(row0 + place[j + i]) * kHeadDim + tid] = __float2bfloat16(v);
-      else p.ws_o[(part + j + i) * kHeadDim + tid] = v;
+      float v = wa[i] != 0u ? __uint_as_float(o[i]) * __uint_as_float(wa[i]) : 0.f;
+      if (kAccs == 2) v += wb[i] != 0u ? __uint_as_float(o2[i]) * __uint_as_float(wb[i]) : 0.f;
+      if (!whole) ws[i * kHeadDim] = v;
+      else if (j + i < end) out[static_cast<size_t>(to[i]) * kHeadDim] = __float2bfloat16(v);
     }
+    ws += 4 * kHeadDim;
   }
 }
 
@@ -515,14 +521,14 @@ __device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, cons
     top = fmaxf(r0, r1);
     const float w0 = had0 ? ex2(r0 - top) : 0.f, w1 = had1 ? ex2(r1 - top) : 0.f;
     sum = (had0 ? w0 * total(0, j) : 0.f) + (had1 ? w1 * total(1, j) : 0.f);
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
     sm.inv[j] = w0 * inv * (sm.codes[0] ? p.v_scale : 1.f);
     sm.inv[64 + j] = w1 * inv * (sm.codes[1] ? p.v_scale : 1.f);
   } else {
     const int wg = j >= CF::kCols;
     top = -sm.ref[j];
     sum = total(wg, j - wg * CF::kCols);
-    sm.inv[j] = sum == 0.f ? 0.f : (sm.codes[0] ? p.v_scale : 1.f) / sum;
+    sm.inv[j] = sum == 0.f ? 0.f : __fdividef(sm.codes[0] ? p.v_scale : 1.f, sum);
   }
   if (j >= rows) return;
   const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
@@ -551,19 +557,18 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
   bool fresh = true;              // this warpgroup has had no tile of the piece
   int t_first = 0;                // the piece's first tile
   bool good = true;               // no wait of this warp has given up
-  int rb = 0, set = -1;           // the piece's row block, and its set of rows
+  int rb = 0, set = -1, piece = -1;  // the piece's row block, its set of rows and number
   auto begin = [&](int t) {
     const TileMeta w = tile_meta(sm, t);
-    if (!sync(wait)) return false;  // the piece before has been written out
     rb = w.rb;
-    if (w.flags & kNewRows) set = (set + 1) & (kRowSets - 1);  // (built before q was staged, so before S)
-    if (key < NC) ref[key] = -kNoRef;
+    ++piece;
+    if (w.flags & kNewRows) set = (set + 1) & (kRowSets - 1);
 #pragma unroll
     for (int j = 0; j < NC / 2; ++j) l[j] = make_float2(0.f, 0.f);
     in_codes = fresh = true;
     t_first = t;
-    return sync(wait);
   };
+  auto rows_built = [&]() { return wait(sm.rfull + 8 * (piece & (kRowSets - 1)), (piece / kRowSets) & 1); };
   // A piece's end, at its last tile t: join the warpgroups and write the rows.
   auto end = [&](int t) {
     int col = 0;
@@ -580,7 +585,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     if (key == 0) sm.codes[wg] = in_codes;
     // O is at rest: P.V of this warpgroup's last tile of the piece is done.
     const int mine = CF::kByTile && (t & 1) != wg ? t - 1 : t;
-    const bool ok = fresh || wait(sm.pvdone + 8 * (mine & 1), (mine >> 1) & 1);
+    const bool ok = (fresh || wait(sm.pvdone + 8 * (mine & 1), (mine >> 1) & 1)) && rows_built();
     if (!__all_sync(0xffffffffu, ok) || !sync(wait)) return false;
     const bool two = t > t_first;
     if (threadIdx.x < CF::kNC) join_sums<CF>(p, smem, sm.rows[set].place, tile_meta(sm, t), threadIdx.x, two || !(t & 1), two || (t & 1));
@@ -603,14 +608,15 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     if (!is_of(flags, t)) flags = tile_flags(sm, t);
     if (CF::kByTile && good && t > 0) {  // the tile before is the other warpgroup's
       if (!is_of(before, t - 1)) before = tile_flags(sm, t - 1);
-      if (before & kFirst) good = begin(t - 1);
+      if (before & kFirst) begin(t - 1);
       if (good && (before & kLast)) good = end(t - 1);
     }
     const bool stop = good && (flags & kStop);
-    if (good && (flags & kFirst) && !stop) good = begin(t);
+    if (good && (flags & kFirst) && !stop) begin(t);
     const bool draft = flags & kDraft;
     const float qs = draft ? p.qscale : p.qscale * p.k_scale;
     uint64_t vis = ~0ull;
+    if (good && !stop && (flags & kMasked)) good = __all_sync(0xffffffffu, rows_built());
     if (good && !stop && (flags & kMasked)) vis = rows_seeing(kp, sm.rows[set], tile_words(sm, t), rb, key) >> col0;
     // The buffer of P is free when P.V of the tile before the last is done (by tile: O is at rest then, too).
     good = good && (stop || __all_sync(0xffffffffu, wait(sm.pvdone + 8 * b, phase ^ 1u)));
@@ -640,9 +646,9 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
       float top = kRefLimit;
 #pragma unroll
       for (int j = 0; j < NC / 2; ++j) top = max3(top, x[j].x, x[j].y);
-      if (!any_of(bar, kGroupThreads, top > kRefLimit || leave_codes || !good || stop)) break;
+      if (!any_of(bar, kGroupThreads, top > kRefLimit || leave_codes || fresh || !good || stop)) break;
       if (any_of(bar, kGroupThreads, !good) || stop) return;
-      move_references(wmax, ref, alpha, wg, NC, scores, qs, vis);  // always with a warpgroup's first keys of a piece
+      move_references(wmax, ref, alpha, wg, NC, scores, qs, vis, fresh);  // always with a warpgroup's first keys of a piece
 #pragma unroll
       for (int j = 0; j < NC / 2; ++j) {
         l[j].x *= alpha[2 * j];
@@ -684,25 +690,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   const Smem sm = carve<CF>(smem_raw, p.C);
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
-#pragma unroll 1
-    for (int s = 0; s < CF::kStages; ++s) {
-      mbar_init(sm.cfull + 8 * s, 1);
-      mbar_init(sm.cempty + 8 * s, 5);  // a decoding warpgroup's warps, and the one that stages q
-    }
-    for (int b = 0; b < 2; ++b) {
-      mbar_init(sm.kfull + 8 * b, 4);
-      mbar_init(sm.vfull + 8 * b, 4);
-      mbar_init(sm.qkdone + 8 * b, 1);
-      mbar_init(sm.pfull + 8 * b, CF::kByTile ? 4 : 8);
-      mbar_init(sm.pvdone + 8 * b, 1);
-      mbar_init(sm.qfull + 8 * b, 1);
-      mbar_init(sm.qempty + 8 * b, 1);
-      mbar_init(sm.mmadone + 8 * b, 1);
-    }
-    mbar_init(sm.ofree, 8);
-    mbar_init(sm.joined, 8);
     init_waits(p);
     *sm.issued = 0;
+  }
+  static_assert(2 * CF::kStages + kBarriers <= 32, "a lane for each barrier");
+  if (threadIdx.x < 2 * CF::kStages + kBarriers) {
+    // Arrivals, in the order of carve(): the ring (of a stage, a decoding warpgroup's warps and the one that stages q), K and
+    // V decoded, then the rest.
+    const int j = threadIdx.x - 2 * CF::kStages;
+    mbar_init(sm.cfull + 8 * threadIdx.x, j < -CF::kStages ? 1 : j < 0 ? 5 : j < 4 ? 4 : (j >> 1) == 3 ? (CF::kByTile ? 4 : 8)
+                                          : (j >> 1) == 8                                             ? 8
+                                                                                                      : 1);
     fence_mbar_init();
   }
   if (warp == kWarpQ && (threadIdx.x & 31) < kMetas)  // (what an earlier CTA left there is of no tile)

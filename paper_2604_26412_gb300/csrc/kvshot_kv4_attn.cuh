@@ -64,11 +64,11 @@ struct Ring {
   int *len, *base;  // the loader's plan
 };
 // The query rows of a unit: their places in a cache's q and out, and, of a draft tree, who sees what, as bits of rows.
-struct Rows {
+struct alignas(16) Rows {
+  int place[64];                      // (read four at a time)
   uint64_t line[kMaxTreeNodes];       // rows whose node is this one or descends from it
   uint64_t upto[kMaxTreeNodes + 1];   // rows whose depth is at most x (with a window)
   uint64_t anc[kMaxTreeNodes];        // nodes: itself and its ancestors
-  int place[64];
   int parent[kMaxTreeNodes];
 };
 
