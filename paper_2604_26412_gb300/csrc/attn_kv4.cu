@@ -38,6 +38,7 @@ constexpr int kPTile = kTile * 128;                // P^T: a row of up to 64 que
 constexpr int kThreads = 20 * 32;
 constexpr int kGroupThreads = 128;                 // a warpgroup
 constexpr int kWarpDecode = 8, kWarpLoad = 16, kWarpQk = 17, kWarpPv = 18, kWarpQ = 19;
+constexpr int kBarTmem = 3;                        // named barrier: all but the loading warp and q's
 constexpr int kBarGroup = 1;                       // named barriers 1 and 2: the threads of a softmax warpgroup
 // NC: query rows of a unit, a multiple of 8.
 template <int NC>
@@ -76,7 +77,7 @@ constexpr int kBarriers = 18 + kRowSets;  // besides the ring's (an even number:
 template <class CF>
 __host__ __device__ constexpr size_t smem_bytes(int C) {
   return 1024 + 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize +
-         sizeof(TileMeta) * kMetas + sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + kRowSets * sizeof(Rows) +
+         sizeof(TileMeta) * (kMetas + 1) + sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + kRowSets * sizeof(Rows) +
          sizeof(int) * (6 * 64 + 8 * 64 + 6) + sizeof(int) * (2 * C + 1);
 }
 
@@ -90,7 +91,8 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.ring = s.q + 2 * CF::kQTile;
   b += 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize;
   s.meta = smem_addr(b);
-  b += sizeof(TileMeta) * kMetas;
+  s.first = s.meta + kMetas * sizeof(TileMeta);
+  b += sizeof(TileMeta) * (kMetas + 1);
   s.cfull = smem_addr(b);
   s.cempty = s.cfull + 8 * CF::kStages;
   s.kfull = s.cempty + 8 * CF::kStages;
@@ -128,16 +130,20 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
   int stage = 0, piece = 0, set = -1;
   uint32_t phase = 0;
 #pragma unroll 1
-  for (int t = 0;; ++t) {
-    if (!__all_sync(0xffffffffu, wait(sm.cfull + 8 * stage, phase))) return;
-    const TileMeta w = tile_meta(sm, t);
-    if (lane == 0) mbar_arrive(sm.cempty + 8 * stage);
-    if (++stage == CF::kStages) {
-      stage = 0;
-      phase ^= 1u;
+  for (int t = -1;; ++t) {
+    // The first piece's (t = -1) before its first tile has landed, the others' with theirs.
+    TileMeta w = tile_meta_at(sm.first);
+    if (t >= 0) {
+      if (!__all_sync(0xffffffffu, wait(sm.cfull + 8 * stage, phase))) return;
+      w = tile_meta(sm, t);
+      if (lane == 0) mbar_arrive(sm.cempty + 8 * stage);
+      if (++stage == CF::kStages) {
+        stage = 0;
+        phase ^= 1u;
+      }
+      if (w.flags & kStop) return;
     }
-    if (w.flags & kStop) return;
-    if (!(w.flags & kFirst)) continue;
+    if (!(w.flags & kFirst) || t == 0) continue;
     const int b = piece & 1;
     if (!__all_sync(0xffffffffu, wait(sm.qempty + 8 * b, ((piece >> 1) & 1) ^ 1u))) return;
     const __nv_bfloat16* q = p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim;
@@ -236,12 +242,12 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
 #pragma unroll 1
   for (int t = wg;; t += 2) {
     // The tile's bytes; K's buffer: QK^T of its previous tile is done.
-    int flags = tile_flags(sm, t);
+    uint32_t flags = tile_flags(sm, t);
     bool ok = wait(sm.cfull + 8 * stage, phase);
     ok = ok && wait(qkdone, freed);
     if (!__all_sync(0xffffffffu, ok)) return;
     tc_fence_after();
-    if (!is_of(flags, t)) flags = tile_flags(sm, t);
+    if (!is_of(flags)) flags = tile_flags(sm, t);
     if (flags & kStop) {
       // (P.V of the tile before has to have seen its V, whose phase this one ends.)
       if (!__all_sync(0xffffffffu, wait(pvdone, freed))) return;
@@ -325,7 +331,7 @@ __device__ __forceinline__ void run_qk(const Smem& smem, const Waiter& wait, uin
     bool ok = wait(sm.pfull + 8 * b, phase ^ 1u);  // S of the tile before the last has been read
     ok = ok && wait(sm.kfull + 8 * b, phase);
     if (!__all_sync(0xffffffffu, ok)) break;
-    if (!is_of(flags, t)) flags = uniform(tile_flags(sm, t));
+    if (!is_of(flags)) flags = uniform(tile_flags(sm, t));
     if (flags & kFirst) {
       ++piece;
       if (!__all_sync(0xffffffffu, wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1))) break;
@@ -363,7 +369,7 @@ __device__ __forceinline__ void run_pv(const Smem& smem, const Waiter& wait, uin
     const uint32_t b = t & 1, phase = (t >> 1) & 1;
     uint32_t flags = uniform(tile_flags(sm, t));
     if (!__all_sync(0xffffffffu, wait(sm.vfull + 8 * b, phase))) break;
-    if (!is_of(flags, t)) flags = uniform(tile_flags(sm, t));
+    if (!is_of(flags)) flags = uniform(tile_flags(sm, t));
     if (flags & kStop) break;
     bool ok = wait(sm.pfull + 8 * b, phase);
     if (flags & kFirst) {
@@ -557,6 +563,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
   bool fresh = true;              // this warpgroup has had no tile of the piece
   int t_first = 0;                // the piece's first tile
   bool good = true;               // no wait of this warp has given up
+  const float qs_prefix = p.qscale * p.k_scale;
   int rb = 0, set = -1, piece = -1;  // the piece's row block, its set of rows and number
   auto begin = [&](int t) {
     const TileMeta w = tile_meta(sm, t);
@@ -601,29 +608,37 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
   for (int t = CF::kByTile ? wg : 0;; t += CF::kAccs) {
     const int b = CF::kByTile ? wg : t & 1;
     const uint32_t phase = (t >> 1) & 1;
-    // S, and with it the words of the tile and of those before it.  (A warp whose wait gives up goes on to the vote: the
-    // warps of a warpgroup leave there, together.)
-    int flags = tile_flags(sm, t), before = CF::kByTile && t > 0 ? tile_flags(sm, t - 1) : 0;
-    good = good && __all_sync(0xffffffffu, wait(sm.qkdone + 8 * b, phase));
-    if (!is_of(flags, t)) flags = tile_flags(sm, t);
+    // S, and with it the words of the tile and of those before it; and the buffer of P, free when P.V of the tile before
+    // the last is done (by tile: O is at rest then, too).  (A warp whose wait gives up goes on to the vote: the warps of a
+    // warpgroup leave there, together.)
+    uint32_t flags = tile_flags(sm, t), before = CF::kByTile && t > 0 ? tile_flags(sm, t - 1) : 0;
+    bool ok = wait(sm.qkdone + 8 * b, phase);
+    ok = ok && wait(sm.pvdone + 8 * b, phase ^ 1u);
+    good = good && __all_sync(0xffffffffu, ok);
+    if (!is_of(flags)) flags = tile_flags(sm, t);
     if (CF::kByTile && good && t > 0) {  // the tile before is the other warpgroup's
-      if (!is_of(before, t - 1)) before = tile_flags(sm, t - 1);
+      if (!is_of(before)) before = tile_flags(sm, t - 1);
       if (before & kFirst) begin(t - 1);
       if (good && (before & kLast)) good = end(t - 1);
     }
-    const bool stop = good && (flags & kStop);
-    if (good && (flags & kFirst) && !stop) begin(t);
-    const bool draft = flags & kDraft;
-    const float qs = draft ? p.qscale : p.qscale * p.k_scale;
+    float qs = qs_prefix;
     uint64_t vis = ~0ull;
-    if (good && !stop && (flags & kMasked)) good = __all_sync(0xffffffffu, rows_built());
-    if (good && !stop && (flags & kMasked)) vis = rows_seeing(kp, sm.rows[set], tile_words(sm, t), rb, key) >> col0;
-    // The buffer of P is free when P.V of the tile before the last is done (by tile: O is at rest then, too).
-    good = good && (stop || __all_sync(0xffffffffu, wait(sm.pvdone + 8 * b, phase ^ 1u)));
+    bool stop = false, leave_codes = false;
+    if (flags != 0 && good) {  // (most tiles have none)
+      stop = flags & kStop;
+      if ((flags & kFirst) && !stop) begin(t);
+      if ((flags & kMasked) && !stop) {
+        good = __all_sync(0xffffffffu, rows_built());
+        if (good) vis = rows_seeing(kp, sm.rows[set], tile_words(sm, t), rb, key) >> col0;
+      }
+      if (flags & kDraft) {
+        qs = p.qscale;
+        leave_codes = in_codes && !fresh && p.v_scale != 1.f;
+        in_codes = false;
+      }
+    }
     tc_fence_after();
     const uint32_t scores = trow + CF::kTmemS + b * CF::kNT + col0;
-    const bool leave_codes = draft && in_codes && !fresh && p.v_scale != 1.f;
-    if (draft) in_codes = false;
     float2 x[NC / 2];
     for (bool moved = false;; moved = true) {
       uint32_t s[NC];
@@ -689,10 +704,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   if (threadIdx.x == 0) allow_dependent_launch();  // the merge may be scheduled as CTAs finish
   const Smem sm = carve<CF>(smem_raw, p.C);
   const int warp = threadIdx.x >> 5;
-  if (threadIdx.x == 0) {
-    init_waits(p);
-    *sm.issued = 0;
-  }
+  if (threadIdx.x == 0) init_waits(p);
   static_assert(2 * CF::kStages + kBarriers <= 32, "a lane for each barrier");
   if (threadIdx.x < 2 * CF::kStages + kBarriers) {
     // Arrivals, in the order of carve(): the ring (of a stage, a decoding warpgroup's warps and the one that stages q), K and
@@ -705,21 +717,30 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   }
   if (warp == kWarpQ && (threadIdx.x & 31) < kMetas)  // (what an earlier CTA left there is of no tile)
     sts128(sm.meta + (threadIdx.x & 31) * sizeof(TileMeta), make_uint4(~0u, 0u, 0u, 0u));
-  if (warp == kWarpQk) {
-    tmem_alloc(smem_addr(sm.tmem), CF::kTmemCols);
-    tmem_relinquish();
-  }
-  tc_fence_before();
+  LoaderStart start;
+  if (warp == kWarpLoad) start = plan_loader(kp, sm);
   __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = *sm.tmem;
   const Waiter wait{p.wait_ns < kPollBelowNs};
-  if (warp < kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem);
-  else if (warp < kWarpLoad) run_decode<CF>(kp, sm, wait, tmem);
-  else if (warp == kWarpLoad) run_loader<CF::kStages, 2>(kp, sm, wait);  // (a last word for each warpgroup)
-  else if (warp == kWarpQk) run_qk<CF>(sm, wait, tmem);
-  else if (warp == kWarpPv) run_pv<CF>(sm, wait, tmem);
-  else if (warp == kWarpQ) run_q<CF>(kp, sm, wait);
+  uint32_t tmem = 0;
+  if (warp == kWarpLoad) {
+    run_loader<CF::kStages, 2>(kp, sm, start, wait);  // (a last word for each warpgroup)
+  } else if (warp == kWarpQ) {
+    run_q<CF>(kp, sm, wait);
+  } else {
+    // The roles that use tensor memory wait for it (and the others need not).
+    if (warp == kWarpQk) {
+      tmem_alloc(smem_addr(sm.tmem), CF::kTmemCols);
+      tmem_relinquish();
+    }
+    tc_fence_before();
+    named_barrier_sync(kBarTmem, kThreads - 64);
+    tc_fence_after();
+    tmem = *sm.tmem;
+    if (warp < kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem);
+    else if (warp < kWarpLoad) run_decode<CF>(kp, sm, wait, tmem);
+    else if (warp == kWarpQk) run_qk<CF>(sm, wait, tmem);
+    else run_pv<CF>(sm, wait, tmem);
+  }
   __syncwarp();
   tc_fence_before();
   __syncthreads();

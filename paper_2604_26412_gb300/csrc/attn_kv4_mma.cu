@@ -48,7 +48,7 @@ struct Smem : Ring {
 template <class CF>
 __host__ __device__ constexpr size_t smem_bytes(int C) {
   return 128 + CF::kStages * kStageSize + kQChunk<CF::kNR> * 4 + sizeof(float) * kWarps * CF::kRows * (kCombStride + 2) +
-         sizeof(TileMeta) * kMetas + sizeof(Rows) + sizeof(uint64_t) * (2 * CF::kStages + 2) + sizeof(int) * (4 + 2 * C + 1);
+         sizeof(TileMeta) * (kMetas + 1) + sizeof(Rows) + sizeof(uint64_t) * (2 * CF::kStages + 2) + sizeof(int) * (4 + 2 * C + 1);
 }
 
 template <class CF>
@@ -62,7 +62,8 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.sum = s.ref + kWarps * CF::kRows;
   TileMeta* meta = reinterpret_cast<TileMeta*>(s.sum + kWarps * CF::kRows);
   s.meta = smem_addr(meta);
-  uint64_t* m = reinterpret_cast<uint64_t*>(meta + kMetas);
+  s.first = smem_addr(meta + kMetas);
+  uint64_t* m = reinterpret_cast<uint64_t*>(meta + kMetas + 1);
   s.cfull = smem_addr(m);
   s.cempty = s.cfull + 8 * CF::kStages;
   s.joined = s.cempty + 8 * CF::kStages;
@@ -234,13 +235,18 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
   int stage = 0, rb = 0;
   uint32_t phase = 0;
 #pragma unroll 1
-  for (int t = 0;; ++t) {
-    if (!__all_sync(0xffffffffu, wait(sm.cfull + 8 * stage, phase))) return;
-    const int4 meta = tile_words(sm, t);  // flags, key0, nkeys, L
-    if (meta.x & kStop) return;
+  for (int t = -1;; ++t) {
+    // The first piece begins (t = -1) before its first tile has landed, the others with theirs.
+    int4 meta = make_int4(kFirst, 0, 0, 0);  // flags, key0, nkeys, L
+    if (t >= 0) {
+      if (!__all_sync(0xffffffffu, wait(sm.cfull + 8 * stage, phase))) return;
+      meta = tile_words(sm, t);
+      if (meta.x & kStop) return;
+    }
     const bool draft = meta.x & kDraft, masked = meta.x & kMasked;
-    if (meta.x & kFirst) {
-      const TileMeta w = tile_meta(sm, t);
+    if ((meta.x & kFirst) && t != 0) {
+      const TileMeta w = tile_meta_at(t < 0 ? sm.first : sm.meta + t % kMetas * sizeof(TileMeta));
+      if (!(w.flags & kFirst)) continue;  // (a CTA without tiles: its stop is next)
       if (!sync(wait)) return;  // the piece before has been written out
       rb = w.rb;
       if (w.flags & kNewRows) {
@@ -264,8 +270,9 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
         st.ref[nr][0] = st.ref[nr][1] = kNoRef;
         st.l[nr][0] = st.l[nr][1] = 0.f;
       }
-      in_codes = !draft;
+      in_codes = true;
       if (!sync(wait)) return;
+      if (t < 0) continue;
     }
     const uint32_t tile = sm.ring + stage * kStageSize;
     if (!draft) {
@@ -449,12 +456,14 @@ __global__ void __launch_bounds__(kThreads, CF::kMinBlocks) attn_kv4_mma_kernel(
     }
     mbar_init(sm.joined, kWarps);
     init_waits(p);
-    *sm.issued = 0;
     fence_mbar_init();
   }
+  const bool loads = threadIdx.x >= 32 * kWarps;
+  LoaderStart start;
+  if (loads) start = plan_loader(kp, sm);
   __syncthreads();
   const Waiter wait{p.wait_ns < kPollBelowNs};
-  if (threadIdx.x >= 32 * kWarps) run_loader<CF::kStages, 1>(kp, sm, wait);
+  if (loads) run_loader<CF::kStages, 1>(kp, sm, start, wait);
   else run_consumer<CF>(kp, sm, wait);
   __syncthreads();
   if (threadIdx.x == 0) drain<CF::kStages>(p, sm);

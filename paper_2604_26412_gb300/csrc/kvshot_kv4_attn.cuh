@@ -44,7 +44,7 @@ constexpr float kNoRef = -1e30f;                   // no score yet
 constexpr int kFirst = 1, kLast = 2;   // of the CTA's piece of a unit
 constexpr int kDraft = 4;              // bf16 draft keys, else codes
 constexpr int kMasked = 8;             // holds keys that some query row does not see
-constexpr int kWhole = 16;             // the piece is the whole unit
+constexpr int kWhole = 16;             // (with kLast) the piece is the whole unit
 constexpr int kNewRows = 32;           // the query rows' nodes differ from the piece's before
 constexpr int kNewTree = 64;           // and so does the draft tree
 constexpr int kStop = 128;             // no tile: the CTA's work is done
@@ -60,6 +60,7 @@ constexpr int kTagShift = 16;
 struct Ring {
   uint32_t ring, cfull, cempty;
   uint32_t meta;    // [kMetas] TileMeta
+  uint32_t first;   // TileMeta of the CTA's first piece, whose q and rows need not wait for a tile (flags 0: there is none)
   int* issued;      // tiles issued by the loader
   int *len, *base;  // the loader's plan
 };
@@ -110,7 +111,7 @@ __device__ __forceinline__ void init_waits(const AttnParams& p) {
 struct Waiter {
   bool poll;
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
-    if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
+    if (!poll && mbar_try_wait(bar, parity)) return true;
     return wait_slow(bar, parity);
   }
 };
@@ -130,14 +131,17 @@ __device__ __forceinline__ int4 tile_words(const Ring& r, int t) {
   const uint4 v = lds128(r.meta + t % kMetas * sizeof(TileMeta));
   return make_int4(v.x, v.y, v.z, v.w);
 }
-__device__ __forceinline__ TileMeta tile_meta(const Ring& r, int t) {
-  const uint4 v = lds128(r.meta + t % kMetas * sizeof(TileMeta)), w = lds128(r.meta + t % kMetas * sizeof(TileMeta) + 16);
+__device__ __forceinline__ TileMeta tile_meta_at(uint32_t at) {
+  const uint4 v = lds128(at), w = lds128(at + 16);
   return TileMeta{static_cast<int>(v.x), static_cast<int>(v.y), static_cast<int>(v.z), static_cast<int>(v.w),
                   static_cast<int>(w.x), static_cast<int>(w.y), static_cast<int>(w.z), static_cast<int>(w.w)};
 }
+__device__ __forceinline__ TileMeta tile_meta(const Ring& r, int t) { return tile_meta_at(r.meta + t % kMetas * sizeof(TileMeta)); }
 // Its flags alone, read ahead of the wait; they are the tile's if is_of says so, and else are read again after it.
-__device__ __forceinline__ int tile_flags(const Ring& r, int t) { return lds32(r.meta + t % kMetas * sizeof(TileMeta)); }
-__device__ __forceinline__ bool is_of(int flags, int t) { return ((flags >> kTagShift) & 0xffff) == (t & 0xffff); }
+__device__ __forceinline__ uint32_t tile_flags(const Ring& r, int t) {
+  return lds32(r.meta + t % kMetas * sizeof(TileMeta)) ^ (static_cast<uint32_t>(t) << kTagShift);
+}
+__device__ __forceinline__ bool is_of(uint32_t flags) { return flags < (1u << kTagShift); }
 
 // ------------------------------------------------------------ loads
 
@@ -177,14 +181,14 @@ __device__ __forceinline__ void build_kv4_plan(const AttnParams& p, int HR, int*
   __syncwarp();
 }
 
-// The loading warp: the CTA's tiles, one after another, each a stage of the ring with a copy per run of groups (a draft
-// tile: two per row); at the end `kStops` tiles that say so.
-template <int kStages, int kStops>
-__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring, const Waiter& wait) {
+// A CTA's range of tiles [t, t_end), which begins in cache c, KV head x row block hr, tile lt of the unit.
+struct LoaderStart {
+  int t, t_end, c, hr, lt;
+};
+// By the loading warp, before the barrier that the roles begin with.
+__device__ __forceinline__ LoaderStart plan_loader(const Kv4Params& kp, const Ring& sm) {
   const AttnParams& p = kp.a;
-  const Ring sm = ring;
   const int lane = threadIdx.x & 31, HR = p.hkv * p.row_blocks;
-  // This CTA's range [t, t_end): cache c, KV head x row block hr, tile lt of the unit.
   int t = 0, t_end, c = 0, hr = 0, lt = 0;
   if (p.unit_ctas > 0) {
     if (lane == 0) sm.len[0] = clamp_len(p, 0);
@@ -212,6 +216,24 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
       lt = rem - hr * ut;
     }
   }
+  if (lane == 0) {
+    const int h = kp.by_blocks(hr);
+    *sm.issued = 0;
+    sts128(sm.first, make_uint4(t < t_end ? kFirst | kNewRows | (p.tree ? kNewTree : 0) : 0, 0, 0, 0));
+    sts128(sm.first + 16, make_uint4(c, h, hr - h * p.row_blocks, kp.by_seq(c)));
+  }
+  return LoaderStart{t, t_end, c, hr, lt};
+}
+
+// The loading warp: the CTA's tiles, one after another, each a stage of the ring with a copy per run of groups (a draft
+// tile: two per row); at the end `kStops` tiles that say so.
+template <int kStages, int kStops>
+__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring, const LoaderStart& start, const Waiter& wait) {
+  const AttnParams& p = kp.a;
+  const Ring sm = ring;
+  const int lane = threadIdx.x & 31, HR = p.hkv * p.row_blocks;
+  const int t_end = start.t_end;
+  int t = start.t, c = start.c, hr = start.hr, lt = start.lt;
   int stage = 0, issued = 0, last_rb = -1, last_seq = -1;
   uint32_t phase = 0;
   bool waited = false, ok = true;
@@ -225,7 +247,8 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
     const WindowSpan span = window_span<kTile>(p, L);
     const int ut = span.tiles + p.draft_tiles, lt1 = min(ut, lt + t_end - t);
     const int h = kp.by_blocks(hr), rb = hr - h * p.row_blocks, seq = kp.by_seq(c);
-    int flags = kFirst | (lt == 0 && lt1 == ut ? kWhole : 0);
+    const int last = kLast | (lt == 0 && lt1 == ut ? kWhole : 0);
+    int flags = kFirst;
     if (rb != last_rb) flags |= kNewRows;
     if (p.tree && seq != last_seq) flags |= kNewRows | kNewTree;
     last_rb = rb;
@@ -261,7 +284,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
       const int nkeys = draft ? min(kDraftTile, p.N - key0) : min(kTile, L - key0);
       if (draft) flags |= kDraft | kMasked;
       else if (nkeys < kTile || (key0 < seen_from && key0 + kTile > p.sinks)) flags |= kMasked;
-      if (lt == lt1 - 1) flags |= kLast;
+      if (lt == lt1 - 1) flags |= last;
       if (draft && !waited) {  // the draft K/V may come from the preceding kernel
         wait_for_prerequisite_grid();
         waited = true;
@@ -285,7 +308,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
       } else if (my_tile == lt - (window - ahead) && bytes > 0) {
         bulk_load(dst + my_g0 * kKv4Bytes, src, bytes, bar);
       }
-      flags &= kWhole;
+      flags = 0;
       ++issued;
       if (++stage == kStages) {
         stage = 0;
