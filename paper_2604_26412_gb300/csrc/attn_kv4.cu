@@ -35,24 +35,23 @@ size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 constexpr int kVHalf = kTile * 128;                // 64 dims of a tile's V: 128 rows of 128 bytes, 128-byte swizzle
 constexpr int kVTile = 2 * kVHalf;
 constexpr int kPTile = kTile * 128;                // P^T: a row of up to 64 query rows per key, 128-byte swizzle
-constexpr int kThreads = 20 * 32;
+constexpr int kCols = 16;                          // query rows of a softmax thread
 constexpr int kGroupThreads = 128;                 // a warpgroup
-constexpr int kWarpDecode = 8, kWarpLoad = 16, kWarpQk = 17, kWarpPv = 18, kWarpQ = 19;
-constexpr int kBarTmem = 3;                        // named barrier: all but the loading warp and q's
-constexpr int kBarGroup = 1;                       // named barriers 1 and 2: the threads of a softmax warpgroup
-// NC: query rows of a unit, a multiple of 8.
+constexpr int kBarTmem = 5;                        // named barrier: all but the loading warp and q's
+constexpr int kBarGroup = 1;                       // named barriers 1 to 4: the threads of a softmax warpgroup
+// NC: query rows of a unit, a multiple of 16 (and the MMAs' N).
 template <int NC>
 struct Cfg {
   static constexpr int kNC = NC;
-  static constexpr int kNT = (NC + 15) / 16 * 16;      // the MMA's N
-  static constexpr bool kByTile = NC <= 32;            // the softmax warpgroups share out the tiles, else the rows
-  static constexpr int kCols = kByTile ? NC : NC / 2;  // rows of a softmax thread
-  static constexpr int kAccs = kByTile ? 2 : 1;        // accumulators
+  static constexpr int kGroups = NC / kCols;           // softmax warpgroups
+  // Warps: the softmax warpgroups, two that decode, then the loading one, QK^T's, P.V's and q's.
+  static constexpr int kWarpDecode = 4 * kGroups, kWarpLoad = kWarpDecode + 8, kWarpQk = kWarpLoad + 1,
+                       kWarpPv = kWarpLoad + 2, kWarpQ = kWarpLoad + 3, kThreads = 32 * (kWarpLoad + 4);
   static constexpr int kStages = NC <= 32 ? 5 : 4;
-  static constexpr int kQTile = kNT * 256;
-  static constexpr uint32_t kTmemK = 0, kTmemS = 128, kTmemO = 128 + 2 * kNT;  // columns
-  static constexpr uint32_t kTmemCols = kTmemO + kAccs * kNT <= 256 ? 256 : 512;
-  static_assert(kTmemO + kAccs * kNT <= 512 && kCols % 8 == 0, "tensor memory");
+  static constexpr int kQTile = NC * 256;
+  static constexpr uint32_t kTmemK = 0, kTmemS = 128, kTmemO = 128 + 2 * NC;  // columns
+  static constexpr uint32_t kTmemCols = kTmemO + NC <= 256 ? 256 : 512;
+  static_assert(kTmemO + NC <= 512, "tensor memory");
 };
 
 constexpr int kRowSets = 4;  // more than the pieces between the warp that builds one and its last reader
@@ -66,9 +65,9 @@ struct Smem : Ring {
   uint32_t ofree, mmadone;           // epilogue has read O; [2] every MMA issued is done
   uint32_t rfull;                    // [kRowSets] a piece's rows built
   uint32_t joined;                   // barrier of the softmax warps
-  float *ref, *alpha, *inv;          // [2][64] per warpgroup and row (ref: negated)
-  int* wmax;                         // [8][64] per warp and row; sums at a piece's end
-  int* codes;                        // [2] the warpgroup's accumulator is in units of the value codes
+  float *ref, *alpha, *inv;          // [64] per row (ref: negated)
+  int* wmax;                         // [softmax warp][64] per warp and row; sums at a piece's end
+  int* codes;                        // O is in units of the value codes
   uint32_t* tmem;
 };
 
@@ -78,7 +77,7 @@ template <class CF>
 __host__ __device__ constexpr size_t smem_bytes(int C) {
   return 1024 + 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize +
          sizeof(TileMeta) * (kMetas + 1) + sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + kRowSets * sizeof(Rows) +
-         sizeof(int) * (6 * 64 + 8 * 64 + 6) + sizeof(int) * (2 * C + 1);
+         sizeof(int) * (3 * 64 + CF::kGroups * 4 * 64 + 8) + sizeof(int) * (2 * C + 1);
 }
 
 template <class CF>
@@ -108,13 +107,13 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.rfull = s.joined + 8;
   s.rows = reinterpret_cast<Rows*>(b + 8 * (2 * CF::kStages + kBarriers));
   s.ref = reinterpret_cast<float*>(s.rows + kRowSets);
-  s.alpha = s.ref + 128;
-  s.inv = s.alpha + 128;
-  s.wmax = reinterpret_cast<int*>(s.inv + 128);
-  s.codes = s.wmax + 8 * 64;
-  s.tmem = reinterpret_cast<uint32_t*>(s.codes + 2);
-  s.issued = s.codes + 4;
-  s.len = s.codes + 6;
+  s.alpha = s.ref + 64;
+  s.inv = s.alpha + 64;
+  s.wmax = reinterpret_cast<int*>(s.inv + 64);
+  s.codes = s.wmax + CF::kGroups * 4 * 64;
+  s.tmem = reinterpret_cast<uint32_t*>(s.codes + 4);
+  s.issued = s.codes + 6;
+  s.len = s.codes + 8;
   s.base = s.len + C;
   return s;
 }
@@ -150,9 +149,9 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
     const int row0 = w.rb * p.rows_per_unit, rows = min(p.rows_per_unit, p.rows_total - row0);
     // 16 bytes of two rows at a time per warp; eight loads of a lane on their way together.
     const int ch = lane & 15;
-    const uint32_t dst = sm.q + b * CF::kQTile + (ch >> 3) * (CF::kNT * 128);
+    const uint32_t dst = sm.q + b * CF::kQTile + (ch >> 3) * (CF::kNC * 128);
 #pragma unroll 1
-    for (int r0 = lane >> 4; r0 < CF::kNT; r0 += 16) {
+    for (int r0 = lane >> 4; r0 < CF::kNC; r0 += 16) {
       uint4 x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -320,7 +319,7 @@ __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sy
 template <class CF>
 __device__ __forceinline__ void run_qk(const Smem& smem, const Waiter& wait, uint32_t tmem_base) {
   const Smem sm = smem;
-  constexpr uint32_t idesc = idesc_f16(128, CF::kNT, false);
+  constexpr uint32_t idesc = idesc_f16(128, CF::kNC, false);
   const uint32_t tmem = uniform(tmem_base);
   const uint64_t q0 = smem_desc_sw128(sm.q, 16, 1024);
   int piece = -1;
@@ -340,7 +339,7 @@ __device__ __forceinline__ void run_qk(const Smem& smem, const Waiter& wait, uin
       ++stops;  // (its S is nothing, and the softmax sees that)
     } else {
       tc_fence_after();
-      const uint32_t d = tmem + CF::kTmemS + b * CF::kNT;
+      const uint32_t d = tmem + CF::kTmemS + b * CF::kNC;
       uint32_t k = tmem + CF::kTmemK + 64 * b;
       uint64_t q = q0 + (piece & 1) * (CF::kQTile >> 4);
 #pragma unroll 1
@@ -348,7 +347,7 @@ __device__ __forceinline__ void run_qk(const Smem& smem, const Waiter& wait, uin
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) tc_mma_tmem_a_elect(d, k + 8 * ks, q + 2 * ks, idesc, half + ks > 0);
         k += 32;
-        q += CF::kNT * 128 >> 4;
+        q += CF::kNC * 128 >> 4;
       }
       if (flags & kLast) tc_commit_elect(sm.qempty + 8 * (piece & 1));
     }
@@ -360,7 +359,7 @@ __device__ __forceinline__ void run_qk(const Smem& smem, const Waiter& wait, uin
 template <class CF>
 __device__ __forceinline__ void run_pv(const Smem& smem, const Waiter& wait, uint32_t tmem_base) {
   const Smem sm = smem;
-  constexpr uint32_t idesc = idesc_f16(128, CF::kNT, true, true);
+  constexpr uint32_t idesc = idesc_f16(128, CF::kNC, true, true);
   const uint32_t tmem = uniform(tmem_base);
   const uint64_t v0 = smem_desc_sw128(sm.v, kVHalf, 1024), p0 = smem_desc_sw128(sm.p, kPTile, 1024);
   int piece = -1, in_piece = 0;
@@ -378,9 +377,9 @@ __device__ __forceinline__ void run_pv(const Smem& smem, const Waiter& wait, uin
     }
     if (!__all_sync(0xffffffffu, ok)) break;
     tc_fence_after();
-    const uint32_t o = tmem + CF::kTmemO + (CF::kByTile ? b * CF::kNT : 0);
+    const uint32_t o = tmem + CF::kTmemO;
     uint64_t v = v0 + b * (kVTile >> 4), x = p0 + b * (kPTile >> 4);
-    uint32_t more = in_piece >= CF::kAccs;  // the accumulator holds tiles of this piece
+    uint32_t more = in_piece > 0;  // the accumulator holds tiles of this piece
 #pragma unroll 1
     for (int half = 0; half < 2; ++half) {
 #pragma unroll
@@ -478,11 +477,9 @@ __device__ __noinline__ void rescale_o(const float* alpha, int n, uint32_t o_col
   tmem_wait_st();
 }
 
-// A piece's rows [j0, j1) of this thread's dim: the final ones, or the piece's part in the workspace.  kAccs 2: O and the
-// other accumulator `next` columns on, each with its own weights (0: it holds nothing).
-template <int kAccs>
+// A piece's rows [j0, j1) of this thread's dim: the final ones, or the piece's part in the workspace.
 __device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, const int* place, const TileMeta& w, int j0, int j1,
-                                        uint32_t o_cols, int next) {
+                                        uint32_t o_cols) {
   const int tid = threadIdx.x & 127;
   const size_t row0 = static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G;
   const size_t part = static_cast<size_t>((w.c * p.hkv + w.h) * p.row_blocks + w.rb + blockIdx.x) * p.rows_per_unit;
@@ -493,17 +490,14 @@ __device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, con
   const uint32_t inv = smem_addr(sm.inv), places = smem_addr(place);
 #pragma unroll 1
   for (int j = j0; j < j1; j += 4) {
-    uint32_t o[4], o2[4];
+    uint32_t o[4];
     tmem_ld4(o_cols + j, o);
-    if (kAccs == 2) tmem_ld4(o_cols + next + j, o2);
     const uint4 a = lds128(inv + 4 * j), at = lds128(places + 4 * j);
-    const uint4 a2 = kAccs == 2 ? lds128(inv + 4 * (64 + j)) : a;
-    const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {a2.x, a2.y, a2.z, a2.w}, to[4] = {at.x, at.y, at.z, at.w};
+    const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, to[4] = {at.x, at.y, at.z, at.w};
     tmem_wait_ld();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float v = wa[i] != 0u ? __uint_as_float(o[i]) * __uint_as_float(wa[i]) : 0.f;
-      if (kAccs == 2) v += wb[i] != 0u ? __uint_as_float(o2[i]) * __uint_as_float(wb[i]) : 0.f;
+      const float v = wa[i] != 0u ? __uint_as_float(o[i]) * __uint_as_float(wa[i]) : 0.f;
       if (!whole) ws[i * kHeadDim] = v;
       else if (j + i < end) out[static_cast<size_t>(to[i]) * kHeadDim] = __float2bfloat16(v);
     }
@@ -511,31 +505,13 @@ __device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, con
   }
 }
 
-// The rows' sums, weights of the accumulators and log-sum-exp.  Thread = row.  had: whether each accumulator holds tiles
-// of this piece.
-template <class CF>
-__device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, const int* place, const TileMeta& w, int j,
-                                       bool had0, bool had1) {
+// The rows' sums, weights and log-sum-exp.  Thread = row.
+__device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, const int* place, const TileMeta& w, int j) {
   const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
-  auto total = [&](int wg, int col) {
-    const int* x = sm.wmax + wg * 256 + col;
-    return (__int_as_float(x[0]) + __int_as_float(x[64])) + (__int_as_float(x[128]) + __int_as_float(x[192]));
-  };
-  float sum, top;
-  if constexpr (CF::kByTile) {
-    const float r0 = had0 ? -sm.ref[j] : kNoRef, r1 = had1 ? -sm.ref[64 + j] : kNoRef;
-    top = fmaxf(r0, r1);
-    const float w0 = had0 ? ex2(r0 - top) : 0.f, w1 = had1 ? ex2(r1 - top) : 0.f;
-    sum = (had0 ? w0 * total(0, j) : 0.f) + (had1 ? w1 * total(1, j) : 0.f);
-    const float inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
-    sm.inv[j] = w0 * inv * (sm.codes[0] ? p.v_scale : 1.f);
-    sm.inv[64 + j] = w1 * inv * (sm.codes[1] ? p.v_scale : 1.f);
-  } else {
-    const int wg = j >= CF::kCols;
-    top = -sm.ref[j];
-    sum = total(wg, j - wg * CF::kCols);
-    sm.inv[j] = sum == 0.f ? 0.f : __fdividef(sm.codes[0] ? p.v_scale : 1.f, sum);
-  }
+  const int* x = sm.wmax + j / kCols * 256 + j % kCols;
+  const float sum = (__int_as_float(x[0]) + __int_as_float(x[64])) + (__int_as_float(x[128]) + __int_as_float(x[192]));
+  const float top = -sm.ref[j];
+  sm.inv[j] = sum == 0.f ? 0.f : __fdividef(*sm.codes ? p.v_scale : 1.f, sum);
   if (j >= rows) return;
   const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
   if (w.flags & kWhole) p.lse[static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G + place[j]] = lse2 * 0.69314718055994531f;
@@ -544,24 +520,23 @@ __device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, cons
 
 template <class CF>
 __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& smem, const Waiter& wait, uint32_t tmem) {
-  constexpr int NC = CF::kCols;
+  constexpr int NC = kCols;
   const AttnParams& p = kp.a;
   const Smem sm = smem;
   const int lane = threadIdx.x & 31, key = threadIdx.x & 127, wg = threadIdx.x >> 7;
-  const int col0 = CF::kByTile ? 0 : wg * NC;  // this thread's first row
+  const int col0 = wg * NC;  // this thread's first row
   const uint32_t trow = tmem + (static_cast<uint32_t>(key & 96) << 16);
-  const uint32_t o_cols = trow + CF::kTmemO + (CF::kByTile ? wg * CF::kNT : col0);
+  const uint32_t o_cols = trow + CF::kTmemO + col0;
   const uint32_t pdst = sm.p + key * 128, sw = static_cast<uint32_t>(key & 7) << 4;
-  float* ref = sm.ref + (CF::kByTile ? 64 * wg : col0);
-  float* alpha = sm.alpha + (CF::kByTile ? 64 * wg : col0);
+  float* ref = sm.ref + col0;
+  float* alpha = sm.alpha + col0;
   int* wmax = sm.wmax + 256 * wg;
   const int bar = kBarGroup + wg;
   WarpSync sync{sm.joined, 0};
   float2 l[NC / 2];               // sums over this thread's keys
   bool in_codes = false;          // O is in units of the value codes
   wait_for_prerequisite_grid();   // outputs and scratch may be the preceding kernel's
-  bool fresh = true;              // this warpgroup has had no tile of the piece
-  int t_first = 0;                // the piece's first tile
+  bool fresh = true;              // the piece has had no tile yet
   bool good = true;               // no wait of this warp has given up
   const float qs_prefix = p.qscale * p.k_scale;
   int rb = 0, set = -1, piece = -1;  // the piece's row block, its set of rows and number
@@ -573,7 +548,6 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
 #pragma unroll
     for (int j = 0; j < NC / 2; ++j) l[j] = make_float2(0.f, 0.f);
     in_codes = fresh = true;
-    t_first = t;
   };
   auto rows_built = [&]() { return wait(sm.rfull + 8 * (piece & (kRowSets - 1)), (piece / kRowSets) & 1); };
   // A piece's end, at its last tile t: join the warpgroups and write the rows.
@@ -589,38 +563,31 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
 #pragma unroll
     for (int i = 0; i < NC; ++i)
       if (i < width) wmax[(key >> 5) * 64 + col + i] = __float_as_int(sums[i]);
-    if (key == 0) sm.codes[wg] = in_codes;
-    // O is at rest: P.V of this warpgroup's last tile of the piece is done.
-    const int mine = CF::kByTile && (t & 1) != wg ? t - 1 : t;
-    const bool ok = (fresh || wait(sm.pvdone + 8 * (mine & 1), (mine >> 1) & 1)) && rows_built();
+    if (threadIdx.x == 0) *sm.codes = in_codes;
+    // O is at rest: P.V of the piece's last tile is done.
+    const bool ok = wait(sm.pvdone + 8 * (t & 1), (t >> 1) & 1) && rows_built();
     if (!__all_sync(0xffffffffu, ok) || !sync(wait)) return false;
-    const bool two = t > t_first;
-    if (threadIdx.x < CF::kNC) join_sums<CF>(p, smem, sm.rows[set].place, tile_meta(sm, t), threadIdx.x, two || !(t & 1), two || (t & 1));
+    if (threadIdx.x < CF::kNC) join_sums(p, smem, sm.rows[set].place, tile_meta(sm, t), threadIdx.x);
     if (!sync(wait)) return false;
     tc_fence_after();
-    write_rows<CF::kAccs>(p, smem, sm.rows[set].place, tile_meta(sm, t), wg * (CF::kNC / 2), (wg + 1) * (CF::kNC / 2), trow + CF::kTmemO, CF::kNT);
+    write_rows(p, smem, sm.rows[set].place, tile_meta(sm, t), col0, col0 + NC, trow + CF::kTmemO);
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(sm.ofree);
     return true;
   };
 #pragma unroll 1
-  for (int t = CF::kByTile ? wg : 0;; t += CF::kAccs) {
-    const int b = CF::kByTile ? wg : t & 1;
+  for (int t = 0;; ++t) {
+    const int b = t & 1;
     const uint32_t phase = (t >> 1) & 1;
     // S, and with it the words of the tile and of those before it; and the buffer of P, free when P.V of the tile before
-    // the last is done (by tile: O is at rest then, too).  (A warp whose wait gives up goes on to the vote: the warps of a
+    // the last is done.  (A warp whose wait gives up goes on to the vote: the warps of a
     // warpgroup leave there, together.)
-    uint32_t flags = tile_flags(sm, t), before = CF::kByTile && t > 0 ? tile_flags(sm, t - 1) : 0;
+    uint32_t flags = tile_flags(sm, t);
     bool ok = wait(sm.qkdone + 8 * b, phase);
     ok = ok && wait(sm.pvdone + 8 * b, phase ^ 1u);
     good = good && __all_sync(0xffffffffu, ok);
     if (!is_of(flags)) flags = tile_flags(sm, t);
-    if (CF::kByTile && good && t > 0) {  // the tile before is the other warpgroup's
-      if (!is_of(before)) before = tile_flags(sm, t - 1);
-      if (before & kFirst) begin(t - 1);
-      if (good && (before & kLast)) good = end(t - 1);
-    }
     float qs = qs_prefix;
     uint64_t vis = ~0ull;
     bool stop = false, leave_codes = false;
@@ -638,7 +605,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
       }
     }
     tc_fence_after();
-    const uint32_t scores = trow + CF::kTmemS + b * CF::kNT + col0;
+    const uint32_t scores = trow + CF::kTmemS + b * CF::kNC + col0;
     float2 x[NC / 2];
     for (bool moved = false;; moved = true) {
       uint32_t s[NC];
@@ -670,10 +637,8 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
         l[j].y *= alpha[2 * j + 1];
       }
       if (!fresh) {
-        if constexpr (!CF::kByTile) {
-          if (any_of(bar, kGroupThreads, !wait(sm.pvdone + 8 * (b ^ 1), ((t - 1) >> 1) & 1))) return;
-          tc_fence_after();
-        }
+        if (any_of(bar, kGroupThreads, !wait(sm.pvdone + 8 * (b ^ 1), ((t - 1) >> 1) & 1))) return;
+        tc_fence_after();
         rescale_o(alpha, NC, o_cols, leave_codes ? p.v_scale : 1.f);
       }
     }
@@ -698,7 +663,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
 }
 
 template <class CF>
-__global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_constant__ Kv4Params kp) {
+__global__ void __launch_bounds__(CF::kThreads, 1) attn_kv4_kernel(const __grid_constant__ Kv4Params kp) {
   extern __shared__ uint8_t smem_raw[];
   const AttnParams& p = kp.a;
   if (threadIdx.x == 0) allow_dependent_launch();  // the merge may be scheduled as CTAs finish
@@ -710,35 +675,33 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
     // Arrivals, in the order of carve(): the ring (of a stage, a decoding warpgroup's warps and the one that stages q), K and
     // V decoded, then the rest.
     const int j = threadIdx.x - 2 * CF::kStages;
-    mbar_init(sm.cfull + 8 * threadIdx.x, j < -CF::kStages ? 1 : j < 0 ? 5 : j < 4 ? 4 : (j >> 1) == 3 ? (CF::kByTile ? 4 : 8)
-                                          : (j >> 1) == 8                                             ? 8
-                                                                                                      : 1);
+    mbar_init(sm.cfull + 8 * threadIdx.x, j < -CF::kStages ? 1 : j < 0 ? 5 : j < 4 ? 4 : (j >> 1) == 3 || (j >> 1) == 8 ? 4 * CF::kGroups : 1);
     fence_mbar_init();
   }
-  if (warp == kWarpQ && (threadIdx.x & 31) < kMetas)  // (what an earlier CTA left there is of no tile)
+  if (warp == CF::kWarpQ && (threadIdx.x & 31) < kMetas)  // (what an earlier CTA left there is of no tile)
     sts128(sm.meta + (threadIdx.x & 31) * sizeof(TileMeta), make_uint4(~0u, 0u, 0u, 0u));
   LoaderStart start;
-  if (warp == kWarpLoad) start = plan_loader(kp, sm);
+  if (warp == CF::kWarpLoad) start = plan_loader(kp, sm);
   __syncthreads();
   const Waiter wait{p.wait_ns < kPollBelowNs};
   uint32_t tmem = 0;
-  if (warp == kWarpLoad) {
+  if (warp == CF::kWarpLoad) {
     run_loader<CF::kStages, 2>(kp, sm, start, wait);  // (a last word for each warpgroup)
-  } else if (warp == kWarpQ) {
+  } else if (warp == CF::kWarpQ) {
     run_q<CF>(kp, sm, wait);
   } else {
     // The roles that use tensor memory wait for it (and the others need not).
-    if (warp == kWarpQk) {
+    if (warp == CF::kWarpQk) {
       tmem_alloc(smem_addr(sm.tmem), CF::kTmemCols);
       tmem_relinquish();
     }
     tc_fence_before();
-    named_barrier_sync(kBarTmem, kThreads - 64);
+    named_barrier_sync(kBarTmem, CF::kThreads - 64);
     tc_fence_after();
     tmem = *sm.tmem;
-    if (warp < kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem);
-    else if (warp < kWarpLoad) run_decode<CF>(kp, sm, wait, tmem);
-    else if (warp == kWarpQk) run_qk<CF>(sm, wait, tmem);
+    if (warp < CF::kWarpDecode) run_softmax<CF>(kp, sm, wait, tmem);
+    else if (warp < CF::kWarpLoad) run_decode<CF>(kp, sm, wait, tmem);
+    else if (warp == CF::kWarpQk) run_qk<CF>(sm, wait, tmem);
     else run_pv<CF>(sm, wait, tmem);
   }
   __syncwarp();
@@ -752,10 +715,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_kv4_kernel(const __grid_cons
   }
   __syncthreads();
   tc_fence_after();
-  if (warp == kWarpQk) tmem_dealloc(tmem, CF::kTmemCols);
+  if (warp == CF::kWarpQk) tmem_dealloc(tmem, CF::kTmemCols);
 }
 
-constexpr int kMmaRows = 16;
 constexpr int kMaxRows = 64;  // query rows of a unit
 
 int rows_of_unit(int rows) {
@@ -770,17 +732,13 @@ cudaError_t launch_cfg(const Kv4Params& kp, bool pdl, cudaStream_t stream) {
   const cudaError_t e =
       cudaFuncSetAttribute(attn_kv4_kernel<CF>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  return launch_maybe_pdl(attn_kv4_kernel<CF>, dim3(kp.a.num_ctas), dim3(kThreads), smem, pdl, stream, kp);
+  return launch_maybe_pdl(attn_kv4_kernel<CF>, dim3(kp.a.num_ctas), dim3(CF::kThreads), smem, pdl, stream, kp);
 }
 
 cudaError_t launch(const Kv4Params& kp, bool pdl, cudaStream_t stream) {
   switch (kp.a.rows_per_unit) {
     case 8:
-      if (kMmaRows >= 8) return launch_attn_kv4_mma(kp, pdl, stream);
-      return launch_cfg<Cfg<8>>(kp, pdl, stream);
-    case 16:
-      if (kMmaRows >= 16) return launch_attn_kv4_mma(kp, pdl, stream);
-      return launch_cfg<Cfg<16>>(kp, pdl, stream);
+    case 16: return launch_attn_kv4_mma(kp, pdl, stream);
     case 32: return launch_cfg<Cfg<32>>(kp, pdl, stream);
     case 48: return launch_cfg<Cfg<48>>(kp, pdl, stream);
     case 64: return launch_cfg<Cfg<64>>(kp, pdl, stream);
@@ -824,7 +782,7 @@ kvshot_status make_kv4_plan(const kvshot_attn_desc* d, int32_t window, int32_t s
   if (grid == 0) {
     const int sms = sm_count();
     int per_sm = 1;
-    if (pl->rows_per_unit <= kMmaRows && attn_kv4_mma_occupancy(pl->rows_per_unit, d->num_caches, &per_sm) != cudaSuccess)
+    if (pl->rows_per_unit <= 16 && attn_kv4_mma_occupancy(pl->rows_per_unit, d->num_caches, &per_sm) != cudaSuccess)
       return KVSHOT_ERR_CUDA;
     if (sms < 1 || per_sm < 1) return KVSHOT_ERR_CUDA;
     grid = std::min<int64_t>(sms * per_sm, std::max((max_tiles + kMinTiles - 1) / kMinTiles, units));
