@@ -107,7 +107,7 @@ __device__ __forceinline__ uint2 scales_of(uint32_t a, uint32_t b, uint32_t sel)
 __device__ __forceinline__ uint32_t select_bits(uint32_t a, uint32_t b, uint32_t m) { return (a & m) | (b & ~m); }
 
 // Join the warps' parts of a piece, which lie in shared memory, and write it: the final bf16 output + lse if it is the
-// whole unit, else the normalised fp32 part + log2-domain lse.  All consumer threads (thread = dim).
+// whole unit, else the normalised fp32 part + log2-domain lse.  All consumer threads.
 template <int n>
 __device__ __noinline__ bool join_warps(const AttnParams& p, const Smem& sm, const TileMeta& w, WarpSync& sync, const Waiter& wait) {
   const int tid = threadIdx.x;
@@ -130,13 +130,23 @@ __device__ __noinline__ bool join_warps(const AttnParams& p, const Smem& sm, con
     else p.ws_lse[part + tid] = lse2;
   }
   if (!sync(wait)) return false;
+  const int lane = tid & 31;  // four dims, of a row of this warp
 #pragma unroll 1
-  for (int r = 0; r < rows; ++r) {
-    float v = 0.f;
+  for (int r = tid >> 5; r < rows; r += kWarps) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) v = fmaf(sm.ref[k * n + r], sm.comb_o[(k * n + r) * kCombStride + tid], v);
-    if (whole) p.out[(orow0 + sm.rows->place[r]) * kHeadDim + tid] = __float2bfloat16(v);
-    else p.ws_o[(part + r) * kHeadDim + tid] = v;
+    for (int k = 0; k < kWarps; ++k) {
+      const float a = sm.ref[k * n + r];
+      const float4 o = *reinterpret_cast<const float4*>(sm.comb_o + (k * n + r) * kCombStride + 4 * lane);
+      v.x = fmaf(a, o.x, v.x);
+      v.y = fmaf(a, o.y, v.y);
+      v.z = fmaf(a, o.z, v.z);
+      v.w = fmaf(a, o.w, v.w);
+    }
+    if (whole)
+      reinterpret_cast<uint2*>(p.out + (orow0 + sm.rows->place[r]) * kHeadDim)[lane] = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    else
+      reinterpret_cast<float4*>(p.ws_o + (part + r) * kHeadDim)[lane] = v;
   }
   return true;
 }

@@ -68,9 +68,9 @@ struct Ring {
 struct alignas(16) Rows {
   int place[64];                      // (read four at a time)
   uint64_t line[kMaxTreeNodes];       // rows whose node is this one or descends from it
-  uint64_t upto[kMaxTreeNodes + 1];   // rows whose depth is at most x (with a window)
+  uint64_t upto[kMaxTreeNodes + 1];   // rows whose depth is at most x
   uint64_t anc[kMaxTreeNodes];        // nodes: itself and its ancestors
-  int parent[kMaxTreeNodes];
+  int parent[kMaxTreeNodes];          // (of build_rows)
 };
 
 // Every wait ends: when its phase completes, when another role has given up, or (which gives up) after the call's limit.
@@ -413,36 +413,56 @@ __device__ __noinline__ void build_rows(const Kv4Params& kp, Rows& r, int nc, in
       r.parent[i] = v;
     }
     __syncwarp();
-#pragma unroll 1
-    for (int i = lane; i < p.N; i += 32) {
-      uint64_t bits = 0;
-#pragma unroll 1
-      for (int m = i; m >= 0; m = r.parent[m]) bits |= 1ull << m;  // parents strictly decrease
-      r.anc[i] = bits;
-    }
+    // Ancestors, by jumps that double: a node's bits so far end above r.parent, where the next ones begin.
+    uint64_t bits[2] = {1ull << lane, 1ull << (lane + 32)};
+    int up[2] = {r.parent[lane], r.parent[lane + 32]};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) r.anc[lane + 32 * k] = bits[k];
     __syncwarp();
+#pragma unroll 1
+    while (__any_sync(0xffffffffu, max(up[0], up[1]) >= 0)) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (up[k] >= 0) {
+          bits[k] |= r.anc[up[k]];
+          up[k] = r.parent[up[k]];
+        }
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        r.anc[lane + 32 * k] = bits[k];
+        r.parent[lane + 32 * k] = up[k];
+      }
+      __syncwarp();
+    }
   }
-  uint64_t anc[2];
-  int depth[2];
+  const int row0 = rb * p.rows_per_unit;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const int j = lane + 32 * k, rr = rb * p.rows_per_unit + j;
-    const int nl = kp.by_group(min(rr, p.rows_total - 1));
-    if (j < nc) r.place[j] = nl * p.hq + rr - nl * p.G;
-    anc[k] = p.tree ? r.anc[p.N - p.Nq + nl] : 0;
-    depth[k] = __popcll(anc[k]);
+    const int j = lane + 32 * k, nl = kp.by_group(min(row0 + j, p.rows_total - 1));
+    if (j < nc) r.place[j] = nl * p.hq + row0 + j - nl * p.G;
   }
   if (p.tree) {
-#pragma unroll 4
-    for (int m = 0; m < p.N; ++m) {
-      const uint32_t lo = __ballot_sync(0xffffffffu, (anc[0] >> m) & 1), hi = __ballot_sync(0xffffffffu, (anc[1] >> m) & 1);
-      if (lane == 0) r.line[m] = lo | static_cast<uint64_t>(hi) << 32;
-    }
+    // The query nodes one after another, whose rows are neighbours: lane m has the rows of nodes m, m + 32, and of depths.
+    uint64_t line[2] = {0ull, 0ull}, upto[2] = {0ull, 0ull};
+    const int last = kp.by_group(min(row0 + 63, p.rows_total - 1));
 #pragma unroll 1
-    for (int x = 0; p.window > 0 && x <= p.N; ++x) {
-      const uint32_t lo = __ballot_sync(0xffffffffu, depth[0] <= x), hi = __ballot_sync(0xffffffffu, depth[1] <= x);
-      if (lane == 0) r.upto[x] = lo | static_cast<uint64_t>(hi) << 32;
+    for (int nl = kp.by_group(row0); nl <= last; ++nl) {
+      const uint64_t anc = r.anc[p.N - p.Nq + nl];
+      const int a = max(nl * p.G - row0, 0), b = min(nl * p.G + p.G - row0, 64);
+      const uint64_t rows = ~0ull >> (64 - b + a) << a;
+      if ((static_cast<uint32_t>(anc) >> lane) & 1) line[0] |= rows;
+      if ((static_cast<uint32_t>(anc >> 32) >> lane) & 1) line[1] |= rows;
+      const int depth = __popcll(anc);
+      if (depth <= lane) upto[0] |= rows;
+      if (depth <= lane + 32) upto[1] |= rows;
     }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      r.line[lane + 32 * k] = line[k];
+      r.upto[lane + 32 * k] = upto[k];
+    }
+    if (lane == 0) r.upto[kMaxTreeNodes] = ~0ull;
   }
   __syncwarp();
 }
