@@ -74,14 +74,14 @@ struct Smem : Ring {
 constexpr int kBarriers = 18 + kRowSets;  // besides the ring's (an even number: what follows is aligned to 16 bytes)
 
 template <class CF>
-__host__ __device__ constexpr size_t smem_bytes(int C) {
+__host__ __device__ constexpr size_t smem_bytes() {
   return 1024 + 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize +
-         sizeof(TileMeta) * (kMetas + 1) + sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + kRowSets * sizeof(Rows) +
-         sizeof(int) * (3 * 64 + CF::kGroups * 4 * 64 + 8) + sizeof(int) * (2 * C + 1);
+         sizeof(TileMeta) * kMetas + kFirstBytes + sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + kRowSets * sizeof(Rows) +
+         sizeof(int) * (3 * 64 + CF::kGroups * 4 * 64 + 8);
 }
 
 template <class CF>
-__device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
+__device__ __forceinline__ Smem carve(uint8_t* raw) {
   Smem s;
   uint8_t* b = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   s.v = smem_addr(b);
@@ -91,7 +91,7 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   b += 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize;
   s.meta = smem_addr(b);
   s.first = s.meta + kMetas * sizeof(TileMeta);
-  b += sizeof(TileMeta) * (kMetas + 1);
+  b += sizeof(TileMeta) * kMetas + kFirstBytes;
   s.cfull = smem_addr(b);
   s.cempty = s.cfull + 8 * CF::kStages;
   s.kfull = s.cempty + 8 * CF::kStages;
@@ -113,8 +113,6 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   s.codes = s.wmax + CF::kGroups * 4 * 64;
   s.tmem = reinterpret_cast<uint32_t*>(s.codes + 4);
   s.issued = s.codes + 6;
-  s.len = s.codes + 8;
-  s.base = s.len + C;
   return s;
 }
 
@@ -662,12 +660,15 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
   }
 }
 
+// (With 28 warps a thread has 72 registers, and the plan inline would spill; the call costs 0.5 us, the spills 4.)
+__device__ __noinline__ void plan_loader_apart(const Kv4Params& kp, const Ring& sm) { plan_loader(kp, sm); }
+
 template <class CF>
 __global__ void __launch_bounds__(CF::kThreads, 1) attn_kv4_kernel(const __grid_constant__ Kv4Params kp) {
   extern __shared__ uint8_t smem_raw[];
   const AttnParams& p = kp.a;
   if (threadIdx.x == 0) allow_dependent_launch();  // the merge may be scheduled as CTAs finish
-  const Smem sm = carve<CF>(smem_raw, p.C);
+  const Smem sm = carve<CF>(smem_raw);
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) init_waits(p);
   static_assert(2 * CF::kStages + kBarriers <= 32, "a lane for each barrier");
@@ -680,13 +681,15 @@ __global__ void __launch_bounds__(CF::kThreads, 1) attn_kv4_kernel(const __grid_
   }
   if (warp == CF::kWarpQ && (threadIdx.x & 31) < kMetas)  // (what an earlier CTA left there is of no tile)
     sts128(sm.meta + (threadIdx.x & 31) * sizeof(TileMeta), make_uint4(~0u, 0u, 0u, 0u));
-  LoaderStart start;
-  if (warp == CF::kWarpLoad) start = plan_loader(kp, sm);
+  if (warp == CF::kWarpLoad) {
+    if constexpr (CF::kThreads > 24 * 32) plan_loader_apart(kp, sm);
+    else plan_loader(kp, sm);
+  }
   __syncthreads();
   const Waiter wait{p.wait_ns < kPollBelowNs};
   uint32_t tmem = 0;
   if (warp == CF::kWarpLoad) {
-    run_loader<CF::kStages, 2>(kp, sm, start, wait);  // (a last word for each warpgroup)
+    run_loader<CF::kStages, 2>(kp, sm, wait);  // (a last word for each warpgroup)
   } else if (warp == CF::kWarpQ) {
     run_q<CF>(kp, sm, wait);
   } else {
@@ -727,8 +730,8 @@ int rows_of_unit(int rows) {
 
 template <class CF>
 cudaError_t launch_cfg(const Kv4Params& kp, bool pdl, cudaStream_t stream) {
-  static_assert(smem_bytes<CF>(kMaxCaches) <= 227 * 1024, "shared memory at the largest number of caches");
-  const size_t smem = smem_bytes<CF>(kp.a.C);
+  constexpr size_t smem = smem_bytes<CF>();
+  static_assert(smem <= 227 * 1024, "shared memory");
   const cudaError_t e =
       cudaFuncSetAttribute(attn_kv4_kernel<CF>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
@@ -782,7 +785,7 @@ kvshot_status make_kv4_plan(const kvshot_attn_desc* d, int32_t window, int32_t s
   if (grid == 0) {
     const int sms = sm_count();
     int per_sm = 1;
-    if (pl->rows_per_unit <= 16 && attn_kv4_mma_occupancy(pl->rows_per_unit, d->num_caches, &per_sm) != cudaSuccess)
+    if (pl->rows_per_unit <= 16 && attn_kv4_mma_occupancy(pl->rows_per_unit, &per_sm) != cudaSuccess)
       return KVSHOT_ERR_CUDA;
     if (sms < 1 || per_sm < 1) return KVSHOT_ERR_CUDA;
     grid = std::min<int64_t>(sms * per_sm, std::max((max_tiles + kMinTiles - 1) / kMinTiles, units));
@@ -867,6 +870,7 @@ extern "C" kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* d, const 
   const double scale = d->scale != 0.f ? static_cast<double>(d->scale) : 1.0 / std::sqrt(static_cast<double>(kHeadDim));
   p.qscale = static_cast<float>(scale * 1.4426950408889634);
   p.num_ctas = pl.num_ctas;
+  p.unit_ctas = d->num_caches == 1 ? pl.num_ctas / pl.units : 0;  // (one cache: its units are cut by themselves)
   p.unit_ctas = d->num_caches == 1 ? pl.num_ctas / pl.units : 0;
   p.wait_ns = d->wait_limit_ns != 0 ? d->wait_limit_ns : 2000000000u;
   p.k_scale = std::ldexp(1.f, d->k_scale_exp);

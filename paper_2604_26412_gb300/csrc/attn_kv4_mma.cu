@@ -46,13 +46,13 @@ struct Smem : Ring {
 };
 
 template <class CF>
-__host__ __device__ constexpr size_t smem_bytes(int C) {
+__host__ __device__ constexpr size_t smem_bytes() {
   return 128 + CF::kStages * kStageSize + kQChunk<CF::kNR> * 4 + sizeof(float) * kWarps * CF::kRows * (kCombStride + 2) +
-         sizeof(TileMeta) * (kMetas + 1) + sizeof(Rows) + sizeof(uint64_t) * (2 * CF::kStages + 2) + sizeof(int) * (4 + 2 * C + 1);
+         sizeof(TileMeta) * kMetas + kFirstBytes + sizeof(Rows) + sizeof(uint64_t) * (2 * CF::kStages + 2) + sizeof(int) * 4;
 }
 
 template <class CF>
-__device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
+__device__ __forceinline__ Smem carve(uint8_t* raw) {
   Smem s;
   uint8_t* b = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~uintptr_t(127));
   s.ring = smem_addr(b);
@@ -63,15 +63,13 @@ __device__ __forceinline__ Smem carve(uint8_t* raw, int C) {
   TileMeta* meta = reinterpret_cast<TileMeta*>(s.sum + kWarps * CF::kRows);
   s.meta = smem_addr(meta);
   s.first = smem_addr(meta + kMetas);
-  uint64_t* m = reinterpret_cast<uint64_t*>(meta + kMetas + 1);
+  uint64_t* m = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(meta + kMetas) + kFirstBytes);
   s.cfull = smem_addr(m);
   s.cempty = s.cfull + 8 * CF::kStages;
   s.joined = s.cempty + 8 * CF::kStages;
   s.rows = reinterpret_cast<Rows*>(m + 2 * CF::kStages + 2);
   int* words = reinterpret_cast<int*>(s.rows + 1);
   s.issued = words;
-  s.len = words + 4;
-  s.base = s.len + C;
   return s;
 }
 
@@ -456,7 +454,7 @@ template <class CF>
 __global__ void __launch_bounds__(kThreads, CF::kMinBlocks) attn_kv4_mma_kernel(const __grid_constant__ Kv4Params kp) {
   extern __shared__ uint8_t smem_raw[];
   const AttnParams& p = kp.a;
-  const Smem sm = carve<CF>(smem_raw, p.C);
+  const Smem sm = carve<CF>(smem_raw);
   if (threadIdx.x == 0) {
     allow_dependent_launch();  // the merge may be scheduled as CTAs finish
 #pragma unroll 1
@@ -469,11 +467,10 @@ __global__ void __launch_bounds__(kThreads, CF::kMinBlocks) attn_kv4_mma_kernel(
     fence_mbar_init();
   }
   const bool loads = threadIdx.x >= 32 * kWarps;
-  LoaderStart start;
-  if (loads) start = plan_loader(kp, sm);
+  if (loads) plan_loader(kp, sm);
   __syncthreads();
   const Waiter wait{p.wait_ns < kPollBelowNs};
-  if (loads) run_loader<CF::kStages, 1>(kp, sm, start, wait);
+  if (loads) run_loader<CF::kStages, 1>(kp, sm, wait);
   else run_consumer<CF>(kp, sm, wait);
   __syncthreads();
   if (threadIdx.x == 0) drain<CF::kStages>(p, sm);
@@ -482,36 +479,29 @@ __global__ void __launch_bounds__(kThreads, CF::kMinBlocks) attn_kv4_mma_kernel(
 using Cfg8 = Cfg<1, 2, 3>;
 using Cfg16 = Cfg<2, 2, 2>;
 
-// Every plan that kMaxCaches allows fits an SM.
-static_assert(smem_bytes<Cfg8>(kMaxCaches) <= 227 * 1024 && smem_bytes<Cfg16>(kMaxCaches) <= 227 * 1024,
-              "shared memory at the largest number of caches");
-
 template <class CF>
-cudaError_t set_smem(int C, size_t* smem) {
-  *smem = smem_bytes<CF>(C);
-  return cudaFuncSetAttribute(attn_kv4_mma_kernel<CF>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(*smem));
+cudaError_t set_smem() {
+  return cudaFuncSetAttribute(attn_kv4_mma_kernel<CF>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<CF>()));
 }
 
 template <class CF>
-cudaError_t occupancy_cfg(int C, int* ctas) {
-  size_t smem;
-  const cudaError_t e = set_smem<CF>(C, &smem);
+cudaError_t occupancy_cfg(int* ctas) {
+  const cudaError_t e = set_smem<CF>();
   if (e != cudaSuccess) return e;
-  return cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas, attn_kv4_mma_kernel<CF>, kThreads, smem);
+  return cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas, attn_kv4_mma_kernel<CF>, kThreads, smem_bytes<CF>());
 }
 
 template <class CF>
 cudaError_t launch_cfg(const Kv4Params& kp, bool pdl, cudaStream_t stream) {
-  size_t smem;
-  const cudaError_t e = set_smem<CF>(kp.a.C, &smem);
+  const cudaError_t e = set_smem<CF>();
   if (e != cudaSuccess) return e;
-  return launch_maybe_pdl(attn_kv4_mma_kernel<CF>, dim3(kp.a.num_ctas), dim3(kThreads), smem, pdl, stream, kp);
+  return launch_maybe_pdl(attn_kv4_mma_kernel<CF>, dim3(kp.a.num_ctas), dim3(kThreads), smem_bytes<CF>(), pdl, stream, kp);
 }
 
 }  // namespace
 
-cudaError_t attn_kv4_mma_occupancy(int rows_per_unit, int C, int* ctas_per_sm) {
-  return rows_per_unit == 8 ? occupancy_cfg<Cfg8>(C, ctas_per_sm) : occupancy_cfg<Cfg16>(C, ctas_per_sm);
+cudaError_t attn_kv4_mma_occupancy(int rows_per_unit, int* ctas_per_sm) {
+  return rows_per_unit == 8 ? occupancy_cfg<Cfg8>(ctas_per_sm) : occupancy_cfg<Cfg16>(ctas_per_sm);
 }
 
 cudaError_t launch_attn_kv4_mma(const Kv4Params& p, bool pdl, cudaStream_t stream) {

@@ -17,7 +17,7 @@ struct Kv4Params {
 };
 
 // attn_kv4_mma.cu: stacks of up to 16 query rows per KV head.
-cudaError_t attn_kv4_mma_occupancy(int rows_per_unit, int C, int* ctas_per_sm);
+cudaError_t attn_kv4_mma_occupancy(int rows_per_unit, int* ctas_per_sm);
 cudaError_t launch_attn_kv4_mma(const Kv4Params& p, bool pdl, cudaStream_t stream);
 
 namespace {  // internal linkage: every translation unit gets its own copy
@@ -62,7 +62,6 @@ struct Ring {
   uint32_t meta;    // [kMetas] TileMeta
   uint32_t first;   // TileMeta of the CTA's first piece, whose q and rows need not wait for a tile (flags 0: there is none)
   int* issued;      // tiles issued by the loader
-  int *len, *base;  // the loader's plan
 };
 // The query rows of a unit: their places in a cache's q and out, and, of a draft tree, who sees what, as bits of rows.
 struct alignas(16) Rows {
@@ -120,6 +119,7 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                : "memory");
 }
+__device__ __forceinline__ void sts32(uint32_t addr, int v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ int lds32(uint32_t addr) {
   int v;
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
@@ -151,89 +151,84 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-// Tiles per cache and their sums (sm.len, sm.base), by one warp.
-__device__ __forceinline__ void build_kv4_plan(const AttnParams& p, int HR, int* s_len, int* s_base) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll 1
-  for (int c = lane; c < p.C; c += 32) {
-    const int L = clamp_len(p, c);
-    s_len[c] = L;
-    s_base[c + 1] = (window_span<kTile>(p, L).tiles + p.draft_tiles) * HR;
-  }
-  __syncwarp();
-  const int per = (p.C + 31) / 32, c0 = min(p.C, lane * per), c1 = min(p.C, c0 + per);
-  int v = 0;
-#pragma unroll 1
-  for (int c = c0; c < c1; ++c) v += s_base[c + 1];
-  int below = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int t = __shfl_up_sync(0xffffffffu, below, o);
-    if (lane >= o) below += t;
-  }
-  below -= v;
-#pragma unroll 1
-  for (int c = c0; c < c1; ++c) {
-    below += s_base[c + 1];
-    s_base[c + 1] = below;
-  }
-  if (lane == 0) s_base[0] = 0;
-  __syncwarp();
-}
-
-// A CTA's range of tiles [t, t_end), which begins in cache c, KV head x row block hr, tile lt of the unit.
+// A CTA's range of tiles [t, t_end), which begins in cache c (of length L), KV head x row block hr, tile lt of the unit.
 struct LoaderStart {
-  int t, t_end, c, hr, lt;
+  int t, t_end, c, L, hr, lt;
 };
-// By the loading warp, before the barrier that the roles begin with.
-__device__ __forceinline__ LoaderStart plan_loader(const Kv4Params& kp, const Ring& sm) {
+constexpr int kFirstBytes = sizeof(TileMeta) + 16;
+// By the loading warp, before the barrier that the roles begin with; left at sm.first: the first piece's words, with t,
+// t_end and L in place of a tile's, then hr and lt.
+__device__ __forceinline__ void plan_loader(const Kv4Params& kp, const Ring& sm) {
   const AttnParams& p = kp.a;
   const int lane = threadIdx.x & 31, HR = p.hkv * p.row_blocks;
-  int t = 0, t_end, c = 0, hr = 0, lt = 0;
+  auto unit_tiles = [&](int L) { return window_span<kTile>(p, L).tiles + p.draft_tiles; };
+  LoaderStart r{0, 0, 0, 0, 0, 0};
   if (p.unit_ctas > 0) {
-    if (lane == 0) sm.len[0] = clamp_len(p, 0);
-    __syncwarp();
-    const int ut = window_span<kTile>(p, sm.len[0]).tiles + p.draft_tiles;
+    r.L = clamp_len(p, 0);
+    const int ut = unit_tiles(r.L);
     const UnitCut u = unit_cut(p.unit_ctas, ut);
-    hr = blockIdx.x / u.per;
-    lt = (blockIdx.x - hr * u.per) * u.tpc;
-    t_end = hr < HR ? min(u.tpc, ut - lt) : 0;
+    r.hr = blockIdx.x / u.per;
+    r.lt = (blockIdx.x - r.hr * u.per) * u.tpc;
+    r.t_end = r.hr < HR ? min(u.tpc, ut - r.lt) : 0;
   } else {
-    build_kv4_plan(p, HR, sm.len, sm.base);
-    const int total = sm.base[p.C], tpc = tiles_per_cta(total, p.num_ctas);
-    t = min(total, static_cast<int>(blockIdx.x) * tpc);
-    t_end = min(total, t + tpc);
-    if (t < t_end) {
-      int hi = p.C - 1;  // last cache whose first tile is <= t
-#pragma unroll 1
-      while (c < hi) {
-        const int mid = (c + hi + 1) >> 1;
-        if (sm.base[mid] <= t) c = mid;
-        else hi = mid - 1;
+    // A lane's cache of 32 from c0 on: its length, and the tiles up to and including it.
+    int L = 0, upto = 0;
+    auto sum = [&](int c0) {
+      const int c = c0 + lane;
+      L = c < p.C ? clamp_len(p, c) : 0;
+      upto = c < p.C ? unit_tiles(L) * HR : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
       }
-      const int rem = t - sm.base[c], ut = window_span<kTile>(p, sm.len[c]).tiles + p.draft_tiles;
-      hr = rem / ut;
-      lt = rem - hr * ut;
+    };
+    int total = 0;
+#pragma unroll 1
+    for (int c0 = 0; c0 < p.C; c0 += 32) {
+      sum(c0);
+      total += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    const int tpc = tiles_per_cta(total, p.num_ctas);
+    r.t = min(total, static_cast<int>(blockIdx.x) * tpc);
+    r.t_end = min(total, r.t + tpc);
+    int below = 0, c0 = 0;
+#pragma unroll 1
+    for (; r.t < r.t_end; c0 += 32) {
+      if (p.C > 32) sum(c0);
+      const int all = __shfl_sync(0xffffffffu, upto, 31);
+      if (r.t < below + all) break;
+      below += all;
+    }
+    if (r.t < r.t_end) {
+      const int i = __popc(__ballot_sync(0xffffffffu, below + upto <= r.t));  // caches of these that end before it
+      r.c = c0 + i;
+      r.L = __shfl_sync(0xffffffffu, L, i);
+      const int before = __shfl_sync(0xffffffffu, upto, max(i - 1, 0));
+      const int rem = r.t - below - (i > 0 ? before : 0), ut = unit_tiles(r.L);
+      r.hr = rem / ut;
+      r.lt = rem - r.hr * ut;
     }
   }
   if (lane == 0) {
-    const int h = kp.by_blocks(hr);
+    const int h = kp.by_blocks(r.hr);
     *sm.issued = 0;
-    sts128(sm.first, make_uint4(t < t_end ? kFirst | kNewRows | (p.tree ? kNewTree : 0) : 0, 0, 0, 0));
-    sts128(sm.first + 16, make_uint4(c, h, hr - h * p.row_blocks, kp.by_seq(c)));
+    sts128(sm.first, make_uint4(r.t < r.t_end ? kFirst | kNewRows | (p.tree ? kNewTree : 0) : 0, r.t, r.t_end, r.L));
+    sts128(sm.first + 16, make_uint4(r.c, h, r.hr - h * p.row_blocks, kp.by_seq(r.c)));
+    sts128(sm.first + 32, make_uint4(r.hr, r.lt, 0, 0));
   }
-  return LoaderStart{t, t_end, c, hr, lt};
 }
 
 // The loading warp: the CTA's tiles, one after another, each a stage of the ring with a copy per run of groups (a draft
 // tile: two per row); at the end `kStops` tiles that say so.
 template <int kStages, int kStops>
-__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring, const LoaderStart& start, const Waiter& wait) {
+__device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring, const Waiter& wait) {
   const AttnParams& p = kp.a;
   const Ring sm = ring;
   const int lane = threadIdx.x & 31, HR = p.hkv * p.row_blocks;
-  const int t_end = start.t_end;
-  int t = start.t, c = start.c, hr = start.hr, lt = start.lt;
+  const TileMeta first = tile_meta_at(sm.first);
+  const int t_end = first.nkeys;
+  int t = first.key0, c = first.c, hr = lds32(sm.first + 32), lt = lds32(sm.first + 36);
   int stage = 0, issued = 0, last_rb = -1, last_seq = -1;
   uint32_t phase = 0;
   bool waited = false, ok = true;
@@ -243,7 +238,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
   const int my_tile = lane / runs, my_g0 = (lane % runs) * kp.run_groups;
 #pragma unroll 1
   for (; ok && t < t_end; lt = 0) {  // a piece
-    const int L = sm.len[c];
+    const int L = lds32(sm.first + 12);
     const WindowSpan span = window_span<kTile>(p, L);
     const int ut = span.tiles + p.draft_tiles, lt1 = min(ut, lt + t_end - t);
     const int h = kp.by_blocks(hr), rb = hr - h * p.row_blocks, seq = kp.by_seq(c);
@@ -318,6 +313,12 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
     if (++hr == HR) {  // (a piece that ends before its unit is the CTA's last)
       hr = 0;
       ++c;
+      if (t < t_end) {
+        const int next = clamp_len(p, c);
+        __syncwarp();
+        if (lane == 0) sts32(sm.first + 12, next);
+        __syncwarp();
+      }
     }
   }
 #pragma unroll 1
