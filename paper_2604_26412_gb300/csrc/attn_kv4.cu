@@ -131,7 +131,7 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
     // The first piece's (t = -1) before its first tile has landed, the others' with theirs.
     TileMeta w = tile_meta_at(sm.first);
     if (t >= 0) {
-      if (!__all_sync(0xffffffffu, wait(sm.cfull + 8 * stage, phase))) return;
+      if (!wait(sm.cfull + 8 * stage, phase)) return;
       w = tile_meta(sm, t);
       if (lane == 0) mbar_arrive(sm.cempty + 8 * stage);
       if (++stage == CF::kStages) {
@@ -142,7 +142,7 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
     }
     if (!(w.flags & kFirst) || t == 0) continue;
     const int b = piece & 1;
-    if (!__all_sync(0xffffffffu, wait(sm.qempty + 8 * b, ((piece >> 1) & 1) ^ 1u))) return;
+    if (!wait(sm.qempty + 8 * b, ((piece >> 1) & 1) ^ 1u)) return;
     const __nv_bfloat16* q = p.q + (static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G) * kHeadDim;
     const int row0 = w.rb * p.rows_per_unit, rows = min(p.rows_per_unit, p.rows_total - row0);
     // 16 bytes of two rows at a time per warp; eight loads of a lane on their way together.
@@ -240,14 +240,12 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
   for (int t = wg;; t += 2) {
     // The tile's bytes; K's buffer: QK^T of its previous tile is done.
     uint32_t flags = tile_flags(sm, t);
-    bool ok = wait(sm.cfull + 8 * stage, phase);
-    ok = ok && wait(qkdone, freed);
-    if (!__all_sync(0xffffffffu, ok)) return;
+    if (!wait(sm.cfull + 8 * stage, phase, qkdone, freed)) return;
     tc_fence_after();
     if (!is_of(flags)) flags = tile_flags(sm, t);
     if (flags & kStop) {
       // (P.V of the tile before has to have seen its V, whose phase this one ends.)
-      if (!__all_sync(0xffffffffu, wait(pvdone, freed))) return;
+      if (!wait(pvdone, freed)) return;
       if (lane == 0) {
         mbar_arrive(kfull);
         mbar_arrive(vfull);
@@ -274,7 +272,7 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
     __syncwarp();
     if (lane == 0) mbar_arrive(kfull);
     // V's buffer: P.V of its previous tile is done.
-    if (!__all_sync(0xffffffffu, wait(pvdone, freed))) return;
+    if (!wait(pvdone, freed)) return;
     if (!draft) {
       uint2 sc = lds64(src + scale0 + kScaleBytes);
       if (flags & kMasked) {
@@ -325,13 +323,11 @@ __device__ __forceinline__ void run_qk(const Smem& smem, const Waiter& wait, uin
   for (int t = 0, stops = 0; stops < 2; ++t) {
     const uint32_t b = t & 1, phase = (t >> 1) & 1;
     uint32_t flags = uniform(tile_flags(sm, t));
-    bool ok = wait(sm.pfull + 8 * b, phase ^ 1u);  // S of the tile before the last has been read
-    ok = ok && wait(sm.kfull + 8 * b, phase);
-    if (!__all_sync(0xffffffffu, ok)) break;
+    if (!wait(sm.pfull + 8 * b, phase ^ 1u, sm.kfull + 8 * b, phase)) break;  // (S of the tile before the last has been read)
     if (!is_of(flags)) flags = uniform(tile_flags(sm, t));
     if (flags & kFirst) {
       ++piece;
-      if (!__all_sync(0xffffffffu, wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1))) break;
+      if (!wait(sm.qfull + 8 * (piece & 1), (piece >> 1) & 1)) break;
     }
     if (flags & kStop) {
       ++stops;  // (its S is nothing, and the softmax sees that)
@@ -365,15 +361,14 @@ __device__ __forceinline__ void run_pv(const Smem& smem, const Waiter& wait, uin
   for (int t = 0;; ++t, ++in_piece) {
     const uint32_t b = t & 1, phase = (t >> 1) & 1;
     uint32_t flags = uniform(tile_flags(sm, t));
-    if (!__all_sync(0xffffffffu, wait(sm.vfull + 8 * b, phase))) break;
+    if (!wait(sm.vfull + 8 * b, phase)) break;
     if (!is_of(flags)) flags = uniform(tile_flags(sm, t));
     if (flags & kStop) break;
-    bool ok = wait(sm.pfull + 8 * b, phase);
+    if (!wait(sm.pfull + 8 * b, phase)) break;
     if (flags & kFirst) {
       in_piece = 0;
-      if (++piece > 0) ok = ok && wait(sm.ofree, (piece - 1) & 1);
+      if (++piece > 0 && !wait(sm.ofree, (piece - 1) & 1)) break;
     }
-    if (!__all_sync(0xffffffffu, ok)) break;
     tc_fence_after();
     const uint32_t o = tmem + CF::kTmemO;
     uint64_t v = v0 + b * (kVTile >> 4), x = p0 + b * (kPTile >> 4);
@@ -563,8 +558,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
       if (i < width) wmax[(key >> 5) * 64 + col + i] = __float_as_int(sums[i]);
     if (threadIdx.x == 0) *sm.codes = in_codes;
     // O is at rest: P.V of the piece's last tile is done.
-    const bool ok = wait(sm.pvdone + 8 * (t & 1), (t >> 1) & 1) && rows_built();
-    if (!__all_sync(0xffffffffu, ok) || !sync(wait)) return false;
+    if (!wait(sm.pvdone + 8 * (t & 1), (t >> 1) & 1) || !rows_built() || !sync(wait)) return false;
     if (threadIdx.x < CF::kNC) join_sums(p, smem, sm.rows[set].place, tile_meta(sm, t), threadIdx.x);
     if (!sync(wait)) return false;
     tc_fence_after();
@@ -582,18 +576,16 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     // the last is done.  (A warp whose wait gives up goes on to the vote: the warps of a
     // warpgroup leave there, together.)
     uint32_t flags = tile_flags(sm, t);
-    bool ok = wait(sm.qkdone + 8 * b, phase);
-    ok = ok && wait(sm.pvdone + 8 * b, phase ^ 1u);
-    good = good && __all_sync(0xffffffffu, ok);
+    good = good && wait(sm.qkdone + 8 * b, phase, sm.pvdone + 8 * b, phase ^ 1u);
     if (!is_of(flags)) flags = tile_flags(sm, t);
     float qs = qs_prefix;
     uint64_t vis = ~0ull;
-    bool stop = false, leave_codes = false;
+    bool stop = false, leave_codes = false, odd = !good;
     if (flags != 0 && good) {  // (most tiles have none)
       stop = flags & kStop;
       if ((flags & kFirst) && !stop) begin(t);
       if ((flags & kMasked) && !stop) {
-        good = __all_sync(0xffffffffu, rows_built());
+        good = rows_built();
         if (good) vis = rows_seeing(kp, sm.rows[set], tile_words(sm, t), rb, key) >> col0;
       }
       if (flags & kDraft) {
@@ -601,6 +593,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
         leave_codes = in_codes && !fresh && p.v_scale != 1.f;
         in_codes = false;
       }
+      odd = !good || fresh || leave_codes || stop;
     }
     tc_fence_after();
     const uint32_t scores = trow + CF::kTmemS + b * CF::kNC + col0;
@@ -615,7 +608,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
         x[j / 2] = fma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), make_float2(qs, qs), make_float2(m.x, m.y));
         x[j / 2 + 1] = fma2(make_float2(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), make_float2(qs, qs), make_float2(m.z, m.w));
       }
-      if (vis != ~0ull) {
+      if (flags & kMasked) {
 #pragma unroll
         for (int j = 0; j < NC; j += 2) {
           if (!((vis >> j) & 1ull)) x[j / 2].x = -INFINITY;
@@ -626,7 +619,7 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
       float top = kRefLimit;
 #pragma unroll
       for (int j = 0; j < NC / 2; ++j) top = max3(top, x[j].x, x[j].y);
-      if (!any_of(bar, kGroupThreads, top > kRefLimit || leave_codes || fresh || !good || stop)) break;
+      if (!any_of(bar, kGroupThreads, top > kRefLimit || odd)) break;
       if (any_of(bar, kGroupThreads, !good) || stop) return;
       move_references(wmax, ref, alpha, wg, NC, scores, qs, vis, fresh);  // always with a warpgroup's first keys of a piece
 #pragma unroll
@@ -655,8 +648,10 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(sm.pfull + 8 * b);
-    fresh = false;
-    if (flags & kLast) good = end(t);
+    if (flags != 0) {
+      fresh = false;
+      if (flags & kLast) good = end(t);
+    }
   }
 }
 
@@ -686,7 +681,7 @@ __global__ void __launch_bounds__(CF::kThreads, 1) attn_kv4_kernel(const __grid_
     else plan_loader(kp, sm);
   }
   __syncthreads();
-  const Waiter wait{p.wait_ns < kPollBelowNs};
+  const Waiter wait(p);
   uint32_t tmem = 0;
   if (warp == CF::kWarpLoad) {
     run_loader<CF::kStages, 2>(kp, sm, wait);  // (a last word for each warpgroup)

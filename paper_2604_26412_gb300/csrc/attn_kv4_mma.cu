@@ -247,7 +247,7 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
     // The first piece begins (t = -1) before its first tile has landed, the others with theirs.
     int4 meta = make_int4(kFirst, 0, 0, 0);  // flags, key0, nkeys, L
     if (t >= 0) {
-      if (!__all_sync(0xffffffffu, wait(sm.cfull + 8 * stage, phase))) return;
+      if (!wait(sm.cfull + 8 * stage, phase)) return;
       meta = tile_words(sm, t);
       if (meta.x & kStop) return;
     }
@@ -469,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, CF::kMinBlocks) attn_kv4_mma_kernel(
   const bool loads = threadIdx.x >= 32 * kWarps;
   if (loads) plan_loader(kp, sm);
   __syncthreads();
-  const Waiter wait{p.wait_ns < kPollBelowNs};
+  const Waiter wait(p);
   if (loads) run_loader<CF::kStages, 1>(kp, sm, wait);
   else run_consumer<CF>(kp, sm, wait);
   __syncthreads();

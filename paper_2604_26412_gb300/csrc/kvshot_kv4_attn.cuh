@@ -73,31 +73,16 @@ struct alignas(16) Rows {
 };
 
 // Every wait ends: when its phase completes, when another role has given up, or (which gives up) after the call's limit.
-// The inline part is one try, which blocks for a while; what the rest needs lies in shared memory, so that the many places
-// that wait are short.
+// A warp waits as one.  The inline part is one try of all lanes, which blocks for a while; what the rest needs lies in
+// shared memory, so that the many places that wait are short.
 struct WaitLimits {
   int32_t* err;
   uint64_t limit_ns;
   int abort;  // a wait has given up
-  int poll;   // a limit that a blocking try could sit out
 };
 __device__ __forceinline__ WaitLimits* wait_limits() {
   __shared__ WaitLimits s_limits;
   return &s_limits;
-}
-__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity) {
-  volatile WaitLimits* w = wait_limits();
-  const uint64_t t0 = global_timer_ns(), limit = w->limit_ns;
-  for (;;) {
-#pragma unroll 1
-    for (int i = 0; i < 16; ++i)
-      if (w->poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
-    if (w->abort) return false;
-    if (global_timer_ns() - t0 > limit) break;
-  }
-  set_error(w->err, KVSHOT_ERR_TIMEOUT);
-  w->abort = 1;
-  return false;
 }
 // One thread, before the first wait and a barrier.
 __device__ __forceinline__ void init_waits(const AttnParams& p) {
@@ -105,13 +90,42 @@ __device__ __forceinline__ void init_waits(const AttnParams& p) {
   w->err = p.err;
   w->limit_ns = p.wait_ns;
   w->abort = 0;
-  w->poll = p.wait_ns < kPollBelowNs;
+}
+// Blocks for up to `hint_ns`.
+__device__ __forceinline__ bool try_wait_for(uint32_t bar, uint32_t parity, uint32_t hint_ns) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(done)
+      : "r"(bar), "r"(parity), "r"(hint_ns)
+      : "memory");
+  return done != 0;
+}
+__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, uint32_t hint_ns) {
+  volatile WaitLimits* w = wait_limits();
+  const uint64_t t0 = global_timer_ns(), limit = w->limit_ns;
+  for (;;) {
+    if (__all_sync(0xffffffffu, try_wait_for(bar, parity, hint_ns))) return true;
+    if (__any_sync(0xffffffffu, w->abort)) return false;
+    if (__any_sync(0xffffffffu, global_timer_ns() - t0 > limit)) break;
+  }
+  if ((threadIdx.x & 31) == 0) {
+    set_error(w->err, KVSHOT_ERR_TIMEOUT);
+    w->abort = 1;
+  }
+  return false;
 }
 struct Waiter {
-  bool poll;
+  uint32_t hint_ns;  // of a try (a limit must not be sat out in one)
+  __device__ __forceinline__ explicit Waiter(const AttnParams& p) : hint_ns(min(p.wait_ns, 20000u)) {}
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
-    if (!poll && mbar_try_wait(bar, parity)) return true;
-    return wait_slow(bar, parity);
+    return __all_sync(0xffffffffu, try_wait_for(bar, parity, hint_ns)) || wait_slow(bar, parity, hint_ns);
+  }
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, uint32_t bar2, uint32_t parity2) const {
+    const bool one = try_wait_for(bar, parity, hint_ns), two = try_wait_for(bar2, parity2, hint_ns);
+    return __all_sync(0xffffffffu, one && two) || (wait_slow(bar, parity, hint_ns) && wait_slow(bar2, parity2, hint_ns));
   }
 };
 
@@ -284,7 +298,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
         wait_for_prerequisite_grid();
         waited = true;
       }
-      ok = __all_sync(0xffffffffu, wait(sm.cempty + 8 * stage, phase ^ 1u));
+      ok = wait(sm.cempty + 8 * stage, phase ^ 1u);
       if (!ok) break;
       const uint32_t bar = sm.cfull + 8 * stage, dst = sm.ring + stage * kStageSize;
       if (lane == 0) {
@@ -323,7 +337,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
   }
 #pragma unroll 1
   for (int i = 0; ok && i < kStops; ++i) {
-    ok = __all_sync(0xffffffffu, wait(sm.cempty + 8 * stage, phase ^ 1u));
+    ok = wait(sm.cempty + 8 * stage, phase ^ 1u);
     if (!ok) break;
     if (lane == 0) {
       sts128(sm.meta + issued % kMetas * sizeof(TileMeta), make_uint4(kStop | issued << kTagShift, 0, 0, 0));
@@ -352,7 +366,7 @@ struct WarpSync {
   __device__ __forceinline__ bool operator()(const Waiter& wait) {
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
-    const bool ok = __all_sync(0xffffffffu, wait(bar, phase));
+    const bool ok = wait(bar, phase);
     phase ^= 1u;
     return ok;
   }
