@@ -64,10 +64,9 @@ struct Smem : Ring {
   uint32_t qfull, qempty;            // [2] q of a piece staged; its last QK^T done
   uint32_t ofree, mmadone;           // epilogue has read O; [2] every MMA issued is done
   uint32_t rfull;                    // [kRowSets] a piece's rows built
-  uint32_t joined;                   // barrier of the softmax warps
-  float *ref, *alpha, *inv;          // [64] per row (ref: negated)
-  int* wmax;                         // [softmax warp][64] per warp and row; sums at a piece's end
-  int* codes;                        // O is in units of the value codes
+  float *ref, *alpha;                // [64] per row (ref: negated)
+  float* sums;                       // [softmax warp][16] of a piece's rows
+  int* wmax;                         // [softmax warp][64] per warp and row
   uint32_t* tmem;
 };
 
@@ -77,7 +76,7 @@ template <class CF>
 __host__ __device__ constexpr size_t smem_bytes() {
   return 1024 + 2 * kVTile + 2 * kPTile + 2 * CF::kQTile + CF::kStages * kStageSize +
          sizeof(TileMeta) * kMetas + kFirstBytes + sizeof(uint64_t) * (2 * CF::kStages + kBarriers) + kRowSets * sizeof(Rows) +
-         sizeof(int) * (3 * 64 + CF::kGroups * 4 * 64 + 8);
+         sizeof(int) * (2 * 64 + 4 * CF::kNC + CF::kGroups * 4 * 64 + 4);
 }
 
 template <class CF>
@@ -103,16 +102,14 @@ __device__ __forceinline__ Smem carve(uint8_t* raw) {
   s.qempty = s.qfull + 16;
   s.mmadone = s.qempty + 16;
   s.ofree = s.mmadone + 16;
-  s.joined = s.ofree + 8;
-  s.rfull = s.joined + 8;
+  s.rfull = s.ofree + 16;
   s.rows = reinterpret_cast<Rows*>(b + 8 * (2 * CF::kStages + kBarriers));
   s.ref = reinterpret_cast<float*>(s.rows + kRowSets);
   s.alpha = s.ref + 64;
-  s.inv = s.alpha + 64;
-  s.wmax = reinterpret_cast<int*>(s.inv + 64);
-  s.codes = s.wmax + CF::kGroups * 4 * 64;
-  s.tmem = reinterpret_cast<uint32_t*>(s.codes + 4);
-  s.issued = s.codes + 6;
+  s.sums = s.alpha + 64;
+  s.wmax = reinterpret_cast<int*>(s.sums + 4 * CF::kNC);
+  s.tmem = reinterpret_cast<uint32_t*>(s.wmax + CF::kGroups * 4 * 64);
+  s.issued = reinterpret_cast<int*>(s.tmem + 2);
   return s;
 }
 
@@ -432,7 +429,7 @@ __device__ __forceinline__ int column_sums(float (&v)[N], int lane, int* column0
 // The references of rows whose scores have passed their limit move: refs (negated), and alpha with what O and the sums are to be
 // multiplied by.  The threads of warpgroup wg; n rows from the first of `scores`, `ref` and `alpha` on.
 __device__ __noinline__ void move_references(int* wmax, float* refs, float* alpha, int wg, int n, uint32_t scores, float qs,
-                                             uint64_t vis, bool fresh) {
+                                             uint32_t vis, bool fresh) {
   const int tid = threadIdx.x & 127, warp = tid >> 5;
 #pragma unroll 1
   for (int j = 0; j < n; j += 8) {
@@ -441,7 +438,7 @@ __device__ __noinline__ void move_references(int* wmax, float* refs, float* alph
     tmem_wait_ld();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float x = (vis >> (j + i)) & 1ull ? __uint_as_float(s[i]) * qs : -INFINITY;
+      const float x = (vis >> (j + i)) & 1u ? __uint_as_float(s[i]) * qs : -INFINITY;
       const int m = __reduce_max_sync(0xffffffffu, ordered(x));
       if ((tid & 31) == 0) wmax[warp * 64 + j + i] = m;
     }
@@ -470,45 +467,41 @@ __device__ __noinline__ void rescale_o(const float* alpha, int n, uint32_t o_col
   tmem_wait_st();
 }
 
-// A piece's rows [j0, j1) of this thread's dim: the final ones, or the piece's part in the workspace.
-__device__ __noinline__ void write_rows(const AttnParams& p, const Smem& sm, const int* place, const TileMeta& w, int j0, int j1,
-                                        uint32_t o_cols) {
-  const int tid = threadIdx.x & 127;
-  const size_t row0 = static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G;
-  const size_t part = static_cast<size_t>((w.c * p.hkv + w.h) * p.row_blocks + w.rb + blockIdx.x) * p.rows_per_unit;
+// A piece's rows row .. row + kCols - 1, a warpgroup's, of this thread's dim: the final ones, or the piece's part in the
+// workspace.  `sums`: [4][kCols] of the rows, by its warps; `refs`: negated.
+__device__ __noinline__ void write_rows(const AttnParams& p, const Rows& rows, const TileMeta& w, int row, const float* sums,
+                                        const float* refs, uint32_t o_cols, float units) {
+  const int tid = threadIdx.x & 127, lane = tid & 31, j = lane % kCols;
   const bool whole = w.flags & kWhole;
-  const int end = whole ? min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit) : j1;  // (a part has room for all rows)
+  const int end = whole ? min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit) : p.rows_per_unit;  // (a part has room for all)
+  const size_t row0 = static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G;
+  const size_t part = static_cast<size_t>((w.c * p.hkv + w.h) * p.row_blocks + w.rb + blockIdx.x) * p.rows_per_unit + row;
+  // Lane j: row + j.
+  const float sum = (sums[j] + sums[kCols + j]) + (sums[2 * kCols + j] + sums[3 * kCols + j]);
+  const float inv = sum == 0.f ? 0.f : __fdividef(units, sum);
+  const int place = rows.place[row + j];
+  if (tid < kCols && row + j < end) {
+    const float lse2 = sum == 0.f ? -INFINITY : __log2f(sum) - refs[j];
+    if (whole) p.lse[row0 + place] = lse2 * 0.69314718055994531f;
+    else p.ws_lse[part + j] = lse2;
+  }
   __nv_bfloat16* out = p.out + row0 * kHeadDim + tid;
-  float* ws = p.ws_o + (part + j0) * kHeadDim + tid;
-  const uint32_t inv = smem_addr(sm.inv), places = smem_addr(place);
+  float* ws = p.ws_o + part * kHeadDim + tid;
 #pragma unroll 1
-  for (int j = j0; j < j1; j += 4) {
+  for (int i0 = 0; i0 < kCols; i0 += 4) {
     uint32_t o[4];
-    tmem_ld4(o_cols + j, o);
-    const uint4 a = lds128(inv + 4 * j), at = lds128(places + 4 * j);
-    const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, to[4] = {at.x, at.y, at.z, at.w};
+    tmem_ld4(o_cols + i0, o);
     tmem_wait_ld();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float v = wa[i] != 0u ? __uint_as_float(o[i]) * __uint_as_float(wa[i]) : 0.f;
+      const float a = __shfl_sync(0xffffffffu, inv, i0 + i);
+      const int to = __shfl_sync(0xffffffffu, place, i0 + i);
+      const float v = a != 0.f ? __uint_as_float(o[i]) * a : 0.f;
       if (!whole) ws[i * kHeadDim] = v;
-      else if (j + i < end) out[static_cast<size_t>(to[i]) * kHeadDim] = __float2bfloat16(v);
+      else if (row + i0 + i < end) out[static_cast<size_t>(to) * kHeadDim] = __float2bfloat16(v);
     }
     ws += 4 * kHeadDim;
   }
-}
-
-// The rows' sums, weights and log-sum-exp.  Thread = row.
-__device__ __noinline__ void join_sums(const AttnParams& p, const Smem& sm, const int* place, const TileMeta& w, int j) {
-  const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
-  const int* x = sm.wmax + j / kCols * 256 + j % kCols;
-  const float sum = (__int_as_float(x[0]) + __int_as_float(x[64])) + (__int_as_float(x[128]) + __int_as_float(x[192]));
-  const float top = -sm.ref[j];
-  sm.inv[j] = sum == 0.f ? 0.f : __fdividef(*sm.codes ? p.v_scale : 1.f, sum);
-  if (j >= rows) return;
-  const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
-  if (w.flags & kWhole) p.lse[static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G + place[j]] = lse2 * 0.69314718055994531f;
-  else p.ws_lse[static_cast<size_t>((w.c * p.hkv + w.h) * p.row_blocks + w.rb + blockIdx.x) * p.rows_per_unit + j] = lse2;
 }
 
 template <class CF>
@@ -525,25 +518,22 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
   float* alpha = sm.alpha + col0;
   int* wmax = sm.wmax + 256 * wg;
   const int bar = kBarGroup + wg;
-  WarpSync sync{sm.joined, 0};
   float2 l[NC / 2];               // sums over this thread's keys
   bool in_codes = false;          // O is in units of the value codes
   wait_for_prerequisite_grid();   // outputs and scratch may be the preceding kernel's
   bool fresh = true;              // the piece has had no tile yet
   bool good = true;               // no wait of this warp has given up
   const float qs_prefix = p.qscale * p.k_scale;
-  int rb = 0, set = -1, piece = -1;  // the piece's row block, its set of rows and number
+  int set = -1, piece = -1;       // the piece's set of rows, and its number
   auto begin = [&](int t) {
-    const TileMeta w = tile_meta(sm, t);
-    rb = w.rb;
     ++piece;
-    if (w.flags & kNewRows) set = (set + 1) & (kRowSets - 1);
+    if (tile_words(sm, t).x & kNewRows) set = (set + 1) & (kRowSets - 1);
 #pragma unroll
     for (int j = 0; j < NC / 2; ++j) l[j] = make_float2(0.f, 0.f);
     in_codes = fresh = true;
   };
   auto rows_built = [&]() { return wait(sm.rfull + 8 * (piece & (kRowSets - 1)), (piece / kRowSets) & 1); };
-  // A piece's end, at its last tile t: join the warpgroups and write the rows.
+  // A piece's end, at its last tile t: a warpgroup has all of its rows.
   auto end = [&](int t) {
     int col = 0;
     float sums[NC];
@@ -553,16 +543,15 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
       sums[2 * j + 1] = l[j].y;
     }
     const int width = column_sums(sums, lane, &col);
+    float* all = sm.sums + wg * 4 * NC;  // (read until this warpgroup's next vote)
 #pragma unroll
     for (int i = 0; i < NC; ++i)
-      if (i < width) wmax[(key >> 5) * 64 + col + i] = __float_as_int(sums[i]);
-    if (threadIdx.x == 0) *sm.codes = in_codes;
+      if (i < width) all[(key >> 5) * NC + col + i] = sums[i];
     // O is at rest: P.V of the piece's last tile is done.
-    if (!wait(sm.pvdone + 8 * (t & 1), (t >> 1) & 1) || !rows_built() || !sync(wait)) return false;
-    if (threadIdx.x < CF::kNC) join_sums(p, smem, sm.rows[set].place, tile_meta(sm, t), threadIdx.x);
-    if (!sync(wait)) return false;
+    const bool ok = wait(sm.pvdone + 8 * (t & 1), (t >> 1) & 1) && rows_built();
+    if (any_of(bar, kGroupThreads, !ok)) return false;
     tc_fence_after();
-    write_rows(p, smem, sm.rows[set].place, tile_meta(sm, t), col0, col0 + NC, trow + CF::kTmemO);
+    write_rows(p, sm.rows[set], tile_meta(sm, t), col0, all, ref, o_cols, in_codes ? p.v_scale : 1.f);
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(sm.ofree);
@@ -579,14 +568,14 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     good = good && wait(sm.qkdone + 8 * b, phase, sm.pvdone + 8 * b, phase ^ 1u);
     if (!is_of(flags)) flags = tile_flags(sm, t);
     float qs = qs_prefix;
-    uint64_t vis = ~0ull;
+    uint32_t vis = ~0u;  // bits of this thread's rows that see the key
     bool stop = false, leave_codes = false, odd = !good;
     if (flags != 0 && good) {  // (most tiles have none)
       stop = flags & kStop;
       if ((flags & kFirst) && !stop) begin(t);
       if ((flags & kMasked) && !stop) {
         good = rows_built();
-        if (good) vis = rows_seeing(kp, sm.rows[set], tile_words(sm, t), rb, key) >> col0;
+        if (good) vis = static_cast<uint32_t>(rows_seeing(kp, sm.rows[set], tile_words(sm, t), tile_meta(sm, t).rb, key) >> col0);
       }
       if (flags & kDraft) {
         qs = p.qscale;
@@ -611,8 +600,8 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
       if (flags & kMasked) {
 #pragma unroll
         for (int j = 0; j < NC; j += 2) {
-          if (!((vis >> j) & 1ull)) x[j / 2].x = -INFINITY;
-          if (!((vis >> j) & 2ull)) x[j / 2].y = -INFINITY;
+          if (!((vis >> j) & 1u)) x[j / 2].x = -INFINITY;
+          if (!((vis >> j) & 2u)) x[j / 2].y = -INFINITY;
         }
       }
       if (moved) break;
