@@ -1,5 +1,6 @@
-// attn_kv4.cu -- draft attention over a 4-bit target cache, with an optional sliding window and sink tokens, on the
-// 5th-generation tensor cores (tcgen05).
+// attn_kv4.cu -- draft attention over a 4-bit target cache, with an optional sliding window and sink tokens: the call,
+// its plan, and the kernel for stacks of 17 query rows and more per KV head, on the 5th-generation tensor cores (tcgen05).
+// (Up to 16 rows: attn_kv4_mma.cu.)
 //
 // Per unit (cache, KV head, block of up to 64 stacked GQA rows), per tile of 128 keys, with keys as the MMA's M and the
 // query rows as its N, so that few rows waste nothing:
@@ -8,13 +9,28 @@
 //   O^T += V^T P^T M = 128 dims, N rows, K = 128 keys:  A = V (f16, shared memory, MN-major), B = P (shared memory)
 // The cache's bytes stream through a ring of tiles (one bulk copy per run of groups) and are decoded by warps of their
 // own: a thread takes one key's codes, two per conversion (e2m1 -> f16, times the block's scale: both exact), K into
-// tensor memory, V into shared memory.
-// Warp roles: 0..7 two softmax warpgroups (thread = key, then dim), 8..15 two decoding warpgroups (thread = key), 16
-// loads, 17 issues QK^T and owns tensor memory, 18 issues P.V, 19 stages q (f16).  A tile's buffers (K and S in tensor
-// memory, V and P in shared memory) are pair t % 2.  Decoding warpgroup w takes tiles t % 2 == w, K and then V.  Up to
-// 32 rows the softmax warpgroups share the tiles out alike, each with its own references, sums and accumulator O_w,
-// joined by log-sum-exp at a piece's end: a role then has two tiles' time for the latencies of one tile's steps, which
-// bound it.  More rows have the warpgroups take half of the rows each, of every tile.
+// tensor memory, V into shared memory.  P and q are rounded to f16 (11 bits: P in [2^-14, 2^15]), sums are fp32.
+// Warp roles: a softmax warpgroup per 16 rows (thread = key, then dim), two decoding warpgroups (thread = key; the tiles
+// t % 2 == w, K and then V), and a warp each that loads, issues QK^T and owns tensor memory, issues P.V, stages q.  A
+// tile's buffers (K and S in tensor memory, V and P in shared memory) are pair t % 2.
+//
+// What bounds it: instructions.  A tile takes ~5300 warp instructions at 48 rows (3100 of softmax, 1600 of decoding), at
+// 57% of the issue rate 0.85 us; its 18 KB are 0.41 us of the copy's bandwidth, its products 0.2 us.  Without the
+// conversions a tile takes 0.79 us, without the exponentials 0.83, with a quarter of the products 0.85.  Beside the tiles,
+// a call's 20 us are its start (5 us to the first scores), a piece's first tile, draft tiles and end (~6 us) and the merge.
+// What the layout rests on (16 sequences of 4096 tokens):
+//  - More softmax warps, not more rows to a thread: their steps wait for one another's latencies.  48 rows on two
+//    warpgroups 61.7 us, on three 59.6; 32 rows, two warpgroups on tiles in turn 52.2, on 16 rows each of every tile 48.5.
+//    Threads of 48 rows that take the scores twice (their registers hold the sums alone): 75 against 64.
+//  - Little code in the tiles' path: the roles share an instruction cache that they about fill, and code that runs once
+//    costs ~20 cycles an instruction.  So the plan is code of one warp, the other roles follow its words for each tile,
+//    decoding is rolled, rare steps are out of line (48 rows 118 -> 69 us on the way).
+//  - MMAs issued by an elected lane in uniform control flow: 10 cycles each, 45 by `if (lane == 0)`.
+//  - What a piece needs beside its tiles is made beside them: rows' tables after q (69 -> 64 us), the CTA's plan and first
+//    q before its first tile (64 -> 61.7), tables by jumps and whole nodes (59.6 -> 53.8), a warpgroup that ends its rows
+//    by itself (53.5 -> 49.8).
+// Measured, attention and merge: 48 rows 49.8 us, 256 rows 172 us (the tree's 64 nodes in four blocks, each of which
+// decodes the cache for itself).
 // Work plan: the units' tiles laid end to end and cut into equal ranges, one per persistent CTA (kvshot_internal.h);
 // with a window a unit's tiles are those of the sinks and those of the window.
 #include <algorithm>
@@ -46,7 +62,7 @@ struct Cfg {
   static constexpr int kGroups = NC / kCols;           // softmax warpgroups
   // Warps: the softmax warpgroups, two that decode, then the loading one, QK^T's, P.V's and q's.
   static constexpr int kWarpDecode = 4 * kGroups, kWarpLoad = kWarpDecode + 8, kWarpQk = kWarpLoad + 1,
-                       kWarpPv = kWarpLoad + 2, kWarpQ = kWarpLoad + 3, kThreads = 32 * (kWarpLoad + 4);
+                       kWarpQ = kWarpLoad + 3, kThreads = 32 * (kWarpLoad + 4);
   static constexpr int kStages = NC <= 32 ? 5 : 4;
   static constexpr int kQTile = NC * 256;
   static constexpr uint32_t kTmemK = 0, kTmemS = 128, kTmemO = 128 + 2 * NC;  // columns
@@ -188,7 +204,8 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
 __device__ __forceinline__ void put_v(uint32_t row, uint32_t sw, int c, const uint32_t* o) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    sts128(row + (c >> 1) * kVHalf + ((((c & 1) * 4 + i) << 4) ^ sw), make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+    sts128(row + (c >> 1) * kVHalf + ((((c & 1) * 4 + i) << 4) ^ sw),
+           make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
 }
 
 // A draft tile's key (bf16 row at `src`, zeros past the valid keys) into tensor memory (K) or the V tile.
@@ -473,7 +490,8 @@ __device__ __noinline__ void write_rows(const AttnParams& p, const Rows& rows, c
                                         const float* refs, uint32_t o_cols, float units) {
   const int tid = threadIdx.x & 127, lane = tid & 31, j = lane % kCols;
   const bool whole = w.flags & kWhole;
-  const int end = whole ? min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit) : p.rows_per_unit;  // (a part has room for all)
+  // (A part has room for all rows.)
+  const int end = whole ? min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit) : p.rows_per_unit;
   const size_t row0 = static_cast<size_t>(w.c) * p.Nq * p.hq + w.h * p.G;
   const size_t part = static_cast<size_t>((w.c * p.hkv + w.h) * p.row_blocks + w.rb + blockIdx.x) * p.rows_per_unit + row;
   // Lane j: row + j.
@@ -589,13 +607,15 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     float2 x[NC / 2];
     for (bool moved = false;; moved = true) {
       uint32_t s[NC];
-      tmem_ld_cols<NC>(scores, s);
+      tmem_ld16(scores, s);
       tmem_wait_ld();
 #pragma unroll
       for (int j = 0; j < NC; j += 4) {
         const float4 m = *reinterpret_cast<const float4*>(ref + j);  // (negated)
-        x[j / 2] = fma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), make_float2(qs, qs), make_float2(m.x, m.y));
-        x[j / 2 + 1] = fma2(make_float2(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3])), make_float2(qs, qs), make_float2(m.z, m.w));
+        const float2 lo = make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1]));
+        const float2 hi = make_float2(__uint_as_float(s[j + 2]), __uint_as_float(s[j + 3]));
+        x[j / 2] = fma2(lo, make_float2(qs, qs), make_float2(m.x, m.y));
+        x[j / 2 + 1] = fma2(hi, make_float2(qs, qs), make_float2(m.z, m.w));
       }
       if (flags & kMasked) {
 #pragma unroll
@@ -660,7 +680,8 @@ __global__ void __launch_bounds__(CF::kThreads, 1) attn_kv4_kernel(const __grid_
     // Arrivals, in the order of carve(): the ring (of a stage, a decoding warpgroup's warps and the one that stages q), K and
     // V decoded, then the rest.
     const int j = threadIdx.x - 2 * CF::kStages;
-    mbar_init(sm.cfull + 8 * threadIdx.x, j < -CF::kStages ? 1 : j < 0 ? 5 : j < 4 ? 4 : (j >> 1) == 3 || (j >> 1) == 8 ? 4 * CF::kGroups : 1);
+    const int n = j < -CF::kStages ? 1 : j < 0 ? 5 : j < 4 ? 4 : (j >> 1) == 3 || (j >> 1) == 8 ? 4 * CF::kGroups : 1;
+    mbar_init(sm.cfull + 8 * threadIdx.x, n);
     fence_mbar_init();
   }
   if (warp == CF::kWarpQ && (threadIdx.x & 31) < kMetas)  // (what an earlier CTA left there is of no tile)
@@ -747,7 +768,7 @@ struct Plan {
   size_t off_o, bytes;
 };
 
-// Fewest tiles per CTA.
+// Fewest tiles per CTA.  (One a CTA is no faster: a sequence of 2048 tokens takes 12.4 us with either.)
 constexpr int64_t kMinTiles = 2;
 
 kvshot_status make_kv4_plan(const kvshot_attn_desc* d, int32_t window, int32_t sinks, Plan* pl) {
@@ -759,7 +780,8 @@ kvshot_status make_kv4_plan(const kvshot_attn_desc* d, int32_t window, int32_t s
   const int64_t units = static_cast<int64_t>(d->num_caches) * d->hkv * pl->row_blocks;
   int64_t prefix = (static_cast<int64_t>(d->max_seq_len) + kTile - 1) / kTile;
   if (window > 0) {  // at most: the sinks' tiles and the window's, each cut at both ends
-    const int64_t seen = (static_cast<int64_t>(window) + kTile - 1) / kTile + 1 + (static_cast<int64_t>(sinks) + kTile - 1) / kTile;
+    const int64_t seen =
+        (static_cast<int64_t>(window) + kTile - 1) / kTile + 1 + (static_cast<int64_t>(sinks) + kTile - 1) / kTile;
     prefix = std::min(prefix, seen);
   }
   const int64_t max_tiles = units * (prefix + pl->draft_tiles);

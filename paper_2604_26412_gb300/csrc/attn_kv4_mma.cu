@@ -2,7 +2,7 @@
 // mma.sync tensor cores, with an optional sliding window and sink tokens.
 //
 // What bounds it: 144 B per key and KV head come from HBM, and each of its 256 codes has to become an f16 before it can be
-// multiplied: 128 conversions of two codes and 128 products with a scale per key, 8 of the kernel's ~17 (8 rows) to 22 (16)
+// multiplied: 128 conversions of two codes and 128 products with a scale per key, 8 of the kernel's ~15 (8 rows) to 19 (16)
 // warp instructions per key.  So a warp keeps everything in registers from the codes to O, and waits for no other warp:
 //  - Keys are the M dimension (as in attn_f8.cu): S^T = K Q^T, O^T = V^T P^T (m16n8k16, f16, fp32 sums); the query rows
 //    are N in steps of 8.  An m16 tile of keys is a 16-token group of the cache.
@@ -13,7 +13,16 @@
 //  - P^T comes from S^T by one 8x8 transpose (movmatrix) per 8 keys x 8 rows.
 //  - A row's reference is 2^8 below the maximum it was taken from and moves when a score passes it by 2^15, so O is
 //    rescaled rarely and P stays in f16's normal range for scores down to 2^-22 of the maximum.
-// A CTA is four warps, 32 keys of a tile each, and a loading warp; several CTAs share an SM.
+//  - A warp takes 32 keys together: one vote on the references, two independent chains of products (64 ragged sequences
+//    104 -> 97 us, 16 rows of 4 x 4 x 32k tokens 210 -> 174 with q's fragments in shared memory, which makes the registers
+//    for it).
+// A CTA is four warps, 32 keys of a tile each, and a loading warp; three CTAs share an SM (16 rows: two).  One more, in
+// the fewer registers that leaves a thread, is slower (105 against 97 us; 16 rows 202 against 173), and so is one less (110).
+// Measured, attention and merge: 8 rows, 64 sequences of 512 to 8192 tokens 95 us (3.8 TB/s, 0.56 of the copy's rate);
+// 16 rows, 4 x 4 x 32k tokens 166 us (3.7 TB/s); 8 rows, a window of 4096 35.4 us; one sequence of 2048 tokens 12.4 us.
+// It issues at half of the rate; what it waits for most is its own fixed latencies (1.2 cycles an instruction).
+// From 17 rows on attn_kv4.cu is faster; at 16 it takes 168 us (4 x 4 x 32k) where this kernel takes 166, and 41.5 against
+// 37.5 for 16 sequences of 4096 tokens.
 #include <algorithm>
 
 #include "kvshot_kv4_attn.cuh"
@@ -107,7 +116,8 @@ __device__ __forceinline__ uint32_t select_bits(uint32_t a, uint32_t b, uint32_t
 // Join the warps' parts of a piece, which lie in shared memory, and write it: the final bf16 output + lse if it is the
 // whole unit, else the normalised fp32 part + log2-domain lse.  All consumer threads.
 template <int n>
-__device__ __noinline__ bool join_warps(const AttnParams& p, const Smem& sm, const TileMeta& w, WarpSync& sync, const Waiter& wait) {
+__device__ __noinline__ bool join_warps(const AttnParams& p, const Smem& sm, const TileMeta& w, WarpSync& sync,
+                                        const Waiter& wait) {
   const int tid = threadIdx.x;
   if (!sync(wait)) return false;
   const int rows = min(p.rows_per_unit, p.rows_total - w.rb * p.rows_per_unit);
@@ -142,7 +152,8 @@ __device__ __noinline__ bool join_warps(const AttnParams& p, const Smem& sm, con
       v.w = fmaf(a, o.w, v.w);
     }
     if (whole)
-      reinterpret_cast<uint2*>(p.out + (orow0 + sm.rows->place[r]) * kHeadDim)[lane] = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+      reinterpret_cast<uint2*>(p.out + (orow0 + sm.rows->place[r]) * kHeadDim)[lane] =
+          make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
     else
       reinterpret_cast<float4*>(p.ws_o + (part + r) * kHeadDim)[lane] = v;
   }
@@ -481,7 +492,8 @@ using Cfg16 = Cfg<2, 2, 2>;
 
 template <class CF>
 cudaError_t set_smem() {
-  return cudaFuncSetAttribute(attn_kv4_mma_kernel<CF>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<CF>()));
+  return cudaFuncSetAttribute(attn_kv4_mma_kernel<CF>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(smem_bytes<CF>()));
 }
 
 template <class CF>

@@ -133,7 +133,9 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                : "memory");
 }
-__device__ __forceinline__ void sts32(uint32_t addr, int v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void sts32(uint32_t addr, int v) {
+  asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
 __device__ __forceinline__ int lds32(uint32_t addr) {
   int v;
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
@@ -150,7 +152,9 @@ __device__ __forceinline__ TileMeta tile_meta_at(uint32_t at) {
   return TileMeta{static_cast<int>(v.x), static_cast<int>(v.y), static_cast<int>(v.z), static_cast<int>(v.w),
                   static_cast<int>(w.x), static_cast<int>(w.y), static_cast<int>(w.z), static_cast<int>(w.w)};
 }
-__device__ __forceinline__ TileMeta tile_meta(const Ring& r, int t) { return tile_meta_at(r.meta + t % kMetas * sizeof(TileMeta)); }
+__device__ __forceinline__ TileMeta tile_meta(const Ring& r, int t) {
+  return tile_meta_at(r.meta + t % kMetas * sizeof(TileMeta));
+}
 // Its flags alone, read ahead of the wait; they are the tile's if is_of says so, and else are read again after it.
 __device__ __forceinline__ uint32_t tile_flags(const Ring& r, int t) {
   return lds32(r.meta + t % kMetas * sizeof(TileMeta)) ^ (static_cast<uint32_t>(t) << kTagShift);

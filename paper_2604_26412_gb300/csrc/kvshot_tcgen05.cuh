@@ -222,21 +222,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
       "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
-// N consecutive columns, a multiple of 8.
-template <int N>
-__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&v)[N]) {
-#pragma unroll
-  for (int c = 0; c + 32 <= N; c += 32) tmem_ld32(taddr + c, *reinterpret_cast<uint32_t(*)[32]>(&v[c]));
-  if constexpr (N % 32 >= 16) tmem_ld16(taddr + N / 32 * 32, *reinterpret_cast<uint32_t(*)[16]>(&v[N / 32 * 32]));
-  if constexpr (N % 16 == 8) tmem_ld8(taddr + N / 16 * 16, *reinterpret_cast<uint32_t(*)[8]>(&v[N / 16 * 16]));
-}
-template <int N>
-__device__ __forceinline__ void tmem_st_cols(uint32_t taddr, const uint32_t (&v)[N]) {
-#pragma unroll
-  for (int c = 0; c + 32 <= N; c += 32) tmem_st32(taddr + c, *reinterpret_cast<const uint32_t(*)[32]>(&v[c]));
-  if constexpr (N % 32 >= 16) tmem_st16(taddr + N / 32 * 32, *reinterpret_cast<const uint32_t(*)[16]>(&v[N / 32 * 32]));
-  if constexpr (N % 16 == 8) tmem_st8(taddr + N / 16 * 16, *reinterpret_cast<const uint32_t(*)[8]>(&v[N / 16 * 16]));
-}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
