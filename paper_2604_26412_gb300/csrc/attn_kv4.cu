@@ -292,8 +292,8 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
       if (flags & kMasked) {
         const int4 meta = tile_words(sm, t);  // flags, key0, nkeys, L
         // Keys that no row sees may hold anything; V of them must not be NaN (0 * NaN; any code times 0 is 0).
-        const int at = meta.y + key, lo = p.window > 0 ? meta.w + p.min_depth - p.window : 0;
-        if (key >= meta.z || (at < lo && at >= p.sinks)) sc = make_uint2(0u, 0u);
+        const int at = meta.y + key, lo = kp.window > 0 ? meta.w + kp.min_depth - kp.window : 0;
+        if (key >= meta.z || (at < lo && at >= kp.sinks)) sc = make_uint2(0u, 0u);
       }
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
@@ -726,6 +726,81 @@ __global__ void __launch_bounds__(CF::kThreads, 1) attn_kv4_kernel(const __grid_
   if (warp == CF::kWarpQk) tmem_dealloc(tmem, CF::kTmemCols);
 }
 
+// Join the pieces of the units that the CTAs' ranges cut, out = sum_k 2^(lse_k - m) o_k / sum_k 2^(lse_k - m): a warp per
+// row, lane = 4 dims.  blockIdx.x: a boundary between two ranges, whose unit it joins if it is the first one inside of it
+// (or, units cut by themselves, the unit).  So the CTAs are as many as the cuts need: 256 rows of 16 sequences, 512 units
+// of which 151 are cut, took 8 us of 174 with a warp for every row of all units.
+constexpr int kMergeWarps = 8;  // rows of a CTA
+// kMergeBatch: pieces loaded together.
+template <int kMergeBatch, int kCtasPerSm>
+__global__ void __launch_bounds__(32 * kMergeWarps, kCtasPerSm) merge_kv4_kernel(const __grid_constant__ Kv4Params kp) {
+  const AttnParams& p = kp.a;
+  // CTA 0 waits in any case: a kernel that depends on this grid alone then comes after the attention, too.
+  if (blockIdx.x == 0 && blockIdx.y == 0) wait_for_prerequisite_grid();
+  if (threadIdx.x == 0) allow_dependent_launch();
+  const int lane = threadIdx.x & 31, r = blockIdx.y * kMergeWarps + (threadIdx.x >> 5);
+  int b0, b1;  // the CTAs that held the unit
+  RangeStart u;
+  if (p.unit_ctas > 0) {
+    u = range_of(kp, 0);
+    const int per = (u.ut + u.tpc - 1) / u.tpc;
+    u.hr = blockIdx.x;
+    b0 = u.hr * per;
+    b1 = b0 + per - 1;
+  } else {
+    u = range_of(kp, blockIdx.x + 1);
+    if (u.t >= u.t_end || u.lt == 0 || u.lt > u.tpc) return;
+    b0 = blockIdx.x;
+    b1 = (u.t - u.lt + u.ut - 1) / u.tpc;
+  }
+  const int h = kp.by_blocks(u.hr), rb = u.hr - h * p.row_blocks, rr = rb * p.rows_per_unit + r, np = b1 - b0 + 1;
+  if (np < 2 || r >= p.rows_per_unit || rr >= p.rows_total) return;
+  const int nl = kp.by_group(rr);
+  const size_t orow = (static_cast<size_t>(u.c) * p.Nq + nl) * p.hq + h * p.G + rr - nl * p.G;
+  const size_t row0 = static_cast<size_t>(u.c * p.hkv * p.row_blocks + u.hr + b0) * p.rows_per_unit + r;
+  const float4* parts = reinterpret_cast<const float4*>(p.ws_o + row0 * kHeadDim) + lane;
+  const int stride = p.rows_per_unit * (kHeadDim / 4);  // from one piece's row to the next one's
+  wait_for_prerequisite_grid();
+  float m = -INFINITY, sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int k0 = 0; k0 < np; k0 += 32) {  // lane k: piece k0 + k
+    const float ls = k0 + lane < np ? p.ws_lse[row0 + static_cast<size_t>(k0 + lane) * p.rows_per_unit] : -INFINITY;
+    float w = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < min(32, np - k0); k += kMergeBatch) {
+      float4 x[kMergeBatch];  // (of the first batch, loaded beside the lse)
+#pragma unroll
+      for (int i = 0; i < kMergeBatch; ++i)
+        x[i] = k0 + k + i < np ? parts[static_cast<size_t>(k0 + k + i) * stride] : make_float4(0.f, 0.f, 0.f, 0.f);
+      if (k == 0) {
+        float top = ls;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        top = fmaxf(top, m);
+        const float keep = m == -INFINITY ? 0.f : exp2f(m - top);
+        w = ls == -INFINITY ? 0.f : exp2f(ls - top);
+        m = top;
+        sum *= keep;
+        acc = make_float4(acc.x * keep, acc.y * keep, acc.z * keep, acc.w * keep);
+      }
+#pragma unroll
+      for (int i = 0; i < kMergeBatch; ++i) {
+        const float a = __shfl_sync(0xffffffffu, w, k + i);  // 0 past the last piece
+        sum += a;
+        acc.x = fmaf(a, x[i].x, acc.x);
+        acc.y = fmaf(a, x[i].y, acc.y);
+        acc.z = fmaf(a, x[i].z, acc.z);
+        acc.w = fmaf(a, x[i].w, acc.w);
+      }
+    }
+  }
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  reinterpret_cast<uint2*>(p.out + orow * kHeadDim)[lane] =
+      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+  if (lane == 0) p.lse[orow] = sum > 0.f ? (m + log2f(sum)) * 0.69314718055994531f : -INFINITY;
+}
+
 constexpr int kMaxRows = 64;  // query rows of a unit
 
 int rows_of_unit(int rows) {
@@ -872,18 +947,17 @@ extern "C" kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* d, const 
   p.n_max = d->n_max;
   p.tree = tree;
   p.draft_tiles = pl.draft_tiles;
-  p.prefix_tile = kTile;
   const double scale = d->scale != 0.f ? static_cast<double>(d->scale) : 1.0 / std::sqrt(static_cast<double>(kHeadDim));
   p.qscale = static_cast<float>(scale * 1.4426950408889634);
   p.num_ctas = pl.num_ctas;
   p.unit_ctas = d->num_caches == 1 ? pl.num_ctas / pl.units : 0;  // (one cache: its units are cut by themselves)
-  p.unit_ctas = d->num_caches == 1 ? pl.num_ctas / pl.units : 0;
   p.wait_ns = d->wait_limit_ns != 0 ? d->wait_limit_ns : 2000000000u;
-  p.k_scale = std::ldexp(1.f, d->k_scale_exp);
+  // (As for the fp8 cache: a prefix score's scale that underflows to 0 would make masked scores 0 * -inf.)
+  p.k_scale = std::max(std::ldexp(1.f, d->k_scale_exp), std::ldexp(1.f, -100) / p.qscale);
   p.v_scale = std::ldexp(1.f, d->v_scale_exp);
-  p.window = window;
-  p.sinks = sinks;
-  p.min_depth = tree ? 1 : d->n_nodes - d->n_query + 1;
+  kp.window = window;
+  kp.sinks = sinks;
+  kp.min_depth = tree ? 1 : d->n_nodes - d->n_query + 1;
   kp.cache = static_cast<const uint8_t*>(cache);
   kp.draft_k = static_cast<const __nv_bfloat16*>(draft_k);
   kp.draft_v = static_cast<const __nv_bfloat16*>(draft_v);
@@ -898,5 +972,9 @@ extern "C" kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* d, const 
   if (launch(kp, (d->flags & KVSHOT_OVERLAP_PREVIOUS) != 0, s) != cudaSuccess) return KVSHOT_ERR_CUDA;
   // A CTA takes whole units, whatever the lengths: nothing to merge.
   if (pl.num_ctas == 1 || p.unit_ctas == 1 || (d->num_caches == 1 && pl.units % pl.num_ctas == 0)) return KVSHOT_OK;
-  return launch_merge(p, sm_count(), s) == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
+  const int rows = std::min(p.rows_per_unit, p.rows_total);
+  const dim3 grid(p.unit_ctas > 0 ? pl.units : pl.num_ctas - 1, (rows + kMergeWarps - 1) / kMergeWarps);
+  const bool few = static_cast<int64_t>(grid.x) * grid.y <= 2 * static_cast<int64_t>(sm_count());
+  const cudaError_t e = launch_maybe_pdl(few ? merge_kv4_kernel<8, 2> : merge_kv4_kernel<2, 6>, grid, dim3(32 * kMergeWarps), 0, true, s, kp);
+  return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
 }

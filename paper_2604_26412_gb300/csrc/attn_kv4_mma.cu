@@ -351,12 +351,12 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
           uint4 sc[2] = {lds128(vat + vscale), lds128(vat + vscale + 64)};  // tokens 2 q4, 2 q4 + 1 and those + 8
           if (masked) {
             // Keys that no row sees may hold anything, NaN scales among it: 0 times them must be 0.
-            const int lo = p.window > 0 ? meta.w + p.min_depth - p.window : 0;
+            const int lo = kp.window > 0 ? meta.w + kp.min_depth - kp.window : 0;
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
               const int key = kw + 16 * i + 8 * a + 2 * q4, pos = meta.y + key;
-              if (key >= meta.z || (pos < lo && pos >= p.sinks)) sc[a].x = sc[a].y = 0u;
-              if (key + 1 >= meta.z || (pos + 1 < lo && pos + 1 >= p.sinks)) sc[a].z = sc[a].w = 0u;
+              if (key >= meta.z || (pos < lo && pos >= kp.sinks)) sc[a].x = sc[a].y = 0u;
+              if (key + 1 >= meta.z || (pos + 1 < lo && pos + 1 >= kp.sinks)) sc[a].z = sc[a].w = 0u;
             }
           }
 #pragma unroll

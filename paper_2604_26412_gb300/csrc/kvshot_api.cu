@@ -539,7 +539,6 @@ extern "C" kvshot_status kvshot_draft_attn(const kvshot_attn_desc* d, const void
   // below 2^-100 every score vanishes beside 1.
   p.k_scale = fp8 ? std::max(std::ldexp(1.f, d->k_scale_exp), std::ldexp(1.f, -100) / p.qscale) : 1.f;
   p.v_scale = fp8 ? std::ldexp(1.f, d->v_scale_exp) : 1.f;
-  p.window = p.sinks = p.min_depth = 0;
 
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const bool pdl = (d->flags & KVSHOT_OVERLAP_PREVIOUS) != 0;

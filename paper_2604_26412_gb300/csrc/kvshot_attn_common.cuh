@@ -302,22 +302,6 @@ __device__ __forceinline__ bool unit_cuts(const AttnParams& p) {
   return kCuts == kCutsEither ? p.unit_ctas > 0 : kCuts == kCutsUnits;
 }
 
-// The prefix tiles of a cache of L tokens that some query row may see, with a sliding window: tiles [0, sink_tiles) and,
-// `skip` tiles further on, those from the window's first key to the last one.  (The shallowest query node stands at
-// L + min_depth - 1 and sees keys from L + min_depth - window on.)
-struct WindowSpan {
-  int tiles, sink_tiles, skip;
-};
-template <int PK>
-__device__ __forceinline__ WindowSpan window_span(const AttnParams& p, int L) {
-  const int all = (L + PK - 1) / PK;
-  if (p.window == 0) return WindowSpan{all, all, 0};
-  const int lo = max(0, L + p.min_depth - p.window);
-  const int sink_tiles = min(all, (min(p.sinks, lo) + PK - 1) / PK);
-  const int skip = max(0, min(all, lo / PK) - sink_tiles);
-  return WindowSpan{all - skip, sink_tiles, skip};
-}
-
 // s_len[c] = clamped L_c; s_base[c] = first global tile of cache c (prefix sum of
 // units x tiles per unit).  Whole block participates.  `len0` may hold
 // seq_lens[threadIdx.x], loaded early by the caller (-1: not loaded).  PK, here and below: keys

@@ -28,7 +28,6 @@ constexpr int kHalfBytes = kTileKeys * 128;           // 64 dims x TK keys, bf16
 constexpr int kKVTileBytes = 2 * kHalfBytes;          // one K (or V) tile
 constexpr int kStageBytes = 2 * kKVTileBytes;         // K + V
 constexpr int kF8PrefixTile = 128;                    // keys per prefix tile of the fp8 mma.sync kernel
-constexpr int kKv4PrefixTile = 128;                   // keys per prefix tile of the 4-bit cache's kernel
 constexpr int kMaxCaches = 1024;
 constexpr int kMaxTreeNodes = 64;
 constexpr int kDraftBoxRows = 8;                      // draft K/V are loaded 8 rows per TMA box
@@ -85,8 +84,6 @@ struct AttnParams {
                             // m16n8k16 kernel: draft tiles too)
   uint32_t wait_ns;         // limit on any one pipeline wait (desc->wait_limit_ns, default 2 s)
   float k_scale, v_scale;   // fp8, 4-bit cache: 2^k_scale_exp, 2^v_scale_exp
-  int window, sinks;        // 4-bit cache: sliding window (0: none) and sink tokens
-  int min_depth;            // depth of the shallowest query node (a lower bound), for the window
 };
 
 struct AppendParams {

@@ -13,7 +13,9 @@ struct Kv4Params {
   const __nv_bfloat16 *draft_k, *draft_v;
   int groups_per_page;
   Div by_page, by_blocks, by_seq, by_group;  // groups per page, row blocks, caches per sequence, heads per KV head
-  int run_groups;  // groups of a tile that are always neighbours in memory (a power of two, at most kTileGroups)
+  int window, sinks;  // sliding window (0: none) and sink tokens
+  int min_depth;      // depth of the shallowest query node (a lower bound), for the window
+  int run_groups;     // groups of a tile that are always neighbours in memory (a power of two, at most kTileGroups)
 };
 
 // attn_kv4_mma.cu: stacks of up to 16 query rows per KV head.
@@ -25,7 +27,7 @@ namespace {  // internal linkage: every translation unit gets its own copy
 using namespace dev;
 using namespace kv4;
 
-constexpr int kTile = kKv4PrefixTile;              // keys per prefix tile
+constexpr int kTile = 128;                         // keys per prefix tile
 constexpr int kTileGroups = kTile / kKv4Tokens;
 constexpr int kStageSize = kTileGroups * kKv4Bytes;
 constexpr int kDraftTile = 32;                     // keys per draft tile: bf16 rows of K and V fill a stage
@@ -161,6 +163,23 @@ __device__ __forceinline__ uint32_t tile_flags(const Ring& r, int t) {
 }
 __device__ __forceinline__ bool is_of(uint32_t flags) { return flags < (1u << kTagShift); }
 
+// ------------------------------------------------------------ the plan
+
+// The prefix tiles of a cache of L tokens that some query row may see, with a sliding window: tiles [0, sink_tiles) and,
+// `skip` tiles further on, those from the window's first key to the last one.  (The shallowest query node stands at
+// L + min_depth - 1 and sees keys from L + min_depth - window on.)
+struct WindowSpan {
+  int tiles, sink_tiles, skip;
+};
+__device__ __forceinline__ WindowSpan window_span(const Kv4Params& p, int L) {
+  const int all = (L + kTile - 1) / kTile;
+  if (p.window == 0) return WindowSpan{all, all, 0};
+  const int lo = max(0, L + p.min_depth - p.window);
+  const int sink_tiles = min(all, (min(p.sinks, lo) + kTile - 1) / kTile);
+  const int skip = max(0, min(all, lo / kTile) - sink_tiles);
+  return WindowSpan{all - skip, sink_tiles, skip};
+}
+
 // ------------------------------------------------------------ loads
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -169,66 +188,74 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-// A CTA's range of tiles [t, t_end), which begins in cache c (of length L), KV head x row block hr, tile lt of the unit.
-struct LoaderStart {
-  int t, t_end, c, L, hr, lt;
+// Where a CTA's range of tiles [t, t_end) begins: cache c (of length L), KV head x row block hr, tile lt of the unit's ut;
+// tpc: tiles of a range.  By a warp.
+struct RangeStart {
+  int t, t_end, c, L, hr, lt, ut, tpc;
 };
+__device__ __forceinline__ RangeStart range_of(const Kv4Params& kp, int cta) {
+  const AttnParams& p = kp.a;
+  const int lane = threadIdx.x & 31, HR = p.hkv * p.row_blocks;
+  auto unit_tiles = [&](int L) { return window_span(kp, L).tiles + p.draft_tiles; };
+  RangeStart r{0, 0, 0, 0, 0, 0, 0, 0};
+  if (p.unit_ctas > 0) {
+    r.L = clamp_len(p, 0);
+    r.ut = unit_tiles(r.L);
+    const UnitCut u = unit_cut(p.unit_ctas, r.ut);
+    r.tpc = u.tpc;
+    r.hr = cta / u.per;
+    r.lt = (cta - r.hr * u.per) * u.tpc;
+    r.t_end = r.hr < HR ? min(u.tpc, r.ut - r.lt) : 0;
+    return r;
+  }
+  // A lane's cache of 32 from c0 on: its length, and the tiles up to and including it.
+  int L = 0, upto = 0;
+  auto sum = [&](int c0) {
+    const int c = c0 + lane;
+    L = c < p.C ? clamp_len(p, c) : 0;
+    upto = c < p.C ? unit_tiles(L) * HR : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+  };
+  int total = 0;
+#pragma unroll 1
+  for (int c0 = 0; c0 < p.C; c0 += 32) {
+    sum(c0);
+    total += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  r.tpc = tiles_per_cta(total, p.num_ctas);
+  r.t = min(total, cta * r.tpc);
+  r.t_end = min(total, r.t + r.tpc);
+  int below = 0, c0 = 0;
+#pragma unroll 1
+  for (; r.t < r.t_end; c0 += 32) {
+    if (p.C > 32) sum(c0);
+    const int all = __shfl_sync(0xffffffffu, upto, 31);
+    if (r.t < below + all) break;
+    below += all;
+  }
+  if (r.t < r.t_end) {
+    const int i = __popc(__ballot_sync(0xffffffffu, below + upto <= r.t));  // caches of these that end before it
+    r.c = c0 + i;
+    r.L = __shfl_sync(0xffffffffu, L, i);
+    const int before = __shfl_sync(0xffffffffu, upto, max(i - 1, 0));
+    const int rem = r.t - below - (i > 0 ? before : 0);
+    r.ut = unit_tiles(r.L);
+    r.hr = rem / r.ut;
+    r.lt = rem - r.hr * r.ut;
+  }
+  return r;
+}
 constexpr int kFirstBytes = sizeof(TileMeta) + 16;
 // By the loading warp, before the barrier that the roles begin with; left at sm.first: the first piece's words, with t,
 // t_end and L in place of a tile's, then hr and lt.
 __device__ __forceinline__ void plan_loader(const Kv4Params& kp, const Ring& sm) {
   const AttnParams& p = kp.a;
-  const int lane = threadIdx.x & 31, HR = p.hkv * p.row_blocks;
-  auto unit_tiles = [&](int L) { return window_span<kTile>(p, L).tiles + p.draft_tiles; };
-  LoaderStart r{0, 0, 0, 0, 0, 0};
-  if (p.unit_ctas > 0) {
-    r.L = clamp_len(p, 0);
-    const int ut = unit_tiles(r.L);
-    const UnitCut u = unit_cut(p.unit_ctas, ut);
-    r.hr = blockIdx.x / u.per;
-    r.lt = (blockIdx.x - r.hr * u.per) * u.tpc;
-    r.t_end = r.hr < HR ? min(u.tpc, ut - r.lt) : 0;
-  } else {
-    // A lane's cache of 32 from c0 on: its length, and the tiles up to and including it.
-    int L = 0, upto = 0;
-    auto sum = [&](int c0) {
-      const int c = c0 + lane;
-      L = c < p.C ? clamp_len(p, c) : 0;
-      upto = c < p.C ? unit_tiles(L) * HR : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += x;
-      }
-    };
-    int total = 0;
-#pragma unroll 1
-    for (int c0 = 0; c0 < p.C; c0 += 32) {
-      sum(c0);
-      total += __shfl_sync(0xffffffffu, upto, 31);
-    }
-    const int tpc = tiles_per_cta(total, p.num_ctas);
-    r.t = min(total, static_cast<int>(blockIdx.x) * tpc);
-    r.t_end = min(total, r.t + tpc);
-    int below = 0, c0 = 0;
-#pragma unroll 1
-    for (; r.t < r.t_end; c0 += 32) {
-      if (p.C > 32) sum(c0);
-      const int all = __shfl_sync(0xffffffffu, upto, 31);
-      if (r.t < below + all) break;
-      below += all;
-    }
-    if (r.t < r.t_end) {
-      const int i = __popc(__ballot_sync(0xffffffffu, below + upto <= r.t));  // caches of these that end before it
-      r.c = c0 + i;
-      r.L = __shfl_sync(0xffffffffu, L, i);
-      const int before = __shfl_sync(0xffffffffu, upto, max(i - 1, 0));
-      const int rem = r.t - below - (i > 0 ? before : 0), ut = unit_tiles(r.L);
-      r.hr = rem / ut;
-      r.lt = rem - r.hr * ut;
-    }
-  }
-  if (lane == 0) {
+  const RangeStart r = range_of(kp, blockIdx.x);
+  if ((threadIdx.x & 31) == 0) {
     const int h = kp.by_blocks(r.hr);
     *sm.issued = 0;
     sts128(sm.first, make_uint4(r.t < r.t_end ? kFirst | kNewRows | (p.tree ? kNewTree : 0) : 0, r.t, r.t_end, r.L));
@@ -257,7 +284,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
 #pragma unroll 1
   for (; ok && t < t_end; lt = 0) {  // a piece
     const int L = lds32(sm.first + 12);
-    const WindowSpan span = window_span<kTile>(p, L);
+    const WindowSpan span = window_span(kp, L);
     const int ut = span.tiles + p.draft_tiles, lt1 = min(ut, lt + t_end - t);
     const int h = kp.by_blocks(hr), rb = hr - h * p.row_blocks, seq = kp.by_seq(c);
     const int last = kLast | (lt == 0 && lt1 == ut ? kWhole : 0);
@@ -268,7 +295,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
     last_seq = seq;
     t += lt1 - lt;
     // A window: rows see keys from L + their depth - window on (and the sinks); a depth is at most N.
-    const int seen_from = p.window > 0 ? L + p.N - p.window : 0;
+    const int seen_from = kp.window > 0 ? L + p.N - kp.window : 0;
     const int32_t* table = p.page_table + (p.paged ? static_cast<size_t>(c) * p.max_pages : 0);
     auto key_of = [&](int x) { return (x < span.sink_tiles ? x : x + span.skip) * kTile; };  // of a prefix tile
     auto group_of = [&](int x) {  // this lane's first group of the window from tile x on, or -1
@@ -296,7 +323,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
       const int key0 = draft ? (lt - span.tiles) * kDraftTile : key_of(lt);
       const int nkeys = draft ? min(kDraftTile, p.N - key0) : min(kTile, L - key0);
       if (draft) flags |= kDraft | kMasked;
-      else if (nkeys < kTile || (key0 < seen_from && key0 + kTile > p.sinks)) flags |= kMasked;
+      else if (nkeys < kTile || (key0 < seen_from && key0 + kTile > kp.sinks)) flags |= kMasked;
       if (lt == lt1 - 1) flags |= last;
       if (draft && !waited) {  // the draft K/V may come from the preceding kernel
         wait_for_prerequisite_grid();
@@ -491,7 +518,7 @@ __device__ __noinline__ uint64_t rows_seeing(const Kv4Params& kp, const Rows& r,
   const AttnParams& p = kp.a;
   if (key >= m.z) return 0ull;
   const bool draft = m.x & kDraft;
-  if (!draft && p.window == 0) return ~0ull;
+  if (!draft && kp.window == 0) return ~0ull;
   const int at = m.y + key, L = m.w;
   // Rows whose node's depth is at most x.  A chain's rows are in the order of depth.
   auto upto = [&](int x) -> uint64_t {
@@ -499,11 +526,11 @@ __device__ __noinline__ uint64_t rows_seeing(const Kv4Params& kp, const Rows& r,
     const int n = min(x - (p.N - p.Nq), p.Nq) * p.G - rb * p.rows_per_unit;
     return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull;
   };
-  if (!draft) return at < p.sinks ? ~0ull : upto(at - L + p.window);
+  if (!draft) return at < kp.sinks ? ~0ull : upto(at - L + kp.window);
   uint64_t bits = p.tree ? r.line[at] : ~upto(at);
-  if (p.window > 0) {
+  if (kp.window > 0) {
     const int depth = p.tree ? __popcll(r.anc[at]) : at + 1;
-    if (L + depth - 1 >= p.sinks) bits &= upto(depth + p.window - 1);
+    if (L + depth - 1 >= kp.sinks) bits &= upto(depth + kp.window - 1);
   }
   return bits;
 }

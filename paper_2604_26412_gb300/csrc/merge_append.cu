@@ -36,8 +36,7 @@ constexpr int kMergeRows = kMergeThreads / 32;  // rows per CTA, one warp per ro
 // in few pieces and whose waves of CTAs are what costs (16 caches, against batches of 16: 128 rows
 // of 32768 tokens 376 -> 369 us per call, 256 rows of 4096 tokens, nothing split, 75.4 -> 73.9,
 // with an fp8 cache 185 -> 174; batches of 4 the same, of 8 in four CTAs per SM 1 to 2 us more).
-// kWindow: the units' tiles are those of a sliding window (window_span).
-template <int kMergeBatch, int kCtasPerSm, bool kWindow = false>
+template <int kMergeBatch, int kCtasPerSm>
 __global__ void __launch_bounds__(kMergeThreads, kCtasPerSm) merge_kernel(const __grid_constant__ AttnParams p) {
   const uint32_t unit_rows = min(p.rows_per_unit, p.rows_total), row = blockIdx.x * kMergeRows + (threadIdx.x >> 5);
   const int u = row / unit_rows, r = row - u * unit_rows;
@@ -52,10 +51,7 @@ __global__ void __launch_bounds__(kMergeThreads, kCtasPerSm) merge_kernel(const 
   const int rr = rb * p.rows_per_unit + r;
   if (u >= p.C * HR || rr >= p.rows_total) return;
   const int shift = __ffs(p.prefix_tile) - 1;  // a power of two
-  auto tiles = [&](int len) {
-    if constexpr (kWindow) return window_span<kKv4PrefixTile>(p, len).tiles + p.draft_tiles;
-    else return ((len + p.prefix_tile - 1) >> shift) + p.draft_tiles;
-  };
+  auto tiles = [&](int len) { return ((len + p.prefix_tile - 1) >> shift) + p.draft_tiles; };
   int b0, b1;  // the CTAs that held the unit
   if (p.unit_ctas > 0) {
     const UnitCut cut = unit_cut(p.unit_ctas, tiles(clamp_len(p, 0)));
@@ -439,9 +435,7 @@ cudaError_t launch_merge(const AttnParams& p, int sms, cudaStream_t stream) {
   cfg.numAttrs = 1;
   // (One cache whose units are in two pieces at most fills no batch of 16: 300 tokens, 4 rows 11.0 -> 10.9 us per call.)
   const bool two_pieces = p.unit_ctas == 1 || p.unit_ctas == 2;
-  const bool batches = blocks <= 2 * sms && !two_pieces;
-  if (p.window > 0) return cudaLaunchKernelEx(&cfg, batches ? merge_kernel<16, 2, true> : merge_kernel<2, 6, true>, p);
-  return cudaLaunchKernelEx(&cfg, batches ? merge_kernel<16, 2> : merge_kernel<2, 6>, p);
+  return cudaLaunchKernelEx(&cfg, blocks <= 2 * sms && !two_pieces ? merge_kernel<16, 2> : merge_kernel<2, 6>, p);
 }
 
 cudaError_t launch_append(AppendParams a, cudaStream_t stream) {

@@ -150,3 +150,18 @@ def test_a_wait_that_runs_out_is_recorded(hq, nodes, lens):
         got = case.run()
         assert int(case.err.item()) == 0
         assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+@pytest.mark.parametrize("lens,hq,nodes,num_ctas", [((3000,), 8, 2, 0), ((3000,), 8, 12, 7), ((700, 3000, 0, 150), 8, 4, 0),
+                                                    ((2000, 1000), 8, 40, 3), ((9000,), 8, 1, 300), ((6000, 40), 8, 14, 120)])
+def test_pieces_are_joined(lens, hq, nodes, num_ctas):
+    """Units in one piece, in two and in more than 32, of one cache (cut by themselves) and of several."""
+    from tests.test_gpu_kv4 import Case
+    Case(list(lens), hq=hq, hkv=2, nodes=nodes, query=nodes, num_ctas=num_ctas, seed=nodes).check()
+
+
+@pytest.mark.parametrize("nodes", [2, 4, 12])
+def test_a_prefix_scale_that_underflows(nodes):
+    """scale * 2^k_scale_exp below fp32: the prefix's scores are 0, its masked keys stay masked."""
+    from tests.test_gpu_kv4 import Case
+    Case([300], nodes=nodes, query=nodes, exps=(-64, 0), scale=1e-30, window=100, sinks=3, seed=nodes).check()
