@@ -57,7 +57,7 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// e4m3 number nearest to x in [2^-9, 448] (or NaN).
+// e4m3 number nearest to x >= 2^-9, at most 448 (or NaN).
 __device__ __forceinline__ uint32_t f32_to_e4m3(float x) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.f), "f"(x));
