@@ -955,7 +955,7 @@ extern "C" kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* d, const 
   // (As for the fp8 cache: a prefix score's scale that underflows to 0 would make masked scores 0 * -inf.)
   p.k_scale = std::max(std::ldexp(1.f, d->k_scale_exp), std::ldexp(1.f, -100) / p.qscale);
   p.v_scale = std::ldexp(1.f, d->v_scale_exp);
-  kp.window = window;
+  kp.window = window < static_cast<int64_t>(p.len_bound) + p.N ? window : 0;  // (a window that no key is out of is none)
   kp.sinks = sinks;
   kp.min_depth = tree ? 1 : d->n_nodes - d->n_query + 1;
   kp.cache = static_cast<const uint8_t*>(cache);

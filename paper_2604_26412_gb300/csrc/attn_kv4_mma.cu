@@ -18,12 +18,13 @@
 //    for it).
 // A CTA is four warps, 32 keys of a tile each, and a loading warp; three CTAs share an SM (16 rows: two).  One more, in
 // the fewer registers that leaves a thread, is slower (105 against 97 us; 16 rows 202 against 173), and so is one less (110).
-// Measured, attention and merge: 8 rows, 64 sequences of 512 to 8192 tokens 95 us (3.8 TB/s, 0.56 of the copy's rate);
-// 16 rows, 4 x 4 x 32k tokens 166 us (3.7 TB/s); 8 rows, a window of 4096 35.4 us; one sequence of 2048 tokens 12.4 us.
+// Measured, attention and merge: 8 rows, 64 sequences of 512 to 8192 tokens 93 us (3.9 TB/s, 0.57 of the copy's rate);
+// 16 rows, 4 x 4 x 32k tokens 166 us (3.7 TB/s); 8 rows, a window of 4096 31.8 us; one sequence of 2048 tokens 12.0 us.
 // It issues at half of the rate; what it waits for most is its own fixed latencies (1.2 cycles an instruction).
 // From 17 rows on attn_kv4.cu is faster; at 16 it takes 168 us (4 x 4 x 32k) where this kernel takes 166, and 41.5 against
 // 37.5 for 16 sequences of 4096 tokens.
 #include <algorithm>
+#include <climits>
 
 #include "kvshot_kv4_attn.cuh"
 
@@ -234,6 +235,18 @@ __device__ __forceinline__ void hide(float (&s)[NR][4], const Kv4Params& kp, con
   }
 }
 
+// Prefix keys, 8 rows: a row of depth d sees the sinks and the positions from L + d - window on.  `from`: of rows 2 q4 + e.
+__device__ __forceinline__ void hide_prefix(float (&s)[4], const int (&from)[2], const int4& meta, int sinks, int key) {
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    const int at = key + 8 * a, pos = meta.y + at;
+    const int bound = at >= meta.z ? INT_MIN : pos < sinks ? INT_MAX : pos;  // (no key: no row; a sink: every row)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (bound < from[e]) s[2 * a + e] = -INFINITY;
+  }
+}
+
 template <class CF>
 __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& smem, const Waiter& wait) {
   constexpr int NR = CF::kNR;
@@ -337,8 +350,18 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
           }
         }
         if (masked) {
+          // (8 rows by compares: a window of 4096 31.8 us, by the rows' bits 35.4.  At 16 rows the compares' registers cost
+          // every tile: 4 x 4 x 32k tokens 171 us, by the bits 166.)
+          if constexpr (NR == 1) {
+            const int2 depth = *reinterpret_cast<const int2*>(sm.rows->depth + 2 * q4);
+            const int from[2] = {kp.window > 0 ? meta.w + depth.x - kp.window : INT_MIN + 1,
+                                 kp.window > 0 ? meta.w + depth.y - kp.window : INT_MIN + 1};
 #pragma unroll
-          for (int i = 0; i < 2; ++i) hide<NR>(s[i], kp, *sm.rows, meta, rb, kw + 16 * i + g, q4);
+            for (int i = 0; i < 2; ++i) hide_prefix(s[i][0], from, meta, kp.sinks, kw + 16 * i + g);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) hide<NR>(s[i], kp, *sm.rows, meta, rb, kw + 16 * i + g, q4);
+          }
         }
         uint32_t pb[2][NR][2];
         softmax_step<NR, 2>(st, s, p.qscale * p.k_scale, false, 1.f, pb);

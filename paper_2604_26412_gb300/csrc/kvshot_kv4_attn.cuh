@@ -67,7 +67,8 @@ struct Ring {
 };
 // The query rows of a unit: their places in a cache's q and out, and, of a draft tree, who sees what, as bits of rows.
 struct alignas(16) Rows {
-  int place[64];                      // (read four at a time)
+  int place[64];
+  int depth[64];                      // of the row's node
   uint64_t line[kMaxTreeNodes];       // rows whose node is this one or descends from it
   uint64_t upto[kMaxTreeNodes + 1];   // rows whose depth is at most x
   uint64_t anc[kMaxTreeNodes];        // nodes: itself and its ancestors
@@ -486,7 +487,10 @@ __device__ __noinline__ void build_rows(const Kv4Params& kp, Rows& r, int nc, in
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int j = lane + 32 * k, nl = kp.by_group(min(row0 + j, p.rows_total - 1));
-    if (j < nc) r.place[j] = nl * p.hq + row0 + j - nl * p.G;
+    if (j < nc) {
+      r.place[j] = nl * p.hq + row0 + j - nl * p.G;
+      r.depth[j] = p.tree ? __popcll(r.anc[p.N - p.Nq + nl]) : p.N - p.Nq + nl + 1;
+    }
   }
   if (p.tree) {
     // The query nodes one after another, whose rows are neighbours: lane m has the rows of nodes m, m + 32, and of depths.

@@ -165,3 +165,12 @@ def test_a_prefix_scale_that_underflows(nodes):
     """scale * 2^k_scale_exp below fp32: the prefix's scores are 0, its masked keys stay masked."""
     from tests.test_gpu_kv4 import Case
     Case([300], nodes=nodes, query=nodes, exps=(-64, 0), scale=1e-30, window=100, sinks=3, seed=nodes).check()
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 305, 304, 299])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("nodes", [2, 4, 12])
+def test_windows_about_as_long_as_the_context(window, tree, nodes):
+    from tests.test_gpu_kv4 import Case, _tree
+    par = _tree(np.random.default_rng(nodes), 1, nodes, 2) if tree else None
+    Case([300], nodes=nodes, query=nodes, parent=par, window=window, sinks=2, seed=nodes).check()
