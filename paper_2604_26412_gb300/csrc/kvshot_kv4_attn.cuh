@@ -13,6 +13,9 @@ struct Kv4Params {
   const __nv_bfloat16 *draft_k, *draft_v;
   int groups_per_page;
   Div by_page, by_blocks, by_seq, by_group;  // groups per page, row blocks, caches per sequence, heads per KV head
+  Div by_cache;    // units of a cache
+  int ctas_per_unit;
+  int spare_tiles; // a CTA may take as many tiles more if that leaves it one piece
   int window, sinks;  // sliding window (0: none) and sink tokens
   int min_depth;      // depth of the shallowest query node (a lower bound), for the window
   int run_groups;     // groups of a tile that are always neighbours in memory (a power of two, at most kTileGroups)
@@ -190,45 +193,57 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 }
 
 // Where a CTA's range of tiles [t, t_end) begins: cache c (of length L), KV head x row block hr, tile lt of the unit's ut;
-// tpc: tiles of a range.  By a warp.
+// tpc: tiles of a range.  The units' tiles laid end to end are cut into equal ranges; or, if there are CTAs for it and the
+// longest range gets no more than spare_tiles longer (and with one cache), each unit by itself into `per` pieces, so that no
+// CTA takes the end of one unit and the start of the next one: a second piece costs it a start and an end, and the units
+// that it cuts a merge.  (per 0: equal ranges.)
 struct RangeStart {
-  int t, t_end, c, L, hr, lt, ut, tpc;
+  int t, t_end, c, L, hr, lt, ut, tpc, per;
 };
-__device__ __forceinline__ RangeStart range_of(const Kv4Params& kp, int cta) {
+// By a warp.  kMerge: not this CTA's, but the range that begins at the boundary after range blockIdx.x, or unit blockIdx.x.
+template <bool kMerge>
+__device__ __forceinline__ RangeStart range_of(const Kv4Params& kp) {
   const AttnParams& p = kp.a;
   const int lane = threadIdx.x & 31, HR = p.hkv * p.row_blocks;
   auto unit_tiles = [&](int L) { return window_span(kp, L).tiles + p.draft_tiles; };
-  RangeStart r{0, 0, 0, 0, 0, 0, 0, 0};
-  if (p.unit_ctas > 0) {
-    r.L = clamp_len(p, 0);
-    r.ut = unit_tiles(r.L);
-    const UnitCut u = unit_cut(p.unit_ctas, r.ut);
-    r.tpc = u.tpc;
-    r.hr = cta / u.per;
-    r.lt = (cta - r.hr * u.per) * u.tpc;
-    r.t_end = r.hr < HR ? min(u.tpc, r.ut - r.lt) : 0;
-    return r;
-  }
+  RangeStart r{0, 0, 0, 0, 0, 0, 0, 0, 0};
   // A lane's cache of 32 from c0 on: its length, and the tiles up to and including it.
-  int L = 0, upto = 0;
+  int L = 0, upto = 0, total = 0, longest = 0;
   auto sum = [&](int c0) {
     const int c = c0 + lane;
     L = c < p.C ? clamp_len(p, c) : 0;
-    upto = c < p.C ? unit_tiles(L) * HR : 0;
+    upto = c < p.C ? unit_tiles(L) : 0;
+    longest = max(longest, upto);
+    upto *= HR;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int x = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += x;
     }
   };
-  int total = 0;
+  r.per = kp.ctas_per_unit;
+  const bool alone = p.C == 1 && r.per > 0;  // (needs no sums)
 #pragma unroll 1
-  for (int c0 = 0; c0 < p.C; c0 += 32) {
+  for (int c0 = 0; !alone && c0 < p.C; c0 += 32) {
     sum(c0);
     total += __shfl_sync(0xffffffffu, upto, 31);
   }
   r.tpc = tiles_per_cta(total, p.num_ctas);
-  r.t = min(total, cta * r.tpc);
+  if (alone || (r.per > 0 && tiles_per_cta(__reduce_max_sync(0xffffffffu, longest), r.per) <= r.tpc + kp.spare_tiles)) {
+    const int unit = kMerge ? blockIdx.x : blockIdx.x / r.per, piece = kMerge ? 0 : blockIdx.x - unit * r.per;
+    r.c = kp.by_cache(unit);
+    r.hr = unit - r.c * HR;
+    if (r.c < p.C) {
+      r.L = clamp_len(p, r.c);
+      r.ut = unit_tiles(r.L);
+      r.tpc = tiles_per_cta(r.ut, r.per);
+      r.lt = piece * r.tpc;
+      r.t_end = max(0, min(r.tpc, r.ut - r.lt));
+    }
+    return r;
+  }
+  r.per = 0;
+  r.t = min(total, static_cast<int>(blockIdx.x + kMerge) * r.tpc);
   r.t_end = min(total, r.t + r.tpc);
   int below = 0, c0 = 0;
 #pragma unroll 1
@@ -255,7 +270,7 @@ constexpr int kFirstBytes = sizeof(TileMeta) + 16;
 // t_end and L in place of a tile's, then hr and lt.
 __device__ __forceinline__ void plan_loader(const Kv4Params& kp, const Ring& sm) {
   const AttnParams& p = kp.a;
-  const RangeStart r = range_of(kp, blockIdx.x);
+  const RangeStart r = range_of<false>(kp);
   if ((threadIdx.x & 31) == 0) {
     const int h = kp.by_blocks(r.hr);
     *sm.issued = 0;

@@ -174,3 +174,12 @@ def test_windows_about_as_long_as_the_context(window, tree, nodes):
     from tests.test_gpu_kv4 import Case, _tree
     par = _tree(np.random.default_rng(nodes), 1, nodes, 2) if tree else None
     Case([300], nodes=nodes, query=nodes, parent=par, window=window, sinks=2, seed=nodes).check()
+
+
+@pytest.mark.parametrize("lens", [(900, 1000, 900, 1000), (900, 10, 2500, 0)])
+@pytest.mark.parametrize("nodes", [2, 4, 8, 12, 16])
+@pytest.mark.parametrize("num_ctas", [8, 9, 16, 17, 23, 40])
+def test_cuts(lens, nodes, num_ctas):
+    """Eight units on as many CTAs and more: whole, cut by themselves (equal lengths), or laid end to end (unequal ones)."""
+    from tests.test_gpu_kv4 import Case
+    Case(list(lens), hq=8, hkv=2, nodes=nodes, query=nodes, num_ctas=num_ctas, seed=nodes).check()
