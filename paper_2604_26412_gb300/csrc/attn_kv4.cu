@@ -70,7 +70,7 @@ struct Cfg {
   static_assert(kTmemO + NC <= 512, "tensor memory");
 };
 
-constexpr int kRowSets = 4;  // more than the pieces between the warp that builds one and its last reader
+constexpr int kRowSets = 4;  // sets of rows, of as many pieces
 
 struct Smem : Ring {
   Rows* rows;                        // [kRowSets]
@@ -79,14 +79,14 @@ struct Smem : Ring {
   uint32_t qkdone, pfull, pvdone;    // [2] QK^T done; P written (and S read); P.V done
   uint32_t qfull, qempty;            // [2] q of a piece staged; its last QK^T done
   uint32_t ofree, mmadone;           // epilogue has read O; [2] every MMA issued is done
-  uint32_t rfull;                    // [kRowSets] a piece's rows built
+  uint32_t rfull, rfree;             // [kRowSets] a piece's rows built; the piece ended
   float *ref, *alpha;                // [64] per row (ref: negated)
   float* sums;                       // [softmax warp][16] of a piece's rows
   int* wmax;                         // [softmax warp][64] per warp and row
   uint32_t* tmem;
 };
 
-constexpr int kBarriers = 18 + kRowSets;  // besides the ring's (an even number: what follows is aligned to 16 bytes)
+constexpr int kBarriers = 18 + 2 * kRowSets;  // besides the ring's (an even number: what follows is aligned to 16 bytes)
 
 template <class CF>
 __host__ __device__ constexpr size_t smem_bytes() {
@@ -119,6 +119,7 @@ __device__ __forceinline__ Smem carve(uint8_t* raw) {
   s.mmadone = s.qempty + 16;
   s.ofree = s.mmadone + 16;
   s.rfull = s.ofree + 16;
+  s.rfree = s.rfull + 8 * kRowSets;
   s.rows = reinterpret_cast<Rows*>(b + 8 * (2 * CF::kStages + kBarriers));
   s.ref = reinterpret_cast<float*>(s.rows + kRowSets);
   s.alpha = s.ref + 64;
@@ -181,6 +182,8 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) mbar_arrive(sm.qfull + 8 * b);
+    // A set's last reader is the end of a piece, at the latest of the fourth before this one.
+    if (!wait(sm.rfree + 8 * (piece & (kRowSets - 1)), ((piece / kRowSets) & 1) ^ 1u)) return;
     if (w.flags & kNewRows) {
       // (A set of another row block has the tree of the one before it copied along.)
       const int before = set & (kRowSets - 1);
@@ -572,7 +575,10 @@ __device__ __forceinline__ void run_softmax(const Kv4Params& kp, const Smem& sme
     write_rows(p, sm.rows[set], tile_meta(sm, t), col0, all, ref, o_cols, in_codes ? p.v_scale : 1.f);
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) mbar_arrive(sm.ofree);
+    if (lane == 0) {
+      mbar_arrive(sm.ofree);
+      mbar_arrive(sm.rfree + 8 * (piece & (kRowSets - 1)));
+    }
     return true;
   };
 #pragma unroll 1
@@ -675,12 +681,12 @@ __global__ void __launch_bounds__(CF::kThreads, 1) attn_kv4_kernel(const __grid_
   const Smem sm = carve<CF>(smem_raw);
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) init_waits(p);
-  static_assert(2 * CF::kStages + kBarriers <= 32, "a lane for each barrier");
   if (threadIdx.x < 2 * CF::kStages + kBarriers) {
     // Arrivals, in the order of carve(): the ring (of a stage, a decoding warpgroup's warps and the one that stages q), K and
     // V decoded, then the rest.
     const int j = threadIdx.x - 2 * CF::kStages;
-    const int n = j < -CF::kStages ? 1 : j < 0 ? 5 : j < 4 ? 4 : (j >> 1) == 3 || (j >> 1) == 8 ? 4 * CF::kGroups : 1;
+    const bool softmax = (j >> 1) == 3 || (j >> 1) == 8 || j >= 18 + kRowSets;  // P written, O read, a piece ended
+    const int n = softmax ? 4 * CF::kGroups : j < -CF::kStages ? 1 : j < 0 ? 5 : j < 4 ? 4 : 1;
     mbar_init(sm.cfull + 8 * threadIdx.x, n);
     fence_mbar_init();
   }

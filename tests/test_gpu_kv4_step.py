@@ -183,3 +183,18 @@ def test_cuts(lens, nodes, num_ctas):
     """Eight units on as many CTAs and more: whole, cut by themselves (equal lengths), or laid end to end (unequal ones)."""
     from tests.test_gpu_kv4 import Case
     Case(list(lens), hq=8, hkv=2, nodes=nodes, query=nodes, num_ctas=num_ctas, seed=nodes).check()
+
+
+@pytest.mark.parametrize("lens", [[0] * 40, [0, 3] * 20, [0, 130, 0, 0, 0, 1] * 7])
+@pytest.mark.parametrize("nodes,hq", [(12, 8), (33, 8), (2, 8), (40, 8), (9, 8)])
+@pytest.mark.parametrize("num_ctas", [1, 3])
+def test_many_short_pieces_to_a_cta(lens, nodes, hq, num_ctas):
+    """Pieces of one or two tiles, each of another tree: what a piece's end still reads must outlast the next ones' starts."""
+    from tests.test_gpu_kv4 import Case, _tree
+    par = _tree(np.random.default_rng(nodes), len(lens), nodes, 3)
+    case = Case(list(lens), hq=hq, hkv=2, nodes=nodes, query=nodes, parent=par, num_ctas=num_ctas, seed=nodes)
+    case.check(caches=range(0, len(lens), 3))
+    first = case.run()
+    for _ in range(5):
+        again = case.run()
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
