@@ -29,8 +29,9 @@
 //  - What a piece needs beside its tiles is made beside them: rows' tables after q (69 -> 64 us), the CTA's plan and first
 //    q before its first tile (64 -> 61.7), tables by jumps and whole nodes (59.6 -> 53.8), a warpgroup that ends its rows
 //    by itself (53.5 -> 49.8).
-// Measured, attention and merge: 48 rows 49.8 us, 256 rows 172 us (the tree's 64 nodes in four blocks, each of which
-// decodes the cache for itself).
+// Measured, attention and merge: 32 rows 42 us, 48 rows 49.5, 64 rows 55.8, 256 rows 170 (the tree's 64 nodes in four
+// blocks, each of which decodes the cache for itself).  Many short contexts cost their pieces: 82 caches of 5 tokens, 48
+// rows, 656 pieces of three tiles 60 us (20k cycles each, most of it code fetched anew).
 // Work plan: the units' tiles laid end to end and cut into equal ranges, one per persistent CTA (kvshot_internal.h);
 // with a window a unit's tiles are those of the sinks and those of the window.
 #include <algorithm>
