@@ -21,7 +21,7 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) %
 // What bounds an extension: a chain of dependent loads (lengths, the pages they join, the free pages, the table) between
 // two barriers, 6 us in a graph for 64 caches; its bytes would take 0.04.  So a small one is one launch, of a cluster whose
 // CTAs make the plan each for itself and check the pages taken each in part (one CTA, loads one at a time: 20 us for
-// 65k pages), and a large one is two, the second of many CTAs (256 prompts of up to 8191 tokens 16.6 us; in one cluster 88.
+// 65k pages), and a large one is two, the second of many CTAs (256 prompts of up to 8191 tokens 14.8 us; in one cluster 88.
 // 64 caches of 1 to 8 new tokens 8.4 us, in two launches 9.2).
 constexpr int kPlanThreads = 1024;  // one cache each
 static_assert(kPlanThreads >= kMaxCaches, "a thread per cache");
@@ -49,39 +49,38 @@ __device__ __forceinline__ int pages_of(const ExtendParams& p, int tokens) {
   return q + (q * p.P < tokens ? 1 : 0);
 }
 
-// Sums over the threads up to and including this one, of two numbers; `warp_sums` [2][32] is scratch.  *total_a, *total_b:
-// over the block.
-__device__ __forceinline__ void block_scan(int64_t& a, int64_t& b, int64_t* warp_sums, int64_t* total_a, int64_t* total_b) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+// Sums over the threads up to and including this one, of two numbers below 2^31 each; `warp_sums` [64] is scratch.
+// *total_a, *total_b: over the block.  Sums stop at 2^31 - 1, which no call's max_tokens allows (nor, with it, the pages of so
+// many tokens).
+__device__ __forceinline__ uint32_t sum31(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }
+__device__ __forceinline__ void warp_scan(uint32_t& a, uint32_t& b, int lane) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, a, o), y = __shfl_up_sync(0xffffffffu, b, o);
+    const uint32_t x = __shfl_up_sync(0xffffffffu, a, o), y = __shfl_up_sync(0xffffffffu, b, o);
     if (lane >= o) {
-      a += x;
-      b += y;
+      a = sum31(a, x);
+      b = sum31(b, y);
     }
   }
-  __syncthreads();
+}
+__device__ __forceinline__ void block_scan(uint32_t& a, uint32_t& b, uint32_t* warp_sums, uint32_t* total_a, uint32_t* total_b) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  warp_scan(a, b, lane);
   if (lane == 31) {
     warp_sums[warp] = a;
     warp_sums[32 + warp] = b;
   }
   __syncthreads();
   // Each warp sums the warps' numbers: lane w those up to warp w.
-  int64_t sa = lane < warps ? warp_sums[lane] : 0, sb = lane < warps ? warp_sums[32 + lane] : 0;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, sa, o), y = __shfl_up_sync(0xffffffffu, sb, o);
-    if (lane >= o) {
-      sa += x;
-      sb += y;
-    }
-  }
+  uint32_t sa = lane < warps ? warp_sums[lane] : 0, sb = lane < warps ? warp_sums[32 + lane] : 0;
+  warp_scan(sa, sb, lane);
   *total_a = __shfl_sync(0xffffffffu, sa, 31);
   *total_b = __shfl_sync(0xffffffffu, sb, 31);
-  const int64_t below_a = __shfl_sync(0xffffffffu, sa, max(warp - 1, 0)), below_b = __shfl_sync(0xffffffffu, sb, max(warp - 1, 0));
-  a += warp > 0 ? below_a : 0;
-  b += warp > 0 ? below_b : 0;
+  const uint32_t below_a = __shfl_sync(0xffffffffu, sa, max(warp - 1, 0)), below_b = __shfl_sync(0xffffffffu, sb, max(warp - 1, 0));
+  if (warp > 0) {
+    a = sum31(a, below_a);
+    b = sum31(b, below_b);
+  }
 }
 
 // Whether the call can be met at all (the same answer in all threads of the cluster), and what this thread's cache gets:
@@ -93,7 +92,7 @@ struct CachePlan {
   int free_count, need, total;  // before the call; of all caches
 };
 struct PlanShared {
-  int64_t sums[64];
+  uint32_t sums[64];
   int ok[kExtendCluster];  // a CTA's answer to the pages it checked
 };
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
@@ -108,15 +107,16 @@ __device__ __forceinline__ bool extend_plan(const ExtendParams& p, PlanShared& s
   ok = ok && after <= p.max_pages;
   int joined = 0;  // the page that the first new token joins (looked at after the sums, which its load need not hold up)
   if (ok && c < p.C && n > 0 && L % p.P != 0) joined = p.page_table[static_cast<size_t>(c) * p.max_pages + used - 1];
-  int64_t pages = after - used, tokens = n, need, total;
+  const uint32_t own = ok ? static_cast<uint32_t>(after - used) : 0;  // (at most max_pages)
+  uint32_t pages = own, tokens = ok ? n : 0, need, total;
   block_scan(pages, tokens, s.sums, &need, &total);
-  ok = ok && need <= F && total <= p.max_tokens && joined >= 0 && joined < p.num_pages;
+  ok = ok && need <= static_cast<uint32_t>(F) && total <= static_cast<uint32_t>(p.max_tokens) && joined >= 0 && joined < p.num_pages;
   ok = __syncthreads_and(ok);
   bool good = ok;
   if (ok) {  // (eight loads of a thread in flight)
     constexpr int threads = kExtendCluster * kPlanThreads;
 #pragma unroll 1
-    for (int64_t i0 = F - need + blockIdx.x * kPlanThreads + threadIdx.x; i0 < F; i0 += 8 * threads) {
+    for (int64_t i0 = F - static_cast<int64_t>(need) + blockIdx.x * kPlanThreads + threadIdx.x; i0 < F; i0 += 8 * threads) {
       int pid[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) pid[i] = i0 + i * threads < F ? p.free_pages[i0 + i * threads] : 0;
@@ -135,7 +135,7 @@ __device__ __forceinline__ bool extend_plan(const ExtendParams& p, PlanShared& s
   cluster_wait();
 #pragma unroll
   for (int i = 0; i < kExtendCluster; ++i) ok = ok && s.ok[i] != 0;
-  *out = CachePlan{L, n, static_cast<int>(tokens) - n, static_cast<int>(pages - (after - used)), F, static_cast<int>(need),
+  *out = CachePlan{L, n, static_cast<int>(tokens - n), static_cast<int>(pages - own), F, static_cast<int>(need),
                    static_cast<int>(total)};
   return ok;
 }
@@ -240,27 +240,41 @@ __global__ void __cluster_dims__(kExtendCluster, 1, 1) __launch_bounds__(kPlanTh
 }
 
 __global__ void __launch_bounds__(kFillThreads) extend_fill_kernel(const __grid_constant__ ExtendParams p) {
-  __shared__ int64_t scratch[64];
+  __shared__ int sums[kFillThreads / 32];
   __shared__ ExtendPlan s;
   wait_for_prerequisite_grid();
-  int64_t base = 0;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int base = 0;  // (what the plan grants is below 2^31 pages)
   for (int c0 = 0; c0 < p.C; c0 += kFillThreads) {
     const int c = c0 + threadIdx.x;
-    int64_t need = 0, none = 0, total, zero;
+    int need = 0;
     if (c < p.C) {
       const int a = p.token_start[c], n = p.token_start[c + 1] - a, L = p.seq_lens_out[c] - n;
       s.start[c] = a;
       s.len[c] = L;
       need = pages_of(p, L + n) - pages_of(p, L);
     }
-    int64_t upto = need;
-    block_scan(upto, none, scratch, &total, &zero);
-    if (c < p.C) s.base[c] = static_cast<int>(base + upto - need);
-    base += total;
+    int upto = need;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 31) sums[warp] = upto;
+    __syncthreads();
+    int below = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kFillThreads / 32; ++w) {
+      below += w < warp ? sums[w] : 0;
+      all += sums[w];
+    }
+    if (c < p.C) s.base[c] = base + below + upto - need;
+    base += all;
+    __syncthreads();
   }
   if (threadIdx.x == 0) s.start[p.C] = p.token_start[p.C];
   __syncthreads();
-  extend_fill(p, s, *p.free_count_out + static_cast<int>(base), blockIdx.x * kFillThreads + threadIdx.x, gridDim.x * kFillThreads);
+  extend_fill(p, s, *p.free_count_out + base, blockIdx.x * kFillThreads + threadIdx.x, gridDim.x * kFillThreads);
 }
 
 // ------------------------------------------------------------ store, load

@@ -198,3 +198,19 @@ def test_many_short_pieces_to_a_cta(lens, nodes, hq, num_ctas):
     for _ in range(5):
         again = case.run()
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("counts", [[2 ** 30] * 4, [2 ** 30] * 2, [2 ** 31 - 1, 1], [1, 0, 2 ** 30 + 5] * 300])
+def test_an_extension_beyond_32_bits_takes_nothing(counts):
+    """Token counts whose sums pass 2^31 and 2^32."""
+    c, page = len(counts), 1 << 20
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    lens, new, free, count = i32([0] * c), i32(counts), i32(list(range(2000))), i32([2000])
+    table = i32(np.full((c, 2047), 7).tolist())
+    start, maps, err = i32([-5] * (c + 1)), [i32([0] * 64) for _ in range(3)], i32([0])
+    desc = kvshot.make_extend_desc(num_caches=c, page_size=page, max_pages_per_seq=2047, num_pages=2000, max_tokens=64,
+                                   err_flag=err)
+    kvshot.cache_extend(desc, lens, new, table, free, count, lens, table, count, start, *maps)
+    assert int(err.item()) == kvshot.KVSHOT_ERR_DEVICE_BOUNDS
+    assert int(lens.abs().max()) == 0 and int(count.item()) == 2000 and bool((table == 7).all())
+    assert int(start.abs().max()) == 0 and all(bool((m == -1).all()) for m in maps)
