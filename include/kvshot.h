@@ -111,8 +111,8 @@ typedef struct kvshot_attn_desc {
   void* workspace;           /* device scratch, 256-byte aligned; see kvshot_draft_attn_workspace_size */
   size_t workspace_bytes;
   int32_t* err_flag;         /* optional device int32, 0 before the call; see conventions above */
-  int32_t k_scale_exp;       /* KVSHOT_TARGET_FP8: target keys are e4m3 x 2^k_scale_exp, |exp| <= 64 */
-  int32_t v_scale_exp;       /* KVSHOT_TARGET_FP8: target values are e4m3 x 2^v_scale_exp, |exp| <= 64 */
+  int32_t k_scale_exp;       /* KVSHOT_TARGET_FP8: target keys are e4m3 x 2^k_scale_exp, |exp| <= 64 (and the 4-bit cache's) */
+  int32_t v_scale_exp;       /* KVSHOT_TARGET_FP8: target values are e4m3 x 2^v_scale_exp, |exp| <= 64 (likewise) */
   uint32_t wait_limit_ns;    /* watchdog: longest any one wait of the attention kernels' load/compute
                                 pipeline may take, in ns; 0 = 2 s.  A wait that runs past it records
                                 KVSHOT_ERR_TIMEOUT; the kernel then stops computing, waits (2 s at most
