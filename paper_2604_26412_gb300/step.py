@@ -8,7 +8,8 @@ once and attend together (whole-tree verification shape).  The target prefix is
 bf16, fp8 or 4 bits; the 4-bit cache grows between steps (kv4.Kv4Cache).
 
 Only device memory is handled here (torch allocations); all arithmetic runs
-in libkvshot's kernels.
+in libkvshot's kernels, but for one sum: over a 4-bit cache a step first adds
+the cache's present lengths to the nodes' places behind the prefix.
 """
 from __future__ import annotations
 
@@ -30,7 +31,8 @@ class DraftStep:
         qk_norm: optional (q_norm_w, k_norm_w, eps): the append normalises q and k per head first
         (kvshot_draft_append_qknorm).
         target_kv4: optional 4-bit cache to attend, with its own lengths and tables, instead of inp's target cache;
-        then also window and sinks (kvshot_draft_attn_kv4)."""
+        then also window and sinks (kvshot_draft_attn_kv4).  Its draft tokens stand behind the lengths that the cache has
+        when run() comes to them in stream order: inp's positions only say how far behind inp's lengths a node stands."""
         if mode not in ("per_depth", "whole"):
             raise ValueError(mode)
         if target_kv4 is None and (window or sinks):
@@ -66,6 +68,8 @@ class DraftStep:
             self.k_in = [torch.cat(inp.k_in, dim=1)]
             self.v_in = [torch.cat(inp.v_in, dim=1)]
             self.pos = [torch.cat(inp.positions, dim=1).contiguous()]
+        if target_kv4 is not None:
+            self._places_behind_the_cache()
         self.q_rot: List[torch.Tensor] = [torch.empty_like(q) for q in self.q_in]
         self.out: List[torch.Tensor] = [torch.empty_like(q) for q in self.q_in]
         self.lse: List[torch.Tensor] = [torch.empty(q.shape[:3], dtype=torch.float32, device=dev) for q in self.q_in]
@@ -105,8 +109,25 @@ class DraftStep:
         """Draft tokens produced per step (a token attending several reused layers counts once)."""
         return self.inp.spec.num_seqs * self.inp.spec.n_nodes
 
+    def _places_behind_the_cache(self) -> None:
+        """Positions of the step's own, and the sums that fill them: consecutive levels of one width take one launch."""
+        behind = [p - self.inp.seq_lens[:, None] for p in self.pos]
+        C, self.pos, self._sums, i = len(self.inp.seq_lens), [], [], 0
+        while i < len(behind):
+            j, n = i, behind[i].shape[1]
+            while j < len(behind) and behind[j].shape[1] == n:
+                j += 1
+            place = torch.empty((j - i, C, n), dtype=torch.int32, device=self.device)
+            self._sums.append((torch.stack(behind[i:j]), place))
+            self.pos += list(place.unbind())
+            i = j
+
     def run(self, stream: Optional[torch.cuda.Stream] = None) -> None:
         inp = self.inp
+        if self.kv4 is not None:
+            with kvshot.torch_stream(stream):
+                for behind, place in self._sums:
+                    torch.add(behind, self.kv4.seq_lens[:, None], out=place)
         stream = kvshot._stream(stream)  # once for all calls
         n0 = 0
         for i, n_step in enumerate(self.levels):

@@ -1,0 +1,139 @@
+"""Drafting over a 4-bit cache that grows: the draft tokens' places behind the grown prefix.
+
+Positions here come from the cache's own lengths and the nodes' depths (a node of depth d stands at L + d - 1), not from
+the step.  The appended q and K have to be the oracle's bits at those positions; bounds of the attention as in
+tests/test_gpu_kv4.py.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv4, oracle
+from paper_2604_26412_gb300 import kv4 as user
+from paper_2604_26412_gb300 import workloads as wl
+from paper_2604_26412_gb300.step import DraftStep
+from tests.test_gpu_kv4 import LSE_MAX_ABS, OUT_MAX_ABS, OUT_REL_L2
+
+pytestmark = pytest.mark.gpu
+HKV = 2
+
+
+def _inputs(levels, tree=True, layers=1, lens=(40, 0, 129), paged=True, seed=3):
+    spec = wl.Spec("kv4-growth", len(lens) // layers, layers, list(lens), levels, tree, paged, page_size=16, hq=8,
+                   hkv=HKV, seed=seed)
+    return spec, wl.make_inputs(spec, "cuda", seed=seed, tail_fill="nan")
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _rows(t, seed=0):
+    gen = torch.Generator("cuda").manual_seed(seed)
+    return [torch.randn((t, HKV, 128), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2)]
+
+
+def _wide(bits):
+    return wl.bits_to_bf16(bits).double().numpy()
+
+
+def _check(step, inp, cache):
+    """The last step against append and attention at the places behind the cache's present lengths."""
+    s = inp.spec
+    lens, table = cache.seq_lens.cpu().numpy(), cache.page_table.cpu().numpy()
+    parent = inp.tree_parent.cpu().numpy()
+    depth = np.zeros(parent.shape, np.int64)
+    for i in range(parent.shape[1]):
+        up = parent[:, i]
+        depth[:, i] = np.where(up < 0, 0, depth[np.arange(len(up)), up]) + 1
+    dk = np.full((s.num_caches, s.hkv, inp.n_max, 128), 0x7FC0, np.uint16)
+    dv = dk.copy()
+    d = oracle.make_desc(num_caches=s.num_caches, num_seqs=s.num_seqs, hq=s.hq, hkv=s.hkv, head_dim=128, n_nodes=0,
+                         n_query=0, n_max=inp.n_max, tree=s.tree, l_cap=1)
+    n0 = 0
+    for i, n in enumerate(step.levels):
+        pos = lens[:, None] + depth[np.arange(s.num_caches) // s.layers, n0:n0 + n] - 1
+        q = oracle.append(d, wl.bf16_bits(step.q_in[i]), wl.bf16_bits(step.k_in[i]), wl.bf16_bits(step.v_in[i]),
+                          pos.astype(np.int32), n0, n, s.rope_base, dk, dv)
+        n0 += n
+        assert np.array_equal(wl.bf16_bits(step.q_rot[i]), q), i
+        assert np.array_equal(wl.bf16_bits(step.draft_k[:, :, n0 - n:n0]), dk[:, :, n0 - n:n0]), i
+        for c in range(s.num_caches):
+            slots = [table[c, j // cache.page_size] * cache.page_size + j % cache.page_size for j in range(lens[c])]
+            k, v = (x.double().cpu().numpy().swapaxes(0, 1) for x in cache.values(_i32(slots)))
+            par = parent[c // s.layers, :n0] if s.tree else None
+            out, lse = kv4.attn(_wide(q[c]), k, v, _wide(dk[c, :, :n0]), _wide(dv[c, :, :n0]), par, step.window,
+                                step.sinks, 128 ** -0.5)
+            o, l = step.out[i][c].double().cpu().numpy(), step.lse[i][c].double().cpu().numpy()
+            assert np.abs(o - out).max() <= OUT_MAX_ABS, (i, c)
+            assert np.linalg.norm(o - out) <= OUT_REL_L2 * np.linalg.norm(out), (i, c)
+            assert np.abs(l - lse).max() <= LSE_MAX_ABS, (i, c)
+    assert step.error_code() == 0 and cache.error_code() == 0
+
+
+# ------------------------------------------------------------------ places of the draft tokens
+
+@pytest.mark.parametrize("mode", ["per_depth", "whole"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (24, 5)])
+@pytest.mark.parametrize("levels,tree,layers", [([2, 3], True, 1), ([1, 1, 1], False, 3), ([2, 2, 4, 4, 1], True, 1)])
+def test_draft_tokens_stand_behind_the_grown_prefix(mode, window, sinks, levels, tree, layers):
+    _, inp = _inputs(levels, tree, layers)
+    cache = user.of_inputs(inp, spare_pages=8, spare_tokens=60)
+    step = DraftStep(inp, mode=mode, target_kv4=cache, window=window, sinks=sinks)
+    step.run()
+    _check(step, inp, cache)
+    for new in ([3, 1, 0], [0, 17, 8]):
+        cache.grow(_i32(new), *_rows(sum(new), seed=sum(new)))
+        step.run()
+        _check(step, inp, cache)
+
+
+def test_draft_tokens_stand_behind_the_grown_prefix_in_a_replayed_graph():
+    _, inp = _inputs([2, 3])
+    cache = user.of_inputs(inp, spare_pages=8, spare_tokens=40)
+    step = DraftStep(inp, target_kv4=cache, window=30, sinks=2)
+    new, (k, v) = _i32([2, 5, 1]), _rows(8)
+    cache.grow(new, k, v)  # (uncaptured: what a first call sets up)
+    step.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.grow(new, k, v)
+        step.run()
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(step, inp, cache)
+
+
+def test_a_cache_of_other_lengths_than_the_inputs():
+    _, inp = _inputs([2, 3])
+    cache = user.Kv4Cache(3, HKV, 20, 8, max_tokens=100)
+    cache.grow(_i32([7, 70, 20]), *_rows(97))
+    step = DraftStep(inp, target_kv4=cache)
+    step.run()
+    _check(step, inp, cache)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_a_step_on_another_stream(handle):
+    """The places are found on the step's stream, after the growth that stands there before it."""
+    _, inp = _inputs([2, 3])
+    cache = user.of_inputs(inp, spare_pages=8, spare_tokens=40)
+    step = DraftStep(inp, target_kv4=cache)
+    new, (k, v) = _i32([2, 5, 1]), _rows(8)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+    on = s.cuda_stream if handle else s
+    cache.grow(new, k, v, stream=on)
+    step.run(on)
+    torch.cuda.synchronize()
+    _check(step, inp, cache)
+
+
+def test_the_steps_of_the_other_caches_keep_their_places():
+    _, inp = _inputs([2, 3])
+    step = DraftStep(inp)
+    assert all(a is b for a, b in zip(step.pos, inp.positions))
