@@ -71,8 +71,6 @@ struct Cfg {
   static_assert(kTmemO + NC <= 512, "tensor memory");
 };
 
-constexpr int kRowSets = 4;  // sets of rows, of as many pieces
-
 struct Smem : Ring {
   Rows* rows;                        // [kRowSets]
   uint32_t v, p, q;                  // shared-memory addresses
@@ -291,14 +289,24 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
     if (lane == 0) mbar_arrive(kfull);
     // V's buffer: P.V of its previous tile is done.
     if (!wait(pvdone, freed)) return;
+    bool seen = true;
+    if (flags & kMasked) {
+      // Keys that no row sees count as zeros; whether one does, for drafts and in a window, the piece's rows say.  (The phase
+      // is theirs: the fourth piece before has its rows, since they are built before q of the next piece is staged, and the
+      // products of the tile before the last, whose K this warp has replaced, have had their q.)
+      const int4 meta = tile_words(sm, t);
+      const uint32_t piece = static_cast<uint32_t>(meta.x) >> kPieceShift, set = static_cast<uint32_t>(meta.x) >> kSetShift;
+      if (draft || kp.window > 0) {
+        if (!wait(sm.rfull + 8 * (piece % kRowSets), piece / kRowSets & 1u)) return;
+        const Rows& rows = sm.rows[set % kRowSets];
+        seen = any_row(rows, rows_seeing(kp, rows, meta, tile_meta(sm, t).rb, key));
+      } else {
+        seen = key < meta.z;
+      }
+    }
     if (!draft) {
       uint2 sc = lds64(src + scale0 + kScaleBytes);
-      if (flags & kMasked) {
-        const int4 meta = tile_words(sm, t);  // flags, key0, nkeys, L
-        // Keys that no row sees may hold anything; V of them must not be NaN (0 * NaN; any code times 0 is 0).
-        const int at = meta.y + key, lo = kp.window > 0 ? meta.w + kp.min_depth - kp.window : 0;
-        if (key >= meta.z || (at < lo && at >= kp.sinks)) sc = make_uint2(0u, 0u);
-      }
+      if (!seen) sc = make_uint2(0u, 0u);  // (any code times 0 is 0)
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
         uint32_t o[16];
@@ -308,7 +316,7 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
         sc.y >>= 16;
       }
     } else {
-      decode_draft<true>(draft0 + kDraftV + stage * kStageSize, key < tile_words(sm, t).z, vdst, sw);
+      decode_draft<true>(draft0 + kDraftV + stage * kStageSize, seen, vdst, sw);
     }
     fence_proxy_async_smem();
     __syncwarp();

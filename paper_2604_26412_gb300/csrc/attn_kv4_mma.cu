@@ -217,13 +217,16 @@ __device__ __forceinline__ void softmax_step(State<NR>& st, const float (&s)[KG]
       }
 }
 
-// Keys that the rows' masks hide: scores of key `key` (of the tile) of s[...][nr][2 a + e].
+// Keys that the rows' masks hide: scores of keys `key` and `key` + 8 (of the tile) of s[...][nr][2 a + e].  Returns whether
+// any row sees them, as bits.
 template <int NR>
-__device__ __forceinline__ void hide(float (&s)[NR][4], const Kv4Params& kp, const Rows& rows, const int4& meta, int rb, int key,
-                                     int q4) {
+__device__ __forceinline__ uint32_t hide(float (&s)[NR][4], const Kv4Params& kp, const Rows& rows, const int4& meta, int rb,
+                                         int key, int q4) {
+  uint32_t seen = 0;
 #pragma unroll 1
   for (int a = 0; a < 2; ++a) {
-    const uint64_t vis = rows_seeing(kp, rows, meta, rb, key + 8 * a) >> (2 * q4);
+    const uint64_t all = rows_seeing(kp, rows, meta, rb, key + 8 * a), vis = all >> (2 * q4);
+    seen |= static_cast<uint32_t>(any_row(rows, all)) << a;
 #pragma unroll
     for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
@@ -233,6 +236,7 @@ __device__ __forceinline__ void hide(float (&s)[NR][4], const Kv4Params& kp, con
           else s[nr][2 + e] = -INFINITY;
         }
   }
+  return seen;
 }
 
 // Prefix keys, 8 rows: a row of depth d sees the sinks and the positions from L + d - window on.  `from`: of rows 2 q4 + e.
@@ -374,7 +378,7 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
           uint4 sc[2] = {lds128(vat + vscale), lds128(vat + vscale + 64)};  // tokens 2 q4, 2 q4 + 1 and those + 8
           if (masked) {
             // Keys that no row sees may hold anything, NaN scales among it: 0 times them must be 0.
-            const int lo = kp.window > 0 ? meta.w + kp.min_depth - kp.window : 0;
+            const int lo = kp.window > 0 ? meta.w + sm.rows->min_depth - kp.window : 0;
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
               const int key = kw + 16 * i + 8 * a + 2 * q4, pos = meta.y + key;
@@ -428,7 +432,9 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
             mma_f16(s[0][nr], f[4], f[5], f[6], f[7], q.z, q.w);
           }
         }
-        hide<NR>(s[0], kp, *sm.rows, meta, rb, kw + g, q4);
+        const uint32_t seen = hide<NR>(s[0], kp, *sm.rows, meta, rb, kw + g, q4);
+        // Of keys 8 a .. 8 a + 7, a bit in each lane of theirs: this lane's V are keys 2 q4 and 2 q4 + 1.
+        const uint32_t live[2] = {__ballot_sync(0xffffffffu, seen & 1u) >> (8 * q4), __ballot_sync(0xffffffffu, seen & 2u) >> (8 * q4)};
         uint32_t pb[1][NR][2];
         softmax_step<NR, 1>(st, s, p.qscale, in_codes && p.v_scale != 1.f, in_codes ? p.v_scale : 1.f, pb);
         in_codes = false;
@@ -439,8 +445,8 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
 #pragma unroll
           for (int a = 0; a < 2; ++a) {  // keys 2 q4 + 8 a, + 1: dims 4 g .. 4 g + 3 of the chunk
             uint2 x = lds64(vrow + 8 * a * kDraftRow + 64 * c), y = lds64(vrow + (8 * a + 1) * kDraftRow + 64 * c);
-            if (kw + 2 * q4 + 8 * a >= meta.z) x = make_uint2(0u, 0u);
-            if (kw + 2 * q4 + 8 * a + 1 >= meta.z) y = make_uint2(0u, 0u);
+            if (!(live[a] & 0x01u)) x = make_uint2(0u, 0u);  // (no row sees it, or there is no such key)
+            if (!(live[a] & 0x10u)) y = make_uint2(0u, 0u);
             f[2 * a] = bf16x2_to_f16x2(__byte_perm(x.x, y.x, 0x5410));
             f[2 * a + 1] = bf16x2_to_f16x2(__byte_perm(x.y, y.y, 0x5410));
             f[4 + 2 * a] = bf16x2_to_f16x2(__byte_perm(x.x, y.x, 0x7632));

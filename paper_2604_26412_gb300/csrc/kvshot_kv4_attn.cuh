@@ -2,6 +2,8 @@
 // window, the loader of the cache's bytes, the query rows' nodes and masks, and the bounded waits.
 #pragma once
 
+#include <climits>
+
 #include "kvshot_attn_common.cuh"
 #include "kvshot_kv4.cuh"
 
@@ -53,6 +55,8 @@ constexpr int kWhole = 16;             // (with kLast) the piece is the whole un
 constexpr int kNewRows = 32;           // the query rows' nodes differ from the piece's before
 constexpr int kNewTree = 64;           // and so does the draft tree
 constexpr int kStop = 128;             // no tile: the CTA's work is done
+constexpr int kPieceShift = 8, kSetShift = 11;  // (with kMasked) bits 8 to 10: the piece's number; 11 and 12: its set of rows
+constexpr int kRowSets = 4;            // sets of rows, of as many pieces (tcgen05 kernel)
 struct TileMeta {
   int flags, key0, nkeys, L;  // (and the tile's number above bit 16); first key (token, or draft slot), valid keys, prefix length
   int c, h, rb, seq;          // cache, KV head, row block, sequence
@@ -76,6 +80,7 @@ struct alignas(16) Rows {
   uint64_t upto[kMaxTreeNodes + 1];   // rows whose depth is at most x
   uint64_t anc[kMaxTreeNodes];        // nodes: itself and its ancestors
   int parent[kMaxTreeNodes];          // (of build_rows)
+  int count, min_depth;               // rows that there are; depth of the shallowest of them
 };
 
 // Every wait ends: when its phase completes, when another role has given up, or (which gives up) after the call's limit.
@@ -290,7 +295,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
   const TileMeta first = tile_meta_at(sm.first);
   const int t_end = first.nkeys;
   int t = first.key0, c = first.c, hr = lds32(sm.first + 32), lt = lds32(sm.first + 36);
-  int stage = 0, issued = 0, last_rb = -1, last_seq = -1;
+  int stage = 0, issued = 0, last_rb = -1, last_seq = -1, piece = -1, set = -1;
   uint32_t phase = 0;
   bool waited = false, ok = true;
   // Page ids come 32 to a load, a window of tiles ahead: lane i holds the address of run i % runs of the window's tile
@@ -309,6 +314,9 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
     if (p.tree && seq != last_seq) flags |= kNewRows | kNewTree;
     last_rb = rb;
     last_seq = seq;
+    ++piece;
+    if (flags & kNewRows) ++set;
+    const int masked = kMasked | (piece & (2 * kRowSets - 1)) << kPieceShift | (set & (kRowSets - 1)) << kSetShift;
     t += lt1 - lt;
     // A window: rows see keys from L + their depth - window on (and the sinks); a depth is at most N.
     const int seen_from = kp.window > 0 ? L + p.N - kp.window : 0;
@@ -338,8 +346,8 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
       const bool draft = lt >= span.tiles;
       const int key0 = draft ? (lt - span.tiles) * kDraftTile : key_of(lt);
       const int nkeys = draft ? min(kDraftTile, p.N - key0) : min(kTile, L - key0);
-      if (draft) flags |= kDraft | kMasked;
-      else if (nkeys < kTile || (key0 < seen_from && key0 + kTile > kp.sinks)) flags |= kMasked;
+      if (draft) flags |= kDraft | masked;
+      else if (nkeys < kTile || (key0 < seen_from && key0 + kTile > kp.sinks)) flags |= masked;
       if (lt == lt1 - 1) flags |= last;
       if (draft && !waited) {  // the draft K/V may come from the preceding kernel
         wait_for_prerequisite_grid();
@@ -499,13 +507,21 @@ __device__ __noinline__ void build_rows(const Kv4Params& kp, Rows& r, int nc, in
     }
   }
   const int row0 = rb * p.rows_per_unit;
+  int least = INT_MAX;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const int j = lane + 32 * k, nl = kp.by_group(min(row0 + j, p.rows_total - 1));
+    const int j = lane + 32 * k, nl = kp.by_group(min(row0 + j, p.rows_total - 1));  // (past the last row: its node)
     if (j < nc) {
+      const int depth = p.tree ? __popcll(r.anc[p.N - p.Nq + nl]) : p.N - p.Nq + nl + 1;
       r.place[j] = nl * p.hq + row0 + j - nl * p.G;
-      r.depth[j] = p.tree ? __popcll(r.anc[p.N - p.Nq + nl]) : p.N - p.Nq + nl + 1;
+      r.depth[j] = depth;
+      least = min(least, depth);
     }
+  }
+  least = __reduce_min_sync(0xffffffffu, least);
+  if (lane == 0) {
+    r.count = min(p.rows_per_unit, p.rows_total - row0);
+    r.min_depth = least;
   }
   if (p.tree) {
     // The query nodes one after another, whose rows are neighbours: lane m has the rows of nodes m, m + 32, and of depths.
@@ -553,6 +569,9 @@ __device__ __noinline__ uint64_t rows_seeing(const Kv4Params& kp, const Rows& r,
   }
   return bits;
 }
+// Whether any row of the unit is among them.  The other keys' values count as zeros: what stands there may be anything, and
+// 0 times an infinity or a NaN is none.
+__device__ __forceinline__ bool any_row(const Rows& r, uint64_t bits) { return (bits << (64 - r.count)) != 0; }
 
 }  // namespace
 }  // namespace kvshot
