@@ -435,7 +435,8 @@ kvshot_status kvshot_kv4_load(const kvshot_kv4_desc* desc, const void* cache, co
  *  - window = W > 0: a node at position p (a node of depth d, 1 for a child of the last verified token, stands at
  *    L_c + d - 1; the target token j at j) sees a key that it would see otherwise only if the key's position is above
  *    p - W, or below `sinks`.  A node always sees itself.  window = 0: no window (sinks is not used then).
- *    Target tokens that no query row sees are not read.
+ *    A page is not read, nor its entry of page_table, if it holds no sink and no token that a node of the least depth
+ *    sees: of depth n_nodes - n_query + 1, for a tree 1.  Of other pages, too, most such tokens are not read.
  *  - q, the softmax weights and the draft K/V are rounded to f16 for the tensor cores (finite magnitudes up to 65504;
  *    those below 2^-14 lose bits), the cache's values are exact.  The running sums are fp32.
  *  - A NaN stored in a token or draft slot that some query row sees may reach the other rows of its KV head's group.

@@ -177,16 +177,18 @@ __device__ __forceinline__ bool is_of(uint32_t flags) { return flags < (1u << kT
 // The prefix tiles of a cache of L tokens that some query row may see, with a sliding window: tiles [0, sink_tiles) and,
 // `skip` tiles further on, those from the window's first key to the last one.  (The shallowest query node stands at
 // L + min_depth - 1 and sees keys from L + min_depth - window on.)
+// Of these tiles the groups of 16 tokens [hide0, hide1) hold neither a sink nor a key that the shallowest node sees.
 struct WindowSpan {
-  int tiles, sink_tiles, skip;
+  int tiles, sink_tiles, skip, hide0, hide1;
 };
 __device__ __forceinline__ WindowSpan window_span(const Kv4Params& p, int L) {
   const int all = (L + kTile - 1) / kTile;
-  if (p.window == 0) return WindowSpan{all, all, 0};
-  const int lo = max(0, L + p.min_depth - p.window);
+  if (p.window == 0) return WindowSpan{all, all, 0, 0, 0};
+  const int lo = min(L, max(0, L + p.min_depth - p.window));
   const int sink_tiles = min(all, (min(p.sinks, lo) + kTile - 1) / kTile);
   const int skip = max(0, min(all, lo / kTile) - sink_tiles);
-  return WindowSpan{all - skip, sink_tiles, skip};
+  const int hide0 = p.sinks / kKv4Tokens + (p.sinks % kKv4Tokens > 0);
+  return WindowSpan{all - skip, sink_tiles, skip, hide0, (lo == L ? lo + kKv4Tokens - 1 : lo) / kKv4Tokens};
 }
 
 // ------------------------------------------------------------ loads
@@ -322,23 +324,31 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
     const int seen_from = kp.window > 0 ? L + p.N - kp.window : 0;
     const int32_t* table = p.page_table + (p.paged ? static_cast<size_t>(c) * p.max_pages : 0);
     auto key_of = [&](int x) { return (x < span.sink_tiles ? x : x + span.skip) * kTile; };  // of a prefix tile
-    auto group_of = [&](int x) {  // this lane's first group of the window from tile x on, or -1
+    const int groups = (L + kKv4Tokens - 1) / kKv4Tokens;
+    // A run of groups loses the hidden ones at its two ends, and with them all of it (its page is not looked up then).
+    auto hidden = [&](int g) { return g >= span.hide0 && g < span.hide1; };
+    auto run_end = [&](int g) {  // of the run that holds group g
+      const int end = min((g | (kp.run_groups - 1)) + 1, groups);
+      return hidden(end - 1) ? max(span.hide0, g) : end;
+    };
+    auto group_of = [&](int x) {  // this lane's first group to load of the window from tile x on, or -1
       x += my_tile;
       if (x >= lt1 || x >= span.tiles) return -1;
-      const int g = key_of(x) / kKv4Tokens + my_g0;
-      return g * kKv4Tokens < L ? g : -1;
+      const int g0 = key_of(x) / kKv4Tokens + my_g0, g = hidden(g0) ? span.hide1 : g0;
+      return g < min(g0 + kp.run_groups, groups) ? g : -1;
     };
     auto page_of = [&](int g) { return g < 0 ? 0 : p.paged ? table[kp.by_page(g)] : c; };
     int window = lt, g = group_of(window), pid = page_of(g);
     const uint8_t* src = nullptr;
-    uint32_t bytes = 0;
+    uint32_t bytes = 0, at = 0;  // of this lane's copy, and its place in the tile
 #pragma unroll 1
     for (; lt < lt1; ++lt) {
       if (lt == window) {
         if (p.paged && g >= 0) pid = valid_page_id(p, pid);
         src = kp.cache + ((static_cast<size_t>(pid) * p.hkv + h) * kp.groups_per_page +
                           (p.paged ? g - kp.by_page(g) * kp.groups_per_page : g)) * kKv4Bytes;
-        bytes = g < 0 ? 0 : min(kp.run_groups, (L + kKv4Tokens - 1) / kKv4Tokens - g) * kKv4Bytes;
+        bytes = g < 0 ? 0 : (run_end(g) - g) * kKv4Bytes;
+        at = g % kTileGroups * kKv4Bytes;
         window += ahead;
         g = group_of(window);
         pid = page_of(g);
@@ -353,6 +363,9 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
         wait_for_prerequisite_grid();
         waited = true;
       }
+      const bool mine = !draft && my_tile == lt - (window - ahead);
+      int tx = draft ? nkeys * 4 * kHeadDim : (nkeys + kKv4Tokens - 1) / kKv4Tokens * kKv4Bytes;
+      if (kp.window > 0 && !draft) tx = __reduce_add_sync(0xffffffffu, mine ? bytes : 0);
       ok = wait(sm.cempty + 8 * stage, phase ^ 1u);
       if (!ok) break;
       const uint32_t bar = sm.cfull + 8 * stage, dst = sm.ring + stage * kStageSize;
@@ -360,7 +373,7 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
         const uint32_t m = sm.meta + issued % kMetas * sizeof(TileMeta);
         sts128(m, make_uint4(flags | issued << kTagShift, key0, nkeys, L));
         sts128(m + 16, make_uint4(c, h, rb, seq));
-        mbar_arrive_expect_tx(bar, draft ? nkeys * 4 * kHeadDim : (nkeys + kKv4Tokens - 1) / kKv4Tokens * kKv4Bytes);
+        mbar_arrive_expect_tx(bar, tx);
       }
       __syncwarp();
       if (draft) {
@@ -369,8 +382,8 @@ __device__ __forceinline__ void run_loader(const Kv4Params& kp, const Ring& ring
           bulk_load(dst + lane * kDraftRow, kp.draft_k + row * kHeadDim, 2 * kHeadDim, bar);
           bulk_load(dst + kDraftV + lane * kDraftRow, kp.draft_v + row * kHeadDim, 2 * kHeadDim, bar);
         }
-      } else if (my_tile == lt - (window - ahead) && bytes > 0) {
-        bulk_load(dst + my_g0 * kKv4Bytes, src, bytes, bar);
+      } else if (mine && bytes > 0) {
+        bulk_load(dst + at, src, bytes, bar);
       }
       flags = 0;
       ++issued;
