@@ -571,7 +571,9 @@ __device__ __noinline__ uint64_t rows_seeing(const Kv4Params& kp, const Rows& r,
   // Rows whose node's depth is at most x.  A chain's rows are in the order of depth.
   auto upto = [&](int x) -> uint64_t {
     if (p.tree) return x < 0 ? 0ull : r.upto[min(x, p.N)];
-    const int n = min(x - (p.N - p.Nq), p.Nq) * p.G - rb * p.rows_per_unit;
+    const int nodes = min(x - (p.N - p.Nq), p.Nq);
+    if (nodes <= 0) return 0ull;  // (x may be as low as -L: no product with it)
+    const int n = nodes * p.G - rb * p.rows_per_unit;
     return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull;
   };
   if (!draft) return at < kp.sinks ? ~0ull : upto(at - L + kp.window);

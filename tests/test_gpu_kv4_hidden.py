@@ -9,7 +9,8 @@ import pytest
 import torch
 
 from oracle import kv4
-from tests.test_gpu_kv4 import Case, _i32, _tree
+from paper_2604_26412_gb300 import kvshot
+from tests.test_gpu_kv4 import D, LSE_MAX_ABS, OUT_MAX_ABS, OUT_REL_L2, Case, _i32, _tree
 
 pytestmark = pytest.mark.gpu
 
@@ -105,3 +106,41 @@ def test_a_window_shorter_than_the_chain_sees_no_prefix():
             case = Case([128, 130, 451], hq=hq, hkv=hkv, nodes=query + 20, query=query, window=9, sinks=sinks, seed=query)
             assert min(_poison(case)) > 0
             case.check()
+
+
+# ------------------------------------------------------------------ very long contexts
+
+@pytest.mark.parametrize("group,length", [(8, 3 * 2 ** 27 + 77), (16, 3 * 2 ** 26 + 77), (32, 3 * 2 ** 25 + 77),
+                                          (64, 3 * 2 ** 24 + 77), (200, 3 * 2 ** 22 + 77)])
+@pytest.mark.parametrize("sinks", [5, 130])
+def test_a_window_at_the_end_of_a_very_long_context(group, length, sinks):
+    """Hidden keys in the sinks' last tile, so far from the window that (distance x rows of a node) passes 2^31.  One page
+    of 2^20 tokens stands for all of them; against the same attention to the sinks and the window's tokens alone."""
+    page, window, nodes = 1 << 20, 100, 3
+    gen = torch.Generator("cuda").manual_seed(group)
+    cache = torch.randint(0, 256, (page // 16, 2304), dtype=torch.uint8, device="cuda", generator=gen)
+    cache[:, 2048:] = torch.randint(0x30, 0x40, (page // 16, 256), dtype=torch.uint8, device="cuda", generator=gen)
+    table = torch.zeros((1, -(-length // page)), dtype=torch.int32, device="cuda")
+    bf = lambda *s: torch.randn(s, device="cuda", generator=gen).to(torch.bfloat16)  # noqa: E731
+    q, dk, dv = bf(1, nodes, group, D), bf(1, 1, nodes, D), bf(1, 1, nodes, D)
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    desc = kvshot.make_desc(num_caches=1, num_seqs=1, hq=group, hkv=1, n_nodes=nodes, n_query=1, n_max=nodes,
+                            max_seq_len=length, page_size=page, max_pages_per_seq=table.shape[1], num_pages=1, err_flag=err)
+    ws = torch.empty(kvshot.draft_attn_kv4_workspace_size(desc, window, sinks), dtype=torch.uint8, device="cuda")
+    desc.workspace, desc.workspace_bytes = ws.data_ptr(), ws.numel()
+    q = q[:, -1:].contiguous()
+    out, lse = torch.empty_like(q), torch.empty((1, 1, group), device="cuda")
+    kvshot.draft_attn_kv4(desc, q, cache, table, _i32([length]), dk, dv, None, window, sinks, out, lse)
+    torch.cuda.synchronize()
+    assert int(err.item()) == 0
+    near = 160  # tokens before the end, more than the window reaches
+    at = np.concatenate([np.arange(sinks), np.arange(length - near, length)]) % page
+    parts = kv4.unpack(cache[torch.from_numpy(at // 16).cuda()].cpu().numpy()[None, :, None].swapaxes(0, 1))
+    kc, ks, vc, vs = (x[np.arange(len(at)), 0, at % 16] for x in parts)
+    k, v = kv4.values(kc, ks, 0)[None], kv4.values(vc, vs, 0)[None]
+    ref, ref_lse = kv4.attn(q[0].double().cpu().numpy(), k, v, dk[0].double().cpu().numpy(), dv[0].double().cpu().numpy(),
+                            None, window, sinks, D ** -0.5)
+    o = out[0].double().cpu().numpy()
+    assert np.abs(o - ref).max() <= OUT_MAX_ABS * max(1.0, np.abs(v).max() / 4)
+    assert np.linalg.norm(o - ref) <= OUT_REL_L2 * np.linalg.norm(ref)
+    assert np.abs(lse[0].double().cpu().numpy() - ref_lse).max() <= LSE_MAX_ABS
