@@ -432,6 +432,8 @@ kvshot_status kvshot_kv4_load(const kvshot_kv4_desc* desc, const void* cache, co
  *    NULL, desc->l_cap a multiple of 16), 16-byte aligned; scales 2^desc->k_scale_exp and 2^desc->v_scale_exp.
  *  - desc->flags: KVSHOT_TREE and KVSHOT_OVERLAP_PREVIOUS (which then covers seq_lens, page_table, cache and
  *    tree_parent); others return KVSHOT_ERR_UNSUPPORTED.
+ *  - Lengths (max_seq_len, or the room that the table or the cache has, if that is less) and twice n_nodes sum up to
+ *    2^31 - 129 at most (else KVSHOT_ERR_UNSUPPORTED): positions are 32-bit numbers.
  *  - window = W > 0: a node at position p (a node of depth d, 1 for a child of the last verified token, stands at
  *    L_c + d - 1; the target token j at j) sees a key that it would see otherwise only if the key's position is above
  *    p - W, or below `sinks`.  A node always sees itself.  window = 0: no window (sinks is not used then).

@@ -919,6 +919,10 @@ extern "C" kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* d, const 
     if (d->l_cap % kKv4Tokens != 0) return KVSHOT_ERR_UNSUPPORTED;
     if (static_cast<double>(d->num_caches) * d->hkv * d->l_cap >= INT_MAX) return KVSHOT_ERR_UNSUPPORTED;
   }
+  // Positions and the ends of tiles are 32-bit numbers, and so is a window's reach from a draft node.
+  const int64_t room = paged ? static_cast<int64_t>(d->max_pages_per_seq) * d->page_size : d->l_cap;
+  const int64_t len_bound = std::min<int64_t>(d->max_seq_len, room);
+  if (len_bound + 2 * static_cast<int64_t>(d->n_nodes) > INT_MAX - kTile) return KVSHOT_ERR_UNSUPPORTED;
   if (d->n_query == 0) return KVSHOT_OK;
   if (!q || !cache || !seq_lens || !draft_k || !draft_v || !out || !lse || (tree && !tree_parent)) return KVSHOT_ERR_NULL;
   if (!aligned(q, 16) || !aligned(cache, 16) || !aligned(draft_k, 16) || !aligned(draft_v, 16) || !aligned(out, 16) ||
@@ -951,7 +955,7 @@ extern "C" kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* d, const 
   p.page_size = paged ? d->page_size : d->l_cap;
   p.max_pages = paged ? d->max_pages_per_seq : 1;
   p.num_pages = paged ? d->num_pages : d->num_caches;
-  p.len_bound = static_cast<int>(std::min<int64_t>(d->max_seq_len, static_cast<int64_t>(p.max_pages) * p.page_size));
+  p.len_bound = static_cast<int>(len_bound);
   p.N = d->n_nodes;
   p.Nq = d->n_query;
   p.n_max = d->n_max;
