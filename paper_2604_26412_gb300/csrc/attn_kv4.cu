@@ -144,7 +144,7 @@ __device__ __forceinline__ void run_q(const Kv4Params& kp, const Smem& smem, con
     // The first piece's (t = -1) before its first tile has landed, the others' with theirs.
     TileMeta w = tile_meta_at(sm.first);
     if (t >= 0) {
-      if (!wait(sm.cfull + 8 * stage, phase)) return;
+      if (!wait.landed(sm.cfull + 8 * stage, phase)) return;
       w = tile_meta(sm, t);
       if (lane == 0) mbar_arrive(sm.cempty + 8 * stage);
       if (++stage == CF::kStages) {
@@ -256,7 +256,7 @@ __device__ __forceinline__ void run_decode(const Kv4Params& kp, const Smem& smem
   for (int t = wg;; t += 2) {
     // The tile's bytes; K's buffer: QK^T of its previous tile is done.
     uint32_t flags = tile_flags(sm, t);
-    if (!wait(sm.cfull + 8 * stage, phase, qkdone, freed)) return;
+    if (!wait.landed(sm.cfull + 8 * stage, phase, qkdone, freed)) return;
     tc_fence_after();
     if (!is_of(flags)) flags = tile_flags(sm, t);
     if (flags & kStop) {

@@ -275,7 +275,7 @@ __device__ __forceinline__ void run_consumer(const Kv4Params& kp, const Smem& sm
     // The first piece begins (t = -1) before its first tile has landed, the others with theirs.
     int4 meta = make_int4(kFirst, 0, 0, 0);  // flags, key0, nkeys, L
     if (t >= 0) {
-      if (!wait(sm.cfull + 8 * stage, phase)) return;
+      if (!wait.landed(sm.cfull + 8 * stage, phase)) return;
       meta = tile_words(sm, t);
       if (meta.x & kStop) return;
     }

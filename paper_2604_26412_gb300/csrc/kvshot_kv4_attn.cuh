@@ -85,7 +85,10 @@ struct alignas(16) Rows {
 
 // Every wait ends: when its phase completes, when another role has given up, or (which gives up) after the call's limit.
 // A warp waits as one.  The inline part is one try of all lanes, which blocks for a while; what the rest needs lies in
-// shared memory, so that the many places that wait are short.
+// shared memory, so that the many places that wait are short.  A blocking try may sit out more than the time it is given
+// (with a limit of 1 ns, and that as its time, no wait ever gave up).  So with limits below kPollBelowNs a try is given none,
+// which keeps it to a few microseconds, and the waits for a tile's bytes are polled.  (A look at the limit at every wait
+// costs 256 rows 2.5 us of 170, polling inline 13.)
 struct WaitLimits {
   int32_t* err;
   uint64_t limit_ns;
@@ -102,7 +105,7 @@ __device__ __forceinline__ void init_waits(const AttnParams& p) {
   w->limit_ns = p.wait_ns;
   w->abort = 0;
 }
-// Blocks for up to `hint_ns`.
+// Blocks for about `hint_ns`, or a few microseconds.
 __device__ __forceinline__ bool try_wait_for(uint32_t bar, uint32_t parity, uint32_t hint_ns) {
   uint32_t done;
   asm volatile(
@@ -118,7 +121,7 @@ __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, uint32_t h
   volatile WaitLimits* w = wait_limits();
   const uint64_t t0 = global_timer_ns(), limit = w->limit_ns;
   for (;;) {
-    if (__all_sync(0xffffffffu, try_wait_for(bar, parity, hint_ns))) return true;
+    if (__all_sync(0xffffffffu, hint_ns == 0 ? mbar_test_wait(bar, parity) : try_wait_for(bar, parity, hint_ns))) return true;
     if (__any_sync(0xffffffffu, w->abort)) return false;
     if (__any_sync(0xffffffffu, global_timer_ns() - t0 > limit)) break;
   }
@@ -129,14 +132,21 @@ __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, uint32_t h
   return false;
 }
 struct Waiter {
-  uint32_t hint_ns;  // of a try (a limit must not be sat out in one)
-  __device__ __forceinline__ explicit Waiter(const AttnParams& p) : hint_ns(min(p.wait_ns, 20000u)) {}
+  uint32_t hint_ns;  // of a try
+  __device__ __forceinline__ explicit Waiter(const AttnParams& p) : hint_ns(p.wait_ns < kPollBelowNs ? 0 : 20000) {}
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
     return __all_sync(0xffffffffu, try_wait_for(bar, parity, hint_ns)) || wait_slow(bar, parity, hint_ns);
   }
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, uint32_t bar2, uint32_t parity2) const {
     const bool one = try_wait_for(bar, parity, hint_ns), two = try_wait_for(bar2, parity2, hint_ns);
     return __all_sync(0xffffffffu, one && two) || (wait_slow(bar, parity, hint_ns) && wait_slow(bar2, parity2, hint_ns));
+  }
+  // The same for a tile's bytes to land (and for another barrier).
+  __device__ __forceinline__ bool landed(uint32_t bar, uint32_t parity) const {
+    return hint_ns == 0 ? wait_slow(bar, parity, 0) : (*this)(bar, parity);
+  }
+  __device__ __forceinline__ bool landed(uint32_t bar, uint32_t parity, uint32_t bar2, uint32_t parity2) const {
+    return hint_ns == 0 ? wait_slow(bar, parity, 0) && wait_slow(bar2, parity2, 0) : (*this)(bar, parity, bar2, parity2);
   }
 };
 
