@@ -23,7 +23,15 @@ class Kv4Cache:
         if size == 0:
             raise kvshot.KvshotError(kvshot.KVSHOT_ERR_SHAPE, "kvshot_kv4_cache_bytes")
         self.num_caches, self.hkv, self.page_size, self.num_pages = num_caches, hkv, page_size, num_pages
+        self.max_pages_per_seq = max_pages_per_seq
         self.k_scale_exp, self.v_scale_exp, self.max_tokens = k_scale_exp, v_scale_exp, max_tokens
+        self.err = torch.zeros(1, dtype=torch.int32, device=device)
+        # Sizes that every call would refuse: without pointers, or tokens, the calls check them and do nothing.
+        self._extend = self._extend_desc(max_tokens)
+        status = kvshot.cache_extend_status(self._extend, *[None] * 12, stream=0)
+        if status != kvshot.KVSHOT_ERR_NULL:
+            raise kvshot.KvshotError(status, "kvshot_cache_extend")
+        kvshot.kv4_store(self._rows(0), None, None, None, None, stream=0)
 
         def i32(*shape):
             return torch.zeros(shape, dtype=torch.int32, device=device)
@@ -32,17 +40,19 @@ class Kv4Cache:
         self.seq_lens, self.page_table = i32(num_caches), i32(num_caches, max_pages_per_seq)
         self.free_pages = torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device)  # taken from its end
         self.free_count = torch.full((1,), num_pages, dtype=torch.int32, device=device)
-        self.err = i32(1)
         # Of the last grow(): first packed token of each cache; slot, cache and position of each packed token (or -1).
         self.token_start = i32(num_caches + 1)
-        self.slots, self.token_cache, self.positions = i32(max_tokens), i32(max_tokens), i32(max_tokens)
-        self._extend = kvshot.make_extend_desc(num_caches=num_caches, page_size=page_size,
-                                               max_pages_per_seq=max_pages_per_seq, num_pages=num_pages,
-                                               max_tokens=max_tokens, err_flag=self.err)
+        self._maps = i32(3, max_tokens)
+        self.slots, self.token_cache, self.positions = self._maps.unbind()
 
     @property
     def max_seq_len(self) -> int:
-        return self.page_table.shape[1] * self.page_size
+        return self.max_pages_per_seq * self.page_size
+
+    def _extend_desc(self, max_tokens: int) -> kvshot.ExtendDesc:
+        return kvshot.make_extend_desc(num_caches=self.num_caches, page_size=self.page_size,
+                                       max_pages_per_seq=self.max_pages_per_seq, num_pages=self.num_pages,
+                                       max_tokens=max_tokens, err_flag=self.err)
 
     def _rows(self, num_tokens: int, k_stride: int = 0, v_stride: int = 0) -> kvshot.Kv4Desc:
         return kvshot.make_kv4_desc(num_tokens=num_tokens, hkv=self.hkv, page_size=self.page_size,
@@ -52,32 +62,50 @@ class Kv4Cache:
 
     def extend(self, new_tokens: torch.Tensor, stream=None) -> None:
         """Pages and slots for new_tokens[c] (int32 [num_caches]) more tokens of each cache; self.slots are theirs."""
-        kvshot.cache_extend(self._extend, self.seq_lens, new_tokens, self.page_table, self.free_pages, self.free_count,
+        self._extend_by(self._extend, new_tokens, stream)
+
+    def _extend_by(self, desc: kvshot.ExtendDesc, new_tokens: torch.Tensor, stream) -> None:
+        kvshot.cache_extend(desc, self.seq_lens, new_tokens, self.page_table, self.free_pages, self.free_count,
                             self.seq_lens, self.page_table, self.free_count, self.token_start, self.slots,
                             self.token_cache, self.positions, stream)
 
-    def store(self, k: torch.Tensor, v: torch.Tensor, slots: Optional[torch.Tensor] = None, stream=None) -> None:
-        """K and V [T, hkv, 128] (bf16; rows may be slices of wider ones) into slots [T] (default: the first T of
-        self.slots)."""
-        t = k.shape[0]
-        slots = self.slots if slots is None else slots
+    def _store_desc(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> kvshot.Kv4Desc:
+        """The descriptor of a store, with everything checked that would make the call refuse it or misread its rows."""
+        t = k.shape[0] if k.dim() == 3 else 0
         if k.shape != v.shape or k.shape[1:] != (self.hkv, 128) or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
             raise ValueError(f"k and v must be bf16 [T, {self.hkv}, 128]")
         if t > slots.shape[0]:
             raise ValueError(f"{t} tokens for {slots.shape[0]} slots")
-        if t == 0:
-            return
         for x in (k, v):
-            if x.stride()[1:] != (128, 1):
-                raise ValueError("a token's heads must be contiguous")
-        stride = (k.stride(0), v.stride(0)) if t > 1 else (0, 0)
-        kvshot.kv4_store(self._rows(t, *stride), k, v, slots, self.data, stream)
+            if x.device != self.data.device:
+                raise ValueError(f"k and v must be on {self.data.device}")
+            if t == 0:
+                continue
+            if x.stride()[1:] != (128, 1) or x.data_ptr() % 16:
+                raise ValueError("a token's heads must be contiguous, from 16-byte aligned addresses on")
+            if t > 1 and (x.stride(0) < self.hkv * 128 or x.stride(0) % 8):
+                raise ValueError("tokens must lie apart by a multiple of 8 elements, and not over one another")
+        return self._rows(t, *((k.stride(0), v.stride(0)) if t > 1 else (0, 0)))
+
+    def store(self, k: torch.Tensor, v: torch.Tensor, slots: Optional[torch.Tensor] = None, stream=None) -> None:
+        """K and V [T, hkv, 128] (bf16; rows may be slices of wider ones) into slots [T] (default: the first T of
+        self.slots)."""
+        slots = self.slots if slots is None else slots
+        desc = self._store_desc(k, v, slots)
+        if desc.num_tokens:
+            kvshot.kv4_store(desc, k, v, slots, self.data, stream)
 
     def grow(self, new_tokens: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
-        """extend(), then store(): K and V packed cache after cache.  Rows past the new tokens are not stored."""
-        stream = kvshot._stream(stream)
-        self.extend(new_tokens, stream)
-        self.store(k, v, stream=stream)
+        """extend(), then store(): K and V packed cache after cache.  Rows past the new tokens are not stored.  Nothing is
+        enqueued if K or V are refused, and nothing taken if the rows are fewer than the new tokens (which the device
+        finds, as extend() its other errors)."""
+        desc, t = self._store_desc(k, v, self.slots), k.shape[0]
+        self._extend_by(self._extend_desc(t), new_tokens, stream)
+        if t < self.max_tokens:  # (the maps of an extension by t tokens at most end there)
+            with kvshot.torch_stream(stream):
+                self._maps[:, t:].fill_(-1)
+        if t:
+            kvshot.kv4_store(desc, k, v, self.slots, self.data, stream)
 
     def values(self, slots: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """K and V [T, hkv, 128] (bf16) of slots [T]; -1 gives zeros."""

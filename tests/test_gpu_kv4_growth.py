@@ -1,4 +1,4 @@
-"""Drafting over a 4-bit cache that grows: the draft tokens' places behind the grown prefix.
+"""Drafting over a 4-bit cache that grows: the draft tokens' places behind the grown prefix, and growth that is refused.
 
 Positions here come from the cache's own lengths and the nodes' depths (a node of depth d stands at L + d - 1), not from
 the step.  The appended q and K have to be the oracle's bits at those positions; bounds of the attention as in
@@ -10,6 +10,7 @@ import torch
 
 from oracle import kv4, oracle
 from paper_2604_26412_gb300 import kv4 as user
+from paper_2604_26412_gb300 import kvshot
 from paper_2604_26412_gb300 import workloads as wl
 from paper_2604_26412_gb300.step import DraftStep
 from tests.test_gpu_kv4 import LSE_MAX_ABS, OUT_MAX_ABS, OUT_REL_L2
@@ -137,3 +138,68 @@ def test_the_steps_of_the_other_caches_keep_their_places():
     _, inp = _inputs([2, 3])
     step = DraftStep(inp)
     assert all(a is b for a, b in zip(step.pos, inp.positions))
+
+
+# ------------------------------------------------------------------ growth that is refused
+
+def _state(cache):
+    return [x.clone() for x in (cache.seq_lens, cache.page_table, cache.free_count, cache.data)]
+
+
+def _unmoved(cache, before):
+    return all(torch.equal(a, b) for a, b in zip(before, _state(cache)))
+
+
+def _wrong_rows(what):
+    k = torch.zeros((4, HKV, 128), dtype=torch.bfloat16, device="cuda")
+    flat = torch.zeros(4 * HKV * 128 + 64, dtype=torch.bfloat16, device="cuda")
+    return {
+        "type": k.float(), "heads": k[:, :1], "order": k.transpose(1, 2), "host": k.cpu(),
+        "many": torch.zeros((200, HKV, 128), dtype=torch.bfloat16, device="cuda"),
+        "shared": k[:1].expand(4, HKV, 128),
+        "address": flat[4:4 + 4 * HKV * 128].view(4, HKV, 128),
+        "stride": torch.as_strided(flat, (4, HKV, 128), (HKV * 128 + 4, 128, 1)),
+        "overlap": torch.as_strided(flat, (4, HKV, 128), (128, 128, 1)),
+        "dims": k[0],
+    }[what]
+
+
+@pytest.mark.parametrize("what", ["type", "heads", "order", "host", "many", "shared", "address", "stride", "overlap", "dims"])
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_growth_with_wrong_rows_moves_nothing(what, which):
+    cache = user.Kv4Cache(3, HKV, 20, 8, max_tokens=100)
+    before = _state(cache)
+    bad = _wrong_rows(what)
+    good = torch.zeros((bad.shape[0], HKV, 128), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises((ValueError, kvshot.KvshotError)):
+        cache.grow(_i32([3, 1, 0]), *((bad, good) if which == "k" else (good, bad)))
+    assert _unmoved(cache, before)
+
+
+def test_growth_with_fewer_rows_than_tokens_moves_nothing():
+    cache = user.Kv4Cache(3, HKV, 20, 8, max_tokens=100)
+    cache.grow(_i32([20, 3, 40]), *_rows(63))
+    before = _state(cache)
+    cache.grow(_i32([3, 1, 0]), *_rows(3))
+    assert _unmoved(cache, before)
+    assert cache.error_code() == kvshot.KVSHOT_ERR_DEVICE_BOUNDS
+    assert all(bool((m == -1).all()) for m in (cache.slots, cache.token_cache, cache.positions))
+    assert int(cache.token_start.abs().max()) == 0
+
+
+def test_maps_past_the_new_tokens_say_so():
+    cache = user.Kv4Cache(3, HKV, 20, 8, max_tokens=100)
+    cache.grow(_i32([20, 3, 40]), *_rows(63))
+    cache.grow(_i32([3, 0, 2]), *_rows(7))
+    assert cache.positions.tolist() == [20, 21, 22, 40, 41] + [-1] * 95
+    assert cache.token_cache.tolist() == [0, 0, 0, 2, 2] + [-1] * 95
+    assert cache.slots[5:].tolist() == [-1] * 95 and int(cache.slots[:5].min()) >= 0
+    assert cache.error_code() == 0
+
+
+@pytest.mark.parametrize("sizes", [dict(k_scale_exp=65), dict(v_scale_exp=-65), dict(hkv=16385, num_pages=1),
+                                   dict(max_tokens=-1), dict(num_caches=0), dict(max_pages_per_seq=0),
+                                   dict(num_caches=1025)])
+def test_sizes_that_no_call_takes_are_refused_at_once(sizes):
+    with pytest.raises((ValueError, kvshot.KvshotError)):
+        user.Kv4Cache(**(dict(num_caches=3, hkv=HKV, num_pages=20, max_pages_per_seq=8, max_tokens=100) | sizes))
