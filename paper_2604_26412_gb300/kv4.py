@@ -64,7 +64,15 @@ class Kv4Cache:
         """Pages and slots for new_tokens[c] (int32 [num_caches]) more tokens of each cache; self.slots are theirs."""
         self._extend_by(self._extend, new_tokens, stream)
 
+    def _check_ints(self, name: str, x: torch.Tensor, shape=None) -> None:
+        """The calls take bare pointers: a tensor of another type or order would be read as other numbers."""
+        if x.dtype != torch.int32 or x.device != self.data.device or not x.is_contiguous() or x.dim() != 1 or \
+                (shape is not None and x.shape != shape):
+            size = "" if shape is None else str(shape[0])
+            raise ValueError(f"{name} must be int32 [{size}] on {self.data.device}, and contiguous")
+
     def _extend_by(self, desc: kvshot.ExtendDesc, new_tokens: torch.Tensor, stream) -> None:
+        self._check_ints("new_tokens", new_tokens, (self.num_caches,))
         kvshot.cache_extend(desc, self.seq_lens, new_tokens, self.page_table, self.free_pages, self.free_count,
                             self.seq_lens, self.page_table, self.free_count, self.token_start, self.slots,
                             self.token_cache, self.positions, stream)
@@ -91,6 +99,7 @@ class Kv4Cache:
         """K and V [T, hkv, 128] (bf16; rows may be slices of wider ones) into slots [T] (default: the first T of
         self.slots)."""
         slots = self.slots if slots is None else slots
+        self._check_ints("slots", slots)
         desc = self._store_desc(k, v, slots)
         if desc.num_tokens:
             kvshot.kv4_store(desc, k, v, slots, self.data, stream)
@@ -109,6 +118,7 @@ class Kv4Cache:
 
     def values(self, slots: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """K and V [T, hkv, 128] (bf16) of slots [T]; -1 gives zeros."""
+        self._check_ints("slots", slots)
         shape = (slots.shape[0], self.hkv, 128)
         k, v = (torch.empty(shape, dtype=torch.bfloat16, device=self.data.device) for _ in range(2))
         if slots.shape[0]:

@@ -203,3 +203,32 @@ def test_maps_past_the_new_tokens_say_so():
 def test_sizes_that_no_call_takes_are_refused_at_once(sizes):
     with pytest.raises((ValueError, kvshot.KvshotError)):
         user.Kv4Cache(**(dict(num_caches=3, hkv=HKV, num_pages=20, max_pages_per_seq=8, max_tokens=100) | sizes))
+
+
+def _wrong_counts(what):
+    return {
+        "int64": torch.tensor([3, 1, 0], device="cuda"), "host": torch.tensor([3, 1, 0], dtype=torch.int32),
+        "short": _i32([3]), "long": _i32([3, 1, 0, 0]), "strided": _i32([3, 9, 1, 9, 0, 9])[::2],
+        "float": torch.tensor([3.0, 1.0, 0.0], device="cuda"), "dims": _i32([[3, 1, 0]]),
+    }[what]
+
+
+@pytest.mark.parametrize("what", ["int64", "host", "short", "long", "strided", "float", "dims"])
+def test_counts_of_another_type_or_shape_are_refused(what):
+    cache = user.Kv4Cache(3, HKV, 20, 8, max_tokens=100)
+    before = _state(cache)
+    for call in (lambda n: cache.grow(n, *_rows(4)), cache.extend):
+        with pytest.raises(ValueError):
+            call(_wrong_counts(what))
+    assert _unmoved(cache, before)
+
+
+@pytest.mark.parametrize("what", ["int64", "host", "strided", "float", "dims"])
+def test_slots_of_another_type_or_shape_are_refused(what):
+    cache = user.Kv4Cache(3, HKV, 20, 8, max_tokens=100)
+    before = _state(cache)
+    with pytest.raises(ValueError):
+        cache.values(_wrong_counts(what))
+    with pytest.raises(ValueError):
+        cache.store(*_rows(1), slots=_wrong_counts(what))
+    assert _unmoved(cache, before)
