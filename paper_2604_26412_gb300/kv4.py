@@ -126,7 +126,11 @@ class Kv4Cache:
         return k, v
 
     def error_code(self) -> int:
-        return int(self.err.item())
+        """The first error that the cache's calls have recorded since the last time this was asked (0: none)."""
+        code = int(self.err.item())
+        if code:
+            self.err.zero_()
+        return code
 
 
 def of_inputs(inp, page_size: int = 16, spare_pages: int = 0, spare_tokens: int = 0, k_exp: int = 0,

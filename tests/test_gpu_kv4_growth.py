@@ -232,3 +232,11 @@ def test_slots_of_another_type_or_shape_are_refused(what):
     with pytest.raises(ValueError):
         cache.store(*_rows(1), slots=_wrong_counts(what))
     assert _unmoved(cache, before)
+
+
+def test_an_error_is_reported_once():
+    cache = user.Kv4Cache(3, HKV, 20, 8, max_tokens=100)
+    cache.grow(_i32([100, 100, 100]), *_rows(100))
+    assert cache.error_code() == kvshot.KVSHOT_ERR_DEVICE_BOUNDS
+    cache.grow(_i32([3, 1, 0]), *_rows(4))
+    assert cache.error_code() == 0 and cache.seq_lens.tolist() == [3, 1, 0]
