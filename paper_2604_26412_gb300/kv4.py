@@ -117,10 +117,11 @@ class Kv4Cache:
             kvshot.kv4_store(desc, k, v, self.slots, self.data, stream)
 
     def values(self, slots: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
-        """K and V [T, hkv, 128] (bf16) of slots [T]; -1 gives zeros."""
+        """K and V [T, hkv, 128] (bf16) of slots [T]; -1 gives zeros.  Both are memory of `stream`, like its own tensors."""
         self._check_ints("slots", slots)
         shape = (slots.shape[0], self.hkv, 128)
-        k, v = (torch.empty(shape, dtype=torch.bfloat16, device=self.data.device) for _ in range(2))
+        with kvshot.torch_stream(stream):
+            k, v = (torch.empty(shape, dtype=torch.bfloat16, device=self.data.device) for _ in range(2))
         if slots.shape[0]:
             kvshot.kv4_load(self._rows(slots.shape[0]), self.data, slots, k, v, stream)
         return k, v

@@ -240,3 +240,21 @@ def test_an_error_is_reported_once():
     assert cache.error_code() == kvshot.KVSHOT_ERR_DEVICE_BOUNDS
     cache.grow(_i32([3, 1, 0]), *_rows(4))
     assert cache.error_code() == 0 and cache.seq_lens.tolist() == [3, 1, 0]
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_values_on_another_stream_are_written_by_it_alone(handle):
+    """Memory that the current stream has let go of, with work on it still to come, is not another stream's to write."""
+    cache = user.Kv4Cache(3, HKV, 600, 200, max_tokens=4096)
+    cache.grow(_i32([3000, 1000, 96]), *_rows(4096))
+    want = cache.values(cache.slots)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    old = [torch.empty((4096, HKV, 128), dtype=torch.bfloat16, device="cuda") for _ in range(8)]
+    torch.cuda._sleep(200_000_000)
+    for x in old:
+        x.fill_(7.0)
+    del x, old
+    got = cache.values(cache.slots, stream=s.cuda_stream if handle else s)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
