@@ -29,7 +29,7 @@
 //  - What a piece needs beside its tiles is made beside them: rows' tables after q (69 -> 64 us), the CTA's plan and first
 //    q before its first tile (64 -> 61.7), tables by jumps and whole nodes (59.6 -> 53.8), a warpgroup that ends its rows
 //    by itself (53.5 -> 49.8).
-// Measured, attention and merge: 32 rows 42 us, 48 rows 49.5, 64 rows 55.8, 256 rows 170 (the tree's 64 nodes in four
+// Measured, attention and merge: 32 rows 42 us, 48 rows 49.2, 64 rows 55.8, 256 rows 170 (the tree's 64 nodes in four
 // blocks, each of which decodes the cache for itself).  Many short contexts cost their pieces: 82 caches of 5 tokens, 48
 // rows, 656 pieces of three tiles 60 us (20k cycles each, most of it code fetched anew).
 // Work plan: the units' tiles laid end to end and cut into equal ranges, one per persistent CTA (kvshot_internal.h);
@@ -850,7 +850,9 @@ struct Plan {
 
 // Tiles that a CTA's range may grow by where that leaves it one piece, about what a second piece and the merge cost: of this
 // kernel (64 rows, 16 sequences of 4096 tokens, 34 tiles instead of 29: 59.5 -> 55.8 us; 48 rows 50.3 -> 49.5), and of the
-// other with 16 rows (12 instead of 9: 39.1 -> 37.8) and 8 (34.2 -> 33.2; with three a window of 4096 32.3 -> 32.9).
+// other with 16 rows (12 instead of 9: 39.1 -> 37.8) and 8 (34.2 -> 33.2; with three a window of 4096 32.3 -> 32.9).  Of 75
+// calls of 4 to 64 rows over 4 to 28 caches of 1500, 4100 or 9000 tokens none loses more than 0.8% against ranges laid end to
+// end, and 35 gain 5% and more (48 rows, 17 caches of 1500: 33.1 -> 27.1 us).
 constexpr int kSpareTiles = 6, kSpareTiles16 = 3, kSpareTiles8 = 1;
 
 // Fewest tiles per CTA.  (One a CTA is no faster: a sequence of 2048 tokens takes 12.4 us with either.)

@@ -18,8 +18,8 @@
 //    for it).
 // A CTA is four warps, 32 keys of a tile each, and a loading warp; three CTAs share an SM (16 rows: two).  One more, in
 // the fewer registers that leaves a thread, is slower (105 against 97 us; 16 rows 202 against 173), and so is one less (110).
-// Measured, attention and merge: 8 rows, 64 sequences of 512 to 8192 tokens 93 us (3.9 TB/s, 0.57 of the copy's rate);
-// 16 rows, 4 x 4 x 32k tokens 166 us (3.7 TB/s); 8 rows, a window of 4096 31.8 us; one sequence of 2048 tokens 12.0 us.
+// Measured, attention and merge: 8 rows, 64 sequences of 512 to 8192 tokens 94 us (3.9 TB/s, 0.57 of the copy's rate);
+// 16 rows, 4 x 4 x 32k tokens 166 us (3.7 TB/s); 8 rows, a window of 4096 32 us; one sequence of 2048 tokens 12.3 us.
 // It issues at half of the rate; what it waits for most is its own fixed latencies (1.2 cycles an instruction).
 // From 17 rows on attn_kv4.cu is faster; at 16 it takes 168 us (4 x 4 x 32k) where this kernel takes 166, and 41.5 against
 // 37.5 for 16 sequences of 4096 tokens.
