@@ -450,6 +450,135 @@ kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* desc, const void* q,
                                     const void* draft_v, const int32_t* tree_parent, int32_t window, int32_t sinks,
                                     void* out, float* lse, kvshot_stream_t stream);
 
+/*
+ * Drafting over a part of a long target cache (not in the paper).  A page of the target cache none of whose keys can score
+ * high need not be read for a draft token, and a token that draft tokens gave little weight need not be kept.
+ *   kvshot_page_bounds   least and greatest key of each page             (after the cache grew)
+ *   kvshot_page_scores   greatest possible score of each page, for every draft token and KV head
+ *   kvshot_select_top    the best entries of each row of scores: pages to read, or tokens to keep
+ *   kvshot_draft_attn_sparse   draft attention over the selected pages and the draft K/V
+ *   kvshot_key_weights   softmax weights that the cached tokens got, accumulated
+ *   kvshot_cache_evict   the tokens to keep moved to the front, and the other pages given back
+ * The first two, the fourth and the fifth take a kvshot_attn_desc and read of it num_caches, num_seqs, hq, hkv, head_dim,
+ * page_size, max_pages_per_seq, num_pages, max_seq_len, n_nodes, n_query, n_max, scale, flags and err_flag as
+ * kvshot_draft_attn does (kvshot_page_bounds no query heads' or nodes' fields).  Caches are bf16 and paged
+ * (kvshot_key_weights: or contiguous), q is [C, Nq, hq, 128] bf16, and the q heads of one KV head are at most 32.
+ * KVSHOT_TARGET_FP8 and the KVSHOT_FORCE_ flags return KVSHOT_ERR_UNSUPPORTED; KVSHOT_OVERLAP_PREVIOUS has no effect.
+ * A length outside [0, min(max_seq_len, capacity)] is recorded as KVSHOT_ERR_DEVICE_BOUNDS and clamped to it, a page id
+ * outside the pool recorded and its page passed over.  16-byte alignment of all bf16 pointers, 4 of int32 and fp32.
+ */
+
+/*
+ * bounds[pid, h, 0, d] = min, bounds[pid, h, 1, d] = max over the tokens of the page below the cache's length, of key
+ * element d of KV head h (NaN if one of them is): [num_pages, hkv, 2, 128] bf16, by pool page, so that bounds stay with
+ * their page.  Computed for the pages that hold a token at or past from_tokens[c] (a length before the cache grew; NULL:
+ * all pages); other entries are left as they are.
+ */
+kvshot_status kvshot_page_bounds(const kvshot_attn_desc* desc, const void* target_k, const int32_t* page_table,
+                                 const int32_t* seq_lens, const int32_t* from_tokens, void* bounds,
+                                 kvshot_stream_t stream);
+
+/*
+ * scores[c, n, h, p] = scale * max over the q heads g of KV head h of sum_d max(q_gd min_d, q_gd max_d), with the bounds
+ * of page p of cache c: no key of the page scores higher for draft token n.  [C, Nq, hkv, max_pages_per_seq] fp32; entries
+ * past a cache's last page are left as they are.  Products accumulate in fp32.  Bounds and q must be finite.
+ */
+kvshot_status kvshot_page_scores(const kvshot_attn_desc* desc, const void* q, const void* bounds,
+                                 const int32_t* page_table, const int32_t* seq_lens, float* scores,
+                                 kvshot_stream_t stream);
+
+/*
+ * The best entries of each row.  Row r has n_r = ceil(seq_lens[r / rows_per_len] / tokens_per_entry) entries, of which
+ * min(n_r, keep) are picked: the first `first`, the last `last`, and of the others those with the highest scores; of equal
+ * ones (0 and -0 are) the lowest index, and a NaN is above every number.
+ * picks: [num_rows, keep] int32, ascending, -1 past the last; counts: [num_rows] int32.
+ * scores: [num_rows, row_len] fp32.  A row that is longer than row_len is recorded as KVSHOT_ERR_DEVICE_BOUNDS and has
+ * row_len entries, a negative length 0.  num_rows == 0 is a no-op.
+ * For kvshot_page_scores: num_rows = C Nq hkv, row_len = max_pages_per_seq, rows_per_len = Nq hkv, tokens_per_entry =
+ * page_size.  For weights of tokens: num_rows = C, rows_per_len = tokens_per_entry = 1.
+ */
+typedef struct kvshot_select_desc {
+  int32_t num_rows;
+  int32_t row_len;
+  int32_t rows_per_len;     /* >= 1; num_rows is a multiple of it */
+  int32_t tokens_per_entry; /* >= 1 */
+  int32_t keep;             /* >= 1 */
+  int32_t first;            /* >= 0 */
+  int32_t last;             /* >= 0; first + last <= keep */
+  int32_t* err_flag;        /* optional device int32, 0 before the call */
+} kvshot_select_desc;
+
+kvshot_status kvshot_select_top(const kvshot_select_desc* desc, const float* scores, const int32_t* seq_lens,
+                                int32_t* picks, int32_t* counts, kvshot_stream_t stream);
+
+/*
+ * kvshot_draft_attn with the prefix tokens of each query row and KV head limited to the pages picked for it: out and lse of
+ * row n and the q heads of KV head h are over the tokens below L_c in the pages page_table[c, picks[c, n, h, i]],
+ * i < counts[c, n, h], and the draft keys that kvshot_draft_attn gives that row.
+ * picks: [C, Nq, hkv, max_picks] int32, each list ascending; counts: [C, Nq, hkv] int32 in [0, max_picks].  A pick that
+ * is not above its predecessor or not a page below the cache's length is recorded as KVSHOT_ERR_DEVICE_BOUNDS and passed
+ * over, a count out of range recorded and clamped.  Other arguments as for kvshot_draft_attn.
+ * The softmax weights are rounded to bf16 for the tensor cores, sums are fp32.
+ * Workspace: kvshot_draft_attn_sparse_workspace_size bytes (0 if the descriptor is invalid), as for kvshot_draft_attn.
+ */
+size_t kvshot_draft_attn_sparse_workspace_size(const kvshot_attn_desc* desc, int32_t max_picks);
+kvshot_status kvshot_draft_attn_sparse(const kvshot_attn_desc* desc, const void* q, const void* target_k,
+                                       const void* target_v, const int32_t* page_table, const int32_t* seq_lens,
+                                       const int32_t* picks, const int32_t* counts, int32_t max_picks,
+                                       const void* draft_k, const void* draft_v, const int32_t* tree_parent, void* out,
+                                       float* lse, kvshot_stream_t stream);
+
+/*
+ * weights_out[c, j] = decay * weights[c, j] + sum over the query rows n and q heads of exp(scale q . k_j - lse[c, n, head])
+ * for every token j < L_c: what the softmax whose lse kvshot_draft_attn returned gave the token, summed.  A row whose lse
+ * is -inf adds nothing.  [C, weights_len] fp32; entries past the length are left as they are.  weights may be weights_out, or NULL (zeros).
+ * decay in [0, 1]; with 0 weights is not read.  Sums are fp32 and their order fixed.
+ * page_table NULL: a contiguous cache [C, hkv, l_cap, 128].  A length above weights_len is recorded as out of bounds, too.
+ */
+kvshot_status kvshot_key_weights(const kvshot_attn_desc* desc, const void* q, const void* target_k,
+                                 const int32_t* page_table, const int32_t* seq_lens, const float* lse, float decay,
+                                 int32_t weights_len, const float* weights, float* weights_out, kvshot_stream_t stream);
+
+/*
+ * Eviction.  Cache c keeps m_c = kept_count[c] of its L_c tokens: token kept[c, i] becomes token i, for all KV heads of K
+ * and V and in the weights.
+ *   k, v -> k_out, v_out    [num_pages, hkv, page_size, 128] bf16, in place (k_out = k, v_out = v, page_table_out =
+ *                           page_table), or into other pools of num_pages_out pages through page_table_out, a smaller
+ *                           copy for instance.  Slots past the last kept token are left as they are.
+ *   weights -> weights_out  [C, weights_len] -> [C, weights_len_out] fp32; in place, or not overlapping; both may be NULL
+ *   seq_lens_out            m_c
+ *   free_pages, free_count_out   page_table's pages past the first ceil(m_c / page_size) of cache c's ceil(L_c / page_size),
+ *                           put behind the *free_count free ones, cache after cache, ascending: what kvshot_cache_extend
+ *                           takes from.  free_pages, free_count and free_count_out may all be NULL.
+ * seq_lens_out may be seq_lens, free_count_out may be free_count; nothing else may overlap.  Pages must not be shared
+ * between caches.  kept: [C, max_kept] int32, ascending, below L_c.
+ * Device errors are recorded as KVSHOT_ERR_DEVICE_BOUNDS: a length that the table has no room for, or a count below 0 or
+ * above what the length, max_kept, page_table_out or weights_len_out has room for (that cache's tokens, length and pages stay
+ * as they are; seq_lens_out is the length, clamped to the table's room); a kept index out of order or range (that cache's
+ * contents are then unspecified); page ids outside their pool, and more free pages than num_free (passed over).
+ */
+typedef struct kvshot_evict_desc {
+  int32_t num_caches;        /* C in [1, 1024] */
+  int32_t hkv;
+  int32_t head_dim;          /* must be 128 */
+  int32_t page_size;         /* >= 1 */
+  int32_t max_pages_per_seq; /* row length of page_table */
+  int32_t num_pages;         /* pages in k and v */
+  int32_t max_pages_out;     /* row length of page_table_out */
+  int32_t num_pages_out;     /* pages in k_out and v_out */
+  int32_t max_kept;          /* row length of kept */
+  int32_t weights_len;       /* row lengths of weights and weights_out */
+  int32_t weights_len_out;
+  int32_t num_free;          /* entries of free_pages */
+  int32_t* err_flag;         /* optional device int32, 0 before the call */
+} kvshot_evict_desc;
+
+kvshot_status kvshot_cache_evict(const kvshot_evict_desc* desc, const void* k, const void* v, const int32_t* page_table,
+                                 const int32_t* seq_lens, const int32_t* kept, const int32_t* kept_count,
+                                 const float* weights, void* k_out, void* v_out, const int32_t* page_table_out,
+                                 int32_t* seq_lens_out, float* weights_out, int32_t* free_pages,
+                                 const int32_t* free_count, int32_t* free_count_out, kvshot_stream_t stream);
+
 /* Static description of a status code (never NULL). */
 const char* kvshot_status_string(kvshot_status status);
 

@@ -1,0 +1,214 @@
+// cache_evict.cu -- eviction: the kept tokens' K, V and weights moved to the front of their cache, and the pages that are
+// left over put back on the list of free pages.
+#include <algorithm>
+#include <climits>
+
+#include "kvshot_partial.cuh"
+
+namespace kvshot {
+namespace {
+
+using namespace dev;
+using partial::aligned;
+
+struct EvictParams {
+  const uint8_t *k, *v;
+  uint8_t *k_out, *v_out;
+  const float* weights;
+  float* weights_out;
+  const int32_t *page_table, *page_table_out, *seq_lens, *kept, *kept_count, *free_count;
+  int32_t *seq_lens_out, *free_pages, *free_count_out, *err;
+  int C, hkv, P, max_pages, num_pages, max_pages_out, num_pages_out, max_kept, weights_len, weights_len_out, num_free;
+  int in_place;
+};
+
+// Length and number of kept tokens of cache c; kept < 0: the cache stays as it is.
+struct CacheKeep {
+  int len, kept;
+};
+__device__ __forceinline__ CacheKeep cache_keep(const EvictParams& p, int c, int L, int m) {
+  const int room = min(static_cast<int64_t>(p.max_pages) * p.P, static_cast<int64_t>(INT_MAX));
+  bool ok = L >= 0 && L <= room;
+  L = min(max(L, 0), room);
+  ok = ok && m >= 0 && m <= L && m <= p.max_kept && m <= static_cast<int64_t>(p.max_pages_out) * p.P;
+  if (p.weights != nullptr) ok = ok && L <= p.weights_len && m <= p.weights_len_out;
+  if (!ok) set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
+  return CacheKeep{L, ok ? m : -1};
+}
+
+// Old place of token i, or -1 if the list is out of order or range there.
+__device__ __forceinline__ int old_place(const EvictParams& p, const int32_t* kept, int i, int L) {
+  const int j = kept[i];
+  if (j >= i && j < L && (i == 0 || kept[i - 1] < j)) return j;
+  set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
+  return -1;
+}
+
+__device__ __forceinline__ int checked_page(const EvictParams& p, const int32_t* table, int row, int c, int page, int pool) {
+  const int id = table[static_cast<size_t>(c) * row + page];
+  if (static_cast<unsigned>(id) < static_cast<unsigned>(pool)) return id;
+  set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
+  return -1;
+}
+
+// Rows move in ascending order, a chunk of them at a time: the chunk is loaded whole, then stored.  A token's new place is
+// never behind its old one and both ascend, so a chunk's stores never reach what a later chunk loads, and in place one
+// barrier between a chunk's loads and stores is enough.  A row's 16-byte pieces are independent of one another, so CTAs
+// take different pieces of all rows (blockIdx.x), heads, and K or V.
+constexpr int kMoveThreads = 256;
+constexpr int kMovePieces = 4;                             // 16-byte pieces of a row that a CTA takes
+constexpr int kMoveRows = kMoveThreads / kMovePieces;      // rows of a load
+constexpr int kMoveLoads = 4;                              // loads of a chunk
+constexpr int kRowPieces = kHeadDim * 2 / 16;
+
+__global__ void __launch_bounds__(kMoveThreads) move_kernel(EvictParams p) {
+  const int c = blockIdx.z, y = blockIdx.y, tid = threadIdx.x;
+  const CacheKeep ck = cache_keep(p, c, p.seq_lens[c], p.kept_count[c]);
+  if (ck.kept <= 0) return;
+  const int32_t* kept = p.kept + static_cast<size_t>(c) * p.max_kept;
+  if (y == 2 * p.hkv) {  // the weights: one CTA
+    if (p.weights == nullptr || blockIdx.x != 0) return;
+    const float* src = p.weights + static_cast<size_t>(c) * p.weights_len;
+    float* dst = p.weights_out + static_cast<size_t>(c) * p.weights_len_out;
+    for (int i0 = 0; i0 < ck.kept; i0 += 8 * kMoveThreads) {
+      float x[8];
+      int j[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int at = i0 + i * kMoveThreads + tid;
+        j[i] = at < ck.kept ? old_place(p, kept, at, ck.len) : -1;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (j[i] >= 0) x[i] = src[j[i]];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (j[i] >= 0) dst[i0 + i * kMoveThreads + tid] = x[i];
+    }
+    return;
+  }
+  const int h = y >> 1, piece = blockIdx.x * kMovePieces + tid % kMovePieces;
+  const uint4* src = reinterpret_cast<const uint4*>((y & 1) != 0 ? p.v : p.k);
+  uint4* dst = reinterpret_cast<uint4*>((y & 1) != 0 ? p.v_out : p.k_out);
+  for (int i0 = 0; i0 < ck.kept; i0 += kMoveLoads * kMoveRows) {
+    uint4 x[kMoveLoads];
+    bool live[kMoveLoads];
+#pragma unroll
+    for (int i = 0; i < kMoveLoads; ++i) {
+      const int at = i0 + i * kMoveRows + tid / kMovePieces;
+      const int j = at < ck.kept ? old_place(p, kept, at, ck.len) : -1;
+      live[i] = j >= 0 && !(p.in_place && j == at);
+      if (!live[i]) continue;
+      const int id = checked_page(p, p.page_table, p.max_pages, c, j / p.P, p.num_pages);
+      live[i] = id >= 0;
+      if (live[i]) x[i] = src[((static_cast<size_t>(id) * p.hkv + h) * p.P + j % p.P) * kRowPieces + piece];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMoveLoads; ++i) {
+      if (!live[i]) continue;
+      const int at = i0 + i * kMoveRows + tid / kMovePieces;
+      const int id = checked_page(p, p.page_table_out, p.max_pages_out, c, at / p.P, p.num_pages_out);
+      if (id >= 0) dst[((static_cast<size_t>(id) * p.hkv + h) * p.P + at % p.P) * kRowPieces + piece] = x[i];
+    }
+  }
+}
+
+// Lengths and free pages: one CTA, a thread per cache, then a warp per cache writes its pages.
+constexpr int kEndThreads = 1024;
+static_assert(kEndThreads >= kMaxCaches, "a thread per cache");
+
+__global__ void __launch_bounds__(kEndThreads) evict_end_kernel(EvictParams p) {
+  __shared__ int s_first[kMaxCaches], s_gone[kMaxCaches], s_base[kMaxCaches], s_warp[32];
+  wait_for_prerequisite_grid();
+  const int c = threadIdx.x, lane = c & 31, warp = c >> 5;
+  CacheKeep ck{0, -1};
+  if (c < p.C) ck = cache_keep(p, c, p.seq_lens[c], p.kept_count[c]);
+  const int used = (ck.len + p.P - 1) / p.P, first = ck.kept >= 0 ? (ck.kept + p.P - 1) / p.P : used;
+  const int gone = p.free_pages != nullptr ? used - first : 0;
+  int scan = gone;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, scan, o);
+    if (lane >= o) scan += x;
+  }
+  if (lane == 31) s_warp[warp] = scan;
+  __syncthreads();
+  int base = scan - gone, total = 0;
+  for (int w = 0; w < 32; ++w) {
+    if (w < warp) base += s_warp[w];
+    total += s_warp[w];
+  }
+  const int F = p.free_pages != nullptr ? *p.free_count : 0;
+  s_first[c] = first;
+  s_gone[c] = gone;
+  s_base[c] = base;
+  __syncthreads();  // (free_count has been read by all)
+  if (c < p.C) p.seq_lens_out[c] = ck.kept >= 0 ? ck.kept : ck.len;
+  if (p.free_pages == nullptr) return;
+  if (F < 0 || static_cast<int64_t>(F) + total > p.num_free) {
+    if (c == 0) {
+      set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
+      *p.free_count_out = F;
+    }
+    return;
+  }
+  if (c == 0) *p.free_count_out = F + total;
+  for (int i = warp; i < p.C; i += 32)
+    for (int j = lane; j < s_gone[i]; j += 32)
+      p.free_pages[F + s_base[i] + j] = p.page_table[static_cast<size_t>(i) * p.max_pages + s_first[i] + j];
+}
+
+}  // namespace
+}  // namespace kvshot
+
+using namespace kvshot;
+
+extern "C" kvshot_status kvshot_cache_evict(const kvshot_evict_desc* d, const void* k, const void* v,
+                                            const int32_t* page_table, const int32_t* seq_lens, const int32_t* kept,
+                                            const int32_t* kept_count, const float* weights, void* k_out, void* v_out,
+                                            const int32_t* page_table_out, int32_t* seq_lens_out, float* weights_out,
+                                            int32_t* free_pages, const int32_t* free_count, int32_t* free_count_out,
+                                            kvshot_stream_t stream) {
+  if (d == nullptr) return KVSHOT_ERR_NULL;
+  if (d->num_caches < 1 || d->hkv < 1 || d->page_size < 1 || d->max_pages_per_seq < 1 || d->num_pages < 1 ||
+      d->max_pages_out < 1 || d->num_pages_out < 1 || d->max_kept < 1 || d->weights_len < 0 || d->weights_len_out < 0 ||
+      d->num_free < 0)
+    return KVSHOT_ERR_SHAPE;
+  const int64_t page_rows = static_cast<int64_t>(d->hkv) * d->page_size;
+  if (d->num_caches > kMaxCaches || d->head_dim != kHeadDim || d->hkv > 16383 || page_rows >= INT_MAX ||
+      d->num_pages * page_rows >= INT_MAX || d->num_pages_out * page_rows >= INT_MAX)
+    return KVSHOT_ERR_UNSUPPORTED;
+  if (!k || !v || !page_table || !seq_lens || !kept || !kept_count || !k_out || !v_out || !page_table_out || !seq_lens_out)
+    return KVSHOT_ERR_NULL;
+  if ((weights == nullptr) != (weights_out == nullptr)) return KVSHOT_ERR_NULL;
+  const int given = (free_pages != nullptr) + (free_count != nullptr) + (free_count_out != nullptr);
+  if (given != 0 && given != 3) return KVSHOT_ERR_NULL;
+  for (const void* x : {k, v, static_cast<const void*>(k_out), static_cast<const void*>(v_out)})
+    if (!aligned(x, 16)) return KVSHOT_ERR_ALIGN;
+  for (const void* x : {static_cast<const void*>(page_table), static_cast<const void*>(seq_lens),
+                        static_cast<const void*>(kept), static_cast<const void*>(kept_count),
+                        static_cast<const void*>(weights), static_cast<const void*>(page_table_out),
+                        static_cast<const void*>(seq_lens_out), static_cast<const void*>(weights_out),
+                        static_cast<const void*>(free_pages), static_cast<const void*>(free_count),
+                        static_cast<const void*>(free_count_out)})
+    if (!aligned(x, 4)) return KVSHOT_ERR_ALIGN;
+  // In place means K, V and the table; weights in place keep their rows.
+  const bool in_place = k_out == k;
+  if (in_place != (v_out == v) || (in_place && (page_table_out != page_table || d->max_pages_out != d->max_pages_per_seq ||
+                                                d->num_pages_out != d->num_pages)))
+    return KVSHOT_ERR_SHAPE;
+  if (weights != nullptr && weights_out == weights && d->weights_len_out != d->weights_len) return KVSHOT_ERR_SHAPE;
+  const EvictParams p{static_cast<const uint8_t*>(k), static_cast<const uint8_t*>(v), static_cast<uint8_t*>(k_out),
+                      static_cast<uint8_t*>(v_out), weights, weights_out, page_table, page_table_out, seq_lens, kept,
+                      kept_count, free_count, seq_lens_out, free_pages, free_count_out, d->err_flag, d->num_caches, d->hkv,
+                      d->page_size, d->max_pages_per_seq, d->num_pages, d->max_pages_out, d->num_pages_out, d->max_kept,
+                      d->weights_len, d->weights_len_out, d->num_free, in_place ? 1 : 0};
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (launch_maybe_pdl(move_kernel, dim3(kRowPieces / kMovePieces, 2 * d->hkv + 1, d->num_caches), dim3(kMoveThreads), 0,
+                       false, s, p) != cudaSuccess)
+    return KVSHOT_ERR_CUDA;
+  const cudaError_t e = launch_maybe_pdl(evict_end_kernel, dim3(1), dim3(kEndThreads), 0, true, s, p);
+  return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
+}

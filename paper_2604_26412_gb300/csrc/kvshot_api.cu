@@ -277,8 +277,6 @@ kvshot_status check_common(const kvshot_attn_desc* d) {
   return KVSHOT_OK;
 }
 
-namespace {
-
 kvshot_status check_attn_desc(const kvshot_attn_desc* d, bool paged) {
   if (kvshot_status st = check_common(d)) return st;
   if (paged) {
@@ -295,6 +293,8 @@ kvshot_status check_attn_desc(const kvshot_attn_desc* d, bool paged) {
   }
   return KVSHOT_OK;
 }
+
+namespace {
 
 // `small_blocks`: an fp8 stack of more than 128 rows takes attn_f8.cu's 64-row blocks.
 kvshot_status make_plan_for(const kvshot_attn_desc* d, bool paged, bool small_blocks, Plan* pl) {

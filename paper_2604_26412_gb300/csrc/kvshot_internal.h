@@ -126,6 +126,8 @@ void rope_turns(float rope_base, uint64_t* turns);
 
 // Descriptor checks that do not depend on the cache layout, and the current device's number of SMs (0: an error).
 kvshot_status check_common(const kvshot_attn_desc* d);
+// With those of the layout, as kvshot_draft_attn makes them.
+kvshot_status check_attn_desc(const kvshot_attn_desc* d, bool paged);
 int sm_count();
 
 // Kernel launchers (one per translation unit).  Return cudaSuccess or the launch error.  `pdl`:

@@ -1,0 +1,88 @@
+// kvshot_partial.cuh -- what the entry points that draft over a part of a long cache have in common: the cache's view,
+// its checks, and operand fragments of mma.sync read straight from rows in global memory.
+#pragma once
+
+#include "kvshot_attn_common.cuh"
+
+namespace kvshot {
+namespace partial {
+namespace {  // internal linkage: every translation unit gets its own copy
+
+constexpr int kMaxGroup = 32;  // q heads of a KV head
+
+// A bf16 cache: paged (page_table) or contiguous (one page of l_cap tokens per cache).
+struct CacheView {
+  const int32_t *page_table, *seq_lens;
+  int32_t* err;
+  int C, hkv, P, max_pages, num_pages, len_bound;
+};
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+// Checks of the descriptor that all of them make.  (What check_attn_desc reads of heads and nodes is valid in a descriptor
+// that gives none of them but hq = hkv.)
+inline kvshot_status check_partial(const kvshot_attn_desc* d, bool paged) {
+  if (kvshot_status st = check_attn_desc(d, paged)) return st;
+  if (d->flags & (KVSHOT_TARGET_FP8 | KVSHOT_FORCE_CC | KVSHOT_FORCE_MMA | KVSHOT_FORCE_TC)) return KVSHOT_ERR_UNSUPPORTED;
+  if (d->hq / d->hkv > kMaxGroup) return KVSHOT_ERR_UNSUPPORTED;
+  // Rows of q, and rows of scores or picks, are 32-bit numbers; so are grids.
+  if (static_cast<int64_t>(d->num_caches) * d->n_query * d->hq >= (int64_t{1} << 31)) return KVSHOT_ERR_UNSUPPORTED;
+  if (d->hkv > 65535) return KVSHOT_ERR_UNSUPPORTED;
+  return KVSHOT_OK;
+}
+
+inline CacheView cache_view(const kvshot_attn_desc* d, const int32_t* page_table, const int32_t* seq_lens) {
+  CacheView v;
+  const bool paged = page_table != nullptr;
+  v.page_table = page_table;
+  v.seq_lens = seq_lens;
+  v.err = d->err_flag;
+  v.C = d->num_caches;
+  v.hkv = d->hkv;
+  v.P = paged ? d->page_size : d->l_cap;
+  v.max_pages = paged ? d->max_pages_per_seq : 1;
+  v.num_pages = paged ? d->num_pages : d->num_caches;
+  const int64_t room = static_cast<int64_t>(v.max_pages) * v.P;
+  v.len_bound = static_cast<int>(room < d->max_seq_len ? room : d->max_seq_len);
+  return v;
+}
+
+inline float score_scale(const kvshot_attn_desc* d) {
+  return d->scale != 0.f ? d->scale : 0.08838834764831845f;  // 1 / sqrt(128)
+}
+
+__device__ __forceinline__ int clamped_len(const CacheView& v, int c) {
+  const int L = v.seq_lens[c];
+  if (L >= 0 && L <= v.len_bound) return L;
+  dev::set_error(v.err, KVSHOT_ERR_DEVICE_BOUNDS);
+  return L < 0 ? 0 : v.len_bound;
+}
+
+// Pool page of page p of cache c, or -1 (recorded) if its id is outside the pool.
+__device__ __forceinline__ int page_id(const CacheView& v, int c, int p) {
+  if (v.page_table == nullptr) return c;
+  const int id = v.page_table[static_cast<size_t>(c) * v.max_pages + p];
+  if (static_cast<unsigned>(id) < static_cast<unsigned>(v.num_pages)) return id;
+  dev::set_error(v.err, KVSHOT_ERR_DEVICE_BOUNDS);
+  return -1;
+}
+
+__device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
+
+// Dot products of rows (keys, or bounds) with rows of q run as mma.sync m16n8k16 with the rows as M.  A sum over the dims
+// does not depend on their order, so lane (g, t) = (lane / 4, lane % 4) takes, of rows g and g + 8, the 16-byte pieces
+// 4 j + t: a load of the warp covers whole 64-byte segments of 8 rows, and piece j holds the A (and from a row of q alike
+// the B) operands of the k-steps 2 j and 2 j + 1.
+__device__ __forceinline__ void mma_piece(float (&d)[4], const uint4& a, const uint4& a8, const uint4& b) {
+  const uint32_t lo[4] = {a.x, a8.x, a.y, a8.y}, hi[4] = {a.z, a8.z, a.w, a8.w};
+  dev::mma_bf16_16816(d, lo, b.x, b.y);
+  dev::mma_bf16_16816(d, hi, b.z, b.w);
+}
+
+// Rows of q staged in shared memory, 16 pieces and 64 bytes of padding each: 8 rows' pieces 4 j .. 4 j + 3 are in different
+// banks.
+constexpr int kQRowBytes = 256 + 64;
+
+}  // namespace
+}  // namespace partial
+}  // namespace kvshot

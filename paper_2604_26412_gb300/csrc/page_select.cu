@@ -1,0 +1,365 @@
+// page_select.cu -- which pages or tokens of a cache matter: bounds of the pages' keys, scores of pages, and the best
+// entries of rows of scores.
+#include <algorithm>
+#include <climits>
+
+#include "kvshot_partial.cuh"
+
+namespace kvshot {
+namespace {
+
+using namespace dev;
+using namespace partial;
+
+// ------------------------------------------------------------ bounds
+
+constexpr int kBoundsThreads = 256;
+
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+  __nv_bfloat162 r = __hmin2_nan(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+  return *reinterpret_cast<uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+  return *reinterpret_cast<uint32_t*>(&r);
+}
+
+// A warp takes one (page, KV head): P rows of 256 bytes, two to a load.
+__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(CacheView v, const uint4* __restrict__ k,
+                                                               const int32_t* __restrict__ from, uint4* bounds) {
+  const int c = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int L = clamped_len(v, c);
+  const int p0 = from == nullptr ? 0 : max(0, from[c]) / v.P, pages = (L + v.P - 1) / v.P;
+  const int64_t units = static_cast<int64_t>(max(0, pages - p0)) * v.hkv;
+  for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kBoundsThreads / 32) + warp; u < units;
+       u += static_cast<int64_t>(gridDim.x) * (kBoundsThreads / 32)) {
+    const int p = p0 + static_cast<int>(u / v.hkv), h = static_cast<int>(u % v.hkv);
+    const int id = page_id(v, c, p);
+    if (id < 0) continue;
+    const int rows = min(v.P, L - p * v.P);
+    const uint4* src = k + (static_cast<size_t>(id) * v.hkv + h) * v.P * 16 + lane;
+    const int own = lane >> 4;  // this half-warp's rows: own, own + 2, ...
+    uint4 lo = make_uint4(0x7f807f80u, 0x7f807f80u, 0x7f807f80u, 0x7f807f80u);  // +inf
+    uint4 hi = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+    for (int r = own; r < rows; r += 16) {
+      uint4 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r + 2 * i < rows) x[i] = __ldg(src + (r - own + 2 * i) * 16);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r + 2 * i < rows) {
+          lo = make_uint4(min2(lo.x, x[i].x), min2(lo.y, x[i].y), min2(lo.z, x[i].z), min2(lo.w, x[i].w));
+          hi = make_uint4(max2(hi.x, x[i].x), max2(hi.y, x[i].y), max2(hi.z, x[i].z), max2(hi.w, x[i].w));
+        }
+    }
+    // The two half-warps' rows; then lanes 0 .. 15 hold the least and lanes 16 .. 31 the greatest.
+    auto other = [](uint32_t x) { return __shfl_xor_sync(0xffffffffu, x, 16); };
+    const uint4 lo2 = make_uint4(other(lo.x), other(lo.y), other(lo.z), other(lo.w));
+    const uint4 hi2 = make_uint4(other(hi.x), other(hi.y), other(hi.z), other(hi.w));
+    lo = make_uint4(min2(lo.x, lo2.x), min2(lo.y, lo2.y), min2(lo.z, lo2.z), min2(lo.w, lo2.w));
+    hi = make_uint4(max2(hi.x, hi2.x), max2(hi.y, hi2.y), max2(hi.z, hi2.z), max2(hi.w, hi2.w));
+    bounds[(static_cast<size_t>(id) * v.hkv + h) * 32 + lane] = own == 0 ? lo : hi;
+  }
+}
+
+// ------------------------------------------------------------ scores
+
+// max(q lo, q hi) = max(q, 0) hi + min(q, 0) lo, so a page's score is the product of [min(q, 0), max(q, 0)] with its
+// bounds [lo, hi], a row of 256 elements: 16 steps of mma.sync with 16 pages as M.
+constexpr int kScoreWarps = 4;
+constexpr int kScoreRows = 128;  // rows of q in shared memory at a time
+
+struct ScoreParams {
+  CacheView v;
+  const uint4* q;       // rows [C, Nq, hq]
+  const uint4* bounds;  // 32 pieces per (page, head): lo, hi
+  float* scores;
+  int hq, G, Nq, log_gp;  // G padded to 2^log_gp columns
+  float scale;
+};
+
+__global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p) {
+  __shared__ __align__(16) uint8_t s_q[kScoreRows * kQRowBytes];
+  const int c = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int g = lane >> 2, t = lane & 3;
+  const int L = clamped_len(p.v, c);
+  const int pages = (L + p.v.P - 1) / p.v.P;
+  const int cta0 = blockIdx.x * kScoreWarps * 16;
+  if (cta0 >= pages) return;
+  const int page[2] = {cta0 + warp * 16 + g, cta0 + warp * 16 + g + 8};
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  uint4 b[2][8];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int id = page[i] < pages ? page_id(p.v, c, page[i]) : -1;
+    const uint4* src = p.bounds + (static_cast<size_t>(max(id, 0)) * p.v.hkv + h) * 32 + t;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b[i][j] = id >= 0 ? __ldg(src + 4 * j) : zero;
+  }
+  const int gp = 1 << p.log_gp, rows = p.Nq << p.log_gp;
+  const int stride = p.v.max_pages * p.v.hkv;
+  float best[2] = {-INFINITY, -INFINITY};  // of a node whose columns are several tiles (gp > 8)
+  for (int r0 = 0; r0 < rows; r0 += kScoreRows) {
+    __syncthreads();
+    const int here = min(kScoreRows, (rows - r0 + 7) / 8 * 8);
+    for (int i = threadIdx.x; i < here * 16; i += kScoreWarps * 32) {
+      const int r = r0 + i / 16, n = r >> p.log_gp, j = r & (gp - 1);
+      const bool live = n < p.Nq && j < p.G;
+      const uint4 x = live ? __ldg(p.q + ((static_cast<size_t>(c) * p.Nq + n) * p.hq + h * p.G + j) * 16 + i % 16) : zero;
+      *reinterpret_cast<uint4*>(s_q + (i / 16) * kQRowBytes + (i % 16) * 16) = x;
+    }
+    __syncthreads();
+    for (int tile = 0; tile < here / 8; ++tile) {
+      float d[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint8_t* row = s_q + (tile * 8 + g) * kQRowBytes + t * 16;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint4 x = *reinterpret_cast<const uint4*>(row + j * 64);
+        mma_piece(d, b[0][j], b[1][j], make_uint4(min2(x.x, 0), min2(x.y, 0), min2(x.z, 0), min2(x.w, 0)));
+        mma_piece(d, b[0][j + 4], b[1][j + 4], make_uint4(max2(x.x, 0), max2(x.y, 0), max2(x.z, 0), max2(x.w, 0)));
+      }
+      // d: page g, columns 2 t and 2 t + 1; page g + 8, the same columns.
+      const int col = r0 + tile * 8 + 2 * t;
+      auto put = [&](int i, int n, float s) {
+        if (n < p.Nq && page[i] < pages)
+          p.scores[(static_cast<size_t>(c) * p.Nq + n) * stride + static_cast<size_t>(h) * p.v.max_pages + page[i]] =
+              s * p.scale;
+      };
+      if (gp == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) put(i >> 1, col + (i & 1), d[i]);
+        continue;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (((col + (i & 1)) & (gp - 1)) >= p.G) d[i] = -INFINITY;
+      float m[2] = {fmaxf(d[0], d[1]), fmaxf(d[2], d[3])};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (gp > 2) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 1));
+        if (gp > 4) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 2));
+      }
+      if (gp > 8) {
+        const bool last = ((col & (gp - 1)) >> 3) == (gp >> 3) - 1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          best[i] = fmaxf(best[i], m[i]);
+          m[i] = best[i];
+          if (last) best[i] = -INFINITY;
+        }
+        if (!last) continue;
+      }
+      if ((2 * t & (gp - 1)) == 0)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) put(i, col >> p.log_gp, m[i]);
+    }
+  }
+}
+
+// ------------------------------------------------------------ selection
+
+// A radix selection: the scores as integers of the same order, the keep-th greatest found digit by digit from counts, then
+// one ordered pass that writes what is above it and the first of what is equal.
+constexpr int kSelectThreads = 256;
+constexpr int kDigitBits = 11;
+constexpr int kBins = 1 << kDigitBits;
+
+struct SelectParams {
+  const float* scores;
+  const int32_t* seq_lens;
+  int32_t *picks, *counts, *err;
+  int row_len, rows_per_len, tokens_per_entry, keep, first, last;
+};
+
+__device__ __forceinline__ uint32_t order_key(float f) {
+  const uint32_t u = __float_as_uint(f);
+  if (f != f) return 0xffffffffu;
+  if (f == 0.f) return 0x80000000u;  // -0 is 0
+  return (u >> 31) != 0 ? ~u : u | 0x80000000u;
+}
+
+__global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p) {
+  constexpr int kWarps = kSelectThreads / 32;
+  __shared__ int s_hist[kBins];
+  __shared__ int s_warp[2][kWarps];
+  __shared__ uint32_t s_prefix;
+  __shared__ int s_need, s_done;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int len = p.seq_lens[row / p.rows_per_len];
+  int64_t entries = len > 0 ? (static_cast<int64_t>(len) + p.tokens_per_entry - 1) / p.tokens_per_entry : 0;
+  if (len < 0 || entries > p.row_len) {
+    set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
+    entries = min(entries, static_cast<int64_t>(p.row_len));
+  }
+  const int n = static_cast<int>(entries);
+  int32_t* picks = p.picks + static_cast<size_t>(row) * p.keep;
+  const int count = min(n, p.keep);
+  if (tid == 0) p.counts[row] = count;
+  for (int i = count + tid; i < p.keep; i += kSelectThreads) picks[i] = -1;
+  if (n <= p.keep) {
+    for (int i = tid; i < n; i += kSelectThreads) picks[i] = i;
+    return;
+  }
+  const float* s = p.scores + static_cast<size_t>(row) * p.row_len;
+  const int a = p.first, b = n - p.last;  // [a, b) compete for `need` places
+  int need = p.keep - p.first - p.last;
+  uint32_t prefix = 0, mask = 0;
+  if (need == 0) {
+    prefix = mask = 0xffffffffu;  // nothing is above a NaN, and of what is equal none is taken
+  } else {
+    for (int shift = 32 - kDigitBits;; shift = max(0, shift - kDigitBits)) {
+      const uint32_t digit_mask = (mask == 0 ? 0xffffffffu : ~mask) >> shift;
+      for (int i = tid; i < kBins; i += kSelectThreads) s_hist[i] = 0;
+      __syncthreads();
+      for (int i = a + tid; i < b; i += kSelectThreads) {
+        const uint32_t key = order_key(__ldg(s + i));
+        if ((key & mask) == prefix) atomicAdd(&s_hist[(key >> shift) & digit_mask], 1);
+      }
+      __syncthreads();
+      // Entries above each thread's bins, from the top bin down.
+      constexpr int kPer = kBins / kSelectThreads;
+      const int top = kBins - 1 - tid * kPer;
+      int sum = 0;
+      for (int i = 0; i < kPer; ++i) sum += s_hist[top - i];
+      int scan = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += x;
+      }
+      if (lane == 31) s_warp[0][warp] = scan;
+      __syncthreads();
+      int above = scan - sum;
+      for (int w = 0; w < warp; ++w) above += s_warp[0][w];
+      if (above < need && above + sum >= need) {
+        for (int i = 0;; ++i) {
+          const int here = s_hist[top - i];
+          if (above + here >= need) {
+            s_prefix = prefix | static_cast<uint32_t>(top - i) << shift;
+            s_need = need - above;
+            s_done = here == need - above;  // the whole bin is taken
+            break;
+          }
+          above += here;
+        }
+      }
+      __syncthreads();
+      prefix = s_prefix;
+      need = s_need;
+      mask |= digit_mask << shift;
+      if (shift == 0 || s_done) break;
+    }
+  }
+  // Each warp counts, then writes, a run of consecutive entries.
+  const int run = (n + kWarps * 32 - 1) / (kWarps * 32) * 32;
+  const int i0 = warp * run, i1 = min(n, i0 + run);
+  auto classify = [&](int i, bool& over, bool& equal) {
+    over = equal = false;
+    if (i >= n) return;
+    if (i < a || i >= b) {
+      over = true;
+      return;
+    }
+    const uint32_t key = order_key(__ldg(s + i)) & mask;
+    over = key > prefix;
+    equal = key == prefix;
+  };
+  int overs = 0, equals = 0;
+  for (int i = i0; i < i1; i += 32) {
+    bool over, equal;
+    classify(i + lane, over, equal);
+    overs += __popc(__ballot_sync(0xffffffffu, over));
+    equals += __popc(__ballot_sync(0xffffffffu, equal));
+  }
+  __syncthreads();
+  if (lane == 0) {
+    s_warp[0][warp] = overs;
+    s_warp[1][warp] = equals;
+  }
+  __syncthreads();
+  overs = equals = 0;
+  for (int w = 0; w < warp; ++w) {
+    overs += s_warp[0][w];
+    equals += s_warp[1][w];
+  }
+  for (int i = i0; i < i1; i += 32) {
+    bool over, equal;
+    classify(i + lane, over, equal);
+    const uint32_t mo = __ballot_sync(0xffffffffu, over), me = __ballot_sync(0xffffffffu, equal);
+    const uint32_t below = (1u << lane) - 1;
+    const int before = equals + __popc(me & below);
+    if (over || (equal && before < need)) picks[overs + __popc(mo & below) + min(before, need)] = i + lane;
+    overs += __popc(mo);
+    equals += __popc(me);
+  }
+}
+
+}  // namespace
+}  // namespace kvshot
+
+using namespace kvshot;
+
+extern "C" kvshot_status kvshot_page_bounds(const kvshot_attn_desc* d, const void* target_k, const int32_t* page_table,
+                                            const int32_t* seq_lens, const int32_t* from_tokens, void* bounds,
+                                            kvshot_stream_t stream) {
+  if (kvshot_status st = check_partial(d, true)) return st;
+  if (!target_k || !page_table || !seq_lens || !bounds) return KVSHOT_ERR_NULL;
+  if (!aligned(target_k, 16) || !aligned(bounds, 16) || !aligned(page_table, 4) || !aligned(seq_lens, 4) ||
+      !aligned(from_tokens, 4))
+    return KVSHOT_ERR_ALIGN;
+  const CacheView v = cache_view(d, page_table, seq_lens);
+  const int64_t units = static_cast<int64_t>((v.len_bound + v.P - 1) / v.P) * v.hkv;
+  if (units == 0) return KVSHOT_OK;
+  const int64_t most = std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * 64 / v.C);
+  const int x = static_cast<int>(std::min<int64_t>(most, (units + kBoundsThreads / 32 - 1) / (kBoundsThreads / 32)));
+  const cudaError_t e = launch_maybe_pdl(bounds_kernel, dim3(x, v.C), dim3(kBoundsThreads), 0, false,
+                                         reinterpret_cast<cudaStream_t>(stream), v, static_cast<const uint4*>(target_k),
+                                         from_tokens, static_cast<uint4*>(bounds));
+  return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
+}
+
+extern "C" kvshot_status kvshot_page_scores(const kvshot_attn_desc* d, const void* q, const void* bounds,
+                                            const int32_t* page_table, const int32_t* seq_lens, float* scores,
+                                            kvshot_stream_t stream) {
+  if (kvshot_status st = check_partial(d, true)) return st;
+  if (d->n_query == 0) return KVSHOT_OK;
+  if (!q || !bounds || !page_table || !seq_lens || !scores) return KVSHOT_ERR_NULL;
+  if (!aligned(q, 16) || !aligned(bounds, 16) || !aligned(page_table, 4) || !aligned(seq_lens, 4) || !aligned(scores, 4))
+    return KVSHOT_ERR_ALIGN;
+  ScoreParams p;
+  p.v = cache_view(d, page_table, seq_lens);
+  p.q = static_cast<const uint4*>(q);
+  p.bounds = static_cast<const uint4*>(bounds);
+  p.scores = scores;
+  p.hq = d->hq;
+  p.G = d->hq / d->hkv;
+  p.Nq = d->n_query;
+  p.log_gp = 0;
+  while ((1 << p.log_gp) < p.G) ++p.log_gp;
+  if ((static_cast<int64_t>(p.Nq) << p.log_gp) >= INT_MAX || static_cast<int64_t>(p.v.max_pages) * p.v.hkv >= INT_MAX)
+    return KVSHOT_ERR_UNSUPPORTED;
+  p.scale = score_scale(d);
+  const int pages = (p.v.len_bound + p.v.P - 1) / p.v.P, per_cta = kScoreWarps * 16;
+  if (pages == 0) return KVSHOT_OK;
+  const cudaError_t e = launch_maybe_pdl(scores_kernel, dim3((pages + per_cta - 1) / per_cta, p.v.hkv, p.v.C),
+                                         dim3(kScoreWarps * 32), 0, false, reinterpret_cast<cudaStream_t>(stream), p);
+  return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
+}
+
+extern "C" kvshot_status kvshot_select_top(const kvshot_select_desc* d, const float* scores, const int32_t* seq_lens,
+                                           int32_t* picks, int32_t* counts, kvshot_stream_t stream) {
+  if (d == nullptr) return KVSHOT_ERR_NULL;
+  if (d->num_rows < 0 || d->row_len < 1 || d->rows_per_len < 1 || d->num_rows % d->rows_per_len != 0 ||
+      d->tokens_per_entry < 1 || d->keep < 1 || d->first < 0 || d->last < 0 ||
+      static_cast<int64_t>(d->first) + d->last > d->keep)
+    return KVSHOT_ERR_SHAPE;
+  if (d->num_rows == 0) return KVSHOT_OK;
+  if (!scores || !seq_lens || !picks || !counts) return KVSHOT_ERR_NULL;
+  if (!aligned(scores, 4) || !aligned(seq_lens, 4) || !aligned(picks, 4) || !aligned(counts, 4)) return KVSHOT_ERR_ALIGN;
+  const SelectParams p{scores,          seq_lens,          picks,               counts,  d->err_flag, d->row_len,
+                       d->rows_per_len, d->tokens_per_entry, d->keep, d->first, d->last};
+  const cudaError_t e = launch_maybe_pdl(select_kernel, dim3(d->num_rows), dim3(kSelectThreads), 0, false,
+                                         reinterpret_cast<cudaStream_t>(stream), p);
+  return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
+}

@@ -39,7 +39,9 @@ EXPORTS = ("kvshot_draft_attn", "kvshot_draft_attn_workspace_size", "kvshot_draf
            "kvshot_version", "kvshot_draft_attn_static", "kvshot_gated_delta", "kvshot_gated_delta_workspace_size",
            "kvshot_kv_project", "kvshot_kv_project_workspace_size", "kvshot_draft_append_qknorm", "kvshot_cache_extend",
            "kvshot_kv4_cache_bytes", "kvshot_kv4_store", "kvshot_kv4_load", "kvshot_draft_attn_kv4_workspace_size",
-           "kvshot_draft_attn_kv4")
+           "kvshot_draft_attn_kv4", "kvshot_page_bounds", "kvshot_page_scores", "kvshot_select_top",
+           "kvshot_draft_attn_sparse_workspace_size", "kvshot_draft_attn_sparse", "kvshot_key_weights",
+           "kvshot_cache_evict")
 KVSHOT_PROJECT_ROPE = 0x1
 KV4_GROUP_TOKENS = 16    # KVSHOT_KV4_GROUP_TOKENS
 KV4_GROUP_BYTES = 2304   # KVSHOT_KV4_GROUP_BYTES
@@ -145,6 +147,41 @@ class Kv4Desc(ctypes.Structure):
     ]
 
 
+class SelectDesc(ctypes.Structure):
+    """Mirror of kvshot_select_desc."""
+
+    _fields_ = [
+        ("num_rows", ctypes.c_int32),
+        ("row_len", ctypes.c_int32),
+        ("rows_per_len", ctypes.c_int32),
+        ("tokens_per_entry", ctypes.c_int32),
+        ("keep", ctypes.c_int32),
+        ("first", ctypes.c_int32),
+        ("last", ctypes.c_int32),
+        ("err_flag", ctypes.c_void_p),
+    ]
+
+
+class EvictDesc(ctypes.Structure):
+    """Mirror of kvshot_evict_desc."""
+
+    _fields_ = [
+        ("num_caches", ctypes.c_int32),
+        ("hkv", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("max_pages_per_seq", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("max_pages_out", ctypes.c_int32),
+        ("num_pages_out", ctypes.c_int32),
+        ("max_kept", ctypes.c_int32),
+        ("weights_len", ctypes.c_int32),
+        ("weights_len_out", ctypes.c_int32),
+        ("num_free", ctypes.c_int32),
+        ("err_flag", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -197,6 +234,20 @@ def load(build_if_missing: bool = True):
     lib.kvshot_draft_attn_kv4.argtypes = [ctypes.POINTER(AttnDesc), P, P, P, P, P, P, P, ctypes.c_int32, ctypes.c_int32,
                                           P, P, P]
     lib.kvshot_draft_attn_kv4.restype = ctypes.c_int
+    lib.kvshot_page_bounds.argtypes = [ctypes.POINTER(AttnDesc), P, P, P, P, P, P]
+    lib.kvshot_page_bounds.restype = ctypes.c_int
+    lib.kvshot_page_scores.argtypes = [ctypes.POINTER(AttnDesc), P, P, P, P, P, P]
+    lib.kvshot_page_scores.restype = ctypes.c_int
+    lib.kvshot_select_top.argtypes = [ctypes.POINTER(SelectDesc), P, P, P, P, P]
+    lib.kvshot_select_top.restype = ctypes.c_int
+    lib.kvshot_draft_attn_sparse_workspace_size.argtypes = [ctypes.POINTER(AttnDesc), ctypes.c_int32]
+    lib.kvshot_draft_attn_sparse_workspace_size.restype = ctypes.c_size_t
+    lib.kvshot_draft_attn_sparse.argtypes = [ctypes.POINTER(AttnDesc), P, P, P, P, P, P, P, ctypes.c_int32, P, P, P, P, P, P]
+    lib.kvshot_draft_attn_sparse.restype = ctypes.c_int
+    lib.kvshot_key_weights.argtypes = [ctypes.POINTER(AttnDesc), P, P, P, P, P, ctypes.c_float, ctypes.c_int32, P, P, P]
+    lib.kvshot_key_weights.restype = ctypes.c_int
+    lib.kvshot_cache_evict.argtypes = [ctypes.POINTER(EvictDesc)] + [P] * 16
+    lib.kvshot_cache_evict.restype = ctypes.c_int
     lib.kvshot_status_string.argtypes = [ctypes.c_int]
     lib.kvshot_status_string.restype = ctypes.c_char_p
     lib.kvshot_version.argtypes = []
@@ -447,3 +498,110 @@ def draft_attn_kv4(desc: AttnDesc, q, cache, page_table, seq_lens, draft_k, draf
                                lse, stream)
     if st != KVSHOT_OK:
         raise KvshotError(st, "kvshot_draft_attn_kv4")
+
+
+def page_bounds_status(desc: AttnDesc, target_k, page_table, seq_lens, from_tokens, bounds, stream=None) -> int:
+    """Call kvshot_page_bounds (least and greatest key of each page); return its status."""
+    return (_lib or load()).kvshot_page_bounds(_dref(desc), _ptr(target_k), _ptr(page_table), _ptr(seq_lens),
+                                         _ptr(from_tokens), _ptr(bounds), _stream(stream))
+
+
+def page_bounds(desc: AttnDesc, target_k, page_table, seq_lens, from_tokens, bounds, stream=None) -> None:
+    st = page_bounds_status(desc, target_k, page_table, seq_lens, from_tokens, bounds, stream)
+    if st != KVSHOT_OK:
+        raise KvshotError(st, "kvshot_page_bounds")
+
+
+def page_scores_status(desc: AttnDesc, q, bounds, page_table, seq_lens, scores, stream=None) -> int:
+    """Call kvshot_page_scores (greatest possible score of each page, per draft token and KV head); return its status."""
+    return (_lib or load()).kvshot_page_scores(_dref(desc), _ptr(q), _ptr(bounds), _ptr(page_table), _ptr(seq_lens),
+                                         _ptr(scores), _stream(stream))
+
+
+def page_scores(desc: AttnDesc, q, bounds, page_table, seq_lens, scores, stream=None) -> None:
+    st = page_scores_status(desc, q, bounds, page_table, seq_lens, scores, stream)
+    if st != KVSHOT_OK:
+        raise KvshotError(st, "kvshot_page_scores")
+
+
+def make_select_desc(*, num_rows, row_len, keep, rows_per_len=1, tokens_per_entry=1, first=0, last=0,
+                     err_flag=None) -> SelectDesc:
+    return SelectDesc(int(num_rows), int(row_len), int(rows_per_len), int(tokens_per_entry), int(keep), int(first),
+                      int(last), _ptr(err_flag))
+
+
+def select_top_status(desc: SelectDesc, scores, seq_lens, picks, counts, stream=None) -> int:
+    """Call kvshot_select_top (the best entries of each row of scores); return its status."""
+    return (_lib or load()).kvshot_select_top(_dref(desc), _ptr(scores), _ptr(seq_lens), _ptr(picks), _ptr(counts),
+                                        _stream(stream))
+
+
+def select_top(desc: SelectDesc, scores, seq_lens, picks, counts, stream=None) -> None:
+    st = select_top_status(desc, scores, seq_lens, picks, counts, stream)
+    if st != KVSHOT_OK:
+        raise KvshotError(st, "kvshot_select_top")
+
+
+def draft_attn_sparse_workspace_size(desc: AttnDesc, max_picks: int) -> int:
+    return int((_lib or load()).kvshot_draft_attn_sparse_workspace_size(_dref(desc), int(max_picks)))
+
+
+def draft_attn_sparse_status(desc: AttnDesc, q, target_k, target_v, page_table, seq_lens, picks, counts, max_picks: int,
+                             draft_k, draft_v, tree_parent, out, lse, stream=None) -> int:
+    """Call kvshot_draft_attn_sparse (draft attention over selected pages) and return its status."""
+    return (_lib or load()).kvshot_draft_attn_sparse(_dref(desc), _ptr(q), _ptr(target_k), _ptr(target_v),
+                                               _ptr(page_table), _ptr(seq_lens), _ptr(picks), _ptr(counts),
+                                               int(max_picks), _ptr(draft_k), _ptr(draft_v), _ptr(tree_parent),
+                                               _ptr(out), _ptr(lse), _stream(stream))
+
+
+def draft_attn_sparse(desc: AttnDesc, q, target_k, target_v, page_table, seq_lens, picks, counts, max_picks: int, draft_k,
+                      draft_v, tree_parent, out, lse, stream=None) -> None:
+    st = draft_attn_sparse_status(desc, q, target_k, target_v, page_table, seq_lens, picks, counts, max_picks, draft_k,
+                                  draft_v, tree_parent, out, lse, stream)
+    if st != KVSHOT_OK:
+        raise KvshotError(st, "kvshot_draft_attn_sparse")
+
+
+def key_weights_status(desc: AttnDesc, q, target_k, page_table, seq_lens, lse, decay: float, weights_len: int, weights,
+                       weights_out, stream=None) -> int:
+    """Call kvshot_key_weights (softmax weights of the cached tokens, accumulated); return its status."""
+    return (_lib or load()).kvshot_key_weights(_dref(desc), _ptr(q), _ptr(target_k), _ptr(page_table), _ptr(seq_lens),
+                                         _ptr(lse), float(decay), int(weights_len), _ptr(weights), _ptr(weights_out),
+                                         _stream(stream))
+
+
+def key_weights(desc: AttnDesc, q, target_k, page_table, seq_lens, lse, decay: float, weights_len: int, weights,
+                weights_out, stream=None) -> None:
+    st = key_weights_status(desc, q, target_k, page_table, seq_lens, lse, decay, weights_len, weights, weights_out, stream)
+    if st != KVSHOT_OK:
+        raise KvshotError(st, "kvshot_key_weights")
+
+
+def make_evict_desc(*, num_caches, hkv, page_size, max_pages_per_seq, num_pages, max_kept, max_pages_out=None,
+                    num_pages_out=None, weights_len=0, weights_len_out=None, num_free=None, head_dim=128,
+                    err_flag=None) -> EvictDesc:
+    """What is not given of the destination is as in the source; num_free: num_pages, the most there can be."""
+    def same(x, y):
+        return int(y if x is None else x)
+    return EvictDesc(int(num_caches), int(hkv), int(head_dim), int(page_size), int(max_pages_per_seq), int(num_pages),
+                     same(max_pages_out, max_pages_per_seq), same(num_pages_out, num_pages), int(max_kept),
+                     int(weights_len), same(weights_len_out, weights_len), same(num_free, num_pages), _ptr(err_flag))
+
+
+def cache_evict_status(desc: EvictDesc, k, v, page_table, seq_lens, kept, kept_count, weights, k_out, v_out,
+                       page_table_out, seq_lens_out, weights_out, free_pages, free_count, free_count_out,
+                       stream=None) -> int:
+    """Call kvshot_cache_evict (kept tokens moved to the front, the other pages given back); return its status."""
+    return (_lib or load()).kvshot_cache_evict(_dref(desc), _ptr(k), _ptr(v), _ptr(page_table), _ptr(seq_lens), _ptr(kept),
+                                         _ptr(kept_count), _ptr(weights), _ptr(k_out), _ptr(v_out),
+                                         _ptr(page_table_out), _ptr(seq_lens_out), _ptr(weights_out), _ptr(free_pages),
+                                         _ptr(free_count), _ptr(free_count_out), _stream(stream))
+
+
+def cache_evict(desc: EvictDesc, k, v, page_table, seq_lens, kept, kept_count, weights, k_out, v_out, page_table_out,
+                seq_lens_out, weights_out, free_pages, free_count, free_count_out, stream=None) -> None:
+    st = cache_evict_status(desc, k, v, page_table, seq_lens, kept, kept_count, weights, k_out, v_out, page_table_out,
+                            seq_lens_out, weights_out, free_pages, free_count, free_count_out, stream)
+    if st != KVSHOT_OK:
+        raise KvshotError(st, "kvshot_cache_evict")
