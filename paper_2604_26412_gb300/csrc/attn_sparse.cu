@@ -29,21 +29,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t cluster_size() {
-  uint32_t n;
-  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
-  return n;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float remote_float(uint32_t addr, uint32_t rank) {
-  float x;
-  asm volatile("{\n\t.reg .u32 ra;\n\tmapa.shared::cluster.u32 ra, %1, %2;\n\tld.shared::cluster.f32 %0, [ra];\n\t}"
-               : "=f"(x) : "r"(addr), "r"(rank) : "memory");
-  return x;
-}
-
 // Running softmax of one warp: the q heads of the KV head (padded to 8 NT rows) are the N columns of both products, so a
 // decoded row costs each MMA little padding; 16 keys at a time are the M rows of S^T = K Q^T and the depth of
 // O^T = V^T P^T.  Lane (g, t) keeps for rows 2 t, 2 t + 1 of each n-tile the reference, its part of the sum, and the

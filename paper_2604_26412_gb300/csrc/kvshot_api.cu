@@ -69,6 +69,8 @@ bool encode_rows_fp8(CUtensorMap* map, const void* base, uint64_t rows, uint32_t
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+}  // namespace
+
 // Grouped views of a [rows, 128] bf16 matrix for the tensor-memory kernel (kGroupBytes in
 // kvshot_internal.h): a box lands as 8-row groups of 2 KB, each holding its rows' dims 0..63
 // (128-byte swizzled) and then dims 64..127.
@@ -100,6 +102,8 @@ bool encode_rows_group3(CUtensorMap* map, const void* base, uint64_t rows) {
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+namespace {
 
 constexpr int kMaxScaleExp = 64;
 
@@ -170,8 +174,6 @@ void rope_turns(float rope_base, uint64_t* turns) {
   std::copy(table, table + kHeadDim / 2, turns);
 }
 
-namespace {
-
 // 4-D view {128 dims, hq, Nq, C} of q [C, Nq, hq, 128]; a box is one 64-dim
 // half of `heads` heads of one KV group for `nodes` draft nodes (rows node-major).
 bool encode_q(CUtensorMap* map, const void* q, int C, int Nq, int hq, QBox qb) {
@@ -187,6 +189,8 @@ bool encode_q(CUtensorMap* map, const void* q, int C, int Nq, int hq, QBox qb) {
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+namespace {
 
 struct Plan {
   Kernel kernel;

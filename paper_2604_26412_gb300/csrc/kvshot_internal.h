@@ -118,6 +118,12 @@ struct TensorMaps {
 bool encode_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint32_t box_cols,
                     uint32_t box_rows);
 
+// Maps that land 8-row groups of a [rows, 128] bf16 matrix as the tensor-memory kernels read them (4-D: `groups` groups
+// from a row-group coordinate, rows a multiple of 8; 3-D: one from any row), and boxes of q [C, Nq, hq, 128].
+bool encode_rows_grouped(CUtensorMap* map, const void* base, uint64_t rows, uint32_t groups);
+bool encode_rows_group3(CUtensorMap* map, const void* base, uint64_t rows);
+bool encode_q(CUtensorMap* map, const void* q, int C, int Nq, int hq, QBox qb);
+
 // inv_freq[j] = rope_base^(-2j/128), j in [0, 64).  Each thread keeps the table of its last rope_base (64 pow calls
 // are ~1.3 us of a call's host time).
 void rope_frequencies(float rope_base, double* inv_freq);

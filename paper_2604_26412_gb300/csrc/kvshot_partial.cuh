@@ -67,6 +67,21 @@ __device__ __forceinline__ int page_id(const CacheView& v, int c, int p) {
   return -1;
 }
 
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t n;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
+  return n;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float remote_float(uint32_t addr, uint32_t rank) {
+  float x;
+  asm volatile("{\n\t.reg .u32 ra;\n\tmapa.shared::cluster.u32 ra, %1, %2;\n\tld.shared::cluster.f32 %0, [ra];\n\t}"
+               : "=f"(x) : "r"(addr), "r"(rank) : "memory");
+  return x;
+}
+
 __device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
 
 // Dot products of rows (keys, or bounds) with rows of q run as mma.sync m16n8k16 with the rows as M.  A sum over the dims
