@@ -51,20 +51,25 @@ __device__ __forceinline__ int checked_page(const EvictParams& p, const int32_t*
   return -1;
 }
 
-// Rows move in ascending order, a chunk of them at a time: the chunk is loaded whole, then stored.  A token's new place is
-// never behind its old one and both ascend, so a chunk's stores never reach what a later chunk loads, and in place one
-// barrier between a chunk's loads and stores is enough.  A row's 16-byte pieces are independent of one another, so CTAs
-// take different pieces of all rows (blockIdx.x), heads, and K or V.
+// A row of 256 bytes is 16 pieces of 16; a thread moves one piece of several rows.  A chunk of rows is loaded whole, then
+// stored, and the next chunk's places are looked up while its bytes are on their way.
+//
+// Into another pool a CTA takes one chunk of a head's K or V.  In place chunks go in ascending order: a token's new place is
+// never behind its old one and both ascend, so a chunk's stores never reach what a later chunk loads, and one barrier
+// between a chunk's loads and its stores is enough.  There a CTA takes all chunks, and where that leaves SMs idle only 4 or 8
+// of the 16 pieces, which are independent of one another.
 constexpr int kMoveThreads = 256;
-constexpr int kMovePieces = 4;                             // 16-byte pieces of a row that a CTA takes
-constexpr int kMoveRows = kMoveThreads / kMovePieces;      // rows of a load
-constexpr int kMoveLoads = 4;                              // loads of a chunk
+constexpr int kMoveLoads = 8;  // rows of a thread and chunk
 constexpr int kRowPieces = kHeadDim * 2 / 16;
+constexpr int kMoveItems = kMoveThreads * kMoveLoads;
 
+template <bool kInPlace, int kPieces>
 __global__ void __launch_bounds__(kMoveThreads) move_kernel(EvictParams p) {
+  constexpr int kRows = kMoveItems / kPieces;  // of a chunk
+  __shared__ int s_src[2][kRows], s_dst[2][kRows];  // row of KV head 0 in its pool, or -1
+  allow_dependent_launch();
   const int c = blockIdx.z, y = blockIdx.y, tid = threadIdx.x;
   const CacheKeep ck = cache_keep(p, c, p.seq_lens[c], p.kept_count[c]);
-  if (ck.kept <= 0) return;
   const int32_t* kept = p.kept + static_cast<size_t>(c) * p.max_kept;
   if (y == 2 * p.hkv) {  // the weights: one CTA
     if (p.weights == nullptr || blockIdx.x != 0) return;
@@ -88,31 +93,57 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(EvictParams p) {
     }
     return;
   }
-  const int h = y >> 1, piece = blockIdx.x * kMovePieces + tid % kMovePieces;
-  const uint4* src = reinterpret_cast<const uint4*>((y & 1) != 0 ? p.v : p.k);
-  uint4* dst = reinterpret_cast<uint4*>((y & 1) != 0 ? p.v_out : p.k_out);
-  for (int i0 = 0; i0 < ck.kept; i0 += kMoveLoads * kMoveRows) {
+  const int head = (y >> 1) * p.P, piece = (kInPlace ? blockIdx.x * kPieces : 0) + tid % kPieces;
+  const uint4* src = reinterpret_cast<const uint4*>((y & 1) != 0 ? p.v : p.k) + static_cast<size_t>(head) * kRowPieces + piece;
+  uint4* dst = reinterpret_cast<uint4*>((y & 1) != 0 ? p.v_out : p.k_out) + static_cast<size_t>(head) * kRowPieces + piece;
+  auto look_up = [&](int i0, int buf) {
+#pragma unroll
+    for (int r = tid; r < kRows; r += kMoveThreads) {
+      const int at = i0 + r, j = at < ck.kept ? old_place(p, kept, at, ck.len) : -1;
+      int from = -1, to = -1;
+      if (j >= 0 && !(kInPlace && j == at)) {
+        const int pj = j / p.P, pa = at / p.P;
+        const int a = checked_page(p, p.page_table, p.max_pages, c, pj, p.num_pages);
+        const int b = checked_page(p, p.page_table_out, p.max_pages_out, c, pa, p.num_pages_out);
+        if (a >= 0 && b >= 0) {
+          from = a * p.hkv * p.P + (j - pj * p.P);
+          to = b * p.hkv * p.P + (at - pa * p.P);
+        }
+      }
+      s_src[buf][r] = from;
+      s_dst[buf][r] = to;
+    }
+  };
+  int i0 = kInPlace ? 0 : blockIdx.x * kRows;
+  if (i0 >= ck.kept) return;
+  look_up(i0, 0);
+  __syncthreads();
+  for (int buf = 0;; buf ^= 1) {
     uint4 x[kMoveLoads];
-    bool live[kMoveLoads];
+    int to[kMoveLoads];  // (read before the barrier: behind it these places may already be a later chunk's)
 #pragma unroll
     for (int i = 0; i < kMoveLoads; ++i) {
-      const int at = i0 + i * kMoveRows + tid / kMovePieces;
-      const int j = at < ck.kept ? old_place(p, kept, at, ck.len) : -1;
-      live[i] = j >= 0 && !(p.in_place && j == at);
-      if (!live[i]) continue;
-      const int id = checked_page(p, p.page_table, p.max_pages, c, j / p.P, p.num_pages);
-      live[i] = id >= 0;
-      if (live[i]) x[i] = src[((static_cast<size_t>(id) * p.hkv + h) * p.P + j % p.P) * kRowPieces + piece];
+      const int from = s_src[buf][i * (kMoveThreads / kPieces) + tid / kPieces];
+      to[i] = s_dst[buf][i * (kMoveThreads / kPieces) + tid / kPieces];
+      if (from >= 0) x[i] = kInPlace ? src[static_cast<size_t>(from) * kRowPieces] : __ldg(src + static_cast<size_t>(from) * kRowPieces);
     }
-    __syncthreads();
+    i0 += kRows;
+    if (kInPlace) {
+      if (i0 < ck.kept) look_up(i0, buf ^ 1);
+      __syncthreads();
+    }
 #pragma unroll
-    for (int i = 0; i < kMoveLoads; ++i) {
-      if (!live[i]) continue;
-      const int at = i0 + i * kMoveRows + tid / kMovePieces;
-      const int id = checked_page(p, p.page_table_out, p.max_pages_out, c, at / p.P, p.num_pages_out);
-      if (id >= 0) dst[((static_cast<size_t>(id) * p.hkv + h) * p.P + at % p.P) * kRowPieces + piece] = x[i];
-    }
+    for (int i = 0; i < kMoveLoads; ++i)
+      if (to[i] >= 0) dst[static_cast<size_t>(to[i]) * kRowPieces] = x[i];
+    if (!kInPlace || i0 >= ck.kept) break;
   }
+}
+
+template <bool kInPlace, int kPieces>
+cudaError_t launch_move(const EvictParams& p, cudaStream_t stream) {
+  const int room = static_cast<int>(std::min<int64_t>(p.max_kept, static_cast<int64_t>(p.max_pages_out) * p.P));
+  const int x = kInPlace ? kRowPieces / kPieces : (room + kMoveItems / kPieces - 1) / (kMoveItems / kPieces);
+  return launch_maybe_pdl(move_kernel<kInPlace, kPieces>, dim3(x, 2 * p.hkv + 1, p.C), dim3(kMoveThreads), 0, false, stream, p);
 }
 
 // Lengths and free pages: one CTA, a thread per cache, then a warp per cache writes its pages.
@@ -206,9 +237,13 @@ extern "C" kvshot_status kvshot_cache_evict(const kvshot_evict_desc* d, const vo
                       d->page_size, d->max_pages_per_seq, d->num_pages, d->max_pages_out, d->num_pages_out, d->max_kept,
                       d->weights_len, d->weights_len_out, d->num_free, in_place ? 1 : 0};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (launch_maybe_pdl(move_kernel, dim3(kRowPieces / kMovePieces, 2 * d->hkv + 1, d->num_caches), dim3(kMoveThreads), 0,
-                       false, s, p) != cudaSuccess)
-    return KVSHOT_ERR_CUDA;
+  // In place: whole rows while those alone are two CTAs to an SM.
+  const int64_t ctas = 2LL * d->hkv * d->num_caches, enough = 2LL * sm_count();
+  const cudaError_t moved = !in_place            ? launch_move<false, 16>(p, s)
+                            : ctas >= enough     ? launch_move<true, 16>(p, s)
+                            : 2 * ctas >= enough ? launch_move<true, 8>(p, s)
+                                                 : launch_move<true, 4>(p, s);
+  if (moved != cudaSuccess) return KVSHOT_ERR_CUDA;
   const cudaError_t e = launch_maybe_pdl(evict_end_kernel, dim3(1), dim3(kEndThreads), 0, true, s, p);
   return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
 }

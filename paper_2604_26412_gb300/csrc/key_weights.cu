@@ -133,18 +133,20 @@ static_assert(kDirectWarps * 32 == kDirectKeys, "a thread per key");
 
 // More than 16 rows per KV head: tcgen05.  128 keys are the M rows of S = K Q^T and the query rows (up to 256 of whole
 // nodes) its N columns, so that a key is a lane of tensor memory and its thread sums its own columns: no exchange between
-// threads.  One persistent CTA per SM takes an equal run of the caches' tiles, cut into pieces of one cache; a piece is
+// threads.  S is handed over in parts of up to 128 columns, two of them for each half of the warps: while one part's
+// exponentials are summed, the products of the next fill the other.  One persistent CTA per SM takes an equal run of the caches' tiles, cut into pieces of one cache; a piece is
 // passed over once per KV head and block of rows, K tiles streaming through a ring while the next pass's q is loaded.  The
 // sums of a piece's keys stay in weights_out between passes (4 bytes per key beside 256 of K, in L2), written and read
 // by the same thread.
-//   warps 0..3, 4..7   sums of the piece's even and odd tiles, each with an S of its own in tensor memory
+//   warps 0..3, 4..7   sums of the piece's even and odd tiles
 //   warp 8             TMA;  warp 9: MMA, and the owner of tensor memory
 constexpr int kTcThreads = 320;
 constexpr int kTcKeys = 128;
 constexpr int kTcMaxRows = 256;
 constexpr int kTcTileBytes = kTcKeys * 256;
 constexpr int kTcMaxStages = 6;
-constexpr int kTcTmemCols = 512;
+constexpr int kTcPart = 128;      // columns of S handed over at a time
+constexpr int kTcTmemCols = 512;  // four parts
 constexpr int kTcSmem = 232448;                      // what a CTA can have
 constexpr int kTcTail = 2 * kTcMaxRows * 4 + 512;    // row sums, barriers
 // Tiles of a piece, at most: one pass's K of all CTAs stays in L2 for the next block of rows; and 32 where there is one block.
@@ -212,7 +214,7 @@ struct TcCursor {
 };
 
 struct TcBarriers {
-  uint64_t kfull[kTcMaxStages], kempty[kTcMaxStages], qfull[2], qempty[2], sfull[2], sempty[2], done;
+  uint64_t kfull[kTcMaxStages], kempty[kTcMaxStages], qfull[2], qempty[2], sfull[4], sempty[4], done;
   uint32_t tmem;
 };
 
@@ -261,6 +263,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_addr(&bar.qfull[i]), 1);
       mbar_init(smem_addr(&bar.qempty[i]), 1);
+    }
+    for (int i = 0; i < 4; ++i) {
       mbar_init(smem_addr(&bar.sfull[i]), 1);
       mbar_init(smem_addr(&bar.sempty[i]), 4);
     }
@@ -343,7 +347,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       mbar_wait(smem_addr(&bar.kfull[i % p.stages]), (i / p.stages) & 1, err);
     for (int i = max(0, q_issued - 2); i < q_issued; ++i) mbar_wait(smem_addr(&bar.qfull[i & 1]), (i >> 1) & 1, err);
   } else if (warp == 9) {  // ---- products
-    const uint32_t idesc = tc::idesc_bf16(kTcKeys, p.cols, false);
     int stage = 0, pass_no = 0;
     uint32_t phase = 0, uses[2] = {0, 0};
     bool ok = true;
@@ -353,22 +356,28 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&bar.qfull[qb]), (pass_no >> 1) & 1, err, limit));
         const uint32_t qbase = smem_addr(smem) + qb * qbytes;
         for (int i = 0; ok && i < pc.tiles; ++i) {
-          const int b = i & 1;
-          if (uses[b] > 0) ok = mbar_wait(smem_addr(&bar.sempty[b]), (uses[b] - 1) & 1, err, limit);
-          ok = ok && mbar_wait(smem_addr(&bar.kfull[stage]), phase, err, limit);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          tc::tc_fence_after();
-          const uint32_t kbase = smem_addr(ring) + stage * kTcTileBytes;
+          const int w = i & 1;
+          for (int col = 0; col < p.cols; col += kTcPart) {
+            // Part n of warpgroup w takes its buffer n & 1 for the (n / 2)th time.
+            const int b = 2 * w + (uses[w] & 1);
+            if (uses[w] >= 2) ok = mbar_wait(smem_addr(&bar.sempty[b]), ((uses[w] >> 1) - 1) & 1, err, limit);
+            if (col == 0) ok = ok && mbar_wait(smem_addr(&bar.kfull[stage]), phase, err, limit);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc::tc_fence_after();
+            const uint32_t idesc = tc::idesc_bf16(kTcKeys, min(kTcPart, p.cols - col), false);
+            const uint32_t kbase = smem_addr(ring) + stage * kTcTileBytes, qpart = qbase + col * 128;
 #pragma unroll
-          for (int ks = 0; ks < 8; ++ks) {
-            const uint64_t ad = tc::smem_desc_sw128(kbase + (ks >> 2) * kGroupHalfBytes + (ks & 3) * 32, 16, kGroupBytes);
-            const uint64_t bd = tc::smem_desc_sw128(qbase + (ks >> 2) * (p.cols * 128) + (ks & 3) * 32, 16, 1024);
-            tc::tc_mma_elect(tmem + b * kTcMaxRows, ad, bd, idesc, ks > 0);
+            for (int ks = 0; ks < 8; ++ks) {
+              const uint64_t ad = tc::smem_desc_sw128(kbase + (ks >> 2) * kGroupHalfBytes + (ks & 3) * 32, 16, kGroupBytes);
+              const uint64_t bd = tc::smem_desc_sw128(qpart + (ks >> 2) * (p.cols * 128) + (ks & 3) * 32, 16, 1024);
+              tc::tc_mma_elect(tmem + b * kTcPart, ad, bd, idesc, ks > 0);
+            }
+            tc::tc_commit_elect(smem_addr(&bar.sfull[b]));
+            ++uses[w];
           }
+          if (!ok) break;
           tc::tc_commit_elect(smem_addr(&bar.kempty[stage]));
-          tc::tc_commit_elect(smem_addr(&bar.sfull[b]));
-          ++uses[b];
           if (++stage == p.stages) {
             stage = 0;
             phase ^= 1u;
@@ -381,7 +390,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     mbar_wait(smem_addr(&bar.done), 0, err);
   } else {  // ---- sums
     const int wg = warp >> 2, tid = threadIdx.x & 127;
-    const uint32_t my_tmem = tmem + wg * kTcMaxRows + (static_cast<uint32_t>(warp & 3) << 21);
+    const uint32_t my_tmem = tmem + 2 * wg * kTcPart + (static_cast<uint32_t>(warp & 3) << 21);
     int pass_no = 0;
     uint32_t uses = 0;
     bool ok = true;
@@ -406,36 +415,41 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             if (pass > 0) before = p.w.weights_out[at];
             else if (p.w.weights != nullptr) before = p.w.decay * p.w.weights[at];
           }
-          ok = mbar_wait(smem_addr(&bar.sfull[wg]), uses & 1, err, limit);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          tc::tc_fence_after();
           float2 sum[2] = {};
-          const int whole = rows / 32;
-          uint32_t v[32], v2[32];
-          if (whole > 0) tc::tmem_ld32(my_tmem, v);
-          for (int cc = 0; cc < whole; cc += 2) {
-            wait_ld_of(v);
-            if (cc + 1 < whole) tc::tmem_ld32(my_tmem + 32 * (cc + 1), v2);
-            add_columns(v, z + 32 * cc, p.w.qscale, sum);
-            if (cc + 1 < whole) {
-              wait_ld_of(v2);
-              if (cc + 2 < whole) tc::tmem_ld32(my_tmem + 32 * (cc + 2), v);
-              add_columns(v2, z + 32 * (cc + 1), p.w.qscale, sum);
+          for (int col = 0; col < p.cols; col += kTcPart, ++uses) {
+            const int b = uses & 1, here = min(kTcPart, rows - col);
+            ok = mbar_wait(smem_addr(&bar.sfull[2 * wg + b]), (uses >> 1) & 1, err, limit);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc::tc_fence_after();
+            const uint32_t at_tmem = my_tmem + b * kTcPart;
+            const float* zc = z + col;
+            const int whole = here / 32;
+            uint32_t v[32], v2[32];
+            if (whole > 0) tc::tmem_ld32(at_tmem, v);
+            for (int cc = 0; cc < whole; cc += 2) {
+              wait_ld_of(v);
+              if (cc + 1 < whole) tc::tmem_ld32(at_tmem + 32 * (cc + 1), v2);
+              add_columns(v, zc + 32 * cc, p.w.qscale, sum);
+              if (cc + 1 < whole) {
+                wait_ld_of(v2);
+                if (cc + 2 < whole) tc::tmem_ld32(at_tmem + 32 * (cc + 2), v);
+                add_columns(v2, zc + 32 * (cc + 1), p.w.qscale, sum);
+              }
             }
-          }
-          for (int col = whole * 32; col < rows; col += 4) {
-            uint32_t u[4];
-            tc::tmem_ld4(my_tmem + col, u);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3])::"memory");
+            for (int x = whole * 32; x < here; x += 4) {
+              uint32_t u[4];
+              tc::tmem_ld4(at_tmem + x, u);
+              asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3])::"memory");
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (col + e < rows) sum[0].x += ex2(fmaf(__uint_as_float(u[e]), p.w.qscale, z[col + e]));
+              for (int e = 0; e < 4; ++e)
+                if (x + e < here) sum[0].x += ex2(fmaf(__uint_as_float(u[e]), p.w.qscale, zc[x + e]));
+            }
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&bar.sempty[2 * wg + b]));
           }
-          tc::tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_addr(&bar.sempty[wg]));
-          ++uses;
+          if (!ok) break;
           if (live) p.w.weights_out[at] = before + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
         }
       }

@@ -80,7 +80,7 @@ struct ScoreParams {
 };
 
 __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p) {
-  __shared__ __align__(16) uint8_t s_q[kScoreRows * kQRowBytes];
+  extern __shared__ __align__(16) uint8_t s_q[];  // up to kScoreRows rows
   const int c = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t = lane & 3;
   const int L = clamped_len(p.v, c);
@@ -159,12 +159,8 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p)
 
 // ------------------------------------------------------------ selection
 
-// A radix selection: the scores as integers of the same order, the keep-th greatest found digit by digit from counts, then
-// one ordered pass that writes what is above it and the first of what is equal.
-constexpr int kSelectThreads = 256;
-constexpr int kDigitBits = 11;
-constexpr int kBins = 1 << kDigitBits;
-
+// A radix selection: the scores as integers of the same order, the last one to be picked found digit by digit from counts of
+// the digits, then one ordered pass that writes what is above it and the first of what is equal.
 struct SelectParams {
   const float* scores;
   const int32_t* seq_lens;
@@ -179,13 +175,10 @@ __device__ __forceinline__ uint32_t order_key(float f) {
   return (u >> 31) != 0 ? ~u : u | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p) {
-  constexpr int kWarps = kSelectThreads / 32;
-  __shared__ int s_hist[kBins];
-  __shared__ int s_warp[2][kWarps];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_need, s_done;
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+struct SelectRow {
+  int n, count;  // entries; picks
+};
+__device__ __forceinline__ SelectRow select_row(const SelectParams& p, int row) {
   const int len = p.seq_lens[row / p.rows_per_len];
   int64_t entries = len > 0 ? (static_cast<int64_t>(len) + p.tokens_per_entry - 1) / p.tokens_per_entry : 0;
   if (len < 0 || entries > p.row_len) {
@@ -193,70 +186,229 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p) 
     entries = min(entries, static_cast<int64_t>(p.row_len));
   }
   const int n = static_cast<int>(entries);
-  int32_t* picks = p.picks + static_cast<size_t>(row) * p.keep;
-  const int count = min(n, p.keep);
-  if (tid == 0) p.counts[row] = count;
-  for (int i = count + tid; i < p.keep; i += kSelectThreads) picks[i] = -1;
-  if (n <= p.keep) {
-    for (int i = tid; i < n; i += kSelectThreads) picks[i] = i;
-    return;
+  return SelectRow{n, min(n, p.keep)};
+}
+
+// The bin in which the need-th greatest entry is, from the bins' counts: each thread takes consecutive bins, the top ones
+// first.  s_warp [warps of the block] is scratch.  Found by one thread, which calls found(bin, entries above it).
+template <int kThreads, int kBins, typename Found>
+__device__ __forceinline__ void find_bin(const int* hist, int need, int* s_warp, Found found) {
+  constexpr int kPer = kBins / kThreads;
+  static_assert(kPer * kThreads == kBins, "whole bins");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, top = kBins - 1 - tid * kPer;
+  int h[kPer], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) sum += h[i] = hist[top - i];
+  int scan = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, scan, o);
+    if (lane >= o) scan += x;
   }
+  if (lane == 31) s_warp[warp] = scan;
+  __syncthreads();
+  int above = scan - sum;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w)
+    if (w < warp) above += s_warp[w];
+  if (above < need && above + sum >= need) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (above < need && above + h[i] >= need) found(top - i, above);
+      above += h[i];
+    }
+  }
+}
+
+__device__ __forceinline__ void remote_add(int* at, uint32_t rank, int v) {
+  asm volatile("{\n\t.reg .u32 ra;\n\tmapa.shared::cluster.u32 ra, %0, %1;\n\tred.shared::cluster.add.s32 [ra], %2;\n\t}" ::"r"(
+                   smem_addr(at)),
+               "r"(rank), "r"(v)
+               : "memory");
+}
+__device__ __forceinline__ int remote_int(const int* at, uint32_t rank) {
+  int v;
+  asm volatile("{\n\t.reg .u32 ra;\n\tmapa.shared::cluster.u32 ra, %1, %2;\n\tld.shared::cluster.s32 %0, [ra];\n\t}"
+               : "=r"(v) : "r"(smem_addr(at)), "r"(rank) : "memory");
+  return v;
+}
+
+// A row is read once: a cluster of CTAs (one, for rows of up to kThreads x kSelectKeys entries) holds its keys in registers,
+// every warp a run of consecutive entries.  Each CTA counts the digits of its own keys and adds what it counted to the
+// counts of all CTAs, which then each find the digit for themselves.  What bounds it: the latencies of a load, two to four
+// rounds of counts and a scan, and the shared atomics of digits that agree.
+constexpr int kSelectKeys = 16;
+constexpr int kMaxSelectCluster = 8;
+
+template <int kThreads, int kBits, bool kCluster>
+__global__ void __launch_bounds__(kThreads) select_kernel(SelectParams p) {
+  constexpr int kBins = 1 << kBits, kWarps = kThreads / 32, kPasses = (32 + kBits - 1) / kBits;
+  __shared__ int s_hist[2][kBins];
+  __shared__ int s_total[kCluster ? kPasses : 1][kCluster ? kBins : 1];  // over the cluster
+  __shared__ int s_warp[2][kWarps], s_sum[2];
+  __shared__ int s_bin, s_above;
+  const int S = kCluster ? static_cast<int>(cluster_size()) : 1, rank = kCluster ? blockIdx.x % S : 0;
+  const int row = blockIdx.x / S, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const SelectRow r = select_row(p, row);
+  const int n = r.n;
+  int32_t* picks = p.picks + static_cast<size_t>(row) * p.keep;
+  if (rank == 0 && tid == 0) p.counts[row] = r.count;
+  for (int i = r.count + rank * kThreads + tid; i < p.keep; i += S * kThreads) picks[i] = -1;
+  if (n <= p.keep) {
+    for (int i = rank * kThreads + tid; i < n; i += S * kThreads) picks[i] = i;
+    return;  // (the whole cluster)
+  }
+  // This CTA's entries [e0, e1), warp w's from e0 + 32 w rounds on.
+  const int chunk = ((n + S - 1) / S + 31) / 32 * 32, e0 = min(n, rank * chunk), e1 = min(n, e0 + chunk);
+  const int rounds = (chunk + kThreads - 1) / kThreads, w0 = e0 + warp * rounds * 32 + lane;
   const float* s = p.scores + static_cast<size_t>(row) * p.row_len;
   const int a = p.first, b = n - p.last;  // [a, b) compete for `need` places
   int need = p.keep - p.first - p.last;
-  uint32_t prefix = 0, mask = 0;
-  if (need == 0) {
-    prefix = mask = 0xffffffffu;  // nothing is above a NaN, and of what is equal none is taken
-  } else {
-    for (int shift = 32 - kDigitBits;; shift = max(0, shift - kDigitBits)) {
-      const uint32_t digit_mask = (mask == 0 ? 0xffffffffu : ~mask) >> shift;
-      for (int i = tid; i < kBins; i += kSelectThreads) s_hist[i] = 0;
-      __syncthreads();
-      for (int i = a + tid; i < b; i += kSelectThreads) {
-        const uint32_t key = order_key(__ldg(s + i));
-        if ((key & mask) == prefix) atomicAdd(&s_hist[(key >> shift) & digit_mask], 1);
-      }
-      __syncthreads();
-      // Entries above each thread's bins, from the top bin down.
-      constexpr int kPer = kBins / kSelectThreads;
-      const int top = kBins - 1 - tid * kPer;
-      int sum = 0;
-      for (int i = 0; i < kPer; ++i) sum += s_hist[top - i];
-      int scan = sum;
+  float f[kSelectKeys];
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, scan, o);
-        if (lane >= o) scan += x;
+  for (int k = 0; k < kSelectKeys; ++k) f[k] = k < rounds && w0 + 32 * k < e1 ? __ldg(s + w0 + 32 * k) : 0.f;
+  for (int i = tid; i < 2 * kBins; i += kThreads) s_hist[i / kBins][i % kBins] = 0;
+  if (kCluster)
+    for (int i = tid; i < kPasses * kBins; i += kThreads) s_total[kCluster ? i / kBins : 0][kCluster ? i % kBins : 0] = 0;
+  if (kCluster) cluster_sync_all();
+  else __syncthreads();
+  uint32_t key[kSelectKeys], inside = 0;  // bit k: entry k competes
+#pragma unroll
+  for (int k = 0; k < kSelectKeys; ++k) {
+    const int i = w0 + 32 * k;
+    key[k] = order_key(f[k]);
+    inside |= static_cast<uint32_t>(k < rounds && i < e1 && i >= a && i < b) << k;
+  }
+  uint32_t prefix = 0, mask = 0;
+  if (need == 0) prefix = mask = 0xffffffffu;  // nothing is above a NaN, and of what is equal none is taken
+  for (int pass = 0, shift = 32 - kBits; need > 0; ++pass, shift = max(0, shift - kBits)) {
+    int* hist = s_hist[pass & 1];
+    const uint32_t digit_mask = (mask == 0 ? 0xffffffffu : ~mask) >> shift;
+#pragma unroll
+    for (int k = 0; k < kSelectKeys; ++k)
+      if ((inside >> k & 1u) != 0 && (key[k] & mask) == prefix) atomicAdd(&hist[(key[k] >> shift) & digit_mask], 1);
+    __syncthreads();
+    if (kCluster) {
+      int* total = s_total[kCluster ? pass : 0];
+      for (int i = tid; i < kBins; i += kThreads) {
+        const int v = hist[i];
+        if (v == 0) continue;
+        hist[i] = 0;
+        for (int x = 0; x < S; ++x) remote_add(total + i, x, v);
       }
-      if (lane == 31) s_warp[0][warp] = scan;
-      __syncthreads();
-      int above = scan - sum;
-      for (int w = 0; w < warp; ++w) above += s_warp[0][w];
-      if (above < need && above + sum >= need) {
-        for (int i = 0;; ++i) {
-          const int here = s_hist[top - i];
-          if (above + here >= need) {
-            s_prefix = prefix | static_cast<uint32_t>(top - i) << shift;
-            s_need = need - above;
-            s_done = here == need - above;  // the whole bin is taken
-            break;
-          }
-          above += here;
-        }
-      }
-      __syncthreads();
-      prefix = s_prefix;
-      need = s_need;
-      mask |= digit_mask << shift;
-      if (shift == 0 || s_done) break;
+      cluster_sync_all();
+      hist = total;
+    } else {
+      for (int i = tid; i < kBins; i += kThreads) s_hist[(pass + 1) & 1][i] = 0;
+    }
+    find_bin<kThreads, kBins>(hist, need, s_warp[0], [&](int bin, int above) {
+      s_bin = bin;
+      s_above = above;
+    });
+    __syncthreads();
+    const int bin = s_bin;
+    prefix |= static_cast<uint32_t>(bin) << shift;
+    mask |= digit_mask << shift;
+    need -= s_above;
+    if (shift == 0 || hist[bin] == need) break;  // (the whole bin is taken)
+  }
+  // What is above the found prefix, and equal to it; forced entries count as above.
+  uint32_t over = 0, equal = 0;
+  int overs = 0, equals = 0;
+#pragma unroll
+  for (int k = 0; k < kSelectKeys; ++k) {
+    const int i = w0 + 32 * k;
+    const bool in = (inside >> k & 1u) != 0, forced = k < rounds && i < e1 && !in;
+    const bool o = forced || (in && (key[k] & mask) > prefix), e = in && (key[k] & mask) == prefix;
+    over |= static_cast<uint32_t>(o) << k;
+    equal |= static_cast<uint32_t>(e) << k;
+    overs += __popc(__ballot_sync(0xffffffffu, o));
+    equals += __popc(__ballot_sync(0xffffffffu, e));
+  }
+  __syncthreads();
+  if (lane == 0) {
+    s_warp[0][warp] = overs;
+    s_warp[1][warp] = equals;
+  }
+  __syncthreads();
+  overs = equals = 0;
+  int all_overs = 0, all_equals = 0;
+  for (int w = 0; w < kWarps; ++w) {
+    if (w == warp) overs = all_overs, equals = all_equals;
+    all_overs += s_warp[0][w];
+    all_equals += s_warp[1][w];
+  }
+  if (kCluster) {
+    if (tid == 0) s_sum[0] = all_overs, s_sum[1] = all_equals;
+    cluster_sync_all();
+    for (int x = 0; x < rank; ++x) {
+      overs += remote_int(&s_sum[0], x);
+      equals += remote_int(&s_sum[1], x);
     }
   }
+  const uint32_t below = (1u << lane) - 1;
+#pragma unroll
+  for (int k = 0; k < kSelectKeys; ++k) {
+    const bool o = (over >> k & 1u) != 0, e = (equal >> k & 1u) != 0;
+    const uint32_t mo = __ballot_sync(0xffffffffu, o), me = __ballot_sync(0xffffffffu, e);
+    const int before = equals + __popc(me & below);
+    if (o || (e && before < need)) picks[overs + __popc(mo & below) + min(before, need)] = w0 + 32 * k;
+    overs += __popc(mo);
+    equals += __popc(me);
+  }
+  if (kCluster) cluster_sync_all();  // (another CTA may still read this one's sums)
+}
+
+// Rows too long for a cluster's registers: one CTA, which reads the scores again for every digit.
+constexpr int kLongThreads = 1024;
+constexpr int kLongBits = 11;
+
+__global__ void __launch_bounds__(kLongThreads) select_long_kernel(SelectParams p) {
+  constexpr int kWarps = kLongThreads / 32, kBins = 1 << kLongBits;
+  __shared__ int s_hist[kBins];
+  __shared__ int s_warp[2][kWarps];
+  __shared__ int s_bin, s_above;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const SelectRow r = select_row(p, row);
+  const int n = r.n;
+  int32_t* picks = p.picks + static_cast<size_t>(row) * p.keep;
+  if (tid == 0) p.counts[row] = r.count;
+  for (int i = r.count + tid; i < p.keep; i += kLongThreads) picks[i] = -1;
+  if (n <= p.keep) {
+    for (int i = tid; i < n; i += kLongThreads) picks[i] = i;
+    return;
+  }
+  const float* s = p.scores + static_cast<size_t>(row) * p.row_len;
+  const int a = p.first, b = n - p.last;
+  int need = p.keep - p.first - p.last;
+  uint32_t prefix = 0, mask = 0;
+  if (need == 0) prefix = mask = 0xffffffffu;
+  for (int shift = 32 - kLongBits; need > 0; shift = max(0, shift - kLongBits)) {
+    const uint32_t digit_mask = (mask == 0 ? 0xffffffffu : ~mask) >> shift;
+    __syncthreads();
+    for (int i = tid; i < kBins; i += kLongThreads) s_hist[i] = 0;
+    __syncthreads();
+    for (int i = a + tid; i < b; i += kLongThreads) {
+      const uint32_t key = order_key(__ldg(s + i));
+      if ((key & mask) == prefix) atomicAdd(&s_hist[(key >> shift) & digit_mask], 1);
+    }
+    __syncthreads();
+    find_bin<kLongThreads, kBins>(s_hist, need, s_warp[0], [&](int bin, int above) {
+      s_bin = bin;
+      s_above = above;
+    });
+    __syncthreads();
+    prefix |= static_cast<uint32_t>(s_bin) << shift;
+    mask |= digit_mask << shift;
+    need -= s_above;
+    if (shift == 0 || s_hist[s_bin] == need) break;
+  }
   // Each warp counts, then writes, a run of consecutive entries.
-  const int run = (n + kWarps * 32 - 1) / (kWarps * 32) * 32;
-  const int i0 = warp * run, i1 = min(n, i0 + run);
+  const int run = ((n + kWarps - 1) / kWarps + 31) / 32 * 32;
+  const int i0 = min(n, warp * run), i1 = min(n, i0 + run);
   auto classify = [&](int i, bool& over, bool& equal) {
     over = equal = false;
-    if (i >= n) return;
+    if (i >= i1) return;
     if (i < a || i >= b) {
       over = true;
       return;
@@ -295,6 +447,21 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p) 
   }
 }
 
+template <int kThreads, int kBits, bool kCluster>
+cudaError_t launch_select(const SelectParams& p, int rows, int S, cudaStream_t stream) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = S;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(rows * S);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = kCluster ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, select_kernel<kThreads, kBits, kCluster>, p);
+}
+
 }  // namespace
 }  // namespace kvshot
 
@@ -311,7 +478,8 @@ extern "C" kvshot_status kvshot_page_bounds(const kvshot_attn_desc* d, const voi
   const CacheView v = cache_view(d, page_table, seq_lens);
   const int64_t units = static_cast<int64_t>((v.len_bound + v.P - 1) / v.P) * v.hkv;
   if (units == 0) return KVSHOT_OK;
-  const int64_t most = std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * 64 / v.C);
+  // After growth most caches have a page or two to do, and CTAs without work are what costs.
+  const int64_t most = std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * (from_tokens != nullptr ? 8 : 64) / v.C);
   const int x = static_cast<int>(std::min<int64_t>(most, (units + kBoundsThreads / 32 - 1) / (kBoundsThreads / 32)));
   const cudaError_t e = launch_maybe_pdl(bounds_kernel, dim3(x, v.C), dim3(kBoundsThreads), 0, false,
                                          reinterpret_cast<cudaStream_t>(stream), v, static_cast<const uint4*>(target_k),
@@ -342,8 +510,9 @@ extern "C" kvshot_status kvshot_page_scores(const kvshot_attn_desc* d, const voi
   p.scale = score_scale(d);
   const int pages = (p.v.len_bound + p.v.P - 1) / p.v.P, per_cta = kScoreWarps * 16;
   if (pages == 0) return KVSHOT_OK;
+  const size_t smem = static_cast<size_t>(std::min(kScoreRows, ((p.Nq << p.log_gp) + 7) / 8 * 8)) * kQRowBytes;
   const cudaError_t e = launch_maybe_pdl(scores_kernel, dim3((pages + per_cta - 1) / per_cta, p.v.hkv, p.v.C),
-                                         dim3(kScoreWarps * 32), 0, false, reinterpret_cast<cudaStream_t>(stream), p);
+                                         dim3(kScoreWarps * 32), smem, false, reinterpret_cast<cudaStream_t>(stream), p);
   return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
 }
 
@@ -354,12 +523,24 @@ extern "C" kvshot_status kvshot_select_top(const kvshot_select_desc* d, const fl
       d->tokens_per_entry < 1 || d->keep < 1 || d->first < 0 || d->last < 0 ||
       static_cast<int64_t>(d->first) + d->last > d->keep)
     return KVSHOT_ERR_SHAPE;
+  if (d->num_rows >= INT_MAX / kMaxSelectCluster) return KVSHOT_ERR_UNSUPPORTED;
   if (d->num_rows == 0) return KVSHOT_OK;
   if (!scores || !seq_lens || !picks || !counts) return KVSHOT_ERR_NULL;
   if (!aligned(scores, 4) || !aligned(seq_lens, 4) || !aligned(picks, 4) || !aligned(counts, 4)) return KVSHOT_ERR_ALIGN;
   const SelectParams p{scores,          seq_lens,          picks,               counts,  d->err_flag, d->row_len,
                        d->rows_per_len, d->tokens_per_entry, d->keep, d->first, d->last};
-  const cudaError_t e = launch_maybe_pdl(select_kernel, dim3(d->num_rows), dim3(kSelectThreads), 0, false,
-                                         reinterpret_cast<cudaStream_t>(stream), p);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const int n = d->row_len, rows = d->num_rows;
+  auto cluster = [&](int per_cta) {
+    int S = 2;
+    while (S < kMaxSelectCluster && S * per_cta < n) S *= 2;
+    return S;
+  };
+  cudaError_t e;
+  if (n <= 128 * kSelectKeys) e = launch_select<128, 8, false>(p, rows, 1, st);
+  else if (n <= 512 * kSelectKeys && 2 * rows > sm_count()) e = launch_select<512, 11, false>(p, rows, 1, st);
+  else if (n <= 512 * kSelectKeys * kMaxSelectCluster) e = launch_select<512, 11, true>(p, rows, cluster(4096), st);
+  else if (n <= 1024 * kSelectKeys * kMaxSelectCluster) e = launch_select<1024, 11, true>(p, rows, kMaxSelectCluster, st);
+  else e = launch_maybe_pdl(select_long_kernel, dim3(rows), dim3(kLongThreads), 0, false, st, p);
   return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
 }
