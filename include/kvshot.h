@@ -517,7 +517,8 @@ kvshot_status kvshot_select_top(const kvshot_select_desc* desc, const float* sco
  * i < counts[c, n, h], and the draft keys that kvshot_draft_attn gives that row.
  * picks: [C, Nq, hkv, max_picks] int32, each list ascending; counts: [C, Nq, hkv] int32 in [0, max_picks].  A pick that
  * is not above its predecessor or not a page below the cache's length is recorded as KVSHOT_ERR_DEVICE_BOUNDS and passed
- * over, a count out of range recorded and clamped.  Other arguments as for kvshot_draft_attn.
+ * over, a count out of range recorded and clamped.  Other arguments as for kvshot_draft_attn, but target_k/v and
+ * draft_k/v 32-byte aligned.
  * The softmax weights are rounded to bf16 for the tensor cores, sums are fp32.
  * Workspace: kvshot_draft_attn_sparse_workspace_size bytes (0 if the descriptor is invalid), as for kvshot_draft_attn.
  */
@@ -531,7 +532,7 @@ kvshot_status kvshot_draft_attn_sparse(const kvshot_attn_desc* desc, const void*
 /*
  * weights_out[c, j] = decay * weights[c, j] + sum over the query rows n and q heads of exp(scale q . k_j - lse[c, n, head])
  * for every token j < L_c: what the softmax whose lse kvshot_draft_attn returned gave the token, summed.  A row whose lse
- * is -inf adds nothing.  [C, weights_len] fp32; entries past the length are left as they are.  weights may be weights_out, or NULL (zeros).
+ * is -inf adds nothing.  q, and keys below the length, must be finite.  [C, weights_len] fp32; entries past the length are left as they are.  weights may be weights_out, or NULL (zeros).
  * decay in [0, 1]; with 0 weights is not read.  Sums are fp32 and their order fixed.
  * page_table NULL: a contiguous cache [C, hkv, l_cap, 128].  A length above weights_len is recorded as out of bounds, too.
  */

@@ -53,24 +53,26 @@ struct WarpState {
   // kr: this lane's rows of K (keys g and g + 8 of the 16), vr: of V (keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9); -1: no key.
   __device__ __forceinline__ void step(const uint4* __restrict__ k, const uint4* __restrict__ v, const int (&kr)[2],
                                        const int (&vr)[4], float qscale, int g, int t) {
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    uint4 a[2][4], b[4][2];
+    // 32-byte loads: lane (g, t) has pieces 2 t, 2 t + 1 of each half of its key rows, and 2 g, 2 g + 1 of its value rows.
+    const Row32 none = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    Row32 a[2][2], b[4];
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) a[e][j] = kr[e] >= 0 ? __ldg(k + static_cast<size_t>(kr[e]) * 16 + 4 * j + t) : zero;
+      for (int j = 0; j < 2; ++j) a[e][j] = kr[e] >= 0 ? load32(k + static_cast<size_t>(kr[e]) * 16 + 8 * j + 2 * t) : none;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) b[e][j] = vr[e] >= 0 ? __ldg(v + static_cast<size_t>(vr[e]) * 16 + 2 * g + j) : zero;
+    for (int e = 0; e < 4; ++e) b[e] = vr[e] >= 0 ? load32(v + static_cast<size_t>(vr[e]) * 16 + 2 * g) : none;
     uint32_t p0[NT], p1[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};  // (two chains of products)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) mma_piece(s, a[0][j], a[1][j], q[nt][j]);
+      for (int j = 0; j < 2; ++j) {
+        mma_piece(s, a[0][j].lo, a[1][j].lo, q[nt][2 * j]);
+        mma_piece(s2, a[0][j].hi, a[1][j].hi, q[nt][2 * j + 1]);
+      }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] = kr[e >> 1] >= 0 ? s[e] * qscale : -INFINITY;
+      for (int e = 0; e < 4; ++e) s[e] = kr[e >> 1] >= 0 ? (s[e] + s2[e]) * qscale : -INFINITY;
       const float top0 = fmaxf(s[0], s[2]), top1 = fmaxf(s[1], s[3]);
       // The reference moves only when a score is more than 2^8 above it: P stays in range, and the exchange and the
       // rescaling are rare.
@@ -104,8 +106,8 @@ struct WarpState {
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t w0 = word(b[0][i >> 2], i & 3), w1 = word(b[1][i >> 2], i & 3);
-      const uint32_t w2 = word(b[2][i >> 2], i & 3), w3 = word(b[3][i >> 2], i & 3);
+      const uint32_t w0 = word(i < 4 ? b[0].lo : b[0].hi, i & 3), w1 = word(i < 4 ? b[1].lo : b[1].hi, i & 3);
+      const uint32_t w2 = word(i < 4 ? b[2].lo : b[2].hi, i & 3), w3 = word(i < 4 ? b[3].lo : b[3].hi, i & 3);
       const uint32_t av[4] = {__byte_perm(w0, w1, 0x5410), __byte_perm(w0, w1, 0x7632), __byte_perm(w2, w3, 0x5410),
                               __byte_perm(w2, w3, 0x7632)};
 #pragma unroll
@@ -144,7 +146,7 @@ __global__ void __launch_bounds__(kSparseThreads) sparse_kernel(SparseParams p) 
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      st.q[nt][j] = nt * 8 + g < p.G ? __ldg(p.q + (qrow + nt * 8 + g) * 16 + 4 * j + t) : make_uint4(0, 0, 0, 0);
+      st.q[nt][j] = nt * 8 + g < p.G ? __ldg(p.q + (qrow + nt * 8 + g) * 16 + 8 * (j >> 1) + 2 * t + (j & 1)) : make_uint4(0, 0, 0, 0);
 
   const int i0 = static_cast<int>(static_cast<int64_t>(count) * rank / S);
   const int i1 = static_cast<int>(static_cast<int64_t>(count) * (rank + 1) / S);
@@ -306,8 +308,10 @@ extern "C" kvshot_status kvshot_draft_attn_sparse(const kvshot_attn_desc* d, con
   if (!q || !target_k || !target_v || !page_table || !seq_lens || !picks || !counts || !draft_k || !draft_v || !out || !lse ||
       (tree && !tree_parent))
     return KVSHOT_ERR_NULL;
-  for (const void* x : {q, target_k, target_v, draft_k, draft_v, static_cast<const void*>(out)})
+  for (const void* x : {q, static_cast<const void*>(out)})
     if (!aligned(x, 16)) return KVSHOT_ERR_ALIGN;
+  for (const void* x : {target_k, target_v, draft_k, draft_v})  // (read 32 bytes at a time)
+    if (!aligned(x, 32)) return KVSHOT_ERR_ALIGN;
   for (const void* x : {static_cast<const void*>(page_table), static_cast<const void*>(seq_lens),
                         static_cast<const void*>(picks), static_cast<const void*>(counts),
                         static_cast<const void*>(tree ? tree_parent : nullptr), static_cast<const void*>(lse)})

@@ -34,7 +34,7 @@ __device__ __forceinline__ float neg_log2_sum(float z) { return z == -INFINITY ?
 
 // ------------------------------------------------------------ few rows
 
-// Up to 16 rows per KV head.  A warp's keys are the M rows of mma.sync, the query rows its columns; operands go from global
+// Up to 8 rows per KV head, 16 in small calls.  A warp's keys are the M rows of mma.sync, the query rows its columns; operands go from global
 // memory straight to registers, the next keys' while the present ones' are multiplied.  A lane sums the exponentials of
 // its keys' columns over its heads; the heads are shared out over a cluster of CTAs where there are few keys, whose sums
 // meet in shared memory in rank order.
@@ -131,22 +131,27 @@ static_assert(kDirectWarps * 32 == kDirectKeys, "a thread per key");
 
 // ------------------------------------------------------------ many rows
 
-// More than 16 rows per KV head: tcgen05.  128 keys are the M rows of S = K Q^T and the query rows (up to 256 of whole
+// More rows per KV head: tcgen05.  128 keys are the M rows of S = K Q^T and the query rows (up to 256 of whole
 // nodes) its N columns, so that a key is a lane of tensor memory and its thread sums its own columns: no exchange between
-// threads.  S is handed over in parts of up to 128 columns, two of them for each half of the warps: while one part's
-// exponentials are summed, the products of the next fill the other.  One persistent CTA per SM takes an equal run of the caches' tiles, cut into pieces of one cache; a piece is
-// passed over once per KV head and block of rows, K tiles streaming through a ring while the next pass's q is loaded.  The
-// sums of a piece's keys stay in weights_out between passes (4 bytes per key beside 256 of K, in L2), written and read
-// by the same thread.
-//   warps 0..3, 4..7   sums of the piece's even and odd tiles
-//   warp 8             TMA;  warp 9: MMA, and the owner of tensor memory
-constexpr int kTcThreads = 320;
+// threads.  One persistent CTA per SM takes an equal run of the caches' tiles, cut into pieces of one cache; a piece is
+// passed over once per KV head and block of rows, K tiles streaming through a ring while the next pass's q is loaded.
+//   warps 0..3, 4..7  sums of the piece's even and odd tiles.  S comes in units of up to 128 columns; each warpgroup has two
+//                     units' room in tensor memory.  Its keys' sums stay with their threads until the piece's end.
+//   warp 8            TMA, and the rows' lse;  warp 9: MMA, and the owner of tensor memory
+// Up to 128 rows the call reads K at the copy's rate (16 x 32K tokens 166 to 170 us, floor 160).  With 256 rows (20K to 32K
+// tokens each) it takes 232 us, 1.0 PFLOP/s: the products alone, with nothing behind them, take 187, the exponentials alone
+// 193, and the two wait for each other.  Slower there: a warpgroup for a unit of every tile 259 us, four warpgroups of 64
+// columns 276; two units' products in turn 250; units taken to registers whole 248; lse kept in registers 400.
+constexpr int kTcGroups = 2;  // warpgroups
+constexpr int kTcLoadWarp = 4 * kTcGroups, kTcMmaWarp = kTcLoadWarp + 1;
+constexpr int kTcThreads = (kTcMmaWarp + 1) * 32;
 constexpr int kTcKeys = 128;
 constexpr int kTcMaxRows = 256;
 constexpr int kTcTileBytes = kTcKeys * 256;
 constexpr int kTcMaxStages = 6;
 constexpr int kTcPart = 128;      // columns of S handed over at a time
-constexpr int kTcTmemCols = 512;  // four parts
+constexpr int kTcUnits = 4;       // room for them in tensor memory
+constexpr int kTcTmemCols = kTcUnits * kTcPart;
 constexpr int kTcSmem = 232448;                      // what a CTA can have
 constexpr int kTcTail = 2 * kTcMaxRows * 4 + 512;    // row sums, barriers
 // Tiles of a piece, at most: one pass's K of all CTAs stays in L2 for the next block of rows; and 32 where there is one block.
@@ -161,6 +166,14 @@ struct WeightTcParams {
 struct WeightMaps {
   CUtensorMap k, q;
 };
+
+// A wait that looks a few times before it takes the time (reading the clock takes long enough to be late).
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int32_t* err, uint64_t limit) {
+  if (limit >= kPollBelowNs)
+    for (int i = 0; i < 32; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+  return mbar_wait(bar, parity, err, limit);
+}
 
 struct TcPiece {
   int c, tile, tiles, len;
@@ -214,7 +227,8 @@ struct TcCursor {
 };
 
 struct TcBarriers {
-  uint64_t kfull[kTcMaxStages], kempty[kTcMaxStages], qfull[2], qempty[2], sfull[4], sempty[4], done;
+  uint64_t kfull[kTcMaxStages], kempty[kTcMaxStages], qfull[2], qempty[2], zfull[2], zempty[2];
+  uint64_t sfull[kTcUnits], sempty[kTcUnits], done;
   uint32_t tmem;
 };
 
@@ -263,8 +277,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_addr(&bar.qfull[i]), 1);
       mbar_init(smem_addr(&bar.qempty[i]), 1);
+      mbar_init(smem_addr(&bar.zfull[i]), 1);
+      mbar_init(smem_addr(&bar.zempty[i]), 4 * kTcGroups);
     }
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kTcUnits; ++i) {
       mbar_init(smem_addr(&bar.sfull[i]), 1);
       mbar_init(smem_addr(&bar.sempty[i]), 4);
     }
@@ -273,7 +289,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     prefetch_tensormap(&maps.k);
     prefetch_tensormap(&maps.q);
   }
-  if (warp == 9) {
+  if (warp == kTcMmaWarp) {
     tc::tmem_alloc(smem_addr(&bar.tmem), kTcTmemCols);
     tc::tmem_relinquish();
   }
@@ -288,7 +304,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   TcPiece pc;
   const int passes = hkv * p.blocks;
 
-  if (warp == 8) {  // ---- loads
+  if (warp == kTcLoadWarp) {  // ---- loads
     const uint64_t once = l2_policy_evict_first();
     const int boxes = kTcKeys / p.box_rows, P = p.w.v.P;
     int stage = 0, pass_no = 0, q_issued = 0;
@@ -306,7 +322,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       for (int pass = 0; ok && pass < passes; ++pass, ++pass_no) {
         const int h = pass / p.blocks, rb = pass % p.blocks, qb = pass_no & 1;
         const uint32_t qbar = smem_addr(&bar.qfull[qb]);
-        if (pass_no >= 2) ok = mbar_wait(smem_addr(&bar.qempty[qb]), ((pass_no >> 1) - 1) & 1, err, limit);
+        if (pass_no >= 2) ok = wait(smem_addr(&bar.qempty[qb]), ((pass_no >> 1) - 1) & 1, err, limit);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (lane == 0) {
@@ -317,11 +333,26 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           tma_load_4d(dst + p.cols * 128, &maps.q, 64, h * G, rb * p.nodes_per_block, pc.c, qbar);
         }
         ++q_issued;
+        // The rows' lse.  (Its loads are under way while the pass's first tiles are asked for.)
+        const int n0 = rb * p.nodes_per_block, rows = min(p.nodes_per_block, p.w.Nq - n0) * G;
+        float z[kTcMaxRows / 32];
+#pragma unroll
+        for (int i = 0; i < kTcMaxRows / 32; ++i) {
+          const int r = i * 32 + lane;
+          z[i] = r < rows ? __ldg(p.w.lse + (static_cast<size_t>(pc.c) * p.w.Nq + n0 + r / G) * p.w.hq + h * G + r % G) : -INFINITY;
+        }
+        auto put_lse = [&] {
+          if (pass_no >= 2) ok = __all_sync(0xffffffffu, wait(smem_addr(&bar.zempty[qb]), ((pass_no >> 1) - 1) & 1, err, limit));
+#pragma unroll
+          for (int i = 0; i < kTcMaxRows / 32; ++i) s_z[qb * kTcMaxRows + i * 32 + lane] = neg_log2_sum(z[i]);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_addr(&bar.zfull[qb]));
+        };
         for (int i = 0; i < pc.tiles; ++i) {
           const int64_t row = next;
           // (the next tile's look-up is under way while this one waits for room)
           next = box_row(pc.c, pc.tile + (i + 1 < pc.tiles ? i + 1 : 0), pc.len);
-          if (issued >= static_cast<uint32_t>(p.stages)) ok = mbar_wait(smem_addr(&bar.kempty[stage]), phase, err, limit);
+          if (issued >= static_cast<uint32_t>(p.stages)) ok = wait(smem_addr(&bar.kempty[stage]), phase, err, limit);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           const uint32_t full = smem_addr(&bar.kfull[stage]);
@@ -339,6 +370,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             stage = 0;
             phase ^= 1u;
           }
+          if (i == 0) put_lse();
+          if (!ok) break;
         }
       }
     }
@@ -346,22 +379,22 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     for (uint32_t i = issued > static_cast<uint32_t>(p.stages) ? issued - p.stages : 0; i < issued; ++i)
       mbar_wait(smem_addr(&bar.kfull[i % p.stages]), (i / p.stages) & 1, err);
     for (int i = max(0, q_issued - 2); i < q_issued; ++i) mbar_wait(smem_addr(&bar.qfull[i & 1]), (i >> 1) & 1, err);
-  } else if (warp == 9) {  // ---- products
+  } else if (warp == kTcMmaWarp) {  // ---- products
     int stage = 0, pass_no = 0;
-    uint32_t phase = 0, uses[2] = {0, 0};
+    uint32_t phase = 0;
+    uint32_t units0 = 0, units1 = 0;  // that each warpgroup has been given
     bool ok = true;
     while (ok && cu.next(p, &pc)) {
       for (int pass = 0; ok && pass < passes; ++pass, ++pass_no) {
         const int qb = pass_no & 1;
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&bar.qfull[qb]), (pass_no >> 1) & 1, err, limit));
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&bar.qfull[qb]), (pass_no >> 1) & 1, err, limit));
         const uint32_t qbase = smem_addr(smem) + qb * qbytes;
         for (int i = 0; ok && i < pc.tiles; ++i) {
-          const int w = i & 1;
-          for (int col = 0; col < p.cols; col += kTcPart) {
-            // Part n of warpgroup w takes its buffer n & 1 for the (n / 2)th time.
-            const int b = 2 * w + (uses[w] & 1);
-            if (uses[w] >= 2) ok = mbar_wait(smem_addr(&bar.sempty[b]), ((uses[w] >> 1) - 1) & 1, err, limit);
-            if (col == 0) ok = ok && mbar_wait(smem_addr(&bar.kfull[stage]), phase, err, limit);
+          uint32_t& n = (i & 1) != 0 ? units1 : units0;
+          for (int col = 0; col < p.cols; col += kTcPart, ++n) {
+            const int room = 2 * (i & 1) + (n & 1);
+            if (n >= 2) ok = wait(smem_addr(&bar.sempty[room]), ((n >> 1) - 1) & 1, err, limit);
+            if (col == 0) ok = ok && wait(smem_addr(&bar.kfull[stage]), phase, err, limit);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc::tc_fence_after();
@@ -371,10 +404,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             for (int ks = 0; ks < 8; ++ks) {
               const uint64_t ad = tc::smem_desc_sw128(kbase + (ks >> 2) * kGroupHalfBytes + (ks & 3) * 32, 16, kGroupBytes);
               const uint64_t bd = tc::smem_desc_sw128(qpart + (ks >> 2) * (p.cols * 128) + (ks & 3) * 32, 16, 1024);
-              tc::tc_mma_elect(tmem + b * kTcPart, ad, bd, idesc, ks > 0);
+              tc::tc_mma_elect(tmem + room * kTcPart, ad, bd, idesc, ks > 0);
             }
-            tc::tc_commit_elect(smem_addr(&bar.sfull[b]));
-            ++uses[w];
+            tc::tc_commit_elect(smem_addr(&bar.sfull[room]));
           }
           if (!ok) break;
           tc::tc_commit_elect(smem_addr(&bar.kempty[stage]));
@@ -392,72 +424,79 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const int wg = warp >> 2, tid = threadIdx.x & 127;
     const uint32_t my_tmem = tmem + 2 * wg * kTcPart + (static_cast<uint32_t>(warp & 3) << 21);
     int pass_no = 0;
-    uint32_t uses = 0;
+    uint32_t units = 0;
     bool ok = true;
-    // (After a wait that ran out the warp still comes to every pass's barrier.)
-    while (cu.next(p, &pc)) {
-      for (int pass = 0; pass < passes; ++pass, ++pass_no) {
-        const int h = pass / p.blocks, rb = pass % p.blocks;
-        const int n0 = rb * p.nodes_per_block, rows = min(p.nodes_per_block, p.w.Nq - n0) * G;
-        float* z = s_z + (pass_no & 1) * kTcMaxRows;
-        if (static_cast<int>(threadIdx.x) < rows) {
-          const int r = threadIdx.x;
-          z[r] = neg_log2_sum(__ldg(p.w.lse + (static_cast<size_t>(pc.c) * p.w.Nq + n0 + r / G) * p.w.hq + h * G + r % G));
-        }
-        // (both warpgroups have left the pass before the last, which used these sums, at the last pass's barrier)
-        named_barrier_sync(1, 256);
-        for (int i = wg; ok && i < pc.tiles; i += 2) {
-          const int j = (pc.tile + i) * kTcKeys + tid;
-          const size_t at = static_cast<size_t>(pc.c) * p.w.weights_len + j;
-          const bool live = j < pc.len && page_id(p.w.v, pc.c, j / p.w.v.P) >= 0;
-          float before = 0.f;
-          if (live) {
-            if (pass > 0) before = p.w.weights_out[at];
-            else if (p.w.weights != nullptr) before = p.w.decay * p.w.weights[at];
-          }
+    while (ok && cu.next(p, &pc)) {
+      float acc[kTcPiece / kTcGroups];
+      for (int x = 0; x < kTcPiece / kTcGroups; ++x) acc[x] = 0.f;
+      for (int pass = 0; ok && pass < passes; ++pass, ++pass_no) {
+        const int rb = pass % p.blocks, rows = min(p.nodes_per_block, p.w.Nq - rb * p.nodes_per_block) * G;
+        const float* z0 = s_z + (pass_no & 1) * kTcMaxRows;
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&bar.zfull[pass_no & 1]), (pass_no >> 1) & 1, err, limit));
+        for (int i = wg; ok && i < pc.tiles; i += kTcGroups) {
           float2 sum[2] = {};
-          for (int col = 0; col < p.cols; col += kTcPart, ++uses) {
-            const int b = uses & 1, here = min(kTcPart, rows - col);
-            ok = mbar_wait(smem_addr(&bar.sfull[2 * wg + b]), (uses >> 1) & 1, err, limit);
+          for (int col = 0; col < p.cols; col += kTcPart, ++units) {
+            const int room = units & 1, here = min(kTcPart, rows - col), whole = here >> 5;
+            ok = wait(smem_addr(&bar.sfull[2 * wg + room]), (units >> 1) & 1, err, limit);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc::tc_fence_after();
-            const uint32_t at_tmem = my_tmem + b * kTcPart;
-            const float* zc = z + col;
-            const int whole = here / 32;
+            const uint32_t at = my_tmem + room * kTcPart;
+            const float* z = z0 + col;
             uint32_t v[32], v2[32];
-            if (whole > 0) tc::tmem_ld32(at_tmem, v);
+            if (whole > 0) tc::tmem_ld32(at, v);
             for (int cc = 0; cc < whole; cc += 2) {
               wait_ld_of(v);
-              if (cc + 1 < whole) tc::tmem_ld32(at_tmem + 32 * (cc + 1), v2);
-              add_columns(v, zc + 32 * cc, p.w.qscale, sum);
+              if (cc + 1 < whole) tc::tmem_ld32(at + 32 * (cc + 1), v2);
+              add_columns(v, z + 32 * cc, p.w.qscale, sum);
               if (cc + 1 < whole) {
                 wait_ld_of(v2);
-                if (cc + 2 < whole) tc::tmem_ld32(at_tmem + 32 * (cc + 2), v);
-                add_columns(v2, zc + 32 * (cc + 1), p.w.qscale, sum);
+                if (cc + 2 < whole) tc::tmem_ld32(at + 32 * (cc + 2), v);
+                add_columns(v2, z + 32 * (cc + 1), p.w.qscale, sum);
               }
             }
-            for (int x = whole * 32; x < here; x += 4) {
+            for (int x = max(whole, 0) * 32; x < here; x += 4) {
               uint32_t u[4];
-              tc::tmem_ld4(at_tmem + x, u);
+              tc::tmem_ld4(at + x, u);
               asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3])::"memory");
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (x + e < here) sum[0].x += ex2(fmaf(__uint_as_float(u[e]), p.w.qscale, zc[x + e]));
+                if (x + e < here) sum[e & 1].x += ex2(fmaf(__uint_as_float(u[e]), p.w.qscale, z[x + e]));
             }
             tc::tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&bar.sempty[2 * wg + b]));
+            if (lane == 0) mbar_arrive(smem_addr(&bar.sempty[2 * wg + room]));
           }
-          if (!ok) break;
-          if (live) p.w.weights_out[at] = before + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
+          acc[i / kTcGroups] += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&bar.zempty[pass_no & 1]));
+      }
+      // What the keys had, and their pages (those passed over are left as they are): eight tiles' loads at a time.
+      for (int i0 = wg; i0 < pc.tiles; i0 += 8 * kTcGroups) {
+        int page[8];
+        float before[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const int i = i0 + x * kTcGroups, j = (pc.tile + i) * kTcKeys + tid;
+          const bool live = i < pc.tiles && j < pc.len;
+          page[x] = !live                          ? -1
+                    : p.w.v.page_table == nullptr ? 0
+                                                  : __ldg(p.w.v.page_table + static_cast<size_t>(pc.c) * p.w.v.max_pages + j / p.w.v.P);
+          before[x] = live && p.w.weights != nullptr ? p.w.weights[static_cast<size_t>(pc.c) * p.w.weights_len + j] : 0.f;
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const int j = (pc.tile + i0 + x * kTcGroups) * kTcKeys + tid;
+          if (static_cast<unsigned>(page[x]) < static_cast<unsigned>(p.w.v.num_pages))
+            p.w.weights_out[static_cast<size_t>(pc.c) * p.w.weights_len + j] = fmaf(p.w.decay, before[x], acc[i0 / kTcGroups + x]);
         }
       }
     }
   }
   tc::tc_fence_before();
   __syncthreads();
-  if (warp == 9) tc::tmem_dealloc(tmem, kTcTmemCols);
+  if (warp == kTcMmaWarp) tc::tmem_dealloc(tmem, kTcTmemCols);
 }
 
 template <int NT>
@@ -531,8 +570,11 @@ extern "C" kvshot_status kvshot_key_weights(const kvshot_attn_desc* d, const voi
   const int most = std::min(p.v.len_bound, weights_len), rows = p.G * p.Nq;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if (rows > kDirectRows) {
-    e = launch_tc(p, q, target_k, static_cast<int64_t>((most + kTcKeys - 1) / kTcKeys) * p.v.C, s);
+  // 9 to 16 rows: two n-tiles of registers a key cost the direct kernel its occupancy (16 x 32K tokens, 16 rows: 221 us, here
+  // 168), which does not matter before the SMs have a tile each (8K tokens: 14.5 us, here 18.6).
+  const int64_t tc_tiles = static_cast<int64_t>((most + kTcKeys - 1) / kTcKeys) * p.v.C;
+  if (rows > kDirectRows || (rows > 8 && tc_tiles > sm_count())) {
+    e = launch_tc(p, q, target_k, tc_tiles, s);
   } else {
     const int tiles = std::max(1, (most + kDirectKeys - 1) / kDirectKeys);  // (lengths are looked at even without room)
     int S = 1;  // CTAs that share the heads: until the SMs have two each

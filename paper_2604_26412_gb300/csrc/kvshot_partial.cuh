@@ -94,6 +94,18 @@ __device__ __forceinline__ void mma_piece(float (&d)[4], const uint4& a, const u
   dev::mma_bf16_16816(d, hi, b.z, b.w);
 }
 
+// 32 bytes of a row by one load: half the requests of 16-byte loads for the same bytes.
+struct Row32 {
+  uint4 lo, hi;
+};
+__device__ __forceinline__ Row32 load32(const uint4* p) {
+  Row32 r;
+  asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r.lo.x), "=r"(r.lo.y), "=r"(r.lo.z), "=r"(r.lo.w), "=r"(r.hi.x), "=r"(r.hi.y), "=r"(r.hi.z), "=r"(r.hi.w)
+               : "l"(p));
+  return r;
+}
+
 // Rows of q staged in shared memory, 16 pieces and 64 bytes of padding each: 8 rows' pieces 4 j .. 4 j + 3 are in different
 // banks.
 constexpr int kQRowBytes = 256 + 64;

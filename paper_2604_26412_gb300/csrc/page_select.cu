@@ -83,76 +83,110 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p)
   extern __shared__ __align__(16) uint8_t s_q[];  // up to kScoreRows rows
   const int c = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t = lane & 3;
-  const int L = clamped_len(p.v, c);
-  const int pages = (L + p.v.P - 1) / p.v.P;
-  const int cta0 = blockIdx.x * kScoreWarps * 16;
-  if (cta0 >= pages) return;
-  const int page[2] = {cta0 + warp * 16 + g, cta0 + warp * 16 + g + 8};
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  uint4 b[2][8];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int id = page[i] < pages ? page_id(p.v, c, page[i]) : -1;
-    const uint4* src = p.bounds + (static_cast<size_t>(max(id, 0)) * p.v.hkv + h) * 32 + t;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) b[i][j] = id >= 0 ? __ldg(src + 4 * j) : zero;
-  }
-  const int gp = 1 << p.log_gp, rows = p.Nq << p.log_gp;
-  const int stride = p.v.max_pages * p.v.hkv;
-  float best[2] = {-INFINITY, -INFINITY};  // of a node whose columns are several tiles (gp > 8)
-  for (int r0 = 0; r0 < rows; r0 += kScoreRows) {
-    __syncthreads();
-    const int here = min(kScoreRows, (rows - r0 + 7) / 8 * 8);
+  const int gp = 1 << p.log_gp, rows = p.Nq << p.log_gp, stride = p.v.max_pages * p.v.hkv;
+  auto stage = [&](int r0) {
+    const int here = min(kScoreRows, (rows - r0 + 15) / 16 * 16);
     for (int i = threadIdx.x; i < here * 16; i += kScoreWarps * 32) {
       const int r = r0 + i / 16, n = r >> p.log_gp, j = r & (gp - 1);
       const bool live = n < p.Nq && j < p.G;
       const uint4 x = live ? __ldg(p.q + ((static_cast<size_t>(c) * p.Nq + n) * p.hq + h * p.G + j) * 16 + i % 16) : zero;
       *reinterpret_cast<uint4*>(s_q + (i / 16) * kQRowBytes + (i % 16) * 16) = x;
     }
-    __syncthreads();
-    for (int tile = 0; tile < here / 8; ++tile) {
-      float d[4] = {0.f, 0.f, 0.f, 0.f};
-      const uint8_t* row = s_q + (tile * 8 + g) * kQRowBytes + t * 16;
+    return here;
+  };
+  // (Table entries are looked up beside the length: their number is the table's, not the length's.)
+  const int32_t* table = p.v.page_table + static_cast<size_t>(c) * p.v.max_pages;
+  int id[2];
+  auto look_up = [&](int cta0) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint4 x = *reinterpret_cast<const uint4*>(row + j * 64);
-        mma_piece(d, b[0][j], b[1][j], make_uint4(min2(x.x, 0), min2(x.y, 0), min2(x.z, 0), min2(x.w, 0)));
-        mma_piece(d, b[0][j + 4], b[1][j + 4], make_uint4(max2(x.x, 0), max2(x.y, 0), max2(x.z, 0), max2(x.w, 0)));
+    for (int i = 0; i < 2; ++i) {
+      const int page = cta0 + warp * 16 + g + 8 * i;
+      id[i] = page < p.v.max_pages ? __ldg(table + page) : 0;
+    }
+  };
+  constexpr int kPages = kScoreWarps * 16;
+  int cta0 = blockIdx.x * kPages;
+  look_up(cta0);
+  const int L = clamped_len(p.v, c);
+  const int pages = (L + p.v.P - 1) / p.v.P;
+  if (cta0 >= pages) return;
+  bool staged = false;
+  for (; cta0 < pages; cta0 += gridDim.x * kPages) {
+    const int page[2] = {cta0 + warp * 16 + g, cta0 + warp * 16 + g + 8};
+    uint4 b[2][8];
+    bool live[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      live[i] = page[i] < pages && static_cast<unsigned>(id[i]) < static_cast<unsigned>(p.v.num_pages);
+      if (page[i] < pages && !live[i]) set_error(p.v.err, KVSHOT_ERR_DEVICE_BOUNDS);
+      const uint4* src = p.bounds + (static_cast<size_t>(live[i] ? id[i] : 0) * p.v.hkv + h) * 32 + t;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) b[i][j] = live[i] ? __ldg(src + 4 * j) : zero;
+    }
+    look_up(cta0 + gridDim.x * kPages);
+    float best[2] = {-INFINITY, -INFINITY};  // of a node whose columns are several tiles (gp > 8)
+    for (int r0 = 0; r0 < rows; r0 += kScoreRows) {
+      int here = min(kScoreRows, (rows - r0 + 15) / 16 * 16);
+      if (!staged || rows > kScoreRows) {
+        __syncthreads();
+        here = stage(r0);
+        __syncthreads();
+        staged = true;
       }
-      // d: page g, columns 2 t and 2 t + 1; page g + 8, the same columns.
-      const int col = r0 + tile * 8 + 2 * t;
-      auto put = [&](int i, int n, float s) {
-        if (n < p.Nq && page[i] < pages)
-          p.scores[(static_cast<size_t>(c) * p.Nq + n) * stride + static_cast<size_t>(h) * p.v.max_pages + page[i]] =
-              s * p.scale;
-      };
-      if (gp == 1) {
+      for (int pair = 0; pair < here / 16; ++pair) {
+        // Two tiles of 8 columns, the products with the least and the greatest keys apart: four chains.
+        float d[2][4] = {}, d2[2][4] = {};
+        const uint8_t* row = s_q + (pair * 16 + g) * kQRowBytes + t * 16;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) put(i >> 1, col + (i & 1), d[i]);
-        continue;
-      }
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (((col + (i & 1)) & (gp - 1)) >= p.G) d[i] = -INFINITY;
-      float m[2] = {fmaxf(d[0], d[1]), fmaxf(d[2], d[3])};
+          for (int x = 0; x < 2; ++x) {
+            const uint4 q = *reinterpret_cast<const uint4*>(row + x * 8 * kQRowBytes + j * 64);
+            mma_piece(d[x], b[0][j], b[1][j], make_uint4(min2(q.x, 0), min2(q.y, 0), min2(q.z, 0), min2(q.w, 0)));
+            mma_piece(d2[x], b[0][j + 4], b[1][j + 4], make_uint4(max2(q.x, 0), max2(q.y, 0), max2(q.z, 0), max2(q.w, 0)));
+          }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (gp > 2) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 1));
-        if (gp > 4) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 2));
-      }
-      if (gp > 8) {
-        const bool last = ((col & (gp - 1)) >> 3) == (gp >> 3) - 1;
+        for (int x = 0; x < 2; ++x) {
+          // d: page g, columns 2 t and 2 t + 1; page g + 8, the same columns.
+          const int col = r0 + pair * 16 + x * 8 + 2 * t;
+          auto put = [&](int i, int n, float s) {
+            if (n < p.Nq && live[i])
+              p.scores[(static_cast<size_t>(c) * p.Nq + n) * stride + static_cast<size_t>(h) * p.v.max_pages + page[i]] =
+                  s * p.scale;
+          };
+          float s[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          best[i] = fmaxf(best[i], m[i]);
-          m[i] = best[i];
-          if (last) best[i] = -INFINITY;
+          for (int i = 0; i < 4; ++i) s[i] = d[x][i] + d2[x][i];
+          if (gp == 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put(i >> 1, col + (i & 1), s[i]);
+            continue;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (((col + (i & 1)) & (gp - 1)) >= p.G) s[i] = -INFINITY;
+          float m[2] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3])};
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (gp > 2) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 1));
+            if (gp > 4) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 2));
+          }
+          if (gp > 8) {
+            const bool last = ((col & (gp - 1)) >> 3) == (gp >> 3) - 1;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              best[i] = fmaxf(best[i], m[i]);
+              m[i] = best[i];
+              if (last) best[i] = -INFINITY;
+            }
+            if (!last) continue;
+          }
+          if ((2 * t & (gp - 1)) == 0)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) put(i, col >> p.log_gp, m[i]);
         }
-        if (!last) continue;
       }
-      if ((2 * t & (gp - 1)) == 0)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) put(i, col >> p.log_gp, m[i]);
     }
   }
 }
@@ -510,8 +544,12 @@ extern "C" kvshot_status kvshot_page_scores(const kvshot_attn_desc* d, const voi
   p.scale = score_scale(d);
   const int pages = (p.v.len_bound + p.v.P - 1) / p.v.P, per_cta = kScoreWarps * 16;
   if (pages == 0) return KVSHOT_OK;
-  const size_t smem = static_cast<size_t>(std::min(kScoreRows, ((p.Nq << p.log_gp) + 7) / 8 * 8)) * kQRowBytes;
-  const cudaError_t e = launch_maybe_pdl(scores_kernel, dim3((pages + per_cta - 1) / per_cta, p.v.hkv, p.v.C),
+  const size_t smem = static_cast<size_t>(std::min(kScoreRows, ((p.Nq << p.log_gp) + 15) / 16 * 16)) * kQRowBytes;
+  // CTAs take several chunks of pages, and q once, where there are more than four waves of them.
+  const int64_t heads = static_cast<int64_t>(p.v.hkv) * p.v.C;
+  const int chunks = (pages + per_cta - 1) / per_cta;
+  const int x = static_cast<int>(std::min<int64_t>(chunks, std::max<int64_t>(1, 16 * sm_count() / heads)));
+  const cudaError_t e = launch_maybe_pdl(scores_kernel, dim3(x, p.v.hkv, p.v.C),
                                          dim3(kScoreWarps * 32), smem, false, reinterpret_cast<cudaStream_t>(stream), p);
   return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
 }

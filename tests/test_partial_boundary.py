@@ -102,6 +102,9 @@ def test_pointers(call, names, wide):
         assert call({name: A + 2}) == ALIGN
     for name in wide:
         assert call({name: A + 8}) == ALIGN
+    if call is sparse:
+        for name in ("k", "v", "dk", "dv"):
+            assert call({name: A + 16}) == ALIGN
     if call is bounds:
         assert call({"fr": A + 2}) == ALIGN
     if call is weights:
