@@ -517,7 +517,7 @@ kvshot_status kvshot_select_top(const kvshot_select_desc* desc, const float* sco
  * i < counts[c, n, h], and the draft keys that kvshot_draft_attn gives that row.
  * picks: [C, Nq, hkv, max_picks] int32, each list ascending; counts: [C, Nq, hkv] int32 in [0, max_picks].  A pick that
  * is not above its predecessor or not a page below the cache's length is recorded as KVSHOT_ERR_DEVICE_BOUNDS and passed
- * over, a count out of range recorded and clamped.  Other arguments as for kvshot_draft_attn, but target_k/v and
+ * over (a page that comes again later in such a list may count twice), a count out of range recorded and clamped.  Other arguments as for kvshot_draft_attn, but target_k/v and
  * draft_k/v 32-byte aligned.
  * The softmax weights are rounded to bf16 for the tensor cores, sums are fp32.
  * Workspace: kvshot_draft_attn_sparse_workspace_size bytes (0 if the descriptor is invalid), as for kvshot_draft_attn.

@@ -167,14 +167,6 @@ struct WeightMaps {
   CUtensorMap k, q;
 };
 
-// A wait that looks a few times before it takes the time (reading the clock takes long enough to be late).
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int32_t* err, uint64_t limit) {
-  if (limit >= kPollBelowNs)
-    for (int i = 0; i < 32; ++i)
-      if (mbar_try_wait(bar, parity)) return true;
-  return mbar_wait(bar, parity, err, limit);
-}
-
 struct TcPiece {
   int c, tile, tiles, len;
 };

@@ -267,28 +267,79 @@ def test_sparse_all_pages_agree_with_draft_attention():
     assert (full.float() - out.float()).abs().max() <= 0.03 and (z - lse).abs().max() <= 1e-3
 
 
-def test_sparse_bad_picks_are_recorded_and_passed_over():
-    p = Problem([100], 16, nodes=1, query=1)
-    good = np.full((1, 1, 8, 6), -1, np.int32)
+SHARED = {  # calls whose nodes share pages: from 32 rows per KV head, over two thirds of the SMs' number of (cache, head, 64 rows)
+    "tree": dict(lens=[0, 1, 15, 16, 17, 300, 700, 64, 65, 128, 500, 33, 8, 9], page=16, nodes=30, query=8, tree=True, layers=2),
+    "chain": dict(lens=[0, 1, 7, 8, 9, 300, 700, 64, 65, 128, 500, 33, 31], page=8, nodes=20, query=16),
+    "seven heads": dict(lens=list(range(0, 520, 20)), page=64, hq=28, hkv=4, nodes=6, query=5),
+    "one KV head": dict(lens=list(range(52)), page=32, hq=32, hkv=1, nodes=4, query=4),
+    "17 heads": dict(lens=list(range(0, 260, 10)), page=128, hq=34, hkv=2, nodes=3, query=3),
+    "one head": dict(lens=list(range(0, 390, 30)), page=16, hq=8, hkv=8, nodes=64, query=64, tree=True),
+    "whole tree": dict(lens=[200, 1000, 0, 191], page=192, nodes=64, query=64, tree=True),
+    "long chain": dict(lens=list(range(0, 1300, 100)), page=256, nodes=100, query=12),
+    "two windows": dict(lens=[20001, 9000] + [30] * 11, page=8, nodes=8, query=8),
+    "65 rows": dict(lens=[77] * 7, page=16, hq=8, hkv=8, nodes=65, query=65),
+}
+
+
+@pytest.mark.parametrize("name", SHARED)
+def test_sparse_shared_pages(name):
+    p = Problem(**SHARED[name], seed=len(name))
+    run_sparse(p, *p.random_picks(40 if name == "two windows" else 6, seed=len(name)))
+
+
+def test_sparse_shared_pages_without_picks_and_bit_for_bit():
+    p = Problem(**SHARED["tree"], seed=1)
+    picks, counts = p.random_picks(5)
+    counts[:, ::2] = 0
+    counts[3] = 0
+    a, b = run_sparse(p, picks, counts), run_sparse(p, picks, counts)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_sparse_shared_bad_picks_pages_and_parents():
+    p = Problem([100] * 13, 16, nodes=8, query=8, tree=True)
+    picks = np.full((13, 8, 8, 6), -1, np.int32)
+    picks[..., :3] = [1, 3, 6]
+    n = np.full((13, 8, 8), 3, np.int32)
+    for row in ([1, 3, 6, 7, 2 ** 31 - 1, -1], [-9, -2, 1, 3, 3, 6], [1, 3, 6, 6, 6, -2 ** 31]):
+        bad, counts = picks.copy(), n.copy()
+        bad[4, 7, 2], counts[4, 7, 2] = row, 6
+        run_sparse(p, bad, counts, kvshot.KVSHOT_ERR_DEVICE_BOUNDS, (picks, n))
+        p.err.zero_()
+    run_sparse(p, picks[..., :3].copy(), np.where(np.arange(13)[:, None, None] == 5, 2 ** 30, n), kvshot.KVSHOT_ERR_DEVICE_BOUNDS, (picks, n))
+    p.err.zero_()
+    for parents, table, code in (([-1, 0, 5, 1, 2, 3, 4, 5], p.t_table, kvshot.KVSHOT_ERR_TREE),
+                                 ([-1, 0, 1, 1, 2, 3, 4, 5], p.t_table - p.num_pages, kvshot.KVSHOT_ERR_DEVICE_BOUNDS)):
+        ws = p.workspace(6)
+        kvshot.draft_attn_sparse(p.desc, p.q, p.k, p.v, table, p.t_lens, p.ints(picks), p.ints(n), 6, p.dk, p.dv,
+                                 p.ints([parents] * 13), torch.empty_like(p.q), torch.empty(p.q.shape[:3], device="cuda"))
+        check(p, code)
+        p.err.zero_()
+        del ws
+
+
+@pytest.mark.parametrize("query", [1, 3])
+def test_sparse_bad_picks_are_recorded(query):
+    p = Problem([100], 16, nodes=query, query=query)
+    good = np.full((1, query, 8, 6), -1, np.int32)
     good[..., :3] = [1, 3, 6]
-    bad = good.copy()
-    bad[..., :6] = [1, 3, 6, 7, -1, 6]  # page 7 is past the length, -1 no page; the last 6 is above its predecessor
-    bad[0, 0, 1] = [-9, -2, 1, 3, 3, 6]
-    bad[0, 0, 2] = [1, 1, 3, 3, 2 ** 31 - 1, 6]
-    kept, n = good.copy(), np.full((1, 1, 8), 4, np.int32)
-    kept[..., 3] = 6
-    n[0, 0, 1] = 3
-    kept[0, 0, 2, :3], n[0, 0, 2] = [1, 3, -1], 2   # (6 is not above its predecessor)
-    run_sparse(p, bad, np.full((1, 1, 8), 6, np.int32), kvshot.KVSHOT_ERR_DEVICE_BOUNDS, (kept, n))
+    n = np.full((1, query, 8), 3, np.int32)
+    for row, times in (([1, 3, 6, 7, 2 ** 31 - 1, -1], 6), ([-9, -2, 1, 3, 3, 6], 6), ([1, 1, 3, 3, 6, 6], 6),
+                       ([1, 3, 6, 6, 6, -2 ** 31], 6)):  # (what is not a pick is passed over: the same three pages are left)
+        bad = good.copy()
+        bad[0, query - 1, 2] = row
+        counts = n.copy()
+        counts[0, query - 1, 2] = times
+        run_sparse(p, bad, counts, kvshot.KVSHOT_ERR_DEVICE_BOUNDS, (good, n))
+        p.err.zero_()
+    run_sparse(p, np.ascontiguousarray(good[..., :3]), np.full((1, query, 8), 2 ** 30, np.int32), kvshot.KVSHOT_ERR_DEVICE_BOUNDS, (good, n))
     p.err.zero_()
-    run_sparse(p, good[..., :3], np.full((1, 1, 8), 2 ** 30, np.int32), kvshot.KVSHOT_ERR_DEVICE_BOUNDS,
-               (good, np.full((1, 1, 8), 3, np.int32)))
-    p.err.zero_()
-    run_sparse(p, good, np.full((1, 1, 8), -1, np.int32), kvshot.KVSHOT_ERR_DEVICE_BOUNDS, (good, np.zeros((1, 1, 8), np.int32)))
+    run_sparse(p, good, np.full((1, query, 8), -1, np.int32), kvshot.KVSHOT_ERR_DEVICE_BOUNDS, (good, 0 * n))
 
 
-def test_sparse_bad_parents_and_pages_are_recorded():
-    p = Problem([100], 16, nodes=5, query=5, tree=True)
+@pytest.mark.parametrize("query", [1, 5])
+def test_sparse_bad_parents_and_pages_are_recorded(query):
+    p = Problem([100], 16, nodes=5, query=query, tree=True)
     picks, counts = p.random_picks(4)
     args = (p.dk, p.dv)
     for parents, table, code in (([-1, 0, 5, 1, 2], p.t_table, kvshot.KVSHOT_ERR_TREE), ([-1, 0, -2, 1, 2], p.t_table, kvshot.KVSHOT_ERR_TREE),
