@@ -214,13 +214,19 @@ struct SelectRow {
 };
 __device__ __forceinline__ SelectRow select_row(const SelectParams& p, int row) {
   const int len = p.seq_lens[row / p.rows_per_len];
-  int64_t entries = len > 0 ? (static_cast<int64_t>(len) + p.tokens_per_entry - 1) / p.tokens_per_entry : 0;
-  if (len < 0 || entries > p.row_len) {
+  int n = len > 0 ? (len - 1) / p.tokens_per_entry + 1 : 0;
+  if (len < 0 || n > p.row_len) {
     set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
-    entries = min(entries, static_cast<int64_t>(p.row_len));
+    n = min(n, p.row_len);
   }
-  const int n = static_cast<int>(entries);
   return SelectRow{n, min(n, p.keep)};
+}
+
+// One more in a bin, if `open`.  (Without a branch: a row has a dozen of these a thread and round.)
+__device__ __forceinline__ void count_in(int* bin, bool open) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %1, 0;\n\t@p red.shared.add.s32 [%0], 1;\n\t}" ::"r"(smem_addr(bin)),
+               "r"(static_cast<int>(open))
+               : "memory");
 }
 
 // The bin in which the need-th greatest entry is, from the bins' counts: each thread takes consecutive bins, the top ones
@@ -268,9 +274,12 @@ __device__ __forceinline__ int remote_int(const int* at, uint32_t rank) {
 }
 
 // A row is read once: a cluster of CTAs (one, for rows of up to kThreads x kSelectKeys entries) holds its keys in registers,
-// every warp a run of consecutive entries.  Each CTA counts the digits of its own keys and adds what it counted to the
-// counts of all CTAs, which then each find the digit for themselves.  What bounds it: the latencies of a load, two to four
-// rounds of counts and a scan, and the shared atomics of digits that agree.
+// every thread a run of consecutive entries, so that the picks' places follow from one scan of the threads' numbers.  Each
+// CTA counts the digits of its own keys that are still in question and adds what it counted to the counts of all CTAs, which
+// then each find the digit for themselves.  What bounds it: the latencies of a load, two to four rounds of counts and a
+// scan, and the instructions for keys that are no longer in question.  4096 of 32K entries in 16 rows: 16.5 us (89 with one
+// CTA that reads the scores for every digit).  1536 rows of 1250 to 2048 entries: 18.6 us; a warp to a row with its keys in
+// registers, bit by bit, took 25.8, tables kept four times 22.5, first digits of half octaves 28.9.
 constexpr int kSelectKeys = 16;
 constexpr int kMaxSelectCluster = 8;
 
@@ -279,7 +288,7 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectParams p) {
   constexpr int kBins = 1 << kBits, kWarps = kThreads / 32, kPasses = (32 + kBits - 1) / kBits;
   __shared__ int s_hist[2][kBins];
   __shared__ int s_total[kCluster ? kPasses : 1][kCluster ? kBins : 1];  // over the cluster
-  __shared__ int s_warp[2][kWarps], s_sum[2];
+  __shared__ int s_warp[kWarps], s_sum;
   __shared__ int s_bin, s_above;
   const int S = kCluster ? static_cast<int>(cluster_size()) : 1, rank = kCluster ? blockIdx.x % S : 0;
   const int row = blockIdx.x / S, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -292,35 +301,37 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectParams p) {
     for (int i = rank * kThreads + tid; i < n; i += S * kThreads) picks[i] = i;
     return;  // (the whole cluster)
   }
-  // This CTA's entries [e0, e1), warp w's from e0 + 32 w rounds on.
-  const int chunk = ((n + S - 1) / S + 31) / 32 * 32, e0 = min(n, rank * chunk), e1 = min(n, e0 + chunk);
-  const int rounds = (chunk + kThreads - 1) / kThreads, w0 = e0 + warp * rounds * 32 + lane;
-  const float* s = p.scores + static_cast<size_t>(row) * p.row_len;
-  const int a = p.first, b = n - p.last;  // [a, b) compete for `need` places
+  // This CTA's entries [e0, e1); this thread's: `rounds` from `first` on.
+  const int chunk = (n + S - 1) / S, e0 = min(n, rank * chunk), e1 = min(n, e0 + chunk);
+  const int rounds = (chunk + kThreads - 1) / kThreads, first = e0 + tid * rounds, mine = min(max(e1 - first, 0), rounds);
+  const float* s = p.scores + static_cast<size_t>(row) * p.row_len + first;
+  const int a = p.first - first, b = n - p.last - first;  // entries [a, b) of this thread compete for `need` places
   int need = p.keep - p.first - p.last;
   float f[kSelectKeys];
 #pragma unroll
-  for (int k = 0; k < kSelectKeys; ++k) f[k] = k < rounds && w0 + 32 * k < e1 ? __ldg(s + w0 + 32 * k) : 0.f;
+  for (int k = 0; k < kSelectKeys; ++k) f[k] = k < mine ? __ldg(s + k) : 0.f;
   for (int i = tid; i < 2 * kBins; i += kThreads) s_hist[i / kBins][i % kBins] = 0;
   if (kCluster)
     for (int i = tid; i < kPasses * kBins; i += kThreads) s_total[kCluster ? i / kBins : 0][kCluster ? i % kBins : 0] = 0;
   if (kCluster) cluster_sync_all();
   else __syncthreads();
-  uint32_t key[kSelectKeys], inside = 0;  // bit k: entry k competes
+  uint32_t key[kSelectKeys], open = 0, over = 0;  // bit k: entry k is still in question; it is picked
 #pragma unroll
   for (int k = 0; k < kSelectKeys; ++k) {
-    const int i = w0 + 32 * k;
+    if (k >= rounds) break;
     key[k] = order_key(f[k]);
-    inside |= static_cast<uint32_t>(k < rounds && i < e1 && i >= a && i < b) << k;
+    const uint32_t bit = k < mine ? 1u << k : 0u;
+    if (k >= a && k < b) open |= bit;
+    else over |= bit;
   }
-  uint32_t prefix = 0, mask = 0;
-  if (need == 0) prefix = mask = 0xffffffffu;  // nothing is above a NaN, and of what is equal none is taken
-  for (int pass = 0, shift = 32 - kBits; need > 0; ++pass, shift = max(0, shift - kBits)) {
+  for (int pass = 0, shift = 32 - kBits; need > 0; ++pass) {
     int* hist = s_hist[pass & 1];
-    const uint32_t digit_mask = (mask == 0 ? 0xffffffffu : ~mask) >> shift;
+    const uint32_t digits = pass == 0 ? kBins - 1 : (1u << min(kBits, 32 - pass * kBits)) - 1;
 #pragma unroll
-    for (int k = 0; k < kSelectKeys; ++k)
-      if ((inside >> k & 1u) != 0 && (key[k] & mask) == prefix) atomicAdd(&hist[(key[k] >> shift) & digit_mask], 1);
+    for (int k = 0; k < kSelectKeys; ++k) {
+      if (k >= rounds) break;
+      count_in(&hist[(key[k] >> shift) & digits], (open >> k & 1u) != 0);
+    }
     __syncthreads();
     if (kCluster) {
       int* total = s_total[kCluster ? pass : 0];
@@ -335,62 +346,63 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectParams p) {
     } else {
       for (int i = tid; i < kBins; i += kThreads) s_hist[(pass + 1) & 1][i] = 0;
     }
-    find_bin<kThreads, kBins>(hist, need, s_warp[0], [&](int bin, int above) {
+    find_bin<kThreads, kBins>(hist, need, s_warp, [&](int bin, int above) {
       s_bin = bin;
       s_above = above;
     });
     __syncthreads();
-    const int bin = s_bin;
-    prefix |= static_cast<uint32_t>(bin) << shift;
-    mask |= digit_mask << shift;
+    const uint32_t bin = s_bin;
+#pragma unroll
+    for (int k = 0; k < kSelectKeys; ++k) {
+      if (k >= rounds) break;
+      if ((open >> k & 1u) == 0) continue;
+      const uint32_t digit = (key[k] >> shift) & digits;
+      if (digit > bin) over |= 1u << k;
+      if (digit != bin) open &= ~(1u << k);
+    }
     need -= s_above;
     if (shift == 0 || hist[bin] == need) break;  // (the whole bin is taken)
+    shift = max(0, shift - kBits);
   }
-  // What is above the found prefix, and equal to it; forced entries count as above.
-  uint32_t over = 0, equal = 0;
-  int overs = 0, equals = 0;
+  if (p.keep == p.first + p.last) open = 0;
+  // What is still in question is equal, and the first `need` of it are picked.  Places: numbers picked and equal before.
+  const int overs = __popc(over), equals = __popc(open);
+  int place = overs | equals << 16;  // (each below 2^14 in a CTA)
+  int scan = place;
 #pragma unroll
-  for (int k = 0; k < kSelectKeys; ++k) {
-    const int i = w0 + 32 * k;
-    const bool in = (inside >> k & 1u) != 0, forced = k < rounds && i < e1 && !in;
-    const bool o = forced || (in && (key[k] & mask) > prefix), e = in && (key[k] & mask) == prefix;
-    over |= static_cast<uint32_t>(o) << k;
-    equal |= static_cast<uint32_t>(e) << k;
-    overs += __popc(__ballot_sync(0xffffffffu, o));
-    equals += __popc(__ballot_sync(0xffffffffu, e));
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, scan, o);
+    if (lane >= o) scan += x;
   }
   __syncthreads();
-  if (lane == 0) {
-    s_warp[0][warp] = overs;
-    s_warp[1][warp] = equals;
-  }
+  if (lane == 31) s_warp[warp] = scan;
   __syncthreads();
-  overs = equals = 0;
-  int all_overs = 0, all_equals = 0;
+  place = scan - place;
+  int total = 0;
+#pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    if (w == warp) overs = all_overs, equals = all_equals;
-    all_overs += s_warp[0][w];
-    all_equals += s_warp[1][w];
+    if (w == warp) place += total;
+    total += s_warp[w];
   }
+  int overs_before = place & 0xffff, equals_before = place >> 16;
   if (kCluster) {
-    if (tid == 0) s_sum[0] = all_overs, s_sum[1] = all_equals;
+    if (tid == 0) s_sum = total;
     cluster_sync_all();
     for (int x = 0; x < rank; ++x) {
-      overs += remote_int(&s_sum[0], x);
-      equals += remote_int(&s_sum[1], x);
+      const int t = remote_int(&s_sum, x);
+      overs_before += t & 0xffff;
+      equals_before += t >> 16;
     }
   }
-  const uint32_t below = (1u << lane) - 1;
 #pragma unroll
   for (int k = 0; k < kSelectKeys; ++k) {
-    const bool o = (over >> k & 1u) != 0, e = (equal >> k & 1u) != 0;
-    const uint32_t mo = __ballot_sync(0xffffffffu, o), me = __ballot_sync(0xffffffffu, e);
-    const int before = equals + __popc(me & below);
-    if (o || (e && before < need)) picks[overs + __popc(mo & below) + min(before, need)] = w0 + 32 * k;
-    overs += __popc(mo);
-    equals += __popc(me);
+    if (k >= rounds) break;
+    const bool o = (over >> k & 1u) != 0, e = (open >> k & 1u) != 0;
+    if (o || (e && equals_before < need)) picks[overs_before + min(equals_before, need)] = first + k;
+    overs_before += o;
+    equals_before += e;
   }
-  if (kCluster) cluster_sync_all();  // (another CTA may still read this one's sums)
+  if (kCluster) cluster_sync_all();  // (another CTA may still read this one's sum)
 }
 
 // Rows too long for a cluster's registers: one CTA, which reads the scores again for every digit.
@@ -575,7 +587,7 @@ extern "C" kvshot_status kvshot_select_top(const kvshot_select_desc* d, const fl
     return S;
   };
   cudaError_t e;
-  if (n <= 128 * kSelectKeys) e = launch_select<128, 8, false>(p, rows, 1, st);
+  if (n <= 128 * kSelectKeys) e = launch_select<128, 9, false>(p, rows, 1, st);
   else if (n <= 512 * kSelectKeys && 2 * rows > sm_count()) e = launch_select<512, 11, false>(p, rows, 1, st);
   else if (n <= 512 * kSelectKeys * kMaxSelectCluster) e = launch_select<512, 11, true>(p, rows, cluster(4096), st);
   else if (n <= 1024 * kSelectKeys * kMaxSelectCluster) e = launch_select<1024, 11, true>(p, rows, kMaxSelectCluster, st);
