@@ -460,7 +460,7 @@ kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* desc, const void* q,
  *   kvshot_key_weights   softmax weights that the cached tokens got, accumulated
  *   kvshot_cache_evict   the tokens to keep moved to the front, and the other pages given back
  * The first two, the fourth and the fifth take a kvshot_attn_desc and read of it num_caches, num_seqs, hq, hkv, head_dim,
- * page_size, max_pages_per_seq, num_pages, max_seq_len, n_nodes, n_query, n_max, scale, flags and err_flag as
+ * page_size, max_pages_per_seq, num_pages, max_seq_len, n_nodes, n_query, n_max, scale, flags, err_flag and wait_limit_ns as
  * kvshot_draft_attn does (kvshot_page_bounds no query heads' or nodes' fields).  Caches are bf16 and paged
  * (kvshot_key_weights: or contiguous), q is [C, Nq, hq, 128] bf16, and the q heads of one KV head are at most 32.
  * KVSHOT_TARGET_FP8 and the KVSHOT_FORCE_ flags return KVSHOT_ERR_UNSUPPORTED; KVSHOT_OVERLAP_PREVIOUS has no effect.
@@ -519,7 +519,8 @@ kvshot_status kvshot_select_top(const kvshot_select_desc* desc, const float* sco
  * is not above its predecessor or not a page below the cache's length is recorded as KVSHOT_ERR_DEVICE_BOUNDS and passed
  * over (a page that comes again later in such a list may count twice), a count out of range recorded and clamped.  Other arguments as for kvshot_draft_attn, but target_k/v and
  * draft_k/v 32-byte aligned.
- * The softmax weights are rounded to bf16 for the tensor cores, sums are fp32.
+ * The softmax weights are rounded to bf16 for the tensor cores, sums are fp32.  A NaN or infinity stored in a value that some
+ * row of the KV head sees may reach the cache's other rows of that head.
  * Workspace: kvshot_draft_attn_sparse_workspace_size bytes (0 if the descriptor is invalid), as for kvshot_draft_attn.
  */
 size_t kvshot_draft_attn_sparse_workspace_size(const kvshot_attn_desc* desc, int32_t max_picks);
@@ -546,7 +547,8 @@ kvshot_status kvshot_key_weights(const kvshot_attn_desc* desc, const void* q, co
  *   k, v -> k_out, v_out    [num_pages, hkv, page_size, 128] bf16, in place (k_out = k, v_out = v, page_table_out =
  *                           page_table), or into other pools of num_pages_out pages through page_table_out, a smaller
  *                           copy for instance.  Slots past the last kept token are left as they are.
- *   weights -> weights_out  [C, weights_len] -> [C, weights_len_out] fp32; in place, or not overlapping; both may be NULL
+ *   weights -> weights_out  [C, weights_len] -> [C, weights_len_out] fp32, 0 past the kept tokens' (what a token that comes
+ *                           later starts with); in place, or not overlapping; both may be NULL
  *   seq_lens_out            m_c
  *   free_pages, free_count_out   page_table's pages past the first ceil(m_c / page_size) of cache c's ceil(L_c / page_size),
  *                           put behind the *free_count free ones, cache after cache, ascending: what kvshot_cache_extend

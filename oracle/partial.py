@@ -130,6 +130,7 @@ def cache_evict(k, v, table, lens, kept, counts, weights, k_out, v_out, table_ou
             for src, dst in ((k, k_out), (v, v_out)):
                 dst[table_out[c, i // P], :, i % P] = src[table[c, j // P], :, j % P]
             weights_out[c, i] = weights[c, j]
+        weights_out[c, int(m):] = 0
         for p in range(pages_of(m, P), pages_of(lens[c], P)):
             free[at] = table[c, p]
             at += 1

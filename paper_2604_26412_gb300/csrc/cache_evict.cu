@@ -91,6 +91,9 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(EvictParams p) {
       for (int i = 0; i < 8; ++i)
         if (j[i] >= 0) dst[i0 + i * kMoveThreads + tid] = x[i];
     }
+    __syncthreads();  // (in place, what is behind the kept tokens' weights has been read)
+    if (ck.kept >= 0)
+      for (int i = ck.kept + tid; i < p.weights_len_out; i += kMoveThreads) dst[i] = 0.f;
     return;
   }
   const int head = (y >> 1) * p.P, piece = (kInPlace ? blockIdx.x * kPieces : 0) + tid % kPieces;

@@ -5,7 +5,8 @@ step d (Nq_d new nodes), the new nodes' q/k/v are RoPE'd and appended
 (kvshot_draft_append), then the new nodes attend over [target prefix | draft
 KV so far] (kvshot_draft_attn).  In "whole" mode all N nodes are appended
 once and attend together (whole-tree verification shape).  The target prefix is
-bf16, fp8 or 4 bits; the 4-bit cache grows between steps (kv4.Kv4Cache).
+bf16, fp8 or 4 bits; the 4-bit cache grows between steps (kv4.Kv4Cache).  Over a paged bf16 prefix a step may read the best
+pages of each node alone, and add up the tokens' softmax weights (partial.PageSelection, partial.TokenWeights).
 
 Only device memory is handled here (torch allocations); all arithmetic runs
 in libkvshot's kernels, but for one sum: over a 4-bit cache a step first adds
@@ -20,26 +21,38 @@ import torch
 from . import kvshot
 from . import workloads as wl
 from .kv4 import Kv4Cache
+from .partial import PageSelection, TokenWeights
 
 
 class DraftStep:
     def __init__(self, inp: wl.Inputs, mode: str = "per_depth", flags: int = 0, num_ctas: int = 0,
                  scale: float = 0.0, err_flag: bool = True, target_fp8=None, qk_norm=None,
-                 target_kv4: Optional[Kv4Cache] = None, window: int = 0, sinks: int = 0):
+                 target_kv4: Optional[Kv4Cache] = None, window: int = 0, sinks: int = 0,
+                 pages: Optional[PageSelection] = None, weights: Optional[TokenWeights] = None):
         """target_fp8: optional (codes_k, codes_v, k_scale_exp, v_scale_exp), an e4m3 copy of the target
         cache (workloads.fp8_target) to attend instead of inp.target_k / inp.target_v.
         qk_norm: optional (q_norm_w, k_norm_w, eps): the append normalises q and k per head first
         (kvshot_draft_append_qknorm).
         target_kv4: optional 4-bit cache to attend, with its own lengths and tables, instead of inp's target cache;
         then also window and sinks (kvshot_draft_attn_kv4).  Its draft tokens stand behind the lengths that the cache has
-        when run() comes to them in stream order: inp's positions only say how far behind inp's lengths a node stands."""
+        when run() comes to them in stream order: inp's positions only say how far behind inp's lengths a node stands.
+        pages: optional selection of inp's pages: each node reads the best ones for it, per KV head.
+        weights: optional weights of inp's tokens, to which every level adds (not with pages: a softmax over some tokens gives no
+        weights to the others)."""
         if mode not in ("per_depth", "whole"):
             raise ValueError(mode)
         if target_kv4 is None and (window or sinks):
             raise ValueError("a window needs the 4-bit target cache")
         if target_kv4 is not None and target_fp8 is not None:
             raise ValueError("one target cache")
+        if (pages is not None or weights is not None) and (target_fp8 is not None or target_kv4 is not None):
+            raise ValueError("pages and weights are of the bf16 target cache")
+        if pages is not None and weights is not None:
+            raise ValueError("weights need the softmax over all tokens")
+        if any(x is not None and x.inp is not inp for x in (pages, weights)):
+            raise ValueError("pages and weights of another cache")
         self.inp, self.mode = inp, mode
+        self.pages, self.weights = pages, weights
         self.qk_norm = qk_norm
         self.kv4, self.window, self.sinks = target_kv4, window, sinks
         s = inp.spec
@@ -94,6 +107,9 @@ class DraftStep:
                 k_scale_exp=k_exp, v_scale_exp=v_exp))
         if target_kv4 is not None:
             ws = [kvshot.draft_attn_kv4_workspace_size(d, window, sinks) for d in self.descs]
+        elif pages is not None:
+            ws = [kvshot.draft_attn_sparse_workspace_size(d, pages.keep) for d in self.descs]
+            self._pick_buffers()
         else:
             ws = [kvshot.workspace_size(d) for d in self.descs]
         ws = max(ws) if min(ws) > 0 else 0
@@ -103,6 +119,15 @@ class DraftStep:
         for d in self.descs:
             d.workspace = self.workspace.data_ptr()
             d.workspace_bytes = ws
+
+    def _pick_buffers(self) -> None:
+        """Of every level: scores of the pages, the picks and their numbers."""
+        s, dev, width = self.inp.spec, self.device, self.inp.page_table.shape[1]
+        self.select = [self.pages.select_desc(n) for n in self.levels]
+        rows = [(s.num_caches, n, s.hkv) for n in self.levels]
+        self.scores = [torch.empty((*r, width), dtype=torch.float32, device=dev) for r in rows]
+        self.picks = [torch.empty((*r, self.pages.keep), dtype=torch.int32, device=dev) for r in rows]
+        self.counts = [torch.empty(r, dtype=torch.int32, device=dev) for r in rows]
 
     @property
     def tokens(self) -> int:
@@ -144,9 +169,17 @@ class DraftStep:
                 kvshot.draft_attn_kv4(d, self.q_rot[i], self.kv4.data, self.kv4.page_table, self.kv4.seq_lens,
                                       self.draft_k, self.draft_v, self.parents[i], self.window, self.sinks,
                                       self.out[i], self.lse[i], stream)
+            elif self.pages is not None:
+                kvshot.page_scores(d, self.q_rot[i], self.pages.bounds, inp.page_table, inp.seq_lens, self.scores[i], stream)
+                kvshot.select_top(self.select[i], self.scores[i], inp.seq_lens, self.picks[i], self.counts[i], stream)
+                kvshot.draft_attn_sparse(d, self.q_rot[i], inp.target_k, inp.target_v, inp.page_table, inp.seq_lens,
+                                         self.picks[i], self.counts[i], self.pages.keep, self.draft_k, self.draft_v,
+                                         self.parents[i], self.out[i], self.lse[i], stream)
             else:
                 kvshot.draft_attn(d, self.q_rot[i], self.target_k, self.target_v, inp.page_table, inp.seq_lens,
                                   self.draft_k, self.draft_v, self.parents[i], self.out[i], self.lse[i], stream)
+            if self.weights is not None:
+                self.weights.add(d, self.q_rot[i], self.lse[i], stream)
             n0 += n_step
 
     def error_code(self) -> int:
