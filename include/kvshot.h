@@ -481,7 +481,8 @@ kvshot_status kvshot_page_bounds(const kvshot_attn_desc* desc, const void* targe
 /*
  * scores[c, n, h, p] = scale * max over the q heads g of KV head h of sum_d max(q_gd min_d, q_gd max_d), with the bounds
  * of page p of cache c: no key of the page scores higher for draft token n.  [C, Nq, hkv, max_pages_per_seq] fp32; entries
- * past a cache's last page are left as they are.  Products accumulate in fp32.  Bounds and q must be finite.
+ * past a cache's last page are left as they are.  Products accumulate in fp32.  Bounds and q must be finite, and bounds
+ * 32-byte aligned.
  */
 kvshot_status kvshot_page_scores(const kvshot_attn_desc* desc, const void* q, const void* bounds,
                                  const int32_t* page_table, const int32_t* seq_lens, float* scores,

@@ -19,7 +19,7 @@ struct EvictParams {
   const int32_t *page_table, *page_table_out, *seq_lens, *kept, *kept_count, *free_count;
   int32_t *seq_lens_out, *free_pages, *free_count_out, *err;
   int C, hkv, P, max_pages, num_pages, max_pages_out, num_pages_out, max_kept, weights_len, weights_len_out, num_free;
-  int in_place;
+  int heads_each;  // of 2 hkv (K and V), that a CTA moves into another pool
 };
 
 // Length and number of kept tokens of cache c; kept < 0: the cache stays as it is.
@@ -54,12 +54,13 @@ __device__ __forceinline__ int checked_page(const EvictParams& p, const int32_t*
 // A row of 256 bytes is 16 pieces of 16; a thread moves one piece of several rows.  A chunk of rows is loaded whole, then
 // stored, and the next chunk's places are looked up while its bytes are on their way.
 //
-// Into another pool a CTA takes one chunk of a head's K or V.  In place chunks go in ascending order: a token's new place is
+// Into another pool a CTA takes one chunk of several heads' K and V, whose rows' places are the same but for the head.  In place chunks go in ascending order: a token's new place is
 // never behind its old one and both ascend, so a chunk's stores never reach what a later chunk loads, and one barrier
 // between a chunk's loads and its stores is enough.  There a CTA takes all chunks, and where that leaves SMs idle only 4 or 8
 // of the 16 pieces, which are independent of one another.
 constexpr int kMoveThreads = 256;
 constexpr int kMoveLoads = 8;  // rows of a thread and chunk
+constexpr int kHeadsEach = 4;  // heads' K or V that a CTA moves into another pool
 constexpr int kRowPieces = kHeadDim * 2 / 16;
 constexpr int kMoveItems = kMoveThreads * kMoveLoads;
 
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(EvictParams p) {
   const int c = blockIdx.z, y = blockIdx.y, tid = threadIdx.x;
   const CacheKeep ck = cache_keep(p, c, p.seq_lens[c], p.kept_count[c]);
   const int32_t* kept = p.kept + static_cast<size_t>(c) * p.max_kept;
-  if (y == 2 * p.hkv) {  // the weights: one CTA
+  if (y == static_cast<int>(gridDim.y) - 1) {  // the weights: one CTA
     if (p.weights == nullptr || blockIdx.x != 0) return;
     const float* src = p.weights + static_cast<size_t>(c) * p.weights_len;
     float* dst = p.weights_out + static_cast<size_t>(c) * p.weights_len_out;
@@ -96,9 +97,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(EvictParams p) {
       for (int i = ck.kept + tid; i < p.weights_len_out; i += kMoveThreads) dst[i] = 0.f;
     return;
   }
-  const int head = (y >> 1) * p.P, piece = (kInPlace ? blockIdx.x * kPieces : 0) + tid % kPieces;
-  const uint4* src = reinterpret_cast<const uint4*>((y & 1) != 0 ? p.v : p.k) + static_cast<size_t>(head) * kRowPieces + piece;
-  uint4* dst = reinterpret_cast<uint4*>((y & 1) != 0 ? p.v_out : p.k_out) + static_cast<size_t>(head) * kRowPieces + piece;
+  const int piece = (kInPlace ? blockIdx.x * kPieces : 0) + tid % kPieces;
   auto look_up = [&](int i0, int buf) {
 #pragma unroll
     for (int r = tid; r < kRows; r += kMoveThreads) {
@@ -121,6 +120,35 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(EvictParams p) {
   if (i0 >= ck.kept) return;
   look_up(i0, 0);
   __syncthreads();
+  // One head's K or V (0 .. 2 hkv - 1) after the other; in place there is one.
+  auto source = [&](int i) {
+    return reinterpret_cast<const uint4*>((i & 1) != 0 ? p.v : p.k) + static_cast<size_t>((i >> 1) * p.P) * kRowPieces + piece;
+  };
+  auto destination = [&](int i) {
+    return reinterpret_cast<uint4*>((i & 1) != 0 ? p.v_out : p.k_out) + static_cast<size_t>((i >> 1) * p.P) * kRowPieces + piece;
+  };
+  if (!kInPlace) {
+    int from[kMoveLoads], to[kMoveLoads];
+#pragma unroll
+    for (int i = 0; i < kMoveLoads; ++i) {
+      from[i] = s_src[0][i * (kMoveThreads / kPieces) + tid / kPieces];
+      to[i] = s_dst[0][i * (kMoveThreads / kPieces) + tid / kPieces];
+    }
+    for (int head = y * p.heads_each; head < min(2 * p.hkv, (y + 1) * p.heads_each); ++head) {
+      const uint4* src = source(head);
+      uint4* dst = destination(head);
+      uint4 x[kMoveLoads];
+#pragma unroll
+      for (int i = 0; i < kMoveLoads; ++i)
+        if (from[i] >= 0) x[i] = __ldg(src + static_cast<size_t>(from[i]) * kRowPieces);
+#pragma unroll
+      for (int i = 0; i < kMoveLoads; ++i)
+        if (from[i] >= 0) dst[static_cast<size_t>(to[i]) * kRowPieces] = x[i];
+    }
+    return;
+  }
+  const uint4* src = source(y);
+  uint4* dst = destination(y);
   for (int buf = 0;; buf ^= 1) {
     uint4 x[kMoveLoads];
     int to[kMoveLoads];  // (read before the barrier: behind it these places may already be a later chunk's)
@@ -128,17 +156,15 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(EvictParams p) {
     for (int i = 0; i < kMoveLoads; ++i) {
       const int from = s_src[buf][i * (kMoveThreads / kPieces) + tid / kPieces];
       to[i] = s_dst[buf][i * (kMoveThreads / kPieces) + tid / kPieces];
-      if (from >= 0) x[i] = kInPlace ? src[static_cast<size_t>(from) * kRowPieces] : __ldg(src + static_cast<size_t>(from) * kRowPieces);
+      if (from >= 0) x[i] = src[static_cast<size_t>(from) * kRowPieces];
     }
     i0 += kRows;
-    if (kInPlace) {
-      if (i0 < ck.kept) look_up(i0, buf ^ 1);
-      __syncthreads();
-    }
+    if (i0 < ck.kept) look_up(i0, buf ^ 1);
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < kMoveLoads; ++i)
       if (to[i] >= 0) dst[static_cast<size_t>(to[i]) * kRowPieces] = x[i];
-    if (!kInPlace || i0 >= ck.kept) break;
+    if (i0 >= ck.kept) break;
   }
 }
 
@@ -146,16 +172,17 @@ template <bool kInPlace, int kPieces>
 cudaError_t launch_move(const EvictParams& p, cudaStream_t stream) {
   const int room = static_cast<int>(std::min<int64_t>(p.max_kept, static_cast<int64_t>(p.max_pages_out) * p.P));
   const int x = kInPlace ? kRowPieces / kPieces : (room + kMoveItems / kPieces - 1) / (kMoveItems / kPieces);
-  return launch_maybe_pdl(move_kernel<kInPlace, kPieces>, dim3(x, 2 * p.hkv + 1, p.C), dim3(kMoveThreads), 0, false, stream, p);
+  const int y = kInPlace ? 2 * p.hkv : (2 * p.hkv + p.heads_each - 1) / p.heads_each;
+  return launch_maybe_pdl(move_kernel<kInPlace, kPieces>, dim3(x, y + 1, p.C), dim3(kMoveThreads), 0, false, stream, p);
 }
 
-// Lengths and free pages: one CTA, a thread per cache, then a warp per cache writes its pages.
+// Lengths and free pages: one CTA, a thread per cache, then a warp per cache writes its pages.  Beside the last rows' moves, which
+// read neither list nor count; the lengths, which they may still read, are written when the moves have ended.
 constexpr int kEndThreads = 1024;
 static_assert(kEndThreads >= kMaxCaches, "a thread per cache");
 
 __global__ void __launch_bounds__(kEndThreads) evict_end_kernel(EvictParams p) {
   __shared__ int s_first[kMaxCaches], s_gone[kMaxCaches], s_base[kMaxCaches], s_warp[32];
-  wait_for_prerequisite_grid();
   const int c = threadIdx.x, lane = c & 31, warp = c >> 5;
   CacheKeep ck{0, -1};
   if (c < p.C) ck = cache_keep(p, c, p.seq_lens[c], p.kept_count[c]);
@@ -179,19 +206,19 @@ __global__ void __launch_bounds__(kEndThreads) evict_end_kernel(EvictParams p) {
   s_gone[c] = gone;
   s_base[c] = base;
   __syncthreads();  // (free_count has been read by all)
-  if (c < p.C) p.seq_lens_out[c] = ck.kept >= 0 ? ck.kept : ck.len;
-  if (p.free_pages == nullptr) return;
-  if (F < 0 || static_cast<int64_t>(F) + total > p.num_free) {
+  if (p.free_pages != nullptr) {
+    const bool room = F >= 0 && static_cast<int64_t>(F) + total <= p.num_free;
     if (c == 0) {
-      set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
-      *p.free_count_out = F;
+      if (!room) set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
+      *p.free_count_out = room ? F + total : F;
     }
-    return;
+    if (room)
+      for (int i = warp; i < p.C; i += 32)
+        for (int j = lane; j < s_gone[i]; j += 32)
+          p.free_pages[F + s_base[i] + j] = p.page_table[static_cast<size_t>(i) * p.max_pages + s_first[i] + j];
   }
-  if (c == 0) *p.free_count_out = F + total;
-  for (int i = warp; i < p.C; i += 32)
-    for (int j = lane; j < s_gone[i]; j += 32)
-      p.free_pages[F + s_base[i] + j] = p.page_table[static_cast<size_t>(i) * p.max_pages + s_first[i] + j];
+  wait_for_prerequisite_grid();  // (by all: what follows this kernel follows the moves, too)
+  if (c < p.C) p.seq_lens_out[c] = ck.kept >= 0 ? ck.kept : ck.len;
 }
 
 }  // namespace
@@ -238,7 +265,7 @@ extern "C" kvshot_status kvshot_cache_evict(const kvshot_evict_desc* d, const vo
                       static_cast<uint8_t*>(v_out), weights, weights_out, page_table, page_table_out, seq_lens, kept,
                       kept_count, free_count, seq_lens_out, free_pages, free_count_out, d->err_flag, d->num_caches, d->hkv,
                       d->page_size, d->max_pages_per_seq, d->num_pages, d->max_pages_out, d->num_pages_out, d->max_kept,
-                      d->weights_len, d->weights_len_out, d->num_free, in_place ? 1 : 0};
+                      d->weights_len, d->weights_len_out, d->num_free, kHeadsEach};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   // In place: whole rows while those alone are two CTAs to an SM.
   const int64_t ctas = 2LL * d->hkv * d->num_caches, enough = 2LL * sm_count();

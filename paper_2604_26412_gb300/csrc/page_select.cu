@@ -66,32 +66,41 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(CacheView v, con
 // ------------------------------------------------------------ scores
 
 // max(q lo, q hi) = max(q, 0) hi + min(q, 0) lo, so a page's score is the product of [min(q, 0), max(q, 0)] with its
-// bounds [lo, hi], a row of 256 elements: 16 steps of mma.sync with 16 pages as M.
+// bounds [lo, hi], a row of 256 elements: 16 steps of mma.sync with 16 pages as M.  The two halves of a row of q lie in shared
+// memory; lane (g, t) has pieces 2 t, 2 t + 1 of every 128 bytes of rows g and g + 8 (32-byte loads of the bounds).
 constexpr int kScoreWarps = 4;
-constexpr int kScoreRows = 128;  // rows of q in shared memory at a time
+constexpr int kScoreRows = 64;                   // rows of q in shared memory at a time
+constexpr int kScoreRowBytes = 2 * 256 + 64;     // 8 rows' pieces are in different banks
 
 struct ScoreParams {
   CacheView v;
   const uint4* q;       // rows [C, Nq, hq]
   const uint4* bounds;  // 32 pieces per (page, head): lo, hi
   float* scores;
-  int hq, G, Nq, log_gp;  // G padded to 2^log_gp columns
+  int hq, G, Nq;
   float scale;
 };
 
-__global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p) {
+// kLogGp: G is padded to 2^kLogGp columns (4: to 16 or 32, in log_gp).
+template <int kLogGp>
+__global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p, int log_gp_arg) {
   extern __shared__ __align__(16) uint8_t s_q[];  // up to kScoreRows rows
+  const int log_gp = kLogGp < 4 ? kLogGp : log_gp_arg, gp = 1 << log_gp;
   const int c = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t = lane & 3;
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  const int gp = 1 << p.log_gp, rows = p.Nq << p.log_gp, stride = p.v.max_pages * p.v.hkv;
+  const int rows = p.Nq << log_gp;
+  const size_t stride = static_cast<size_t>(p.v.max_pages) * p.v.hkv;
+  float* out = p.scores + (static_cast<size_t>(c) * p.Nq * p.v.hkv + h) * p.v.max_pages;
   auto stage = [&](int r0) {
     const int here = min(kScoreRows, (rows - r0 + 15) / 16 * 16);
     for (int i = threadIdx.x; i < here * 16; i += kScoreWarps * 32) {
-      const int r = r0 + i / 16, n = r >> p.log_gp, j = r & (gp - 1);
+      const int r = r0 + i / 16, n = r >> log_gp, j = r & (gp - 1);
       const bool live = n < p.Nq && j < p.G;
       const uint4 x = live ? __ldg(p.q + ((static_cast<size_t>(c) * p.Nq + n) * p.hq + h * p.G + j) * 16 + i % 16) : zero;
-      *reinterpret_cast<uint4*>(s_q + (i / 16) * kQRowBytes + (i % 16) * 16) = x;
+      uint4* row = reinterpret_cast<uint4*>(s_q + (i / 16) * kScoreRowBytes) + i % 16;
+      row[0] = make_uint4(min2(x.x, 0), min2(x.y, 0), min2(x.z, 0), min2(x.w, 0));
+      row[16] = make_uint4(max2(x.x, 0), max2(x.y, 0), max2(x.z, 0), max2(x.w, 0));
     }
     return here;
   };
@@ -111,18 +120,19 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p)
   const int L = clamped_len(p.v, c);
   const int pages = (L + p.v.P - 1) / p.v.P;
   if (cta0 >= pages) return;
+  const bool masked = p.G != gp;
   bool staged = false;
   for (; cta0 < pages; cta0 += gridDim.x * kPages) {
     const int page[2] = {cta0 + warp * 16 + g, cta0 + warp * 16 + g + 8};
-    uint4 b[2][8];
+    Row32 b[2][4];  // the 128-byte parts of the two pages' rows: lo, lo, hi, hi
     bool live[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       live[i] = page[i] < pages && static_cast<unsigned>(id[i]) < static_cast<unsigned>(p.v.num_pages);
       if (page[i] < pages && !live[i]) set_error(p.v.err, KVSHOT_ERR_DEVICE_BOUNDS);
-      const uint4* src = p.bounds + (static_cast<size_t>(live[i] ? id[i] : 0) * p.v.hkv + h) * 32 + t;
+      const uint4* src = p.bounds + (static_cast<size_t>(live[i] ? id[i] : 0) * p.v.hkv + h) * 32 + 2 * t;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) b[i][j] = live[i] ? __ldg(src + 4 * j) : zero;
+      for (int j = 0; j < 4; ++j) b[i][j] = live[i] ? load32(src + 8 * j) : Row32{zero, zero};
     }
     look_up(cta0 + gridDim.x * kPages);
     float best[2] = {-INFINITY, -INFINITY};  // of a node whose columns are several tiles (gp > 8)
@@ -137,42 +147,42 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p)
       for (int pair = 0; pair < here / 16; ++pair) {
         // Two tiles of 8 columns, the products with the least and the greatest keys apart: four chains.
         float d[2][4] = {}, d2[2][4] = {};
-        const uint8_t* row = s_q + (pair * 16 + g) * kQRowBytes + t * 16;
+        const uint8_t* row = s_q + (pair * 16 + g) * kScoreRowBytes + t * 32;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const uint4 q = *reinterpret_cast<const uint4*>(row + x * 8 * kQRowBytes + j * 64);
-            mma_piece(d[x], b[0][j], b[1][j], make_uint4(min2(q.x, 0), min2(q.y, 0), min2(q.z, 0), min2(q.w, 0)));
-            mma_piece(d2[x], b[0][j + 4], b[1][j + 4], make_uint4(max2(q.x, 0), max2(q.y, 0), max2(q.z, 0), max2(q.w, 0)));
+            const uint4* q = reinterpret_cast<const uint4*>(row + x * 8 * kScoreRowBytes + j * 128);
+            float (&acc)[4] = j < 2 ? d[x] : d2[x];
+            mma_piece(acc, b[0][j].lo, b[1][j].lo, q[0]);
+            mma_piece(acc, b[0][j].hi, b[1][j].hi, q[1]);
           }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           // d: page g, columns 2 t and 2 t + 1; page g + 8, the same columns.
           const int col = r0 + pair * 16 + x * 8 + 2 * t;
           auto put = [&](int i, int n, float s) {
-            if (n < p.Nq && live[i])
-              p.scores[(static_cast<size_t>(c) * p.Nq + n) * stride + static_cast<size_t>(h) * p.v.max_pages + page[i]] =
-                  s * p.scale;
+            if (n < p.Nq && live[i]) out[n * stride + page[i]] = s * p.scale;
           };
           float s[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[i] = d[x][i] + d2[x][i];
-          if (gp == 1) {
+          if (kLogGp == 0) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) put(i >> 1, col + (i & 1), s[i]);
             continue;
           }
+          if (masked)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (((col + (i & 1)) & (gp - 1)) >= p.G) s[i] = -INFINITY;
+            for (int i = 0; i < 4; ++i)
+              if (((col + (i & 1)) & (gp - 1)) >= p.G) s[i] = -INFINITY;
           float m[2] = {fmaxf(s[0], s[1]), fmaxf(s[2], s[3])};
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            if (gp > 2) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 1));
-            if (gp > 4) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 2));
+            if (kLogGp > 1) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 1));
+            if (kLogGp > 2) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 2));
           }
-          if (gp > 8) {
+          if (kLogGp > 3) {
             const bool last = ((col & (gp - 1)) >> 3) == (gp >> 3) - 1;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -184,7 +194,7 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p)
           }
           if ((2 * t & (gp - 1)) == 0)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) put(i, col >> p.log_gp, m[i]);
+            for (int i = 0; i < 2; ++i) put(i, col >> log_gp, m[i]);
         }
       }
     }
@@ -539,7 +549,7 @@ extern "C" kvshot_status kvshot_page_scores(const kvshot_attn_desc* d, const voi
   if (kvshot_status st = check_partial(d, true)) return st;
   if (d->n_query == 0) return KVSHOT_OK;
   if (!q || !bounds || !page_table || !seq_lens || !scores) return KVSHOT_ERR_NULL;
-  if (!aligned(q, 16) || !aligned(bounds, 16) || !aligned(page_table, 4) || !aligned(seq_lens, 4) || !aligned(scores, 4))
+  if (!aligned(q, 16) || !aligned(bounds, 32) || !aligned(page_table, 4) || !aligned(seq_lens, 4) || !aligned(scores, 4))
     return KVSHOT_ERR_ALIGN;
   ScoreParams p;
   p.v = cache_view(d, page_table, seq_lens);
@@ -549,20 +559,26 @@ extern "C" kvshot_status kvshot_page_scores(const kvshot_attn_desc* d, const voi
   p.hq = d->hq;
   p.G = d->hq / d->hkv;
   p.Nq = d->n_query;
-  p.log_gp = 0;
-  while ((1 << p.log_gp) < p.G) ++p.log_gp;
-  if ((static_cast<int64_t>(p.Nq) << p.log_gp) >= INT_MAX || static_cast<int64_t>(p.v.max_pages) * p.v.hkv >= INT_MAX)
+  int log_gp = 0;
+  while ((1 << log_gp) < p.G) ++log_gp;
+  if ((static_cast<int64_t>(p.Nq) << log_gp) >= INT_MAX || static_cast<int64_t>(p.v.max_pages) * p.v.hkv >= INT_MAX)
     return KVSHOT_ERR_UNSUPPORTED;
   p.scale = score_scale(d);
   const int pages = (p.v.len_bound + p.v.P - 1) / p.v.P, per_cta = kScoreWarps * 16;
   if (pages == 0) return KVSHOT_OK;
-  const size_t smem = static_cast<size_t>(std::min(kScoreRows, ((p.Nq << p.log_gp) + 15) / 16 * 16)) * kQRowBytes;
-  // CTAs take several chunks of pages, and q once, where there are more than four waves of them.
+  const size_t smem = static_cast<size_t>(std::min(kScoreRows, ((p.Nq << log_gp) + 15) / 16 * 16)) * kScoreRowBytes;
+  // Where there are more than sixteen CTAs to an SM, each takes several chunks of pages, and q once.
   const int64_t heads = static_cast<int64_t>(p.v.hkv) * p.v.C;
   const int chunks = (pages + per_cta - 1) / per_cta;
-  const int x = static_cast<int>(std::min<int64_t>(chunks, std::max<int64_t>(1, 16 * sm_count() / heads)));
-  const cudaError_t e = launch_maybe_pdl(scores_kernel, dim3(x, p.v.hkv, p.v.C),
-                                         dim3(kScoreWarps * 32), smem, false, reinterpret_cast<cudaStream_t>(stream), p);
+  const int64_t each = std::max<int64_t>(1, (chunks * heads + 16 * sm_count() - 1) / (16 * sm_count()));
+  const int x = static_cast<int>((chunks + each - 1) / each);
+  auto* kernel = log_gp == 0   ? scores_kernel<0>
+                 : log_gp == 1 ? scores_kernel<1>
+                 : log_gp == 2 ? scores_kernel<2>
+                 : log_gp == 3 ? scores_kernel<3>
+                               : scores_kernel<4>;
+  const cudaError_t e = launch_maybe_pdl(kernel, dim3(x, p.v.hkv, p.v.C), dim3(kScoreWarps * 32), smem, false,
+                                         reinterpret_cast<cudaStream_t>(stream), p, log_gp);
   return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
 }
 

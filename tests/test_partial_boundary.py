@@ -102,6 +102,8 @@ def test_pointers(call, names, wide):
         assert call({name: A + 2}) == ALIGN
     for name in wide:
         assert call({name: A + 8}) == ALIGN
+    if call is scores:
+        assert call({"b": A + 16}) == ALIGN
     if call is sparse:
         for name in ("k", "v", "dk", "dv"):
             assert call({name: A + 16}) == ALIGN
