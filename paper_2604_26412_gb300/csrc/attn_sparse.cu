@@ -124,12 +124,13 @@ struct WarpState {
   }
 };
 
-// A unit is one (cache, KV head, query row); its CTAs (a cluster of 1 to 8) take equal parts of its pages, the last one
-// the draft keys too, and the CTA's warps 16 keys in turn.  Nodes of one cache and head are next to one another in the
-// grid: their pages overlap, and meet in L2.
+// A unit is one (cache, KV head, query row); the CTAs of a cluster (1 to 8) take its picks in turn, the last one the draft keys
+// too, and a CTA's warps 16 keys in turn.  Nodes of one cache and head are next to one another in the grid: their pages
+// overlap, and meet in L2.  A call of few units is a chain of latencies: picks, table, K and V, the states' meeting.  So picks
+// and table entries are loaded before the length and the count are known, as far as the lists and the table reach.
 template <int NT>
 __global__ void __launch_bounds__(kSparseThreads) sparse_kernel(SparseParams p) {
-  extern __shared__ __align__(16) float s_part[];  // [warps][8 NT][kPartStride]
+  extern __shared__ __align__(16) float s_part[];  // [warps][8 NT][kPartStride]; the CTA's state is joined in the first warp's
   __shared__ int s_row[kSparseThreads], s_valid[kSparseThreads];
   __shared__ float s_m[kSparseWarps][8 * NT], s_l[kSparseWarps][8 * NT];
   __shared__ int s_parent[kMaxTreeNodes], s_line[kMaxTreeNodes];
@@ -138,14 +139,26 @@ __global__ void __launch_bounds__(kSparseThreads) sparse_kernel(SparseParams p) 
   const int rank = blockIdx.x % S, unit = blockIdx.x / S;
   const int n = unit % p.Nq, h = unit / p.Nq % p.v.hkv, c = unit / p.Nq / p.v.hkv;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int L = clamped_len(p.v, c);
   const size_t list = (static_cast<size_t>(c) * p.Nq + n) * p.v.hkv + h;
+  const int32_t* picks = p.picks + list * p.max_picks;
+  const int32_t* table = p.v.page_table + static_cast<size_t>(c) * p.v.max_pages;
+  // This CTA's picks are rank, rank + S, ...; a thread looks up one of a batch.
+  int pick = -1, before = -1, id = -1;
+  auto look_up = [&](int base) {
+    const int64_t at = (static_cast<int64_t>(base) + tid) * S + rank;
+    pick = at < p.max_picks ? __ldg(picks + at) : -1;
+    before = at > 0 && at < p.max_picks ? __ldg(picks + at - 1) : -1;
+    id = pick >= 0 && pick < p.v.max_pages ? __ldg(table + pick) : -1;
+  };
+  look_up(0);
   int count = p.counts[list];
+  const int L = clamped_len(p.v, c);
+  const bool draft = rank == S - 1, tree = p.tree_parent != nullptr;
+  if (draft && tree && tid < p.N) s_parent[tid] = p.tree_parent[static_cast<size_t>(c / p.per_seq) * p.N + tid];
   if (count < 0 || count > p.max_picks) {
     set_error(p.v.err, KVSHOT_ERR_DEVICE_BOUNDS);
     count = min(max(count, 0), p.max_picks);
   }
-  const int32_t* picks = p.picks + list * p.max_picks;
 
   WarpState<NT> st;
   st.init();
@@ -156,24 +169,23 @@ __global__ void __launch_bounds__(kSparseThreads) sparse_kernel(SparseParams p) 
     for (int j = 0; j < 4; ++j)
       st.q[nt][j] = nt * 8 + g < p.G ? __ldg(p.q + (qrow + nt * 8 + g) * 16 + 8 * (j >> 1) + 2 * t + (j & 1)) : make_uint4(0, 0, 0, 0);
 
-  const int i0 = static_cast<int>(static_cast<int64_t>(count) * rank / S);
-  const int i1 = static_cast<int>(static_cast<int64_t>(count) * (rank + 1) / S);
+  const int own = count > rank ? (count - rank + S - 1) / S : 0;  // picks of this CTA
   const int groups_per_page = p.v.P / 8;
-  for (int base = i0; base < i1; base += kSparseThreads) {
-    __syncthreads();
-    const int here = min(kSparseThreads, i1 - base);
+  for (int base = 0; base < own; base += kSparseThreads) {
+    if (base > 0) {
+      __syncthreads();
+      look_up(base);
+    }
+    const int here = min(kSparseThreads, own - base);
     if (tid < here) {
-      const int pick = picks[base + tid], before = base + tid > 0 ? picks[base + tid - 1] : -1;
       int row = 0, valid = 0;
       if (pick >= 0 && pick > before && static_cast<int64_t>(pick) * p.v.P < L) {
-        const int id = page_id(p.v, c, pick);
-        if (id >= 0) {
+        if (static_cast<unsigned>(id) < static_cast<unsigned>(p.v.num_pages)) {
           row = (id * p.v.hkv + h) * p.v.P;
           valid = min(p.v.P, L - pick * p.v.P);
         }
-      } else {
-        set_error(p.v.err, KVSHOT_ERR_DEVICE_BOUNDS);
       }
+      if (valid == 0) set_error(p.v.err, KVSHOT_ERR_DEVICE_BOUNDS);
       s_row[tid] = row;
       s_valid[tid] = valid;
     }
@@ -194,11 +206,9 @@ __global__ void __launch_bounds__(kSparseThreads) sparse_kernel(SparseParams p) 
     }
   }
 
-  if (rank == S - 1) {  // the node itself and its ancestors
+  if (draft) {  // the node itself and its ancestors
     const int node = p.N - p.Nq + n;
-    if (p.tree_parent != nullptr) {
-      const int32_t* parent = p.tree_parent + static_cast<size_t>(c / p.per_seq) * p.N;
-      if (tid < p.N) s_parent[tid] = parent[tid];
+    if (tree) {
       __syncthreads();
       if (tid == 0) {
         int at = node, len = 0;
@@ -215,17 +225,18 @@ __global__ void __launch_bounds__(kSparseThreads) sparse_kernel(SparseParams p) 
       }
       __syncthreads();
     }
-    const int line = p.tree_parent != nullptr ? s_line_len : node + 1;
+    const int line = tree ? s_line_len : node + 1;
     const int draft0 = (c * p.v.hkv + h) * p.n_max;
-    auto slot = [&](int i) { return i >= line ? -1 : draft0 + (p.tree_parent != nullptr ? s_line[i] : i); };
-    for (int s = warp; s * 16 < line; s += kSparseWarps) {
+    auto slot = [&](int i) { return i >= line ? -1 : draft0 + (tree ? s_line[i] : i); };
+    // (From the last warp down: it has the fewest of the pages' keys.)
+    for (int s = kSparseWarps - 1 - warp; s * 16 < line; s += kSparseWarps) {
       const int kr[2] = {slot(s * 16 + g), slot(s * 16 + g + 8)};
       const int vr[4] = {slot(s * 16 + 2 * t), slot(s * 16 + 2 * t + 1), slot(s * 16 + 2 * t + 8), slot(s * 16 + 2 * t + 9)};
       st.step(p.dk, p.dv, kr, vr, p.qscale, g, t);
     }
   }
 
-  // The warps' states joined: reference and sum of every row, then a weighted sum of the O's.
+  // The warps' states joined, then the CTAs': reference and sum of every row, and a weighted sum of the O's.
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -243,21 +254,43 @@ __global__ void __launch_bounds__(kSparseThreads) sparse_kernel(SparseParams p) 
       for (int i = 0; i < 8; ++i)
         *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(st.o[nt][i][e], st.o[nt][i][2 + e]);
     }
+  __syncthreads();
+  __shared__ float s_top[8 * NT], s_sum[8 * NT];  // of the CTA
+  for (int i = tid; i < p.G * kHeadDim; i += kSparseThreads) {
+    const int r = i / kHeadDim, d = i % kHeadDim;
+    float top = s_m[0][r];
+#pragma unroll
+    for (int w = 1; w < kSparseWarps; ++w) top = fmaxf(top, s_m[w][r]);
+    float sum = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < kSparseWarps; ++w) {
+      const float f = s_m[w][r] == -INFINITY ? 0.f : ex2(s_m[w][r] - top);
+      sum += f * s_l[w][r];
+      o += f * s_part[(w * 8 * NT + r) * kPartStride + d];
+    }
+    s_part[r * kPartStride + d] = o;
+    if (d == 0) {
+      s_top[r] = top;
+      s_sum[r] = sum;
+    }
+  }
   if (S > 1) cluster_sync_all();
   else __syncthreads();
   for (int i = rank * kSparseThreads + tid; i < p.G * kHeadDim; i += S * kSparseThreads) {
     const int r = i / kHeadDim, d = i % kHeadDim;
-    float top = -INFINITY;
-    for (int x = 0; x < S; ++x)
-      for (int w = 0; w < kSparseWarps; ++w) top = fmaxf(top, remote_float(smem_addr(&s_m[w][r]), x));
-    float sum = 0.f, o = 0.f;
-    for (int x = 0; x < S; ++x)
-      for (int w = 0; w < kSparseWarps; ++w) {
-        const float m = remote_float(smem_addr(&s_m[w][r]), x);
-        const float f = m == -INFINITY ? 0.f : ex2(m - top);
-        sum += f * remote_float(smem_addr(&s_l[w][r]), x);
-        o += f * remote_float(smem_addr(s_part + (w * 8 * NT + r) * kPartStride + d), x);
-      }
+    float m[8], top = -INFINITY, sum = 0.f, o = 0.f;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      m[x] = x < S ? remote_float(smem_addr(&s_top[r]), x) : -INFINITY;
+      top = fmaxf(top, m[x]);
+    }
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      if (x >= S) break;
+      const float f = m[x] == -INFINITY ? 0.f : ex2(m[x] - top);
+      sum += f * remote_float(smem_addr(&s_sum[r]), x);
+      o += f * remote_float(smem_addr(s_part + r * kPartStride + d), x);
+    }
     p.out[(qrow + r) * kHeadDim + d] = __float2bfloat16_rn(o / sum);
     if (d == 0) p.lse[qrow + r] = (top + log2f(sum)) * 0.6931471805599453f;
   }

@@ -49,8 +49,21 @@ __global__ void __launch_bounds__(kDirectWarps * 32) weights_kernel(WeightParams
   const int S = static_cast<int>(cluster_size());
   const int rank = blockIdx.x % S, c = blockIdx.y;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int L = weights_len_of(p, c);
   const int cta0 = blockIdx.x / S * kDirectKeys;
+  // (Table entries are looked up beside the length, and what the keys had before beside everything.)
+  int id[kDirectChunks][2];
+#pragma unroll
+  for (int i = 0; i < kDirectChunks; ++i)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int page = (cta0 + (warp * kDirectChunks + i) * 16 + g + 8 * e) / p.v.P;
+      id[i][e] = p.v.page_table == nullptr ? c : page < p.v.max_pages ? __ldg(p.v.page_table + static_cast<size_t>(c) * p.v.max_pages + page) : -1;
+    }
+  const int key0 = cta0 + threadIdx.x;
+  const bool sums = static_cast<int>(threadIdx.x) % S == rank && key0 < p.weights_len;  // this thread ends key0's
+  const size_t key_at = static_cast<size_t>(c) * p.weights_len + key0;
+  const float had = sums && p.weights != nullptr ? p.weights[key_at] : 0.f;
+  const int L = weights_len_of(p, c);
   if (cta0 >= L) return;  // (the whole cluster)
   const uint4 zero = make_uint4(0, 0, 0, 0);
   bool live[kDirectChunks][2];
@@ -60,10 +73,10 @@ __global__ void __launch_bounds__(kDirectWarps * 32) weights_kernel(WeightParams
   for (int i = 0; i < kDirectChunks; ++i)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int j = cta0 + (warp * kDirectChunks + i) * 16 + g + 8 * e;
-      const int page = j / p.v.P, id = j < L ? page_id(p.v, c, page) : -1;
-      row[i][e] = (static_cast<size_t>(max(id, 0)) * p.v.hkv * p.v.P + (j - page * p.v.P)) * 16 + t;
-      live[i][e] = id >= 0;
+      const int j = cta0 + (warp * kDirectChunks + i) * 16 + g + 8 * e, page = j / p.v.P;
+      live[i][e] = j < L && static_cast<unsigned>(id[i][e]) < static_cast<unsigned>(p.v.num_pages);
+      if (j < L && !live[i][e]) set_error(p.v.err, KVSHOT_ERR_DEVICE_BOUNDS);
+      row[i][e] = (static_cast<size_t>(live[i][e] ? id[i][e] : 0) * p.v.hkv * p.v.P + (j - page * p.v.P)) * 16 + t;
     }
   const int h0 = p.v.hkv * rank / S, h1 = p.v.hkv * (rank + 1) / S, rows = p.Nq * p.G;
   const size_t head = static_cast<size_t>(p.v.P) * 16;
@@ -118,12 +131,13 @@ __global__ void __launch_bounds__(kDirectWarps * 32) weights_kernel(WeightParams
     }
   if (S > 1) cluster_sync_all();
   else __syncthreads();
-  const int i = threadIdx.x, j = cta0 + i;
-  if (i % S == rank && j < L) {
-    float x = 0.f;
-    for (int r = 0; r < S; ++r) x += remote_float(smem_addr(&s_w[i]), r);
-    const size_t at = static_cast<size_t>(c) * p.weights_len + j;
-    if (!(s_w[i] == -1.f)) p.weights_out[at] = p.weights != nullptr ? fmaf(p.decay, p.weights[at], x) : x;
+  if (sums && key0 < L) {
+    float x[8], sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) x[r] = r < S ? remote_float(smem_addr(&s_w[threadIdx.x]), r) : 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) sum += x[r];
+    if (!(s_w[threadIdx.x] == -1.f)) p.weights_out[key_at] = fmaf(p.decay, had, sum);
   }
   if (S > 1) cluster_sync_all();  // (another CTA may still read this one's sums)
 }

@@ -28,8 +28,9 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
 __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(CacheView v, const uint4* __restrict__ k,
                                                                const int32_t* __restrict__ from, uint4* bounds) {
   const int c = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int since = from == nullptr ? 0 : from[c];
   const int L = clamped_len(v, c);
-  const int p0 = from == nullptr ? 0 : max(0, from[c]) / v.P, pages = (L + v.P - 1) / v.P;
+  const int p0 = max(0, since) / v.P, pages = (L + v.P - 1) / v.P;
   const int64_t units = static_cast<int64_t>(max(0, pages - p0)) * v.hkv;
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kBoundsThreads / 32) + warp; u < units;
        u += static_cast<int64_t>(gridDim.x) * (kBoundsThreads / 32)) {
@@ -98,7 +99,8 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p,
       const int r = r0 + i / 16, n = r >> log_gp, j = r & (gp - 1);
       const bool live = n < p.Nq && j < p.G;
       const uint4 x = live ? __ldg(p.q + ((static_cast<size_t>(c) * p.Nq + n) * p.hq + h * p.G + j) * 16 + i % 16) : zero;
-      uint4* row = reinterpret_cast<uint4*>(s_q + (i / 16) * kScoreRowBytes) + i % 16;
+      // (of 128 bytes the even pieces, then the odd ones: a load of the warp has no two rows in one bank)
+      uint4* row = reinterpret_cast<uint4*>(s_q + (i / 16) * kScoreRowBytes) + (i & 8) + (i & 1) * 4 + (i >> 1 & 3);
       row[0] = make_uint4(min2(x.x, 0), min2(x.y, 0), min2(x.z, 0), min2(x.w, 0));
       row[16] = make_uint4(max2(x.x, 0), max2(x.y, 0), max2(x.z, 0), max2(x.w, 0));
     }
@@ -147,7 +149,7 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p,
       for (int pair = 0; pair < here / 16; ++pair) {
         // Two tiles of 8 columns, the products with the least and the greatest keys apart: four chains.
         float d[2][4] = {}, d2[2][4] = {};
-        const uint8_t* row = s_q + (pair * 16 + g) * kScoreRowBytes + t * 32;
+        const uint8_t* row = s_q + (pair * 16 + g) * kScoreRowBytes + t * 16;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -155,7 +157,7 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p,
             const uint4* q = reinterpret_cast<const uint4*>(row + x * 8 * kScoreRowBytes + j * 128);
             float (&acc)[4] = j < 2 ? d[x] : d2[x];
             mma_piece(acc, b[0][j].lo, b[1][j].lo, q[0]);
-            mma_piece(acc, b[0][j].hi, b[1][j].hi, q[1]);
+            mma_piece(acc, b[0][j].hi, b[1][j].hi, q[4]);
           }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
