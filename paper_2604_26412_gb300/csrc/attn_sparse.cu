@@ -757,8 +757,8 @@ cudaError_t launch_shared(const SparseParams& s, int caches, int S, uint32_t wai
   SharedMaps maps;
   const uint64_t rows = static_cast<uint64_t>(s.v.num_pages) * s.v.hkv * s.v.P;
   const uint64_t drows = static_cast<uint64_t>(caches) * s.v.hkv * s.n_max;
-  if (!encode_rows_grouped(&maps.k, s.k, rows, p.box_keys / 8) || !encode_rows_grouped(&maps.v, s.val, rows, p.box_keys / 8) ||
-      !encode_rows_group3(&maps.dk, s.dk, drows) || !encode_rows_group3(&maps.dv, s.dv, drows))
+  if (!map_groups(&maps.k, s.k, rows, p.box_keys / 8) || !map_groups(&maps.v, s.val, rows, p.box_keys / 8) ||
+      !map_any_8(&maps.dk, s.dk, drows) || !map_any_8(&maps.dv, s.dv, drows))
     return cudaErrorInvalidValue;
   const int warps = ((p.nodes_per_block << p.log_gp) + 7) / 8 + 1;
   auto* kernel = warps <= 7 ? sparse_shared_kernel<6> : sparse_shared_kernel<kSharedWarps>;
@@ -783,6 +783,7 @@ constexpr size_t kSparseWorkspace = 256;
 kvshot_status check_sparse(const kvshot_attn_desc* d, int max_picks) {
   if (kvshot_status st = check_partial(d, true)) return st;
   if (max_picks < 1) return KVSHOT_ERR_SHAPE;
+  if (max_picks > 1 << 24) return KVSHOT_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(d->num_caches) * d->hkv * d->n_query >= (int64_t{1} << 27)) return KVSHOT_ERR_UNSUPPORTED;
   return KVSHOT_OK;
 }
@@ -846,7 +847,7 @@ extern "C" kvshot_status kvshot_draft_attn_sparse(const kvshot_attn_desc* d, con
   int log_gp = 0;
   while ((1 << log_gp) < p.G) ++log_gp;
   const int64_t rows = static_cast<int64_t>(p.Nq) << log_gp, shared = int64_t{d->num_caches} * d->hkv * ((rows + 63) / 64);
-  if (rows >= 32 && 3 * shared >= 2 * sm_count()) {
+  if (rows >= 32 && 3 * shared >= 2 * sm_count() && rows < 64 * 65535) {
     const uint32_t wait_ns = d->wait_limit_ns != 0 ? d->wait_limit_ns : static_cast<uint32_t>(kWaitLimitNs);
     const int S = shared < 2 * sm_count() ? 2 : 1;
     return launch_shared(p, d->num_caches, S, wait_ns, s) == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;

@@ -239,7 +239,10 @@ extern "C" kvshot_status kvshot_cache_evict(const kvshot_evict_desc* d, const vo
     return KVSHOT_ERR_SHAPE;
   const int64_t page_rows = static_cast<int64_t>(d->hkv) * d->page_size;
   if (d->num_caches > kMaxCaches || d->head_dim != kHeadDim || d->hkv > 16383 || page_rows >= INT_MAX ||
-      d->num_pages * page_rows >= INT_MAX || d->num_pages_out * page_rows >= INT_MAX)
+      d->num_pages * page_rows >= INT_MAX || d->num_pages_out * page_rows >= INT_MAX ||
+      static_cast<int64_t>(d->num_caches) * d->max_pages_per_seq >= INT_MAX / 2 ||
+      static_cast<int64_t>(d->num_caches) * d->max_pages_out >= INT_MAX / 2 || d->max_kept > 1 << 30 ||
+      d->weights_len > 1 << 30 || d->weights_len_out > 1 << 30)
     return KVSHOT_ERR_UNSUPPORTED;
   if (!k || !v || !page_table || !seq_lens || !kept || !kept_count || !k_out || !v_out || !page_table_out || !seq_lens_out)
     return KVSHOT_ERR_NULL;

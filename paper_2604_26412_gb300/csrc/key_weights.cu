@@ -534,8 +534,8 @@ cudaError_t launch_tc(const WeightParams& w, const void* q, const void* k, int64
   p.box_rows = !p.grouped ? 8 : paged ? std::min(w.v.P, 64) : 64;
   const uint64_t rows = static_cast<uint64_t>(w.v.num_pages) * w.v.hkv * w.v.P;
   WeightMaps maps;
-  const bool kmap = p.grouped ? encode_rows_grouped(&maps.k, k, rows, p.box_rows / 8) : encode_rows_group3(&maps.k, k, rows);
-  if (!kmap || !encode_q(&maps.q, q, w.v.C, w.Nq, w.hq, QBox{w.G, p.nodes_per_block})) return cudaErrorInvalidValue;
+  const bool kmap = p.grouped ? map_groups(&maps.k, k, rows, p.box_rows / 8) : map_any_8(&maps.k, k, rows);
+  if (!kmap || !map_q(&maps.q, q, w.v.C, w.Nq, w.hq, w.G, p.nodes_per_block)) return cudaErrorInvalidValue;
   const size_t smem = 2 * p.cols * 256 + p.stages * kTcTileBytes + kTcTail;
   static_assert(sizeof(TcBarriers) <= 512, "barriers fit the tail");
   cudaError_t e = cudaFuncSetAttribute(weights_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem);

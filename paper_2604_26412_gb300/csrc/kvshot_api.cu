@@ -69,8 +69,6 @@ bool encode_rows_fp8(CUtensorMap* map, const void* base, uint64_t rows, uint32_t
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-}  // namespace
-
 // Grouped views of a [rows, 128] bf16 matrix for the tensor-memory kernel (kGroupBytes in
 // kvshot_internal.h): a box lands as 8-row groups of 2 KB, each holding its rows' dims 0..63
 // (128-byte swizzled) and then dims 64..127.
@@ -102,8 +100,6 @@ bool encode_rows_group3(CUtensorMap* map, const void* base, uint64_t rows) {
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-
-namespace {
 
 constexpr int kMaxScaleExp = 64;
 
@@ -174,6 +170,8 @@ void rope_turns(float rope_base, uint64_t* turns) {
   std::copy(table, table + kHeadDim / 2, turns);
 }
 
+namespace {
+
 // 4-D view {128 dims, hq, Nq, C} of q [C, Nq, hq, 128]; a box is one 64-dim
 // half of `heads` heads of one KV group for `nodes` draft nodes (rows node-major).
 bool encode_q(CUtensorMap* map, const void* q, int C, int Nq, int hq, QBox qb) {
@@ -189,8 +187,6 @@ bool encode_q(CUtensorMap* map, const void* q, int C, int Nq, int hq, QBox qb) {
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-
-namespace {
 
 struct Plan {
   Kernel kernel;
@@ -281,6 +277,8 @@ kvshot_status check_common(const kvshot_attn_desc* d) {
   return KVSHOT_OK;
 }
 
+namespace {
+
 kvshot_status check_attn_desc(const kvshot_attn_desc* d, bool paged) {
   if (kvshot_status st = check_common(d)) return st;
   if (paged) {
@@ -297,8 +295,6 @@ kvshot_status check_attn_desc(const kvshot_attn_desc* d, bool paged) {
   }
   return KVSHOT_OK;
 }
-
-namespace {
 
 // `small_blocks`: an fp8 stack of more than 128 rows takes attn_f8.cu's 64-row blocks.
 kvshot_status make_plan_for(const kvshot_attn_desc* d, bool paged, bool small_blocks, Plan* pl) {

@@ -118,12 +118,6 @@ struct TensorMaps {
 bool encode_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint32_t box_cols,
                     uint32_t box_rows);
 
-// Maps that land 8-row groups of a [rows, 128] bf16 matrix as the tensor-memory kernels read them (4-D: `groups` groups
-// from a row-group coordinate, rows a multiple of 8; 3-D: one from any row), and boxes of q [C, Nq, hq, 128].
-bool encode_rows_grouped(CUtensorMap* map, const void* base, uint64_t rows, uint32_t groups);
-bool encode_rows_group3(CUtensorMap* map, const void* base, uint64_t rows);
-bool encode_q(CUtensorMap* map, const void* q, int C, int Nq, int hq, QBox qb);
-
 // inv_freq[j] = rope_base^(-2j/128), j in [0, 64).  Each thread keeps the table of its last rope_base (64 pow calls
 // are ~1.3 us of a call's host time).
 void rope_frequencies(float rope_base, double* inv_freq);
@@ -132,8 +126,6 @@ void rope_turns(float rope_base, uint64_t* turns);
 
 // Descriptor checks that do not depend on the cache layout, and the current device's number of SMs (0: an error).
 kvshot_status check_common(const kvshot_attn_desc* d);
-// With those of the layout, as kvshot_draft_attn makes them.
-kvshot_status check_attn_desc(const kvshot_attn_desc* d, bool paged);
 int sm_count();
 
 // Kernel launchers (one per translation unit).  Return cudaSuccess or the launch error.  `pdl`:

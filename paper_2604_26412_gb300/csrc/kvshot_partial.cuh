@@ -2,6 +2,8 @@
 // its checks, and operand fragments of mma.sync read straight from rows in global memory.
 #pragma once
 
+#include <cudaTypedefs.h>
+
 #include "kvshot_attn_common.cuh"
 
 namespace kvshot {
@@ -19,16 +21,66 @@ struct CacheView {
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
-// Checks of the descriptor that all of them make.  (What check_attn_desc reads of heads and nodes is valid in a descriptor
-// that gives none of them but hq = hkv.)
+// Checks of the descriptor that all of them make: heads and nodes as kvshot_draft_attn has them (valid, too, in a descriptor that
+// gives none of them but hq = hkv), then the cache's layout.
 inline kvshot_status check_partial(const kvshot_attn_desc* d, bool paged) {
-  if (kvshot_status st = check_attn_desc(d, paged)) return st;
+  if (kvshot_status st = check_common(d)) return st;
+  const int64_t kRows = int64_t{1} << 31;  // rows of K, of tables and of q are 32-bit numbers
+  if (paged) {
+    const int P = d->page_size;  // groups of 8 keys, and boxes of up to 64, lie in one page
+    if (P < 8 || P > 256 || !(64 % P == 0 || P % 64 == 0)) return KVSHOT_ERR_UNSUPPORTED;
+    if (d->max_pages_per_seq < 1 || d->num_pages < 1) return KVSHOT_ERR_SHAPE;
+    if (static_cast<int64_t>(d->num_pages) * d->hkv * P >= kRows - 1 ||
+        static_cast<int64_t>(d->num_caches) * d->max_pages_per_seq >= kRows - 1)
+      return KVSHOT_ERR_UNSUPPORTED;
+  } else {
+    if (d->l_cap < 1) return KVSHOT_ERR_SHAPE;
+    if (static_cast<int64_t>(d->num_caches) * d->hkv * d->l_cap >= kRows - 1) return KVSHOT_ERR_UNSUPPORTED;
+  }
   if (d->flags & (KVSHOT_TARGET_FP8 | KVSHOT_FORCE_CC | KVSHOT_FORCE_MMA | KVSHOT_FORCE_TC)) return KVSHOT_ERR_UNSUPPORTED;
-  if (d->hq / d->hkv > kMaxGroup) return KVSHOT_ERR_UNSUPPORTED;
-  // Rows of q, and rows of scores or picks, are 32-bit numbers; so are grids.
-  if (static_cast<int64_t>(d->num_caches) * d->n_query * d->hq >= (int64_t{1} << 31)) return KVSHOT_ERR_UNSUPPORTED;
-  if (d->hkv > 65535) return KVSHOT_ERR_UNSUPPORTED;
+  // (Places of tokens stay 32-bit numbers where they are rounded up.)
+  const int64_t room = paged ? static_cast<int64_t>(d->max_pages_per_seq) * d->page_size : d->l_cap;
+  if ((room < d->max_seq_len ? room : d->max_seq_len) > kRows - 4096) return KVSHOT_ERR_UNSUPPORTED;
+  if (d->hq / d->hkv > kMaxGroup || d->hkv > 65535) return KVSHOT_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(d->num_caches) * d->n_query * d->hq >= kRows) return KVSHOT_ERR_UNSUPPORTED;
   return KVSHOT_OK;
+}
+
+// Tensor map of a bf16 tensor of `rank` dimensions, 128-byte swizzle; strides (of dimensions 1 ...) in bytes.  False if the
+// encoder is not there or refuses.
+inline bool encode_bf16(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                        const cuuint32_t* box) {
+  static const PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+    return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f) : nullptr;
+  }();
+  const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+  return encode != nullptr &&
+         encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, ones,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Rows of 128 dims landed in groups of 8 (kGroupBytes): {64 dims, 8 rows, 2 halves, rows / 8}, `groups` of them to a box ...
+inline bool map_groups(CUtensorMap* map, const void* base, uint64_t rows, uint32_t groups) {
+  const cuuint64_t dims[4] = {64, 8, 2, rows / 8}, strides[3] = {256, 128, 2048};
+  const cuuint32_t box[4] = {64, 8, 2, groups};
+  return rows % 8 == 0 && encode_bf16(map, base, 4, dims, strides, box);
+}
+// ... or one, from any row: {64 dims, rows, 2 halves}.
+inline bool map_any_8(CUtensorMap* map, const void* base, uint64_t rows) {
+  const cuuint64_t dims[3] = {64, rows, 2}, strides[2] = {256, 128};
+  const cuuint32_t box[3] = {64, 8, 2};
+  return encode_bf16(map, base, 3, dims, strides, box);
+}
+// Half the dims of `heads` heads of `nodes` rows of q [C, Nq, hq, 128].
+inline bool map_q(CUtensorMap* map, const void* q, int C, int Nq, int hq, uint32_t heads, uint32_t nodes) {
+  const cuuint64_t row = kHeadDim * 2;
+  const cuuint64_t dims[4] = {kHeadDim, static_cast<cuuint64_t>(hq), static_cast<cuuint64_t>(Nq), static_cast<cuuint64_t>(C)};
+  const cuuint64_t strides[3] = {row, row * hq, row * hq * Nq};
+  const cuuint32_t box[4] = {64, heads, nodes, 1};
+  return encode_bf16(map, q, 4, dims, strides, box);
 }
 
 inline CacheView cache_view(const kvshot_attn_desc* d, const int32_t* page_table, const int32_t* seq_lens) {
@@ -94,11 +146,18 @@ __device__ __forceinline__ void mma_piece(float (&d)[4], const uint4& a, const u
   dev::mma_bf16_16816(d, hi, b.z, b.w);
 }
 
-// A wait that looks a few times before it takes the time (reading the clock takes long enough to be late).
+// A wait that looks a few times before it takes the time (reading the clock takes long enough to be late).  A limit below the
+// clock's step gives up on the first look that finds the wait unfinished.
+constexpr uint64_t kNoWaitNs = 1000;
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int32_t* err, uint64_t limit) {
-  if (limit >= dev::kPollBelowNs)
+  if (limit >= dev::kPollBelowNs) {
     for (int i = 0; i < 32; ++i)
       if (dev::mbar_try_wait(bar, parity)) return true;
+  } else if (limit < kNoWaitNs) {
+    if (dev::mbar_test_wait(bar, parity)) return true;
+    dev::set_error(err, KVSHOT_ERR_TIMEOUT);
+    return false;
+  }
   return dev::mbar_wait(bar, parity, err, limit);
 }
 

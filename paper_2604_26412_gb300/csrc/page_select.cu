@@ -569,10 +569,10 @@ extern "C" kvshot_status kvshot_page_scores(const kvshot_attn_desc* d, const voi
   const int pages = (p.v.len_bound + p.v.P - 1) / p.v.P, per_cta = kScoreWarps * 16;
   if (pages == 0) return KVSHOT_OK;
   const size_t smem = static_cast<size_t>(std::min(kScoreRows, ((p.Nq << log_gp) + 15) / 16 * 16)) * kScoreRowBytes;
-  // Where there are more than sixteen CTAs to an SM, each takes several chunks of pages, and q once.
+  // Where there are more than twelve CTAs to an SM, each takes several chunks of pages, and q once.
   const int64_t heads = static_cast<int64_t>(p.v.hkv) * p.v.C;
   const int chunks = (pages + per_cta - 1) / per_cta;
-  const int64_t each = std::max<int64_t>(1, (chunks * heads + 16 * sm_count() - 1) / (16 * sm_count()));
+  const int64_t each = std::max<int64_t>(1, (chunks * heads + 12 * sm_count() - 1) / (12 * sm_count()));
   const int x = static_cast<int>((chunks + each - 1) / each);
   auto* kernel = log_gp == 0   ? scores_kernel<0>
                  : log_gp == 1 ? scores_kernel<1>
@@ -591,7 +591,7 @@ extern "C" kvshot_status kvshot_select_top(const kvshot_select_desc* d, const fl
       d->tokens_per_entry < 1 || d->keep < 1 || d->first < 0 || d->last < 0 ||
       static_cast<int64_t>(d->first) + d->last > d->keep)
     return KVSHOT_ERR_SHAPE;
-  if (d->num_rows >= INT_MAX / kMaxSelectCluster) return KVSHOT_ERR_UNSUPPORTED;
+  if (d->num_rows >= INT_MAX / kMaxSelectCluster || d->row_len > 1 << 30 || d->keep > 1 << 30) return KVSHOT_ERR_UNSUPPORTED;
   if (d->num_rows == 0) return KVSHOT_OK;
   if (!scores || !seq_lens || !picks || !counts) return KVSHOT_ERR_NULL;
   if (!aligned(scores, 4) || !aligned(seq_lens, 4) || !aligned(picks, 4) || !aligned(counts, 4)) return KVSHOT_ERR_ALIGN;

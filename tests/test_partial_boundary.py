@@ -72,6 +72,7 @@ BAD_DESC = [
     (dict(flags=kvshot.KVSHOT_TARGET_FP8), UNSUPPORTED), (dict(flags=kvshot.KVSHOT_FORCE_TC), UNSUPPORTED),
     (dict(flags=kvshot.KVSHOT_FORCE_MMA), UNSUPPORTED), (dict(flags=kvshot.KVSHOT_FORCE_CC), UNSUPPORTED),
     (dict(n_nodes=1 << 26, n_query=1 << 26, n_max=1 << 26), UNSUPPORTED),
+    (dict(max_pages_per_seq=1 << 27, max_seq_len=2 ** 31 - 1), UNSUPPORTED),
 ]
 
 
@@ -121,6 +122,7 @@ def test_calls_without_rows_do_nothing():
 
 def test_sparse_workspace_and_lists():
     assert sparse(max_picks=0) == SHAPE
+    assert sparse(max_picks=1 << 25) == UNSUPPORTED
     assert sparse(ws=(0, 1 << 40)) == WORKSPACE
     assert sparse(ws=(A + 128, 1 << 40)) == WORKSPACE
     need = kvshot.draft_attn_sparse_workspace_size(_desc(), 4)
@@ -147,6 +149,12 @@ def test_select_sizes(kw):
     assert kvshot.select_top_status(kvshot.make_select_desc(**d), A, A, A, A, stream=0) == SHAPE
 
 
+def test_select_sizes_beyond_its_numbers():
+    for kw in (dict(row_len=2 ** 31 - 1), dict(keep=2 ** 31 - 1), dict(num_rows=2 ** 28)):
+        d = dict(num_rows=4, row_len=16, keep=4) | kw
+        assert kvshot.select_top_status(kvshot.make_select_desc(**d), A, A, A, A, stream=0) == UNSUPPORTED
+
+
 def test_select_pointers():
     d = kvshot.make_select_desc(num_rows=4, row_len=16, keep=4)
     for i in range(4):
@@ -169,7 +177,9 @@ def evict(ptrs=None, **kw):
     (dict(page_size=0), SHAPE), (dict(max_pages_per_seq=0), SHAPE), (dict(num_pages=0), SHAPE), (dict(max_pages_out=0), SHAPE),
     (dict(num_pages_out=0), SHAPE), (dict(max_kept=0), SHAPE), (dict(weights_len=-1), SHAPE), (dict(weights_len_out=-1), SHAPE),
     (dict(num_free=-1), SHAPE), (dict(num_pages=1 << 28), UNSUPPORTED), (dict(num_pages_out=1 << 28), UNSUPPORTED),
-    (dict(head_dim=64), UNSUPPORTED), (dict(page_size=1 << 30), UNSUPPORTED),
+    (dict(head_dim=64), UNSUPPORTED), (dict(page_size=1 << 30), UNSUPPORTED), (dict(max_pages_per_seq=1 << 29), UNSUPPORTED),
+    (dict(max_pages_out=1 << 29), UNSUPPORTED), (dict(max_kept=2 ** 31 - 1), UNSUPPORTED),
+    (dict(weights_len=2 ** 31 - 1), UNSUPPORTED), (dict(weights_len_out=2 ** 31 - 1), UNSUPPORTED),
 ])
 def test_evict_sizes(kw, code):
     assert evict(**kw) == code
