@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "kvshot_partial.cuh"
+#include "kvshot_tcgen05.cuh"
 
 namespace kvshot {
 namespace {
@@ -322,93 +323,170 @@ cudaError_t launch_sparse(const SparseParams& p, int units, int S, cudaStream_t 
 // ------------------------------------------------------------ several query rows
 
 // Nodes of one level pick much the same pages.  Here a CTA takes up to 64 rows (nodes x q heads of the KV head) of a cache, and
-// each page that any of its nodes picked once: by TMA into a ring in shared memory, from where the warps, 8 rows each, take
-// those that a node of theirs picked.  A cluster shares out the pages, by their number; its CTAs' states meet in shared memory.
-//   a window of pages: the nodes' picks as a bit set for each page, then the list of the pages that have any
-//   a ring of stages of 32 keys in groups of 8 (2 KB: dims 0 .. 63, then 64 .. 127, 128-byte swizzled rows); one warp loads
+// each page that any of its nodes picked once, 128 keys to a tile, on tcgen05: keys are the M rows of S^T = K Q^T, so that a
+// thread has one key and knows with one 64-bit word which columns, rows of q, picked its page; dims are the M rows of
+// O^T += V^T P^T, whose accumulator never leaves tensor memory.  The columns' sums stay in the threads' registers, each its own
+// keys' share, to the end.  A cluster shares out the pages, by their number; its CTAs' states meet in shared memory.
+//   a window of pages: the nodes' picks as a set of columns for each page, then the list of the pages that have any
+//   warps 0..7  softmax, a key to a thread: the first four of columns 0 to 31, the others of the rest
+//   warp 8      TMA;  warp 9: MMA, and the owner of tensor memory
+// Two CTAs to an SM, each with one K and one V tile: while one waits for its bytes the other multiplies.
 // The tree's level of 16 x 32K tokens (12 nodes, 128 pages each, 3 to 4 nodes to a page) reads 400 MB so, and not 1.6 GB:
-// 110 us, 162 with a CTA for each node.
-constexpr int kSharedWarps = 8;                      // at most: 8 rows each (and one more warp, which loads)
-constexpr int kWindow = 1024;                        // pages
-constexpr int kStageKeys = 32;
-constexpr int kStageHalf = kStageKeys * kHeadDim * 2;  // K; V is behind it
-constexpr int kStageBytes = 2 * kStageHalf;
-constexpr int kRingStages = 5;
+// 98 us, 162 with a CTA for each node, 110 with mma.sync and eight rows to a warp (five times the instructions).  Of the 98 the
+// list of pages takes 8, the first tile's references 4, the tiles 60 (at 6.5 TB/s), the wait for the cluster's slower CTA and
+// the join 10.  Four softmax warps of 64 columns each in turn were 112, a join by single floats 15 us longer.
+constexpr int kTileKeys128 = 128;
+constexpr int kTileBytes128 = kTileKeys128 * kHeadDim * 2;  // of K, and of V
+constexpr int kColumns = 64;
+constexpr int kWindow = 1024;                      // pages
+constexpr int kSharedThreads = 10 * 32;
+constexpr int kSoftmaxThreads = 128;               // of 32 columns
+constexpr int kPagesEach = (kWindow + kSharedThreads - 1) / kSharedThreads, kPicksEach = 6;
+constexpr int kQEach = (kColumns * 16 + kSharedThreads - 1) / kSharedThreads;
+constexpr int kSharedTmem = 128;                   // columns: O 64, S 64
+constexpr int kTmemS = 64;
 
 struct SharedSpace {
-  uint8_t ring[kRingStages * kStageBytes];           // at the end: the warps' states
-  unsigned long long mask[kWindow], line[kMaxTreeNodes];  // nodes (of this block) by page; by draft slot of a tree
-  unsigned long long list_mask[kWindow];
-  int list_row[kWindow];                             // first row of the page in the pool, KV head included; -1: passed over
-  uint16_t list_live[kWindow];                       // its tokens below the length
-  uint16_t list_page[kWindow];                       // page, from the window's first
-  uint64_t full[kRingStages], empty[kRingStages];
-  int counts[64], parent[kMaxTreeNodes], warp_sum[kSharedWarps + 1];
-  float m[64], l[64];
+  uint8_t k[kTileBytes128], v[kTileBytes128];      // in groups of 8 keys; at the end: the CTA's state
+  uint8_t q[kColumns * 256], p[kTileKeys128 * 128];
+  uint32_t mask[kWindow][2];                       // columns by page of the window; then those of the pages that have any,
+  int list_row[kWindow];                           // and such a page's first row in the pool, KV head included; -1: passed over
+  unsigned long long line[kMaxTreeNodes];          // columns by draft slot of a tree
+  float neg_ref[kColumns], factor[kColumns], m[kColumns], l[kColumns], part_l[4][kColumns];
+  int top[8][32];
+  uint64_t kfull, vfull, sdone, pfull, pvdone, done;
+  int counts[kColumns], parent[kMaxTreeNodes], warp_sum[kSharedThreads / 32], ends;  // ends: the cache's last page is listed
+  uint32_t tmem;
 };
-static_assert(sizeof(float) * 64 * kPartStride <= kRingStages * kStageBytes, "the states fit the ring");
+static_assert(sizeof(float) * kColumns * kPartStride <= 2 * kTileBytes128, "the state fits the tiles' place");
+static_assert(2 * (sizeof(SharedSpace) + 1024) <= 228 * 1024, "two CTAs to an SM");
 
 struct SharedParams {
   SparseParams s;
-  int nodes_per_block, log_gp;
-  int box_keys;         // keys of a box: a page, or 32 keys of one
-  uint32_t by_page;     // ceil(2^32 / groups of a page)
+  int nodes_per_block, cols;  // cols: the block's rows rounded up to 16
+  int box_keys;               // keys of a box: a page, or 64 keys of one
+  uint32_t by_page;           // ceil(2^32 / groups of a page)
   uint32_t wait_ns;
 };
 struct SharedMaps {
   CUtensorMap k, v, dk, dv;
 };
 
-// Offset in a stage's K or V of 16-byte piece `piece` of key `row`.
-__device__ __forceinline__ uint32_t stage_off(int row, int piece) {
-  return static_cast<uint32_t>((row >> 3) * kGroupBytes + (piece >> 3) * kGroupHalfBytes + (row & 7) * 128 +
-                               (((piece & 7) ^ (row & 7)) << 4));
+// Whether x holds in any of the softmax threads of one half of the columns: one barrier of theirs.
+__device__ __forceinline__ bool any_softmax(int barrier, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred in, out;\n\tsetp.ne.u32 in, %1, 0;\n\tbar.red.or.pred out, %3, %2, in;\n\tselp.u32 %0, 1, 0, out;\n\t}"
+      : "=r"(r) : "r"(static_cast<uint32_t>(x)), "n"(kSoftmaxThreads), "r"(barrier) : "memory");
+  return r != 0;
+}
+// Floats as integers of the same order.
+__device__ __forceinline__ int ordered(float x) {
+  const int i = __float_as_int(x);
+  return i >= 0 ? i : i ^ 0x7fffffff;
+}
+__device__ __forceinline__ float unordered(int i) { return __int_as_float(i >= 0 ? i : i ^ 0x7fffffff); }
+
+__device__ __forceinline__ void wait_columns(uint32_t (&v)[32]) {  // nothing computed from v moves before the wait
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+                 "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]),
+                 "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
+                 "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
 }
 
-// kConsumers: the most warps that multiply (two CTAs to an SM: 144 registers with 6 of them, 112 with 8).
-template <int kConsumers>
-__global__ void __launch_bounds__((kConsumers + 1) * 32, 2)
+__global__ void __launch_bounds__(kSharedThreads, 2)
     sparse_shared_kernel(const __grid_constant__ SharedParams sp, const __grid_constant__ SharedMaps maps) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   SharedSpace& sm = *reinterpret_cast<SharedSpace*>(smem_raw);
   const SparseParams& p = sp.s;
   const int S = static_cast<int>(cluster_size()), rank = blockIdx.x % S;
   const int h = blockIdx.x / S % p.v.hkv, c = blockIdx.x / S / p.v.hkv;
-  const int n0 = blockIdx.y * sp.nodes_per_block, nodes = min(sp.nodes_per_block, p.Nq - n0);
-  const int gp = 1 << sp.log_gp, threads = blockDim.x, consumers = threads / 32 - 1;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int n0 = blockIdx.y * sp.nodes_per_block, nodes = min(sp.nodes_per_block, p.Nq - n0), rows = nodes * p.G;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int L = clamped_len(p.v, c), P = p.v.P;
   const uint64_t limit = sp.wait_ns;
   int32_t* err = p.v.err;
+  if ((smem_addr(smem_raw) & 1023u) != 0) {  // (the swizzled tiles' layout counts on it; dynamic shared memory is, alone)
+    set_error(err, KVSHOT_ERR_CUDA);
+    return;
+  }
 
   if (tid == 0) {
-    for (int i = 0; i < kRingStages; ++i) {
-      mbar_init(smem_addr(&sm.full[i]), 1);
-      mbar_init(smem_addr(&sm.empty[i]), consumers);
-    }
+    mbar_init(smem_addr(&sm.kfull), 1);
+    mbar_init(smem_addr(&sm.vfull), 1);
+    mbar_init(smem_addr(&sm.sdone), 1);
+    mbar_init(smem_addr(&sm.pfull), sp.cols > 32 ? 8 : 4);
+    mbar_init(smem_addr(&sm.pvdone), 1);
+    mbar_init(smem_addr(&sm.done), 1);
     fence_mbar_init();
     prefetch_tensormap(&maps.k);
     prefetch_tensormap(&maps.v);
   }
-  // The nodes' counts, and of a tree the lines of ancestors as bits of the draft slots.
+  if (warp == 9) {
+    tc::tmem_alloc(smem_addr(&sm.tmem), kSharedTmem);
+    tc::tmem_relinquish();
+  }
+  const int pages = (L + P - 1) / P, groups_per_page = P / 8, total = nodes * p.max_picks;
+  const int page0 = static_cast<int>(static_cast<int64_t>(pages) * rank / S);
+  const int page1 = static_cast<int>(static_cast<int64_t>(pages) * (rank + 1) / S);
+  const int32_t* picks = p.picks + ((static_cast<size_t>(c) * p.Nq + n0) * p.v.hkv + h) * p.max_picks;
+  const size_t list_stride = static_cast<size_t>(p.v.hkv) * p.max_picks;
+  // A window's page ids, consecutive ones to a thread, and the first of the picks: on their way together.
+  int pick[kPicksEach], before[kPicksEach], id[kPagesEach];
+  auto fetch_picks = [&](int i0) {
+#pragma unroll
+    for (int x = 0; x < kPicksEach; ++x) {
+      const int i = i0 + x * kSharedThreads, node = i / p.max_picks, at = i - node * p.max_picks;
+      pick[x] = i < total ? __ldg(picks + node * list_stride + at) : -2;
+      before[x] = i < total && at > 0 ? __ldg(picks + node * list_stride + at - 1) : -1;
+    }
+  };
+  auto fetch = [&](int w0) {
+#pragma unroll
+    for (int x = 0; x < kPagesEach; ++x) {
+      const int page = w0 + tid * kPagesEach + x;
+      id[x] = page >= page1 ? -1 : p.v.page_table == nullptr ? c : __ldg(p.v.page_table + static_cast<size_t>(c) * p.v.max_pages + page);
+    }
+    fetch_picks(tid);
+  };
+  fetch(page0);
+  // The nodes' counts, and of a tree the lines of ancestors as columns of the draft slots.
+  const unsigned long long node_columns = (1ull << p.G) - 1;  // of node 0
+  const unsigned long long all_columns = rows < 64 ? (1ull << rows) - 1 : ~0ull;
+  if (tid < kColumns) sm.neg_ref[tid] = INFINITY;  // (no reference yet)
+  // q as the B operand: rows of 64 dims, 128-byte swizzled, the first half of the dims of all rows, then the second.
+  int count = tid < nodes ? __ldg(p.counts + (static_cast<size_t>(c) * p.Nq + n0 + tid) * p.v.hkv + h) : 0;
+  uint4 qx[kQEach];
+#pragma unroll
+  for (int x = 0; x < kQEach; ++x) {
+    const int i = tid + x * kSharedThreads, r = i / 16, node = r / p.G;
+    qx[x] = r < rows ? __ldg(p.q + ((static_cast<size_t>(c) * p.Nq + n0 + node) * p.hq + h * p.G + (r - node * p.G)) * 16 + i % 16)
+                     : make_uint4(0, 0, 0, 0);
+  }
   if (tid < nodes) {
-    int count = p.counts[(static_cast<size_t>(c) * p.Nq + n0 + tid) * p.v.hkv + h];
     if (count < 0 || count > p.max_picks) {
       set_error(err, KVSHOT_ERR_DEVICE_BOUNDS);
       count = min(max(count, 0), p.max_picks);
     }
     sm.counts[tid] = count;
   }
+#pragma unroll
+  for (int x = 0; x < kQEach; ++x) {
+    const int i = tid + x * kSharedThreads, r = i / 16, piece = i % 16;
+    if (r < sp.cols) *reinterpret_cast<uint4*>(sm.q + (piece >> 3) * (sp.cols * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = qx[x];
+  }
+  fence_proxy_async_smem();
   const bool draft = rank == S - 1, tree = p.tree_parent != nullptr;
   if (draft && tree) {
-    for (int i = tid; i < p.N; i += threads) {
+    for (int i = tid; i < p.N; i += kSharedThreads) {
       sm.parent[i] = p.tree_parent[static_cast<size_t>(c / p.per_seq) * p.N + i];
       sm.line[i] = 0;
     }
     __syncthreads();
     if (tid < nodes) {
       for (int at = p.N - p.Nq + n0 + tid; at >= 0;) {
-        atomicOr(&sm.line[at], 1ull << tid);
+        atomicOr(&sm.line[at], node_columns << (tid * p.G));
         const int up = sm.parent[at];
         if (up < -1 || up >= at) {
           set_error(err, KVSHOT_ERR_TREE);
@@ -418,194 +496,197 @@ __global__ void __launch_bounds__((kConsumers + 1) * 32, 2)
       }
     }
   }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = sm.tmem, quarter = static_cast<uint32_t>(warp & 3) << 21;
 
-  // A consumer's rows: columns 2 t, 2 t + 1 of its products, and column g's q.
-  uint32_t q[8][2];
-  {
-    const int r = warp * 8 + g, node = r >> sp.log_gp, j = r & (gp - 1);
-    const bool live = node < nodes && j < p.G;
-    const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q) + ((static_cast<size_t>(c) * p.Nq + n0 + node) * p.hq + h * p.G + j) * 64 + t;
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-      q[ks][0] = live ? __ldg(src + 8 * ks) : 0;
-      q[ks][1] = live ? __ldg(src + 8 * ks + 4) : 0;
-    }
-  }
-  // Nodes of the warp's rows: node0 and up to 7 more, of which columns 2 t and 2 t + 1 are the bits bit[0] and bit[1].
-  const int node0 = warp * 8 >> sp.log_gp;
-  uint32_t bit[2], tile_nodes = 0;
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const int node = (warp * 8 + 2 * t + e) >> sp.log_gp;
-    bit[e] = node < nodes ? 1u << (node - node0) : 0;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int node = (warp * 8 + i) >> sp.log_gp;
-    if (node < nodes) tile_nodes |= 1u << (node - node0);
-  }
-  // Offsets of this lane's rows for ldmatrix: K by pairs of pieces of a half, V transposed alike.
-  uint32_t koff[4], voff[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    koff[i] = stage_off(lane & 15, 2 * i + (lane >> 4));
-    voff[i] = kStageHalf + stage_off((lane & 7) + ((lane >> 4) << 3), 2 * i + ((lane >> 3) & 1));
-  }
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[8][4];
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
-
-  // S^T = K Q^T of 16 keys from `base` on; see: the tile's nodes that see keys g and g + 8.
-  auto scores = [&](uint32_t base, uint32_t see0, uint32_t see1, float (&s)[4]) {
-    float d[2][4] = {};
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-      uint32_t a[4];
-      ldmatrix_x4(base + koff[ks & 3] + (ks >> 2) * kGroupHalfBytes, a[0], a[1], a[2], a[3]);
-      mma_bf16_16816(d[ks & 1], a, q[ks][0], q[ks][1]);
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      s[e] = ((e < 2 ? see0 : see1) & bit[e & 1]) != 0 ? (d[0][e] + d[1][e]) * p.qscale : -INFINITY;
-  };
-  // O^T += V^T P^T; mask: which of this lane's keys (2 t, 2 t + 1 of each group) are tokens: of others V may hold anything.
-  auto values = [&](uint32_t base, uint32_t p0, uint32_t p1, bool whole, uint32_t mask0, uint32_t mask1) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      uint32_t a[4];
-      ldmatrix_x4_trans(base + voff[i & 3] + (i >> 2) * kGroupHalfBytes, a[0], a[1], a[2], a[3]);
-      if (!whole) {
-        a[0] &= mask0;
-        a[1] &= mask0;
-        a[2] &= mask1;
-        a[3] &= mask1;
-      }
-      mma_bf16_16816(o[i], a, p0, p1);
-    }
-  };
-  auto raise = [&](float top0, float top1) {  // the reference, when a score is more than 2^8 above it
-    if (!__any_sync(0xffffffffu, top0 > m[0] + 8.f || top1 > m[1] + 8.f)) return;
-    float top[2] = {top0, top1};
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-#pragma unroll
-      for (int x = 4; x < 32; x <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], x));
-      const float now = fmaxf(m[e], top[e]);
-      const float f = now == -INFINITY ? 1.f : ex2(m[e] - now);
-      m[e] = now;
-      l[e] *= f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        o[i][e] *= f;
-        o[i][2 + e] *= f;
-      }
-    }
-  };
-  auto weigh = [&](float (&s)[4], uint32_t* p0, uint32_t* p1) {
-    const float m0 = m[0] == -INFINITY ? 0.f : m[0], m1 = m[1] == -INFINITY ? 0.f : m[1];
-    s[0] = ex2(s[0] - m0);
-    s[1] = ex2(s[1] - m1);
-    s[2] = ex2(s[2] - m0);
-    s[3] = ex2(s[3] - m1);
-    l[0] += s[0] + s[2];
-    l[1] += s[1] + s[3];
-    *p0 = transpose8x8(pack_bf16x2(s[0], s[1]));
-    *p1 = transpose8x8(pack_bf16x2(s[2], s[3]));
-  };
-  // A stage.  Lane x < 4 knows of group x its tokens (none below 1, 8 or more: all); see[i]: the tile's nodes that see key g of
-  // group i.
-  auto consume = [&](uint32_t base, int lane_live, const uint32_t (&see)[4]) {
-    const bool both0 = __any_sync(0xffffffffu, ((see[0] | see[1]) & tile_nodes) != 0);
-    const bool both1 = __any_sync(0xffffffffu, ((see[2] | see[3]) & tile_nodes) != 0);
-    if (!both0 && !both1) return;
-    const bool whole = __all_sync(0xffffffffu, lane >= 4 || lane_live >= 8);
-    uint32_t mask[4] = {};
-    if (!whole)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int live = __shfl_sync(0xffffffffu, lane_live, i);
-        mask[i] = (2 * t < live ? 0xffffu : 0u) | (2 * t + 1 < live ? 0xffff0000u : 0u);
-      }
-    constexpr uint32_t kSecond = 2 * kGroupBytes;  // the stage's keys 16 .. 31
-    uint32_t p0, p1;
-    if (both0 && both1) {
-      float s[4], s2[4];
-      scores(base, see[0], see[1], s);
-      scores(base + kSecond, see[2], see[3], s2);
-      raise(max3(fmaxf(s[0], s[2]), s2[0], s2[2]), max3(fmaxf(s[1], s[3]), s2[1], s2[3]));
-      uint32_t p2, p3;
-      weigh(s, &p0, &p1);
-      weigh(s2, &p2, &p3);
-      values(base, p0, p1, whole, mask[0], mask[1]);
-      values(base + kSecond, p2, p3, whole, mask[2], mask[3]);
-    } else {
-      float s[4];
-      const uint32_t from = both0 ? base : base + kSecond;
-      scores(from, both0 ? see[0] : see[2], both0 ? see[1] : see[3], s);
-      raise(fmaxf(s[0], s[2]), fmaxf(s[1], s[3]));
-      weigh(s, &p0, &p1);
-      values(from, p0, p1, whole, both0 ? mask[0] : mask[2], both0 ? mask[1] : mask[3]);
-    }
-  };
-
-  uint32_t filled = 0;  // stages so far, the same in all warps
+  const int half = warp >> 2;  // of the columns, in the softmax warps
+  float2 sums[16] = {};        // of the softmax threads: their keys' shares of the columns'
+  int done = 0;  // tiles so far, the same in all warps while nothing fails
+  int k_issued = 0, v_issued = 0;
   bool ok = true;
-  // `stages` stages through the ring: load(stage, base, bar) issues a stage's copies and returns its bytes (the whole loading warp;
-  // it announces them first), use(stage, base).
-  auto stream = [&](int stages, auto load, auto use) {
-    for (int st = 0; ok && st < stages; ++st, ++filled) {
-      const uint32_t slot = filled % kRingStages, round = filled / kRingStages;
-      const uint32_t base = smem_addr(sm.ring) + slot * kStageBytes;
-      if (warp == consumers) {
-        if (round > 0) ok = __all_sync(0xffffffffu, wait(smem_addr(&sm.empty[slot]), (round - 1) & 1, err, limit));
+  // `tiles` tiles through the two products.  load(tile, kdst, vdst, kbar or vbar, which) issues a tile's copies (the whole loading
+  // warp, which announces their bytes first); columns(tile, key, half, &live) which of the half's
+  // columns see this key, and whether it is a token.
+  auto stream = [&](int tiles, auto load, auto columns) {
+    if (warp == 8) {
+      for (int t = 0; ok && t < tiles; ++t, ++done) {
+        if (done > 0) ok = __all_sync(0xffffffffu, wait(smem_addr(&sm.sdone), (done - 1) & 1, err, limit));
         if (!ok) break;
-        load(st, base, smem_addr(&sm.full[slot]));
-      } else {
-        ok = __all_sync(0xffffffffu, wait(smem_addr(&sm.full[slot]), round & 1, err, limit));
+        load(t, false, smem_addr(sm.k), smem_addr(&sm.kfull));
+        ++k_issued;
+        if (done > 0) ok = __all_sync(0xffffffffu, wait(smem_addr(&sm.pvdone), (done - 1) & 1, err, limit));
         if (!ok) break;
-        use(st, base);
+        load(t, true, smem_addr(sm.v), smem_addr(&sm.vfull));
+        ++v_issued;
+      }
+    } else if (warp == 9) {
+      const uint32_t idesc_s = tc::idesc_bf16(128, sp.cols, false);
+      const uint32_t idesc_o = tc::idesc_bf16(128, sp.cols, true) | 1u << 15;  // V^T: A is MN-major too
+      const uint32_t k = smem_addr(sm.k), v = smem_addr(sm.v), q = smem_addr(sm.q), pb = smem_addr(sm.p);
+      for (int t = 0; ok && t < tiles; ++t, ++done) {
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&sm.kfull), done & 1, err, limit));
+        if (!ok) break;
+        tc::tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+          tc::tc_mma_elect(tmem + kTmemS, tc::smem_desc_sw128(k + (ks >> 2) * kGroupHalfBytes + (ks & 3) * 32, 16, kGroupBytes),
+                           tc::smem_desc_sw128(q + (ks >> 2) * (sp.cols * 128) + (ks & 3) * 32, 16, 1024), idesc_s, ks > 0);
+        tc::tc_commit_elect(smem_addr(&sm.sdone));
+        ok = wait(smem_addr(&sm.vfull), done & 1, err, limit);
+        ok = ok && wait(smem_addr(&sm.pfull), done & 1, err, limit);  // (S has been read by then)
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc::tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)  // 16 keys: two groups
+          tc::tc_mma_elect(tmem, tc::smem_desc_sw128(v + ks * 2 * kGroupBytes, kGroupHalfBytes, kGroupBytes),
+                           tc::smem_desc_sw128(pb + ks * 2048, 16, 1024), idesc_o, done > 0 || ks > 0);
+        tc::tc_commit_elect(smem_addr(&sm.pvdone));
+      }
+    } else {
+      const uint32_t s_at = tmem + quarter + kTmemS + 32 * half;
+      const int barrier = 1 + half, key = tid & 127;
+      float* neg_ref = sm.neg_ref + 32 * half;
+      float* factor = sm.factor + 32 * half;
+      if (32 * half >= sp.cols) {  // nothing to do
+        done += tiles;
+        tiles = 0;
+      }
+      for (int t = 0; ok && t < tiles; ++t, ++done) {
+        bool live;
+        const uint32_t see = columns(t, key, half, &live);
+        ok = wait(smem_addr(&sm.sdone), done & 1, err, limit);
+        if (done > 0) ok = ok && wait(smem_addr(&sm.pvdone), (done - 1) & 1, err, limit);  // (P's place is free, O at rest)
+        if (!live && ok && half == 0) {
+          // V of what is no token may hold anything, and a NaN times P's 0 is one: zeros.
+          ok = wait(smem_addr(&sm.vfull), done & 1, err, limit);
+          uint4* row = reinterpret_cast<uint4*>(sm.v + (key >> 3) * kGroupBytes + (key & 7) * 128);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) row[i] = row[i + kGroupHalfBytes / 16] = make_uint4(0, 0, 0, 0);
+        }
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_addr(&sm.empty[slot]));
+        tc::tc_fence_after();
+        uint32_t x[32];
+        float top = -INFINITY;
+        auto refer = [&] {  // scores less the reference, where the key is seen
+          tc::tmem_ld32(s_at, x);
+          wait_columns(x);
+          const float2 qs = make_float2(p.qscale, p.qscale);
+          top = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 r = *reinterpret_cast<const float4*>(neg_ref + i);
+            const float2 a = fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), qs, make_float2(r.x, r.y));
+            const float2 b = fma2(make_float2(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3])), qs, make_float2(r.z, r.w));
+            const float y0 = see >> i & 1 ? a.x : -INFINITY, y1 = see >> (i + 1) & 1 ? a.y : -INFINITY;
+            const float y2 = see >> (i + 2) & 1 ? b.x : -INFINITY, y3 = see >> (i + 3) & 1 ? b.y : -INFINITY;
+            top = max3(top, y0, y1);
+            top = max3(top, y2, y3);
+            x[i] = __float_as_uint(y0);
+            x[i + 1] = __float_as_uint(y1);
+            x[i + 2] = __float_as_uint(y2);
+            x[i + 3] = __float_as_uint(y3);
+          }
+        };
+        // References move only when a score is more than 2^8 above its column's (or the column has none): P stays in range.
+        bool moved = false;
+        for (;;) {
+          refer();
+          if (moved || !any_softmax(barrier, !ok || top > 8.f)) break;
+          if (any_softmax(barrier, !ok)) {
+            ok = false;
+            break;
+          }
+          moved = true;
+          tc::tmem_ld32(s_at, x);
+          wait_columns(x);
+          int mine = 0;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const int best = __reduce_max_sync(0xffffffffu, ordered(see >> i & 1 ? __uint_as_float(x[i]) * p.qscale : -INFINITY));
+            if (lane == i) mine = best;
+          }
+          sm.top[warp][lane] = mine;
+          named_barrier_sync(barrier, kSoftmaxThreads);
+          if (key < 32) {
+            const int(*tops)[32] = sm.top + 4 * half;
+            const float best = unordered(max(max(tops[0][key], tops[1][key]), max(tops[2][key], tops[3][key])));
+            const float old = -neg_ref[key], now = fmaxf(old, best);
+            factor[key] = now == -INFINITY ? 1.f : ex2(old - now);
+            neg_ref[key] = -now;
+          }
+          named_barrier_sync(barrier, kSoftmaxThreads);
+          if (done > 0) {
+            tc::tmem_ld32(tmem + quarter + 32 * half, x);
+            wait_columns(x);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * factor[i]);
+            tc::tmem_st32(tmem + quarter + 32 * half, x);
+            tc::tmem_wait_st();
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            sums[i].x *= factor[2 * i];
+            sums[i].y *= factor[2 * i + 1];
+          }
+        }
+        if (!ok) break;
+        // P, rounded to bf16 as the second product takes it; the sums are of what it was before.
+        uint4* prow = reinterpret_cast<uint4*>(sm.p + key * 128);
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 y = make_float2(ex2(__uint_as_float(x[i + 2 * e])), ex2(__uint_as_float(x[i + 2 * e + 1])));
+            sums[i / 2 + e] = add2(sums[i / 2 + e], y);
+            w[e] = pack_bf16x2(y.x, y.y);
+          }
+          prow[(4 * half + i / 8) ^ (key & 7)] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        fence_proxy_async_smem();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&sm.pfull));
       }
     }
   };
 
-  const int pages = (L + P - 1) / P, groups_per_page = P / 8;
-  const int page0 = static_cast<int>(static_cast<int64_t>(pages) * rank / S);
-  const int page1 = static_cast<int>(static_cast<int64_t>(pages) * (rank + 1) / S);
-  const int32_t* picks = p.picks + ((static_cast<size_t>(c) * p.Nq + n0) * p.v.hkv + h) * p.max_picks;
-  const size_t list_stride = static_cast<size_t>(p.v.hkv) * p.max_picks;
   // (Every CTA of the cluster has a window at least, in which it checks all picks.)
   for (int w0 = page0; w0 < page1 || w0 == page0; w0 += kWindow) {
     const int w1 = min(page1, w0 + kWindow);
+    if (w0 > page0) fetch(w0);
+    __syncthreads();  // (the list is no longer read)
+    for (int i = tid; i < w1 - w0; i += kSharedThreads) sm.mask[i][0] = sm.mask[i][1] = 0;
+    if (tid == 0) sm.ends = 0;
     __syncthreads();
-    for (int i = tid; i < w1 - w0; i += threads) sm.mask[i] = 0;
-    __syncthreads();
-    const int total = nodes * p.max_picks;
-    for (int i0 = tid; i0 < total; i0 += 8 * threads) {
-      int pick[8], before[8];
+    for (int i0 = tid; i0 < total; i0 += kPicksEach * kSharedThreads) {
+      if (i0 > tid) fetch_picks(i0);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const int i = i0 + x * threads, node = i / p.max_picks, at = i - node * p.max_picks;
-        const bool live = i < total && at < sm.counts[node];
-        pick[x] = live ? __ldg(picks + node * list_stride + at) : -2;
-        before[x] = live && at > 0 ? __ldg(picks + node * list_stride + at - 1) : -1;
-      }
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const int i = i0 + x * threads, node = i / p.max_picks, at = i - node * p.max_picks;
+      for (int x = 0; x < kPicksEach; ++x) {
+        const int i = i0 + x * kSharedThreads, node = i / p.max_picks, at = i - node * p.max_picks;
         if (i >= total || at >= sm.counts[node]) continue;
-        if (pick[x] >= w0 && pick[x] < w1 && pick[x] > before[x]) atomicOr(&sm.mask[pick[x] - w0], 1ull << node);
-        else if (pick[x] < 0 || pick[x] >= pages || pick[x] <= before[x]) set_error(err, KVSHOT_ERR_DEVICE_BOUNDS);
+        if (pick[x] >= w0 && pick[x] < w1 && pick[x] > before[x]) {
+          const unsigned long long columns = node_columns << (node * p.G);
+          if (static_cast<uint32_t>(columns) != 0) atomicOr(&sm.mask[pick[x] - w0][0], static_cast<uint32_t>(columns));
+          if (columns >> 32 != 0) atomicOr(&sm.mask[pick[x] - w0][1], static_cast<uint32_t>(columns >> 32));
+        } else if (pick[x] < 0 || pick[x] >= pages || pick[x] <= before[x]) {
+          set_error(err, KVSHOT_ERR_DEVICE_BOUNDS);
+        }
       }
     }
     __syncthreads();
     // The pages that some node picked, in order.
-    const int per = (w1 - w0 + threads - 1) / threads;
+    uint2 mask[kPagesEach];
     int mine = 0;
-    for (int i = tid * per; i < min(w1 - w0, tid * per + per); ++i) mine += sm.mask[i] != 0;
+#pragma unroll
+    for (int x = 0; x < kPagesEach; ++x) {
+      const int i = tid * kPagesEach + x;
+      mask[x] = i < w1 - w0 ? *reinterpret_cast<const uint2*>(sm.mask[i]) : make_uint2(0, 0);
+      mine += (mask[x].x | mask[x].y) != 0;
+    }
     int scan = mine;
 #pragma unroll
     for (int x = 1; x < 32; x <<= 1) {
@@ -615,130 +696,153 @@ __global__ void __launch_bounds__((kConsumers + 1) * 32, 2)
     if (lane == 31) sm.warp_sum[warp] = scan;
     __syncthreads();
     int at = scan - mine, listed = 0;
-    for (int x = 0; x <= consumers; ++x) {
+#pragma unroll
+    for (int x = 0; x < kSharedThreads / 32; ++x) {
       if (x < warp) at += sm.warp_sum[x];
       listed += sm.warp_sum[x];
     }
-    for (int i = tid * per; i < min(w1 - w0, tid * per + per); ++i)
-      if (sm.mask[i] != 0) {
-        sm.list_page[at] = static_cast<uint16_t>(i);
-        sm.list_mask[at++] = sm.mask[i];
+#pragma unroll
+    for (int x = 0; x < kPagesEach; ++x)
+      if ((mask[x].x | mask[x].y) != 0) {
+        const bool bad = static_cast<unsigned>(id[x]) >= static_cast<unsigned>(p.v.num_pages);
+        if (bad) set_error(err, KVSHOT_ERR_DEVICE_BOUNDS);
+        sm.list_row[at] = bad ? -1 : (id[x] * p.v.hkv + h) * P;
+        *reinterpret_cast<uint2*>(sm.mask[at++]) = mask[x];
+        if (w0 + tid * kPagesEach + x == pages - 1) sm.ends = 1;
       }
     __syncthreads();
-    for (int i = tid; i < listed; i += threads) {
-      const int page = w0 + sm.list_page[i], id = page_id(p.v, c, page);
-      sm.list_row[i] = id >= 0 ? (id * p.v.hkv + h) * P : -1;
-      sm.list_live[i] = static_cast<uint16_t>(id >= 0 ? min(P, L - page * P) : 0);
-    }
-    __syncthreads();
+    const int last = listed - 1;  // in whose page the cache may end
+    const int last_live = w1 == pages && sm.ends != 0 ? L - (pages - 1) * P : P;
     // Group i (8 keys of one page): the page's place in the list, and its first key there.
     const uint32_t groups = listed * groups_per_page;
     auto page_of = [&](uint32_t i) { return groups_per_page == 1 ? i : __umulhi(i, sp.by_page); };
-    const int box_groups = sp.box_keys / 8, boxes = kStageKeys / sp.box_keys;
-    stream(static_cast<int>(groups * 8 + kStageKeys - 1) / kStageKeys,
-           [&](int st, uint32_t base, uint32_t bar) {
-             const uint32_t i = st * (kStageKeys / 8) + lane * box_groups, page = page_of(min(i, groups));
+    const int box_groups = sp.box_keys / 8, boxes = kTileKeys128 / sp.box_keys;
+    stream(static_cast<int>(groups * 8 + kTileKeys128 - 1) / kTileKeys128,
+           [&](int t, bool values, uint32_t base, uint32_t bar) {
+             const uint32_t i = t * (kTileKeys128 / 8) + lane * box_groups;
              int row = -1;
-             if (lane < boxes && i < groups && sm.list_row[page] >= 0) row = sm.list_row[page] + (i - page * groups_per_page) * 8;
-             const int live = __popc(__ballot_sync(0xffffffffu, row >= 0));
-             if (lane == 0) mbar_arrive_expect_tx(bar, live * sp.box_keys * 512);
-             __syncwarp();
-             if (row >= 0) {
-               const uint32_t dst = base + lane * sp.box_keys * 256;
-               tma_load_4d(dst, &maps.k, 0, 0, 0, row >> 3, bar);
-               tma_load_4d(dst + kStageHalf, &maps.v, 0, 0, 0, row >> 3, bar);
-             }
-           },
-           [&](int st, uint32_t base) {
-             int live = 0;
-             uint32_t nodes_of = 0;
-             const uint32_t i = st * (kStageKeys / 8) + lane;
-             if (lane < 4 && i < groups) {
+             if (lane < boxes && i < groups) {
                const uint32_t page = page_of(i);
-               live = sm.list_live[page] - static_cast<int>(i - page * groups_per_page) * 8;
-               nodes_of = static_cast<uint32_t>(sm.list_mask[page] >> node0) & 0xffu;
+               if (sm.list_row[page] >= 0) row = sm.list_row[page] + (i - page * groups_per_page) * 8;
              }
-             uint32_t see[4];
-#pragma unroll
-             for (int x = 0; x < 4; ++x) {
-               const uint32_t both = __shfl_sync(0xffffffffu, nodes_of | static_cast<uint32_t>(min(max(live, 0), 8)) << 8, x);
-               see[x] = g < static_cast<int>(both >> 8) ? both & 0xffu : 0u;
-             }
-             consume(base, live, see);
+             const int live = __popc(__ballot_sync(0xffffffffu, row >= 0));
+             if (lane == 0) mbar_arrive_expect_tx(bar, live * sp.box_keys * 256);
+             __syncwarp();
+             if (row >= 0) tma_load_4d(base + lane * sp.box_keys * 256, values ? &maps.v : &maps.k, 0, 0, 0, row >> 3, bar);
+           },
+           [&](int t, int key, int half, bool* live) {
+             const uint32_t i = t * (kTileKeys128 / 8) + (key >> 3);
+             *live = false;
+             if (i >= groups) return 0u;
+             const uint32_t page = page_of(i);
+             const int at = static_cast<int>(i - page * groups_per_page) * 8 + (key & 7);
+             *live = sm.list_row[page] >= 0 && at < (static_cast<int>(page) == last ? last_live : P);
+             return *live ? sm.mask[page][half] : 0u;
            });
   }
 
   if (draft) {  // the nodes themselves and their ancestors
     const int first_row = (c * p.v.hkv + h) * p.n_max, first_node = p.N - p.Nq + n0;
     const int slots = min(p.N, first_node + nodes);  // (no node sees a later one)
-    stream((slots + kStageKeys - 1) / kStageKeys,
-           [&](int st, uint32_t base, uint32_t bar) {
-             const int slot = st * kStageKeys + lane * 8;
-             const bool live = lane < kStageKeys / 8 && slot < slots;
+    stream((slots + kTileKeys128 - 1) / kTileKeys128,
+           [&](int t, bool values, uint32_t base, uint32_t bar) {
+             const int slot = t * kTileKeys128 + lane * 8;
+             const bool live = lane < kTileKeys128 / 8 && slot < slots;
              const int boxes = __popc(__ballot_sync(0xffffffffu, live));
-             if (lane == 0) mbar_arrive_expect_tx(bar, boxes * 2 * kGroupBytes);
+             if (lane == 0) mbar_arrive_expect_tx(bar, boxes * kGroupBytes);
              __syncwarp();
-             if (live) {
-               const uint32_t dst = base + lane * kGroupBytes;
-               tma_load_3d_plain(dst, &maps.dk, 0, first_row + slot, 0, bar);
-               tma_load_3d_plain(dst + kStageHalf, &maps.dv, 0, first_row + slot, 0, bar);
-             }
+             if (live) tma_load_3d_plain(base + lane * kGroupBytes, values ? &maps.dv : &maps.dk, 0, first_row + slot, 0, bar);
            },
-           [&](int st, uint32_t base) {
-             uint32_t see[4];
-#pragma unroll
-             for (int x = 0; x < 4; ++x) {
-               const int slot = st * kStageKeys + 8 * x + g;
-               // A chain's node sees the slots up to its own: nodes from slot - first_node on see this one.
-               const unsigned long long nodes_of = slot >= slots ? 0ull : tree ? sm.line[slot] : ~0ull << max(0, slot - first_node);
-               see[x] = static_cast<uint32_t>(nodes_of >> node0) & 0xffu;
-             }
-             consume(base, slots - st * kStageKeys - 8 * lane, see);
+           [&](int t, int key, int half, bool* live) {
+             const int slot = t * kTileKeys128 + key;
+             *live = slot < slots;
+             // A chain's node sees the slots up to its own: nodes from slot - first_node on see this one.
+             const unsigned long long see =
+                 !*live ? 0ull : tree ? sm.line[slot] : all_columns & ~0ull << (max(0, slot - first_node) * p.G);
+             return static_cast<uint32_t>(see >> (32 * half));
            });
   }
-  if (warp == consumers)  // no copy is in flight when the ring becomes the states' place, or the CTA ends
-    for (uint32_t i = filled > kRingStages ? filled - kRingStages : 0; i < filled; ++i)
-      mbar_wait(smem_addr(&sm.full[i % kRingStages]), (i / kRingStages) & 1, err);
+  // Every product has completed, and every copy landed, when the tiles' place becomes the state's.
+  if (warp == 9) {
+    tc::tc_commit_elect(smem_addr(&sm.done));
+    mbar_wait(smem_addr(&sm.done), 0, err);
+  }
+  if (warp == 8) {
+    if (k_issued > 0) mbar_wait(smem_addr(&sm.kfull), (k_issued - 1) & 1, err);
+    if (v_issued > 0) mbar_wait(smem_addr(&sm.vfull), (v_issued - 1) & 1, err);
+  }
+  tc::tc_fence_before();
   __syncthreads();
-
-  // The CTAs' states joined.
-  float* part = reinterpret_cast<float*>(sm.ring);  // [64 rows][kPartStride]
-  if (warp < consumers) {
+  tc::tc_fence_after();
+  float* part = reinterpret_cast<float*>(sm.k);  // [64 rows][kPartStride]
+  if (warp < 8) {
+    uint32_t o[32];
+    if (done > 0 && 32 * half < sp.cols) {
+      tc::tmem_ld32(tmem + quarter + 32 * half, o);
+      wait_columns(o);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float sum = l[e];
+      for (int i = 0; i < 32; ++i) o[i] = 0;
+    }
 #pragma unroll
-      for (int x = 4; x < 32; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-      const int r = warp * 8 + 2 * t + e;
-      if (g == 0) {
-        sm.m[r] = m[e];
-        sm.l[r] = sum;
-      }
+    for (int i = 0; i < 32; ++i) part[(32 * half + i) * kPartStride + (tid & 127)] = __uint_as_float(o[i]);
+    tc::tc_fence_before();
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        part[r * kPartStride + 16 * i + g] = o[i][e];
-        part[r * kPartStride + 16 * i + g + 8] = o[i][2 + e];
-      }
+    for (int i = 0; i < 16; ++i) {
+      float2 x = sums[i];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) x = add2(x, make_float2(__shfl_xor_sync(0xffffffffu, x.x, o), __shfl_xor_sync(0xffffffffu, x.y, o)));
+      if (lane == i) *reinterpret_cast<float2*>(&sm.part_l[warp & 3][32 * half + 2 * i]) = x;
+    }
+    named_barrier_sync(1 + half, kSoftmaxThreads);
+    if ((tid & 127) < 32) {
+      const int r = 32 * half + lane;
+      sm.m[r] = -sm.neg_ref[r];
+      sm.l[r] = (sm.part_l[0][r] + sm.part_l[1][r]) + (sm.part_l[2][r] + sm.part_l[3][r]);
     }
   }
+
+  // The CTAs' states joined: a row's weight of each, then the sums of four dims to a thread.
   if (S > 1) cluster_sync_all();
   else __syncthreads();
-  const int rows = nodes << sp.log_gp;
-  for (int i = rank * threads + tid; i < rows * kHeadDim; i += S * threads) {
-    const int r = i / kHeadDim, d = i % kHeadDim, j = r & (gp - 1);
-    if (j >= p.G) continue;
-    float top = -INFINITY;
-    for (int x = 0; x < S; ++x) top = fmaxf(top, remote_float(smem_addr(&sm.m[r]), x));
-    float sum = 0.f, out = 0.f;
+  if (warp == 9) {
+    tc::tc_fence_after();
+    tc::tmem_dealloc(tmem, kSharedTmem);
+  }
+  float(*weight)[kColumns] = reinterpret_cast<float(*)[kColumns]>(sm.p);  // [S]
+  if (tid < rows) {
+    float top = -INFINITY, sum = 0.f;
+    for (int x = 0; x < S; ++x) top = fmaxf(top, remote_float(smem_addr(&sm.m[tid]), x));
     for (int x = 0; x < S; ++x) {
-      const float mx = remote_float(smem_addr(&sm.m[r]), x);
-      const float f = mx == -INFINITY ? 0.f : ex2(mx - top);
-      sum += f * remote_float(smem_addr(&sm.l[r]), x);
-      out += f * remote_float(smem_addr(part + r * kPartStride + d), x);
+      const float mx = remote_float(smem_addr(&sm.m[tid]), x), f = mx == -INFINITY ? 0.f : ex2(mx - top);
+      weight[x][tid] = f;
+      sum += f * remote_float(smem_addr(&sm.l[tid]), x);
     }
-    const size_t row = (static_cast<size_t>(c) * p.Nq + n0 + (r >> sp.log_gp)) * p.hq + h * p.G + j;
-    p.out[row * kHeadDim + d] = __float2bfloat16_rn(out / sum);
-    if (d == 0) p.lse[row] = (top + log2f(sum)) * 0.6931471805599453f;
+    sm.factor[tid] = sum;
+    if (tid % S == rank) {
+      const int node = tid / p.G;
+      p.lse[(static_cast<size_t>(c) * p.Nq + n0 + node) * p.hq + h * p.G + (tid - node * p.G)] =
+          (top + log2f(sum)) * 0.6931471805599453f;
+    }
+  }
+  __syncthreads();
+  for (int i = rank * kSharedThreads + tid; i < rows * (kHeadDim / 4); i += S * kSharedThreads) {
+    const int r = i / (kHeadDim / 4), d = i % (kHeadDim / 4) * 4, node = r / p.G;
+    const float sum = sm.factor[r];
+    float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (int x = 0; x < S; ++x) {
+      const float f = weight[x][r];
+      if (f == 0.f) continue;
+      const float4 y = remote_float4(smem_addr(part + r * kPartStride + d), x);
+      out.x += f * y.x;
+      out.y += f * y.y;
+      out.z += f * y.z;
+      out.w += f * y.w;
+    }
+    const size_t row = (static_cast<size_t>(c) * p.Nq + n0 + node) * p.hq + h * p.G + (r - node * p.G);
+    *reinterpret_cast<uint2*>(p.out + row * kHeadDim + d) =
+        make_uint2(pack_bf16x2(out.x / sum, out.y / sum), pack_bf16x2(out.z / sum, out.w / sum));
   }
   if (S > 1) cluster_sync_all();  // (another CTA may still read this one's state)
 }
@@ -746,11 +850,10 @@ __global__ void __launch_bounds__((kConsumers + 1) * 32, 2)
 cudaError_t launch_shared(const SparseParams& s, int caches, int S, uint32_t wait_ns, cudaStream_t stream) {
   SharedParams p;
   p.s = s;
-  p.log_gp = 0;
-  while ((1 << p.log_gp) < s.G) ++p.log_gp;
-  const int most = 64 >> p.log_gp, blocks = (s.Nq + most - 1) / most;
+  const int most = kColumns / s.G, blocks = (s.Nq + most - 1) / most;
   p.nodes_per_block = (s.Nq + blocks - 1) / blocks;
-  p.box_keys = std::min(s.v.P, kStageKeys);
+  p.cols = (p.nodes_per_block * s.G + 15) / 16 * 16;
+  p.box_keys = std::min(s.v.P, 64);
   const uint32_t groups = s.v.P / 8;
   p.by_page = groups > 1 ? static_cast<uint32_t>(((uint64_t{1} << 32) + groups - 1) / groups) : 0;
   p.wait_ns = wait_ns;
@@ -760,9 +863,7 @@ cudaError_t launch_shared(const SparseParams& s, int caches, int S, uint32_t wai
   if (!map_groups(&maps.k, s.k, rows, p.box_keys / 8) || !map_groups(&maps.v, s.val, rows, p.box_keys / 8) ||
       !map_any_8(&maps.dk, s.dk, drows) || !map_any_8(&maps.dv, s.dv, drows))
     return cudaErrorInvalidValue;
-  const int warps = ((p.nodes_per_block << p.log_gp) + 7) / 8 + 1;
-  auto* kernel = warps <= 7 ? sparse_shared_kernel<6> : sparse_shared_kernel<kSharedWarps>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SharedSpace));
+  cudaError_t e = cudaFuncSetAttribute(sparse_shared_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SharedSpace));
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -770,12 +871,12 @@ cudaError_t launch_shared(const SparseParams& s, int caches, int S, uint32_t wai
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(caches * s.v.hkv * S, blocks);
-  cfg.blockDim = dim3(warps * 32);
+  cfg.blockDim = dim3(kSharedThreads);
   cfg.dynamicSmemBytes = sizeof(SharedSpace);
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, p, maps);
+  return cudaLaunchKernelEx(&cfg, sparse_shared_kernel, p, maps);
 }
 
 constexpr size_t kSparseWorkspace = 256;
@@ -841,13 +942,12 @@ extern "C" kvshot_status kvshot_draft_attn_sparse(const kvshot_attn_desc* d, con
   p.qscale = score_scale(d) * 1.4426950408889634f;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   // Pages are shared between nodes from 32 rows on, and where that leaves the SMs enough to do (us with a CTA for each node
-  // against shared; 16 caches of 20K to 32K tokens and 128 pages a node, 48 rows: 162, 110; 8 rows: 44, 56; 256 rows and 64
-  // pages: 403, 347; 16 caches of 4K tokens and 32 pages, 48 rows: 59, 45; one of 8K and 64 pages, 256 rows: 33, 47).  Two CTAs
-  // of a cluster fill the SMs' two places, and more are slower.
-  int log_gp = 0;
-  while ((1 << log_gp) < p.G) ++log_gp;
-  const int64_t rows = static_cast<int64_t>(p.Nq) << log_gp, shared = int64_t{d->num_caches} * d->hkv * ((rows + 63) / 64);
-  if (rows >= 32 && 3 * shared >= 2 * sm_count() && rows < 64 * 65535) {
+  // against shared; 16 caches of 20K to 32K tokens and 128 pages a node, 48 rows: 162, 98; 8 rows: 43, 58; 256 rows and 64
+  // pages: 403, 223; 64 caches of up to 8K and 32 pages, 16 rows: 79, 84; 16 caches of 4K and 32 pages, 48 rows: 59, 45; one of
+  // 8K and 64 pages, 256 rows: 33, 36).  Two CTAs of a cluster fill the SMs' two places (one: 131, and four: 122 for the 98).
+  const int each = kColumns / p.G;
+  const int64_t rows = static_cast<int64_t>(p.Nq) * p.G, blocks = (p.Nq + each - 1) / each, shared = blocks * d->num_caches * d->hkv;
+  if (rows >= 32 && 3 * shared >= 2 * sm_count() && blocks < 65536) {
     const uint32_t wait_ns = d->wait_limit_ns != 0 ? d->wait_limit_ns : static_cast<uint32_t>(kWaitLimitNs);
     const int S = shared < 2 * sm_count() ? 2 : 1;
     return launch_shared(p, d->num_caches, S, wait_ns, s) == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;

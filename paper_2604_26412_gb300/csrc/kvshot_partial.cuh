@@ -134,6 +134,13 @@ __device__ __forceinline__ float remote_float(uint32_t addr, uint32_t rank) {
   return x;
 }
 
+__device__ __forceinline__ float4 remote_float4(uint32_t addr, uint32_t rank) {
+  float4 x;
+  asm volatile("{\n\t.reg .u32 ra;\n\tmapa.shared::cluster.u32 ra, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [ra];\n\t}"
+               : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr), "r"(rank) : "memory");
+  return x;
+}
+
 __device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
 
 // Dot products of rows (keys, or bounds) with rows of q run as mma.sync m16n8k16 with the rows as M.  A sum over the dims
