@@ -296,6 +296,24 @@ def test_sparse_shared_pages_without_picks_and_bit_for_bit():
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("scale,std", [(1.0, 4.0), (0.05, 0.5), (3.0, 8.0)])
+def test_sparse_shared_scales(scale, std):
+    p = Problem(**SHARED["chain"], scale=scale, std=std, seed=12)
+    run_sparse(p, *p.random_picks(9, seed=12))
+
+
+def test_sparse_shared_scores_that_rise_and_fall_along_the_cache():
+    """Keys of every tile longer than the last one's, then shorter again, and rows whose scores all fall: references that move
+    at each tile, beside rows that keep theirs."""
+    p = Problem([1500] * 13, 16, nodes=8, query=8, std=2.0, seed=13)
+    for i, row in enumerate(p.table):
+        for at, page in enumerate(row[:94]):
+            p.k[page] *= float(1 + (at // 8 if i % 2 else 12 - at // 8))
+    p.q[:, 3] = -p.q[:, 2].abs()
+    picks = np.broadcast_to(np.arange(94, dtype=np.int32), (13, 8, 8, 94))
+    run_sparse(p, picks, np.full((13, 8, 8), 94, np.int32))
+
+
 def test_sparse_shared_bad_picks_pages_and_parents():
     p = Problem([100] * 13, 16, nodes=8, query=8, tree=True)
     picks = np.full((13, 8, 8, 6), -1, np.int32)
