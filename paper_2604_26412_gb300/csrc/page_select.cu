@@ -215,10 +215,9 @@ struct SelectParams {
 };
 
 __device__ __forceinline__ uint32_t order_key(float f) {
-  const uint32_t u = __float_as_uint(f);
-  if (f != f) return 0xffffffffu;
-  if (f == 0.f) return 0x80000000u;  // -0 is 0
-  return (u >> 31) != 0 ? ~u : u | 0x80000000u;
+  uint32_t u;
+  asm("add.rn.f32 %0, %1, 0f00000000;" : "=r"(u) : "r"(__float_as_uint(f)));  // -0 is 0, and every NaN 0x7fffffff
+  return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
 
 struct SelectRow {
@@ -234,10 +233,10 @@ __device__ __forceinline__ SelectRow select_row(const SelectParams& p, int row) 
   return SelectRow{n, min(n, p.keep)};
 }
 
-// One more in a bin, if `open`.  (Without a branch: a row has a dozen of these a thread and round.)
-__device__ __forceinline__ void count_in(int* bin, bool open) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %1, 0;\n\t@p red.shared.add.s32 [%0], 1;\n\t}" ::"r"(smem_addr(bin)),
-               "r"(static_cast<int>(open))
+// One more in bin i, if i < bins.  (Without a branch: a row has a dozen of these a thread and round.)
+__device__ __forceinline__ void count_in(uint32_t hist, uint32_t i, uint32_t bins) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.u32 p, %1, %2;\n\t@p red.shared.add.s32 [%0], 1;\n\t}" ::"r"(hist + 4 * i),
+               "r"(i), "r"(bins)
                : "memory");
 }
 
@@ -289,19 +288,33 @@ __device__ __forceinline__ int remote_int(const int* at, uint32_t rank) {
 // every thread a run of consecutive entries, so that the picks' places follow from one scan of the threads' numbers.  Each
 // CTA counts the digits of its own keys that are still in question and adds what it counted to the counts of all CTAs, which
 // then each find the digit for themselves.  What bounds it: the latencies of a load, two to four rounds of counts and a
-// scan, and the instructions for keys that are no longer in question.  4096 of 32K entries in 16 rows: 16.5 us (89 with one
-// CTA that reads the scores for every digit).  1536 rows of 1250 to 2048 entries: 18.6 us; a warp to a row with its keys in
-// registers, bit by bit, took 25.8, tables kept four times 22.5, first digits of half octaves 28.9.
+// scan, and, where there are many rows, the instructions of each key (keys that do not compete are 0, so that a key in
+// question is one subtraction and one comparison).  4096 of 32K entries in 16 rows: 11.6 us (89 with one CTA that reads the
+// scores for every digit; 13.5 with eight CTAs of 4096 entries to a row and not four of 8192).  1536 rows of 1250 to 2048
+// entries: 11.5 us; a warp to a row with its keys in registers, bit by bit, took 25.8, a set of keys in question kept as bits
+// 17.1, digits of 8 and 10 bits 12.5 and 11.8, 256 threads to a row 15.2.
 constexpr int kSelectKeys = 16;
 constexpr int kMaxSelectCluster = 8;
 
 template <int kThreads, int kBits, bool kCluster>
+struct SelectSpace {
+  static constexpr int kBins = 1 << kBits, kWarps = kThreads / 32, kPasses = (32 + kBits - 1) / kBits;
+  int hist[2][kBins];
+  int total[kCluster ? kPasses : 1][kCluster ? kBins : 1];  // over the cluster
+  float scores[kWarps][33 * kSelectKeys];
+  int warp[kWarps], sum, bin, above;
+};
+
+template <int kThreads, int kBits, bool kCluster>
 __global__ void __launch_bounds__(kThreads) select_kernel(SelectParams p) {
-  constexpr int kBins = 1 << kBits, kWarps = kThreads / 32, kPasses = (32 + kBits - 1) / kBits;
-  __shared__ int s_hist[2][kBins];
-  __shared__ int s_total[kCluster ? kPasses : 1][kCluster ? kBins : 1];  // over the cluster
-  __shared__ int s_warp[kWarps], s_sum;
-  __shared__ int s_bin, s_above;
+  using Space = SelectSpace<kThreads, kBits, kCluster>;
+  constexpr int kBins = Space::kBins, kWarps = Space::kWarps, kPasses = Space::kPasses;
+  extern __shared__ __align__(16) uint8_t s_raw[];
+  Space& sm = *reinterpret_cast<Space*>(s_raw);
+  int(&s_hist)[2][kBins] = sm.hist;
+  auto& s_total = sm.total;
+  int(&s_warp)[kWarps] = sm.warp;
+  int &s_sum = sm.sum, &s_bin = sm.bin, &s_above = sm.above;
   const int S = kCluster ? static_cast<int>(cluster_size()) : 1, rank = kCluster ? blockIdx.x % S : 0;
   const int row = blockIdx.x / S, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const SelectRow r = select_row(p, row);
@@ -316,33 +329,45 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectParams p) {
   // This CTA's entries [e0, e1); this thread's: `rounds` from `first` on.
   const int chunk = (n + S - 1) / S, e0 = min(n, rank * chunk), e1 = min(n, e0 + chunk);
   const int rounds = (chunk + kThreads - 1) / kThreads, first = e0 + tid * rounds, mine = min(max(e1 - first, 0), rounds);
-  const float* s = p.scores + static_cast<size_t>(row) * p.row_len + first;
-  const int a = p.first - first, b = n - p.last - first;  // entries [a, b) of this thread compete for `need` places
+  // (A warp reads its threads' runs together, and hands them out through shared memory; a gap in 33 keeps the banks apart.)
+  const int of_warp = min(max(e1 - (e0 + warp * 32 * rounds), 0), 32 * rounds);
+  const float* s = p.scores + static_cast<size_t>(row) * p.row_len + e0 + warp * 32 * rounds;
   int need = p.keep - p.first - p.last;
   float f[kSelectKeys];
 #pragma unroll
-  for (int k = 0; k < kSelectKeys; ++k) f[k] = k < mine ? __ldg(s + k) : 0.f;
+  for (int k = 0; k < kSelectKeys; ++k) f[k] = k * 32 + lane < of_warp ? __ldg(s + k * 32 + lane) : 0.f;
   for (int i = tid; i < 2 * kBins; i += kThreads) s_hist[i / kBins][i % kBins] = 0;
   if (kCluster)
     for (int i = tid; i < kPasses * kBins; i += kThreads) s_total[kCluster ? i / kBins : 0][kCluster ? i % kBins : 0] = 0;
+#pragma unroll
+  for (int k = 0; k < kSelectKeys; ++k)
+    if (k < rounds) sm.scores[warp][k * 33 + lane] = f[k];
   if (kCluster) cluster_sync_all();
   else __syncthreads();
-  uint32_t key[kSelectKeys], open = 0, over = 0;  // bit k: entry k is still in question; it is picked
+  // Of this thread's entries those past the row's, and those that are picked anyway, have key 0, which no score has.
+  const uint32_t all = (1u << mine) - 1;
+  auto below = [&](int e) { return (1u << min(max(e - first, 0), mine)) - 1; };
+  const uint32_t anyway = all & (below(p.first) | ~below(n - p.last)), competing = all & ~anyway;
+  const bool edge = __any_sync(0xffffffffu, competing != (1u << rounds) - 1);
+  uint32_t key[kSelectKeys];
 #pragma unroll
   for (int k = 0; k < kSelectKeys; ++k) {
     if (k >= rounds) break;
-    key[k] = order_key(f[k]);
-    const uint32_t bit = k < mine ? 1u << k : 0u;
-    if (k >= a && k < b) open |= bit;
-    else over |= bit;
+    const int at = lane * rounds + k;
+    key[k] = order_key(sm.scores[warp][at + (at >> 5)]);
+    if (edge && (competing >> k & 1) == 0) key[k] = 0;
   }
-  for (int pass = 0, shift = 32 - kBits; need > 0; ++pass) {
+  // Still in question: keys from lo on, of which the bits below `width` are open.
+  uint32_t lo = 0;
+  int width = 32;
+  for (int pass = 0; need > 0; ++pass) {
     int* hist = s_hist[pass & 1];
-    const uint32_t digits = pass == 0 ? kBins - 1 : (1u << min(kBits, 32 - pass * kBits)) - 1;
+    const int shift = max(width - kBits, 0);
+    const uint32_t bins = 1u << (width - shift), hist_at = smem_addr(hist);
 #pragma unroll
     for (int k = 0; k < kSelectKeys; ++k) {
       if (k >= rounds) break;
-      count_in(&hist[(key[k] >> shift) & digits], (open >> k & 1u) != 0);
+      count_in(hist_at, (key[k] - lo) >> shift, bins);
     }
     __syncthreads();
     if (kCluster) {
@@ -363,21 +388,23 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectParams p) {
       s_above = above;
     });
     __syncthreads();
-    const uint32_t bin = s_bin;
+    lo += static_cast<uint32_t>(s_bin) << shift;
+    need -= s_above;
+    width = shift;
+    if (width == 0 || hist[s_bin] == need) break;  // (the whole bin is taken)
+  }
+  // Picked is what is above; what is still in question is equal, and the first `need` of it are picked.
+  uint32_t over = anyway, open = 0;
+  if (p.keep > p.first + p.last) {
+    const uint32_t span = (1u << width) - 1;  // (width < 32 after a pass)
 #pragma unroll
     for (int k = 0; k < kSelectKeys; ++k) {
       if (k >= rounds) break;
-      if ((open >> k & 1u) == 0) continue;
-      const uint32_t digit = (key[k] >> shift) & digits;
-      if (digit > bin) over |= 1u << k;
-      if (digit != bin) open &= ~(1u << k);
+      if (key[k] > lo + span) over |= 1u << k;
+      if (key[k] - lo <= span) open |= 1u << k;
     }
-    need -= s_above;
-    if (shift == 0 || hist[bin] == need) break;  // (the whole bin is taken)
-    shift = max(0, shift - kBits);
   }
-  if (p.keep == p.first + p.last) open = 0;
-  // What is still in question is equal, and the first `need` of it are picked.  Places: numbers picked and equal before.
+  // Places: numbers picked and equal before.
   const int overs = __popc(over), equals = __popc(open);
   int place = overs | equals << 16;  // (each below 2^14 in a CTA)
   int scan = place;
@@ -406,13 +433,12 @@ __global__ void __launch_bounds__(kThreads) select_kernel(SelectParams p) {
       equals_before += t >> 16;
     }
   }
-#pragma unroll
-  for (int k = 0; k < kSelectKeys; ++k) {
-    if (k >= rounds) break;
-    const bool o = (over >> k & 1u) != 0, e = (open >> k & 1u) != 0;
-    if (o || (e && equals_before < need)) picks[overs_before + min(equals_before, need)] = first + k;
-    overs_before += o;
-    equals_before += e;
+  for (uint32_t left = over | open; left != 0; left &= left - 1) {
+    const int k = __ffs(left) - 1;
+    const bool equal = (open >> k & 1u) != 0;
+    if (!equal || equals_before < need) picks[overs_before + min(equals_before, need)] = first + k;
+    if (equal) ++equals_before;
+    else ++overs_before;
   }
   if (kCluster) cluster_sync_all();  // (another CTA may still read this one's sum)
 }
@@ -514,9 +540,15 @@ cudaError_t launch_select(const SelectParams& p, int rows, int S, cudaStream_t s
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(rows * S);
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sizeof(SelectSpace<kThreads, kBits, kCluster>);
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = kCluster ? 1 : 0;
+  if (cfg.dynamicSmemBytes > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(select_kernel<kThreads, kBits, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               static_cast<int>(cfg.dynamicSmemBytes));
+    if (e != cudaSuccess) return e;
+  }
   return cudaLaunchKernelEx(&cfg, select_kernel<kThreads, kBits, kCluster>, p);
 }
 
@@ -607,7 +639,7 @@ extern "C" kvshot_status kvshot_select_top(const kvshot_select_desc* d, const fl
   cudaError_t e;
   if (n <= 128 * kSelectKeys) e = launch_select<128, 9, false>(p, rows, 1, st);
   else if (n <= 512 * kSelectKeys && 2 * rows > sm_count()) e = launch_select<512, 11, false>(p, rows, 1, st);
-  else if (n <= 512 * kSelectKeys * kMaxSelectCluster) e = launch_select<512, 11, true>(p, rows, cluster(4096), st);
+  else if (n <= 512 * kSelectKeys * kMaxSelectCluster) e = launch_select<512, 11, true>(p, rows, cluster(8192), st);
   else if (n <= 1024 * kSelectKeys * kMaxSelectCluster) e = launch_select<1024, 11, true>(p, rows, kMaxSelectCluster, st);
   else e = launch_maybe_pdl(select_long_kernel, dim3(rows), dim3(kLongThreads), 0, false, st, p);
   return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;

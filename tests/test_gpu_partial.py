@@ -142,6 +142,18 @@ def test_select_of_long_rows(n):
         run_select(some_scores(kind, 2, n, n), [n, n - 1000], 1, 1, keep, 16 if keep > 100 else 0, keep // 8)
 
 
+@pytest.mark.parametrize("n,keep", [(700, 60), (5000, 600), (20000, 2000), (150000, 9)])
+def test_select_takes_every_nan_alike(n, keep):
+    """NaNs of either sign and of any payload come first, in their entries' order; every -inf last but two zeros alike."""
+    x = np.where(np.arange(2 * n).reshape(2, n) % 5 == 0, 0.0, -np.inf).astype(np.float32)
+    bits = x.view(np.uint32)
+    bits[0, ::n // 40] = 0xff800001  # (a signalling one, negative)
+    bits[0, 7::n // 40] = 0x7fffffff
+    bits[1, 3::n // 30] = 0xffc00000
+    bits[1, ::10] = 0x80000000
+    run_select(x, [n, n - 1], 1, 1, keep, 1, 2)
+
+
 def test_select_of_the_pages_of_ragged_caches():
     lens = [0, 1, 16, 17, 1000, 555]
     run_select(some_scores("ties", len(lens) * 24, 63, 3), lens, 24, 16, 12, 1, 2)
