@@ -153,9 +153,9 @@ static_assert(kDirectWarps * 32 == kDirectKeys, "a thread per key");
 //                     units' room in tensor memory.  Its keys' sums stay with their threads until the piece's end.
 //   warp 8            TMA, and the rows' lse;  warp 9: MMA, and the owner of tensor memory
 // Up to 128 rows the call reads K at the copy's rate (16 x 32K tokens 166 to 170 us, floor 160).  With 256 rows (20K to 32K
-// tokens each) it takes 232 us, 1.0 PFLOP/s: the products alone, with nothing behind them, take 187, the exponentials alone
-// 193, and the two wait for each other.  Slower there: a warpgroup for a unit of every tile 259 us, four warpgroups of 64
-// columns 276; two units' products in turn 250; units taken to registers whole 248; lse kept in registers 400.
+// tokens each) it takes 192 us, 1.2 PFLOP/s, in which a unit waits 590 cycles for its product, issued after the other
+// warpgroup's, and is summed in 1010, half of them at the exponentials' rate.  Both units of a tile as one product took 198,
+// as did five tiles in the ring with one place for q; operands not in uniform registers 218.
 constexpr int kTcGroups = 2;  // warpgroups
 constexpr int kTcLoadWarp = 4 * kTcGroups, kTcMmaWarp = kTcLoadWarp + 1;
 constexpr int kTcThreads = (kTcMmaWarp + 1) * 32;
@@ -263,7 +263,7 @@ __device__ __forceinline__ void add_columns(const uint32_t (&v)[32], const float
 __global__ void __launch_bounds__(kTcThreads, 1)
     weights_tc_kernel(const __grid_constant__ WeightTcParams p, const __grid_constant__ WeightMaps maps) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (known to be uniform)
   const int qbytes = p.cols * 256, hkv = p.w.v.hkv, G = p.w.G;
   uint8_t* ring = smem + 2 * qbytes;
   float* s_z = reinterpret_cast<float*>(ring + p.stages * kTcTileBytes);  // [2][kTcMaxRows], by pass
@@ -386,16 +386,18 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       mbar_wait(smem_addr(&bar.kfull[i % p.stages]), (i / p.stages) & 1, err);
     for (int i = max(0, q_issued - 2); i < q_issued; ++i) mbar_wait(smem_addr(&bar.qfull[i & 1]), (i >> 1) & 1, err);
   } else if (warp == kTcMmaWarp) {  // ---- products
+    // (All control is uniform, so that operands are in uniform registers: 26 cycles to issue an MMA, and not 50.)
     int stage = 0, pass_no = 0;
     uint32_t phase = 0;
     uint32_t units0 = 0, units1 = 0;  // that each warpgroup has been given
     bool ok = true;
-    while (ok && cu.next(p, &pc)) {
+    while (__all_sync(0xffffffffu, ok && cu.next(p, &pc))) {
+      const int tiles = __shfl_sync(0xffffffffu, pc.tiles, 0);
       for (int pass = 0; ok && pass < passes; ++pass, ++pass_no) {
         const int qb = pass_no & 1;
         ok = __all_sync(0xffffffffu, wait(smem_addr(&bar.qfull[qb]), (pass_no >> 1) & 1, err, limit));
         const uint32_t qbase = smem_addr(smem) + qb * qbytes;
-        for (int i = 0; ok && i < pc.tiles; ++i) {
+        for (int i = 0; ok && i < tiles; ++i) {
           uint32_t& n = (i & 1) != 0 ? units1 : units0;
           for (int col = 0; col < p.cols; col += kTcPart, ++n) {
             const int room = 2 * (i & 1) + (n & 1);
@@ -450,16 +452,30 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             const uint32_t at = my_tmem + room * kTcPart;
             const float* z = z0 + col;
             uint32_t v[32], v2[32];
+            // (The room is given back as soon as its last columns are in registers.)
+            auto give_back = [&] {
+              tc::tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(smem_addr(&bar.sempty[2 * wg + room]));
+            };
             if (whole > 0) tc::tmem_ld32(at, v);
-            for (int cc = 0; cc < whole; cc += 2) {
-              wait_ld_of(v);
-              if (cc + 1 < whole) tc::tmem_ld32(at + 32 * (cc + 1), v2);
-              add_columns(v, z + 32 * cc, p.w.qscale, sum);
-              if (cc + 1 < whole) {
+            if (here == kTcPart) {  // (the common case without a branch between its loads)
+#pragma unroll
+              for (int cc = 0; cc < kTcPart / 32; cc += 2) {
+                wait_ld_of(v);
+                tc::tmem_ld32(at + 32 * (cc + 1), v2);
+                add_columns(v, z + 32 * cc, p.w.qscale, sum);
                 wait_ld_of(v2);
-                if (cc + 2 < whole) tc::tmem_ld32(at + 32 * (cc + 2), v);
+                if (cc + 2 < kTcPart / 32) tc::tmem_ld32(at + 32 * (cc + 2), v);
+                else give_back();
                 add_columns(v2, z + 32 * (cc + 1), p.w.qscale, sum);
               }
+              continue;
+            }
+            for (int cc = 0; cc < whole; ++cc) {
+              wait_ld_of(v);
+              add_columns(v, z + 32 * cc, p.w.qscale, sum);
+              if (cc + 1 < whole) tc::tmem_ld32(at + 32 * (cc + 1), v);
             }
             for (int x = max(whole, 0) * 32; x < here; x += 4) {
               uint32_t u[4];
@@ -469,9 +485,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
               for (int e = 0; e < 4; ++e)
                 if (x + e < here) sum[e & 1].x += ex2(fmaf(__uint_as_float(u[e]), p.w.qscale, z[x + e]));
             }
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&bar.sempty[2 * wg + room]));
+            give_back();
           }
           acc[i / kTcGroups] += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         }
