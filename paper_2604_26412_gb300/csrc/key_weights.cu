@@ -153,9 +153,9 @@ static_assert(kDirectWarps * 32 == kDirectKeys, "a thread per key");
 //                     units' room in tensor memory.  Its keys' sums stay with their threads until the piece's end.
 //   warp 8            TMA, and the rows' lse;  warp 9: MMA, and the owner of tensor memory
 // Up to 128 rows the call reads K at the copy's rate (16 x 32K tokens 166 to 170 us, floor 160).  With 256 rows (20K to 32K
-// tokens each) it takes 192 us, 1.2 PFLOP/s, in which a unit waits 590 cycles for its product, issued after the other
-// warpgroup's, and is summed in 1010, half of them at the exponentials' rate.  Both units of a tile as one product took 198,
-// as did five tiles in the ring with one place for q; operands not in uniform registers 218.
+// tokens each) it takes 192 us, 1.2 PFLOP/s: the bytes and the hand-overs alone take 149, with the products 182, with the
+// exponentials 175.  No faster: both units of a tile as one product (198), five tiles in the ring with one place for q (197),
+// four warpgroups of a unit each (192).  Operands not in uniform registers cost 26 us, rooms given back after their sums 11.
 constexpr int kTcGroups = 2;  // warpgroups
 constexpr int kTcLoadWarp = 4 * kTcGroups, kTcMmaWarp = kTcLoadWarp + 1;
 constexpr int kTcThreads = (kTcMmaWarp + 1) * 32;
