@@ -518,8 +518,9 @@ kvshot_status kvshot_select_top(const kvshot_select_desc* desc, const float* sco
  * i < counts[c, n, h], and the draft keys that kvshot_draft_attn gives that row.
  * picks: [C, Nq, hkv, max_picks] int32, each list ascending; counts: [C, Nq, hkv] int32 in [0, max_picks].  A pick that
  * is not above its predecessor or not a page below the cache's length is recorded as KVSHOT_ERR_DEVICE_BOUNDS and passed
- * over (a page that comes again later in such a list may count twice), a count out of range recorded and clamped.  Other arguments as for kvshot_draft_attn, but target_k/v and
- * draft_k/v 32-byte aligned.
+ * over (a page that comes again later in such a list may count twice), a count out of range recorded and clamped; entries
+ * of picks past a count may be anything.  Other arguments as for kvshot_draft_attn, but target_k/v and draft_k/v 32-byte
+ * aligned.
  * The softmax weights are rounded to bf16 for the tensor cores, sums are fp32.  A NaN or infinity stored in a value that some
  * row of the KV head sees may reach the cache's other rows of that head.
  * Workspace: kvshot_draft_attn_sparse_workspace_size bytes (0 if the descriptor is invalid), as for kvshot_draft_attn.
@@ -534,8 +535,9 @@ kvshot_status kvshot_draft_attn_sparse(const kvshot_attn_desc* desc, const void*
 /*
  * weights_out[c, j] = decay * weights[c, j] + sum over the query rows n and q heads of exp(scale q . k_j - lse[c, n, head])
  * for every token j < L_c: what the softmax whose lse kvshot_draft_attn returned gave the token, summed.  A row whose lse
- * is -inf adds nothing.  q, and keys below the length, must be finite.  [C, weights_len] fp32; entries past the length are left as they are.  weights may be weights_out, or NULL (zeros).
- * decay in [0, 1]; with 0 weights is not read.  Sums are fp32 and their order fixed.
+ * is -inf adds nothing.  q, and keys below the length, must be finite.  [C, weights_len] fp32; entries past the length are
+ * left as they are.  weights may be weights_out, or NULL (zeros).  decay in [0, 1]; with 0 weights is not read.  Sums are
+ * fp32 and their order fixed.
  * page_table NULL: a contiguous cache [C, hkv, l_cap, 128].  A length above weights_len is recorded as out of bounds, too.
  */
 kvshot_status kvshot_key_weights(const kvshot_attn_desc* desc, const void* q, const void* target_k,
@@ -559,7 +561,8 @@ kvshot_status kvshot_key_weights(const kvshot_attn_desc* desc, const void* q, co
  * Device errors are recorded as KVSHOT_ERR_DEVICE_BOUNDS: a length that the table has no room for, or a count below 0 or
  * above what the length, max_kept, page_table_out or weights_len_out has room for (that cache's tokens, length and pages stay
  * as they are; seq_lens_out is the length, clamped to the table's room); a kept index out of order or range (that cache's
- * contents are then unspecified); page ids outside their pool, and more free pages than num_free (passed over).
+ * contents are then unspecified); page ids outside their pool (nothing is moved there; one that is given back goes on the
+ * list as it is); more free pages than num_free (none is given back).
  */
 typedef struct kvshot_evict_desc {
   int32_t num_caches;        /* C in [1, 1024] */

@@ -216,8 +216,11 @@ __global__ void __launch_bounds__(kEndThreads) evict_end_kernel(EvictParams p) {
     }
     if (room)
       for (int i = warp; i < p.C; i += 32)
-        for (int j = lane; j < s_gone[i]; j += 32)
-          p.free_pages[F + s_base[i] + j] = p.page_table[static_cast<size_t>(i) * p.max_pages + s_first[i] + j];
+        for (int j = lane; j < s_gone[i]; j += 32) {
+          const int id = p.page_table[static_cast<size_t>(i) * p.max_pages + s_first[i] + j];
+          if (static_cast<unsigned>(id) >= static_cast<unsigned>(p.num_pages)) set_error(p.err, KVSHOT_ERR_DEVICE_BOUNDS);
+          p.free_pages[F + s_base[i] + j] = id;
+        }
   }
   wait_for_prerequisite_grid();  // (by all: what follows this kernel follows the moves, too)
   if (c < p.C) p.seq_lens_out[c] = ck.kept >= 0 ? ck.kept : ck.len;

@@ -605,3 +605,12 @@ def test_evict_bad_lists_stay_in_the_cache():
     check(p, kvshot.KVSHOT_ERR_DEVICE_BOUNDS)
     assert torch.equal(other.view(torch.int16), p.k[p.t_table[1, :4].long()].view(torch.int16))  # (all kept: nothing moves)
     assert lens.tolist() == [60, 50]
+
+
+def test_evict_records_a_page_outside_the_pool_among_those_given_back():
+    p = Problem([100, 40], 16)
+    p.table[0, 5] = p.num_pages  # page 5 of 7; the first 30 kept tokens come from before it, and need 2
+    p.t_table = p.ints(p.table)
+    kept = np.stack([np.arange(30), np.arange(30)]).astype(np.int32)
+    got = run_evict(p, [30, 30], kept=kept, code=kvshot.KVSHOT_ERR_DEVICE_BOUNDS)
+    assert p.num_pages in got[4] and got[5] == len(p.free) + 5 + 1
