@@ -4,6 +4,7 @@
 #include <climits>
 
 #include "kvshot_partial.cuh"
+#include "kvshot_tcgen05.cuh"
 
 namespace kvshot {
 namespace {
@@ -70,7 +71,8 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(CacheView v, con
 // max(q lo, q hi) = max(q, 0) hi + min(q, 0) lo, so a page's score is the product of [min(q, 0), max(q, 0)] with its
 // bounds [lo, hi], a row of 256 elements: 16 steps of mma.sync with 16 pages as M.  The two halves of a row of q lie in shared
 // memory; lane (g, t) has pieces 2 t, 2 t + 1 of every 128 bytes of rows g and g + 8 (32-byte loads of the bounds).
-// 12 nodes of 4 q heads over 16 caches of 20K to 32K tokens: 36.5 us, bound by the loads in flight of 16 warps an SM (HBM 0.53).
+// Bound by the loads in flight of 16 warps an SM: 12 nodes of 4 q heads over 64 caches of up to 8K tokens 30 us.  Small calls are
+// a launch and two dependent loads: one row over 8K tokens 2.4 us in a graph.
 constexpr int kScoreWarps = 4;
 constexpr int kScoreRows = 64;                   // rows of q in shared memory at a time
 constexpr int kScoreRowBytes = 2 * 256 + 64;     // 8 rows' pieces are in different banks
@@ -203,6 +205,357 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p,
       }
     }
   }
+}
+
+// Many rows over many pages: tcgen05.  128 pages are the M rows of a product of 256 dims, and the query rows (up to 128 of
+// whole nodes) its N columns, so that a thread has a page's row of scores, finds each node's best in its own registers, and a
+// warp stores 32 consecutive pages.  One persistent CTA per SM takes an equal run of the caches' tiles, KV head after KV
+// head.  Pages are 512 bytes at any place of the pool, which a tensor map has no box for: four warps copy them 16 bytes a
+// lane, half a page (lo, hi) to a stage, all but two of the stages on their way.  The next head's q is loaded meanwhile.
+//   warps 0..3 scores;  4..7 copies, and q's two halves;  8 MMA, and the owner of tensor memory
+// 12 nodes of 4 q heads over 16 caches of 20K to 32K tokens: 28.8 us (mma.sync 36.5).  Once begun, a CTA takes a tile in 1.5 us
+// (6.5 TB/s with the scores that are written); its start, q and the first tile take 8.
+constexpr int kStPages = 128;
+constexpr int kStCols = 128;
+constexpr int kStStageBytes = kStPages * 256, kStChunkBytes = kStPages * 128;
+constexpr int kStMaxStages = 5, kStMinStages = 3;
+constexpr int kStSmem = 232448;  // what a CTA can have
+constexpr int kStRooms = 4;  // of kStCols columns in tensor memory
+constexpr int kStThreads = 9 * 32;
+constexpr int kStQEach = kStCols * 16 / 128;
+
+struct ScoreTcParams {
+  ScoreParams s;
+  int nodes_per_block, blocks, cols;  // blocks of whole nodes; cols: a block's columns rounded up to 16
+  int stages;
+  uint32_t wait_ns;
+};
+struct ScoreTcBarriers {
+  uint64_t kfull[kStMaxStages], kempty[kStMaxStages], qfull[2], qempty[2], sfull[kStRooms], sempty[kStRooms], done;
+  uint32_t tmem;
+};
+struct ScoreUnit {
+  int c, hr, tile, pages;  // hr: KV head and block of nodes; pages: of the cache
+  bool fresh;              // its q is another one's than the last unit's
+};
+
+// A CTA's run of units.
+struct ScoreCursor {
+  int c, hr, tile, pages;
+  int64_t left;
+  bool fresh;
+  __device__ __forceinline__ static int pages_of(const ScoreTcParams& p, int c) {
+    const int L = clamped_len(p.s.v, c);
+    return (L + p.s.v.P - 1) / p.s.v.P;
+  }
+  __device__ __forceinline__ static int tiles(int pages) { return (pages + kStPages - 1) / kStPages; }
+  __device__ __forceinline__ void init(const ScoreTcParams& p) {
+    const int lane = threadIdx.x & 31, heads = p.s.v.hkv * p.blocks;
+    const int own = lane < p.s.v.C ? pages_of(p, lane) : 0;  // (of up to 32 caches, looked at once)
+    int64_t total = static_cast<int64_t>(tiles(own)) * heads;
+    for (int i = lane + 32; i < p.s.v.C; i += 32) total += static_cast<int64_t>(tiles(pages_of(p, i))) * heads;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    const int64_t t0 = total * blockIdx.x / gridDim.x;
+    left = total * (blockIdx.x + 1) / gridDim.x - t0;
+    c = hr = tile = pages = 0;
+    fresh = true;
+    if (left == 0) return;
+    int64_t before = 0;
+    for (int base = 0;; base += 32) {  // (t0 is below the total)
+      const int here = base == 0 ? own : base + lane < p.s.v.C ? pages_of(p, base + lane) : 0;
+      const int64_t n = static_cast<int64_t>(tiles(here)) * heads;
+      int64_t scan = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += x;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, before + scan > t0);
+      if (past != 0) {
+        const int at = __ffs(past) - 1;
+        c = base + at;
+        pages = __shfl_sync(0xffffffffu, here, at);
+        const int64_t in = t0 - before - __shfl_sync(0xffffffffu, scan - n, at);
+        hr = static_cast<int>(in / tiles(pages));
+        tile = static_cast<int>(in % tiles(pages));
+        return;
+      }
+      before += __shfl_sync(0xffffffffu, scan, 31);
+    }
+  }
+  __device__ __forceinline__ bool next(const ScoreTcParams& p, ScoreUnit* out) {
+    if (left == 0) return false;
+    while (tile == tiles(pages)) {
+      tile = 0;
+      fresh = true;
+      if (++hr < p.s.v.hkv * p.blocks) continue;
+      hr = 0;
+      pages = pages_of(p, ++c);
+    }
+    *out = ScoreUnit{c, hr, tile++, pages, fresh};
+    fresh = false;
+    --left;
+    return true;
+  }
+};
+
+__device__ __forceinline__ void copy_async_16(uint32_t dst, const void* src, bool live) {  // zeros if not
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void wait_ld_of(uint32_t (&v)[32]) {  // nothing computed from v moves before the wait
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+                 "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]),
+                 "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
+                 "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
+}
+
+template <int kLogGp>
+__global__ void __launch_bounds__(kStThreads, 1) scores_tc_kernel(ScoreTcParams p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  constexpr int kGp = 1 << kLogGp;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (known to be uniform)
+  const ScoreParams& s = p.s;
+  const int hkv = s.v.hkv, q_chunk = p.cols * 128;  // bytes of 64 dims of the block's rows
+  const int stages = p.stages;
+  uint8_t* q_at = smem + stages * kStStageBytes;
+  ScoreTcBarriers& bar = *reinterpret_cast<ScoreTcBarriers*>(q_at + 2 * 4 * q_chunk);
+  int32_t* err = s.v.err;
+  const uint64_t limit = p.wait_ns;
+  if ((smem_addr(smem) & 1023u) != 0) {  // (the swizzled tiles' layout counts on it; dynamic shared memory is, alone)
+    set_error(err, KVSHOT_ERR_CUDA);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < stages; ++i) {
+      mbar_init(smem_addr(&bar.kfull[i]), 4);
+      mbar_init(smem_addr(&bar.kempty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_addr(&bar.qfull[i]), 4);
+      mbar_init(smem_addr(&bar.qempty[i]), 1);
+    }
+    for (int i = 0; i < kStRooms; ++i) {
+      mbar_init(smem_addr(&bar.sfull[i]), 1);
+      mbar_init(smem_addr(&bar.sempty[i]), 4);
+    }
+    mbar_init(smem_addr(&bar.done), 1);
+    fence_mbar_init();
+  }
+  if (warp == 8) {
+    tc::tmem_alloc(smem_addr(&bar.tmem), kStRooms * kStCols);
+    tc::tmem_relinquish();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = bar.tmem;
+  ScoreCursor cu;
+  cu.init(p);
+  ScoreUnit u;
+  bool ok = true;
+
+  if (warp == 8) {  // ---- products
+    const uint32_t idesc = tc::idesc_bf16(kStPages, p.cols, false);
+    int stage = 0, n = 0, group = -1;
+    uint32_t phase = 0;
+    while (__all_sync(0xffffffffu, ok && cu.next(p, &u))) {
+      if (__any_sync(0xffffffffu, u.fresh)) {
+        if (group >= 0) tc::tc_commit_elect(smem_addr(&bar.qempty[group & 1]));
+        ++group;
+        ok = __all_sync(0xffffffffu, wait(smem_addr(&bar.qfull[group & 1]), (group >> 1) & 1, err, limit));
+        if (!ok) break;
+      }
+      const int room = n % kStRooms;
+      if (n >= kStRooms) ok = __all_sync(0xffffffffu, wait(smem_addr(&bar.sempty[room]), (n / kStRooms - 1) & 1, err, limit));
+      const uint32_t q = smem_addr(q_at) + (group & 1) * 4 * q_chunk;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (ok) ok = __all_sync(0xffffffffu, wait(smem_addr(&bar.kfull[stage]), phase, err, limit));
+        if (!ok) break;
+        tc::tc_fence_after();
+        const uint32_t k = smem_addr(smem) + stage * kStStageBytes;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+          tc::tc_mma_elect(tmem + room * kStCols, tc::smem_desc_sw128(k + (ks >> 2) * kStChunkBytes + (ks & 3) * 32, 16, 1024),
+                           tc::smem_desc_sw128(q + (2 * half + (ks >> 2)) * q_chunk + (ks & 3) * 32, 16, 1024), idesc,
+                           half > 0 || ks > 0);
+        tc::tc_commit_elect(smem_addr(&bar.kempty[stage]));
+        if (++stage == stages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+      if (!ok) break;
+      tc::tc_commit_elect(smem_addr(&bar.sfull[room]));
+      ++n;
+    }
+    tc::tc_commit_elect(smem_addr(&bar.done));  // every product this warp issued has completed
+    mbar_wait(smem_addr(&bar.done), 0, err);
+  } else if (warp >= 4) {  // ---- copies
+    const int w = warp - 4, tid = threadIdx.x - 128;
+    int issued = 0, arrived = 0, group = -1, first = 0;  // halves; the first of the present group
+    int stage = 0, arrive_stage = 0;
+    uint32_t phase = 1;  // of the kempty barriers (a stage's first use waits for none)
+    auto arrive = [&](int until) {  // (those copies of this warp have landed)
+      fence_proxy_async_smem();
+      __syncwarp();
+      for (; arrived < until; ++arrived) {
+        if (lane == 0) mbar_arrive(smem_addr(&bar.kfull[arrive_stage]));
+        if (++arrive_stage == stages) arrive_stage = 0;
+      }
+    };
+    auto look_up = [&](const ScoreUnit& x) {  // this lane's page, looked at a unit later
+      const int page = x.tile * kStPages + w * 32 + lane;
+      return page < x.pages ? __ldg(s.v.page_table + static_cast<size_t>(x.c) * s.v.max_pages + page) : 0;
+    };
+    uint4 x[kStQEach];
+    auto load_q = [&](const ScoreUnit& v) {
+      const int h = v.hr / p.blocks, n0 = v.hr % p.blocks * p.nodes_per_block, nodes = min(p.nodes_per_block, s.Nq - n0);
+      const uint4* q = s.q + ((static_cast<size_t>(v.c) * s.Nq + n0) * s.hq + h * s.G) * 16 + (tid & 15);
+      // (Rows past the last one are other rows' here, and zeros in shared memory: without branches all loads are on their way.)
+      auto load = [&](int e) {  // 8 rows
+        const int r = e * 8 + (tid >> 4), n = min(r >> kLogGp, nodes - 1), j = min(r & (kGp - 1), s.G - 1);
+        x[e] = __ldg(q + (n * s.hq + j) * 16);
+      };
+#pragma unroll
+      for (int e = 0; e < kStQEach / 2; ++e) load(e);
+      if (p.cols > kStCols / 2)
+#pragma unroll
+        for (int e = kStQEach / 2; e < kStQEach; ++e) load(e);
+    };
+    auto put_q = [&](const ScoreUnit& v) {  // of the next group
+      if (arrived < first) {  // (what waits for the halves of the group before this one must not be waited for)
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        arrive(issued);
+      }
+      first = issued;
+      ++group;
+      if (group >= 2) ok = __all_sync(0xffffffffu, wait(smem_addr(&bar.qempty[group & 1]), ((group >> 1) - 1) & 1, err, limit));
+      if (!ok) return;
+      uint8_t* q = q_at + (group & 1) * 4 * q_chunk + (tid >> 3 & 1) * q_chunk + (tid >> 4) * 128 + (((tid & 7) ^ (tid >> 4)) << 4);
+      const int nodes = min(p.nodes_per_block, s.Nq - v.hr % p.blocks * p.nodes_per_block);
+#pragma unroll
+      for (int e = 0; e < kStQEach; ++e) {
+        if (e * 8 >= p.cols) break;
+        const int r = e * 8 + (tid >> 4);
+        if (r >> kLogGp >= nodes || (r & (kGp - 1)) >= s.G) x[e] = make_uint4(0, 0, 0, 0);
+        uint4* dst = reinterpret_cast<uint4*>(q + e * 1024);
+        *dst = make_uint4(min2(x[e].x, 0), min2(x[e].y, 0), min2(x[e].z, 0), min2(x[e].w, 0));
+        dst[2 * q_chunk / 16] = make_uint4(max2(x[e].x, 0), max2(x[e].y, 0), max2(x[e].z, 0), max2(x[e].w, 0));
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_addr(&bar.qfull[group & 1]));
+    };
+    bool more = cu.next(p, &u);
+    int next_id = more ? look_up(u) : 0;
+    if (more) {
+      load_q(u);
+      put_q(u);
+    }
+    while (ok && more) {
+      const ScoreUnit now = u;
+      const int id = next_id;
+      more = cu.next(p, &u);
+      next_id = more ? look_up(u) : 0;
+      const bool another = more && u.fresh;
+      if (another) load_q(u);
+      const bool in_pool = static_cast<unsigned>(id) < static_cast<unsigned>(s.v.num_pages);
+      const bool there = now.tile * kStPages + w * 32 + lane < now.pages;
+      if (there && !in_pool) set_error(err, KVSHOT_ERR_DEVICE_BOUNDS);
+      const int row = there && in_pool ? id * hkv + now.hr / p.blocks : -1;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        if (issued >= stages) ok = __all_sync(0xffffffffu, wait(smem_addr(&bar.kempty[stage]), phase, err, limit));
+        if (!ok) break;
+        // Rows r = 2 i and 2 i + 1 of the warp's 32: piece 0 .. 15 of the half, at (piece & 7) ^ (r & 7) of its 128 bytes.
+        const uint32_t dst = smem_addr(smem) + stage * kStStageBytes + (lane >> 3 & 1) * kStChunkBytes + w * 4096 + (lane >> 4) * 128;
+        const uint4* src = s.bounds + half * 16 + (lane & 15);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int from = __shfl_sync(0xffffffffu, row, 2 * i + (lane >> 4));
+          copy_async_16(dst + 256 * i + (((lane & 7) ^ (lane >> 4) ^ (2 * i & 7)) << 4), src + static_cast<size_t>(max(from, 0)) * 32,
+                        from >= 0);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++stage == stages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+        if (++issued - arrived > stages - 2) {  // (two stages are not on their way: one multiplied, one full)
+          if (stages == 5) asm volatile("cp.async.wait_group 3;" ::: "memory");
+          else if (stages == 4) asm volatile("cp.async.wait_group 2;" ::: "memory");
+          else asm volatile("cp.async.wait_group 1;" ::: "memory");
+          arrive(arrived + 1);
+        }
+      }
+      if (ok && another) put_q(u);
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    arrive(issued);
+  } else {  // ---- scores
+    int n = 0;
+    while (ok && cu.next(p, &u)) {
+      const int room = n % kStRooms, page = u.tile * kStPages + threadIdx.x;
+      const int h = u.hr / p.blocks, n0 = u.hr % p.blocks * p.nodes_per_block, nodes = min(p.nodes_per_block, s.Nq - n0);
+      const unsigned id = page < u.pages ? __ldg(s.v.page_table + static_cast<size_t>(u.c) * s.v.max_pages + page) : 0xffffffffu;
+      ok = __all_sync(0xffffffffu, wait(smem_addr(&bar.sfull[room]), (n / kStRooms) & 1, err, limit));
+      if (!ok) break;
+      tc::tc_fence_after();
+      const uint32_t at = tmem + room * kStCols + (static_cast<uint32_t>(warp) << 21);
+      const size_t stride = static_cast<size_t>(s.v.max_pages) * hkv;
+      float* out = s.scores + ((static_cast<size_t>(u.c) * s.Nq + n0) * hkv + h) * s.v.max_pages + page;
+      const bool live = id < static_cast<unsigned>(s.v.num_pages);
+#pragma unroll
+      for (int half = 0; half < kStCols / 64; ++half) {
+        if (half * 64 >= p.cols) break;
+        uint32_t v[2][32];
+        tc::tmem_ld32(at + half * 64, v[0]);
+        tc::tmem_ld32(at + half * 64 + 32, v[1]);  // (what is behind the columns is not used)
+        wait_ld_of(v[0]);
+        wait_ld_of(v[1]);
+        if ((half + 1) * 64 >= p.cols) {
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_addr(&bar.sempty[room]));
+        }
+#pragma unroll
+        for (int x = 0; x < 64 / kGp; ++x) {
+          float best = __uint_as_float(v[x * kGp >> 5][x * kGp & 31]);
+#pragma unroll
+          for (int j = 1; j < kGp; ++j)
+            if (j < s.G) best = fmaxf(best, __uint_as_float(v[(x * kGp + j) >> 5][(x * kGp + j) & 31]));
+          const int node = half * (64 / kGp) + x;
+          if (node < nodes && live) out[node * stride] = best * s.scale;
+        }
+      }
+      ++n;
+    }
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  if (warp == 8) tc::tmem_dealloc(tmem, kStRooms * kStCols);
+}
+
+template <int kLogGp>
+cudaError_t launch_scores_tc(const ScoreParams& s, int64_t most_tiles, uint32_t wait_ns, cudaStream_t stream) {
+  ScoreTcParams p;
+  p.s = s;
+  const int most = kStCols >> kLogGp;
+  p.blocks = (s.Nq + most - 1) / most;
+  p.nodes_per_block = (s.Nq + p.blocks - 1) / p.blocks;
+  p.cols = ((p.nodes_per_block << kLogGp) + 15) / 16 * 16;
+  p.wait_ns = wait_ns;
+  const int rest = kStSmem - 2 * 4 * p.cols * 128 - static_cast<int>(sizeof(ScoreTcBarriers));
+  static_assert(kStSmem - 2 * 4 * kStCols * 128 - sizeof(ScoreTcBarriers) >= kStMinStages * kStStageBytes, "room for the stages");
+  p.stages = std::min(kStMaxStages, rest / kStStageBytes);
+  const size_t smem = p.stages * kStStageBytes + 2 * 4 * p.cols * 128 + sizeof(ScoreTcBarriers);
+  cudaError_t e = cudaFuncSetAttribute(scores_tc_kernel<kLogGp>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  const int grid = static_cast<int>(std::min<int64_t>(sm_count(), most_tiles * p.blocks));
+  return launch_maybe_pdl(scores_tc_kernel<kLogGp>, dim3(grid), dim3(kStThreads), smem, false, stream, p);
 }
 
 // ------------------------------------------------------------ selection
@@ -602,6 +955,22 @@ extern "C" kvshot_status kvshot_page_scores(const kvshot_attn_desc* d, const voi
   p.scale = score_scale(d);
   const int pages = (p.v.len_bound + p.v.P - 1) / p.v.P, per_cta = kScoreWarps * 16;
   if (pages == 0) return KVSHOT_OK;
+  const int64_t tiles = static_cast<int64_t>((pages + kStPages - 1) / kStPages) * p.v.hkv * p.v.C;
+  // Graph times (us, mma.sync against tcgen05) of 16 caches of 20K to 32K tokens: 16 rows 23, 25; 32: 28, 26; 48: 35, 27; 64: 41,
+  // 29; 256: 141, 68.  64 caches of up to 8K: 32 rows 25, 32; 48: 30, 33; 64: 35, 35; 128: 64, 43.  4 of 32K: 48 rows 10.7,
+  // 12.3; 64: 12.8, 12.6.  One of 32K: 64 rows 5.9, 7.6; 128: 9.1, 8.5.  One of 8K: 128 rows 7.1, 8.0; 256: 12, 8.1.
+  const int64_t columns = static_cast<int64_t>(p.Nq) << log_gp;
+  if (columns >= 48 && columns * tiles >= (columns >= 128 ? 8 : 48) * 1024) {
+    const uint32_t wait_ns = d->wait_limit_ns != 0 ? d->wait_limit_ns : static_cast<uint32_t>(kWaitLimitNs);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const cudaError_t e = log_gp == 0   ? launch_scores_tc<0>(p, tiles, wait_ns, st)
+                          : log_gp == 1 ? launch_scores_tc<1>(p, tiles, wait_ns, st)
+                          : log_gp == 2 ? launch_scores_tc<2>(p, tiles, wait_ns, st)
+                          : log_gp == 3 ? launch_scores_tc<3>(p, tiles, wait_ns, st)
+                          : log_gp == 4 ? launch_scores_tc<4>(p, tiles, wait_ns, st)
+                                        : launch_scores_tc<5>(p, tiles, wait_ns, st);
+    return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
+  }
   const size_t smem = static_cast<size_t>(std::min(kScoreRows, ((p.Nq << log_gp) + 15) / 16 * 16)) * kScoreRowBytes;
   // Where there are more than twelve CTAs to an SM, each takes several chunks of pages, and q once.
   const int64_t heads = static_cast<int64_t>(p.v.hkv) * p.v.C;

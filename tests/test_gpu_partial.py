@@ -95,6 +95,47 @@ def test_scores_of_a_call_of_many_pages_bound_every_key():
         assert np.all(got[0, :, h].repeat(16, axis=-1)[:, :5003] >= s - 1e-4)
 
 
+MANY = {  # calls of 48 rows per KV head and more over many tiles of 128 pages
+    "level": dict(lens=[0, 1, 8, 1016, 1023, 1024, 1025, 1032, 2049, 5003] * 4, page=8, nodes=12, query=12),
+    "one head": dict(lens=[40] * 20 + [2100] * 40, page=16, hq=8, hkv=8, nodes=70, query=70),
+    "pairs": dict(lens=[0] * 40 + [77] * 80, page=64, hq=16, hkv=8, nodes=33, query=33),
+    "seven heads": dict(lens=list(range(0, 1600, 16)), page=8, hq=28, hkv=4, nodes=9, query=9),
+    "14 heads": dict(lens=[900] * 20, page=8, hq=112, hkv=8, nodes=8, query=8),
+    "17 heads": dict(lens=[17] * 200, page=32, hq=34, hkv=2, nodes=5, query=5),
+    "one KV head": dict(lens=[1100] * 200, page=8, hq=32, hkv=1, nodes=4, query=4),
+    "whole tree": dict(lens=[33000, 0, 200], page=8, nodes=64, query=64),
+}
+
+
+@pytest.mark.parametrize("name", MANY)
+def test_scores_of_many_pages(name):
+    p = Problem(**MANY[name], seed=len(name))
+    b = torch.randn((p.num_pages, p.hkv, 2, D), device="cuda").sort(dim=2).values.to(torch.bfloat16)
+    first = run_scores(p, b)
+    assert np.array_equal(first, run_scores(p, b))
+
+
+def test_scores_of_many_pages_pass_over_bad_pages_and_lengths():
+    p = Problem(**MANY["level"], seed=1)
+    b = torch.randn((p.num_pages, 8, 2, D), device="cuda").sort(dim=2).values.to(torch.bfloat16)
+    good = torch.full((40, 12, 8, p.table.shape[1]), 7.0, device="cuda")
+    kvshot.page_scores(p.desc, p.q, b, p.t_table, p.t_lens, good)
+    check(p)
+    for at, bad in (((9, 3), p.num_pages), ((19, 200), -1), ((28, 128), 2 ** 31 - 1)):
+        table, want = p.t_table.clone(), good.clone()
+        table[at], want[at[0], :, :, at[1]] = bad, 7.0
+        got = torch.full_like(good, 7.0)
+        kvshot.page_scores(p.desc, p.q, b, table, p.t_lens, got)
+        check(p, kvshot.KVSHOT_ERR_DEVICE_BOUNDS)
+        assert torch.equal(got, want)
+        p.err.zero_()
+    lens, want, got = p.t_lens.clone(), good.clone(), torch.full_like(good, 7.0)
+    lens[9], want[9] = -5, 7.0
+    kvshot.page_scores(p.desc, p.q, b, p.t_table, lens, got)
+    check(p, kvshot.KVSHOT_ERR_DEVICE_BOUNDS)
+    assert torch.equal(got, want)
+
+
 # ------------------------------------------------------------ selection
 
 def run_select(scores, lens, per, unit, keep, first, last, code=0):

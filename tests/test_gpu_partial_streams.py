@@ -8,7 +8,7 @@ from oracle import partial
 from paper_2604_26412_gb300 import kvshot
 
 from .partial_problems import D, Problem, f64
-from .test_gpu_partial import SHARED, check, run_sparse, run_weights, some_lse
+from .test_gpu_partial import MANY, SHARED, check, run_scores, run_sparse, run_weights, some_lse
 
 pytestmark = pytest.mark.gpu
 
@@ -46,7 +46,8 @@ def large():
     return Problem([300, 9001, 700, 64, 65, 128, 500, 33, 31, 900, 1000, 77, 90], 16, nodes=12, query=12, tree=True, seed=3)
 
 
-@pytest.mark.parametrize("make", [large, lambda: Problem([300, 0, 65], 16, nodes=3, query=2, seed=5)])
+@pytest.mark.parametrize("make", [large, lambda: Problem([300, 0, 65], 16, nodes=3, query=2, seed=5),
+                                  lambda: Problem(**MANY["level"], seed=6)])
 def test_other_streams_and_graphs_give_the_same(make):
     p = make()
     run, o = calls(p)
@@ -103,8 +104,10 @@ def test_waits_that_run_out_are_reported_and_the_next_calls_are_right():
     p = Problem(**SHARED["tree"], seed=2)
     picks, counts = p.random_picks(6)
     w = Problem([700, 300, 65], 16, nodes=24, query=24, seed=3)
+    m = Problem(**MANY["level"], seed=4)
+    bounds = torch.randn((m.num_pages, 8, 2, D), device="cuda").sort(dim=2).values.to(torch.bfloat16)
     for _ in range(2):  # (twice in a row: a call that gave up leaves nothing that blocks the next one)
-        p.desc.wait_limit_ns = w.desc.wait_limit_ns = 1
+        p.desc.wait_limit_ns = w.desc.wait_limit_ns = m.desc.wait_limit_ns = 1
         ws = p.workspace(6)
         kvshot.draft_attn_sparse(p.desc, p.q, p.k, p.v, p.t_table, p.t_lens, p.ints(picks), p.ints(counts), 6, p.dk, p.dv,
                                  p.t_parent, torch.empty_like(p.q), torch.empty(p.q.shape[:3], device="cuda"))
@@ -112,12 +115,16 @@ def test_waits_that_run_out_are_reported_and_the_next_calls_are_right():
         kvshot.key_weights(w.desc, w.q, w.k, w.t_table, w.t_lens, torch.from_numpy(some_lse(w)).cuda(), 0.0, 700, None,
                            torch.empty((3, 700), device="cuda"))
         check(w, kvshot.KVSHOT_ERR_TIMEOUT)
+        kvshot.page_scores(m.desc, m.q, bounds, m.t_table, m.t_lens, torch.empty((40, 12, 8, m.table.shape[1]), device="cuda"))
+        check(m, kvshot.KVSHOT_ERR_TIMEOUT)
+        m.err.zero_()
         p.err.zero_()
         w.err.zero_()
         del ws
-    p.desc.wait_limit_ns = w.desc.wait_limit_ns = 0
+    p.desc.wait_limit_ns = w.desc.wait_limit_ns = m.desc.wait_limit_ns = 0
     run_sparse(p, picks, counts)
     run_weights(w)
+    run_scores(m, bounds)
 
 
 def test_weights_do_not_change_from_run_to_run():
