@@ -326,13 +326,13 @@ cudaError_t launch_sparse(const SparseParams& p, int units, int S, cudaStream_t 
 // each page that any of its nodes picked once, 128 keys to a tile, on tcgen05: keys are the M rows of S^T = K Q^T, so that a
 // thread has one key and knows with one 64-bit word which columns, rows of q, picked its page; dims are the M rows of
 // O^T += V^T P^T, whose accumulator never leaves tensor memory.  The columns' sums stay in the threads' registers, each its own
-// keys' share, to the end.  A cluster shares out the pages, by their number; its CTAs' states meet in shared memory.
+// keys' share, to the end.  A cluster's CTAs take its pages in turn, by their number; their states meet in shared memory.
 //   a window of pages: the nodes' picks as a set of columns for each page, then the list of the pages that have any
 //   warps 0..7  softmax, a key to a thread: the first four of columns 0 to 31, the others of the rest
 //   warp 8      TMA;  warp 9: MMA, and the owner of tensor memory
 // Two CTAs to an SM, each with one K and one V tile: while one waits for its bytes the other multiplies.
 // The tree's level of 16 x 32K tokens (12 nodes, 128 pages each, 3 to 4 nodes to a page) reads 400 MB so, and not 1.6 GB:
-// 98 us, 162 with a CTA for each node, 110 with mma.sync and eight rows to a warp (five times the instructions).  Of the 98 the
+// 97 us, 162 with a CTA for each node, 110 with mma.sync and eight rows to a warp (five times the instructions).  Of the 97 the
 // list of pages takes 8, the first tile's references 4, the tiles 60 (at 6.5 TB/s), the wait for the cluster's slower CTA and
 // the join 10.  Four softmax warps of 64 columns each in turn were 112, a join by single floats 15 us longer.
 constexpr int kTileKeys128 = 128;
@@ -428,8 +428,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
     tc::tmem_relinquish();
   }
   const int pages = (L + P - 1) / P, groups_per_page = P / 8, total = nodes * p.max_picks;
-  const int page0 = static_cast<int>(static_cast<int64_t>(pages) * rank / S);
-  const int page1 = static_cast<int>(static_cast<int64_t>(pages) * (rank + 1) / S);
+  const int own = (pages - rank + S - 1) / S;  // pages of this CTA: rank, rank + S, ... (what is picked tends to be close together)
   const int32_t* picks = p.picks + ((static_cast<size_t>(c) * p.Nq + n0) * p.v.hkv + h) * p.max_picks;
   const size_t list_stride = static_cast<size_t>(p.v.hkv) * p.max_picks;
   // A window's page ids, consecutive ones to a thread, and the first of the picks: on their way together.
@@ -445,12 +444,12 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
   auto fetch = [&](int w0) {
 #pragma unroll
     for (int x = 0; x < kPagesEach; ++x) {
-      const int page = w0 + tid * kPagesEach + x;
-      id[x] = page >= page1 ? -1 : p.v.page_table == nullptr ? c : __ldg(p.v.page_table + static_cast<size_t>(c) * p.v.max_pages + page);
+      const int at = w0 + tid * kPagesEach + x, page = at * S + rank;
+      id[x] = at >= own ? -1 : p.v.page_table == nullptr ? c : __ldg(p.v.page_table + static_cast<size_t>(c) * p.v.max_pages + page);
     }
     fetch_picks(tid);
   };
-  fetch(page0);
+  fetch(0);
   // The nodes' counts, and of a tree the lines of ancestors as columns of the draft slots.
   const unsigned long long node_columns = (1ull << p.G) - 1;  // of node 0
   const unsigned long long all_columns = rows < 64 ? (1ull << rows) - 1 : ~0ull;
@@ -655,9 +654,9 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
   };
 
   // (Every CTA of the cluster has a window at least, in which it checks all picks.)
-  for (int w0 = page0; w0 < page1 || w0 == page0; w0 += kWindow) {
-    const int w1 = min(page1, w0 + kWindow);
-    if (w0 > page0) fetch(w0);
+  for (int w0 = 0; w0 < own || w0 == 0; w0 += kWindow) {
+    const int w1 = min(own, w0 + kWindow);
+    if (w0 > 0) fetch(w0);
     __syncthreads();  // (the list is no longer read)
     for (int i = tid; i < w1 - w0; i += kSharedThreads) sm.mask[i][0] = sm.mask[i][1] = 0;
     if (tid == 0) sm.ends = 0;
@@ -668,13 +667,15 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
       for (int x = 0; x < kPicksEach; ++x) {
         const int i = i0 + x * kSharedThreads, node = i / p.max_picks, at = i - node * p.max_picks;
         if (i >= total || at >= sm.counts[node]) continue;
-        if (pick[x] >= w0 && pick[x] < w1 && pick[x] > before[x]) {
-          const unsigned long long columns = node_columns << (node * p.G);
-          if (static_cast<uint32_t>(columns) != 0) atomicOr(&sm.mask[pick[x] - w0][0], static_cast<uint32_t>(columns));
-          if (columns >> 32 != 0) atomicOr(&sm.mask[pick[x] - w0][1], static_cast<uint32_t>(columns >> 32));
-        } else if (pick[x] < 0 || pick[x] >= pages || pick[x] <= before[x]) {
+        if (pick[x] < 0 || pick[x] >= pages || pick[x] <= before[x]) {
           set_error(err, KVSHOT_ERR_DEVICE_BOUNDS);
+          continue;
         }
+        const int own_at = pick[x] / S;
+        if (pick[x] - own_at * S != rank || own_at < w0 || own_at >= w1) continue;
+        const unsigned long long columns = node_columns << (node * p.G);
+        if (static_cast<uint32_t>(columns) != 0) atomicOr(&sm.mask[own_at - w0][0], static_cast<uint32_t>(columns));
+        if (columns >> 32 != 0) atomicOr(&sm.mask[own_at - w0][1], static_cast<uint32_t>(columns >> 32));
       }
     }
     __syncthreads();
@@ -708,11 +709,11 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
         if (bad) set_error(err, KVSHOT_ERR_DEVICE_BOUNDS);
         sm.list_row[at] = bad ? -1 : (id[x] * p.v.hkv + h) * P;
         *reinterpret_cast<uint2*>(sm.mask[at++]) = mask[x];
-        if (w0 + tid * kPagesEach + x == pages - 1) sm.ends = 1;
+        if ((w0 + tid * kPagesEach + x) * S + rank == pages - 1) sm.ends = 1;
       }
     __syncthreads();
     const int last = listed - 1;  // in whose page the cache may end
-    const int last_live = w1 == pages && sm.ends != 0 ? L - (pages - 1) * P : P;
+    const int last_live = sm.ends != 0 ? L - (pages - 1) * P : P;
     // Group i (8 keys of one page): the page's place in the list, and its first key there.
     const uint32_t groups = listed * groups_per_page;
     auto page_of = [&](uint32_t i) { return groups_per_page == 1 ? i : __umulhi(i, sp.by_page); };
@@ -942,9 +943,9 @@ extern "C" kvshot_status kvshot_draft_attn_sparse(const kvshot_attn_desc* d, con
   p.qscale = score_scale(d) * 1.4426950408889634f;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   // Pages are shared between nodes from 32 rows on, and where that leaves the SMs enough to do (us with a CTA for each node
-  // against shared; 16 caches of 20K to 32K tokens and 128 pages a node, 48 rows: 162, 98; 8 rows: 43, 58; 256 rows and 64
-  // pages: 403, 223; 64 caches of up to 8K and 32 pages, 16 rows: 79, 84; 16 caches of 4K and 32 pages, 48 rows: 59, 45; one of
-  // 8K and 64 pages, 256 rows: 33, 36).  Two CTAs of a cluster fill the SMs' two places (one: 131, and four: 122 for the 98).
+  // against shared; 16 caches of 20K to 32K tokens and 128 pages a node, 48 rows: 162, 97; 8 rows: 43, 58; 256 rows and 64
+  // pages: 403, 226; 64 caches of up to 8K and 32 pages, 16 rows: 79, 84; 16 caches of 4K and 32 pages, 48 rows: 59, 44; one of
+  // 8K and 64 pages, 256 rows: 33, 36).  Two CTAs of a cluster fill the SMs' two places (one: 131, and four: 122 for the 97).
   const int each = kColumns / p.G;
   const int64_t rows = static_cast<int64_t>(p.Nq) * p.G, blocks = (p.Nq + each - 1) / each, shared = blocks * d->num_caches * d->hkv;
   if (rows >= 32 && 3 * shared >= 2 * sm_count() && blocks < 65536) {
