@@ -453,15 +453,16 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
   // The nodes' counts, and of a tree the lines of ancestors as columns of the draft slots.
   const unsigned long long node_columns = (1ull << p.G) - 1;  // of node 0
   const unsigned long long all_columns = rows < 64 ? (1ull << rows) - 1 : ~0ull;
-  if (tid < kColumns) sm.neg_ref[tid] = INFINITY;  // (no reference yet)
+  if (tid >= rows && tid < kColumns) sm.neg_ref[tid] = INFINITY;  // (no row, and no key that it sees)
   // q as the B operand: rows of 64 dims, 128-byte swizzled, the first half of the dims of all rows, then the second.
   int count = tid < nodes ? __ldg(p.counts + (static_cast<size_t>(c) * p.Nq + n0 + tid) * p.v.hkv + h) : 0;
-  uint4 qx[kQEach];
+  // A row's first reference is its score for the node itself, which every row sees: a sum then cannot vanish.
+  uint4 qx[kQEach], self[kQEach];
 #pragma unroll
   for (int x = 0; x < kQEach; ++x) {
-    const int i = tid + x * kSharedThreads, r = i / 16, node = r / p.G;
-    qx[x] = r < rows ? __ldg(p.q + ((static_cast<size_t>(c) * p.Nq + n0 + node) * p.hq + h * p.G + (r - node * p.G)) * 16 + i % 16)
-                     : make_uint4(0, 0, 0, 0);
+    const int i = tid + x * kSharedThreads, r = min(i / 16, rows - 1), node = r / p.G;
+    qx[x] = __ldg(p.q + ((static_cast<size_t>(c) * p.Nq + n0 + node) * p.hq + h * p.G + (r - node * p.G)) * 16 + i % 16);
+    self[x] = __ldg(p.dk + (static_cast<size_t>(c * p.v.hkv + h) * p.n_max + p.N - p.Nq + n0 + node) * 16 + i % 16);
   }
   if (tid < nodes) {
     if (count < 0 || count > p.max_picks) {
@@ -473,6 +474,17 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
 #pragma unroll
   for (int x = 0; x < kQEach; ++x) {
     const int i = tid + x * kSharedThreads, r = i / 16, piece = i % 16;
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t a = word(qx[x], e), b = word(self[x], e);
+      s = fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), s);
+      s = fmaf(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u), s);
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (piece == 0 && r < rows) sm.neg_ref[r] = -s * p.qscale;
+    if (r >= rows) qx[x] = make_uint4(0, 0, 0, 0);
     if (r < sp.cols) *reinterpret_cast<uint4*>(sm.q + (piece >> 3) * (sp.cols * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = qx[x];
   }
   fence_proxy_async_smem();
@@ -589,11 +601,11 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
             x[i + 3] = __float_as_uint(y3);
           }
         };
-        // References move only when a score is more than 2^8 above its column's (or the column has none): P stays in range.
+        // References move only when a score is more than 2^32 above its column's: P and the sums stay in range.
         bool moved = false;
         for (;;) {
           refer();
-          if (moved || !any_softmax(barrier, !ok || top > 8.f)) break;
+          if (moved || !any_softmax(barrier, !ok || top > 32.f)) break;
           if (any_softmax(barrier, !ok)) {
             ok = false;
             break;
