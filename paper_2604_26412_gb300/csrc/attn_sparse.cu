@@ -332,9 +332,10 @@ cudaError_t launch_sparse(const SparseParams& p, int units, int S, cudaStream_t 
 //   warp 8      TMA;  warp 9: MMA, and the owner of tensor memory
 // Two CTAs to an SM, each with one K and one V tile: while one waits for its bytes the other multiplies.
 // The tree's level of 16 x 32K tokens (12 nodes, 128 pages each, 3 to 4 nodes to a page) reads 400 MB so, and not 1.6 GB:
-// 97 us, 162 with a CTA for each node, 110 with mma.sync and eight rows to a warp (five times the instructions).  Of the 97 the
-// list of pages takes 8, the first tile's references 4, the tiles 60 (at 6.5 TB/s), the wait for the cluster's slower CTA and
-// the join 10.  Four softmax warps of 64 columns each in turn were 112, a join by single floats 15 us longer.
+// 95 us, 162 with a CTA for each node, 110 with mma.sync and eight rows to a warp (five times the instructions).  Of the 95 the
+// list of pages takes 8, the tiles 50 to 75 (6.5 TB/s in all; the 104 of 152 SMs that have two of the 256 CTAs are the slower
+// ones), the wait for the cluster's other CTA and the join 5.  Four softmax warps of 64 columns each in turn were 112, a join
+// by single floats 15 us longer, references that start at the first tile's greatest scores 1.5 us.
 constexpr int kTileKeys128 = 128;
 constexpr int kTileBytes128 = kTileKeys128 * kHeadDim * 2;  // of K, and of V
 constexpr int kColumns = 64;
@@ -955,9 +956,9 @@ extern "C" kvshot_status kvshot_draft_attn_sparse(const kvshot_attn_desc* d, con
   p.qscale = score_scale(d) * 1.4426950408889634f;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   // Pages are shared between nodes from 32 rows on, and where that leaves the SMs enough to do (us with a CTA for each node
-  // against shared; 16 caches of 20K to 32K tokens and 128 pages a node, 48 rows: 162, 97; 8 rows: 43, 58; 256 rows and 64
-  // pages: 403, 226; 64 caches of up to 8K and 32 pages, 16 rows: 79, 84; 16 caches of 4K and 32 pages, 48 rows: 59, 44; one of
-  // 8K and 64 pages, 256 rows: 33, 36).  Two CTAs of a cluster fill the SMs' two places (one: 131, and four: 122 for the 97).
+  // against shared; 16 caches of 20K to 32K tokens and 128 pages a node, 48 rows: 162, 95; 8 rows: 43, 58; 256 rows and 64
+  // pages: 403, 224; 64 caches of up to 8K and 32 pages, 16 rows: 79, 84; 16 caches of 4K and 32 pages, 48 rows: 59, 43; one of
+  // 8K and 64 pages, 256 rows: 33, 36).  Two CTAs of a cluster fill the SMs' two places (one: 131, and four: 122 for the 95).
   const int each = kColumns / p.G;
   const int64_t rows = static_cast<int64_t>(p.Nq) * p.G, blocks = (p.Nq + each - 1) / each, shared = blocks * d->num_caches * d->hkv;
   if (rows >= 32 && 3 * shared >= 2 * sm_count() && blocks < 65536) {
