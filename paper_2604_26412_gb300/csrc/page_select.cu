@@ -289,7 +289,7 @@ struct ScoreCursor {
     while (tile == tiles(pages)) {
       tile = 0;
       fresh = true;
-      if (++hr < p.s.v.hkv * p.blocks) continue;
+      if (pages > 0 && ++hr < p.s.v.hkv * p.blocks) continue;
       hr = 0;
       pages = pages_of(p, ++c);
     }
