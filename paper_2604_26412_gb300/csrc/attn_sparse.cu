@@ -961,7 +961,9 @@ extern "C" kvshot_status kvshot_draft_attn_sparse(const kvshot_attn_desc* d, con
   // 8K and 64 pages, 256 rows: 33, 36).  Two CTAs of a cluster fill the SMs' two places (one: 131, and four: 122 for the 95).
   const int each = kColumns / p.G;
   const int64_t rows = static_cast<int64_t>(p.Nq) * p.G, blocks = (p.Nq + each - 1) / each, shared = blocks * d->num_caches * d->hkv;
-  if (rows >= 32 && 3 * shared >= 2 * sm_count() && blocks < 65536) {
+  // What a node picks has to be worth the list (12 nodes of 16 caches of 4K: 16 tokens 19, 21; 128 27, 27; 256 40, 34).
+  const int64_t picked = std::min<int64_t>(static_cast<int64_t>(max_picks) * d->page_size, p.v.len_bound);
+  if (rows >= 32 && picked >= 128 && 3 * shared >= 2 * sm_count() && blocks < 65536) {
     const uint32_t wait_ns = d->wait_limit_ns != 0 ? d->wait_limit_ns : static_cast<uint32_t>(kWaitLimitNs);
     const int S = shared < 2 * sm_count() ? 2 : 1;
     return launch_shared(p, d->num_caches, S, wait_ns, s) == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;

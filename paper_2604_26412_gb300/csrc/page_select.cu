@@ -960,7 +960,8 @@ extern "C" kvshot_status kvshot_page_scores(const kvshot_attn_desc* d, const voi
   // 29; 256: 141, 68.  64 caches of up to 8K: 32 rows 25, 32; 48: 30, 33; 64: 35, 35; 128: 64, 43.  4 of 32K: 48 rows 10.7,
   // 12.3; 64: 12.8, 12.6.  One of 32K: 64 rows 5.9, 7.6; 128: 9.1, 8.5.  One of 8K: 128 rows 7.1, 8.0; 256: 12, 8.1.
   const int64_t columns = static_cast<int64_t>(p.Nq) << log_gp;
-  if (columns >= 48 && columns * tiles >= (columns >= 128 ? 8 : 48) * 1024) {
+  // Tiles that no cache fills: 192 rows, 50 caches of 68 pages 17, 27; 256 rows, 64 of 128 pages 42, 35.
+  if (columns >= 48 && pages >= kStPages && columns * tiles >= (columns >= 128 ? 8 : 48) * 1024) {
     const uint32_t wait_ns = d->wait_limit_ns != 0 ? d->wait_limit_ns : static_cast<uint32_t>(kWaitLimitNs);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const cudaError_t e = log_gp == 0   ? launch_scores_tc<0>(p, tiles, wait_ns, st)

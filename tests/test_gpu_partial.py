@@ -98,10 +98,10 @@ def test_scores_of_a_call_of_many_pages_bound_every_key():
 MANY = {  # calls of 48 rows per KV head and more over many tiles of 128 pages
     "level": dict(lens=[0, 1, 8, 1016, 1023, 1024, 1025, 1032, 2049, 5003] * 4, page=8, nodes=12, query=12),
     "one head": dict(lens=[40] * 20 + [2100] * 40, page=16, hq=8, hkv=8, nodes=70, query=70),
-    "pairs": dict(lens=[0] * 40 + [77] * 80, page=64, hq=16, hkv=8, nodes=33, query=33),
+    "pairs": dict(lens=[0] * 40 + [1030] * 80, page=8, hq=16, hkv=8, nodes=33, query=33),
     "seven heads": dict(lens=list(range(0, 1600, 16)), page=8, hq=28, hkv=4, nodes=9, query=9),
-    "14 heads": dict(lens=[900] * 20, page=8, hq=112, hkv=8, nodes=8, query=8),
-    "17 heads": dict(lens=[17] * 200, page=32, hq=34, hkv=2, nodes=5, query=5),
+    "14 heads": dict(lens=[1030] * 20, page=8, hq=112, hkv=8, nodes=8, query=8),
+    "17 heads": dict(lens=[1100] * 40, page=8, hq=34, hkv=2, nodes=5, query=5),
     "one KV head": dict(lens=[1100] * 200, page=8, hq=32, hkv=1, nodes=4, query=4),
     "whole tree": dict(lens=[33000, 0, 200], page=8, nodes=64, query=64),
 }
@@ -320,29 +320,31 @@ def test_sparse_all_pages_agree_with_draft_attention():
     assert (full.float() - out.float()).abs().max() <= 0.03 and (z - lse).abs().max() <= 1e-3
 
 
-SHARED = {  # calls whose nodes share pages: from 32 rows per KV head, over two thirds of the SMs' number of (cache, head, 64 rows)
+# Calls whose nodes share pages: 32 rows per KV head and more that pick 128 tokens or more each, over two thirds of the SMs' number
+# of (cache, head, 64 rows).
+SHARED = {
     "tree": dict(lens=[0, 1, 15, 16, 17, 300, 700, 64, 65, 128, 500, 33, 8, 9], page=16, nodes=30, query=8, tree=True, layers=2),
     "chain": dict(lens=[0, 1, 7, 8, 9, 300, 700, 64, 65, 128, 500, 33, 31], page=8, nodes=20, query=16),
     "seven heads": dict(lens=list(range(0, 520, 20)), page=64, hq=28, hkv=4, nodes=6, query=5),
-    "one KV head": dict(lens=list(range(52)), page=32, hq=32, hkv=1, nodes=4, query=4),
+    "one KV head": dict(lens=list(range(51)) + [130], page=32, hq=32, hkv=1, nodes=4, query=4),
     "17 heads": dict(lens=list(range(0, 260, 10)), page=128, hq=34, hkv=2, nodes=3, query=3),
     "one head": dict(lens=list(range(0, 390, 30)), page=16, hq=8, hkv=8, nodes=64, query=64, tree=True),
     "whole tree": dict(lens=[200, 1000, 0, 191], page=192, nodes=64, query=64, tree=True),
     "long chain": dict(lens=list(range(0, 1300, 100)), page=256, nodes=100, query=12),
     "two windows": dict(lens=[20001, 9000] + [30] * 11, page=8, nodes=8, query=8),
-    "65 rows": dict(lens=[77] * 7, page=16, hq=8, hkv=8, nodes=65, query=65),
+    "65 rows": dict(lens=[177] * 7, page=16, hq=8, hkv=8, nodes=65, query=65),
 }
 
 
 @pytest.mark.parametrize("name", SHARED)
 def test_sparse_shared_pages(name):
     p = Problem(**SHARED[name], seed=len(name))
-    run_sparse(p, *p.random_picks(40 if name == "two windows" else 6, seed=len(name)))
+    run_sparse(p, *p.random_picks(40 if name == "two windows" else 16, seed=len(name)))
 
 
 def test_sparse_shared_pages_without_picks_and_bit_for_bit():
     p = Problem(**SHARED["tree"], seed=1)
-    picks, counts = p.random_picks(5)
+    picks, counts = p.random_picks(9)
     counts[:, ::2] = 0
     counts[3] = 0
     a, b = run_sparse(p, picks, counts), run_sparse(p, picks, counts)
@@ -352,7 +354,7 @@ def test_sparse_shared_pages_without_picks_and_bit_for_bit():
 @pytest.mark.parametrize("scale,std", [(1.0, 4.0), (0.05, 0.5), (3.0, 8.0)])
 def test_sparse_shared_scales(scale, std):
     p = Problem(**SHARED["chain"], scale=scale, std=std, seed=12)
-    run_sparse(p, *p.random_picks(9, seed=12))
+    run_sparse(p, *p.random_picks(16, seed=12))
 
 
 def test_sparse_shared_scores_that_rise_and_fall_along_the_cache():
@@ -368,21 +370,25 @@ def test_sparse_shared_scores_that_rise_and_fall_along_the_cache():
 
 
 def test_sparse_shared_bad_picks_pages_and_parents():
-    p = Problem([100] * 13, 16, nodes=8, query=8, tree=True)
-    picks = np.full((13, 8, 8, 6), -1, np.int32)
+    p = Problem([100] * 12 + [150], 16, nodes=8, query=8, tree=True)
+    picks = np.full((13, 8, 8, 8), -1, np.int32)
     picks[..., :3] = [1, 3, 6]
     n = np.full((13, 8, 8), 3, np.int32)
     for row in ([1, 3, 6, 7, 2 ** 31 - 1, -1], [-9, -2, 1, 3, 3, 6], [1, 3, 6, 6, 6, -2 ** 31]):
         bad, counts = picks.copy(), n.copy()
-        bad[4, 7, 2], counts[4, 7, 2] = row, 6
+        bad[4, 7, 2, :6], counts[4, 7, 2] = row, 6
         run_sparse(p, bad, counts, kvshot.KVSHOT_ERR_DEVICE_BOUNDS, (picks, n))
         p.err.zero_()
-    run_sparse(p, picks[..., :3].copy(), np.where(np.arange(13)[:, None, None] == 5, 2 ** 30, n), kvshot.KVSHOT_ERR_DEVICE_BOUNDS, (picks, n))
+    full, many = picks.copy(), n.copy()
+    full[5], many[5] = np.arange(8), 2 ** 30  # (of which 7 are pages)
+    want, seven = full.copy(), n.copy()
+    seven[5] = 7
+    run_sparse(p, full, many, kvshot.KVSHOT_ERR_DEVICE_BOUNDS, (want, seven))
     p.err.zero_()
     for parents, table, code in (([-1, 0, 5, 1, 2, 3, 4, 5], p.t_table, kvshot.KVSHOT_ERR_TREE),
                                  ([-1, 0, 1, 1, 2, 3, 4, 5], p.t_table - p.num_pages, kvshot.KVSHOT_ERR_DEVICE_BOUNDS)):
-        ws = p.workspace(6)
-        kvshot.draft_attn_sparse(p.desc, p.q, p.k, p.v, table, p.t_lens, p.ints(picks), p.ints(n), 6, p.dk, p.dv,
+        ws = p.workspace(8)
+        kvshot.draft_attn_sparse(p.desc, p.q, p.k, p.v, table, p.t_lens, p.ints(picks), p.ints(n), 8, p.dk, p.dv,
                                  p.ints([parents] * 13), torch.empty_like(p.q), torch.empty(p.q.shape[:3], device="cuda"))
         check(p, code)
         p.err.zero_()

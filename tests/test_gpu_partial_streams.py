@@ -102,14 +102,14 @@ def test_two_calls_at_once():
 
 def test_waits_that_run_out_are_reported_and_the_next_calls_are_right():
     p = Problem(**SHARED["tree"], seed=2)
-    picks, counts = p.random_picks(6)
+    picks, counts = p.random_picks(9)
     w = Problem([700, 300, 65], 16, nodes=24, query=24, seed=3)
     m = Problem(**MANY["level"], seed=4)
     bounds = torch.randn((m.num_pages, 8, 2, D), device="cuda").sort(dim=2).values.to(torch.bfloat16)
     for _ in range(2):  # (twice in a row: a call that gave up leaves nothing that blocks the next one)
         p.desc.wait_limit_ns = w.desc.wait_limit_ns = m.desc.wait_limit_ns = 1
-        ws = p.workspace(6)
-        kvshot.draft_attn_sparse(p.desc, p.q, p.k, p.v, p.t_table, p.t_lens, p.ints(picks), p.ints(counts), 6, p.dk, p.dv,
+        ws = p.workspace(9)
+        kvshot.draft_attn_sparse(p.desc, p.q, p.k, p.v, p.t_table, p.t_lens, p.ints(picks), p.ints(counts), 9, p.dk, p.dv,
                                  p.t_parent, torch.empty_like(p.q), torch.empty(p.q.shape[:3], device="cuda"))
         check(p, kvshot.KVSHOT_ERR_TIMEOUT)
         kvshot.key_weights(w.desc, w.q, w.k, w.t_table, w.t_lens, torch.from_numpy(some_lse(w)).cuda(), 0.0, 700, None,
