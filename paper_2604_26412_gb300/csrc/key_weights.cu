@@ -34,11 +34,11 @@ __device__ __forceinline__ float neg_log2_sum(float z) { return z == -INFINITY ?
 
 // ------------------------------------------------------------ few rows
 
-// Up to 8 rows per KV head, 16 in small calls.  A warp's keys are the M rows of mma.sync, the query rows its columns; operands go from global
-// memory straight to registers, the next keys' while the present ones' are multiplied.  A lane sums the exponentials of
+// Up to 8 rows per KV head, 64 in small calls.  A warp's keys are the M rows of mma.sync, the query rows its columns; operands go
+// from global memory straight to registers, the next keys' while the present ones' are multiplied.  A lane sums the exponentials of
 // its keys' columns over its heads; the heads are shared out over a cluster of CTAs where there are few keys, whose sums
 // meet in shared memory in rank order.
-constexpr int kDirectRows = 16;  // rows of a KV head, at most
+constexpr int kDirectRows = 64;  // rows of a KV head, at most
 constexpr int kDirectWarps = 4;
 constexpr int kDirectChunks = 2;  // of 16 keys, per warp
 constexpr int kDirectKeys = kDirectWarps * kDirectChunks * 16;
@@ -590,16 +590,21 @@ extern "C" kvshot_status kvshot_key_weights(const kvshot_attn_desc* d, const voi
   const int most = std::min(p.v.len_bound, weights_len), rows = p.G * p.Nq;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e;
-  // 9 to 16 rows: two n-tiles of registers a key cost the direct kernel its occupancy (16 x 32K tokens, 16 rows: 221 us, here
-  // 168), which does not matter before the SMs have a tile each (8K tokens: 14.5 us, here 18.6).
+  // 9 to 64 rows: two to eight n-tiles of registers a key cost the direct kernel its occupancy, which does not matter before the
+  // SMs have tiles enough (us in a graph, direct against tcgen05; 16 rows over 8K tokens 11, 16, over 16 x 32K 221, 168; 32 rows
+  // over 4K 7.0, 16.2, over 8K 13.1, 16.6, over 16K 18.5, 17.0; 64 rows over 4K 10.3, 17.9, over 8K 19.6, 17.3).
   const int64_t tc_tiles = static_cast<int64_t>((most + kTcKeys - 1) / kTcKeys) * p.v.C;
-  if (rows > kDirectRows || (rows > 8 && tc_tiles > sm_count())) {
+  const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 32 ? 4 : 8;
+  if (rows > kDirectRows || (nt > 1 && nt / 2 * tc_tiles > sm_count())) {
     e = launch_tc(p, q, target_k, tc_tiles, s);
   } else {
     const int tiles = std::max(1, (most + kDirectKeys - 1) / kDirectKeys);  // (lengths are looked at even without room)
     int S = 1;  // CTAs that share the heads: until the SMs have two each
     while (S < 8 && 2 * S <= p.v.hkv && static_cast<int64_t>(tiles) * p.v.C * S < 2 * sm_count()) S *= 2;
-    e = rows <= 8 ? launch_direct<1>(p, tiles, S, s) : launch_direct<2>(p, tiles, S, s);
+    e = nt == 1   ? launch_direct<1>(p, tiles, S, s)
+        : nt == 2 ? launch_direct<2>(p, tiles, S, s)
+        : nt == 4 ? launch_direct<4>(p, tiles, S, s)
+                  : launch_direct<8>(p, tiles, S, s);
   }
   return e == cudaSuccess ? KVSHOT_OK : KVSHOT_ERR_CUDA;
 }

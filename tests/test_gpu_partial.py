@@ -483,6 +483,12 @@ def test_weights_of_a_contiguous_cache(query):
     run_weights(Problem([777, 5, 0, 128], 16, nodes=query, query=query, contiguous=True, seed=query), 0.5)
 
 
+@pytest.mark.parametrize("page", [8, 64, 192])
+@pytest.mark.parametrize("query", [3, 6, 11, 16])
+def test_weights_of_many_caches(page, query):
+    run_weights(Problem([0, 1, 127, 128, 129, 300] * 30, page, hq=8, hkv=2, nodes=query, query=query, seed=query), 0.5)
+
+
 @pytest.mark.parametrize("query", [1, 64])
 def test_weights_of_a_long_cache(query):
     run_weights(Problem([3001], 64, nodes=query, query=query, seed=1, hq=8, hkv=2), 0.5)
