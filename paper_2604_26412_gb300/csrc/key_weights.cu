@@ -153,7 +153,7 @@ static_assert(kDirectWarps * 32 == kDirectKeys, "a thread per key");
 //                     units' room in tensor memory.  Its keys' sums stay with their threads until the piece's end.
 //   warp 8            TMA, and the rows' lse;  warp 9: MMA, and the owner of tensor memory
 // Up to 128 rows the call reads K at the copy's rate (16 x 32K tokens 166 to 170 us, floor 160).  With 256 rows (20K to 32K
-// tokens each) it takes 192 us, 1.2 PFLOP/s: the bytes and the hand-overs alone take 149, with the products 182, with the
+// tokens each) it takes 190 us, 1.2 PFLOP/s: the bytes and the hand-overs alone take 149, with the products 182, with the
 // exponentials 175.  No faster: both units of a tile as one product (198), five tiles in the ring with one place for q (197),
 // four warpgroups of a unit each (192).  Operands not in uniform registers cost 26 us, rooms given back after their sums 11.
 constexpr int kTcGroups = 2;  // warpgroups
@@ -295,6 +295,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     prefetch_tensormap(&maps.k);
     prefetch_tensormap(&maps.q);
   }
+  TcCursor cu;  // (the lengths are on their way beside the rest of the start)
+  cu.init(p);
   if (warp == kTcMmaWarp) {
     tc::tmem_alloc(smem_addr(&bar.tmem), kTcTmemCols);
     tc::tmem_relinquish();
@@ -305,8 +307,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const uint32_t tmem = bar.tmem;
   const uint64_t limit = p.w.wait_ns;
   int32_t* err = p.w.v.err;
-  TcCursor cu;
-  cu.init(p);
   TcPiece pc;
   const int passes = hkv * p.blocks;
 

@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p,
 // lane, half a page (lo, hi) to a stage, all but two of the stages on their way.  The next head's q is loaded meanwhile.
 //   warps 0..3 scores;  4..7 copies, and q's two halves;  8 MMA, and the owner of tensor memory
 // 12 nodes of 4 q heads over 16 caches of 20K to 32K tokens: 28.8 us (mma.sync 36.5).  Once begun, a CTA takes a tile in 1.5 us
-// (6.5 TB/s with the scores that are written); its start, q and the first tile take 8.
+// (6.5 TB/s with the scores that are written); its start, q and the first tile take 7.
 constexpr int kStPages = 128;
 constexpr int kStCols = 128;
 constexpr int kStStageBytes = kStPages * 256, kStChunkBytes = kStPages * 128;
@@ -343,6 +343,8 @@ __global__ void __launch_bounds__(kStThreads, 1) scores_tc_kernel(ScoreTcParams 
     mbar_init(smem_addr(&bar.done), 1);
     fence_mbar_init();
   }
+  ScoreCursor cu;  // (the lengths are on their way beside the rest of the start)
+  cu.init(p);
   if (warp == 8) {
     tc::tmem_alloc(smem_addr(&bar.tmem), kStRooms * kStCols);
     tc::tmem_relinquish();
@@ -351,8 +353,6 @@ __global__ void __launch_bounds__(kStThreads, 1) scores_tc_kernel(ScoreTcParams 
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = bar.tmem;
-  ScoreCursor cu;
-  cu.init(p);
   ScoreUnit u;
   bool ok = true;
 
