@@ -520,7 +520,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
   bool ok = true;
   // `tiles` tiles through the two products.  load(tile, kdst, vdst, kbar or vbar, which) issues a tile's copies (the whole loading
   // warp, which announces their bytes first); columns(tile, key, half, &live) which of the half's
-  // columns see this key, and whether it is a token.
+  // columns see this key, and whether it is a token that any column of either half sees.
   auto stream = [&](int tiles, auto load, auto columns) {
     if (warp == 8) {
       for (int t = 0; ok && t < tiles; ++t, ++done) {
@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
         ok = wait(smem_addr(&sm.sdone), done & 1, err, limit);
         if (done > 0) ok = ok && wait(smem_addr(&sm.pvdone), (done - 1) & 1, err, limit);  // (P's place is free, O at rest)
         if (!live && ok && half == 0) {
-          // V of what is no token may hold anything, and a NaN times P's 0 is one: zeros.
+          // V of what no column sees may hold anything, and a NaN times P's 0 is one: zeros.
           ok = wait(smem_addr(&sm.vfull), done & 1, err, limit);
           uint4* row = reinterpret_cast<uint4*>(sm.v + (key >> 3) * kGroupBytes + (key & 7) * 128);
 #pragma unroll
@@ -769,10 +769,10 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
            },
            [&](int t, int key, int half, bool* live) {
              const int slot = t * kTileKeys128 + key;
-             *live = slot < slots;
              // A chain's node sees the slots up to its own: nodes from slot - first_node on see this one.
              const unsigned long long see =
-                 !*live ? 0ull : tree ? sm.line[slot] : all_columns & ~0ull << (max(0, slot - first_node) * p.G);
+                 slot >= slots ? 0ull : tree ? sm.line[slot] : all_columns & ~0ull << (max(0, slot - first_node) * p.G);
+             *live = see != 0;  // (a tree's branch without any of these nodes may hold anything)
              return static_cast<uint32_t>(see >> (32 * half));
            });
   }
