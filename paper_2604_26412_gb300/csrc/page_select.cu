@@ -552,7 +552,8 @@ cudaError_t launch_scores_tc(const ScoreParams& s, int64_t most_tiles, uint32_t 
   static_assert(kStSmem - 2 * 4 * kStCols * 128 - sizeof(ScoreTcBarriers) >= kStMinStages * kStStageBytes, "room for the stages");
   p.stages = std::min(kStMaxStages, rest / kStStageBytes);
   const size_t smem = p.stages * kStStageBytes + 2 * 4 * p.cols * 128 + sizeof(ScoreTcBarriers);
-  cudaError_t e = cudaFuncSetAttribute(scores_tc_kernel<kLogGp>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  // (The limit is the process's, and the same in every call: another thread's call of another size must not lower it.)
+  cudaError_t e = cudaFuncSetAttribute(scores_tc_kernel<kLogGp>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStSmem);
   if (e != cudaSuccess) return e;
   const int grid = static_cast<int>(std::min<int64_t>(sm_count(), most_tiles * p.blocks));
   return launch_maybe_pdl(scores_tc_kernel<kLogGp>, dim3(grid), dim3(kStThreads), smem, false, stream, p);
