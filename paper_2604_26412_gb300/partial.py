@@ -25,6 +25,13 @@ def _paged(inp) -> None:
         raise ValueError("a paged target cache is needed")
 
 
+def _reported(err) -> int:
+    code = int(err.item())
+    if code:
+        err.zero_()
+    return code
+
+
 def _check_select(**sizes) -> kvshot.SelectDesc:
     """A descriptor whose sizes the call does not refuse (without pointers it checks them and does nothing)."""
     desc = kvshot.make_select_desc(**sizes)
@@ -63,6 +70,11 @@ class PageSelection:
         return _check_select(num_rows=s.num_caches * n_query * s.hkv, row_len=pages, rows_per_len=n_query * s.hkv,
                              tokens_per_entry=s.page_size, keep=self.keep, first=self.first, last=self.last,
                              err_flag=self.err)
+
+    def error_code(self) -> int:
+        """The first error that the bounds' and the selection's calls have recorded since the last time this was asked (0:
+        none)."""
+        return _reported(self.err)
 
 
 class TokenWeights:
@@ -107,7 +119,4 @@ class TokenWeights:
 
     def error_code(self) -> int:
         """The first error that the calls have recorded since the last time this was asked (0: none)."""
-        code = int(self.err.item())
-        if code:
-            self.err.zero_()
-        return code
+        return _reported(self.err)

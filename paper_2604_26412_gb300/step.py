@@ -183,4 +183,7 @@ class DraftStep:
             n0 += n_step
 
     def error_code(self) -> int:
-        return int(self.err.item()) if self.err is not None else 0
+        """An error that the step's calls have recorded, or else its selection's (PageSelection.error_code ends that one); 0:
+        none."""
+        code = int(self.err.item()) if self.err is not None else 0
+        return code or (int(self.pages.err.item()) if self.pages is not None else 0)
