@@ -472,7 +472,9 @@ kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* desc, const void* q,
  * bounds[pid, h, 0, d] = min, bounds[pid, h, 1, d] = max over the tokens of the page below the cache's length, of key
  * element d of KV head h (NaN if one of them is): [num_pages, hkv, 2, 128] bf16, by pool page, so that bounds stay with
  * their page.  Computed for the pages that hold a token at or past from_tokens[c] (a length before the cache grew; NULL:
- * all pages); other entries are left as they are.
+ * all pages); other entries are left as they are.  Whatever else writes keys below a length, kvshot_cache_evict in place
+ * among it, leaves bounds behind that are not of these keys: compute them anew with NULL.  A page that several caches
+ * share has to hold the same number of tokens below each one's length.
  */
 kvshot_status kvshot_page_bounds(const kvshot_attn_desc* desc, const void* target_k, const int32_t* page_table,
                                  const int32_t* seq_lens, const int32_t* from_tokens, void* bounds,
@@ -549,7 +551,8 @@ kvshot_status kvshot_key_weights(const kvshot_attn_desc* desc, const void* q, co
  * and V and in the weights.
  *   k, v -> k_out, v_out    [num_pages, hkv, page_size, 128] bf16, in place (k_out = k, v_out = v, page_table_out =
  *                           page_table), or into other pools of num_pages_out pages through page_table_out, a smaller
- *                           copy for instance.  Slots past the last kept token are left as they are.
+ *                           copy for instance.  Slots past the last kept token are left as they are.  Bounds of the
+ *                           pages (kvshot_page_bounds) do not follow: compute them anew for all pages.
  *   weights -> weights_out  [C, weights_len] -> [C, weights_len_out] fp32, 0 past the kept tokens' (what a token that comes
  *                           later starts with); in place, or not overlapping; both may be NULL
  *   seq_lens_out            m_c

@@ -1,18 +1,19 @@
 """Drafting over a part of a long target cache: which pages a draft token reads, and which tokens a cache keeps.
 
-PageSelection holds the bounds of the pages' keys (kvshot_page_bounds).  DraftStep(pages=...) scores every page for every
-draft token and KV head (kvshot_page_scores), picks the best (kvshot_select_top) and attends to those and the draft K/V
-(kvshot_draft_attn_sparse).
+PageSelection holds the bounds of the pages' keys (kvshot_page_bounds); update() brings them up to date after the cache
+grew.  DraftStep(pages=...) scores every page for every draft token and KV head (kvshot_page_scores), picks the best
+(kvshot_select_top) and attends to those and the draft K/V (kvshot_draft_attn_sparse).
 
 TokenWeights adds up the softmax weight that each cached token gets (kvshot_key_weights); DraftStep(weights=...) adds to it
 at every level.  evict() keeps the tokens with the most (kvshot_select_top), moves them to the front of their cache and gives
-the other pages back (kvshot_cache_evict).
+the other pages back (kvshot_cache_evict); the bounds of every PageSelection of that cache follow.
 
 Both are of a paged bf16 cache, as workloads.Inputs holds one.  All of it is enqueued on the device in stream order, with
 sizes known beforehand, and can be captured in a graph together with the step.
 """
 from __future__ import annotations
 
+import weakref
 from typing import Optional
 
 import torch
@@ -23,6 +24,11 @@ from . import kvshot
 def _paged(inp) -> None:
     if inp.page_table is None:
         raise ValueError("a paged target cache is needed")
+
+
+def _selections(inp) -> weakref.WeakSet:
+    """The PageSelections of inp's pages, whose bounds have to follow when its keys move."""
+    return vars(inp).setdefault("selections", weakref.WeakSet())
 
 
 def _reported(err) -> int:
@@ -55,6 +61,7 @@ class PageSelection:
         self.select_desc(1)
         self.bounds = torch.empty((inp.num_pages, s.hkv, 2, s.head_dim), dtype=torch.bfloat16, device=inp.target_k.device)
         self.update()
+        _selections(inp).add(self)
 
     def update(self, from_tokens: Optional[torch.Tensor] = None, stream=None) -> None:
         """Bounds of the pages that hold tokens at or past from_tokens (int32 [num_caches], lengths before the cache grew;
@@ -90,6 +97,7 @@ class TokenWeights:
         self.free_pages = torch.full((inp.num_pages,), -1, dtype=torch.int32, device=dev)
         self.free_count = torch.zeros(1, dtype=torch.int32, device=dev)
         self._kept = {}
+        self._captured = set()
 
     def add(self, desc: kvshot.AttnDesc, q, lse, stream=None) -> None:
         """The weights of a level's query rows: q and lse as the draft attention took and gave them."""
@@ -99,7 +107,9 @@ class TokenWeights:
 
     def evict(self, keep: int, first: int = 4, last: int = 64, stream=None) -> None:
         """Keep `keep` tokens of each cache (all of a shorter one): the first `first`, the last `last`, and the others with the
-        most weight.  Changes the cache, its lengths and weights in place."""
+        most weight.  Changes the cache, its lengths and weights in place, then computes anew the bounds of the selections that
+        there are of inp's pages, whose keys are others now.  (Those that are made after an eviction was captured are not in its
+        graph: update() them behind it.)"""
         inp, s = self.inp, self.inp.spec
         sizes = (keep, first, last)
         if sizes not in self._kept:  # (buffers of a captured eviction stay as they are)
@@ -116,6 +126,13 @@ class TokenWeights:
         kvshot.cache_evict(evict, inp.target_k, inp.target_v, inp.page_table, inp.seq_lens, kept, counts, self.weights,
                            inp.target_k, inp.target_v, inp.page_table, inp.seq_lens, self.weights, self.free_pages,
                            self.free_count, self.free_count, stream)
+        selections = list(_selections(inp))
+        if selections:
+            with kvshot.torch_stream(stream):
+                if torch.cuda.is_current_stream_capturing():
+                    self._captured.update(selections)  # (the graph writes their bounds as long as it is replayed)
+            for pages in selections:
+                pages.update(stream=stream)
 
     def error_code(self) -> int:
         """The first error that the calls have recorded since the last time this was asked (0: none)."""
