@@ -923,10 +923,10 @@ extern "C" kvshot_status kvshot_page_bounds(const kvshot_attn_desc* d, const voi
     return KVSHOT_ERR_ALIGN;
   const CacheView v = cache_view(d, page_table, seq_lens);
   const int64_t units = static_cast<int64_t>((v.len_bound + v.P - 1) / v.P) * v.hkv;
-  if (units == 0) return KVSHOT_OK;
   // After growth most caches have a page or two to do, and CTAs without work are what costs.
   const int64_t most = std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * (from_tokens != nullptr ? 8 : 64) / v.C);
-  const int x = static_cast<int>(std::min<int64_t>(most, (units + kBoundsThreads / 32 - 1) / (kBoundsThreads / 32)));
+  // (One CTA at least: lengths are looked at even without room.)
+  const int x = static_cast<int>(std::clamp<int64_t>((units + kBoundsThreads / 32 - 1) / (kBoundsThreads / 32), 1, most));
   const cudaError_t e = launch_maybe_pdl(bounds_kernel, dim3(x, v.C), dim3(kBoundsThreads), 0, false,
                                          reinterpret_cast<cudaStream_t>(stream), v, static_cast<const uint4*>(target_k),
                                          from_tokens, static_cast<uint4*>(bounds));
@@ -955,7 +955,6 @@ extern "C" kvshot_status kvshot_page_scores(const kvshot_attn_desc* d, const voi
     return KVSHOT_ERR_UNSUPPORTED;
   p.scale = score_scale(d);
   const int pages = (p.v.len_bound + p.v.P - 1) / p.v.P, per_cta = kScoreWarps * 16;
-  if (pages == 0) return KVSHOT_OK;
   const int64_t tiles = static_cast<int64_t>((pages + kStPages - 1) / kStPages) * p.v.hkv * p.v.C;
   // Graph times (us, mma.sync against tcgen05) of 16 caches of 20K to 32K tokens: 16 rows 23, 25; 32: 28, 26; 48: 35, 27; 64: 41,
   // 29; 256: 141, 68.  64 caches of up to 8K: 32 rows 25, 32; 48: 30, 33; 64: 35, 35; 128: 64, 43.  4 of 32K: 48 rows 10.7,
@@ -976,7 +975,7 @@ extern "C" kvshot_status kvshot_page_scores(const kvshot_attn_desc* d, const voi
   const size_t smem = static_cast<size_t>(std::min(kScoreRows, ((p.Nq << log_gp) + 15) / 16 * 16)) * kScoreRowBytes;
   // Where there are more than twelve CTAs to an SM, each takes several chunks of pages, and q once.
   const int64_t heads = static_cast<int64_t>(p.v.hkv) * p.v.C;
-  const int chunks = (pages + per_cta - 1) / per_cta;
+  const int chunks = std::max(1, (pages + per_cta - 1) / per_cta);  // (lengths are looked at even without room)
   const int64_t each = std::max<int64_t>(1, (chunks * heads + 12 * sm_count() - 1) / (12 * sm_count()));
   const int x = static_cast<int>((chunks + each - 1) / each);
   auto* kernel = log_gp == 0   ? scores_kernel<0>
