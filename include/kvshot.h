@@ -461,8 +461,9 @@ kvshot_status kvshot_draft_attn_kv4(const kvshot_attn_desc* desc, const void* q,
  *   kvshot_cache_evict   the tokens to keep moved to the front, and the other pages given back
  * The first two, the fourth and the fifth take a kvshot_attn_desc and read of it num_caches, num_seqs, hq, hkv, head_dim,
  * page_size, max_pages_per_seq, num_pages, max_seq_len, n_nodes, n_query, n_max, scale, flags, err_flag and wait_limit_ns as
- * kvshot_draft_attn does (kvshot_page_bounds no query heads' or nodes' fields).  Caches are bf16 and paged
- * (kvshot_key_weights: or contiguous), q is [C, Nq, hq, 128] bf16, and the q heads of one KV head are at most 32.
+ * kvshot_draft_attn does (kvshot_page_bounds no query heads' or nodes' fields: they may be 0, and are checked if they are
+ * not).  Caches are bf16 and paged (kvshot_key_weights: or contiguous), q is [C, Nq, hq, 128] bf16, and the q heads of one
+ * KV head are at most 32.
  * KVSHOT_TARGET_FP8 and the KVSHOT_FORCE_ flags return KVSHOT_ERR_UNSUPPORTED; KVSHOT_OVERLAP_PREVIOUS has no effect.
  * A length outside [0, min(max_seq_len, capacity)] is recorded as KVSHOT_ERR_DEVICE_BOUNDS and clamped to it, a page id
  * outside the pool recorded and its page passed over.  16-byte alignment of all bf16 pointers, 4 of int32 and fp32.

@@ -916,6 +916,12 @@ using namespace kvshot;
 extern "C" kvshot_status kvshot_page_bounds(const kvshot_attn_desc* d, const void* target_k, const int32_t* page_table,
                                             const int32_t* seq_lens, const int32_t* from_tokens, void* bounds,
                                             kvshot_stream_t stream) {
+  kvshot_attn_desc heads;
+  if (d != nullptr && d->hq == 0) {  // no query heads are read: a descriptor without them is as good
+    heads = *d;
+    heads.hq = heads.hkv;
+    d = &heads;
+  }
   if (kvshot_status st = check_partial(d, true)) return st;
   if (!target_k || !page_table || !seq_lens || !bounds) return KVSHOT_ERR_NULL;
   if (!aligned(target_k, 16) || !aligned(bounds, 16) || !aligned(page_table, 4) || !aligned(seq_lens, 4) ||

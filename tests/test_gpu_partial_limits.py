@@ -31,3 +31,14 @@ def test_lengths_without_room_are_looked_at(lens, code):
         p.err.zero_()
     del ws
     assert all(bool((x == 7).all()) for x in (bounds, scores, w))
+
+
+@pytest.mark.parametrize("hq", [0, 8])
+def test_bounds_need_no_query_heads(hq):
+    p = Problem([20, 300], 16, hq=8, hkv=8)
+    want, got = (torch.full((p.num_pages, 8, 2, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    kvshot.page_bounds(p.desc, p.k, p.t_table, p.t_lens, None, want)
+    p.desc.hq, p.desc.n_nodes, p.desc.n_query, p.desc.n_max, p.desc.scale = hq, 0, 0, 0, 0.0
+    kvshot.page_bounds(p.desc, p.k, p.t_table, p.t_lens, None, got)
+    torch.cuda.synchronize()
+    assert int(p.err.item()) == 0 and torch.equal(want, got)
