@@ -101,6 +101,7 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
 }
 
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();  // (.aligned: the whole warp at once, which a branch of one lane before it does not promise)
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Two floats from the shared memory of CTA `rank` of the cluster, at this CTA's address `addr`.
@@ -243,16 +244,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_commit(smem_addr(done));  // every MMA this thread issued has completed
   }
   __syncwarp();
-  if (!mbar_wait(smem_addr(done), 0, p.err, kPipeLimitNs)) *gave_up = 1;
+  if (!__all_sync(0xffffffffu, mbar_wait(smem_addr(done), 0, p.err, kPipeLimitNs))) *gave_up = 1;
   tc_fence_after();
   // A producer that gives up makes the MMA thread give up, which says so before its commit: after `done` every warp knows
   // whether all loads were consumed, and leaves the ring alone if not.
-  const bool failed = *gave_up;
+  const bool failed = __any_sync(0xffffffffu, *gave_up);
   if (failed && threadIdx.x == 0) {  // let the copies and MMAs in flight end before the CTA does
     for (int kt = max(0, issued - p.stages); kt < issued; ++kt)
       mbar_wait(smem_addr(&full[kt % p.stages]), (kt / p.stages) & 1, p.err);
     mbar_wait(smem_addr(done), 0, p.err);
   }
+  __syncwarp();
   // Partial sums to shared memory, [token][feature], over the ring (every load has been consumed).
   float* sums = reinterpret_cast<float*>(base);
   const int quarter = warp & 3;  // of the TMEM lanes (features); the two warpgroups take alternate chunks of tokens
