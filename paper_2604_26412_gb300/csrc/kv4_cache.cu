@@ -95,8 +95,14 @@ struct PlanShared {
   uint32_t sums[64];
   int ok[kExtendCluster];  // a CTA's answer to the pages it checked
 };
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() {
+  __syncwarp();  // (.aligned: the whole warp at once)
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ bool extend_plan(const ExtendParams& p, PlanShared& s, CachePlan* out) {
   cluster_arrive();
   const int c = threadIdx.x;

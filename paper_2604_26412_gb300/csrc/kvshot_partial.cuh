@@ -125,6 +125,7 @@ __device__ __forceinline__ uint32_t cluster_size() {
   return n;
 }
 __device__ __forceinline__ void cluster_sync_all() {
+  __syncwarp();  // (.aligned: the whole warp at once, which loops and branches of single lanes before it do not promise)
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ float remote_float(uint32_t addr, uint32_t rank) {

@@ -95,6 +95,7 @@ __device__ __forceinline__ void store_in_pair(uint32_t addr, int rank, int v) {
 }
 
 __device__ __forceinline__ void pair_sync() {
+  __syncwarp();  // (.aligned: the whole warp at once)
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // The address, in the cluster's shared memory, of `addr` in the pair's even CTA.

@@ -511,6 +511,7 @@ __global__ void __launch_bounds__(kStThreads, 1) scores_tc_kernel(ScoreTcParams 
 #pragma unroll
       for (int half = 0; half < kStCols / 64; ++half) {
         if (half * 64 >= p.cols) break;
+        __syncwarp();
         uint32_t v[2][32];
         tc::tmem_ld32(at + half * 64, v[0]);
         tc::tmem_ld32(at + half * 64 + 32, v[1]);  // (what is behind the columns is not used)
