@@ -109,7 +109,8 @@ struct WarpState {
       s[3] = ex2(s[3] - m1);
       l[nt][0] += s[0] + s[2];
       l[nt][1] += s[1] + s[3];
-      // (key, row pair) -> (row, key pair): the B operand of the second product.  bf16: the range of P's products with V.
+      // (key, row pair) -> (row, key pair): the B operand of the second product.  bf16, as the draft attention has it: V is bf16
+      // and a product's operands have one type.  A weight is off by 2^-8 of itself at most; the sums are of what it was before.
       p0[nt] = transpose8x8(pack_bf16x2(s[0], s[1]));
       p1[nt] = transpose8x8(pack_bf16x2(s[2], s[3]));
     }
@@ -645,7 +646,8 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
           }
         }
         if (!ok) break;
-        // P, rounded to bf16 as the second product takes it; the sums are of what it was before.
+        // P, rounded to bf16 (2^-8 of a weight at most) as the second product takes it beside a bf16 V; the sums are of what it
+        // was before.
         uint4* prow = reinterpret_cast<uint4*>(sm.p + key * 128);
 #pragma unroll
         for (int i = 0; i < 32; i += 8) {
@@ -893,6 +895,7 @@ cudaError_t launch_shared(const SparseParams& s, int caches, int S, uint32_t wai
   return cudaLaunchKernelEx(&cfg, sparse_shared_kernel, p, maps);
 }
 
+// The states meet in shared memory, and nothing is written here: the call asks for a workspace as the other attention calls do.
 constexpr size_t kSparseWorkspace = 256;
 
 kvshot_status check_sparse(const kvshot_attn_desc* d, int max_picks) {

@@ -58,8 +58,10 @@ __device__ __forceinline__ int checked_page(const EvictParams& p, const int32_t*
 // place chunks go in ascending order: a token's new place is never behind its old one and both ascend, so a chunk's stores
 // never reach what a later chunk loads, and one barrier between a chunk's loads and its stores is enough.  There a CTA takes
 // all chunks, and where that leaves SMs idle only 4 or 8 of the 16 pieces, which are independent of one another.
-// Bound by HBM: 4096 of 32K tokens of 16 caches 89 us (6.1 TB/s; 97 with a head's K or V to a CTA, 189 with places looked up
-// by each row's loads); 512 of up to 8K tokens of 64 caches 54 us, where most CTAs end after one chunk.
+// Bound by HBM: 4096 of 32K tokens of 16 caches into another pool 88 us (6.1 TB/s; 97 with a head's K or V to a CTA, 189 with
+// places looked up by each row's loads); 512 of up to 8K tokens of 64 caches 54 us, where most CTAs end after one chunk.  In
+// place, in a graph: the same 98 and 52 us; 4096 of 32K tokens of one cache 27 us (1.3 TB/s), 2048 of 8K 13 us, where each of the
+// 64 CTAs goes through its chunks one after the other, one chunk's loads on their way.
 constexpr int kMoveThreads = 256;
 constexpr int kMoveLoads = 8;  // rows of a thread and chunk
 constexpr int kHeadsEach = 4;  // heads' K or V that a CTA moves into another pool

@@ -153,8 +153,8 @@ static_assert(kDirectWarps * 32 == kDirectKeys, "a thread per key");
 //                     units' room in tensor memory.  Its keys' sums stay with their threads until the piece's end.
 //   warp 8            TMA, and the rows' lse;  warp 9: MMA, and the owner of tensor memory
 // Up to 128 rows the call reads K at the copy's rate (16 x 32K tokens 166 to 170 us, floor 160).  With 256 rows (20K to 32K
-// tokens each) it takes 190 us, 1.2 PFLOP/s: the bytes and the hand-overs alone take 149, with the products 182, with the
-// exponentials 175.  No faster: both units of a tile as one product (198), five tiles in the ring with one place for q (197),
+// tokens each) it takes 188 to 192 us in a graph, 1.2 PFLOP/s, and 190 to 209 by box as calls one after another: the bytes and
+// the hand-overs alone take 149, with the products 182, with the exponentials 175.  No faster: both units of a tile as one product (198), five tiles in the ring with one place for q (197),
 // four warpgroups of a unit each (192).  Operands not in uniform registers cost 26 us, rooms given back after their sums 11.
 constexpr int kTcGroups = 2;  // warpgroups
 constexpr int kTcLoadWarp = 4 * kTcGroups, kTcMmaWarp = kTcLoadWarp + 1;

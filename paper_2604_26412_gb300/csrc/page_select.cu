@@ -26,7 +26,8 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
 }
 
 // A warp takes one (page, KV head): P rows of 256 bytes, two to a load.  Bound by HBM: 16 caches of 32K tokens in 166 us, 6.6
-// TB/s.  After growth, by the launch and three dependent loads (length, table, keys): 64 caches of up to 8K tokens 6.3 us.
+// TB/s.  After growth, by the launch and three dependent loads (length, table, keys): 64 caches of up to 8K tokens 6.1 us (3.4 in
+// a graph).
 __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(CacheView v, const uint4* __restrict__ k,
                                                                const int32_t* __restrict__ from, uint4* bounds) {
   const int c = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -210,8 +211,9 @@ __global__ void __launch_bounds__(kScoreWarps * 32) scores_kernel(ScoreParams p,
 // Many rows over many pages: tcgen05.  128 pages are the M rows of a product of 256 dims, and the query rows (up to 128 of
 // whole nodes) its N columns, so that a thread has a page's row of scores, finds each node's best in its own registers, and a
 // warp stores 32 consecutive pages.  One persistent CTA per SM takes an equal run of the caches' tiles, KV head after KV
-// head.  Pages are 512 bytes at any place of the pool, which a tensor map has no box for: four warps copy them 16 bytes a
-// lane, half a page (lo, hi) to a stage, all but two of the stages on their way.  The next head's q is loaded meanwhile.
+// head.  Pages are 512 bytes at any place of the pool: four warps copy them 16 bytes a lane, half a page (lo, hi) to a stage,
+// all but two of the stages on their way.  (A tensor map's gather, four rows to an instruction, was not tried.)  The next head's
+// q is loaded meanwhile.
 //   warps 0..3 scores;  4..7 copies, and q's two halves;  8 MMA, and the owner of tensor memory
 // 12 nodes of 4 q heads over 16 caches of 20K to 32K tokens: 28.8 us (mma.sync 36.5).  Once begun, a CTA takes a tile in 1.5 us
 // (6.5 TB/s with the scores that are written); its start, q and the first tile take 7.
@@ -646,9 +648,9 @@ __device__ __forceinline__ int remote_int(const int* at, uint32_t rank) {
 // CTA counts the digits of its own keys that are still in question and adds what it counted to the counts of all CTAs, which
 // then each find the digit for themselves.  What bounds it: the latencies of a load, two to four rounds of counts and a
 // scan, and, where there are many rows, the instructions of each key (keys that do not compete are 0, so that a key in
-// question is one subtraction and one comparison).  4096 of 32K entries in 16 rows: 11.6 us (89 with one CTA that reads the
-// scores for every digit; 13.5 with eight CTAs of 4096 entries to a row and not four of 8192).  1536 rows of 1250 to 2048
-// entries: 11.5 us; a warp to a row with its keys in registers, bit by bit, took 25.8, a set of keys in question kept as bits
+// question is one subtraction and one comparison).  In a graph, and as calls one after another where that is said: 4096 of 32K
+// entries in 16 rows 11.8 us, calls 14.3 (89 with one CTA that reads the scores for every digit; 13.5 with eight CTAs of 4096
+// entries to a row and not four of 8192).  1536 rows of 1250 to 2048 entries 11.7 us, calls 14.3; a warp to a row with its keys in registers, bit by bit, took 25.8, a set of keys in question kept as bits
 // 17.1, digits of 8 and 10 bits 12.5 and 11.8, 256 threads to a row 15.2.
 constexpr int kSelectKeys = 16;
 constexpr int kMaxSelectCluster = 8;
@@ -1009,7 +1011,7 @@ extern "C" kvshot_status kvshot_select_top(const kvshot_select_desc* d, const fl
   const SelectParams p{scores,          seq_lens,          picks,               counts,  d->err_flag, d->row_len,
                        d->rows_per_len, d->tokens_per_entry, d->keep, d->first, d->last};
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const int n = d->row_len, rows = d->num_rows;
+  const int n = d->row_len, rows = d->num_rows;  // (the longest that a row can be: lengths are known to the device alone)
   auto cluster = [&](int per_cta) {
     int S = 2;
     while (S < kMaxSelectCluster && S * per_cta < n) S *= 2;
