@@ -112,6 +112,16 @@ struct TensorMaps {
   CUtensorMap q;  // [C, Nq, hq, 128] as 4-D {128, hq, Nq, C}; used by the tensor-memory kernel
 };
 
+// Whether a tensor map was encoded.  The driver wants a context current to the calling thread, which a host thread has none of
+// before its first call that needs the device: then it gets the current device's.
+template <typename Encode>
+bool encoded(Encode encode) {
+  CUresult r = encode();
+  int device = 0;
+  if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess) r = encode();
+  return r == CUDA_SUCCESS;
+}
+
 // Encodes a 2-D tiled tensor map over a row-major bf16 matrix [rows, cols] (row pitch cols * 2
 // bytes), boxes of {box_cols, box_rows}, 128-byte swizzle.  False if the encoder is unavailable
 // or rejects the layout.
