@@ -335,16 +335,14 @@ __global__ void __launch_bounds__(kThreads, 2)
 
 cudaError_t attn_cc_occupancy(int C, int* ctas_per_sm) {
   const size_t smem = smem_bytes(C);
-  cudaError_t e = cudaFuncSetAttribute(attn_cc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+  cudaError_t e = cudaFuncSetAttribute(attn_cc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxCtaSmem);
   if (e != cudaSuccess) return e;
   return cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas_per_sm, attn_cc_kernel, kThreads, smem);
 }
 
 cudaError_t launch_attn_cc(const AttnParams& p, const TensorMaps& maps, bool pdl, cudaStream_t stream) {
   const size_t smem = smem_bytes(p.C);
-  cudaError_t e = cudaFuncSetAttribute(attn_cc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+  cudaError_t e = cudaFuncSetAttribute(attn_cc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxCtaSmem);
   if (e != cudaSuccess) return e;
   return launch_maybe_pdl(attn_cc_kernel, dim3(p.num_ctas), dim3(kThreads), smem, pdl, stream, p, maps);
 }

@@ -656,10 +656,9 @@ using Cfg48 = Cfg<2, 3, 2, 5, 1>;
 using Cfg64 = Cfg<2, 4, 2, 5, 1>;
 
 // Every plan that kMaxCaches allows fits an SM.
-constexpr size_t kMaxSmem = 227 * 1024;
-static_assert(smem_bytes<Cfg8>(kMaxCaches) <= kMaxSmem && smem_bytes<Cfg16>(kMaxCaches) <= kMaxSmem &&
-                  smem_bytes<Cfg32>(kMaxCaches) <= kMaxSmem && smem_bytes<Cfg48>(kMaxCaches) <= kMaxSmem &&
-                  smem_bytes<Cfg64>(kMaxCaches) <= kMaxSmem,
+static_assert(smem_bytes<Cfg8>(kMaxCaches) <= kMaxCtaSmem && smem_bytes<Cfg16>(kMaxCaches) <= kMaxCtaSmem &&
+                  smem_bytes<Cfg32>(kMaxCaches) <= kMaxCtaSmem && smem_bytes<Cfg48>(kMaxCaches) <= kMaxCtaSmem &&
+                  smem_bytes<Cfg64>(kMaxCaches) <= kMaxCtaSmem,
               "shared memory at the largest number of caches");
 
 // The plan takes 8 bytes of shared memory per cache: past this many, two CTAs of three stages no longer fit an SM.
@@ -671,7 +670,7 @@ template <class CF>
 cudaError_t launch_cfg(const AttnParams& p, const TensorMaps& maps, bool pdl, cudaStream_t stream) {
   const size_t smem = smem_bytes<CF>(p.C);
   auto* kernel = p.v_scale < 0x1p-4f || p.v_scale > 0x1p8f ? attn_f8_kernel<CF, true> : attn_f8_kernel<CF, false>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxCtaSmem);
   if (e != cudaSuccess) return e;
   return launch_maybe_pdl(kernel, dim3(p.num_ctas), dim3(CF::kThreads), smem, pdl, stream, p, maps);
 }
@@ -680,8 +679,7 @@ cudaError_t launch_cfg(const AttnParams& p, const TensorMaps& maps, bool pdl, cu
 template <class CF>
 cudaError_t occupancy_cfg(int C, int* ctas) {
   const size_t smem = smem_bytes<CF>(C);
-  cudaError_t e = cudaFuncSetAttribute(attn_f8_kernel<CF, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+  cudaError_t e = cudaFuncSetAttribute(attn_f8_kernel<CF, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxCtaSmem);
   if (e != cudaSuccess) return e;
   return cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas, attn_f8_kernel<CF, false>, CF::kThreads, smem);
 }

@@ -407,8 +407,7 @@ template <bool GR> using Cfg4 = Cfg<4, 2, 4, 1, GR>;
 template <class CF>
 cudaError_t launch_cfg(const AttnParams& p, const TensorMaps& maps, bool pdl, cudaStream_t stream) {
   const size_t smem = smem_bytes<CF>(p.C);
-  cudaError_t e = cudaFuncSetAttribute(attn_mma_kernel<CF>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+  cudaError_t e = cudaFuncSetAttribute(attn_mma_kernel<CF>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxCtaSmem);
   if (e != cudaSuccess) return e;
   return launch_maybe_pdl(attn_mma_kernel<CF>, dim3(p.num_ctas), dim3(CF::kThreads), smem, pdl, stream, p, maps);
 }
@@ -416,8 +415,7 @@ cudaError_t launch_cfg(const AttnParams& p, const TensorMaps& maps, bool pdl, cu
 template <class CF>
 cudaError_t occupancy_cfg(int C, int* ctas) {
   const size_t smem = smem_bytes<CF>(C);
-  cudaError_t e = cudaFuncSetAttribute(attn_mma_kernel<CF>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+  cudaError_t e = cudaFuncSetAttribute(attn_mma_kernel<CF>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxCtaSmem);
   if (e != cudaSuccess) return e;
   return cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas, attn_mma_kernel<CF>, CF::kThreads, smem);
 }

@@ -1708,8 +1708,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 cudaError_t attn_tc_occupancy(int C, int* ctas_per_sm) {
   const size_t smem = smem_bytes(C, false);
-  cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem));
+  cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxCtaSmem);
   if (e != cudaSuccess) return e;
   return cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas_per_sm, attn_tc_kernel<false, false>, kThreads, smem);
 }
@@ -1718,8 +1717,7 @@ cudaError_t launch_attn_tc(const AttnParams& p, const TensorMaps& maps, int nq_b
                            cudaStream_t stream) {
   if (pair) {
     const size_t smem = smem_bytes_pair(p.C);
-    cudaError_t e = cudaFuncSetAttribute(attn_tc_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         static_cast<int>(smem));
+    cudaError_t e = cudaFuncSetAttribute(attn_tc_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxCtaSmem);
     if (e != cudaSuccess) return e;
     return launch_maybe_pdl(attn_tc_pair_kernel, dim3(p.num_ctas), dim3(kPairThreads), smem, pdl, stream, p, maps,
                             nq_box);
@@ -1729,7 +1727,7 @@ cudaError_t launch_attn_tc(const AttnParams& p, const TensorMaps& maps, int nq_b
   auto* kernel = p.unit_ctas > 0 ? (f8 ? attn_tc_kernel<true, true, true> : attn_tc_kernel<true, false, true>)
                  : f8            ? (spread ? attn_tc_kernel<true, true> : attn_tc_kernel<false, true>)
                                  : (spread ? attn_tc_kernel<true, false> : attn_tc_kernel<false, false>);
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxCtaSmem);
   if (e != cudaSuccess) return e;
   return launch_maybe_pdl(kernel, dim3(p.num_ctas), dim3(kThreads), smem, pdl, stream, p, maps, nq_box);
 }

@@ -403,7 +403,7 @@ extern "C" kvshot_status kvshot_kv_project(const kvshot_project_desc* d, const v
       !encode_bf16_2d(&maps.a[1], v_in, K, T, kKT, static_cast<uint32_t>(p.box_tok)))
     return KVSHOT_ERR_CUDA;
   const size_t smem = smem_bytes(p.stages, p.box_tok);
-  if (cudaFuncSetAttribute(kv_project_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) !=
+  if (cudaFuncSetAttribute(kv_project_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxCtaSmem) !=
       cudaSuccess)
     return KVSHOT_ERR_CUDA;
   cudaLaunchAttribute attr[2];

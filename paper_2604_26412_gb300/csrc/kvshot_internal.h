@@ -29,6 +29,9 @@ constexpr int kKVTileBytes = 2 * kHalfBytes;          // one K (or V) tile
 constexpr int kStageBytes = 2 * kKVTileBytes;         // K + V
 constexpr int kF8PrefixTile = 128;                    // keys per prefix tile of the fp8 mma.sync kernel
 constexpr int kMaxCaches = 1024;
+// Shared memory of a CTA, at most: the limit that kernels whose needs differ from call to call are given, always the same one, since
+// it is the process's and another thread's call must not lower it between this one's setting and its launch.
+constexpr int kMaxCtaSmem = 227 * 1024;
 constexpr int kMaxTreeNodes = 64;
 constexpr int kDraftBoxRows = 8;                      // draft K/V are loaded 8 rows per TMA box
 constexpr int kCcRows = 4;                            // rows per unit of the CUDA-core kernel
