@@ -1,5 +1,6 @@
 // attn_sparse.cu -- draft attention over the pages picked for each query row and KV head, and the draft K/V.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "kvshot_partial.cuh"
@@ -485,7 +486,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2)
     }
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (piece == 0 && r < rows) sm.neg_ref[r] = -s * p.qscale;
+    if (piece == 0 && r < rows) sm.neg_ref[r] = fminf(-s * p.qscale, FLT_MAX);  // (finite: a score of -inf less itself is no number)
     if (r >= rows) qx[x] = make_uint4(0, 0, 0, 0);
     if (r < sp.cols) *reinterpret_cast<uint4*>(sm.q + (piece >> 3) * (sp.cols * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = qx[x];
   }

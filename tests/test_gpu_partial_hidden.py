@@ -10,7 +10,7 @@ import torch
 from oracle import partial
 from paper_2604_26412_gb300 import kvshot
 
-from .partial_problems import Problem
+from .partial_problems import Problem, f64
 from .test_gpu_partial import SHARED, run_sparse
 
 pytestmark = pytest.mark.gpu
@@ -68,3 +68,37 @@ def test_one_branch_of_a_level_does_not_reach_another(name):
     assert torch.equal(out[keep], want[0][keep]) and torch.equal(lse, want[1])
     assert bool(torch.isnan(out[c, -1, :g]).all())
     assert np.isfinite(lse.cpu().numpy()).all()
+
+
+@pytest.mark.parametrize("name", CASES)
+def test_keys_of_minus_infinity_weigh_nothing(name):
+    """Scores of -inf, of the nodes' own keys and of some of a page's, beside finite ones.  Bounds as in tests/test_gpu_partial.py, of
+    the finite keys: a weight of 0 is exact."""
+    p = Problem(**CASES[name], seed=19)
+    picks, counts = p.random_picks(16, seed=19)
+    p.q[..., 0] = p.q[..., 0].abs() + 1
+    own, k0 = slice(p.N - p.Nq, p.N), [int(x) for x in p.table[:, 0] if x >= 0]
+    p.dk[:, :, own, 0] = 0
+    p.k[k0, :, ::3, 0] = 0
+    mag = oracle(p, picks, counts)[3]
+    p.dk[:, :, own, 0] = float("-inf")
+    p.k[k0, :, ::3, 0] = float("-inf")
+    with np.errstate(invalid="ignore"):  # (rows of -inf alone have no softmax)
+        want, z, spread, _ = oracle(p, picks, counts)
+    ws = p.workspace(16)
+    out, lse = torch.empty_like(p.q), torch.empty(p.q.shape[:3], device="cuda")
+    kvshot.draft_attn_sparse(p.desc, p.q, p.k, p.v, p.t_table, p.t_lens, p.ints(picks), p.ints(counts), 16, p.dk, p.dv,
+                             p.t_parent, out, lse)
+    torch.cuda.synchronize()
+    assert int(p.err.item()) == 0
+    del ws
+    seen = np.isfinite(z)
+    assert seen.sum() > seen.size // 2
+    tol = 2.0 ** -16 * mag + 2.0 ** -18
+    assert np.all(np.abs(f64(lse) - z)[seen] <= tol[seen])
+    assert np.all((np.abs(f64(out) - want) <= (2.0 ** -7 + 2 * tol[..., None]) * spread)[seen])
+
+
+def oracle(p, picks, counts):
+    return partial.attn_sparse(f64(p.q), f64(p.k), f64(p.v), p.table, p.lens, picks, counts, f64(p.dk), f64(p.dv), p.parent,
+                               p.layers, p.N, p.scale)
