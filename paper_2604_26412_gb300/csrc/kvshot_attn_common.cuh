@@ -71,6 +71,9 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;
 // on every iteration (mbarrier.try_wait may suspend the thread for longer than
 // such a limit, so the timer would never be looked at in time).
 constexpr uint64_t kPollBelowNs = 100000;
+// Limits below this may be shorter than a step of the clock (32 ns to 2 us, by driver): the first look that finds the wait
+// unfinished gives up.
+constexpr uint64_t kNoWaitNs = 1000;
 
 // Non-blocking test of a phase's completion.
 __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
@@ -92,7 +95,7 @@ __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, int32
   if (limit_ns < kPollBelowNs) {
     for (;;) {
       if (mbar_test_wait(bar, parity)) return true;
-      if (global_timer_ns() - t0 > limit_ns) break;
+      if (limit_ns < kNoWaitNs || global_timer_ns() - t0 > limit_ns) break;
     }
   } else {
     for (;;) {

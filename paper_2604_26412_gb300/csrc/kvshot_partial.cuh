@@ -155,17 +155,11 @@ __device__ __forceinline__ void mma_piece(float (&d)[4], const uint4& a, const u
   dev::mma_bf16_16816(d, hi, b.z, b.w);
 }
 
-// A wait that looks a few times before it takes the time (reading the clock takes long enough to be late).  A limit below the
-// clock's step gives up on the first look that finds the wait unfinished.
-constexpr uint64_t kNoWaitNs = 1000;
+// A wait that looks a few times before it takes the time (reading the clock takes long enough to be late).
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int32_t* err, uint64_t limit) {
   if (limit >= dev::kPollBelowNs) {
     for (int i = 0; i < 32; ++i)
       if (dev::mbar_try_wait(bar, parity)) return true;
-  } else if (limit < kNoWaitNs) {
-    if (dev::mbar_test_wait(bar, parity)) return true;
-    dev::set_error(err, KVSHOT_ERR_TIMEOUT);
-    return false;
   }
   return dev::mbar_wait(bar, parity, err, limit);
 }
