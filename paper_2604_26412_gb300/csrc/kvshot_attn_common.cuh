@@ -71,7 +71,7 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;
 // on every iteration (mbarrier.try_wait may suspend the thread for longer than
 // such a limit, so the timer would never be looked at in time).
 constexpr uint64_t kPollBelowNs = 100000;
-// Limits below this may be shorter than a step of the clock (32 ns to 2 us, by driver): the first look that finds the wait
+// Limits below this may be shorter than a step of the clock (32 ns on some machines, 2 us on others): the first look that finds the wait
 // unfinished gives up.
 constexpr uint64_t kNoWaitNs = 1000;
 
